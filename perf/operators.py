@@ -20,7 +20,6 @@ own = False
 
 LLAMA_V = 128256
 QWEN_V = 151936
-TINY = float("-inf")
 
 
 # ---------------------------------------------------------------------- the cases
@@ -175,7 +174,7 @@ def prepare(case, seed):
         coin = torch.rand(R, generator=g, device="cuda")
         labels = torch.where(coin < 0.5, labels, other)
         if R > 1:
-            labels[coin > 0.95] = -1               # padding of the batch
+            labels[coin > 0.95] = -1               # padding of the batch: ignored rows, of which nothing is read
         s["labels"] = labels
         s["g"] = torch.full((R,), 1.0 / max(1, int((labels >= 0).sum())), device="cuda")
         s.update(loss=f32(R), lse=f32(R, 2))
@@ -292,7 +291,7 @@ def _plain_distill(s):
             loss = loss + alpha * tau * tau * (q * (logq - logp)).sum(dim=1)
         out.append(torch.where(live, loss, torch.zeros_like(loss)))
         if c["kind"] == "loss":
-            return out[0], torch.stack([lse_tau, lse_one], dim=1)
+            return out[0], torch.where(live[:, None], torch.stack([lse_tau, lse_one], dim=1), 0.0)
     d = (1.0 - alpha) * torch.exp(z - lse_one[:, None])
     d.scatter_add_(1, y, torch.full_like(y, alpha - 1.0, dtype=torch.float32))
     if q is not None:
@@ -313,13 +312,14 @@ def work(case):
         return {"bytes": logits + 4 * R * (named + 1 + 3), "flops": 3 * R * V}
     if case["kind"] == "top":
         return {"bytes": logits + 8 * R * case["K"], "flops": R * V}
+    read = logits if R == 1 else 0.95 * logits   # ignored rows need not be read
     exps = (0 < case["alpha"]) + (case["alpha"] < 1 and not (case["alpha"] > 0 and case["tau"] == 1))
     small = R * (8 * case["K"] + 4)
     if case["kind"] == "loss":
-        return {"bytes": logits + small + 12 * R, "flops": 3 * exps * R * V}
+        return {"bytes": read + small + 12 * R, "flops": 3 * exps * R * V}
     if case["kind"] == "grad":
-        return {"bytes": 2 * logits + small + 12 * R, "flops": 4 * exps * R * V}
-    return {"bytes": 2 * logits + small + 8 * R, "flops": 6 * exps * R * V}
+        return {"bytes": read + logits + small + 12 * R, "flops": 4 * exps * R * V}
+    return {"bytes": read + logits + small + 8 * R, "flops": 6 * exps * R * V}
 
 
 # ---------------------------------------------------------------------- 64 bits
@@ -398,7 +398,7 @@ def _exact_distill(s):
             lq = torch.log_softmax(t, 1)
             soft = tau * tau * (lq.exp() * (lq - (torch.gather(a, 1, i) / tau - lt[:, None]))).sum(1)
         losses.append(live * (alpha * soft + (1 - alpha) * hard))
-        lses.append(torch.stack([lt, l1], 1))
+        lses.append(torch.stack([lt, l1], 1) * live[:, None])
         if target is not None:
             target[rows, y.clamp(min=0)] += 1 - alpha
             d = (1 - alpha) * (a - l1[:, None]).exp()
