@@ -428,6 +428,123 @@ SATS_API sats_status sats_route_calibrate(const float *score, int V, const int32
                                           size_t ws_bytes, void *stream);
 
 /*
+ * Vocabulary operators: rows of logits, on either side of the token routing.
+ * The token ids that sats_route looks up are drawn from logits, and the losses
+ * that sats_token_scores takes are losses of logits; the paper leaves both to
+ * the model around the method.
+ *
+ * In all of them logits is a device array of rows of V elements (bf16, or fp32
+ * in the _f32 calls), row r starting at element r * ld (ld >= V; what lies
+ * between the rows is not read).  A pointer needs the alignment of its elements
+ * only; rows that start on 16-byte boundaries are no faster.  The calls need
+ * no workspace, their waits are the hardware's own, and what they write does
+ * not depend on the order in which their threads run.  V up to 2^31 - 65 and
+ * 2^28 - 1 rows (else SATS_ESHAPE); no rows: nothing is done.
+ *
+ * sats_top_logits -- the K largest logits of each row, as a teacher hands them
+ *   over: values (device fp32 [T][K]) in descending order, ties by the lower
+ *   index first, and their indices idx (device int32 [T][K]).  -inf and NaN
+ *   are never selected: a row with fewer other elements gets -inf and index -1
+ *   in the places left (an absent entry, for the calls below).  1 <= K <= V;
+ *   K up to 1024 (else SATS_ESHAPE).
+ *
+ * sats_distill_loss -- the loss of a row z against a teacher's top logits and
+ *   a label, with temperature tau and share alpha:
+ *     q = softmax over the row's entries of top_val / tau
+ *     KD = tau^2 sum_k q_k (log q_k - log softmax(z / tau)[top_idx_k])
+ *     CE = log sum_j exp(z_j) - z[label]
+ *     loss = alpha KD + (1 - alpha) CE
+ *   With alpha 0 (K may be 0 then) it is the next-token loss that
+ *   sats_token_scores takes for the base and the sparse path.
+ *   top_idx, top_val : device int32 and fp32 [T][K] (K 0 to 1024; NULL if 0).  An
+ *                index below 0 is an absent entry, and so is one with the value
+ *                -inf; a row without any has KD = 0.  An index may occur twice.
+ *   labels     : device int32 [T], or NULL for no CE term (CE = 0).  A label
+ *                below 0 makes its row an ignored one: nothing of it is read,
+ *                its loss, lse and gradient are 0.
+ *   tau, alpha : 0 < tau < inf, 0 <= alpha <= 1; at least one of the two terms
+ *                must be there (else SATS_EINVAL).
+ *   loss       : device fp32 [T], written.
+ *   lse        : device fp32 [T][2] or NULL; log sum_j exp(z_j / tau) and
+ *                log sum_j exp(z_j), for sats_distill_grad.
+ *   dev_status : device int32 [1] or NULL.  An index or label >= V sets it
+ *                (SATS_EDEVICE from sats_get_status_word); the entry is then
+ *                absent, the row an ignored one.
+ *   A row with a NaN or +inf logit, or with none above -inf, has the loss NaN.
+ *
+ * sats_distill_grad -- its backward pass:
+ *     dlogits_j = g (alpha tau (softmax(z / tau)_j - sum_{k: top_idx_k = j} q_k)
+ *                    + (1 - alpha) (softmax(z)_j - [j = label]))
+ *   from the same arguments and the lse that sats_distill_loss wrote.
+ *   g          : device fp32 [T], the gradient of each row's loss, or NULL for 1.
+ *   dlogits    : device, the logits' type, rows of V elements ld_d >= V apart,
+ *                written (each value rounded once).  It may be the logits
+ *                themselves (the same pointer and row stride); any other
+ *                overlap returns SATS_EINVAL.
+ *
+ * sats_distill_loss_grad -- both in one pass over the logits, for a caller who
+ *   knows g beforehand (a mean over the batch): loss and dlogits as above.
+ *
+ * sats_sample -- draws one token from each of B rows, from given random numbers.
+ *   With z the row, T its temperature and w_i = exp((z_i - max z) / T):
+ *     top-k: the k largest logits are kept (ties: the lower index first);
+ *     top-p: of these the shortest run of the largest (ties as before) whose
+ *            share of their mass sum w reaches p, one at least;
+ *     min-p: of these the ones with w_i >= min_p;
+ *   the token is the first kept one, in the vocabulary's order, at which the
+ *   running sum of w exceeds u times its total over the kept ones.
+ *   temperature, top_k, top_p, min_p : device fp32 / int32 / fp32 / fp32 [B],
+ *                or NULL for 1, off, off, off.  T >= 0 and finite, 0: the largest
+ *                logit (the lowest index that has it).  top_k <= 0 or >= V is off,
+ *                top_p >= 1 is off, top_p <= 0 keeps one, min_p <= 0 is off,
+ *                min_p <= 1.
+ *   u          : device fp32 [B], random numbers in [0, 1).
+ *   ids        : device int32 [B], written.
+ *   logprob    : device fp32 [B] or NULL; the log of the drawn token's share of
+ *                the kept mass.
+ *   n_kept     : device int32 [B] or NULL; how many tokens were kept.
+ *   -inf and NaN logits are never kept; where there are no others, the id is -1,
+ *   logprob -inf and n_kept 0.  If the largest logit is +inf, all that have it
+ *   weigh the same and the others nothing.  A setting outside its range (a NaN,
+ *   T < 0, min_p > 1, u outside [0, 1)) gives the id -1, logprob NaN and n_kept 0 and
+ *   sets *dev_status (device int32 [1] or NULL; SATS_EDEVICE).
+ *   Weights carry 35 bits or more relative to themselves, sums of them are exact;
+ *   weights below about 2^-44 of the largest count as 0 (2^-(60 - log2 V)).
+ */
+SATS_API sats_status sats_top_logits(const void *logits, int64_t ld, int T, int V, int K, float *values, int32_t *idx,
+                                     void *stream);
+SATS_API sats_status sats_top_logits_f32(const float *logits, int64_t ld, int T, int V, int K, float *values,
+                                         int32_t *idx, void *stream);
+SATS_API sats_status sats_distill_loss(const void *logits, int64_t ld, int T, int V, const int32_t *top_idx,
+                                       const float *top_val, int K, const int32_t *labels, float tau, float alpha,
+                                       float *loss, float *lse, int32_t *dev_status, void *stream);
+SATS_API sats_status sats_distill_loss_f32(const float *logits, int64_t ld, int T, int V, const int32_t *top_idx,
+                                           const float *top_val, int K, const int32_t *labels, float tau, float alpha,
+                                           float *loss, float *lse, int32_t *dev_status, void *stream);
+SATS_API sats_status sats_distill_grad(const void *logits, int64_t ld, int T, int V, const int32_t *top_idx,
+                                       const float *top_val, int K, const int32_t *labels, float tau, float alpha,
+                                       const float *lse, const float *g, void *dlogits, int64_t ld_d,
+                                       int32_t *dev_status, void *stream);
+SATS_API sats_status sats_distill_grad_f32(const float *logits, int64_t ld, int T, int V, const int32_t *top_idx,
+                                           const float *top_val, int K, const int32_t *labels, float tau, float alpha,
+                                           const float *lse, const float *g, float *dlogits, int64_t ld_d,
+                                           int32_t *dev_status, void *stream);
+SATS_API sats_status sats_distill_loss_grad(const void *logits, int64_t ld, int T, int V, const int32_t *top_idx,
+                                            const float *top_val, int K, const int32_t *labels, float tau,
+                                            float alpha, const float *g, float *loss, void *dlogits, int64_t ld_d,
+                                            int32_t *dev_status, void *stream);
+SATS_API sats_status sats_distill_loss_grad_f32(const float *logits, int64_t ld, int T, int V, const int32_t *top_idx,
+                                                const float *top_val, int K, const int32_t *labels, float tau,
+                                                float alpha, const float *g, float *loss, float *dlogits, int64_t ld_d,
+                                                int32_t *dev_status, void *stream);
+SATS_API sats_status sats_sample(const void *logits, int64_t ld, int B, int V, const float *temperature,
+                                 const int32_t *top_k, const float *top_p, const float *min_p, const float *u,
+                                 int32_t *ids, float *logprob, int32_t *n_kept, int32_t *dev_status, void *stream);
+SATS_API sats_status sats_sample_f32(const float *logits, int64_t ld, int B, int V, const float *temperature,
+                                     const int32_t *top_k, const float *top_p, const float *min_p, const float *u,
+                                     int32_t *ids, float *logprob, int32_t *n_kept, int32_t *dev_status, void *stream);
+
+/*
  * sats_selftest_wait_timeout -- exercises the failure path of the device-side
  * waits without a fault: one small kernel runs the library's bounded waits on
  * conditions nothing satisfies (an mbarrier phase no thread completes, a
