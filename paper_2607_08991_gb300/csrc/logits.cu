@@ -42,21 +42,20 @@ __device__ __forceinline__ float key_float(uint32_t k)
 }
 
 // ------------------------------------------------------------------ weights
-// 2^(j / 1024) in two floats: the leading 24 bits, and the rest times 2^41.
+// 2^(j / 1024) in two floats.
 struct Exp2Table {
-    float v[1024][2];
+    float2 v[1024];
 };
 constexpr Exp2Table make_exp2_table()
 {
     Exp2Table t{};
     for (int j = 0; j < 1024; ++j) {
         const double x = j * (0.69314718055994530942 / 1024.0);
-        double term = 1.0, sum = 0.0;
-        for (int k = 24; k > 0; --k) sum = (1.0 + sum) * (x / k);   // exp(x) - 1
-        term += sum;
-        const float hi = (float)term;
-        t.v[j][0] = hi;
-        t.v[j][1] = (float)((term - (double)hi) * 2199023255552.0);
+        double rest = 0.0;
+        for (int k = 24; k > 0; --k) rest = (1.0 + rest) * (x / k);   // exp(x) - 1
+        const double v = 1.0 + rest;
+        t.v[j].x = (float)v;
+        t.v[j].y = (float)(v - (double)t.v[j].x);
     }
     return t;
 }
@@ -66,8 +65,9 @@ __device__ const Exp2Table kExp2 = make_exp2_table();
 struct Scale {
     float top;        // the row's largest logit
     float chi, clo;   // log2(e) / T in two floats
-    int F;            // fraction bits of a weight
-    bool hard;        // only the largest logits weigh anything (they are +inf, or T next to nothing)
+    float magic;      // 1.5 * 2^(23 - F): one unit in the last place is 2^-F
+    int F;            // fraction bits of a weight, 43 at most
+    bool hard;        // only the largest logits weigh anything (they are +inf, or T is next to nothing)
 };
 
 // chi + clo = log2(e) / T to twice the precision.
@@ -78,35 +78,76 @@ __device__ __forceinline__ void set_scale(Scale &s, float top, float T, int V)
     s.hard = top == INFINITY || T < 1e-30f;
     s.chi = __fdiv_rn(Lh, T);
     s.clo = __fdiv_rn(__fadd_rn(fmaf(-s.chi, T, Lh), Ll), T);
-    const int bits = 32 - __clz(V - 1);       // V - 1 < 2^bits
-    s.F = min(50, 62 - (V > 1 ? bits : 0));   // V weights of at most 2^F + 1 stay below 2^63
+    s.F = min(43, 62 - (32 - __clz(V)));      // V weights of 2^F stay below 2^62
+    s.magic = __int_as_float(((127 + 23 - s.F) << 23) | 0x400000);
 }
 
-// round-to-odd keeps the sums unbiased: what the shift drops counts as one half of the last place kept.
+constexpr float kMagicG = 12288.f;   // 1.5 * 2^13: one unit in the last place is 2^-10
+constexpr float kMagicW = 6.f;       // 1.5 * 2^2: 2^-21
+
+// Two weights 2^F exp((z - top) / T) as whole numbers (i1 << (F - 21)) + i2, where z <= top; `in` says whether they
+// can be other than 0 (false for NaN and -inf, whose numbers mean nothing).  g: -g / 1024 octaves below the top.
+// Sums of floats in pairs throughout; relative error about 2^-35, from the rounding of r L and T.x q to 24 bits.
+struct Weights2 {
+    int i1[2], i2[2], g[2];
+    bool in[2];
+};
+__device__ __forceinline__ Weights2 weights2(f32x2 z, const Scale &s, const float2 *tab)
+{
+    const auto both = [](float v) { return pack2(v, v); };
+    constexpr float L = 0.69314718055994530942f;
+    const f32x2 minus1 = both(-1.f);
+    // x = z - top exactly, xh + xl
+    const f32x2 nt = both(-s.top);
+    const f32x2 xh = fadd2(z, nt);
+    const f32x2 bv = ffma2(xh, minus1, z);               // z - xh
+    const f32x2 av = fadd2(xh, bv);
+    const f32x2 xl = fadd2(ffma2(av, minus1, z), fadd2(bv, nt));
+    // p + e = x log2(e) / T
+    const f32x2 chi = both(s.chi);
+    const f32x2 p = fmul2(xh, chi);
+    const f32x2 e = ffma2(xl, chi, ffma2(xh, both(s.clo), ffma2(xh, chi, fmul2(p, minus1))));
+    // p = g / 1024 + what r starts from, exactly
+    const f32x2 m = fadd2(p, both(kMagicG));
+    const f32x2 r = fadd2(ffma2(fadd2(m, both(-kMagicG)), minus1, p), e);   // |r| <= 2^-11, and a little
+    // q = 2^r - 1
+    const f32x2 q = fmul2(r, ffma2(r, ffma2(r, both(L * L * L / 6.f), both(L * L / 2.f)), both(L)));
+    const float2 mm = unpack2(m), pp = unpack2(p);
+    Weights2 w;
+    w.g[0] = __float_as_int(mm.x) - __float_as_int(kMagicG);
+    w.g[1] = __float_as_int(mm.y) - __float_as_int(kMagicG);
+    w.in[0] = pp.x > -60.f;
+    w.in[1] = pp.y > -60.f;
+    const float2 t0 = tab[w.g[0] & 1023], t1 = tab[w.g[1] & 1023];
+    const f32x2 tx = pack2(t0.x, t1.x);
+    const f32x2 lo = ffma2(tx, q, pack2(t0.y, t1.y));
+    // h + l = 2^(g mod 1024 / 1024 + r), scaled by 2^(g div 1024)
+    const f32x2 h = fadd2(tx, lo);
+    const f32x2 l = fadd2(lo, fmul2(ffma2(tx, minus1, h), minus1));
+    const f32x2 sc = pack2(__int_as_float(0x3f800000 + ((w.g[0] << 13) & 0xff800000)),
+                           __int_as_float(0x3f800000 + ((w.g[1] << 13) & 0xff800000)));
+    const f32x2 hs = fmul2(h, sc);
+    const f32x2 m1 = fadd2(hs, both(kMagicW));
+    const f32x2 d = ffma2(l, sc, ffma2(fadd2(m1, both(-kMagicW)), minus1, hs));
+    const float2 a = unpack2(m1), b = unpack2(fadd2(d, both(s.magic)));
+    w.i1[0] = __float_as_int(a.x) - __float_as_int(kMagicW);
+    w.i1[1] = __float_as_int(a.y) - __float_as_int(kMagicW);
+    w.i2[0] = __float_as_int(b.x) - __float_as_int(s.magic);
+    w.i2[1] = __float_as_int(b.y) - __float_as_int(s.magic);
+    return w;
+}
+
+__device__ __forceinline__ unsigned long long whole_weight(int i1, int i2, const Scale &s)
+{
+    return ((unsigned long long)(unsigned)i1 << (s.F - 21)) + (long long)i2;
+}
+
+// One weight.
 __device__ __forceinline__ unsigned long long weight(float z, const Scale &s, const float2 *tab)
 {
-    if (s.hard) return z == s.top ? (1ull << s.F) | 1ull : 0ull;
-    // x = z - top exactly, in two floats
-    const float xh = __fsub_rn(z, s.top);
-    const float bv = __fsub_rn(z, xh), av = __fadd_rn(xh, bv);
-    const float xl = __fadd_rn(__fsub_rn(z, av), __fsub_rn(bv, s.top));
-    const float p = __fmul_rn(xh, s.chi);
-    if (!(p > -(float)(s.F - 1))) return 0ull;   // (-inf among them)
-    const float e = fmaf(xl, s.chi, fmaf(xh, s.clo, fmaf(xh, s.chi, -p)));
-    // p = g / 1024 + rest, exactly
-    constexpr float kMagic = 12288.f;            // 1.5 * 2^13: one unit in the last place is 2^-10
-    const float m = __fadd_rn(p, kMagic);
-    const int g = __float_as_int(m) - __float_as_int(kMagic);
-    const float r = __fadd_rn(__fsub_rn(p, __fsub_rn(m, kMagic)), e);   // |r| <= 2^-11, and a little
-    // 2^r - 1, times 2^41
-    constexpr float L = 0.69314718055994530942f, S41 = 2199023255552.f;
-    const float q = r * fmaf(r, fmaf(r, S41 * (L * L * L / 6.f), S41 * (L * L / 2.f)), S41 * L);
-    const float2 t = tab[g & 1023];
-    const int lo = __float2int_rn(fmaf(t.x, q, t.y));
-    const uint32_t hi24 = __float_as_uint(t.x) - 0x3f000000u;   // t.x = hi24 / 2^23
-    const unsigned long long w = ((unsigned long long)hi24 << 18) + (long long)lo;   // 41 fraction bits
-    const int down = 61 - s.F - (g >> 10);       // in 0..61 (p > 1 - F)
-    return ((w << 20) >> down) | 1ull;
+    if (s.hard) return z == s.top ? 1ull << s.F : 0ull;
+    const Weights2 w = weights2(pack2(z, z), s, tab);
+    return w.in[0] ? whole_weight(w.i1[0], w.i2[0], s) : 0ull;
 }
 
 // f * total for 0 <= f < 1, exactly and rounded down (and up): shares of a mass at a border are not to depend on a
@@ -155,7 +196,8 @@ struct Shared {
     int found_idx;
     uint32_t found_key;
     uint32_t kminp;
-    int flag;
+    uint32_t bin, bin_kmin, bin_kmax;                // the nucleus' border
+    unsigned long long bin_above;
 };
 
 template <bool F32>
@@ -234,48 +276,57 @@ __device__ __forceinline__ unsigned long long cluster_sum(Ctx<F32> &c, unsigned 
     return t;
 }
 
-// What is kept: keys above `key`, and of those equal to it the ones up to index `idx`.
+// What is kept: keys above `key`, and of those equal to it the ones up to index `idx` (INT_MIN: none; the places of a
+// granule before the row have indices below 0).
 struct Cut {
     uint32_t key;
     int idx;
     __device__ __forceinline__ bool keeps(uint32_t k, int i) const { return k > key || (k == key && i <= idx); }
 };
 
-// Sum of f(logit, key, index) over granule v.
-template <bool F32, typename F>
-__device__ __forceinline__ unsigned long long granule_sum(const Ctx<F32> &c, int v, F f)
-{
-    constexpr int E = RowElem<F32>::kPer;
-    float x[E];
-    granule_floats<F32>(c.get(v), x);
-    const int i0 = c.r.first(c.gb + v);
-    unsigned long long s = 0;
+// A sum over the row's tokens is given by a functor: elem(logit, key, index) for one of them, granule(c, v) for the
+// ones of granule v.  ByElem makes one of a function of an element.
+template <typename F>
+struct ByElem {
+    F f;
+    __device__ __forceinline__ unsigned long long elem(float x, uint32_t k, int i) const { return f(x, k, i); }
+    template <bool F32>
+    __device__ __forceinline__ unsigned long long granule(const Ctx<F32> &c, int v) const
+    {
+        constexpr int E = RowElem<F32>::kPer;
+        float x[E];
+        granule_floats<F32>(c.get(v), x);
+        const int i0 = c.r.first(c.gb + v);
+        unsigned long long s = 0;
 #pragma unroll
-    for (int j = 0; j < E; ++j) {
-        const uint32_t k = key_of(x[j]);
-        if (k > kKeyNone) s += f(x[j], k, i0 + j);   // (places outside the row are -inf)
+        for (int j = 0; j < E; ++j) {
+            const uint32_t k = key_of(x[j]);
+            if (k > kKeyNone) s += f(x[j], k, i0 + j);   // (places outside the row are -inf)
+        }
+        return s;
     }
-    return s;
-}
+};
+template <typename F>
+__device__ __forceinline__ ByElem<F> by_elem(F f) { return ByElem<F>{f}; }
 
 // Sum over this thread's granules, lanes in turn over the warp's run of them.
-template <bool F32, typename F>
-__device__ __forceinline__ unsigned long long thread_sum(const Ctx<F32> &c, F f)
+template <bool F32, typename S>
+__device__ __forceinline__ unsigned long long thread_sum(const Ctx<F32> &c, const S &f)
 {
     unsigned long long s = 0;
-    for (int v = c.wb + (int)(threadIdx.x & 31); v < c.we; v += 32) s += granule_sum(c, v, f);
+    for (int v = c.wb + (int)(threadIdx.x & 31); v < c.we; v += 32) s += f.granule(c, v);
     return s;
 }
 
 // The first token in the vocabulary's order at which the running sum of f passes `target` (which is below the sum
-// over the row): *idx, *key in every CTA.  The CTA that holds it narrows a run of granules down sixteenfold a step.
-template <bool F32, typename F>
-__device__ void locate(Ctx<F32> &c, unsigned long long target, F f, int *idx, uint32_t *key)
+// over the row): *idx, *key in every CTA.  The warps' sums are in sh->wsum (block_sum_u64 of thread_sum), the CTA's is
+// `mine`, the CTAs' are in `slot`.  The CTA that holds the token narrows a run of granules down sixteenfold a step.
+template <bool F32, typename S>
+__device__ void locate(Ctx<F32> &c, unsigned long long target, const S &f, unsigned long long mine,
+                       const unsigned long long *slot, int *idx, uint32_t *key)
 {
     Shared *sh = c.sh;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const unsigned long long mine = block_sum_u64(thread_sum(c, f), sh);
-    const unsigned long long *slot = cluster_gather(c, mine);
     unsigned long long before = 0;
     for (unsigned k = 0; k < c.rank; ++k) before += slot[k];
     if (target >= before && target - before < mine) {   // (one CTA)
@@ -290,12 +341,12 @@ __device__ void locate(Ctx<F32> &c, unsigned long long target, F f, int *idx, ui
             per = (b - a + kRowWarps - 1) / kRowWarps;
             unsigned long long s = 0;
             const int wb = min(b, a + warp * per), we = min(b, wb + per);
-            for (int v = wb + lane; v < we; v += 32) s += granule_sum(c, v, f);
+            for (int v = wb + lane; v < we; v += 32) s += f.granule(c, v);
             block_sum_u64(s, sh);
         }
         if (warp == 0) {
             const int v = a + lane;
-            const unsigned long long s = v < b ? granule_sum(c, v, f) : 0ull;
+            const unsigned long long s = v < b ? f.granule(c, v) : 0ull;
             unsigned long long incl = s;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -313,7 +364,7 @@ __device__ void locate(Ctx<F32> &c, unsigned long long target, F f, int *idx, ui
 #pragma unroll
                 for (int j = 0; j < E; ++j) {
                     const uint32_t k = key_of(x[j]);
-                    if (k > kKeyNone) run += f(x[j], k, i0 + j);
+                    if (k > kKeyNone) run += f.elem(x[j], k, i0 + j);
                     if (!hit && run > t) {
                         hit = true;
                         for (int q = 0; q < c.C; ++q) {
@@ -331,17 +382,27 @@ __device__ void locate(Ctx<F32> &c, unsigned long long target, F f, int *idx, ui
     *key = sh->found_key;
 }
 
-// The largest key at which sum(f over keys >= it) is at least `want` (1 <= want <= the sum over all), the sum over
-// the keys above it in *above.
-template <bool F32, typename F>
-__device__ uint32_t bisect_key(Ctx<F32> &c, uint32_t kmax, unsigned long long want, F f, unsigned long long *above)
+// The same, with the sums to be taken first.
+template <bool F32, typename S>
+__device__ void sum_and_locate(Ctx<F32> &c, unsigned long long target, const S &f, int *idx, uint32_t *key)
 {
-    uint32_t lo = kKeyNone + 1, hi = kmax + 1;   // sum(lo) >= want > sum(hi)
+    const unsigned long long mine = block_sum_u64(thread_sum(c, f), c.sh);
+    const unsigned long long *slot = cluster_gather(c, mine);
+    locate(c, target, f, mine, slot, idx, key);
+}
+
+// The largest key at which sum(f over keys >= it) is at least `want` (1 <= want <= the sum over all): between kmin and
+// kmax, the least and the largest key that f counts.  The sum over the keys above it in *above.
+template <bool F32, typename F>
+__device__ uint32_t bisect_key(Ctx<F32> &c, uint32_t kmin, uint32_t kmax, unsigned long long want, F f,
+                               unsigned long long *above)
+{
+    uint32_t lo = kmin, hi = kmax + 1;   // sum(lo) >= want > sum(hi)
     unsigned long long s_hi = 0;
     while (hi - lo > 1) {
         const uint32_t mid = lo + (hi - lo) / 2;
-        const unsigned long long s =
-            cluster_sum(c, thread_sum(c, [&](float x, uint32_t k, int i) { return k >= mid ? f(x, k, i) : 0ull; }));
+        const auto from_mid = by_elem([&](float x, uint32_t k, int i) { return k >= mid ? f(x, k, i) : 0ull; });
+        const unsigned long long s = cluster_sum(c, thread_sum(c, from_mid));
         if (s >= want) lo = mid;
         else { hi = mid; s_hi = s; }
     }
@@ -354,18 +415,96 @@ template <bool F32>
 __device__ Cut cut_count(Ctx<F32> &c, uint32_t kmax, int k)
 {
     const auto one = [](float, uint32_t, int) { return 1ull; };
-    if (cluster_sum(c, thread_sum(c, one)) <= (unsigned long long)k) return Cut{kKeyNone, -1};
+    if (cluster_sum(c, thread_sum(c, by_elem(one))) <= (unsigned long long)k) return Cut{kKeyNone, INT_MIN};
     unsigned long long above;
     Cut cut;
-    cut.key = bisect_key(c, kmax, (unsigned long long)k, one, &above);
+    cut.key = bisect_key(c, kKeyNone + 1, kmax, (unsigned long long)k, one, &above);
     const uint32_t at = cut.key;
     uint32_t key;
-    locate(c, (unsigned long long)k - above - 1ull, [at](float, uint32_t q, int) { return q == at ? 1ull : 0ull; },
-           &cut.idx, &key);
+    sum_and_locate(c, (unsigned long long)k - above - 1ull,
+                   by_elem([at](float, uint32_t q, int) { return q == at ? 1ull : 0ull; }), &cut.idx, &key);
     return cut;
 }
 
+// The kept tokens' weights.
+struct KeptMass {
+    const Scale &s;
+    const float2 *tab;
+    Cut cut;
+    float at;   // the cut's key as a logit
+    __device__ __forceinline__ KeptMass(const Scale &s_, const float2 *t_, Cut c_)
+        : s(s_), tab(t_), cut(c_), at(key_float(c_.key)) {}
+    __device__ __forceinline__ unsigned long long elem(float x, uint32_t k, int i) const
+    {
+        return cut.keeps(k, i) ? weight(x, s, tab) : 0ull;
+    }
+    __device__ __forceinline__ bool keeps(float x, int i) const { return x > at || (x == at && i <= cut.idx); }
+    template <bool F32>
+    __device__ __forceinline__ unsigned long long granule(const Ctx<F32> &c, int v) const
+    {
+        int n = 0;
+        return granule(c, v, n);
+    }
+    // ... and their number, added to n
+    template <bool F32>
+    __device__ __forceinline__ unsigned long long granule(const Ctx<F32> &c, int v, int &n) const
+    {
+        constexpr int P = RowElem<F32>::kPer / 2;
+        const uint4 x = c.get(v);
+        if (!(granule_max<F32>(x) >= at)) return 0ull;
+        f32x2 z[P];
+        granule_pairs<F32>(x, z);
+        const int i0 = c.r.first(c.gb + v);
+        int a1 = 0, a2 = 0;
+        if (s.hard) {
+#pragma unroll
+            for (int j = 0; j < P; ++j) {
+                const float2 y = unpack2(z[j]);
+                const bool k0 = keeps(y.x, i0 + 2 * j), k1 = keeps(y.y, i0 + 2 * j + 1);
+                n += k0 + k1;
+                a1 += ((k0 && y.x == s.top) + (k1 && y.y == s.top)) << 21;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < P; ++j) {
+                const float2 y = unpack2(z[j]);
+                const Weights2 w = weights2(z[j], s, tab);
+                const bool k0 = keeps(y.x, i0 + 2 * j), k1 = keeps(y.y, i0 + 2 * j + 1);
+                n += k0 + k1;
+                if (k0 && w.in[0]) { a1 += w.i1[0]; a2 += w.i2[0]; }
+                if (k1 && w.in[1]) { a1 += w.i1[1]; a2 += w.i2[1]; }
+            }
+        }
+        return whole_weight(a1, a2, s);   // (eight weights at most)
+    }
+};
+
 // ------------------------------------------------------------------ the list
+constexpr int kListPer = kListCap / kRowThreads;   // list entries of a thread, in a row
+
+// Exclusive sums of the threads' values over the CTA, the total in *total.
+__device__ __forceinline__ unsigned long long block_scan_u64(unsigned long long v, Shared *sh, unsigned long long *total)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    unsigned long long incl = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const unsigned long long u = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += u;
+    }
+    __syncthreads();
+    if (lane == 31) sh->scan[warp] = incl;
+    __syncthreads();
+    unsigned long long before = 0, t = 0;
+#pragma unroll
+    for (int w = 0; w < kRowWarps; ++w) {
+        if (w < warp) before += sh->scan[w];
+        t += sh->scan[w];
+    }
+    *total = t;
+    return before + incl - v;
+}
+
 // Sorts n2 (a power of two) words descending; all threads of the CTA.
 __device__ void sort_desc(unsigned long long *a, int n2)
 {
@@ -390,8 +529,31 @@ __device__ void sort_desc(unsigned long long *a, int n2)
 
 __device__ __forceinline__ int pow2_at_least(int n) { return n <= 1 ? 1 : 1 << (32 - __clz(n - 1)); }
 
-// Elements with keys from `bound` on that `cut` keeps, to the list of the cluster's first CTA, in no order.  Returns
-// how many there are (in every CTA; the list is complete only if they fit, and `ok` says so).
+// Brings the CTAs' parts of the list (sh->nlist entries each, of which up to kListCap are there) together in the
+// cluster's first CTA.  Returns how many there are (in every CTA); *ok: they fit and are there.
+template <bool F32>
+__device__ int push_list(Ctx<F32> &c, unsigned long long *list, bool *ok)
+{
+    Shared *sh = c.sh;
+    __syncthreads();
+    const uint32_t mine = sh->nlist;
+    const unsigned long long *slot = cluster_gather(c, (unsigned long long)mine);
+    unsigned long long total = 0, before = 0;
+    for (int k = 0; k < c.C; ++k) {
+        if (k < (int)c.rank) before += slot[k];
+        total += slot[k];
+    }
+    *ok = total <= kListCap;
+    if (*ok && c.C > 1) {
+        if (c.rank != 0)
+            for (uint32_t i = threadIdx.x; i < mine; i += kRowThreads)
+                st_peer_u64(peer_addr(list + before + i, 0), list[i]);
+        cluster_sync_all();
+    }
+    return (int)(total < (unsigned long long)INT_MAX ? total : INT_MAX);
+}
+
+// Elements with keys from `bound` on that `cut` keeps, to the list of the cluster's first CTA, in no order (push_list).
 template <bool F32>
 __device__ int gather_list(Ctx<F32> &c, unsigned long long *list, uint32_t bound, Cut cut, bool *ok)
 {
@@ -415,22 +577,7 @@ __device__ int gather_list(Ctx<F32> &c, unsigned long long *list, uint32_t bound
             }
         }
     }
-    __syncthreads();
-    const uint32_t mine = sh->nlist;
-    const unsigned long long *slot = cluster_gather(c, (unsigned long long)mine);
-    unsigned long long total = 0, before = 0;
-    for (int k = 0; k < c.C; ++k) {
-        if (k < (int)c.rank) before += slot[k];
-        total += slot[k];
-    }
-    *ok = total <= kListCap;
-    if (*ok && c.C > 1) {
-        if (c.rank != 0)
-            for (uint32_t i = threadIdx.x; i < mine; i += kRowThreads)
-                st_peer_u64(peer_addr(list + before + i, 0), list[i]);
-        cluster_sync_all();
-    }
-    return (int)(total < (unsigned long long)INT_MAX ? total : INT_MAX);
+    return push_list(c, list, ok);
 }
 
 // Pads the list with zeros and sorts it; n <= kListCap.  (First CTA.)
@@ -439,6 +586,166 @@ __device__ void sort_list(unsigned long long *list, int n)
     const int n2 = pow2_at_least(n);
     for (int i = n + threadIdx.x; i < n2; i += kRowThreads) list[i] = 0ull;
     sort_desc(list, n2);
+}
+
+// ------------------------------------------------------------------ the nucleus
+// The masses of 2048 steps of the weight, in whole numbers: a word for their lower 32 bits and one for what is above.
+constexpr int kBins = 2048;
+static_assert(2 * kBins * 4 <= kListCap * 8, "the histogram lies where the list does");
+
+// The step (of 1 / 1024 octave << shift, from the top down) of a weight; the same function in both of its uses.
+__device__ __forceinline__ uint32_t bin_of(int g, int shift) { return min((uint32_t)(-g) >> shift, (uint32_t)kBins - 1u); }
+
+template <bool F32, typename F>
+__device__ __forceinline__ void each_weight(const Ctx<F32> &c, const Scale &s, const float2 *tab, const KeptMass &kept, F f)
+{
+    constexpr int P = RowElem<F32>::kPer / 2;
+    for (int v = c.wb + (int)(threadIdx.x & 31); v < c.we; v += 32) {
+        const uint4 x = c.get(v);
+        if (!(granule_max<F32>(x) >= kept.at)) continue;
+        f32x2 z[P];
+        granule_pairs<F32>(x, z);
+        const int i0 = c.r.first(c.gb + v);
+#pragma unroll
+        for (int j = 0; j < P; ++j) {
+            const float2 y = unpack2(z[j]);
+            if (s.hard) {
+                if (y.x == s.top && kept.keeps(y.x, i0 + 2 * j)) f(y.x, i0 + 2 * j, 0, 1 << 21, 0);
+                if (y.y == s.top && kept.keeps(y.y, i0 + 2 * j + 1)) f(y.y, i0 + 2 * j + 1, 0, 1 << 21, 0);
+            } else {
+                const Weights2 w = weights2(z[j], s, tab);
+                if (w.in[0] && kept.keeps(y.x, i0 + 2 * j)) f(y.x, i0 + 2 * j, w.g[0], w.i1[0], w.i2[0]);
+                if (w.in[1] && kept.keeps(y.y, i0 + 2 * j + 1)) f(y.y, i0 + 2 * j + 1, w.g[1], w.i1[1], w.i2[1]);
+            }
+        }
+    }
+}
+
+// The cut that keeps, of what by_k keeps, the largest up to a share top_p < 1 of the mass: the step in which the mass
+// from the top reaches it, by a histogram of masses, and the place within the step by sorting its elements.
+template <bool F32>
+__device__ Cut cut_mass(Ctx<F32> &c, const Scale &s, const float2 *tab, unsigned long long *list, Cut by_k, float top_p)
+{
+    Shared *sh = c.sh;
+    const int tid = threadIdx.x;
+    uint32_t *lo = reinterpret_cast<uint32_t *>(list), *hi = lo + kBins;
+    // steps as fine as 32 logits, or what weighs more than 2^-64, allow
+    int shift = 0;
+    while (shift < 5 && (float)(2 << shift) < 32.f * s.chi) ++shift;
+    for (int i = tid; i < 2 * kBins; i += kRowThreads) lo[i] = 0u;
+    __syncthreads();
+    const KeptMass kept(s, tab, by_k);
+    each_weight(c, s, tab, kept, [&](float, int, int g, int i1, int i2) {
+        const unsigned long long w = whole_weight(i1, i2, s);
+        if (w == 0) return;
+        const uint32_t b = bin_of(g, shift), wl = (uint32_t)w, was = atomicAdd(lo + b, wl);
+        const uint32_t up = (uint32_t)(w >> 32) + (was + wl < was ? 1u : 0u);
+        if (up) atomicAdd(hi + b, up);
+    });
+    if (c.C > 1) cluster_sync_all();
+    else __syncthreads();
+    // a run of steps per CTA, over all CTAs' histograms
+    const int nb = kBins / c.C, per = (nb + kRowThreads - 1) / kRowThreads, b0 = (int)c.rank * nb + tid * per;
+    unsigned long long m[kBins / kRowThreads], mine = 0;
+#pragma unroll
+    for (int j = 0; j < kBins / kRowThreads; ++j) {
+        m[j] = 0;
+        if (j < per && tid * per + j < nb) {
+            for (int k = 0; k < c.C; ++k)
+                m[j] += ((unsigned long long)ld_peer_u32(peer_addr(hi + b0 + j, k)) << 32) + ld_peer_u32(peer_addr(lo + b0 + j, k));
+        }
+        mine += m[j];
+    }
+    unsigned long long total;
+    unsigned long long run = block_scan_u64(mine, sh, &total);
+    const unsigned long long *slot = cluster_gather(c, total);
+    unsigned long long Z = 0;
+    for (int k = 0; k < c.C; ++k) {
+        if (k < (int)c.rank) run += slot[k];
+        Z += slot[k];
+    }
+    const unsigned long long target = share_ceil(top_p, Z);   // 1 <= target <= Z
+#pragma unroll
+    for (int j = 0; j < kBins / kRowThreads; ++j) {
+        if (run < target && target - run <= m[j])   // (one thread)
+            for (int k = 0; k < c.C; ++k) {
+                st_peer_u32(peer_addr(&sh->bin, k), (uint32_t)(b0 + j));
+                st_peer_u64(peer_addr(&sh->bin_above, k), run);
+            }
+        run += m[j];
+    }
+    if (tid == 0) {
+        sh->nlist = 0;
+        sh->bin_kmin = 0xffffffffu;
+        sh->bin_kmax = 0u;
+    }
+    if (c.C > 1) cluster_sync_all();
+    else __syncthreads();
+    const uint32_t bin = sh->bin;
+    const unsigned long long want = target - sh->bin_above;
+
+    // the step's elements
+    each_weight(c, s, tab, kept, [&](float x, int i, int g, int, int) {
+        if (bin_of(g, shift) != bin) return;
+        const uint32_t at = atomicAdd(&sh->nlist, 1u), k = key_of(x);
+        if (at < kListCap) list[at] = ((unsigned long long)k << 32) | (uint32_t)~(uint32_t)i;
+        else { atomicMin(&sh->bin_kmin, k); atomicMax(&sh->bin_kmax, k); }
+    });
+    bool ok;
+    const int n = push_list(c, list, &ok);
+    if (ok) {
+        if (c.rank == 0) {
+            sort_list(list, n);
+            unsigned long long w[kListPer], sum = 0, all;
+#pragma unroll
+            for (int j = 0; j < kListPer; ++j) {
+                const int i = tid * kListPer + j;
+                w[j] = i < n ? weight(key_float((uint32_t)(list[i] >> 32)), s, tab) : 0ull;
+                sum += w[j];
+            }
+            unsigned long long at = block_scan_u64(sum, sh, &all);
+#pragma unroll
+            for (int j = 0; j < kListPer; ++j) {
+                if (at < want && want - at <= w[j]) {   // the last one kept (one thread)
+                    const unsigned long long e = list[tid * kListPer + j];
+                    for (int k = 0; k < c.C; ++k) {
+                        st_peer_u32(peer_addr(&sh->found_key, k), (uint32_t)(e >> 32));
+                        st_peer_u32(peer_addr(&sh->found_idx, k), ~(uint32_t)e);
+                    }
+                }
+                at += w[j];
+            }
+        }
+        if (c.C > 1) cluster_sync_all();
+        else __syncthreads();
+        return Cut{sh->found_key, sh->found_idx};
+    }
+    // more of them than the list holds, as a rule equal ones: the key by bisection among the step's, then the ties
+    for (uint32_t i = tid; i < min(sh->nlist, (uint32_t)kListCap); i += kRowThreads) {
+        atomicMin(&sh->bin_kmin, (uint32_t)(list[i] >> 32));
+        atomicMax(&sh->bin_kmax, (uint32_t)(list[i] >> 32));
+    }
+    __syncthreads();
+    slot = cluster_gather(c, ((unsigned long long)sh->bin_kmin << 32) | sh->bin_kmax);
+    uint32_t kmin = 0xffffffffu, kmax = 0u;
+    for (int k = 0; k < c.C; ++k) {
+        kmin = min(kmin, (uint32_t)(slot[k] >> 32));
+        kmax = max(kmax, (uint32_t)slot[k]);
+    }
+    const auto in_step = [&](float x, uint32_t q, int i) {
+        return q >= kmin && q <= kmax && by_k.keeps(q, i) ? weight(x, s, tab) : 0ull;
+    };
+    unsigned long long above;
+    const uint32_t key = bisect_key(c, kmin, kmax, want, in_step, &above);
+    const unsigned long long w = weight(key_float(key), s, tab);
+    const unsigned long long ties = (want - above + w - 1ull) / w;   // the first of them that reach the mass
+    Cut cut;
+    uint32_t at;
+    sum_and_locate(c, ties - 1ull,
+                   by_elem([=](float, uint32_t q, int i) { return q == key && by_k.keeps(q, i) ? 1ull : 0ull; }),
+                   &cut.idx, &at);
+    cut.key = key;
+    return cut;
 }
 
 // Brings the row in and finds its largest key and, for want > 0, a bound with at least `want` elements at or above
@@ -608,7 +915,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) top_kernel(const TopParams p)
     uint32_t kmax, bound;
     load_row(c, smem, p.K, &kmax, &bound);
     bool ok;
-    int n = gather_list(c, list, bound, Cut{kKeyNone, -1}, &ok);
+    int n = gather_list(c, list, bound, Cut{kKeyNone, INT_MIN}, &ok);
     if (!ok) {   // (the same in every CTA of the row)
         const Cut cut = cut_count(c, kmax, p.K);
         n = gather_list(c, list, max(cut.key, kKeyNone + 1), cut, &ok);   // at most K
@@ -650,31 +957,6 @@ __device__ __forceinline__ float log_share(float z, float T, const Scale &s, uns
     return (z == s.top ? 0.f : (z - s.top) / T) - log1pf(rest);
 }
 
-// Exclusive sums of the threads' values over the CTA, the total in *total.
-__device__ __forceinline__ unsigned long long block_scan_u64(unsigned long long v, Shared *sh, unsigned long long *total)
-{
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    unsigned long long incl = v;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const unsigned long long u = __shfl_up_sync(0xffffffffu, incl, o);
-        if (lane >= o) incl += u;
-    }
-    __syncthreads();
-    if (lane == 31) sh->scan[warp] = incl;
-    __syncthreads();
-    unsigned long long before = 0, t = 0;
-#pragma unroll
-    for (int w = 0; w < kRowWarps; ++w) {
-        if (w < warp) before += sh->scan[w];
-        t += sh->scan[w];
-    }
-    *total = t;
-    return before + incl - v;
-}
-
-constexpr int kListPer = kListCap / kRowThreads;   // list entries of a thread, in a row
-
 template <bool F32>
 __global__ void __launch_bounds__(kRowThreads, 2) sample_kernel(const SampleParams p)
 {
@@ -697,9 +979,9 @@ __global__ void __launch_bounds__(kRowThreads, 2) sample_kernel(const SamplePara
     if (k < 0 || k >= p.V) k = 0;
     const bool greedy = T == 0.f || k == 1 || top_p <= 0.f;
     const bool nucleus = top_p < 1.f;
-    // the list serves a top-k that fits it, and without one the nucleus if it lies within the largest logits
-    const int want = greedy ? 0 : (k > 0 && k <= kMaxTop ? k : (k == 0 && nucleus ? kMaxTop : 0));
-    for (int i = tid; i < 1024; i += kRowThreads) tab[i] = make_float2(kExp2.v[i][0], kExp2.v[i][1]);
+    const int want = !greedy && k > 0 && k <= kMaxTop ? k : 0;   // what the list serves
+    if (!greedy)
+        for (int i = tid; i < 1024; i += kRowThreads) tab[i] = kExp2.v[i];
     Ctx<F32> c{Row<F32>(p.z, row, p.ld, p.V)};
     set_ctx(c, smem, p.cached, p.cluster, &sh);
     uint32_t kmax, bound;
@@ -727,114 +1009,84 @@ __global__ void __launch_bounds__(kRowThreads, 2) sample_kernel(const SamplePara
         __syncthreads();
         kminp = sh.kminp;
     }
-    const auto mass = [&](float x, uint32_t, int) { return weight(x, s, tab); };
 
-    const bool only_minp = k == 0 && !nucleus && kminp > kKeyNone;
-    if (want > 0 || only_minp) {
-        unsigned long long Z = 0;
-        if (k == 0 && nucleus) Z = cluster_sum(c, thread_sum(c, mass));
-        // with a top-k the list must hold all of it: its mass is what top-p refers to
-        const uint32_t from = k > 0 ? bound : max(want > 0 ? bound : kKeyNone + 1, kminp);
+    if (want > 0) {
         bool ok;
-        const int n = gather_list(c, list, from, Cut{kKeyNone, -1}, &ok);
-        if (ok) {
-            if (c.rank == 0) {
-                sort_list(list, n);
-                int m = k > 0 ? min(n, k) : n;
-                unsigned long long w[kListPer], sum = 0, total;
-                if (nucleus || k > 0) {
-                    int in_minp = 0;
+        const int n = gather_list(c, list, bound, Cut{kKeyNone, INT_MIN}, &ok);
+        if (ok) {   // (the same in every CTA of the row)
+            if (c.rank != 0) return;   // (nobody reads this CTA's memory any more)
+            sort_list(list, n);
+            int m = min(n, k);
+            unsigned long long w[kListPer], sum = 0, total;
+            if (nucleus || kminp > 0) {
+                int in_minp = 0;
 #pragma unroll
-                    for (int j = 0; j < kListPer; ++j) {
-                        const int i = tid * kListPer + j;
-                        const uint32_t key = i < m ? (uint32_t)(list[i] >> 32) : 0u;
-                        w[j] = i < m ? weight(key_float(key), s, tab) : 0ull;
-                        sum += w[j];
-                        in_minp += i < m && key >= kminp;
-                    }
-                    unsigned long long run = block_scan_u64(sum, &sh, &total);
-                    if (k > 0) Z = total;
-                    const unsigned long long target = nucleus ? share_ceil(top_p, Z) : ~0ull;
-                    int in_p = 0;
-#pragma unroll
-                    for (int j = 0; j < kListPer; ++j) {
-                        in_p += tid * kListPer + j < m && run < target;
-                        run += w[j];
-                    }
-                    const unsigned long long both =
-                        block_sum_u64(((unsigned long long)(unsigned)in_p << 32) | (unsigned)in_minp, &sh);
-                    // the nucleus may reach beyond the list
-                    if (k == 0 && total < target && from > kminp && from > kKeyNone + 1) m = -1;
-                    else m = min((int)(both >> 32), (int)(uint32_t)both);
+                for (int j = 0; j < kListPer; ++j) {
+                    const int i = tid * kListPer + j;
+                    const uint32_t key = i < m ? (uint32_t)(list[i] >> 32) : 0u;
+                    w[j] = i < m ? weight(key_float(key), s, tab) : 0ull;
+                    sum += w[j];
+                    in_minp += i < m && key >= kminp;
                 }
-                if (m > 0) {
-                    // the kept ones in the vocabulary's order
-                    const int m2 = pow2_at_least(m);
-                    __syncthreads();
-                    for (int i = tid; i < m2; i += kRowThreads) {
-                        const unsigned long long e = list[i];
-                        list[i] = i < m ? (e << 32) | (e >> 32) : 0ull;
-                    }
-                    sort_desc(list, m2);
-                    sum = 0;
+                unsigned long long run = block_scan_u64(sum, &sh, &total);
+                const unsigned long long target = nucleus ? share_ceil(top_p, total) : ~0ull;
+                int in_p = 0;
 #pragma unroll
-                    for (int j = 0; j < kListPer; ++j) {
-                        const int i = tid * kListPer + j;
-                        w[j] = i < m ? weight(key_float((uint32_t)list[i]), s, tab) : 0ull;
-                        sum += w[j];
-                    }
-                    unsigned long long run = block_scan_u64(sum, &sh, &total);
-                    const unsigned long long target = share_floor(u, total);
-#pragma unroll
-                    for (int j = 0; j < kListPer; ++j) {
-                        const unsigned long long next = run + w[j];
-                        if (target >= run && target < next) {   // one entry
-                            const unsigned long long e = list[tid * kListPer + j];
-                            put_sample(p, row, (int)~(uint32_t)(e >> 32),
-                                       log_share(key_float((uint32_t)e), T, s, total), m);
-                        }
-                        run = next;
-                    }
+                for (int j = 0; j < kListPer; ++j) {
+                    in_p += tid * kListPer + j < m && run < target;
+                    run += w[j];
                 }
-                if (k == 0) {   // the others wait to hear whether that was all
-                    __syncthreads();
-                    if (tid < c.C) st_peer_u32(peer_addr(&sh.flag, tid), m > 0);
-                }
+                const unsigned long long both =
+                    block_sum_u64(((unsigned long long)(unsigned)in_p << 32) | (unsigned)in_minp, &sh);
+                m = min((int)(both >> 32), (int)(uint32_t)both);
             }
-            if (k > 0) return;
-            if (c.C > 1) cluster_sync_all();
-            else __syncthreads();
-            if (sh.flag) return;
+            // the kept ones in the vocabulary's order
+            const int m2 = pow2_at_least(m);
+            __syncthreads();
+            for (int i = tid; i < m2; i += kRowThreads) {
+                const unsigned long long e = list[i];
+                list[i] = i < m ? (e << 32) | (e >> 32) : 0ull;
+            }
+            sort_desc(list, m2);
+            sum = 0;
+#pragma unroll
+            for (int j = 0; j < kListPer; ++j) {
+                const int i = tid * kListPer + j;
+                w[j] = i < m ? weight(key_float((uint32_t)list[i]), s, tab) : 0ull;
+                sum += w[j];
+            }
+            unsigned long long run = block_scan_u64(sum, &sh, &total);
+            const unsigned long long target = share_floor(u, total);
+#pragma unroll
+            for (int j = 0; j < kListPer; ++j) {
+                const unsigned long long next = run + w[j];
+                if (target >= run && target < next) {   // one entry
+                    const unsigned long long e = list[tid * kListPer + j];
+                    put_sample(p, row, (int)~(uint32_t)(e >> 32), log_share(key_float((uint32_t)e), T, s, total), m);
+                }
+                run = next;
+            }
+            return;
         }
     }
 
-    // the general way: the cuts one after the other, over the whole row
-    Cut cut{kKeyNone, -1};
+    // over the whole row: the cuts one after the other, then the kept mass and the token in it
+    Cut cut{kKeyNone, INT_MIN};
     if (k > 0) cut = cut_count(c, kmax, k);
-    if (nucleus) {
-        const Cut by_k = cut;
-        const auto kept = [&](float x, uint32_t q, int i) { return by_k.keeps(q, i) ? weight(x, s, tab) : 0ull; };
-        const unsigned long long Z = cluster_sum(c, thread_sum(c, kept));
-        const unsigned long long want_mass = max(share_ceil(top_p, Z), 1ull);
-        unsigned long long above;
-        const uint32_t key = bisect_key(c, kmax, want_mass, kept, &above);
-        // ties at the border: the first of them that reach the mass
-        const unsigned long long w = weight(key_float(key), s, tab);
-        const unsigned long long ties = (want_mass - above + w - 1ull) / w;
-        uint32_t at;
-        locate(c, ties - 1ull, [=](float, uint32_t q, int i) { return q == key && by_k.keeps(q, i) ? 1ull : 0ull; },
-               &cut.idx, &at);
-        cut.key = key;
-    }
-    if (kminp > cut.key) cut = Cut{kminp - 1u, -1};
-    const Cut last = cut;
-    const unsigned long long count =
-        cluster_sum(c, thread_sum(c, [&](float, uint32_t q, int i) { return last.keeps(q, i) ? 1ull : 0ull; }));
-    const auto kept = [&](float x, uint32_t q, int i) { return last.keeps(q, i) ? weight(x, s, tab) : 0ull; };
-    const unsigned long long total = cluster_sum(c, thread_sum(c, kept));
+    if (nucleus) cut = cut_mass(c, s, tab, list, cut, top_p);
+    if (kminp > cut.key) cut = Cut{kminp, INT_MAX};
+    const KeptMass kept(s, tab, cut);
+    unsigned long long sum = 0;
+    int n = 0;
+    for (int v = c.wb + (tid & 31); v < c.we; v += 32) sum += kept.granule(c, v, n);
+    const unsigned long long count = cluster_sum(c, (unsigned long long)(unsigned)n);
+    const unsigned long long mine = block_sum_u64(sum, &sh);
+    const unsigned long long *slot = cluster_gather(c, mine);
+    unsigned long long total = 0;
+    for (int q = 0; q < c.C; ++q) total += slot[q];
     int id;
     uint32_t key;
-    locate(c, share_floor(u, total), kept, &id, &key);
+    locate(c, share_floor(u, total), kept, mine, slot, &id, &key);
     if (c.rank == 0 && tid == 0) put_sample(p, row, id, log_share(key_float(key), T, s, total), (long long)count);
 }
 
