@@ -20,14 +20,23 @@ namespace sats {
 namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
-constexpr int kMaxEntries = 1024;                                 // teacher entries of a row
-constexpr int kEntriesPer = kMaxEntries / kRowThreads;            // of a thread
-constexpr int kAhead = 8;                                         // granules in flight per thread on the way to shared memory
+constexpr int kMaxEntries = 1024;             // teacher entries of a row
+constexpr int kAhead = 8;                     // granules in flight per thread on the way to shared memory
 constexpr int kHashSlots = 2 * kMaxEntries;
-constexpr size_t kStageBytes = (size_t)kRowThreads * 16;          // one granule per thread
-constexpr size_t kMaxCache = 192 * 1024;                          // of a row's share in shared memory
+constexpr size_t kMaxCache = 192 * 1024;      // of a row's share in shared memory
+
+constexpr size_t kGradShare = 72 * 1024;      // of a row per CTA, where the cluster allows: several CTAs to an SM
+constexpr size_t kMaxSmem = kMaxCache + (size_t)kRowThreads * 16 + (size_t)kMaxEntries * 12;
 
 enum { kLoss = 0, kLossGrad = 1, kGrad = 2 };
+
+// Threads of a CTA, and CTAs that an SM is to hold.
+template <int MODE>
+struct Shape {
+    static constexpr int kThreads = MODE == kLoss ? 512 : 256;
+    static constexpr int kWarps = kThreads / 32;
+    static constexpr int kPerSm = MODE == kGrad ? 4 : MODE == kLossGrad ? 3 : 2;
+};
 
 struct DistillParams {
     const void *z;
@@ -46,6 +55,7 @@ struct DistillParams {
     int32_t *status;
     int cluster;              // CTAs of a row
     int cached;               // granules of a CTA's share that stay in shared memory
+    int work;                 // granules of shared memory behind them: the stage, and before that the hash table
 };
 
 // Sums of 2^((z - m) c) for one or two c, m the largest z so far.
@@ -111,26 +121,28 @@ __device__ __forceinline__ void run_add(RunSum<NT> &r, const uint4 (&v)[N], cons
     }
 }
 
+template <int WARPS>
 __device__ __forceinline__ float block_max(float v, float *part)
 {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
     if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
     __syncthreads();
-    v = part[threadIdx.x & (kRowWarps - 1)];
+    v = part[threadIdx.x & (WARPS - 1)];
 #pragma unroll
-    for (int o = kRowWarps / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+    for (int o = WARPS / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
     return v;
 }
 
+template <int WARPS>
 __device__ __forceinline__ float block_sum(float v, float *part)
 {
     v = warp_sum(v);
     if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
     __syncthreads();
-    v = part[threadIdx.x & (kRowWarps - 1)];
+    v = part[threadIdx.x & (WARPS - 1)];
 #pragma unroll
-    for (int o = kRowWarps / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    for (int o = WARPS / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
 
@@ -182,7 +194,7 @@ __device__ __forceinline__ void st_row_v4(void *p, const uint4 &v)
 // Stores the elements of the n granules from g0 on (their values in `stage`) to a row of the output that does not
 // lie on the granules' boundaries: whole 16-byte vectors of the output where these granules cover them, single
 // elements at both ends.  All threads of the CTA; `stage` complete before, free again after the call's end and a sync.
-template <bool F32>
+template <bool F32, int TH>
 __device__ __forceinline__ void store_shifted(char *out, const Row<F32> &r, int g0, int n, const uint4 *stage)
 {
     constexpr int E = RowElem<F32>::kPer, B = RowElem<F32>::kBytes;
@@ -191,7 +203,7 @@ __device__ __forceinline__ void store_shifted(char *out, const Row<F32> &r, int 
     const int64_t end = (int64_t)f0 + (int64_t)n * E, hi = end < r.V ? end : r.V;
     const int oh = (int)(reinterpret_cast<uintptr_t>(out) & 15u) / B;
     const int64_t o0 = (lo + oh) / E, o1 = (hi + oh + E - 1) / E;
-    for (int64_t o = o0 + threadIdx.x; o < o1; o += kRowThreads) {
+    for (int64_t o = o0 + threadIdx.x; o < o1; o += TH) {
         const int64_t e0 = o * E - oh;
         uint32_t w[4];
         const bool full = e0 >= lo && e0 + E <= hi;
@@ -221,62 +233,42 @@ __device__ __forceinline__ void store_shifted(char *out, const Row<F32> &r, int 
     }
 }
 
-// A row's entries, as the threads hold them: thread t has entries t and t + kRowThreads.
+// A row's entries in shared memory (of K each).
 struct Entries {
-    int i[kEntriesPer];       // -1: absent
-    float lq[kEntriesPer];    // log2 q
-    float q[kEntriesPer];
-    float z[kEntriesPer];     // the row's logit there
-    bool any;                 // the row has an entry with a share
+    int *i;       // -1: absent
+    float *lq;    // log2 q
+    float *z;     // the row's logit there
 };
 
-__device__ __forceinline__ void load_entries(Entries &e, const DistillParams &p, int row, float c, bool f32, float *part,
+// Fills them in; whether any entry has a share.  All threads; part: 2 WARPS floats.
+template <bool F32, int TH>
+__device__ __forceinline__ bool load_entries(const Entries &e, const DistillParams &p, int row, float c, float *part,
                                              bool report)
 {
     float gm = -INFINITY;
     bool nan = false;
-#pragma unroll
-    for (int u = 0; u < kEntriesPer; ++u) {
-        const int k = threadIdx.x + u * kRowThreads;
-        e.i[u] = -1;
-        e.lq[u] = -INFINITY;
-        e.q[u] = 0.f;
-        e.z[u] = 0.f;
-        if (k < p.K) {
-            const int i = p.idx[(size_t)row * p.K + k];
-            if (i >= 0 && i < p.V) {
-                e.i[u] = i;
-                e.lq[u] = p.val[(size_t)row * p.K + k];
-                e.z[u] = load_logit(p.z, (int64_t)row * p.ldz + i, f32);
-                gm = fmaxf(gm, e.lq[u]);
-                nan |= e.lq[u] != e.lq[u];
-            } else if (i >= p.V && report && p.status) {
-                atomicOr(p.status, kStatusBadToken);
-            }
-        }
+    for (int k = threadIdx.x; k < p.K; k += TH) {
+        const int i = p.idx[(size_t)row * p.K + k];
+        const bool there = i >= 0 && i < p.V;
+        const float g = there ? p.val[(size_t)row * p.K + k] : -INFINITY;
+        e.i[k] = there ? i : -1;
+        e.lq[k] = g;
+        e.z[k] = there ? load_logit(p.z, (int64_t)row * p.ldz + i, F32) : 0.f;
+        gm = fmaxf(gm, g);
+        nan |= g != g;
+        if (i >= p.V && report && p.status) atomicOr(p.status, kStatusBadToken);
     }
-    gm = block_max(gm, part);
-    e.any = __syncthreads_or(gm > -INFINITY || nan);
-    if (!e.any) {
-#pragma unroll
-        for (int u = 0; u < kEntriesPer; ++u) e.i[u] = -1;   // (entries of no weight at all are absent ones)
-        return;
-    }
+    gm = block_max<TH / 32>(gm, part);
+    if (!__syncthreads_or(gm > -INFINITY || nan)) return false;   // (entries of no weight at all are absent ones)
     float sum = 0.f;
-#pragma unroll
-    for (int u = 0; u < kEntriesPer; ++u) {
-        if (e.i[u] < 0) continue;
-        e.lq[u] = (e.lq[u] - gm) * c;
-        e.q[u] = exp2f(e.lq[u]);
-        sum += e.q[u];
+    for (int k = threadIdx.x; k < p.K; k += TH) {
+        const float l = (e.lq[k] - gm) * c;
+        e.lq[k] = l;
+        sum += exp2f(l);
     }
-    sum = block_sum(sum, part + kRowWarps);
-    const float l2 = log2f(sum), inv = 1.f / sum;
-#pragma unroll
-    for (int u = 0; u < kEntriesPer; ++u) {
-        e.lq[u] -= l2;
-        e.q[u] *= inv;
-    }
+    const float l2 = log2f(block_sum<TH / 32>(sum, part + TH / 32));
+    for (int k = threadIdx.x; k < p.K; k += TH) e.lq[k] -= l2;
+    return true;
 }
 
 // One row per cluster of p.cluster CTAs.
@@ -284,13 +276,13 @@ __device__ __forceinline__ void load_entries(Entries &e, const DistillParams &p,
 // not fit is read again); kGrad needs no sums, they come in lse_in.
 // NT: 2 where sums at tau and at 1 are both needed and differ, c[0] being tau's.
 template <bool F32, int MODE, int NT>
-__global__ void __launch_bounds__(kRowThreads, 2) distill_kernel(const DistillParams p)
+__global__ void __launch_bounds__(Shape<MODE>::kThreads, Shape<MODE>::kPerSm) distill_kernel(const DistillParams p)
 {
     extern __shared__ __align__(16) uint4 row_smem[];
-    __shared__ float part[4 * kRowWarps];
-    __shared__ float wsum[kRowWarps][4];
+    constexpr int TH = Shape<MODE>::kThreads, WARPS = Shape<MODE>::kWarps;
+    __shared__ float part[3 * WARPS];
+    __shared__ float wsum[WARPS][4];
     __shared__ __align__(16) float csum[kRowMaxCluster][4];
-    __shared__ int hash[MODE == kLoss ? 1 : kHashSlots];
     constexpr int E = RowElem<F32>::kPer, B = RowElem<F32>::kBytes;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int C = p.cluster, row = blockIdx.x / C;
@@ -310,6 +302,10 @@ __global__ void __launch_bounds__(kRowThreads, 2) distill_kernel(const DistillPa
     // whether output vectors lie on the same boundaries as the input's
     const bool same = MODE == kLoss || ((reinterpret_cast<uintptr_t>(out) - (uintptr_t)r.head * B) & 15u) == 0;
     uint4 *stage = row_smem + p.cached;
+    Entries ent;
+    ent.i = reinterpret_cast<int *>(stage + p.work);
+    ent.lq = reinterpret_cast<float *>(ent.i + p.K);
+    ent.z = ent.lq + p.K;
     if (label < 0 || bad) {
         if (rank == 0 && tid == 0) {
             if (MODE != kGrad && p.loss) p.loss[row] = 0.f;
@@ -319,10 +315,10 @@ __global__ void __launch_bounds__(kRowThreads, 2) distill_kernel(const DistillPa
             const uint4 zero = make_uint4(0, 0, 0, 0);
             if (!same) stage[tid] = zero;
             __syncthreads();
-            for (int v0 = 0; v0 < n; v0 += kRowThreads) {
+            for (int v0 = 0; v0 < n; v0 += TH) {
                 const int g = gb + v0 + tid;
                 if (!same) {
-                    store_shifted<F32>(out, r, gb + v0, min(kRowThreads, n - v0), stage);
+                    store_shifted<F32, TH>(out, r, gb + v0, min(TH, n - v0), stage);
                 } else if (v0 + tid < n) {
                     if (r.whole(g)) st_row_v4(out + (int64_t)r.first(g) * B, zero);
                     else
@@ -338,18 +334,17 @@ __global__ void __launch_bounds__(kRowThreads, 2) distill_kernel(const DistillPa
     // start the row on its way first: the entries are small
     if constexpr (MODE == kLossGrad) {
         for (int i = 0; i < kAhead; ++i) {
-            const int v = tid + i * kRowThreads;
+            const int v = tid + i * TH;
             if (v < min(n, p.cached)) fetch_granule<F32>(r, gb + v, row_smem + v);
             cp_async_commit();
         }
     }
-    Entries ent;
-    ent.any = false;
-    const bool soft = p.alpha > 0.f && p.K > 0;
-    if (soft && (MODE != kLoss || rank == 0)) load_entries(ent, p, row, ctau, F32, part, rank == 0);
+    bool any = false;   // the row has an entry with a share
+    if (p.alpha > 0.f && p.K > 0 && (MODE != kLoss || rank == 0))
+        any = load_entries<F32, TH>(ent, p, row, ctau, part, rank == 0);
     const bool hard = p.alpha < 1.f && p.labels;
     const float zy = hard ? load_logit(p.z, (int64_t)row * p.ldz + label, F32) : 0.f;
-    const float wt = ent.any ? p.alpha : 0.f, wh = hard ? 1.f - p.alpha : 0.f;
+    const float wt = any ? p.alpha : 0.f, wh = hard ? 1.f - p.alpha : 0.f;
 
     float off = 0.f, inv[NT];   // 2^((z - off) c) * inv = probability; MODE kGrad: see there
     if constexpr (MODE != kGrad) {
@@ -360,9 +355,9 @@ __global__ void __launch_bounds__(kRowThreads, 2) distill_kernel(const DistillPa
         int done = 0;
         if constexpr (MODE == kLossGrad) {
             const int nc = min(n, p.cached);
-            for (int i = 0; tid + i * kRowThreads < nc; ++i) {
+            for (int i = 0; tid + i * TH < nc; ++i) {
                 cp_async_wait<kAhead - 1>();
-                const int v = tid + i * kRowThreads, next = v + kAhead * kRowThreads;
+                const int v = tid + i * TH, next = v + kAhead * TH;
                 const uint4 one[1] = {row_smem[v]};
                 if (next < nc) fetch_granule<F32>(r, gb + next, row_smem + next);
                 cp_async_commit();
@@ -371,13 +366,13 @@ __global__ void __launch_bounds__(kRowThreads, 2) distill_kernel(const DistillPa
             done = nc;
         }
         int v = done + tid;
-        for (; v + 3 * kRowThreads < n; v += 4 * kRowThreads) {
+        for (; v + 3 * TH < n; v += 4 * TH) {
             uint4 x[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) x[k] = load_granule<F32>(r, gb + v + k * kRowThreads);
+            for (int k = 0; k < 4; ++k) x[k] = load_granule<F32>(r, gb + v + k * TH);
             run_add<F32, NT, 4>(sum, x, c);
         }
-        for (; v < n; v += kRowThreads) {
+        for (; v < n; v += TH) {
             const uint4 one[1] = {load_granule<F32>(r, gb + v)};
             run_add<F32, NT, 1>(sum, one, c);
         }
@@ -396,11 +391,11 @@ __global__ void __launch_bounds__(kRowThreads, 2) distill_kernel(const DistillPa
             for (int t = 0; t < NT; ++t) wsum[warp][1 + t] = sum.s[t];
         }
         __syncthreads();
-        sum.m = wsum[lane & (kRowWarps - 1)][0];
+        sum.m = wsum[lane & (WARPS - 1)][0];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) sum.s[t] = wsum[lane & (kRowWarps - 1)][1 + t];
+        for (int t = 0; t < NT; ++t) sum.s[t] = wsum[lane & (WARPS - 1)][1 + t];
 #pragma unroll
-        for (int o = kRowWarps / 2; o > 0; o >>= 1) {
+        for (int o = WARPS / 2; o > 0; o >>= 1) {
             RunSum<NT> other;
             other.m = __shfl_xor_sync(0xffffffffu, sum.m, o);
 #pragma unroll
@@ -431,12 +426,12 @@ __global__ void __launch_bounds__(kRowThreads, 2) distill_kernel(const DistillPa
         }
         if (rank == 0) {
             float kd = 0.f;
-            if (ent.any) {
-#pragma unroll
-                for (int u = 0; u < kEntriesPer; ++u)
-                    if (ent.i[u] >= 0 && !(ent.q[u] == 0.f))   // (0 log 0 = 0)
-                        kd += ent.q[u] * (ent.lq[u] - fmaf(ent.z[u] - off, ctau, -l2[0]));
-                kd = block_sum(kd, part + 2 * kRowWarps);
+            if (any) {
+                for (int o = tid; o < p.K; o += TH) {
+                    const float q = exp2f(ent.lq[o]);
+                    if (!(q == 0.f)) kd += q * (ent.lq[o] - fmaf(ent.z[o] - off, ctau, -l2[0]));   // (0 log 0 = 0)
+                }
+                kd = block_sum<WARPS>(kd, part + 2 * WARPS);
             }
             if (tid == 0) {
                 constexpr int H = NT - 1;   // the sums at temperature 1
@@ -493,43 +488,54 @@ __global__ void __launch_bounds__(kRowThreads, 2) distill_kernel(const DistillPa
             return unpack2(d);
         };
         const auto grad = [&](float x) { return grad2(pack2(x, x)).x; };
-        for (int v0 = 0; v0 < n; v0 += kRowThreads) {
-            const int v = v0 + tid, g = gb + v;
-            uint4 o = make_uint4(0, 0, 0, 0);
-            if (v < n) {
-                const uint4 x = MODE == kLossGrad && v < p.cached ? row_smem[v] : load_granule<F32>(r, g);
-                f32x2 f[E / 2];
-                float2 d[E / 2];
-                granule_pairs<F32>(x, f);
+        const auto one = [&](const uint4 &x) {
+            f32x2 f[E / 2];
+            float2 d[E / 2];
+            granule_pairs<F32>(x, f);
 #pragma unroll
-                for (int j = 0; j < E / 2; ++j) d[j] = grad2(f[j]);
-                o = pack_granule<F32>(d);
+            for (int j = 0; j < E / 2; ++j) d[j] = grad2(f[j]);
+            return pack_granule<F32>(d);
+        };
+        const auto put = [&](int g, const uint4 &o) {
+            if (r.whole(g)) st_row_v4(out + (int64_t)r.first(g) * B, o);
+            else
+#pragma unroll
+                for (int j = 0; j < E; ++j)
+                    if (r.inside(r.first(g) + j)) store_elem<F32>(out, r.first(g) + j, granule_elem<F32>(o, j));
+        };
+        const auto fetched = [&](int v) {
+            return MODE == kLossGrad && v < p.cached ? row_smem[v] : load_granule<F32>(r, gb + v);
+        };
+        if (same) {
+            constexpr int U = MODE == kGrad ? 4 : 1;   // loads in flight per thread
+            int v = tid;
+            for (; v + (U - 1) * TH < n; v += U * TH) {
+                uint4 x[U];
+#pragma unroll
+                for (int k = 0; k < U; ++k) x[k] = fetched(v + k * TH);
+#pragma unroll
+                for (int k = 0; k < U; ++k) put(gb + v + k * TH, one(x[k]));
             }
-            if (same) {
-                if (v < n) {
-                    if (r.whole(g)) st_row_v4(out + (int64_t)r.first(g) * B, o);
-                    else
-#pragma unroll
-                        for (int j = 0; j < E; ++j)
-                            if (r.inside(r.first(g) + j)) store_elem<F32>(out, r.first(g) + j, granule_elem<F32>(o, j));
-                }
-            } else {
-                stage[tid] = o;
+            for (; v < n; v += TH) put(gb + v, one(fetched(v)));
+        } else {
+            for (int v0 = 0; v0 < n; v0 += TH) {
+                if (v0 + tid < n) stage[tid] = one(fetched(v0 + tid));
                 __syncthreads();
-                store_shifted<F32>(out, r, gb + v0, min(kRowThreads, n - v0), stage);
+                store_shifted<F32, TH>(out, r, gb + v0, min(TH, n - v0), stage);
                 __syncthreads();
             }
         }
         // the targets' places, each computed as a whole and rounded once, after everybody's stores
         const int lo = max(0, r.first(gb)), hi = (int)min((int64_t)p.V, (int64_t)r.first(gb) + (int64_t)n * E);
         bool twice = false;
-        if (ent.any) {
+        int *hash = reinterpret_cast<int *>(row_smem);   // (over the cached row, which nobody needs any more)
+        if (any) {
             // does an index occur twice?  (open addressing; as many slots as twice the entries)
-            for (int i = tid; i < kHashSlots; i += kRowThreads) hash[i] = -1;
             __syncthreads();
-#pragma unroll
-            for (int u = 0; u < kEntriesPer; ++u) {
-                const int i = ent.i[u];
+            for (int i = tid; i < kHashSlots; i += TH) hash[i] = -1;
+            __syncthreads();
+            for (int o = tid; o < p.K; o += TH) {
+                const int i = ent.i[o];
                 if (i < lo || i >= hi) continue;
                 unsigned slot = ((unsigned)i * 2654435761u) >> 21;
                 static_assert(kHashSlots == 2048, "the shift above");
@@ -542,50 +548,33 @@ __global__ void __launch_bounds__(kRowThreads, 2) distill_kernel(const DistillPa
             }
         }
         twice = __syncthreads_or(twice);
-        if (ent.any) {
-            if (twice) {
-                // entries and their shares where every thread finds them: an index's first entry adds them in order
-                int *all = hash;
-                float *share = reinterpret_cast<float *>(hash + kMaxEntries);
-#pragma unroll
-                for (int u = 0; u < kEntriesPer; ++u) {
-                    all[tid + u * kRowThreads] = ent.i[u];
-                    share[tid + u * kRowThreads] = ent.q[u];
-                }
-                __syncthreads();
-#pragma unroll
-                for (int u = 0; u < kEntriesPer; ++u) {
-                    const int k = tid + u * kRowThreads;
-                    if (ent.i[u] < lo || ent.i[u] >= hi) continue;
-                    float q = 0.f;
-                    bool first = true;
-                    for (int o = 0; o < p.K; ++o)
-                        if (all[o] == ent.i[u]) {
-                            if (o < k) first = false;
-                            q += share[o];
-                        }
-                    ent.q[u] = q;
-                    if (!first) ent.i[u] = -1;
-                }
-            }
-#pragma unroll
-            for (int u = 0; u < kEntriesPer; ++u) {
-                const int i = ent.i[u];
+        bool labelled = false;
+        if (any)
+            for (int o = tid; o < p.K; o += TH) {
+                const int i = ent.i[o];
                 if (i < lo || i >= hi) continue;
-                float d = fmaf(-up * wt * p.tau, ent.q[u], grad(ent.z[u]));
-                if (hard && i == label) d -= up * wh;
+                float q = exp2f(ent.lq[o]);
+                if (twice) {   // an index's first entry adds them all, in their order
+                    q = 0.f;
+                    bool first = true;
+                    for (int k = 0; k < p.K; ++k)
+                        if (ent.i[k] == i) {
+                            first &= k >= o;
+                            q += exp2f(ent.lq[k]);
+                        }
+                    if (!first) continue;
+                }
+                float d = fmaf(-up * wt * p.tau, q, grad(ent.z[o]));
+                if (hard && i == label) {
+                    d -= up * wh;
+                    labelled = true;
+                }
                 store_elem<F32>(out, i, F32 ? __float_as_uint(d) : bf16_bits(d, 0.f) & 0xffffu);
             }
-        }
-        if (hard && label >= lo && label < hi) {
-            // the label, where it is not one of the entries
-            bool mine = false;
-#pragma unroll
-            for (int u = 0; u < kEntriesPer; ++u) mine |= ent.any && ent.i[u] == label;
-            if (!__syncthreads_or(mine) && tid == 0) {
-                const float d = grad(zy) - up * wh;
-                store_elem<F32>(out, label, F32 ? __float_as_uint(d) : bf16_bits(d, 0.f) & 0xffffu);
-            }
+        // the label, where it is not one of the entries
+        if (hard && label >= lo && label < hi && !__syncthreads_or(labelled) && tid == 0) {
+            const float d = grad(zy) - up * wh;
+            store_elem<F32>(out, label, F32 ? __float_as_uint(d) : bf16_bits(d, 0.f) & 0xffffu);
         }
     }
 }
@@ -607,23 +596,30 @@ template <bool F32, int MODE, int NT>
 cudaError_t launch_distill(DistillParams p, cudaStream_t st)
 {
     const int64_t bytes = (int64_t)p.V * RowElem<F32>::kBytes;
-    p.cluster = row_cluster(p.T, bytes, MODE == kLossGrad ? 64 * 1024 : 0);
-    p.cached = 0;
-    size_t smem = 0;
+    p.cluster = row_cluster(p.T, bytes, MODE == kLossGrad ? kGradShare : 0);
+    p.cached = p.work = 0;
     if (MODE == kLossGrad) {
         const size_t share = al16((size_t)((bytes + 32 + p.cluster - 1) / p.cluster) + 32);
         p.cached = (int)((share < kMaxCache ? share : kMaxCache) / 16);
     }
-    if (MODE != kLoss) smem = (size_t)p.cached * 16 + kStageBytes;
+    if (MODE != kLoss) {
+        // a stage where the gradient's rows do not lie on the logits' 16-byte boundaries; room for the hash table
+        constexpr int B = RowElem<F32>::kBytes;
+        const bool same = (reinterpret_cast<uintptr_t>(p.z) - reinterpret_cast<uintptr_t>(p.d)) % 16 == 0 &&
+                          (p.T == 1 || (p.ldz - p.ldd) * B % 16 == 0);
+        p.work = same ? 0 : Shape<MODE>::kThreads;
+        const int least = p.K > 0 ? kHashSlots * 4 / 16 : 0;
+        if (p.cached + p.work < least) p.work = least - p.cached;
+    }
+    const size_t smem = ((size_t)p.cached + p.work) * 16 + (size_t)p.K * 12;
     auto kern = distill_kernel<F32, MODE, NT>;
-    if (smem > 32 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                   (int)(kMaxCache + kStageBytes));
+    if (smem > 40 * 1024) {
+        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMaxSmem);
         if (e != cudaSuccess) return e;
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)p.T * (unsigned)p.cluster);
-    cfg.blockDim = dim3(kRowThreads);
+    cfg.blockDim = dim3(Shape<MODE>::kThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
