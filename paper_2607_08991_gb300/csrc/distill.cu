@@ -21,22 +21,10 @@ namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr int kMaxEntries = 1024;             // teacher entries of a row
-constexpr int kAhead = 8;                     // granules in flight per thread on the way to shared memory
-constexpr int kHashSlots = 2 * kMaxEntries;
-constexpr size_t kMaxCache = 192 * 1024;      // of a row's share in shared memory
-
-constexpr size_t kGradShare = 72 * 1024;      // of a row per CTA, where the cluster allows: several CTAs to an SM
-constexpr size_t kMaxSmem = kMaxCache + (size_t)kRowThreads * 16 + (size_t)kMaxEntries * 12;
-
-enum { kLoss = 0, kLossGrad = 1, kGrad = 2 };
-
-// Threads of a CTA, and CTAs that an SM is to hold.
-template <int MODE>
-struct Shape {
-    static constexpr int kThreads = MODE == kLoss ? 512 : 256;
-    static constexpr int kWarps = kThreads / 32;
-    static constexpr int kPerSm = MODE == kGrad ? 4 : MODE == kLossGrad ? 3 : 2;
-};
+constexpr size_t kMaxCache = 180 * 1024;      // of a row's share in shared memory
+constexpr size_t kMaxSmem = kSmemPerCta - 2 * 1024;   // dynamic: a row's share, a stage, two tables of entries
+constexpr size_t kStepShare = 72 * 1024;      // of a row per CTA, where the cluster allows: several CTAs to an SM
+constexpr int kLossThreads = 512, kGradThreads = 256, kStepThreads = 256, kStepPerSm = 3;
 
 struct DistillParams {
     const void *z;
@@ -55,7 +43,8 @@ struct DistillParams {
     int32_t *status;
     int cluster;              // CTAs of a row
     int cached;               // granules of a CTA's share that stay in shared memory
-    int work;                 // granules of shared memory behind them: the stage, and before that the hash table
+    int work;                 // granules of shared memory behind them, where the gradient's rows lie otherwise
+    int slots;                // of the table of entries' indices (a power of two)
 };
 
 // Sums of 2^((z - m) c) for one or two c, m the largest z so far.
@@ -64,20 +53,6 @@ struct RunSum {
     float m;
     float s[NT];
 };
-
-template <int NT>
-__device__ __forceinline__ void run_join(RunSum<NT> &a, const RunSum<NT> &b, const float (&c)[NT])
-{
-    const float m = fmaxf(a.m, b.m);
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        // (a side that has seen nothing above -inf has the sum 0, or NaN if it has seen one)
-        const float fa = a.m == m ? 1.f : ex2_approx((a.m - m) * c[t]);
-        const float fb = b.m == m ? 1.f : ex2_approx((b.m - m) * c[t]);
-        a.s[t] = a.s[t] * fa + b.s[t] * fb;
-    }
-    a.m = m;
-}
 
 // What is subtracted from logits whose maximum is m (-inf - (-inf) would be NaN).
 __device__ __forceinline__ float offset_of(float m) { return m == -INFINITY ? 0.f : m; }
@@ -121,31 +96,29 @@ __device__ __forceinline__ void run_add(RunSum<NT> &r, const uint4 (&v)[N], cons
     }
 }
 
-template <int WARPS>
-__device__ __forceinline__ float block_max(float v, float *part)
+// The largest of the warp's values (no NaN among them): as whole numbers that order like them.
+__device__ __forceinline__ float warp_max(float v)
 {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
-    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
-    __syncthreads();
-    v = part[threadIdx.x & (WARPS - 1)];
-#pragma unroll
-    for (int o = WARPS / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
-    return v;
+    const int b = __float_as_int(v);
+    const int m = __reduce_max_sync(0xffffffffu, b ^ ((b >> 31) & 0x7fffffff));
+    return __int_as_float(m ^ ((m >> 31) & 0x7fffffff));
 }
 
-template <int WARPS>
-__device__ __forceinline__ float block_sum(float v, float *part)
+// Joins the sums of N lanes (a power of two), each lane's own in a warp's first N lanes or repeated every N lanes:
+// brings them to the largest maximum, then adds.
+template <int NT>
+__device__ __forceinline__ void warp_join(RunSum<NT> &sum, const float (&c)[NT], int N)
 {
-    v = warp_sum(v);
-    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
-    __syncthreads();
-    v = part[threadIdx.x & (WARPS - 1)];
+    const float m = warp_max(sum.m);
 #pragma unroll
-    for (int o = WARPS / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    return v;
+    for (int t = 0; t < NT; ++t) {
+        // (a lane that has seen nothing above -inf has the sum 0, or NaN if it has seen one)
+        float v = sum.s[t] * (sum.m == m ? 1.f : ex2_approx((sum.m - m) * c[t]));
+        for (int o = N / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        sum.s[t] = v;
+    }
+    sum.m = m;
 }
-
 __device__ __forceinline__ float load_logit(const void *z, int64_t at, bool f32)
 {
     if (f32) return reinterpret_cast<const volatile float *>(z)[at];
@@ -236,347 +209,658 @@ __device__ __forceinline__ void store_shifted(char *out, const Row<F32> &r, int 
 // A row's entries in shared memory (of K each).
 struct Entries {
     int *i;       // -1: absent
-    float *lq;    // log2 q
+    float *g;     // the teacher's value, -inf where absent
     float *z;     // the row's logit there
+
+    __device__ __forceinline__ Entries(void *at, int K)
+        : i(reinterpret_cast<int *>(at)), g(reinterpret_cast<float *>(i + K)), z(g + K)
+    {
+    }
 };
 
-// Fills them in; whether any entry has a share.  All threads; part: 2 WARPS floats.
-template <bool F32, int TH>
-__device__ __forceinline__ bool load_entries(const Entries &e, const DistillParams &p, int row, float c, float *part,
-                                             bool report)
+// What makes shares of the values: log2 q = (g - m) c - l2, m their maximum, l2 = log2 sum 2^((g - m) c).
+struct Shares {
+    float m, c, l2;
+    __device__ __forceinline__ float log2_of(float g) const { return fmaf(g - m, c, -l2); }
+};
+
+// Indices seen, to tell whether one occurs twice: open addressing, at least twice as many slots as entries.
+struct Seen {
+    int *slot;
+    unsigned mask;
+    __device__ __forceinline__ bool before(int i) const
+    {
+        unsigned at = ((unsigned)i * 2654435761u >> 16) & mask;
+        for (;;) {
+            const int was = atomicCAS(slot + at, -1, i);
+            if (was == -1) return false;
+            if (was == i) return true;
+            at = (at + 1) & mask;
+        }
+    }
+};
+
+// Facts about a row's entries that its threads join.
+enum { kEntryTwice = 1, kEntryNan = 2, kEntryLabel = 4 };
+
+// One entry of a row: its index, its value and (within [lo, hi)) its logit to shared memory.  *gm: the largest value of
+// the thread's.
+template <bool F32>
+__device__ __forceinline__ void put_entry(const Entries &e, const DistillParams &p, int row, int k, int i, float g,
+                                          int label, int lo, int hi, bool report, float *gm, int *facts)
 {
-    float gm = -INFINITY;
-    bool nan = false;
-    for (int k = threadIdx.x; k < p.K; k += TH) {
-        const int i = p.idx[(size_t)row * p.K + k];
-        const bool there = i >= 0 && i < p.V;
-        const float g = there ? p.val[(size_t)row * p.K + k] : -INFINITY;
-        e.i[k] = there ? i : -1;
-        e.lq[k] = g;
-        e.z[k] = there ? load_logit(p.z, (int64_t)row * p.ldz + i, F32) : 0.f;
-        gm = fmaxf(gm, g);
-        nan |= g != g;
-        if (i >= p.V && report && p.status) atomicOr(p.status, kStatusBadToken);
+    const bool there = i >= 0 && i < p.V;
+    e.i[k] = there ? i : -1;
+    e.g[k] = there ? g : -INFINITY;
+    if (i >= lo && i < hi) e.z[k] = load_logit(p.z, (int64_t)row * p.ldz + i, F32);
+    if (there) {
+        *gm = fmaxf(*gm, g);
+        *facts |= (g != g ? kEntryNan : 0) | (i == label ? kEntryLabel : 0);
     }
-    gm = block_max<TH / 32>(gm, part);
-    if (!__syncthreads_or(gm > -INFINITY || nan)) return false;   // (entries of no weight at all are absent ones)
-    float sum = 0.f;
-    for (int k = threadIdx.x; k < p.K; k += TH) {
-        const float l = (e.lq[k] - gm) * c;
-        e.lq[k] = l;
-        sum += exp2f(l);
-    }
-    const float l2 = log2f(block_sum<TH / 32>(sum, part + TH / 32));
-    for (int k = threadIdx.x; k < p.K; k += TH) e.lq[k] -= l2;
-    return true;
+    if (i >= p.V && report && p.status) atomicOr(p.status, kStatusBadToken);
 }
 
-// One row per cluster of p.cluster CTAs.
-// MODE kLoss reads the row once; kLossGrad keeps it in shared memory between the sums and the gradient (what does
-// not fit is read again); kGrad needs no sums, they come in lse_in.
-// NT: 2 where sums at tau and at 1 are both needed and differ, c[0] being tau's.
-template <bool F32, int MODE, int NT>
-__global__ void __launch_bounds__(Shape<MODE>::kThreads, Shape<MODE>::kPerSm) distill_kernel(const DistillParams p)
+// A warp's part of the row's shares, from its threads' own entries and their largest value: {maximum, sum, facts}.
+template <int TH>
+__device__ __forceinline__ float4 warp_shares(const Entries &e, int K, float c, float gm, int facts)
 {
-    extern __shared__ __align__(16) uint4 row_smem[];
-    constexpr int TH = Shape<MODE>::kThreads, WARPS = Shape<MODE>::kWarps;
-    __shared__ float part[3 * WARPS];
-    __shared__ float wsum[WARPS][4];
-    __shared__ __align__(16) float csum[kRowMaxCluster][4];
-    constexpr int E = RowElem<F32>::kPer, B = RowElem<F32>::kBytes;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int C = p.cluster, row = blockIdx.x / C;
-    const unsigned rank = blockIdx.x % C;
-    const Row<F32> r(p.z, row, p.ldz, p.V);
-    const int per = (r.G + C - 1) / C, gb = min(r.G, (int)rank * per), n = min(r.G - gb, per);
-    const float ctau = kLog2e / p.tau;
-    float c[NT];
+    gm = warp_max(gm);
+    const float off = offset_of(gm);
+    float sum = 0.f;
+    for (int k = threadIdx.x; k < K; k += TH) sum += exp2f((e.g[k] - off) * c);
+    return make_float4(gm, warp_sum(sum), __int_as_float((int)__reduce_or_sync(0xffffffffu, facts)), 0.f);
+}
+
+// The CTA's, from all warps' parts (in shared memory; a barrier before).  Returns whether any entry has a share
+// (entries of no weight at all are absent ones).
+template <int WARPS>
+__device__ __forceinline__ bool join_shares(const float4 *part, float c, Shares *s, int *facts)
+{
+    const float4 v = part[threadIdx.x & (WARPS - 1)];
+    s->m = warp_max(v.x);
+    s->c = c;
+    float sum = v.y * (v.x == s->m ? 1.f : exp2f((v.x - s->m) * c));
+#pragma unroll
+    for (int o = WARPS / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    s->l2 = log2f(sum);
+    *facts = (int)__reduce_or_sync(0xffffffffu, __float_as_int(v.z));
+    return s->m > -INFINITY || (*facts & kEntryNan);
+}
+
+// All of it at once, with one barrier.
+template <bool F32, int TH>
+__device__ __forceinline__ bool load_entries(const Entries &e, const DistillParams &p, int row, int label, int lo,
+                                             int hi, float c, float4 *part, bool report, Shares *s, int *facts)
+{
+    float gm = -INFINITY;
+    int mine = 0;
+    for (int k = threadIdx.x; k < p.K; k += TH)
+        put_entry<F32>(e, p, row, k, p.idx[(size_t)row * p.K + k], p.val[(size_t)row * p.K + k], label, lo, hi,
+                       report, &gm, &mine);
+    const float4 w = warp_shares<TH>(e, p.K, c, gm, mine);
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = w;
+    __syncthreads();
+    return join_shares<TH / 32>(part, c, s, facts);
+}
+
+// A thread's part of KD / (tau^2 ln 2), l2 = log2 of the row's sum at tau.
+template <int TH>
+__device__ __forceinline__ float kd_part(const Entries &e, int K, const Shares &s, float off, float l2)
+{
+    float kd = 0.f;
+    for (int o = threadIdx.x; o < K; o += TH) {
+        const float lq = s.log2_of(e.g[o]), q = exp2f(lq);
+        if (!(q == 0.f)) kd += q * (lq - fmaf(e.z[o] - off, s.c, -l2));   // (0 log 0 = 0)
+    }
+    return kd;
+}
+
+// d_j = A 2^(x_0) + B 2^(x_1), less the targets; with one exponential (NT 1) it is one of the two, or both at tau = 1
+// in A.  From sums, x = (z - off) c; from log-sum-exps, x = (z / tau - lse) log2 e: the difference comes first, it is
+// exact where the probability is large.  A coefficient of 0 is exactly 0, also for a row that has no sum.
+template <int NT, bool LSE>
+struct GradFn {
+    float A, B, s0, a0, m0, a1;
+    __device__ __forceinline__ float2 operator()(f32x2 x) const
+    {
+        const f32x2 x0 = LSE ? ffma2(x, pack2(s0, s0), pack2(a0, a0)) : fadd2(x, pack2(a0, a0));
+        const float2 e0 = unpack2(fmul2(x0, pack2(m0, m0)));
+        f32x2 d = fmul2(pack2(A, A), pack2(ex2_approx(e0.x), ex2_approx(e0.y)));
+        if constexpr (NT == 2) {
+            const f32x2 x1 = LSE ? fadd2(x, pack2(a1, a1)) : x0;
+            const float2 e1 = unpack2(fmul2(x1, pack2(kLog2e, kLog2e)));
+            d = ffma2(pack2(B, B), pack2(ex2_approx(e1.x), ex2_approx(e1.y)), d);
+        }
+        return unpack2(d);
+    }
+    __device__ __forceinline__ float operator()(float x) const { return (*this)(pack2(x, x)).x; }
+    template <bool F32>
+    __device__ __forceinline__ uint4 granule(const uint4 &x) const
+    {
+        constexpr int P = RowElem<F32>::kPer / 2;
+        f32x2 f[P];
+        float2 d[P];
+        granule_pairs<F32>(x, f);
+#pragma unroll
+        for (int j = 0; j < P; ++j) d[j] = (*this)(f[j]);
+        return pack_granule<F32>(d);
+    }
+};
+
+// Stores granule g of the gradient's row `out`, which lies on the same 16-byte boundaries as the logits' row.
+// (The ends of a row out of line: their stores would be executed without effect for every granule otherwise.)
+template <bool F32>
+__device__ __noinline__ void put_edge_granule(char *out, int first, int V, uint4 o)
+{
+    constexpr int E = RowElem<F32>::kPer;
+#pragma unroll
+    for (int j = 0; j < E; ++j)
+        if ((unsigned)(first + j) < (unsigned)V) store_elem<F32>(out, first + j, granule_elem<F32>(o, j));
+}
+template <bool F32>
+__device__ __forceinline__ void put_granule(char *out, const Row<F32> &r, int g, const uint4 &o)
+{
+    if (r.whole(g)) st_row_v4(out + (int64_t)r.first(g) * RowElem<F32>::kBytes, o);
+    else put_edge_granule<F32>(out, r.first(g), r.V, o);
+}
+
+// The places of the entries and the label within [lo, hi), each computed as a whole and rounded once; after everybody's
+// stores and a barrier.  up: the row's upstream gradient, wt, wh: the terms' shares (wt 0: no entries).
+template <bool F32, int TH, typename G>
+__device__ __forceinline__ void put_targets(char *out, const DistillParams &p, const Entries &e, const Shares &s,
+                                            int facts, int lo, int hi, float up, float wt, float wh, int label,
+                                            float zy, const G &grad)
+{
+    if (wt > 0.f)
+        for (int o = threadIdx.x; o < p.K; o += TH) {
+            const int i = e.i[o];
+            if (i < lo || i >= hi) continue;
+            float q = exp2f(s.log2_of(e.g[o]));
+            if (facts & kEntryTwice) {   // an index's first entry adds them all, in their order
+                q = 0.f;
+                bool first = true;
+                for (int k = 0; k < p.K; ++k)
+                    if (e.i[k] == i) {
+                        first &= k >= o;
+                        q += exp2f(s.log2_of(e.g[k]));
+                    }
+                if (!first) continue;
+            }
+            float d = fmaf(-up * wt * p.tau, q, grad(e.z[o]));
+            if (i == label) d -= up * wh;
+            store_elem<F32>(out, i, F32 ? __float_as_uint(d) : bf16_bits(d, 0.f) & 0xffffu);
+        }
+    // the label, where it is not one of the entries
+    if (threadIdx.x == 0 && wh > 0.f && label >= lo && label < hi && !(wt > 0.f && (facts & kEntryLabel))) {
+        const float d = grad(zy) - up * wh;
+        store_elem<F32>(out, label, F32 ? __float_as_uint(d) : bf16_bits(d, 0.f) & 0xffffu);
+    }
+}
+
+template <int NT>
+__device__ __forceinline__ void put_sum(float (&at)[4], const RunSum<NT> &sum)
+{
+    at[0] = sum.m;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) at[1 + t] = sum.s[t];
+}
+template <int NT>
+__device__ __forceinline__ RunSum<NT> get_sum(const float (&at)[4])
+{
+    RunSum<NT> sum;
+    sum.m = at[0];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) sum.s[t] = at[1 + t];
+    return sum;
+}
+template <int NT>
+__device__ __forceinline__ RunSum<NT> empty_sum()
+{
+    RunSum<NT> sum;
+    sum.m = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) sum.s[t] = 0.f;
+    return sum;
+}
+
+// Adds the granules from v0 on of a CTA's n, from memory, to a thread's sum.
+template <bool F32, int NT, int TH>
+__device__ __forceinline__ void stream_sum(RunSum<NT> &sum, const Row<F32> &r, int gb, int v0, int n, const float (&c)[NT])
+{
+    int v = v0 + threadIdx.x;
+    for (; v + 3 * TH < n; v += 4 * TH) {
+        uint4 x[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] = load_granule<F32>(r, gb + v + k * TH);
+        run_add<F32, NT, 4>(sum, x, c);
+    }
+    for (; v < n; v += TH) {
+        const uint4 one[1] = {load_granule<F32>(r, gb + v)};
+        run_add<F32, NT, 1>(sum, one, c);
+    }
+}
+
+// The exponents' factors: c[0] is tau's, c[1] (NT 2) that of temperature 1.
+template <int NT>
+__device__ __forceinline__ void set_factors(float (&c)[NT], const DistillParams &p, float ctau)
+{
     c[0] = NT == 2 || p.alpha > 0.f ? ctau : kLog2e;
     if constexpr (NT == 2) c[1] = kLog2e;
+}
 
-    // an ignored row: nothing of it is read
+// The loss of a row from its sum, by one thread; kd: KD / (tau^2 ln 2).
+template <int NT>
+__device__ __forceinline__ void put_loss(const DistillParams &p, int row, const float (&l2)[NT], float off, float kd,
+                                         float wt, float wh, float zy)
+{
+    constexpr int H = NT - 1;   // the sums at temperature 1
+    float loss = 0.f;
+    if (wt > 0.f) loss += wt * p.tau * p.tau * kLn2 * kd;
+    if (wh > 0.f) loss += wh * fmaf(kLn2, l2[H], off - zy);
+    p.loss[row] = loss;
+    if (p.lse) {
+        p.lse[2 * (size_t)row] = fmaf(kLn2, l2[0], off / p.tau);   // (NT 1 is tau = 1 here)
+        p.lse[2 * (size_t)row + 1] = fmaf(kLn2, l2[H], off);
+    }
+}
+
+// A CTA's run of a row's granules: first, number.
+template <bool F32>
+__device__ __forceinline__ int2 run_of(const Row<F32> &r, int C, int rank)
+{
+    const int per = (r.G + C - 1) >> (31 - __clz(C)), gb = min(r.G, rank * per);   // (C is a power of two)
+    return make_int2(gb, min(r.G - gb, per));
+}
+
+// The granules [x, y) of a run that are all row (the row's first and last may not be).
+template <bool F32>
+__device__ __forceinline__ int2 whole_of(const Row<F32> &r, int2 run)
+{
+    const int x = run.x == 0 && run.y > 0 && !r.whole(0) ? 1 : 0;
+    const int y = run.x + run.y == r.G && run.y > 0 && !r.whole(r.G - 1) ? run.y - 1 : run.y;
+    return make_int2(x, y);
+}
+
+// ------------------------------------------------------------------ the loss
+// One row per cluster, read once.
+template <bool F32, int NT>
+__global__ void __launch_bounds__(kLossThreads, 2) distill_loss_kernel(const DistillParams p)
+{
+    constexpr int TH = kLossThreads, WARPS = TH / 32;
+    extern __shared__ __align__(16) uint4 smem[];
+    __shared__ float4 part[WARPS];
+    __shared__ float wsum[WARPS][4], wkd[WARPS];
+    __shared__ __align__(16) float csum[kRowMaxCluster][4];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int C = p.cluster, row = blockIdx.x / C, rank = blockIdx.x % C;
     const int label = p.labels ? p.labels[row] : 0;
     const bool bad = p.labels && label >= p.V;
-    if (bad && rank == 0 && tid == 0 && p.status) atomicOr(p.status, kStatusBadToken);
-    char *out = MODE == kLoss ? nullptr : reinterpret_cast<char *>(p.d) + (size_t)((int64_t)row * p.ldd) * B;
-    // whether output vectors lie on the same boundaries as the input's
-    const bool same = MODE == kLoss || ((reinterpret_cast<uintptr_t>(out) - (uintptr_t)r.head * B) & 15u) == 0;
-    uint4 *stage = row_smem + p.cached;
-    Entries ent;
-    ent.i = reinterpret_cast<int *>(stage + p.work);
-    ent.lq = reinterpret_cast<float *>(ent.i + p.K);
-    ent.z = ent.lq + p.K;
-    if (label < 0 || bad) {
+    if (label < 0 || bad) {   // an ignored row: nothing of it is read, all its CTAs leave here
         if (rank == 0 && tid == 0) {
-            if (MODE != kGrad && p.loss) p.loss[row] = 0.f;
-            if (MODE != kGrad && p.lse) p.lse[2 * (size_t)row] = p.lse[2 * (size_t)row + 1] = 0.f;
+            if (bad && p.status) atomicOr(p.status, kStatusBadToken);
+            p.loss[row] = 0.f;
+            if (p.lse) p.lse[2 * (size_t)row] = p.lse[2 * (size_t)row + 1] = 0.f;
         }
-        if constexpr (MODE != kLoss) {
-            const uint4 zero = make_uint4(0, 0, 0, 0);
-            if (!same) stage[tid] = zero;
-            __syncthreads();
-            for (int v0 = 0; v0 < n; v0 += TH) {
-                const int g = gb + v0 + tid;
-                if (!same) {
-                    store_shifted<F32, TH>(out, r, gb + v0, min(TH, n - v0), stage);
-                } else if (v0 + tid < n) {
-                    if (r.whole(g)) st_row_v4(out + (int64_t)r.first(g) * B, zero);
-                    else
-                        for (int j = 0; j < E; ++j)
-                            if (r.inside(r.first(g) + j)) store_elem<F32>(out, r.first(g) + j, 0u);
-                }
-            }
-        }
-        return;   // (all CTAs of the row leave here: none of them waits)
+        return;
     }
+    if (C > 1) cluster_arrive();
+    const Row<F32> r(p.z, row, p.ldz, p.V);
+    const int2 run = run_of(r, C, rank);
+    const float ctau = kLog2e / p.tau;
+    float c[NT];
+    set_factors(c, p, ctau);
+    const Entries ent(smem, p.K);
+    Shares shares;
+    int facts;
+    const bool any = p.alpha > 0.f && p.K > 0 && rank == 0 &&
+                     load_entries<F32, TH>(ent, p, row, label, 0, p.V, ctau, part, true, &shares, &facts);
+    const bool hard = p.alpha < 1.f && p.labels;
+    const float zy = hard ? load_logit(p.z, (int64_t)row * p.ldz + label, F32) : 0.f;
 
-    if (MODE != kGrad && C > 1) cluster_arrive();
-    // start the row on its way first: the entries are small
-    if constexpr (MODE == kLossGrad) {
-        for (int i = 0; i < kAhead; ++i) {
+    RunSum<NT> sum = empty_sum<NT>();
+    stream_sum<F32, NT, TH>(sum, r, run.x, 0, run.y, c);
+    warp_join(sum, c, 32);
+    if (lane == 0) put_sum(wsum[warp], sum);
+    __syncthreads();
+    sum = get_sum<NT>(wsum[lane & (WARPS - 1)]);
+    warp_join(sum, c, WARPS);
+    if (C > 1) {
+        cluster_wait();
+        if (tid < C) st_peer_v4(peer_addr(csum[rank], tid), sum.m, sum.s[0], sum.s[NT - 1], 0.f);
+        cluster_sync_all();
+        if (rank != 0) return;
+        sum = get_sum<NT>(csum[lane & (C - 1)]);
+        warp_join(sum, c, C);
+    }
+    const float off = offset_of(sum.m);
+    float l2[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) l2[t] = log2f(sum.s[t]);
+    float kd = 0.f;
+    if (any) {
+        kd = warp_sum(kd_part<TH>(ent, p.K, shares, off, l2[0]));
+        if (lane == 0) wkd[warp] = kd;
+        __syncthreads();
+        kd = 0.f;
+        for (int w = 0; w < WARPS; ++w) kd += wkd[w];
+    }
+    if (tid == 0) put_loss(p, row, l2, off, kd, any ? p.alpha : 0.f, hard ? 1.f - p.alpha : 0.f, zy);
+}
+
+// ------------------------------------------------------------------ the gradient from the log-sum-exps
+// p.cluster CTAs per row that need nothing of one another; the row streams through registers, four granules in
+// flight per thread.
+template <bool F32, int NT>
+__global__ void __launch_bounds__(kGradThreads, 4) distill_grad_kernel(const DistillParams p)
+{
+    constexpr int TH = kGradThreads, WARPS = TH / 32, E = RowElem<F32>::kPer, B = RowElem<F32>::kBytes;
+    extern __shared__ __align__(16) uint4 smem[];
+    __shared__ float4 part[WARPS];
+    const int tid = threadIdx.x;
+    const int C = p.cluster, row = blockIdx.x / C, rank = blockIdx.x % C;
+    const Row<F32> r(p.z, row, p.ldz, p.V);
+    const int2 run = run_of(r, C, rank);
+    const int lo = max(0, r.first(run.x)), hi = (int)min((int64_t)p.V, (int64_t)r.first(run.x) + (int64_t)run.y * E);
+    char *out = reinterpret_cast<char *>(p.d) + (size_t)((int64_t)row * p.ldd) * B;
+    // whether the output's vectors lie on the same boundaries as the input's
+    const bool same = ((reinterpret_cast<uintptr_t>(out) - (uintptr_t)r.head * B) & 15u) == 0;
+    uint4 *stage = smem;
+    const Entries ent(smem + p.work, p.K);
+    const Seen seen{reinterpret_cast<int *>(ent.z + p.K), (unsigned)p.slots - 1u};
+    const int label = p.labels ? p.labels[row] : 0;
+    const bool bad = p.labels && label >= p.V, ignored = label < 0 || bad;
+    if (bad && rank == 0 && tid == 0 && p.status) atomicOr(p.status, kStatusBadToken);
+
+    bool any = false;
+    Shares shares;
+    int facts = 0;
+    const bool hard = !ignored && p.alpha < 1.f && p.labels;
+    float zy = 0.f;
+    if (!ignored) {
+        const float ctau = kLog2e / p.tau;
+        if (p.alpha > 0.f && p.K > 0)
+            any = load_entries<F32, TH>(ent, p, row, label, lo, hi, ctau, part, rank == 0, &shares, &facts);
+        if (hard) zy = load_logit(p.z, (int64_t)row * p.ldz + label, F32);
+        __syncthreads();   // in place: the targets' logits are read before anybody stores
+    }
+    const float wt = any ? p.alpha : 0.f, wh = hard ? 1.f - p.alpha : 0.f;
+    const float up = ignored ? 0.f : p.g ? p.g[row] : 1.f;
+    GradFn<NT, true> grad;
+    const bool tau_first = NT == 2 || p.alpha > 0.f;   // what the first exponential is of
+    grad.A = NT == 2 ? up * wt * p.tau : up * (wt * p.tau + wh);
+    grad.B = NT == 2 ? up * wh : 0.f;
+    grad.s0 = tau_first ? 1.f / p.tau : 1.f;
+    grad.m0 = kLog2e;
+    grad.a0 = grad.A == 0.f ? -INFINITY : -p.lse_in[2 * (size_t)row + (tau_first ? 0 : 1)];
+    grad.a1 = grad.B == 0.f ? -INFINITY : -p.lse_in[2 * (size_t)row + 1];
+
+    const auto value = [&](int v) {
+        return ignored ? make_uint4(0, 0, 0, 0) : grad.template granule<F32>(load_granule<F32>(r, run.x + v));
+    };
+    if (same) {
+        constexpr int U = 4;
+        int v = tid;
+        if (!ignored)
+            for (; v + (U - 1) * TH < run.y; v += U * TH) {
+                uint4 x[U];
+#pragma unroll
+                for (int k = 0; k < U; ++k) x[k] = load_granule<F32>(r, run.x + v + k * TH);
+#pragma unroll
+                for (int k = 0; k < U; ++k) put_granule<F32>(out, r, run.x + v + k * TH, grad.template granule<F32>(x[k]));
+            }
+        for (; v < run.y; v += TH) put_granule<F32>(out, r, run.x + v, value(v));
+    } else {
+        for (int v0 = 0; v0 < run.y; v0 += TH) {
+            if (v0 + tid < run.y) stage[tid] = value(v0 + tid);
+            __syncthreads();
+            store_shifted<F32, TH>(out, r, run.x + v0, min(TH, run.y - v0), stage);
+            __syncthreads();
+        }
+    }
+    if (ignored) return;
+    bool twice = false;
+    if (any) {
+        for (int i = tid; i < p.slots; i += TH) seen.slot[i] = -1;
+        __syncthreads();
+        for (int o = tid; o < p.K; o += TH)
+            if (ent.i[o] >= lo && ent.i[o] < hi) twice |= seen.before(ent.i[o]);
+    }
+    if (__syncthreads_or(twice)) facts |= kEntryTwice;
+    put_targets<F32, TH>(out, p, ent, shares, facts, lo, hi, up, wt, wh, label, zy, grad);
+}
+
+// ------------------------------------------------------------------ both in one pass
+// Clusters that stay for many rows.  A row's share of a CTA is in shared memory from the sums to the gradient; as soon
+// as a thread has a granule's gradient it sends for the same granule of the cluster's next row, into the same place:
+// nobody else touches it, so the next row arrives while this one is stored, without a barrier.  The CTAs of a row
+// exchange their sums by stores that count on an mbarrier of the receiver (a cluster barrier would wait for the
+// gradient's stores as well); a wait that gives up leaves NaN and says so in the status word.
+template <bool F32, int NT>
+__global__ void __launch_bounds__(kStepThreads, kStepPerSm) distill_step_kernel(const DistillParams p)
+{
+    constexpr int TH = kStepThreads, WARPS = TH / 32, E = RowElem<F32>::kPer, B = RowElem<F32>::kBytes;
+    constexpr int kLate = 4;                 // of a thread's granules that may still be on their way when a row begins
+    constexpr int kBatch = F32 ? 4 : 2;      // granules summed together
+    extern __shared__ __align__(16) uint4 row_smem[];
+    __shared__ float4 part[WARPS];
+    __shared__ float wsum[WARPS][4], wkd[WARPS];
+    __shared__ __align__(16) float csum[2][kRowMaxCluster][4];
+    __shared__ uint64_t arrived[2];
+    __shared__ int never;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int C = p.cluster, rank = blockIdx.x % C, stride = gridDim.x / C;
+    uint4 *stage = row_smem + p.cached;
+    char *tables = reinterpret_cast<char *>(stage + p.work);   // entries and their indices' table, two of each in turn
+    const size_t table_bytes = (size_t)p.K * 12 + (size_t)p.slots * 4;
+    const auto seen_in = [&](int t) {
+        return Seen{reinterpret_cast<int *>(tables + t * table_bytes + (size_t)p.K * 12), (unsigned)p.slots - 1u};
+    };
+    const float ctau = kLog2e / p.tau;
+    float c[NT];
+    set_factors(c, p, ctau);
+    const bool soft = p.alpha > 0.f && p.K > 0, hard = p.alpha < 1.f && p.labels;
+    const float wh = hard ? 1.f - p.alpha : 0.f;
+    const int turns = (p.cached + TH - 1) / TH;   // cached granules per thread, at most
+
+    const auto label_of = [&](int row) { return p.labels && row < p.T ? p.labels[row] : 0; };
+    const auto alive = [&](int row, int label) { return row < p.T && label >= 0 && label < p.V; };
+
+    if (tid == 0) {
+        mbar_init(&arrived[0], 1);
+        mbar_init(&arrived[1], 1);
+        mbar_init_fence();
+        never = 0;
+    }
+    if (soft)
+        for (int t = 0; t < 2; ++t)
+            for (int i = tid; i < p.slots; i += TH) seen_in(t).slot[i] = -1;
+    int row = blockIdx.x / C, label = label_of(row), uses = 0;
+    {
+        const Row<F32> r(p.z, row, p.ldz, p.V);
+        const int2 run = run_of(r, C, rank);
+        const int n = alive(row, label) ? min(run.y, p.cached) : 0;
+        for (int i = 0; i < turns; ++i) {
             const int v = tid + i * TH;
-            if (v < min(n, p.cached)) fetch_granule<F32>(r, gb + v, row_smem + v);
+            if (v < n) fetch_granule<F32>(r, run.x + v, row_smem + v);
             cp_async_commit();
         }
     }
-    bool any = false;   // the row has an entry with a share
-    if (p.alpha > 0.f && p.K > 0 && (MODE != kLoss || rank == 0))
-        any = load_entries<F32, TH>(ent, p, row, ctau, part, rank == 0);
-    const bool hard = p.alpha < 1.f && p.labels;
-    const float zy = hard ? load_logit(p.z, (int64_t)row * p.ldz + label, F32) : 0.f;
-    const float wt = any ? p.alpha : 0.f, wh = hard ? 1.f - p.alpha : 0.f;
+    if (C > 1) cluster_sync_all();   // every CTA runs, and its mbarriers are there
+    else __syncthreads();
 
-    float off = 0.f, inv[NT];   // 2^((z - off) c) * inv = probability; MODE kGrad: see there
-    if constexpr (MODE != kGrad) {
-        RunSum<NT> sum;
-        sum.m = -INFINITY;
+    for (; row < p.T; row += stride) {
+        const Row<F32> r(p.z, row, p.ldz, p.V);
+        const int2 run = run_of(r, C, rank);
+        const int n = run.y, nc = min(n, p.cached);
+        const int lo = max(0, r.first(run.x)), hi = (int)min((int64_t)p.V, (int64_t)r.first(run.x) + (int64_t)n * E);
+        char *out = reinterpret_cast<char *>(p.d) + (size_t)((int64_t)row * p.ldd) * B;
+        // whether the output's vectors lie on the same boundaries as the input's
+        const bool same = ((reinterpret_cast<uintptr_t>(out) - (uintptr_t)r.head * B) & 15u) == 0;
+        const bool live = alive(row, label);
+        const int nlabel = label_of(row + stride);
+        const bool next = alive(row + stride, nlabel);
+        const Row<F32> nr(p.z, next ? row + stride : row, p.ldz, p.V);
+        const int2 nrun = run_of(nr, C, rank);
+        const int nn = next ? min(nrun.y, p.cached) : 0;
+
+        const int turn = uses & 1;
+        const Entries ent(tables + turn * table_bytes, p.K);
+        GradFn<NT, false> grad;
+        Shares shares;
+        float up = 0.f, wt = 0.f, zy = 0.f, off = 0.f, l2[NT];
+        int facts = 0;
+        bool any = false;
+        if (live) {
+            // the entries and the label's logit are on their way while the row is summed
+            int i0 = -1;
+            float g0 = 0.f;
+            if (soft && tid < p.K) {
+                i0 = p.idx[(size_t)row * p.K + tid];
+                g0 = p.val[(size_t)row * p.K + tid];
+            }
+            if (hard) zy = load_logit(p.z, (int64_t)row * p.ldz + label, F32);
+            up = p.g ? p.g[row] : 1.f;
+
+            RunSum<NT> sum = empty_sum<NT>();
+            int v = tid;
+            const auto batches = [&](int end) {
+                for (; v + (kBatch - 1) * TH < end; v += kBatch * TH) {
+                    uint4 x[kBatch];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) sum.s[t] = 0.f;
-        int done = 0;
-        if constexpr (MODE == kLossGrad) {
-            const int nc = min(n, p.cached);
-            for (int i = 0; tid + i * TH < nc; ++i) {
-                cp_async_wait<kAhead - 1>();
-                const int v = tid + i * TH, next = v + kAhead * TH;
+                    for (int k = 0; k < kBatch; ++k) x[k] = row_smem[v + k * TH];
+                    run_add<F32, NT, kBatch>(sum, x, c);
+                }
+            };
+            cp_async_wait<kLate>();
+            batches(min(nc, (turns - kLate) * TH));
+            cp_async_wait<0>();
+            batches(nc);
+            for (; v < nc; v += TH) {
                 const uint4 one[1] = {row_smem[v]};
-                if (next < nc) fetch_granule<F32>(r, gb + next, row_smem + next);
-                cp_async_commit();
                 run_add<F32, NT, 1>(sum, one, c);
             }
-            done = nc;
-        }
-        int v = done + tid;
-        for (; v + 3 * TH < n; v += 4 * TH) {
-            uint4 x[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) x[k] = load_granule<F32>(r, gb + v + k * TH);
-            run_add<F32, NT, 4>(sum, x, c);
-        }
-        for (; v < n; v += TH) {
-            const uint4 one[1] = {load_granule<F32>(r, gb + v)};
-            run_add<F32, NT, 1>(sum, one, c);
-        }
-        // the warp, the CTA, the cluster
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-            RunSum<NT> other;
-            other.m = __shfl_xor_sync(0xffffffffu, sum.m, o);
-#pragma unroll
-            for (int t = 0; t < NT; ++t) other.s[t] = __shfl_xor_sync(0xffffffffu, sum.s[t], o);
-            run_join(sum, other, c);
-        }
-        if (lane == 0) {
-            wsum[warp][0] = sum.m;
-#pragma unroll
-            for (int t = 0; t < NT; ++t) wsum[warp][1 + t] = sum.s[t];
-        }
-        __syncthreads();
-        sum.m = wsum[lane & (WARPS - 1)][0];
-#pragma unroll
-        for (int t = 0; t < NT; ++t) sum.s[t] = wsum[lane & (WARPS - 1)][1 + t];
-#pragma unroll
-        for (int o = WARPS / 2; o > 0; o >>= 1) {
-            RunSum<NT> other;
-            other.m = __shfl_xor_sync(0xffffffffu, sum.m, o);
-#pragma unroll
-            for (int t = 0; t < NT; ++t) other.s[t] = __shfl_xor_sync(0xffffffffu, sum.s[t], o);
-            run_join(sum, other, c);
-        }
-        if (C > 1) {
-            cluster_wait();
-            if (tid < C) st_peer_v4(peer_addr(csum[rank], tid), sum.m, sum.s[0], sum.s[NT - 1], 0.f);
-            cluster_sync_all();
-            sum.m = -INFINITY;
-#pragma unroll
-            for (int t = 0; t < NT; ++t) sum.s[t] = 0.f;
-            for (int k = 0; k < C; ++k) {
-                RunSum<NT> other;
-                other.m = csum[k][0];
-#pragma unroll
-                for (int t = 0; t < NT; ++t) other.s[t] = csum[k][1 + t];
-                run_join(sum, other, c);
-            }
-        }
-        float l2[NT];
-        off = offset_of(sum.m);
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            l2[t] = log2f(sum.s[t]);
-            inv[t] = 1.f / sum.s[t];
-        }
-        if (rank == 0) {
-            float kd = 0.f;
-            if (any) {
-                for (int o = tid; o < p.K; o += TH) {
-                    const float q = exp2f(ent.lq[o]);
-                    if (!(q == 0.f)) kd += q * (ent.lq[o] - fmaf(ent.z[o] - off, ctau, -l2[0]));   // (0 log 0 = 0)
+            stream_sum<F32, NT, TH>(sum, r, run.x, nc, n, c);
+            if (soft) {
+                const Seen seen = seen_in(turn);
+                float gm = -INFINITY;
+                int mine = 0;
+                for (int k = tid; k < p.K; k += TH) {
+                    const int i = k == tid ? i0 : p.idx[(size_t)row * p.K + k];
+                    const float g = k == tid ? g0 : p.val[(size_t)row * p.K + k];
+                    put_entry<F32>(ent, p, row, k, i, g, label, rank ? lo : 0, rank ? hi : p.V, rank == 0, &gm, &mine);
+                    if (i >= lo && i < hi && seen.before(i)) mine |= kEntryTwice;
                 }
-                kd = block_sum<WARPS>(kd, part + 2 * WARPS);
+                const float4 w = warp_shares<TH>(ent, p.K, ctau, gm, mine);
+                if (lane == 0) part[warp] = w;
             }
-            if (tid == 0) {
-                constexpr int H = NT - 1;   // the sums at temperature 1
-                float loss = 0.f;
-                if (wt > 0.f) loss += wt * p.tau * p.tau * kLn2 * kd;
-                if (wh > 0.f) loss += wh * fmaf(kLn2, l2[H], off - zy);
-                p.loss[row] = loss;
-                if (p.lse) {
-                    p.lse[2 * (size_t)row] = fmaf(kLn2, l2[0], off / p.tau);   // (NT 1 is tau = 1 here)
-                    p.lse[2 * (size_t)row + 1] = fmaf(kLn2, l2[H], off);
+            warp_join(sum, c, 32);
+            if (lane == 0) put_sum(wsum[warp], sum);
+            __syncthreads();
+            sum = get_sum<NT>(wsum[lane & (WARPS - 1)]);
+            warp_join(sum, c, WARPS);
+            bool met = true;
+            if (C > 1) {
+                if (tid == 0) mbar_arrive_expect_tx(&arrived[turn], 16u * C);
+                if (tid < C)
+                    st_async_v4(peer_addr(csum[turn][rank], tid), sum.m, sum.s[0], sum.s[NT - 1], 0.f,
+                                peer_addr(&arrived[turn], tid));
+            }
+            if (soft) {
+                any = join_shares<WARPS>(part, ctau, &shares, &facts);
+                // the table that the next row uses
+                const Seen seen = seen_in(turn ^ 1);
+                for (int i = tid; i < p.slots; i += TH) seen.slot[i] = -1;
+            }
+            if (C > 1) {
+                met = mbar_wait(&arrived[turn], (uses >> 1) & 1, &never);
+                sum = get_sum<NT>(csum[turn][lane & (C - 1)]);
+                warp_join(sum, c, C);
+                if (!met) {
+                    sum.s[0] = sum.s[NT - 1] = __int_as_float(0x7fffffff);
+                    if (lane == 0 && p.status) atomicOr(p.status, kStatusTimeout);
                 }
             }
-        }
-    }
-
-    if constexpr (MODE != kLoss) {
-        const float up = p.g ? p.g[row] : 1.f;
-        // d_j = A 2^(x_0) + B 2^(x_1) less the targets; NT 1: one of the two, or both at tau = 1 in A
-        float A, Bq = 0.f;
-        float itau = 1.f, l0 = 0.f, l1 = 0.f;
-        if constexpr (NT == 2) {
-            A = up * wt * p.tau;
-            Bq = up * wh;
-        } else {
-            A = up * (wt * p.tau + wh);
-        }
-        if constexpr (MODE == kLossGrad) {
-            // (a row of no weight has the gradient 0, also where it has no sum)
-            if (A != 0.f) A *= inv[0];
-            if constexpr (NT == 2)
-                if (Bq != 0.f) Bq *= inv[1];
-        } else {
-            // p = 2^((z / tau - lse) log2 e): the difference first, it is exact where p is large
-            itau = NT == 2 || p.alpha > 0.f ? 1.f / p.tau : 1.f;
-            l0 = p.lse_in[2 * (size_t)row + (NT == 2 || p.alpha > 0.f ? 0 : 1)];
-            if constexpr (NT == 2) l1 = p.lse_in[2 * (size_t)row + 1];
-            if (A == 0.f) l0 = INFINITY;
-            if (Bq == 0.f) l1 = INFINITY;
-            __syncthreads();   // in place: the targets' logits are read before anybody stores
-        }
-        // the two steps of an exponent: to pairs, and to single values the same way
-        const float s0 = MODE == kLossGrad ? 1.f : itau, a0 = MODE == kLossGrad ? -off : -l0;
-        const float a1 = MODE == kLossGrad ? -off : -l1;
-        const float m0 = MODE == kLossGrad ? c[0] : kLog2e, m1 = kLog2e;
-        const auto grad2 = [&](f32x2 x) {
-            const f32x2 x0 = MODE == kLossGrad ? fadd2(x, pack2(a0, a0)) : ffma2(x, pack2(s0, s0), pack2(a0, a0));
-            const float2 e0 = unpack2(fmul2(x0, pack2(m0, m0)));
-            f32x2 d = fmul2(pack2(A, A), pack2(ex2_approx(e0.x), ex2_approx(e0.y)));
-            if constexpr (NT == 2) {
-                const f32x2 x1 = MODE == kLossGrad ? x0 : fadd2(x, pack2(a1, a1));
-                const float2 e1 = unpack2(fmul2(x1, pack2(m1, m1)));
-                d = ffma2(pack2(Bq, Bq), pack2(ex2_approx(e1.x), ex2_approx(e1.y)), d);
-            }
-            return unpack2(d);
-        };
-        const auto grad = [&](float x) { return grad2(pack2(x, x)).x; };
-        const auto one = [&](const uint4 &x) {
-            f32x2 f[E / 2];
-            float2 d[E / 2];
-            granule_pairs<F32>(x, f);
+            ++uses;
+            wt = any ? p.alpha : 0.f;
+            off = offset_of(sum.m);
 #pragma unroll
-            for (int j = 0; j < E / 2; ++j) d[j] = grad2(f[j]);
-            return pack_granule<F32>(d);
+            for (int t = 0; t < NT; ++t) l2[t] = log2f(sum.s[t]);
+            grad.A = NT == 2 ? up * wt * p.tau : up * (wt * p.tau + wh);
+            grad.B = NT == 2 ? up * wh : 0.f;
+            if (grad.A != 0.f) grad.A /= sum.s[0];
+            if (grad.B != 0.f) grad.B /= sum.s[NT - 1];
+            grad.s0 = 1.f;
+            grad.a0 = grad.a1 = -off;
+            grad.m0 = c[0];
+        }
+        // the gradient, and the next row's granules into the places that become free
+        const auto value = [&](int v) {
+            if (!live) return make_uint4(0, 0, 0, 0);   // an ignored row: nothing of it is read
+            return grad.template granule<F32>(v < nc ? row_smem[v] : load_granule<F32>(r, run.x + v));
         };
-        const auto put = [&](int g, const uint4 &o) {
-            if (r.whole(g)) st_row_v4(out + (int64_t)r.first(g) * B, o);
-            else
-#pragma unroll
-                for (int j = 0; j < E; ++j)
-                    if (r.inside(r.first(g) + j)) store_elem<F32>(out, r.first(g) + j, granule_elem<F32>(o, j));
-        };
-        const auto fetched = [&](int v) {
-            return MODE == kLossGrad && v < p.cached ? row_smem[v] : load_granule<F32>(r, gb + v);
+        const auto send = [&](int i) {
+            const int v = tid + i * TH;
+            if (v < nn) fetch_granule<F32>(nr, nrun.x + v, row_smem + v);
+            cp_async_commit();
         };
         if (same) {
-            constexpr int U = MODE == kGrad ? 4 : 1;   // loads in flight per thread
-            int v = tid;
-            for (; v + (U - 1) * TH < n; v += U * TH) {
-                uint4 x[U];
+            const int2 whole = whole_of(r, run), nwhole = whole_of(nr, nrun);
+            // turns in which every thread has a whole granule to store and one to send for
+            const int plain0 = whole.x | nwhole.x;
+            const int plain1 = live && next ? min(min(whole.y, nc), min(nwhole.y, nn)) / TH : 0;
+            const auto turn_of = [&](int i) {
+                const int v = tid + i * TH;
+                if (v < nc) put_granule<F32>(out, r, run.x + v, value(v));
+                send(i);
+            };
+            int i = 0;
+            if (plain0 && turns > 0) turn_of(i++);
+            char *dst = out + ((int64_t)r.first(run.x) * B + (int64_t)tid * 16);   // (aligned)
+            const char *src = nr.base + ((size_t)nrun.x + tid) * 16;
+            uint4 *at = row_smem + tid;
+            for (; i + kBatch <= plain1; i += kBatch) {
+                uint4 x[kBatch];
 #pragma unroll
-                for (int k = 0; k < U; ++k) x[k] = fetched(v + k * TH);
+                for (int k = 0; k < kBatch; ++k) x[k] = at[(i + k) * TH];
 #pragma unroll
-                for (int k = 0; k < U; ++k) put(gb + v + k * TH, one(x[k]));
+                for (int k = 0; k < kBatch; ++k) {
+                    const size_t o = (size_t)(i + k) * (TH * 16);
+                    st_row_v4(dst + o, grad.template granule<F32>(x[k]));
+                    cp_async16(at + (i + k) * TH, src + o);
+                    cp_async_commit();
+                }
             }
-            for (; v < n; v += TH) put(gb + v, one(fetched(v)));
+            for (; i < turns; ++i) turn_of(i);
+            for (int v = nc + tid; v < n; v += TH) put_granule<F32>(out, r, run.x + v, value(v));
         } else {
             for (int v0 = 0; v0 < n; v0 += TH) {
-                if (v0 + tid < n) stage[tid] = one(fetched(v0 + tid));
+                if (v0 + tid < n) stage[tid] = value(v0 + tid);
+                if (v0 / TH < turns) send(v0 / TH);
                 __syncthreads();
-                store_shifted<F32, TH>(out, r, gb + v0, min(TH, n - v0), stage);
+                store_shifted<F32, TH>(out, r, run.x + v0, min(TH, n - v0), stage);
                 __syncthreads();
             }
+            for (int i = (n + TH - 1) / TH; i < turns; ++i) send(i);
         }
-        // the targets' places, each computed as a whole and rounded once, after everybody's stores
-        const int lo = max(0, r.first(gb)), hi = (int)min((int64_t)p.V, (int64_t)r.first(gb) + (int64_t)n * E);
-        bool twice = false;
-        int *hash = reinterpret_cast<int *>(row_smem);   // (over the cached row, which nobody needs any more)
-        if (any) {
-            // does an index occur twice?  (open addressing; as many slots as twice the entries)
-            __syncthreads();
-            for (int i = tid; i < kHashSlots; i += TH) hash[i] = -1;
-            __syncthreads();
-            for (int o = tid; o < p.K; o += TH) {
-                const int i = ent.i[o];
-                if (i < lo || i >= hi) continue;
-                unsigned slot = ((unsigned)i * 2654435761u) >> 21;
-                static_assert(kHashSlots == 2048, "the shift above");
-                for (;;) {
-                    const int was = atomicCAS(&hash[slot], -1, i);
-                    if (was == -1) break;
-                    if (was == i) { twice = true; break; }
-                    slot = (slot + 1) & (kHashSlots - 1);
-                }
+        if (live) {
+            if (rank == 0 && any) {
+                const float kd = warp_sum(kd_part<TH>(ent, p.K, shares, off, l2[0]));
+                if (lane == 0) wkd[warp] = kd;
             }
-        }
-        twice = __syncthreads_or(twice);
-        bool labelled = false;
-        if (any)
-            for (int o = tid; o < p.K; o += TH) {
-                const int i = ent.i[o];
-                if (i < lo || i >= hi) continue;
-                float q = exp2f(ent.lq[o]);
-                if (twice) {   // an index's first entry adds them all, in their order
-                    q = 0.f;
-                    bool first = true;
-                    for (int k = 0; k < p.K; ++k)
-                        if (ent.i[k] == i) {
-                            first &= k >= o;
-                            q += exp2f(ent.lq[k]);
-                        }
-                    if (!first) continue;
-                }
-                float d = fmaf(-up * wt * p.tau, q, grad(ent.z[o]));
-                if (hard && i == label) {
-                    d -= up * wh;
-                    labelled = true;
-                }
-                store_elem<F32>(out, i, F32 ? __float_as_uint(d) : bf16_bits(d, 0.f) & 0xffffu);
+            __syncthreads();
+            if (rank == 0 && tid == 0) {
+                float kd = 0.f;
+                for (int w = 0; any && w < WARPS; ++w) kd += wkd[w];
+                put_loss(p, row, l2, off, kd, wt, wh, zy);
             }
-        // the label, where it is not one of the entries
-        if (hard && label >= lo && label < hi && !__syncthreads_or(labelled) && tid == 0) {
-            const float d = grad(zy) - up * wh;
-            store_elem<F32>(out, label, F32 ? __float_as_uint(d) : bf16_bits(d, 0.f) & 0xffffu);
+            put_targets<F32, TH>(out, p, ent, shares, facts, lo, hi, up, wt, wh, label, zy, grad);
+        } else if (rank == 0 && tid == 0) {
+            p.loss[row] = 0.f;
+            if (label >= p.V && p.status) atomicOr(p.status, kStatusBadToken);
         }
+        label = nlabel;
     }
+    if (C > 1) cluster_sync_all();   // nobody leaves while another may still write to its memory
 }
 
 size_t al16(size_t v) { return (v + 15) & ~(size_t)15; }
@@ -592,55 +876,74 @@ int row_cluster(int T, int64_t row_bytes, size_t share)
     return C;
 }
 
-template <bool F32, int MODE, int NT>
-cudaError_t launch_distill(DistillParams p, cudaStream_t st)
+static_assert((kLossThreads & (kLossThreads - 1)) == 0 && (kGradThreads & (kGradThreads - 1)) == 0 &&
+                  (kStepThreads & (kStepThreads - 1)) == 0 && kLossThreads <= 1024 && kGradThreads >= 64 &&
+                  kStepThreads >= 64,
+              "the sums over warps halve their number");
+
+// Two exponentials per element only where both temperatures count and differ.
+bool two_sums(const DistillParams &p) { return p.tau != 1.f && p.alpha > 0.f && p.alpha < 1.f; }
+
+template <bool F32>
+cudaError_t launch_loss(DistillParams p, cudaStream_t st)
+{
+    p.cluster = row_cluster(p.T, (int64_t)p.V * RowElem<F32>::kBytes, 0);
+    const size_t smem = (size_t)p.K * 12;
+    const bool two = two_sums(p) || (p.lse && p.tau != 1.f);   // both log-sum-exps are asked for
+    const int64_t ctas = (int64_t)p.T * p.cluster;
+    return two ? launch_clusters<distill_loss_kernel<F32, 2>>(ctas, kLossThreads, smem, kMaxSmem, p.cluster, st, p)
+               : launch_clusters<distill_loss_kernel<F32, 1>>(ctas, kLossThreads, smem, kMaxSmem, p.cluster, st, p);
+}
+
+// Shared memory of the gradient's kernels behind the cached row: a stage where the gradient's rows do not lie on the
+// logits' 16-byte boundaries, and the entries and the table of their indices, once or twice.
+template <bool F32>
+size_t plan_grad(DistillParams &p, int threads, int tables)
+{
+    constexpr int B = RowElem<F32>::kBytes;
+    const bool same = (reinterpret_cast<uintptr_t>(p.z) - reinterpret_cast<uintptr_t>(p.d)) % 16 == 0 &&
+                      (p.T == 1 || (p.ldz - p.ldd) * B % 16 == 0);
+    p.work = same ? 0 : threads;
+    p.slots = 32;
+    while (p.slots < 2 * p.K) p.slots *= 2;
+    return ((size_t)p.cached + p.work) * 16 + tables * ((size_t)p.K * 12 + (size_t)p.slots * 4);
+}
+
+template <bool F32>
+cudaError_t launch_grad(DistillParams p, cudaStream_t st)
+{
+    p.cluster = row_cluster(p.T, (int64_t)p.V * RowElem<F32>::kBytes, 0);
+    p.cached = 0;
+    const size_t smem = plan_grad<F32>(p, kGradThreads, 1);
+    // (the CTAs of a row need no cluster)
+    const int64_t ctas = (int64_t)p.T * p.cluster;
+    return two_sums(p) ? launch_clusters<distill_grad_kernel<F32, 2>>(ctas, kGradThreads, smem, kMaxSmem, 1, st, p)
+                       : launch_clusters<distill_grad_kernel<F32, 1>>(ctas, kGradThreads, smem, kMaxSmem, 1, st, p);
+}
+
+template <bool F32, int NT>
+cudaError_t launch_step(DistillParams p, cudaStream_t st)
 {
     const int64_t bytes = (int64_t)p.V * RowElem<F32>::kBytes;
-    p.cluster = row_cluster(p.T, bytes, MODE == kLossGrad ? kGradShare : 0);
-    p.cached = p.work = 0;
-    if (MODE == kLossGrad) {
-        const size_t share = al16((size_t)((bytes + 32 + p.cluster - 1) / p.cluster) + 32);
-        p.cached = (int)((share < kMaxCache ? share : kMaxCache) / 16);
-    }
-    if (MODE != kLoss) {
-        // a stage where the gradient's rows do not lie on the logits' 16-byte boundaries; room for the hash table
-        constexpr int B = RowElem<F32>::kBytes;
-        const bool same = (reinterpret_cast<uintptr_t>(p.z) - reinterpret_cast<uintptr_t>(p.d)) % 16 == 0 &&
-                          (p.T == 1 || (p.ldz - p.ldd) * B % 16 == 0);
-        p.work = same ? 0 : Shape<MODE>::kThreads;
-        const int least = p.K > 0 ? kHashSlots * 4 / 16 : 0;
-        if (p.cached + p.work < least) p.work = least - p.cached;
-    }
-    const size_t smem = ((size_t)p.cached + p.work) * 16 + (size_t)p.K * 12;
-    auto kern = distill_kernel<F32, MODE, NT>;
-    if (smem > 40 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMaxSmem);
-        if (e != cudaSuccess) return e;
-    }
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)p.T * (unsigned)p.cluster);
-    cfg.blockDim = dim3(Shape<MODE>::kThreads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)p.cluster;
-    attr[0].val.clusterDim.y = 1;
-    attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kern, p);
+    p.cluster = row_cluster(p.T, bytes, kStepShare);
+    const size_t share = al16((size_t)((bytes + 32 + p.cluster - 1) / p.cluster) + 32);
+    p.cached = (int)((share < kMaxCache ? share : kMaxCache) / 16);
+    const size_t smem = plan_grad<F32>(p, kStepThreads, 2);
+    // as many clusters as the GPU holds at a time, each for every so many rows
+    int fit = 0;
+    const cudaError_t e = resident_clusters<distill_step_kernel<F32, NT>>(kStepThreads, smem, kMaxSmem, p.cluster, &fit);
+    if (e != cudaSuccess) return e;
+    const int64_t clusters = p.T < fit ? p.T : fit < 1 ? 1 : fit;
+    return launch_clusters<distill_step_kernel<F32, NT>>(clusters * p.cluster, kStepThreads, smem, kMaxSmem, p.cluster, st, p);
 }
 
-template <bool F32, int MODE>
-cudaError_t launch_distill_nt(const DistillParams &p, cudaStream_t st)
+template <bool F32>
+cudaError_t launch_step(const DistillParams &p, cudaStream_t st)
 {
-    const bool both = MODE == kLoss ? p.lse != nullptr || (p.alpha > 0.f && p.alpha < 1.f)
-                                    : p.alpha > 0.f && p.alpha < 1.f;
-    return p.tau != 1.f && both ? launch_distill<F32, MODE, 2>(p, st) : launch_distill<F32, MODE, 1>(p, st);
+    return two_sums(p) ? launch_step<F32, 2>(p, st) : launch_step<F32, 1>(p, st);
 }
 
-// What the three calls have in common; MODE's own outputs are checked by the entries.
+// What the three calls have in common; their own outputs are checked by each.
 template <bool F32>
 sats_status check_distill(const DistillParams &p)
 {
@@ -680,7 +983,7 @@ sats_status distill_loss(const void *logits, int64_t ld, int T, int V, const int
     const sats_status s = check_distill<F32>(p);
     if (s != SATS_OK || T == 0) return s;
     if (!loss) return SATS_EINVAL;
-    return launched(launch_distill_nt<F32, kLoss>(p, static_cast<cudaStream_t>(stream)));
+    return launched(launch_loss<F32>(p, static_cast<cudaStream_t>(stream)));
 }
 
 template <bool F32>
@@ -697,7 +1000,7 @@ sats_status distill_grad(const void *logits, int64_t ld, int T, int V, const int
     if (T == 0) return SATS_OK;
     if (!lse || !dlogits || reinterpret_cast<uintptr_t>(dlogits) % RowElem<F32>::kBytes || bad_overlap<F32>(p))
         return SATS_EINVAL;
-    return launched(launch_distill_nt<F32, kGrad>(p, static_cast<cudaStream_t>(stream)));
+    return launched(launch_grad<F32>(p, static_cast<cudaStream_t>(stream)));
 }
 
 template <bool F32>
@@ -714,7 +1017,7 @@ sats_status distill_loss_grad(const void *logits, int64_t ld, int T, int V, cons
     if (T == 0) return SATS_OK;
     if (!loss || !dlogits || reinterpret_cast<uintptr_t>(dlogits) % RowElem<F32>::kBytes || bad_overlap<F32>(p))
         return SATS_EINVAL;
-    return launched(launch_distill_nt<F32, kLossGrad>(p, static_cast<cudaStream_t>(stream)));
+    return launched(launch_step<F32>(p, static_cast<cudaStream_t>(stream)));
 }
 
 }  // namespace

@@ -1100,32 +1100,18 @@ int logits_cluster(int rows, int64_t row_bytes)
 }
 
 // Cluster and shared memory of a launch over `rows` rows.
-template <bool F32, typename P>
-cudaError_t launch_rows(void (*kern)(const P), P p, int rows, cudaStream_t st)
+constexpr size_t kMaxSmem = kMaxCache + (size_t)kListCap * 8;
+static_assert(kMaxSmem + 10 * 1024 <= kSmemPerCta, "with the kernels' static part");
+
+template <bool F32, auto Kern, typename P>
+cudaError_t launch_rows(P p, int rows, cudaStream_t st)
 {
     const int64_t bytes = (int64_t)p.V * RowElem<F32>::kBytes;
     p.cluster = logits_cluster(rows, bytes);
     const size_t share = (size_t)((bytes + 32 + p.cluster - 1) / p.cluster) + 32;
     p.cached = (int)((share < kMaxCache ? share : kMaxCache) / 16);
     const size_t smem = (size_t)p.cached * 16 + kListCap * 8;
-    if (smem > 32 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                   (int)(kMaxCache + kListCap * 8));
-        if (e != cudaSuccess) return e;
-    }
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)rows * (unsigned)p.cluster);
-    cfg.blockDim = dim3(kRowThreads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)p.cluster;
-    attr[0].val.clusterDim.y = 1;
-    attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kern, p);
+    return launch_clusters<Kern>((int64_t)rows * p.cluster, kRowThreads, smem, kMaxSmem, p.cluster, st, p);
 }
 
 sats_status check_rows(const void *logits, int64_t ld, int rows, int V, int bytes)
@@ -1147,7 +1133,7 @@ sats_status top_logits(const void *logits, int64_t ld, int T, int V, int K, floa
     if (!values || !idx) return SATS_EINVAL;
     TopParams p{};
     p.z = logits; p.ld = ld; p.T = T; p.V = V; p.K = K; p.values = values; p.idx = idx;
-    const cudaError_t e = launch_rows<F32, TopParams>(top_kernel<F32>, p, T, static_cast<cudaStream_t>(stream));
+    const cudaError_t e = launch_rows<F32, top_kernel<F32>>(p, T, static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? SATS_OK : cuda_fail(e, "top-logits kernel launch");
 }
 
@@ -1162,7 +1148,7 @@ sats_status sample(const void *logits, int64_t ld, int B, int V, const float *te
     SampleParams p{};
     p.z = logits; p.ld = ld; p.B = B; p.V = V; p.temperature = temperature; p.top_k = top_k; p.top_p = top_p;
     p.min_p = min_p; p.u = u; p.ids = ids; p.logprob = logprob; p.n_kept = n_kept; p.status = dev_status;
-    const cudaError_t e = launch_rows<F32, SampleParams>(sample_kernel<F32>, p, B, static_cast<cudaStream_t>(stream));
+    const cudaError_t e = launch_rows<F32, sample_kernel<F32>>(p, B, static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? SATS_OK : cuda_fail(e, "sampling kernel launch");
 }
 

@@ -6,6 +6,7 @@
 // the row read as -inf.  The C CTAs of a cluster take consecutive runs of granules.
 #pragma once
 
+#include <atomic>
 #include <cstdint>
 #include <cuda_runtime.h>
 
@@ -218,12 +219,97 @@ __device__ __forceinline__ void st_peer_v4(uint32_t addr, float a, float b, floa
                  : "memory");
 }
 
+// The same without a barrier: counts 16 bytes on the mbarrier `bar` of the CTA written to (both addresses its).
+__device__ __forceinline__ void st_async_v4(uint32_t addr, float a, float b, float c, float d, uint32_t bar)
+{
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];"
+                 ::"r"(addr), "f"(a), "f"(b), "f"(c), "f"(d), "r"(bar)
+                 : "memory");
+}
+
 // 2^x (2 ulp; results below the normal range are 0).
 __device__ __forceinline__ float ex2_approx(float x)
 {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+
+// ------------------------------------------------------------------ launches (host)
+// Shared memory that a CTA may have, less what the system takes.
+constexpr size_t kSmemPerCta = 227 * 1024;
+
+// Lets Kern have up to max_smem bytes of dynamic shared memory on the current device; asked once per device.
+template <auto Kern>
+cudaError_t allow_smem(size_t max_smem)
+{
+    static std::atomic<uint64_t> done{0};
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const uint64_t bit = 1ull << (dev & 63);
+    if (dev < 64 && (done.load(std::memory_order_relaxed) & bit)) return cudaSuccess;
+    e = cudaFuncSetAttribute(Kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)max_smem);
+    if (e == cudaSuccess && dev < 64) done.fetch_or(bit, std::memory_order_relaxed);
+    return e;
+}
+
+struct ClusterConfig {
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1];
+
+    ClusterConfig(int64_t ctas, int threads, size_t smem, int cluster, cudaStream_t st)
+    {
+        cfg.gridDim = dim3((unsigned)ctas);
+        cfg.blockDim = dim3(threads);
+        cfg.dynamicSmemBytes = smem;
+        cfg.stream = st;
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = (unsigned)cluster;
+        attr[0].val.clusterDim.y = 1;
+        attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+    }
+};
+
+// Launches Kern with `ctas` CTAs in clusters of `cluster`; max_smem: the most dynamic shared memory it is ever given.
+template <auto Kern, typename P>
+cudaError_t launch_clusters(int64_t ctas, int threads, size_t smem, size_t max_smem, int cluster, cudaStream_t st,
+                            const P &p)
+{
+    const cudaError_t e = allow_smem<Kern>(max_smem);
+    if (e != cudaSuccess) return e;
+    ClusterConfig c(ctas, threads, smem, cluster, st);
+    return cudaLaunchKernelEx(&c.cfg, Kern, p);
+}
+
+// Clusters of this shape that the current device holds at a time (the last answer is kept per host thread).
+template <auto Kern>
+cudaError_t resident_clusters(int threads, size_t smem, size_t max_smem, int cluster, int *n)
+{
+    struct Last {
+        int dev = -1, cluster = 0, n = 0;
+        size_t smem = 0;
+    };
+    static thread_local Last last;
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (last.dev != dev || last.cluster != cluster || last.smem != smem) {
+        e = allow_smem<Kern>(max_smem);
+        if (e != cudaSuccess) return e;
+        ClusterConfig c((int64_t)cluster, threads, smem, cluster, nullptr);
+        int got = 0;
+        e = cudaOccupancyMaxActiveClusters(&got, Kern, &c.cfg);
+        if (e != cudaSuccess) return e;
+        last.dev = dev;
+        last.cluster = cluster;
+        last.smem = smem;
+        last.n = got;
+    }
+    *n = last.n;
+    return cudaSuccess;
 }
 
 }  // namespace sats
