@@ -26,6 +26,7 @@ namespace {
 constexpr int kMaxTop = 1024;          // largest K of the list's way
 constexpr int kListCap = 2048;         // entries of the list
 constexpr uint32_t kKeyNone = 0x007fffffu;   // key of -inf: never selected
+constexpr int kFew = 8;                // elements per thread at the end of a search
 constexpr int kAhead = 8;              // granules in flight per thread while the row arrives
 constexpr size_t kShare = 64 * 1024;   // of a row's bytes per CTA, where the cluster allows
 constexpr size_t kMaxCache = 184 * 1024;
@@ -188,10 +189,11 @@ __device__ __forceinline__ unsigned long long share_ceil(float f, unsigned long 
 struct Shared {
     unsigned long long wsum[kRowWarps];
     unsigned long long scan[kRowWarps];
-    unsigned long long slot[2][kRowMaxCluster];      // all-reduce, two buffers in turn
-    uint32_t kmax[kRowMaxCluster], bound[kRowMaxCluster], cnt[kRowMaxCluster];
-    int part[2][kRowWarps];
-    uint32_t ktop[kRowWarps];
+    unsigned long long slot[2][2][kRowMaxCluster];   // the CTAs' values, one or two of each; two buffers in turn
+    uint32_t kmax[kRowMaxCluster], bound[kRowMaxCluster];
+    int part[kRowWarps];
+    uint32_t ktop[kRowWarps], klow[kRowWarps];
+    int border;
     uint32_t nlist;
     int found_idx;
     uint32_t found_key;
@@ -229,6 +231,22 @@ struct Ctx {
         }
         return x;
     }
+    // One element of granule v.
+    __device__ __forceinline__ float get(int v, int j) const
+    {
+        float x;
+        if constexpr (F32) {
+            x = v < cached ? reinterpret_cast<const float *>(cache + v)[j] : __uint_as_float(pick(load_granule<F32>(r, gb + v), j));
+        } else {
+            x = v < cached ? __uint_as_float((uint32_t)reinterpret_cast<const uint16_t *>(cache + v)[j] << 16)
+                           : __uint_as_float(pick(load_granule<F32>(r, gb + v), j >> 1) << ((j & 1) ? 0 : 16) & 0xffff0000u);
+        }
+        return x == x ? x : -INFINITY;
+    }
+    static __device__ __forceinline__ uint32_t pick(const uint4 &x, int w)
+    {
+        return w == 0 ? x.x : w == 1 ? x.y : w == 2 ? x.z : x.w;
+    }
 };
 
 __device__ __forceinline__ unsigned long long warp_sum_u64(unsigned long long v)
@@ -251,29 +269,63 @@ __device__ __forceinline__ unsigned long long block_sum_u64(unsigned long long v
     return t;
 }
 
-// The CTAs' values, in every CTA's slots; returns their buffer.
-template <bool F32>
-__device__ __forceinline__ const unsigned long long *cluster_gather(Ctx<F32> &c, unsigned long long v)
+// Exclusive sums of the threads' values over the CTA, the total in *total.
+__device__ __forceinline__ unsigned long long block_scan_u64(unsigned long long v, Shared *sh, unsigned long long *total)
 {
-    unsigned long long *slot = c.sh->slot[c.turn];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    unsigned long long incl = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const unsigned long long u = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += u;
+    }
+    __syncthreads();
+    if (lane == 31) sh->scan[warp] = incl;
+    __syncthreads();
+    unsigned long long before = 0, t = 0;
+#pragma unroll
+    for (int w = 0; w < kRowWarps; ++w) {
+        if (w < warp) before += sh->scan[w];
+        t += sh->scan[w];
+    }
+    *total = t;
+    return before + incl - v;
+}
+
+// The CTAs' values, in every CTA's slots; returns their buffer (of second values: behind the first ones).
+template <bool F32>
+__device__ __forceinline__ const unsigned long long *cluster_gather(Ctx<F32> &c, unsigned long long v,
+                                                                    unsigned long long second = 0)
+{
+    unsigned long long (*slot)[kRowMaxCluster] = c.sh->slot[c.turn];
     c.turn ^= 1;
     if (c.C == 1) {
-        if (threadIdx.x == 0) slot[0] = v;
+        if (threadIdx.x == 0) {
+            slot[0][0] = v;
+            slot[1][0] = second;
+        }
         __syncthreads();
-        return slot;
+        return slot[0];
     }
-    if (threadIdx.x < (unsigned)c.C) st_peer_u64(peer_addr(slot + c.rank, threadIdx.x), v);
+    if (threadIdx.x < (unsigned)c.C) {
+        st_peer_u64(peer_addr(&slot[0][c.rank], threadIdx.x), v);
+        st_peer_u64(peer_addr(&slot[1][c.rank], threadIdx.x), second);
+    }
     cluster_sync_all();
-    return slot;
+    return slot[0];
+}
+
+__device__ __forceinline__ unsigned long long slot_sum(const unsigned long long *slot, int C)
+{
+    unsigned long long t = 0;
+    for (int k = 0; k < C; ++k) t += slot[k];
+    return t;
 }
 
 template <bool F32>
 __device__ __forceinline__ unsigned long long cluster_sum(Ctx<F32> &c, unsigned long long v)
 {
-    const unsigned long long *slot = cluster_gather(c, block_sum_u64(v, c.sh));
-    unsigned long long t = 0;
-    for (int k = 0; k < c.C; ++k) t += slot[k];
-    return t;
+    return slot_sum(cluster_gather(c, block_sum_u64(v, c.sh)), c.C);
 }
 
 // What is kept: keys above `key`, and of those equal to it the ones up to index `idx` (INT_MIN: none; the places of a
@@ -320,7 +372,8 @@ __device__ __forceinline__ unsigned long long thread_sum(const Ctx<F32> &c, cons
 
 // The first token in the vocabulary's order at which the running sum of f passes `target` (which is below the sum
 // over the row): *idx, *key in every CTA.  The warps' sums are in sh->wsum (block_sum_u64 of thread_sum), the CTA's is
-// `mine`, the CTAs' are in `slot`.  The CTA that holds the token narrows a run of granules down sixteenfold a step.
+// `mine`, the CTAs' are in `slot`.  The CTA that holds the token narrows a run of granules down
+// sixteenfold a step until its threads have a few elements each.
 template <bool F32, typename S>
 __device__ void locate(Ctx<F32> &c, unsigned long long target, const S &f, unsigned long long mine,
                        const unsigned long long *slot, int *idx, uint32_t *key)
@@ -337,42 +390,35 @@ __device__ void locate(Ctx<F32> &c, unsigned long long target, const S &f, unsig
             while (w < kRowWarps - 1 && t >= sh->wsum[w]) t -= sh->wsum[w++];
             a = a + w * per;
             b = min(b, a + per);
-            if (b - a <= 32) break;
+            if (b - a <= kRowThreads * kFew / RowElem<F32>::kPer) break;
             per = (b - a + kRowWarps - 1) / kRowWarps;
             unsigned long long s = 0;
             const int wb = min(b, a + warp * per), we = min(b, wb + per);
             for (int v = wb + lane; v < we; v += 32) s += f.granule(c, v);
             block_sum_u64(s, sh);
         }
-        if (warp == 0) {
-            const int v = a + lane;
-            const unsigned long long s = v < b ? f.granule(c, v) : 0ull;
-            unsigned long long incl = s;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const unsigned long long u = __shfl_up_sync(0xffffffffu, incl, o);
-                if (lane >= o) incl += u;
+        // a few elements per thread, in order
+        constexpr int E = RowElem<F32>::kPer;
+        const int n = (b - a) * E, each = (n + kRowThreads - 1) / kRowThreads, first = tid * each;
+        const int i0 = c.r.first(c.gb + a);
+        const auto at = [&](int e, uint32_t *k) {
+            const float x = c.get(a + e / E, e % E);
+            *k = key_of(x);
+            return *k > kKeyNone ? f.elem(x, *k, i0 + e) : 0ull;
+        };
+        uint32_t k;
+        unsigned long long s = 0, total;
+        for (int e = first; e < min(n, first + each); ++e) s += at(e, &k);
+        unsigned long long run = block_scan_u64(s, sh, &total);
+        if (t >= run && t - run < s) {   // (one thread)
+            int e = first;
+            for (const int last = min(n, first + each) - 1;; ++e) {
+                run += at(e, &k);
+                if (run > t || e == last) break;   // (t is below the sum of the thread's elements)
             }
-            const unsigned long long excl = incl - s;
-            if (t >= excl && t < incl) {
-                constexpr int E = RowElem<F32>::kPer;
-                float x[E];
-                granule_floats<F32>(c.get(v), x);
-                const int i0 = c.r.first(c.gb + v);
-                unsigned long long run = excl;
-                bool hit = false;
-#pragma unroll
-                for (int j = 0; j < E; ++j) {
-                    const uint32_t k = key_of(x[j]);
-                    if (k > kKeyNone) run += f.elem(x[j], k, i0 + j);
-                    if (!hit && run > t) {
-                        hit = true;
-                        for (int q = 0; q < c.C; ++q) {
-                            st_peer_u32(peer_addr(&sh->found_idx, q), (uint32_t)(i0 + j));
-                            st_peer_u32(peer_addr(&sh->found_key, q), k);
-                        }
-                    }
-                }
+            for (int q = 0; q < c.C; ++q) {
+                st_peer_u32(peer_addr(&sh->found_idx, q), (uint32_t)(i0 + e));
+                st_peer_u32(peer_addr(&sh->found_key, q), k);
             }
         }
     }
@@ -482,29 +528,6 @@ struct KeptMass {
 // ------------------------------------------------------------------ the list
 constexpr int kListPer = kListCap / kRowThreads;   // list entries of a thread, in a row
 
-// Exclusive sums of the threads' values over the CTA, the total in *total.
-__device__ __forceinline__ unsigned long long block_scan_u64(unsigned long long v, Shared *sh, unsigned long long *total)
-{
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    unsigned long long incl = v;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const unsigned long long u = __shfl_up_sync(0xffffffffu, incl, o);
-        if (lane >= o) incl += u;
-    }
-    __syncthreads();
-    if (lane == 31) sh->scan[warp] = incl;
-    __syncthreads();
-    unsigned long long before = 0, t = 0;
-#pragma unroll
-    for (int w = 0; w < kRowWarps; ++w) {
-        if (w < warp) before += sh->scan[w];
-        t += sh->scan[w];
-    }
-    *total = t;
-    return before + incl - v;
-}
-
 // Sorts n2 (a power of two) words descending; all threads of the CTA.
 __device__ void sort_desc(unsigned long long *a, int n2)
 {
@@ -588,6 +611,65 @@ __device__ void sort_list(unsigned long long *list, int n)
     sort_desc(list, n2);
 }
 
+// A list of at most kSmall entries needs no sorting: each is compared with all others, by kRowThreads / (the entries'
+// number, rounded up to a power of two) threads each.  (128 entries: sorting took 3 us, this a fifth of it.)
+constexpr int kSmall = 256;
+struct Small {
+    unsigned long long e;   // (key << 32) | ~index
+    int i, part, per;       // the entry, the thread's part of the comparisons, threads per entry (a power of two <= 16)
+    bool on;
+
+    __device__ __forceinline__ Small(const unsigned long long *list, int n)
+    {
+        const int n2 = max(32, pow2_at_least(n));
+        per = kRowThreads / n2;
+        i = (int)threadIdx.x / per;
+        part = (int)threadIdx.x & (per - 1);
+        on = i < n;
+        e = on ? list[i] : 0ull;
+    }
+    __device__ __forceinline__ uint32_t key() const { return (uint32_t)(e >> 32); }
+    __device__ __forceinline__ int idx() const { return (int)~(uint32_t)e; }
+    // Weights lie behind the entries.
+    __device__ __forceinline__ void put_weight(unsigned long long *list, unsigned long long w) const
+    {
+        if (part == 0 && on) list[kSmall + i] = w;
+    }
+    // Number of the entries before this one in descending order, and (weights given) their sum.
+    __device__ __forceinline__ int larger(const unsigned long long *list, int n) const
+    {
+        int rank = 0;
+        for (int j = part; j < n; j += per) rank += list[j] > e;
+        for (int o = per / 2; o > 0; o >>= 1) rank += __shfl_xor_sync(0xffffffffu, rank, o);
+        return rank;
+    }
+    __device__ __forceinline__ void larger(const unsigned long long *list, int n, int *rank, unsigned long long *sum) const
+    {
+        int r = 0;
+        unsigned long long s = 0;
+        for (int j = part; j < n; j += per)
+            if (list[j] > e) {
+                ++r;
+                s += list[kSmall + j];
+            }
+        for (int o = per / 2; o > 0; o >>= 1) {
+            r += __shfl_xor_sync(0xffffffffu, r, o);
+            s += __shfl_xor_sync(0xffffffffu, s, o);
+        }
+        *rank = r;
+        *sum = s;
+    }
+    // Sum of the weights of the entries with lower indices.
+    __device__ __forceinline__ unsigned long long earlier(const unsigned long long *list, int n) const
+    {
+        unsigned long long s = 0;
+        for (int j = part; j < n; j += per)
+            if ((uint32_t)list[j] > (uint32_t)e) s += list[kSmall + j];
+        for (int o = per / 2; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+        return s;
+    }
+};
+
 // ------------------------------------------------------------------ the nucleus
 // The masses of 2048 steps of the weight, in whole numbers: a word for their lower 32 bits and one for what is above.
 constexpr int kBins = 2048;
@@ -651,8 +733,14 @@ __device__ Cut cut_mass(Ctx<F32> &c, const Scale &s, const float2 *tab, unsigned
     for (int j = 0; j < kBins / kRowThreads; ++j) {
         m[j] = 0;
         if (j < per && tid * per + j < nb) {
-            for (int k = 0; k < c.C; ++k)
-                m[j] += ((unsigned long long)ld_peer_u32(peer_addr(hi + b0 + j, k)) << 32) + ld_peer_u32(peer_addr(lo + b0 + j, k));
+            uint32_t h[kRowMaxCluster], l[kRowMaxCluster];   // (all loads on their way before the first is added)
+#pragma unroll
+            for (int k = 0; k < kRowMaxCluster; ++k) {
+                h[k] = k < c.C ? ld_peer_u32(peer_addr(hi + b0 + j, k)) : 0u;
+                l[k] = k < c.C ? ld_peer_u32(peer_addr(lo + b0 + j, k)) : 0u;
+            }
+#pragma unroll
+            for (int k = 0; k < kRowMaxCluster; ++k) m[j] += ((unsigned long long)h[k] << 32) + l[k];
         }
         mine += m[j];
     }
@@ -684,17 +772,48 @@ __device__ Cut cut_mass(Ctx<F32> &c, const Scale &s, const float2 *tab, unsigned
     const uint32_t bin = sh->bin;
     const unsigned long long want = target - sh->bin_above;
 
-    // the step's elements
-    each_weight(c, s, tab, kept, [&](float x, int i, int g, int, int) {
-        if (bin_of(g, shift) != bin) return;
-        const uint32_t at = atomicAdd(&sh->nlist, 1u), k = key_of(x);
-        if (at < kListCap) list[at] = ((unsigned long long)k << 32) | (uint32_t)~(uint32_t)i;
-        else { atomicMin(&sh->bin_kmin, k); atomicMax(&sh->bin_kmax, k); }
-    });
+    // the step's elements: first by where its logits lie, generously, then exactly
+    const float unit = 1.f / (1024.f * s.chi), slack = 0x1p-20f * fabsf(s.top);
+    const float z_hi = s.hard ? s.top : s.top - ((float)(bin << shift) - 2.f) * unit * (1.f - 0x1p-20f) + slack;
+    const float z_lo = s.hard             ? s.top
+                       : bin == kBins - 1 ? -INFINITY
+                                          : s.top - ((float)((bin + 1) << shift) + 2.f) * unit * (1.f + 0x1p-20f) - slack;
+    for (int v = c.wb + (tid & 31); v < c.we; v += 32) {
+        constexpr int E = RowElem<F32>::kPer;
+        const uint4 x = c.get(v);
+        if (!(granule_max<F32>(x) >= z_lo)) continue;
+        float f[E];
+        granule_floats<F32>(x, f);
+        const int i0 = c.r.first(c.gb + v);
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            if (!(f[j] >= z_lo && f[j] <= z_hi) || !kept.keeps(f[j], i0 + j)) continue;
+            if (!s.hard) {
+                const Weights2 w = weights2(pack2(f[j], f[j]), s, tab);
+                if (!w.in[0] || bin_of(w.g[0], shift) != bin) continue;
+            }
+            const uint32_t at = atomicAdd(&sh->nlist, 1u), k = key_of(f[j]);
+            if (at < kListCap) list[at] = ((unsigned long long)k << 32) | (uint32_t)~(uint32_t)(i0 + j);
+            else { atomicMin(&sh->bin_kmin, k); atomicMax(&sh->bin_kmax, k); }
+        }
+    }
     bool ok;
     const int n = push_list(c, list, &ok);
     if (ok) {
-        if (c.rank == 0) {
+        if (c.rank == 0 && n <= kSmall) {
+            const Small e(list, n);
+            const unsigned long long w = e.on ? weight(key_float(e.key()), s, tab) : 0ull;
+            e.put_weight(list, w);
+            __syncthreads();
+            int rank;
+            unsigned long long above_w;
+            e.larger(list, n, &rank, &above_w);
+            if (e.on && e.part == 0 && above_w < want && want - above_w <= w)   // the last one kept (one thread)
+                for (int k = 0; k < c.C; ++k) {
+                    st_peer_u32(peer_addr(&sh->found_key, k), e.key());
+                    st_peer_u32(peer_addr(&sh->found_idx, k), (uint32_t)e.idx());
+                }
+        } else if (c.rank == 0) {
             sort_list(list, n);
             unsigned long long w[kListPer], sum = 0, all;
 #pragma unroll
@@ -748,14 +867,30 @@ __device__ Cut cut_mass(Ctx<F32> &c, const Scale &s, const float2 *tab, unsigned
     return cut;
 }
 
-// Brings the row in and finds its largest key and, for want > 0, a bound with at least `want` elements at or above
-// it (or below every element, if there are not so many).
+// Sends for a thread's first granules.
 template <bool F32>
-__device__ void load_row(Ctx<F32> &c, uint4 *cache, int want, uint32_t *kmax, uint32_t *bound)
+__device__ __forceinline__ void start_row(const Ctx<F32> &c, uint4 *cache)
+{
+    if (c.C > 1) cluster_arrive();   // (load_row waits)
+    const int end = min(c.we, c.cached);
+    for (int i = 0; i < kAhead; ++i) {
+        const int v = c.wb + (int)(threadIdx.x & 31) + 32 * i;
+        if (v < end) fetch_granule<F32>(c.r, c.gb + v, cache + v);
+        cp_async_commit();
+    }
+}
+
+// Brings the row in and finds its largest key and, for want > 0, a bound with at least `want` elements at or above
+// it (or below every element, if there are not so many).  scratch: kBoundBins words.
+constexpr int kBoundBins = 512;
+template <bool F32>
+__device__ void load_row(Ctx<F32> &c, uint4 *cache, int want, uint32_t *scratch, uint32_t *kmax, uint32_t *bound)
 {
     constexpr int NG = F32 ? 4 : 8;   // groups of a thread
     Shared *sh = c.sh;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    if (want > 0) scratch[tid] = 0u;
+    static_assert(kBoundBins == kRowThreads, "one word per thread");
     uint32_t gm[4] = {0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u};
     if constexpr (!F32)
         for (int k = 0; k < 4; ++k) gm[k] = 0xff80ff80u;
@@ -772,13 +907,7 @@ __device__ void load_row(Ctx<F32> &c, uint4 *cache, int want, uint32_t *kmax, ui
             gm[3] = bf16x2_max(gm[3], x.w);
         }
     };
-    if (c.C > 1) cluster_arrive();
     const int end = min(c.we, c.cached);
-    for (int i = 0; i < kAhead; ++i) {
-        const int v = c.wb + lane + 32 * i;
-        if (v < end) fetch_granule<F32>(c.r, c.gb + v, cache + v);
-        cp_async_commit();
-    }
     for (int v = c.wb + lane; v < end; v += 32) {
         cp_async_wait<kAhead - 1>();
         join(cache[v]);
@@ -788,7 +917,8 @@ __device__ void load_row(Ctx<F32> &c, uint4 *cache, int want, uint32_t *kmax, ui
     }
     for (int v = max(c.wb, c.cached) + lane; v < c.we; v += 32) join(load_granule<F32>(c.r, c.gb + v));
 
-    uint32_t key[NG], top = 0;
+    // the groups' keys, the largest and the least that is one
+    uint32_t key[NG], top = 0, least = 0xffffffffu;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         if constexpr (F32) {
@@ -799,38 +929,69 @@ __device__ void load_row(Ctx<F32> &c, uint4 *cache, int want, uint32_t *kmax, ui
         }
     }
 #pragma unroll
-    for (int k = 0; k < NG; ++k) top = max(top, key[k]);
+    for (int k = 0; k < NG; ++k) {
+        top = max(top, key[k]);
+        if (key[k] > kKeyNone) least = min(least, key[k]);
+    }
     top = __reduce_max_sync(0xffffffffu, top);
-    if (lane == 0) sh->ktop[warp] = top;
+    least = __reduce_min_sync(0xffffffffu, least);
+    if (lane == 0) {
+        sh->ktop[warp] = top;
+        sh->klow[warp] = least;
+    }
+    if (tid == 0) sh->border = kBoundBins;
     __syncthreads();
-    top = sh->ktop[lane & (kRowWarps - 1)];
-    top = __reduce_max_sync(0xffffffffu, top);
+    top = __reduce_max_sync(0xffffffffu, sh->ktop[lane & (kRowWarps - 1)]);
+    least = __reduce_min_sync(0xffffffffu, sh->klow[lane & (kRowWarps - 1)]);
 
     uint32_t low = kKeyNone + 1;
     if (want > 0) {
-        // the want-th largest of this CTA's group maxima, or a little below it
+        // a value that R of this CTA's group maxima reach: their histogram from the largest down, in equal steps
         const int R = (want + c.C - 1) / c.C;
-        constexpr int kShift = F32 ? 0 : 16;         // bf16 keys differ in their upper halves alone
-        uint32_t lo = (kKeyNone >> kShift) + (F32 ? 1 : 0), hi = (top >> kShift) + 1;   // count(lo) >= R is assumed: see below
-        int turn = 0;
-        while (hi - lo > 1) {
-            const uint32_t mid = lo + (hi - lo) / 2;
-            int n = 0;
+        const float ft = key_float(top), range = ft - key_float(least);
+        const float scale = range > 0.f && range < INFINITY ? (float)kBoundBins / range : 0.f;
+        const auto bin = [&](uint32_t k) { return (int)fminf((ft - key_float(k)) * scale, (float)(kBoundBins - 1)); };
 #pragma unroll
-            for (int k = 0; k < NG; ++k) n += (key[k] >> kShift) >= mid;
-            n = __reduce_add_sync(0xffffffffu, n);
-            if (lane == 0) sh->part[turn][warp] = n;
-            __syncthreads();
-            n = __reduce_add_sync(0xffffffffu, lane < kRowWarps ? sh->part[turn][lane] : 0);
-            turn ^= 1;
-            if (n >= R) {
-                lo = mid;
-                if (n <= R + (R >> 3)) break;
-            } else {
-                hi = mid;
+        for (int k = 0; k < NG; ++k)
+            if (key[k] > kKeyNone) atomicAdd(scratch + (scale > 0.f ? bin(key[k]) : 0), 1u);
+        __syncthreads();
+        if (warp == 0) {
+            constexpr int kPer = kBoundBins / 32;
+            uint32_t n[kPer], sum = 0;
+#pragma unroll
+            for (int k = 0; k < kPer; ++k) {
+                n[k] = scratch[lane * kPer + k];
+                sum += n[k];
+            }
+            uint32_t incl = sum;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const uint32_t u = __shfl_up_sync(0xffffffffu, incl, o);
+                if (lane >= o) incl += u;
+            }
+            uint32_t run = incl - sum;
+            if (run < (uint32_t)R && incl >= (uint32_t)R) {   // (at most one lane)
+                int b = lane * kPer;
+#pragma unroll
+                for (int k = 0; k < kPer; ++k) {
+                    run += n[k];
+                    b += run < (uint32_t)R;
+                }
+                sh->border = b;
             }
         }
-        low = max(lo << kShift, kKeyNone + 1);   // the search ends at its lower end if there are fewer than R
+        __syncthreads();
+        // the least group maximum down to that step; everything, where there are fewer than R
+        const int border = sh->border;
+        uint32_t at = 0xffffffffu;
+#pragma unroll
+        for (int k = 0; k < NG; ++k)
+            if (key[k] > kKeyNone && (scale > 0.f ? bin(key[k]) : 0) <= border) at = min(at, key[k]);
+        at = __reduce_min_sync(0xffffffffu, at);
+        if (lane == 0) sh->klow[warp] = at;
+        __syncthreads();
+        at = __reduce_min_sync(0xffffffffu, sh->klow[lane & (kRowWarps - 1)]);
+        if (border < kBoundBins) low = at;
     }
     if (c.C > 1) {
         cluster_wait();
@@ -886,9 +1047,9 @@ __device__ int lowest_at(Ctx<F32> &c, uint32_t kmax)
     }
     best = __reduce_min_sync(0xffffffffu, best);
     __syncthreads();
-    if ((threadIdx.x & 31) == 0) c.sh->part[0][threadIdx.x >> 5] = best;
+    if ((threadIdx.x & 31) == 0) c.sh->part[threadIdx.x >> 5] = best;
     __syncthreads();
-    best = __reduce_min_sync(0xffffffffu, c.sh->part[0][threadIdx.x & (kRowWarps - 1)]);
+    best = __reduce_min_sync(0xffffffffu, c.sh->part[threadIdx.x & (kRowWarps - 1)]);
     const unsigned long long *slot = cluster_gather(c, (unsigned long long)(unsigned)best);
     for (int k = 0; k < c.C; ++k) best = min(best, (int)(unsigned)slot[k]);
     return best;
@@ -912,8 +1073,9 @@ __global__ void __launch_bounds__(kRowThreads, 2) top_kernel(const TopParams p)
     unsigned long long *list = reinterpret_cast<unsigned long long *>(smem + p.cached);
     Ctx<F32> c{Row<F32>(p.z, row, p.ld, p.V)};
     set_ctx(c, smem, p.cached, p.cluster, &sh);
+    start_row(c, smem);
     uint32_t kmax, bound;
-    load_row(c, smem, p.K, &kmax, &bound);
+    load_row(c, smem, p.K, reinterpret_cast<uint32_t *>(list), &kmax, &bound);
     bool ok;
     int n = gather_list(c, list, bound, Cut{kKeyNone, INT_MIN}, &ok);
     if (!ok) {   // (the same in every CTA of the row)
@@ -921,6 +1083,19 @@ __global__ void __launch_bounds__(kRowThreads, 2) top_kernel(const TopParams p)
         n = gather_list(c, list, max(cut.key, kKeyNone + 1), cut, &ok);   // at most K
     }
     if (c.rank != 0) return;   // (nobody reads this CTA's memory any more)
+    if (n <= kSmall) {
+        const Small e(list, n);
+        const int at = e.larger(list, n);
+        if (e.on && e.part == 0 && at < p.K) {
+            p.values[(size_t)row * p.K + at] = key_float(e.key());
+            p.idx[(size_t)row * p.K + at] = e.idx();
+        }
+        for (int i = n + threadIdx.x; i < p.K; i += kRowThreads) {
+            p.values[(size_t)row * p.K + i] = -INFINITY;
+            p.idx[(size_t)row * p.K + i] = -1;
+        }
+        return;
+    }
     sort_list(list, n);
     for (int i = threadIdx.x; i < p.K; i += kRowThreads) {
         const unsigned long long e = i < n ? list[i] : 0ull;
@@ -965,6 +1140,9 @@ __global__ void __launch_bounds__(kRowThreads, 2) sample_kernel(const SamplePara
     __shared__ float2 tab[1024];
     const int row = blockIdx.x / p.cluster, tid = threadIdx.x;
     unsigned long long *list = reinterpret_cast<unsigned long long *>(smem + p.cached);
+    Ctx<F32> c{Row<F32>(p.z, row, p.ld, p.V)};
+    set_ctx(c, smem, p.cached, p.cluster, &sh);
+    start_row(c, smem);
     const float T = p.temperature ? p.temperature[row] : 1.f;
     const float top_p = p.top_p ? p.top_p[row] : 1.f, min_p = p.min_p ? p.min_p[row] : 0.f;
     const float u = p.u[row];
@@ -974,6 +1152,8 @@ __global__ void __launch_bounds__(kRowThreads, 2) sample_kernel(const SamplePara
             put_sample(p, row, -1, __int_as_float(0x7fffffff), 0);
             if (p.status) atomicOr(p.status, kStatusBadToken);
         }
+        cp_async_wait<0>();
+        if (c.C > 1) cluster_wait();
         return;   // (every CTA of the row)
     }
     if (k < 0 || k >= p.V) k = 0;
@@ -982,10 +1162,8 @@ __global__ void __launch_bounds__(kRowThreads, 2) sample_kernel(const SamplePara
     const int want = !greedy && k > 0 && k <= kMaxTop ? k : 0;   // what the list serves
     if (!greedy)
         for (int i = tid; i < 1024; i += kRowThreads) tab[i] = kExp2.v[i];
-    Ctx<F32> c{Row<F32>(p.z, row, p.ld, p.V)};
-    set_ctx(c, smem, p.cached, p.cluster, &sh);
     uint32_t kmax, bound;
-    load_row(c, smem, want, &kmax, &bound);
+    load_row(c, smem, want, reinterpret_cast<uint32_t *>(list), &kmax, &bound);
     if (kmax <= kKeyNone) {   // nothing can be drawn
         if (c.rank == 0 && tid == 0) put_sample(p, row, -1, -INFINITY, 0);
         return;
@@ -1015,6 +1193,27 @@ __global__ void __launch_bounds__(kRowThreads, 2) sample_kernel(const SamplePara
         const int n = gather_list(c, list, bound, Cut{kKeyNone, INT_MIN}, &ok);
         if (ok) {   // (the same in every CTA of the row)
             if (c.rank != 0) return;   // (nobody reads this CTA's memory any more)
+            if (n <= kSmall) {
+                const Small e(list, n);
+                const unsigned long long w = e.on ? weight(key_float(e.key()), s, tab) : 0ull;
+                e.put_weight(list, w);
+                __syncthreads();
+                int at;
+                unsigned long long above;
+                e.larger(list, n, &at, &above);
+                bool kept = e.on && at < k && e.key() >= kminp;
+                if (nucleus) {
+                    const unsigned long long Z = block_sum_u64(e.on && e.part == 0 && at < k ? w : 0ull, &sh);
+                    kept = kept && above < share_ceil(top_p, Z);
+                }
+                const int m = __syncthreads_count(kept && e.part == 0);
+                e.put_weight(list, kept ? w : 0ull);
+                const unsigned long long total = block_sum_u64(kept && e.part == 0 ? w : 0ull, &sh);
+                const unsigned long long before = e.earlier(list, n), target = share_floor(u, total);
+                if (kept && e.part == 0 && target >= before && target - before < w)   // one entry
+                    put_sample(p, row, e.idx(), log_share(key_float(e.key()), T, s, total), m);
+                return;
+            }
             sort_list(list, n);
             int m = min(n, k);
             unsigned long long w[kListPer], sum = 0, total;
@@ -1079,11 +1278,12 @@ __global__ void __launch_bounds__(kRowThreads, 2) sample_kernel(const SamplePara
     unsigned long long sum = 0;
     int n = 0;
     for (int v = c.wb + (tid & 31); v < c.we; v += 32) sum += kept.granule(c, v, n);
-    const unsigned long long count = cluster_sum(c, (unsigned long long)(unsigned)n);
+    n = (int)__reduce_add_sync(0xffffffffu, n);
+    if ((tid & 31) == 0) sh.part[tid >> 5] = n;
     const unsigned long long mine = block_sum_u64(sum, &sh);
-    const unsigned long long *slot = cluster_gather(c, mine);
-    unsigned long long total = 0;
-    for (int q = 0; q < c.C; ++q) total += slot[q];
+    n = __reduce_add_sync(0xffffffffu, (tid & 31) < kRowWarps ? sh.part[tid & 31] : 0);
+    const unsigned long long *slot = cluster_gather(c, mine, (unsigned long long)(unsigned)n);
+    const unsigned long long total = slot_sum(slot, c.C), count = slot_sum(slot + kRowMaxCluster, c.C);
     int id;
     uint32_t key;
     locate(c, share_floor(u, total), kept, mine, slot, &id, &key);
