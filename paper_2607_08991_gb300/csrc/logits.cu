@@ -198,8 +198,9 @@ struct Shared {
     int found_idx;
     uint32_t found_key;
     uint32_t kminp;
-    uint32_t bin, bin_kmin, bin_kmax;                // the nucleus' border
-    unsigned long long bin_above;
+    // the nucleus: steps of the border, and of each CTA the entries, the tokens kept and their mass
+    uint32_t bin0, bin1, cnt[kRowMaxCluster], above[kRowMaxCluster];
+    unsigned long long mass[kRowMaxCluster];
 };
 
 template <bool F32>
@@ -371,18 +372,18 @@ __device__ __forceinline__ unsigned long long thread_sum(const Ctx<F32> &c, cons
 }
 
 // The first token in the vocabulary's order at which the running sum of f passes `target` (which is below the sum
-// over the row): *idx, *key in every CTA.  The warps' sums are in sh->wsum (block_sum_u64 of thread_sum), the CTA's is
-// `mine`, the CTAs' are in `slot`.  The CTA that holds the token narrows a run of granules down
+// over the row): found(idx, key) by one thread.  The warps' sums are in sh->wsum (block_sum_u64 of thread_sum), the
+// CTAs' are in `slot`.  The CTA that holds the token narrows a run of granules down
 // sixteenfold a step until its threads have a few elements each.
-template <bool F32, typename S>
-__device__ void locate(Ctx<F32> &c, unsigned long long target, const S &f, unsigned long long mine,
-                       const unsigned long long *slot, int *idx, uint32_t *key)
+template <bool F32, typename S, typename Found>
+__device__ __forceinline__ void locate(Ctx<F32> &c, unsigned long long target, const S &f,
+                                       const unsigned long long *slot, Found found)
 {
     Shared *sh = c.sh;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     unsigned long long before = 0;
     for (unsigned k = 0; k < c.rank; ++k) before += slot[k];
-    if (target >= before && target - before < mine) {   // (one CTA)
+    if (target >= before && target - before < slot[c.rank]) {   // (one CTA)
         unsigned long long t = target - before;
         int a = 0, b = c.n, per = (c.n + kRowWarps - 1) / kRowWarps;
         for (;;) {
@@ -416,25 +417,28 @@ __device__ void locate(Ctx<F32> &c, unsigned long long target, const S &f, unsig
                 run += at(e, &k);
                 if (run > t || e == last) break;   // (t is below the sum of the thread's elements)
             }
-            for (int q = 0; q < c.C; ++q) {
-                st_peer_u32(peer_addr(&sh->found_idx, q), (uint32_t)(i0 + e));
-                st_peer_u32(peer_addr(&sh->found_key, q), k);
-            }
+            found(i0 + e, k);
         }
     }
-    if (c.C > 1) cluster_sync_all();
-    else __syncthreads();
-    *idx = sh->found_idx;
-    *key = sh->found_key;
 }
 
-// The same, with the sums to be taken first.
+// The same, with the sums to be taken first; *idx, *key in every CTA.
 template <bool F32, typename S>
 __device__ void sum_and_locate(Ctx<F32> &c, unsigned long long target, const S &f, int *idx, uint32_t *key)
 {
     const unsigned long long mine = block_sum_u64(thread_sum(c, f), c.sh);
     const unsigned long long *slot = cluster_gather(c, mine);
-    locate(c, target, f, mine, slot, idx, key);
+    Shared *sh = c.sh;
+    locate(c, target, f, slot, [&](int i, uint32_t k) {
+        for (int q = 0; q < c.C; ++q) {
+            st_peer_u32(peer_addr(&sh->found_idx, q), (uint32_t)i);
+            st_peer_u32(peer_addr(&sh->found_key, q), k);
+        }
+    });
+    if (c.C > 1) cluster_sync_all();
+    else __syncthreads();
+    *idx = sh->found_idx;
+    *key = sh->found_key;
 }
 
 // The largest key at which sum(f over keys >= it) is at least `want` (1 <= want <= the sum over all): between kmin and
@@ -671,193 +675,27 @@ struct Small {
 };
 
 // ------------------------------------------------------------------ the nucleus
-// The masses of 2048 steps of the weight, in whole numbers: a word for their lower 32 bits and one for what is above.
+// Where the mass from the top reaches a share of the whole, in two passes over the row.  The first counts the tokens in
+// 2048 equal steps of the weight's logarithm, each as 4096 times its weight relative to the middle of its step (right
+// to kOff): no exponential, one addition in shared memory a token.  From all CTAs' counts follow the steps in which the
+// border can lie, as a rule one or two.  The second pass takes the exact weights: of all tokens, of the ones above these
+// steps, and a list of the ones within, which settles the border; that it lies there at all is checked.
 constexpr int kBins = 2048;
-static_assert(2 * kBins * 4 <= kListCap * 8, "the histogram lies where the list does");
+static_assert(2 * kBins * 4 <= kListCap * 8, "the counts, and their exchange, lie where the list does");
+// Half a 1 / 1024 octave, the straight line instead of the power within a step, the rounding to 1 / 4096.
+constexpr float kOff = 7e-4f;
 
-// The step (of 1 / 1024 octave << shift, from the top down) of a weight; the same function in both of its uses.
-__device__ __forceinline__ uint32_t bin_of(int g, int shift) { return min((uint32_t)(-g) >> shift, (uint32_t)kBins - 1u); }
+struct Nucleus {
+    Cut cut;
+    bool sums;   // sh->wsum has the warps' kept mass, sh->mass and sh->above the CTAs' and their numbers of kept tokens
+};
 
-template <bool F32, typename F>
-__device__ __forceinline__ void each_weight(const Ctx<F32> &c, const Scale &s, const float2 *tab, const KeptMass &kept, F f)
-{
-    constexpr int P = RowElem<F32>::kPer / 2;
-    for (int v = c.wb + (int)(threadIdx.x & 31); v < c.we; v += 32) {
-        const uint4 x = c.get(v);
-        if (!(granule_max<F32>(x) >= kept.at)) continue;
-        f32x2 z[P];
-        granule_pairs<F32>(x, z);
-        const int i0 = c.r.first(c.gb + v);
-#pragma unroll
-        for (int j = 0; j < P; ++j) {
-            const float2 y = unpack2(z[j]);
-            if (s.hard) {
-                if (y.x == s.top && kept.keeps(y.x, i0 + 2 * j)) f(y.x, i0 + 2 * j, 0, 1 << 21, 0);
-                if (y.y == s.top && kept.keeps(y.y, i0 + 2 * j + 1)) f(y.y, i0 + 2 * j + 1, 0, 1 << 21, 0);
-            } else {
-                const Weights2 w = weights2(z[j], s, tab);
-                if (w.in[0] && kept.keeps(y.x, i0 + 2 * j)) f(y.x, i0 + 2 * j, w.g[0], w.i1[0], w.i2[0]);
-                if (w.in[1] && kept.keeps(y.y, i0 + 2 * j + 1)) f(y.y, i0 + 2 * j + 1, w.g[1], w.i1[1], w.i2[1]);
-            }
-        }
-    }
-}
-
-// The cut that keeps, of what by_k keeps, the largest up to a share top_p < 1 of the mass: the step in which the mass
-// from the top reaches it, by a histogram of masses, and the place within the step by sorting its elements.
+// Ties at one key, `above` the mass before them: the cut at the first of them with which the mass reaches `want`.
 template <bool F32>
-__device__ Cut cut_mass(Ctx<F32> &c, const Scale &s, const float2 *tab, unsigned long long *list, Cut by_k, float top_p)
+__device__ Cut cut_ties(Ctx<F32> &c, uint32_t key, unsigned long long w, unsigned long long above,
+                        unsigned long long want, Cut by_k)
 {
-    Shared *sh = c.sh;
-    const int tid = threadIdx.x;
-    uint32_t *lo = reinterpret_cast<uint32_t *>(list), *hi = lo + kBins;
-    // steps as fine as 32 logits, or what weighs more than 2^-64, allow
-    int shift = 0;
-    while (shift < 5 && (float)(2 << shift) < 32.f * s.chi) ++shift;
-    for (int i = tid; i < 2 * kBins; i += kRowThreads) lo[i] = 0u;
-    __syncthreads();
-    const KeptMass kept(s, tab, by_k);
-    each_weight(c, s, tab, kept, [&](float, int, int g, int i1, int i2) {
-        const unsigned long long w = whole_weight(i1, i2, s);
-        if (w == 0) return;
-        const uint32_t b = bin_of(g, shift), wl = (uint32_t)w, was = atomicAdd(lo + b, wl);
-        const uint32_t up = (uint32_t)(w >> 32) + (was + wl < was ? 1u : 0u);
-        if (up) atomicAdd(hi + b, up);
-    });
-    if (c.C > 1) cluster_sync_all();
-    else __syncthreads();
-    // a run of steps per CTA, over all CTAs' histograms
-    const int nb = kBins / c.C, per = (nb + kRowThreads - 1) / kRowThreads, b0 = (int)c.rank * nb + tid * per;
-    unsigned long long m[kBins / kRowThreads], mine = 0;
-#pragma unroll
-    for (int j = 0; j < kBins / kRowThreads; ++j) {
-        m[j] = 0;
-        if (j < per && tid * per + j < nb) {
-            uint32_t h[kRowMaxCluster], l[kRowMaxCluster];   // (all loads on their way before the first is added)
-#pragma unroll
-            for (int k = 0; k < kRowMaxCluster; ++k) {
-                h[k] = k < c.C ? ld_peer_u32(peer_addr(hi + b0 + j, k)) : 0u;
-                l[k] = k < c.C ? ld_peer_u32(peer_addr(lo + b0 + j, k)) : 0u;
-            }
-#pragma unroll
-            for (int k = 0; k < kRowMaxCluster; ++k) m[j] += ((unsigned long long)h[k] << 32) + l[k];
-        }
-        mine += m[j];
-    }
-    unsigned long long total;
-    unsigned long long run = block_scan_u64(mine, sh, &total);
-    const unsigned long long *slot = cluster_gather(c, total);
-    unsigned long long Z = 0;
-    for (int k = 0; k < c.C; ++k) {
-        if (k < (int)c.rank) run += slot[k];
-        Z += slot[k];
-    }
-    const unsigned long long target = share_ceil(top_p, Z);   // 1 <= target <= Z
-#pragma unroll
-    for (int j = 0; j < kBins / kRowThreads; ++j) {
-        if (run < target && target - run <= m[j])   // (one thread)
-            for (int k = 0; k < c.C; ++k) {
-                st_peer_u32(peer_addr(&sh->bin, k), (uint32_t)(b0 + j));
-                st_peer_u64(peer_addr(&sh->bin_above, k), run);
-            }
-        run += m[j];
-    }
-    if (tid == 0) {
-        sh->nlist = 0;
-        sh->bin_kmin = 0xffffffffu;
-        sh->bin_kmax = 0u;
-    }
-    if (c.C > 1) cluster_sync_all();
-    else __syncthreads();
-    const uint32_t bin = sh->bin;
-    const unsigned long long want = target - sh->bin_above;
-
-    // the step's elements: first by where its logits lie, generously, then exactly
-    const float unit = 1.f / (1024.f * s.chi), slack = 0x1p-20f * fabsf(s.top);
-    const float z_hi = s.hard ? s.top : s.top - ((float)(bin << shift) - 2.f) * unit * (1.f - 0x1p-20f) + slack;
-    const float z_lo = s.hard             ? s.top
-                       : bin == kBins - 1 ? -INFINITY
-                                          : s.top - ((float)((bin + 1) << shift) + 2.f) * unit * (1.f + 0x1p-20f) - slack;
-    for (int v = c.wb + (tid & 31); v < c.we; v += 32) {
-        constexpr int E = RowElem<F32>::kPer;
-        const uint4 x = c.get(v);
-        if (!(granule_max<F32>(x) >= z_lo)) continue;
-        float f[E];
-        granule_floats<F32>(x, f);
-        const int i0 = c.r.first(c.gb + v);
-#pragma unroll
-        for (int j = 0; j < E; ++j) {
-            if (!(f[j] >= z_lo && f[j] <= z_hi) || !kept.keeps(f[j], i0 + j)) continue;
-            if (!s.hard) {
-                const Weights2 w = weights2(pack2(f[j], f[j]), s, tab);
-                if (!w.in[0] || bin_of(w.g[0], shift) != bin) continue;
-            }
-            const uint32_t at = atomicAdd(&sh->nlist, 1u), k = key_of(f[j]);
-            if (at < kListCap) list[at] = ((unsigned long long)k << 32) | (uint32_t)~(uint32_t)(i0 + j);
-            else { atomicMin(&sh->bin_kmin, k); atomicMax(&sh->bin_kmax, k); }
-        }
-    }
-    bool ok;
-    const int n = push_list(c, list, &ok);
-    if (ok) {
-        if (c.rank == 0 && n <= kSmall) {
-            const Small e(list, n);
-            const unsigned long long w = e.on ? weight(key_float(e.key()), s, tab) : 0ull;
-            e.put_weight(list, w);
-            __syncthreads();
-            int rank;
-            unsigned long long above_w;
-            e.larger(list, n, &rank, &above_w);
-            if (e.on && e.part == 0 && above_w < want && want - above_w <= w)   // the last one kept (one thread)
-                for (int k = 0; k < c.C; ++k) {
-                    st_peer_u32(peer_addr(&sh->found_key, k), e.key());
-                    st_peer_u32(peer_addr(&sh->found_idx, k), (uint32_t)e.idx());
-                }
-        } else if (c.rank == 0) {
-            sort_list(list, n);
-            unsigned long long w[kListPer], sum = 0, all;
-#pragma unroll
-            for (int j = 0; j < kListPer; ++j) {
-                const int i = tid * kListPer + j;
-                w[j] = i < n ? weight(key_float((uint32_t)(list[i] >> 32)), s, tab) : 0ull;
-                sum += w[j];
-            }
-            unsigned long long at = block_scan_u64(sum, sh, &all);
-#pragma unroll
-            for (int j = 0; j < kListPer; ++j) {
-                if (at < want && want - at <= w[j]) {   // the last one kept (one thread)
-                    const unsigned long long e = list[tid * kListPer + j];
-                    for (int k = 0; k < c.C; ++k) {
-                        st_peer_u32(peer_addr(&sh->found_key, k), (uint32_t)(e >> 32));
-                        st_peer_u32(peer_addr(&sh->found_idx, k), ~(uint32_t)e);
-                    }
-                }
-                at += w[j];
-            }
-        }
-        if (c.C > 1) cluster_sync_all();
-        else __syncthreads();
-        return Cut{sh->found_key, sh->found_idx};
-    }
-    // more of them than the list holds, as a rule equal ones: the key by bisection among the step's, then the ties
-    for (uint32_t i = tid; i < min(sh->nlist, (uint32_t)kListCap); i += kRowThreads) {
-        atomicMin(&sh->bin_kmin, (uint32_t)(list[i] >> 32));
-        atomicMax(&sh->bin_kmax, (uint32_t)(list[i] >> 32));
-    }
-    __syncthreads();
-    slot = cluster_gather(c, ((unsigned long long)sh->bin_kmin << 32) | sh->bin_kmax);
-    uint32_t kmin = 0xffffffffu, kmax = 0u;
-    for (int k = 0; k < c.C; ++k) {
-        kmin = min(kmin, (uint32_t)(slot[k] >> 32));
-        kmax = max(kmax, (uint32_t)slot[k]);
-    }
-    const auto in_step = [&](float x, uint32_t q, int i) {
-        return q >= kmin && q <= kmax && by_k.keeps(q, i) ? weight(x, s, tab) : 0ull;
-    };
-    unsigned long long above;
-    const uint32_t key = bisect_key(c, kmin, kmax, want, in_step, &above);
-    const unsigned long long w = weight(key_float(key), s, tab);
-    const unsigned long long ties = (want - above + w - 1ull) / w;   // the first of them that reach the mass
+    const unsigned long long ties = (want - above + w - 1ull) / w;
     Cut cut;
     uint32_t at;
     sum_and_locate(c, ties - 1ull,
@@ -865,6 +703,270 @@ __device__ Cut cut_mass(Ctx<F32> &c, const Scale &s, const float2 *tab, unsigned
                    &cut.idx, &at);
     cut.key = key;
     return cut;
+}
+
+// The cut that keeps, of what by_k keeps, the largest up to a share top_p < 1 of the mass, by counts and exact weights;
+// false (the same in every CTA of the row) where the border does not lie where the counts have it, or among more
+// tokens than the list holds.
+template <bool F32>
+__device__ bool cut_by_counts(Ctx<F32> &c, const Scale &s, const float2 *tab, unsigned long long *list, Cut by_k,
+                              float top_p, Nucleus *res)
+{
+    constexpr int E = RowElem<F32>::kPer, P = E / 2;
+    Shared *sh = c.sh;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, C = c.C;
+    const KeptMass all(s, tab, by_k);
+    const bool filtered = by_k.key > kKeyNone;
+    // steps as fine as 128 logits, or what weighs more than 2^-64, allow
+    int shift = 0;
+    while (shift < 5 && (float)(2 << shift) < 128.f * s.chi) ++shift;
+    uint32_t *count = reinterpret_cast<uint32_t *>(list), *got = count + kBins;
+    for (int i = tid; i < kBins / 4; i += kRowThreads) reinterpret_cast<uint4 *>(count)[i] = make_uint4(0, 0, 0, 0);
+    __syncthreads();
+    {
+        const f32x2 nt = pack2(-s.top, -s.top), chi = pack2(s.chi, s.chi), magic = pack2(kMagicG, kMagicG);
+        const uint32_t mask = (1u << shift) - 1u;
+        const auto add = [&](float p, float m) {
+            if (!(p > -60.f)) return;
+            const uint32_t d = (uint32_t)(__float_as_int(kMagicG) - __float_as_int(m));   // 1 / 1024 octaves below the top
+            const int v = 4096 + (((int)mask - 2 * (int)(d & mask)) * 2839 >> 11);         // ln 2 * 2 = 2839 / 2048
+            atomicAdd(count + min(d >> shift, (uint32_t)kBins - 1u), (uint32_t)v);
+        };
+        for (int v = c.wb + lane; v < c.we; v += 32) {
+            f32x2 z[P];
+            granule_pairs<F32>(c.get(v), z);
+            const int i0 = c.r.first(c.gb + v);
+#pragma unroll
+            for (int j = 0; j < P; ++j) {
+                const f32x2 p2 = fmul2(fadd2(z[j], nt), chi);   // (as weights2 does)
+                const float2 y = unpack2(z[j]), p = unpack2(p2), m = unpack2(fadd2(p2, magic));
+                if (!filtered || all.keeps(y.x, i0 + 2 * j)) add(p.x, m.x);
+                if (!filtered || all.keeps(y.y, i0 + 2 * j + 1)) add(p.y, m.y);
+            }
+        }
+    }
+    __syncthreads();
+    // a run of steps per CTA: its counts in all CTAs
+    const int nb = kBins / C;
+    if (C > 1) {
+        const uint4 q = reinterpret_cast<const uint4 *>(count)[tid];
+        const int b = 4 * tid;
+        st_peer_v4(peer_addr(got + c.rank * nb + b % nb, b / nb), __uint_as_float(q.x), __uint_as_float(q.y),
+                   __uint_as_float(q.z), __uint_as_float(q.w));
+        cluster_sync_all();
+    } else {
+        got = count;
+    }
+    constexpr int kMost = kBins / kRowThreads;
+    const int per = (nb + kRowThreads - 1) / kRowThreads;
+    unsigned long long m[kMost], mine = 0;   // masses in whole numbers: their sums are the same in every CTA
+#pragma unroll
+    for (int j = 0; j < kMost; ++j) {
+        const int b = tid * per + j;
+        m[j] = 0;
+        if (j < per && b < nb) {
+            unsigned long long n = 0;
+            for (int k = 0; k < C; ++k) n += got[k * nb + b];
+            const float mid = ((float)((c.rank * nb + b) << shift) + 0.5f * (float)(1 << shift)) * (1.f / 1024.f);
+            m[j] = (unsigned long long)__float2ll_rn((float)n * exp2f(20.f - mid));
+        }
+        mine += m[j];
+    }
+    unsigned long long total;
+    unsigned long long run = block_scan_u64(mine, sh, &total);
+    const unsigned long long *slot = cluster_gather(c, total);
+    unsigned long long Zs = slot_sum(slot, C);
+    for (unsigned k = 0; k < c.rank; ++k) run += slot[k];
+    {
+        const float rest = 1.f - top_p;
+        const auto reached = [&](unsigned long long cum, float off) {   // cum / Z >= top_p, both sides off by a factor
+            return (float)cum * (rest * (1.f + off)) >= (float)(Zs - cum) * (top_p * (1.f - off));
+        };
+#pragma unroll
+        for (int j = 0; j < kMost; ++j) {
+            if (m[j] != 0) {
+                const uint32_t b = c.rank * nb + tid * per + j;
+                if (!reached(run, kOff) && reached(run + m[j], kOff))   // (one thread)
+                    for (int k = 0; k < C; ++k) st_peer_u32(peer_addr(&sh->bin0, k), b);
+                if (!reached(run, -kOff) && reached(run + m[j], -kOff))   // (one thread)
+                    for (int k = 0; k < C; ++k) st_peer_u32(peer_addr(&sh->bin1, k), b);
+            }
+            run += m[j];
+        }
+    }
+    if (tid == 0) sh->nlist = 0;
+    if (C > 1) cluster_sync_all();
+    else __syncthreads();
+
+    // exact weights; each CTA's entries have a part of the list of their own, in every CTA
+    const int seg = kListCap / C;
+    unsigned long long *own = list + c.rank * seg;
+    const int d0 = (int)sh->bin0 << shift, d1 = sh->bin1 >= kBins - 1u ? INT_MAX : (int)(sh->bin1 + 1u) << shift;
+    unsigned long long w_all = 0, w_above = 0;
+    int n_above = 0;
+    for (int v = c.wb + lane; v < c.we; v += 32) {
+        const uint4 x = c.get(v);
+        if (!(granule_max<F32>(x) >= all.at)) continue;
+        f32x2 z[P];
+        granule_pairs<F32>(x, z);
+        const int i0 = c.r.first(c.gb + v);
+        int a1 = 0, a2 = 0, t1 = 0, t2 = 0;
+#pragma unroll
+        for (int j = 0; j < P; ++j) {
+            const Weights2 w = weights2(z[j], s, tab);
+            const float2 y = unpack2(z[j]);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const float f = h ? y.y : y.x;
+                const int i = i0 + 2 * j + h, d = -w.g[h];
+                const bool in = w.in[h] && (!filtered || all.keeps(f, i));
+                if (in) { t1 += w.i1[h]; t2 += w.i2[h]; }
+                if (in && d < d0) { a1 += w.i1[h]; a2 += w.i2[h]; ++n_above; }
+                if (in && d >= d0 && d < d1) {
+                    const uint32_t at = atomicAdd(&sh->nlist, 1u);
+                    if (at < (uint32_t)seg) own[at] = ((unsigned long long)key_of(f) << 32) | (uint32_t)~(uint32_t)i;
+                }
+            }
+        }
+        w_all += whole_weight(t1, t2, s);
+        w_above += whole_weight(a1, a2, s);
+    }
+    w_all = warp_sum_u64(w_all);
+    w_above = warp_sum_u64(w_above);
+    n_above = (int)__reduce_add_sync(0xffffffffu, n_above);
+    if (lane == 0) {
+        sh->scan[warp] = w_all;
+        sh->wsum[warp] = w_above;
+        sh->part[warp] = n_above;
+    }
+    __syncthreads();
+    w_all = w_above = 0;
+    for (int w = 0; w < kRowWarps; ++w) {
+        w_all += sh->scan[w];
+        w_above += sh->wsum[w];
+    }
+    n_above = (int)__reduce_add_sync(0xffffffffu, lane < kRowWarps ? sh->part[lane] : 0);
+    const int here = (int)sh->nlist;
+    if (here <= seg)
+        for (int q = 1; q < C; ++q) {   // (each CTA begins with its neighbour)
+            const unsigned to = (c.rank + q) % C;
+            for (int i = tid; i < here; i += kRowThreads) st_peer_u64(peer_addr(own + i, to), own[i]);
+        }
+    if (tid < C) {
+        st_peer_u32(peer_addr(&sh->cnt[c.rank], tid), (uint32_t)here);
+        st_peer_u32(peer_addr(&sh->above[c.rank], tid), (uint32_t)n_above);
+    }
+    slot = cluster_gather(c, w_all, w_above);
+    const unsigned long long Z = slot_sum(slot, C), A = slot_sum(slot + kRowMaxCluster, C), target = share_ceil(top_p, Z);
+    int n = 0, off = 0;   // entries; of the CTAs before this one
+    bool fits = A < target;
+    for (int k = 0; k < C; ++k) {
+        fits = fits && sh->cnt[k] <= (uint32_t)seg;
+        if (k < (int)c.rank) off += (int)sh->cnt[k];
+        n += (int)sh->cnt[k];
+    }
+    if (!fits || n == 0) return false;
+    const unsigned long long want = target - A;
+    // every CTA does what follows: the entries one behind another, and the last one that is kept
+    if (tid == 0) sh->found_idx = -1;
+    {
+        unsigned long long e[kListPer];
+#pragma unroll
+        for (int j = 0; j < kListPer; ++j) {
+            int i = tid + j * kRowThreads, k = 0, from = 0;
+            e[j] = 0;
+            if (i < n) {
+                while (i - from >= (int)sh->cnt[k]) from += (int)sh->cnt[k++];
+                e[j] = list[k * seg + i - from];
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < kListPer; ++j)
+            if (tid + j * kRowThreads < n) list[tid + j * kRowThreads] = e[j];
+        __syncthreads();
+    }
+    if (n <= kSmall) {
+        const Small m(list, n);
+        const unsigned long long w = m.on ? weight(key_float(m.key()), s, tab) : 0ull;
+        m.put_weight(list, w);
+        __syncthreads();
+        int rank;
+        unsigned long long before;
+        m.larger(list, n, &rank, &before);
+        if (m.on && m.part == 0 && before < want && want - before <= w) {   // (one thread)
+            sh->found_key = m.key();
+            sh->found_idx = m.idx();
+        }
+    } else {
+        sort_list(list, n);
+        unsigned long long w[kListPer], sum = 0, rest;
+#pragma unroll
+        for (int j = 0; j < kListPer; ++j) {
+            const int i = tid * kListPer + j;
+            w[j] = i < n ? weight(key_float((uint32_t)(list[i] >> 32)), s, tab) : 0ull;
+            sum += w[j];
+        }
+        unsigned long long before = block_scan_u64(sum, sh, &rest);
+#pragma unroll
+        for (int j = 0; j < kListPer; ++j) {
+            if (before < want && want - before <= w[j]) {   // (one thread)
+                const unsigned long long x = list[tid * kListPer + j];
+                sh->found_key = (uint32_t)(x >> 32);
+                sh->found_idx = (int)~(uint32_t)x;
+            }
+            before += w[j];
+        }
+    }
+    __syncthreads();
+    const Cut cut{sh->found_key, sh->found_idx};
+    *res = Nucleus{cut, false};
+    if (cut.idx < 0 || n > kSmall) return cut.idx >= 0;
+    // what is kept of the CTAs, a warp each; then of this CTA's warps
+    if (warp < C) {
+        int from = 0;
+        for (int k = 0; k < warp; ++k) from += (int)sh->cnt[k];
+        unsigned long long w = 0;
+        int kept = 0;
+        for (int i = from + lane; i < from + (int)sh->cnt[warp]; i += 32)
+            if (cut.keeps((uint32_t)(list[i] >> 32), (int)~(uint32_t)list[i])) {
+                w += list[kSmall + i];
+                ++kept;
+            }
+        w = warp_sum_u64(w);
+        kept = (int)__reduce_add_sync(0xffffffffu, kept);
+        if (lane == 0) {
+            sh->mass[warp] = slot[kRowMaxCluster + warp] + w;
+            sh->above[warp] += (uint32_t)kept;
+        }
+    }
+    const int wper = (c.n + kRowWarps - 1) / kRowWarps;
+    unsigned long long w = 0;
+    for (int i = off + lane; i < off + here; i += 32) {
+        const unsigned long long e = list[i];
+        const int idx = (int)~(uint32_t)e, v = (int)(((unsigned)idx + (unsigned)c.r.head) / E) - c.gb;
+        if (v >= warp * wper && v < (warp + 1) * wper && cut.keeps((uint32_t)(e >> 32), idx)) w += list[kSmall + i];
+    }
+    w = warp_sum_u64(w);
+    if (lane == 0) sh->wsum[warp] += w;
+    __syncthreads();
+    res->sums = true;
+    return true;
+}
+
+// The same in any case: where the counts do not do, the key by bisection and its ties by their order.
+template <bool F32>
+__device__ Nucleus cut_mass(Ctx<F32> &c, const Scale &s, const float2 *tab, unsigned long long *list, uint32_t kmax,
+                            Cut by_k, float top_p)
+{
+    Nucleus res;
+    if (!s.hard && cut_by_counts(c, s, tab, list, by_k, top_p, &res)) return res;
+    const KeptMass all(s, tab, by_k);
+    const auto f = [&](float x, uint32_t q, int i) { return by_k.keeps(q, i) ? weight(x, s, tab) : 0ull; };
+    const unsigned long long Z = cluster_sum(c, thread_sum(c, all)), want = share_ceil(top_p, Z);
+    unsigned long long above = 0;
+    const uint32_t key = s.hard ? kmax : bisect_key(c, kKeyNone + 1, kmax, want, f, &above);
+    return Nucleus{cut_ties(c, key, weight(key_float(key), s, tab), above, want, by_k), false};
 }
 
 // Sends for a thread's first granules.
@@ -1272,22 +1374,37 @@ __global__ void __launch_bounds__(kRowThreads, 2) sample_kernel(const SamplePara
     // over the whole row: the cuts one after the other, then the kept mass and the token in it
     Cut cut{kKeyNone, INT_MIN};
     if (k > 0) cut = cut_count(c, kmax, k);
-    if (nucleus) cut = cut_mass(c, s, tab, list, cut, top_p);
-    if (kminp > cut.key) cut = Cut{kminp, INT_MAX};
+    bool sums = false;
+    if (nucleus) {
+        const Nucleus q = cut_mass(c, s, tab, list, kmax, cut, top_p);
+        cut = q.cut;
+        sums = q.sums;
+    }
+    if (kminp > cut.key) {
+        cut = Cut{kminp, INT_MAX};
+        sums = false;
+    }
     const KeptMass kept(s, tab, cut);
-    unsigned long long sum = 0;
-    int n = 0;
-    for (int v = c.wb + (tid & 31); v < c.we; v += 32) sum += kept.granule(c, v, n);
-    n = (int)__reduce_add_sync(0xffffffffu, n);
-    if ((tid & 31) == 0) sh.part[tid >> 5] = n;
-    const unsigned long long mine = block_sum_u64(sum, &sh);
-    n = __reduce_add_sync(0xffffffffu, (tid & 31) < kRowWarps ? sh.part[tid & 31] : 0);
-    const unsigned long long *slot = cluster_gather(c, mine, (unsigned long long)(unsigned)n);
-    const unsigned long long total = slot_sum(slot, c.C), count = slot_sum(slot + kRowMaxCluster, c.C);
-    int id;
-    uint32_t key;
-    locate(c, share_floor(u, total), kept, mine, slot, &id, &key);
-    if (c.rank == 0 && tid == 0) put_sample(p, row, id, log_share(key_float(key), T, s, total), (long long)count);
+    const unsigned long long *mass = sh.mass;
+    unsigned long long count = 0;
+    if (sums) {
+        for (int q = 0; q < c.C; ++q) count += sh.above[q];
+    } else {
+        int n = 0;
+        unsigned long long mine = 0;
+        for (int v = c.wb + (tid & 31); v < c.we; v += 32) mine += kept.granule(c, v, n);
+        n = (int)__reduce_add_sync(0xffffffffu, n);
+        __syncthreads();
+        if ((tid & 31) == 0) sh.part[tid >> 5] = n;
+        mine = block_sum_u64(mine, &sh);
+        n = __reduce_add_sync(0xffffffffu, (tid & 31) < kRowWarps ? sh.part[tid & 31] : 0);
+        mass = cluster_gather(c, mine, (unsigned long long)(unsigned)n);
+        count = slot_sum(mass + kRowMaxCluster, c.C);
+    }
+    const unsigned long long total = slot_sum(mass, c.C);
+    locate(c, share_floor(u, total), kept, mass, [&](int id, uint32_t key) {
+        put_sample(p, row, id, log_share(key_float(key), T, s, total), (long long)count);
+    });
 }
 
 int logits_cluster(int rows, int64_t row_bytes)
@@ -1301,7 +1418,7 @@ int logits_cluster(int rows, int64_t row_bytes)
 
 // Cluster and shared memory of a launch over `rows` rows.
 constexpr size_t kMaxSmem = kMaxCache + (size_t)kListCap * 8;
-static_assert(kMaxSmem + 10 * 1024 <= kSmemPerCta, "with the kernels' static part");
+static_assert(kMaxSmem + 11 * 1024 <= kSmemPerCta, "with the kernels' static part");
 
 template <bool F32, auto Kern, typename P>
 cudaError_t launch_rows(P p, int rows, cudaStream_t st)
