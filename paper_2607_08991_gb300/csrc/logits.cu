@@ -23,6 +23,7 @@
 namespace sats {
 namespace {
 
+constexpr int kSelThreads = 512, kSelWarps = kSelThreads / 32, kSelPerSm = 2;
 constexpr int kMaxTop = 1024;          // largest K of the list's way
 constexpr int kListCap = 2048;         // entries of the list
 constexpr uint32_t kKeyNone = 0x007fffffu;   // key of -inf: never selected
@@ -43,7 +44,7 @@ __device__ __forceinline__ float key_float(uint32_t k)
 }
 
 // ------------------------------------------------------------------ weights
-// 2^(j / 1024) in two floats.
+// 2^(-j / 1024) in two floats.
 struct Exp2Table {
     float2 v[1024];
 };
@@ -51,7 +52,7 @@ constexpr Exp2Table make_exp2_table()
 {
     Exp2Table t{};
     for (int j = 0; j < 1024; ++j) {
-        const double x = j * (0.69314718055994530942 / 1024.0);
+        const double x = -j * (0.69314718055994530942 / 1024.0);
         double rest = 0.0;
         for (int k = 24; k > 0; --k) rest = (1.0 + rest) * (x / k);   // exp(x) - 1
         const double v = 1.0 + rest;
@@ -87,7 +88,7 @@ constexpr float kMagicG = 12288.f;   // 1.5 * 2^13: one unit in the last place i
 constexpr float kMagicW = 6.f;       // 1.5 * 2^2: 2^-21
 
 // Two weights 2^F exp((z - top) / T) as whole numbers (i1 << (F - 21)) + i2, where z <= top; `in` says whether they
-// can be other than 0 (false for NaN and -inf, whose numbers mean nothing).  g: -g / 1024 octaves below the top.
+// can be other than 0 (false for NaN and -inf, whose numbers mean nothing).  g: g / 1024 octaves below the top.
 // Sums of floats in pairs throughout; relative error about 2^-35, from the rounding of r L and T.x q to 24 bits.
 struct Weights2 {
     int i1[2], i2[2], g[2];
@@ -97,36 +98,32 @@ __device__ __forceinline__ Weights2 weights2(f32x2 z, const Scale &s, const floa
 {
     const auto both = [](float v) { return pack2(v, v); };
     constexpr float L = 0.69314718055994530942f;
-    const f32x2 minus1 = both(-1.f);
-    // x = z - top exactly, xh + xl
-    const f32x2 nt = both(-s.top);
+    const f32x2 minus1 = both(-1.f), nt = both(-s.top), chi = both(s.chi);
     const f32x2 xh = fadd2(z, nt);
-    const f32x2 bv = ffma2(xh, minus1, z);               // z - xh
-    const f32x2 av = fadd2(xh, bv);
-    const f32x2 xl = fadd2(ffma2(av, minus1, z), fadd2(bv, nt));
-    // p + e = x log2(e) / T
-    const f32x2 chi = both(s.chi);
-    const f32x2 p = fmul2(xh, chi);
-    const f32x2 e = ffma2(xl, chi, ffma2(xh, both(s.clo), ffma2(xh, chi, fmul2(p, minus1))));
-    // p = g / 1024 + what r starts from, exactly
-    const f32x2 m = fadd2(p, both(kMagicG));
-    const f32x2 r = fadd2(ffma2(fadd2(m, both(-kMagicG)), minus1, p), e);   // |r| <= 2^-11, and a little
-    // q = 2^r - 1
-    const f32x2 q = fmul2(r, ffma2(r, ffma2(r, both(L * L * L / 6.f), both(L * L / 2.f)), both(L)));
-    const float2 mm = unpack2(m), pp = unpack2(p);
+    const f32x2 bv = ffma2(xh, minus1, z);
+    const f32x2 xl = fadd2(ffma2(fadd2(xh, bv), minus1, z), fadd2(bv, nt));   // xh + xl = z - top, exactly
+    // y - e = (top - z) log2(e) / T
+    const f32x2 y = fmul2(xh, both(-s.chi));
+    const f32x2 e = ffma2(xl, chi, ffma2(xh, both(s.clo), ffma2(xh, chi, y)));
+    // y = g / 1024 - what r starts from, exactly
+    const f32x2 m = fadd2(y, both(kMagicG));
+    const f32x2 r = fadd2(ffma2(y, minus1, fadd2(m, both(-kMagicG))), e);   // |r| <= 2^-11, and a little
+    // q = 2^r - 1 (the next term is below 2^-37)
+    const f32x2 q = fmul2(r, ffma2(r, both(L * L / 2.f), both(L)));
+    const float2 mm = unpack2(m), yy = unpack2(y);
     Weights2 w;
     w.g[0] = __float_as_int(mm.x) - __float_as_int(kMagicG);
     w.g[1] = __float_as_int(mm.y) - __float_as_int(kMagicG);
-    w.in[0] = pp.x > -60.f;
-    w.in[1] = pp.y > -60.f;
+    w.in[0] = yy.x < 60.f;
+    w.in[1] = yy.y < 60.f;
     const float2 t0 = tab[w.g[0] & 1023], t1 = tab[w.g[1] & 1023];
     const f32x2 tx = pack2(t0.x, t1.x);
     const f32x2 lo = ffma2(tx, q, pack2(t0.y, t1.y));
-    // h + l = 2^(g mod 1024 / 1024 + r), scaled by 2^(g div 1024)
+    // h + l = 2^(-(g mod 1024) / 1024 + r), scaled by 2^(-(g div 1024))
     const f32x2 h = fadd2(tx, lo);
-    const f32x2 l = fadd2(lo, fmul2(ffma2(tx, minus1, h), minus1));
-    const f32x2 sc = pack2(__int_as_float(0x3f800000 + ((w.g[0] << 13) & 0xff800000)),
-                           __int_as_float(0x3f800000 + ((w.g[1] << 13) & 0xff800000)));
+    const f32x2 l = ffma2(ffma2(tx, minus1, h), minus1, lo);
+    const f32x2 sc = pack2(__int_as_float(0x3f800000 - ((w.g[0] << 13) & 0xff800000)),
+                           __int_as_float(0x3f800000 - ((w.g[1] << 13) & 0xff800000)));
     const f32x2 hs = fmul2(h, sc);
     const f32x2 m1 = fadd2(hs, both(kMagicW));
     const f32x2 d = ffma2(l, sc, ffma2(fadd2(m1, both(-kMagicW)), minus1, hs));
@@ -187,12 +184,12 @@ __device__ __forceinline__ unsigned long long share_ceil(float f, unsigned long 
 
 // ------------------------------------------------------------------ the row in a cluster
 struct Shared {
-    unsigned long long wsum[kRowWarps];
-    unsigned long long scan[kRowWarps];
+    unsigned long long wsum[kSelWarps];
+    unsigned long long scan[kSelWarps];
     unsigned long long slot[2][2][kRowMaxCluster];   // the CTAs' values, one or two of each; two buffers in turn
     uint32_t kmax[kRowMaxCluster], bound[kRowMaxCluster];
-    int part[kRowWarps];
-    uint32_t ktop[kRowWarps], klow[kRowWarps];
+    int part[kSelWarps];
+    uint32_t ktop[kSelWarps], klow[kSelWarps];
     int border;
     uint32_t nlist;
     int found_idx;
@@ -266,7 +263,7 @@ __device__ __forceinline__ unsigned long long block_sum_u64(unsigned long long v
     __syncthreads();
     unsigned long long t = 0;
 #pragma unroll
-    for (int w = 0; w < kRowWarps; ++w) t += sh->wsum[w];
+    for (int w = 0; w < kSelWarps; ++w) t += sh->wsum[w];
     return t;
 }
 
@@ -285,7 +282,7 @@ __device__ __forceinline__ unsigned long long block_scan_u64(unsigned long long 
     __syncthreads();
     unsigned long long before = 0, t = 0;
 #pragma unroll
-    for (int w = 0; w < kRowWarps; ++w) {
+    for (int w = 0; w < kSelWarps; ++w) {
         if (w < warp) before += sh->scan[w];
         t += sh->scan[w];
     }
@@ -385,14 +382,14 @@ __device__ __forceinline__ void locate(Ctx<F32> &c, unsigned long long target, c
     for (unsigned k = 0; k < c.rank; ++k) before += slot[k];
     if (target >= before && target - before < slot[c.rank]) {   // (one CTA)
         unsigned long long t = target - before;
-        int a = 0, b = c.n, per = (c.n + kRowWarps - 1) / kRowWarps;
+        int a = 0, b = c.n, per = (c.n + kSelWarps - 1) / kSelWarps;
         for (;;) {
             int w = 0;
-            while (w < kRowWarps - 1 && t >= sh->wsum[w]) t -= sh->wsum[w++];
+            while (w < kSelWarps - 1 && t >= sh->wsum[w]) t -= sh->wsum[w++];
             a = a + w * per;
             b = min(b, a + per);
-            if (b - a <= kRowThreads * kFew / RowElem<F32>::kPer) break;
-            per = (b - a + kRowWarps - 1) / kRowWarps;
+            if (b - a <= kSelThreads * kFew / RowElem<F32>::kPer) break;
+            per = (b - a + kSelWarps - 1) / kSelWarps;
             unsigned long long s = 0;
             const int wb = min(b, a + warp * per), we = min(b, wb + per);
             for (int v = wb + lane; v < we; v += 32) s += f.granule(c, v);
@@ -400,7 +397,7 @@ __device__ __forceinline__ void locate(Ctx<F32> &c, unsigned long long target, c
         }
         // a few elements per thread, in order
         constexpr int E = RowElem<F32>::kPer;
-        const int n = (b - a) * E, each = (n + kRowThreads - 1) / kRowThreads, first = tid * each;
+        const int n = (b - a) * E, each = (n + kSelThreads - 1) / kSelThreads, first = tid * each;
         const int i0 = c.r.first(c.gb + a);
         const auto at = [&](int e, uint32_t *k) {
             const float x = c.get(a + e / E, e % E);
@@ -476,6 +473,9 @@ __device__ Cut cut_count(Ctx<F32> &c, uint32_t kmax, int k)
     return cut;
 }
 
+// Granules whose weights' parts add up in 32 bits (256 weights of at most 2^21 and less).
+constexpr int kFlush = 32;
+
 // The kept tokens' weights.
 struct KeptMass {
     const Scale &s;
@@ -499,13 +499,19 @@ struct KeptMass {
     template <bool F32>
     __device__ __forceinline__ unsigned long long granule(const Ctx<F32> &c, int v, int &n) const
     {
+        int a1 = 0, a2 = 0;
+        add(c, v, a1, a2, n);
+        return whole_weight(a1, a2, s);   // (eight weights at most)
+    }
+    template <bool F32>
+    __device__ __forceinline__ void add(const Ctx<F32> &c, int v, int &a1, int &a2, int &n) const
+    {
         constexpr int P = RowElem<F32>::kPer / 2;
         const uint4 x = c.get(v);
-        if (!(granule_max<F32>(x) >= at)) return 0ull;
+        if (!(granule_max<F32>(x) >= at)) return;
         f32x2 z[P];
         granule_pairs<F32>(x, z);
         const int i0 = c.r.first(c.gb + v);
-        int a1 = 0, a2 = 0;
         if (s.hard) {
 #pragma unroll
             for (int j = 0; j < P; ++j) {
@@ -525,12 +531,23 @@ struct KeptMass {
                 if (k1 && w.in[1]) { a1 += w.i1[1]; a2 += w.i2[1]; }
             }
         }
-        return whole_weight(a1, a2, s);   // (eight weights at most)
+    }
+    // Sum over this thread's granules.
+    template <bool F32>
+    __device__ __forceinline__ unsigned long long over_row(const Ctx<F32> &c, int &n) const
+    {
+        unsigned long long sum = 0;
+        for (int v0 = c.wb + (int)(threadIdx.x & 31); v0 < c.we; v0 += 32 * kFlush) {
+            int a1 = 0, a2 = 0;
+            for (int v = v0; v < min(c.we, v0 + 32 * kFlush); v += 32) add(c, v, a1, a2, n);
+            sum += whole_weight(a1, a2, s);
+        }
+        return sum;
     }
 };
 
 // ------------------------------------------------------------------ the list
-constexpr int kListPer = kListCap / kRowThreads;   // list entries of a thread, in a row
+constexpr int kListPer = kListCap / kSelThreads;   // list entries of a thread, in a row
 
 // Sorts n2 (a power of two) words descending; all threads of the CTA.
 __device__ void sort_desc(unsigned long long *a, int n2)
@@ -538,7 +555,7 @@ __device__ void sort_desc(unsigned long long *a, int n2)
     __syncthreads();
     for (int k = 2; k <= n2; k <<= 1) {
         for (int j = k >> 1; j > 0; j >>= 1) {
-            for (int t = threadIdx.x; t < n2 / 2; t += kRowThreads) {
+            for (int t = threadIdx.x; t < n2 / 2; t += kSelThreads) {
                 const int i = 2 * t - (t & (j - 1));
                 const unsigned long long x = a[i], y = a[i + j];
                 if ((x < y) == ((i & k) == 0)) {
@@ -573,7 +590,7 @@ __device__ int push_list(Ctx<F32> &c, unsigned long long *list, bool *ok)
     *ok = total <= kListCap;
     if (*ok && c.C > 1) {
         if (c.rank != 0)
-            for (uint32_t i = threadIdx.x; i < mine; i += kRowThreads)
+            for (uint32_t i = threadIdx.x; i < mine; i += kSelThreads)
                 st_peer_u64(peer_addr(list + before + i, 0), list[i]);
         cluster_sync_all();
     }
@@ -611,11 +628,11 @@ __device__ int gather_list(Ctx<F32> &c, unsigned long long *list, uint32_t bound
 __device__ void sort_list(unsigned long long *list, int n)
 {
     const int n2 = pow2_at_least(n);
-    for (int i = n + threadIdx.x; i < n2; i += kRowThreads) list[i] = 0ull;
+    for (int i = n + threadIdx.x; i < n2; i += kSelThreads) list[i] = 0ull;
     sort_desc(list, n2);
 }
 
-// A list of at most kSmall entries needs no sorting: each is compared with all others, by kRowThreads / (the entries'
+// A list of at most kSmall entries needs no sorting: each is compared with all others, by kSelThreads / (the entries'
 // number, rounded up to a power of two) threads each.  (128 entries: sorting took 3 us, this a fifth of it.)
 constexpr int kSmall = 256;
 struct Small {
@@ -626,7 +643,7 @@ struct Small {
     __device__ __forceinline__ Small(const unsigned long long *list, int n)
     {
         const int n2 = max(32, pow2_at_least(n));
-        per = kRowThreads / n2;
+        per = kSelThreads / n2;
         i = (int)threadIdx.x / per;
         part = (int)threadIdx.x & (per - 1);
         on = i < n;
@@ -721,14 +738,14 @@ __device__ bool cut_by_counts(Ctx<F32> &c, const Scale &s, const float2 *tab, un
     int shift = 0;
     while (shift < 5 && (float)(2 << shift) < 128.f * s.chi) ++shift;
     uint32_t *count = reinterpret_cast<uint32_t *>(list), *got = count + kBins;
-    for (int i = tid; i < kBins / 4; i += kRowThreads) reinterpret_cast<uint4 *>(count)[i] = make_uint4(0, 0, 0, 0);
+    for (int i = tid; i < kBins / 4; i += kSelThreads) reinterpret_cast<uint4 *>(count)[i] = make_uint4(0, 0, 0, 0);
     __syncthreads();
     {
-        const f32x2 nt = pack2(-s.top, -s.top), chi = pack2(s.chi, s.chi), magic = pack2(kMagicG, kMagicG);
+        const f32x2 nt = pack2(-s.top, -s.top), chi = pack2(-s.chi, -s.chi), magic = pack2(kMagicG, kMagicG);
         const uint32_t mask = (1u << shift) - 1u;
-        const auto add = [&](float p, float m) {
-            if (!(p > -60.f)) return;
-            const uint32_t d = (uint32_t)(__float_as_int(kMagicG) - __float_as_int(m));   // 1 / 1024 octaves below the top
+        const auto add = [&](float y, float m) {
+            if (!(y < 60.f)) return;
+            const uint32_t d = (uint32_t)(__float_as_int(m) - __float_as_int(kMagicG));   // 1 / 1024 octaves below the top
             const int v = 4096 + (((int)mask - 2 * (int)(d & mask)) * 2839 >> 11);         // ln 2 * 2 = 2839 / 2048
             atomicAdd(count + min(d >> shift, (uint32_t)kBins - 1u), (uint32_t)v);
         };
@@ -738,10 +755,10 @@ __device__ bool cut_by_counts(Ctx<F32> &c, const Scale &s, const float2 *tab, un
             const int i0 = c.r.first(c.gb + v);
 #pragma unroll
             for (int j = 0; j < P; ++j) {
-                const f32x2 p2 = fmul2(fadd2(z[j], nt), chi);   // (as weights2 does)
-                const float2 y = unpack2(z[j]), p = unpack2(p2), m = unpack2(fadd2(p2, magic));
-                if (!filtered || all.keeps(y.x, i0 + 2 * j)) add(p.x, m.x);
-                if (!filtered || all.keeps(y.y, i0 + 2 * j + 1)) add(p.y, m.y);
+                const f32x2 y2 = fmul2(fadd2(z[j], nt), chi);   // (as weights2 does)
+                const float2 f = unpack2(z[j]), y = unpack2(y2), m = unpack2(fadd2(y2, magic));
+                if (!filtered || all.keeps(f.x, i0 + 2 * j)) add(y.x, m.x);
+                if (!filtered || all.keeps(f.y, i0 + 2 * j + 1)) add(y.y, m.y);
             }
         }
     }
@@ -749,16 +766,18 @@ __device__ bool cut_by_counts(Ctx<F32> &c, const Scale &s, const float2 *tab, un
     // a run of steps per CTA: its counts in all CTAs
     const int nb = kBins / C;
     if (C > 1) {
-        const uint4 q = reinterpret_cast<const uint4 *>(count)[tid];
-        const int b = 4 * tid;
-        st_peer_v4(peer_addr(got + c.rank * nb + b % nb, b / nb), __uint_as_float(q.x), __uint_as_float(q.y),
-                   __uint_as_float(q.z), __uint_as_float(q.w));
+        for (int i = tid; i < kBins / 4; i += kSelThreads) {
+            const uint4 q = reinterpret_cast<const uint4 *>(count)[i];
+            const int b = 4 * i;
+            st_peer_v4(peer_addr(got + c.rank * nb + b % nb, b / nb), __uint_as_float(q.x), __uint_as_float(q.y),
+                       __uint_as_float(q.z), __uint_as_float(q.w));
+        }
         cluster_sync_all();
     } else {
         got = count;
     }
-    constexpr int kMost = kBins / kRowThreads;
-    const int per = (nb + kRowThreads - 1) / kRowThreads;
+    constexpr int kMost = kBins / kSelThreads;
+    const int per = (nb + kSelThreads - 1) / kSelThreads;
     unsigned long long m[kMost], mine = 0;   // masses in whole numbers: their sums are the same in every CTA
 #pragma unroll
     for (int j = 0; j < kMost; ++j) {
@@ -804,27 +823,27 @@ __device__ bool cut_by_counts(Ctx<F32> &c, const Scale &s, const float2 *tab, un
     const int d0 = (int)sh->bin0 << shift, d1 = sh->bin1 >= kBins - 1u ? INT_MAX : (int)(sh->bin1 + 1u) << shift;
     unsigned long long w_all = 0, w_above = 0;
     int n_above = 0;
-    for (int v = c.wb + lane; v < c.we; v += 32) {
-        const uint4 x = c.get(v);
-        if (!(granule_max<F32>(x) >= all.at)) continue;
-        f32x2 z[P];
-        granule_pairs<F32>(x, z);
-        const int i0 = c.r.first(c.gb + v);
+    for (int v0 = c.wb + lane; v0 < c.we; v0 += 32 * kFlush) {
         int a1 = 0, a2 = 0, t1 = 0, t2 = 0;
+        for (int v = v0; v < min(c.we, v0 + 32 * kFlush); v += 32) {
+            f32x2 z[P];
+            granule_pairs<F32>(c.get(v), z);
+            const int i0 = c.r.first(c.gb + v);
 #pragma unroll
-        for (int j = 0; j < P; ++j) {
-            const Weights2 w = weights2(z[j], s, tab);
-            const float2 y = unpack2(z[j]);
+            for (int j = 0; j < P; ++j) {
+                const Weights2 w = weights2(z[j], s, tab);
+                const float2 y = unpack2(z[j]);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const float f = h ? y.y : y.x;
-                const int i = i0 + 2 * j + h, d = -w.g[h];
-                const bool in = w.in[h] && (!filtered || all.keeps(f, i));
-                if (in) { t1 += w.i1[h]; t2 += w.i2[h]; }
-                if (in && d < d0) { a1 += w.i1[h]; a2 += w.i2[h]; ++n_above; }
-                if (in && d >= d0 && d < d1) {
-                    const uint32_t at = atomicAdd(&sh->nlist, 1u);
-                    if (at < (uint32_t)seg) own[at] = ((unsigned long long)key_of(f) << 32) | (uint32_t)~(uint32_t)i;
+                for (int h = 0; h < 2; ++h) {
+                    const float f = h ? y.y : y.x;
+                    const int i = i0 + 2 * j + h, d = w.g[h];
+                    const bool in = w.in[h] && (!filtered || all.keeps(f, i));
+                    if (in) { t1 += w.i1[h]; t2 += w.i2[h]; }
+                    if (in && d < d0) { a1 += w.i1[h]; a2 += w.i2[h]; ++n_above; }
+                    if (in && d >= d0 && d < d1) {
+                        const uint32_t at = atomicAdd(&sh->nlist, 1u);
+                        if (at < (uint32_t)seg) own[at] = ((unsigned long long)key_of(f) << 32) | (uint32_t)~(uint32_t)i;
+                    }
                 }
             }
         }
@@ -841,16 +860,16 @@ __device__ bool cut_by_counts(Ctx<F32> &c, const Scale &s, const float2 *tab, un
     }
     __syncthreads();
     w_all = w_above = 0;
-    for (int w = 0; w < kRowWarps; ++w) {
+    for (int w = 0; w < kSelWarps; ++w) {
         w_all += sh->scan[w];
         w_above += sh->wsum[w];
     }
-    n_above = (int)__reduce_add_sync(0xffffffffu, lane < kRowWarps ? sh->part[lane] : 0);
+    n_above = (int)__reduce_add_sync(0xffffffffu, lane < kSelWarps ? sh->part[lane] : 0);
     const int here = (int)sh->nlist;
     if (here <= seg)
         for (int q = 1; q < C; ++q) {   // (each CTA begins with its neighbour)
             const unsigned to = (c.rank + q) % C;
-            for (int i = tid; i < here; i += kRowThreads) st_peer_u64(peer_addr(own + i, to), own[i]);
+            for (int i = tid; i < here; i += kSelThreads) st_peer_u64(peer_addr(own + i, to), own[i]);
         }
     if (tid < C) {
         st_peer_u32(peer_addr(&sh->cnt[c.rank], tid), (uint32_t)here);
@@ -873,7 +892,7 @@ __device__ bool cut_by_counts(Ctx<F32> &c, const Scale &s, const float2 *tab, un
         unsigned long long e[kListPer];
 #pragma unroll
         for (int j = 0; j < kListPer; ++j) {
-            int i = tid + j * kRowThreads, k = 0, from = 0;
+            int i = tid + j * kSelThreads, k = 0, from = 0;
             e[j] = 0;
             if (i < n) {
                 while (i - from >= (int)sh->cnt[k]) from += (int)sh->cnt[k++];
@@ -883,7 +902,7 @@ __device__ bool cut_by_counts(Ctx<F32> &c, const Scale &s, const float2 *tab, un
         __syncthreads();
 #pragma unroll
         for (int j = 0; j < kListPer; ++j)
-            if (tid + j * kRowThreads < n) list[tid + j * kRowThreads] = e[j];
+            if (tid + j * kSelThreads < n) list[tid + j * kSelThreads] = e[j];
         __syncthreads();
     }
     if (n <= kSmall) {
@@ -940,7 +959,7 @@ __device__ bool cut_by_counts(Ctx<F32> &c, const Scale &s, const float2 *tab, un
             sh->above[warp] += (uint32_t)kept;
         }
     }
-    const int wper = (c.n + kRowWarps - 1) / kRowWarps;
+    const int wper = (c.n + kSelWarps - 1) / kSelWarps;
     unsigned long long w = 0;
     for (int i = off + lane; i < off + here; i += 32) {
         const unsigned long long e = list[i];
@@ -991,8 +1010,8 @@ __device__ void load_row(Ctx<F32> &c, uint4 *cache, int want, uint32_t *scratch,
     constexpr int NG = F32 ? 4 : 8;   // groups of a thread
     Shared *sh = c.sh;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    if (want > 0) scratch[tid] = 0u;
-    static_assert(kBoundBins == kRowThreads, "one word per thread");
+    if (want > 0)
+        for (int i = tid; i < kBoundBins; i += kSelThreads) scratch[i] = 0u;
     uint32_t gm[4] = {0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u};
     if constexpr (!F32)
         for (int k = 0; k < 4; ++k) gm[k] = 0xff80ff80u;
@@ -1043,8 +1062,8 @@ __device__ void load_row(Ctx<F32> &c, uint4 *cache, int want, uint32_t *scratch,
     }
     if (tid == 0) sh->border = kBoundBins;
     __syncthreads();
-    top = __reduce_max_sync(0xffffffffu, sh->ktop[lane & (kRowWarps - 1)]);
-    least = __reduce_min_sync(0xffffffffu, sh->klow[lane & (kRowWarps - 1)]);
+    top = __reduce_max_sync(0xffffffffu, sh->ktop[lane & (kSelWarps - 1)]);
+    least = __reduce_min_sync(0xffffffffu, sh->klow[lane & (kSelWarps - 1)]);
 
     uint32_t low = kKeyNone + 1;
     if (want > 0) {
@@ -1092,7 +1111,7 @@ __device__ void load_row(Ctx<F32> &c, uint4 *cache, int want, uint32_t *scratch,
         at = __reduce_min_sync(0xffffffffu, at);
         if (lane == 0) sh->klow[warp] = at;
         __syncthreads();
-        at = __reduce_min_sync(0xffffffffu, sh->klow[lane & (kRowWarps - 1)]);
+        at = __reduce_min_sync(0xffffffffu, sh->klow[lane & (kSelWarps - 1)]);
         if (border < kBoundBins) low = at;
     }
     if (c.C > 1) {
@@ -1121,7 +1140,7 @@ __device__ __forceinline__ void set_ctx(Ctx<F32> &c, const uint4 *cache, int cac
     const int per = (c.r.G + C - 1) / C;
     c.gb = min(c.r.G, (int)c.rank * per);
     c.n = min(c.r.G - c.gb, per);
-    const int wper = (c.n + kRowWarps - 1) / kRowWarps, warp = threadIdx.x >> 5;
+    const int wper = (c.n + kSelWarps - 1) / kSelWarps, warp = threadIdx.x >> 5;
     c.wb = min(c.n, warp * wper);
     c.we = min(c.n, c.wb + wper);
     c.cached = cached;
@@ -1151,7 +1170,7 @@ __device__ int lowest_at(Ctx<F32> &c, uint32_t kmax)
     __syncthreads();
     if ((threadIdx.x & 31) == 0) c.sh->part[threadIdx.x >> 5] = best;
     __syncthreads();
-    best = __reduce_min_sync(0xffffffffu, c.sh->part[threadIdx.x & (kRowWarps - 1)]);
+    best = __reduce_min_sync(0xffffffffu, c.sh->part[threadIdx.x & (kSelWarps - 1)]);
     const unsigned long long *slot = cluster_gather(c, (unsigned long long)(unsigned)best);
     for (int k = 0; k < c.C; ++k) best = min(best, (int)(unsigned)slot[k]);
     return best;
@@ -1167,7 +1186,7 @@ struct TopParams {
 };
 
 template <bool F32>
-__global__ void __launch_bounds__(kRowThreads, 2) top_kernel(const TopParams p)
+__global__ void __launch_bounds__(kSelThreads, kSelPerSm) top_kernel(const TopParams p)
 {
     extern __shared__ __align__(16) uint4 smem[];
     __shared__ Shared sh;
@@ -1192,14 +1211,14 @@ __global__ void __launch_bounds__(kRowThreads, 2) top_kernel(const TopParams p)
             p.values[(size_t)row * p.K + at] = key_float(e.key());
             p.idx[(size_t)row * p.K + at] = e.idx();
         }
-        for (int i = n + threadIdx.x; i < p.K; i += kRowThreads) {
+        for (int i = n + threadIdx.x; i < p.K; i += kSelThreads) {
             p.values[(size_t)row * p.K + i] = -INFINITY;
             p.idx[(size_t)row * p.K + i] = -1;
         }
         return;
     }
     sort_list(list, n);
-    for (int i = threadIdx.x; i < p.K; i += kRowThreads) {
+    for (int i = threadIdx.x; i < p.K; i += kSelThreads) {
         const unsigned long long e = i < n ? list[i] : 0ull;
         p.values[(size_t)row * p.K + i] = i < n ? key_float((uint32_t)(e >> 32)) : -INFINITY;
         p.idx[(size_t)row * p.K + i] = i < n ? (int32_t)~(uint32_t)e : -1;
@@ -1235,7 +1254,7 @@ __device__ __forceinline__ float log_share(float z, float T, const Scale &s, uns
 }
 
 template <bool F32>
-__global__ void __launch_bounds__(kRowThreads, 2) sample_kernel(const SampleParams p)
+__global__ void __launch_bounds__(kSelThreads, kSelPerSm) sample_kernel(const SampleParams p)
 {
     extern __shared__ __align__(16) uint4 smem[];
     __shared__ Shared sh;
@@ -1263,7 +1282,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) sample_kernel(const SamplePara
     const bool nucleus = top_p < 1.f;
     const int want = !greedy && k > 0 && k <= kMaxTop ? k : 0;   // what the list serves
     if (!greedy)
-        for (int i = tid; i < 1024; i += kRowThreads) tab[i] = kExp2.v[i];
+        for (int i = tid; i < 1024; i += kSelThreads) tab[i] = kExp2.v[i];
     uint32_t kmax, bound;
     load_row(c, smem, want, reinterpret_cast<uint32_t *>(list), &kmax, &bound);
     if (kmax <= kKeyNone) {   // nothing can be drawn
@@ -1344,7 +1363,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) sample_kernel(const SamplePara
             // the kept ones in the vocabulary's order
             const int m2 = pow2_at_least(m);
             __syncthreads();
-            for (int i = tid; i < m2; i += kRowThreads) {
+            for (int i = tid; i < m2; i += kSelThreads) {
                 const unsigned long long e = list[i];
                 list[i] = i < m ? (e << 32) | (e >> 32) : 0ull;
             }
@@ -1391,13 +1410,12 @@ __global__ void __launch_bounds__(kRowThreads, 2) sample_kernel(const SamplePara
         for (int q = 0; q < c.C; ++q) count += sh.above[q];
     } else {
         int n = 0;
-        unsigned long long mine = 0;
-        for (int v = c.wb + (tid & 31); v < c.we; v += 32) mine += kept.granule(c, v, n);
+        unsigned long long mine = kept.over_row(c, n);
         n = (int)__reduce_add_sync(0xffffffffu, n);
         __syncthreads();
         if ((tid & 31) == 0) sh.part[tid >> 5] = n;
         mine = block_sum_u64(mine, &sh);
-        n = __reduce_add_sync(0xffffffffu, (tid & 31) < kRowWarps ? sh.part[tid & 31] : 0);
+        n = __reduce_add_sync(0xffffffffu, (tid & 31) < kSelWarps ? sh.part[tid & 31] : 0);
         mass = cluster_gather(c, mine, (unsigned long long)(unsigned)n);
         count = slot_sum(mass + kRowMaxCluster, c.C);
     }
@@ -1411,7 +1429,7 @@ int logits_cluster(int rows, int64_t row_bytes)
 {
     int C = 1;
     while (C < kRowMaxCluster && (row_bytes > (int64_t)C * (int64_t)kShare ||
-                                  ((int64_t)rows * C < 2 * 152 && row_bytes >= 2 * (int64_t)C * kRowThreads * 16)))
+                                  ((int64_t)rows * C < 2 * 152 && row_bytes >= 2 * (int64_t)C * kSelThreads * 16)))
         C *= 2;
     return C;
 }
@@ -1428,7 +1446,7 @@ cudaError_t launch_rows(P p, int rows, cudaStream_t st)
     const size_t share = (size_t)((bytes + 32 + p.cluster - 1) / p.cluster) + 32;
     p.cached = (int)((share < kMaxCache ? share : kMaxCache) / 16);
     const size_t smem = (size_t)p.cached * 16 + kListCap * 8;
-    return launch_clusters<Kern>((int64_t)rows * p.cluster, kRowThreads, smem, kMaxSmem, p.cluster, st, p);
+    return launch_clusters<Kern>((int64_t)rows * p.cluster, kSelThreads, smem, kMaxSmem, p.cluster, st, p);
 }
 
 sats_status check_rows(const void *logits, int64_t ld, int rows, int V, int bytes)
