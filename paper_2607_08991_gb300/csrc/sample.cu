@@ -1,47 +1,21 @@
-// logits.cu -- the top logits of a row and the drawing of a token from it (sats_top_logits, sats_sample).
-//
-// One row per thread-block cluster.  The row's share of a CTA is brought to shared memory once; all passes after
-// that run there.  Both calls start from the row's largest logits:
-//   - while the row arrives, each thread keeps the maxima of a few groups of its elements.  At least R groups have
-//     their maximum at or above the R-th largest of these maxima, so that at least R elements do: with
-//     R = ceil(K / C) in each of C CTAs, the least of their bounds has K elements of the row at or above it;
-//   - the elements at or above the bound (about K of them in a row of no particular order) go to a list in the first
-//     CTA, which sorts it: descending logits, ties by the lower index.
-// A row whose list would not fit (many equal logits, or large ones that share few groups) takes the general way: the
-// exact K-th largest key by bisection over the keys, counting in every step.
+// sample.cu -- drawing a token from each row of logits (sats_sample).
 //
 // Drawing needs sums over up to V tokens that decide next to borders as close as the smallest token's probability.
 // A token's weight is therefore a whole number, w = 2^F exp((z - max) / T) to about 35 bits relative (never less
 // than 2^-F absolute), computed in pairs of floats; sums of whole numbers do not depend on their order, and every
 // decision (the nucleus, the drawn token) is the same in whichever grouping it is found.
-#include <climits>
-#include <cmath>
-
 #include "internal.h"
 #include "rows.cuh"
 
 namespace sats {
 namespace {
-
-constexpr int kSelThreads = 512, kSelWarps = kSelThreads / 32, kSelPerSm = 2;
-constexpr int kMaxTop = 1024;          // largest K of the list's way
-constexpr int kListCap = 2048;         // entries of the list
-constexpr uint32_t kKeyNone = 0x007fffffu;   // key of -inf: never selected
-constexpr int kFew = 8;                // elements per thread at the end of a search
-constexpr int kAhead = 8;              // granules in flight per thread while the row arrives
-constexpr size_t kShare = 64 * 1024;   // of a row's bytes per CTA, where the cluster allows
-constexpr size_t kMaxCache = 184 * 1024;
-
-// Keys order as the floats do; both zeros have one key.  NaN has none (cleaned to -inf before).
-__device__ __forceinline__ uint32_t key_of(float x)
-{
-    const uint32_t b = __float_as_uint(x + 0.f);
-    return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+constexpr int kSelThreads = 256, kSelPerSm = 3;
 }
-__device__ __forceinline__ float key_float(uint32_t k)
-{
-    return __uint_as_float((k & 0x80000000u) ? k ^ 0x80000000u : ~k);
-}
+}  // namespace sats
+#include "logits.cuh"
+
+namespace sats {
+namespace {
 
 // ------------------------------------------------------------------ weights
 // 2^(-j / 1024) in two floats.
@@ -182,297 +156,6 @@ __device__ __forceinline__ unsigned long long share_ceil(float f, unsigned long 
     return exact ? r : r + 1ull;
 }
 
-// ------------------------------------------------------------------ the row in a cluster
-struct Shared {
-    unsigned long long wsum[kSelWarps];
-    unsigned long long scan[kSelWarps];
-    unsigned long long slot[2][2][kRowMaxCluster];   // the CTAs' values, one or two of each; two buffers in turn
-    uint32_t kmax[kRowMaxCluster], bound[kRowMaxCluster];
-    int part[kSelWarps];
-    uint32_t ktop[kSelWarps], klow[kSelWarps];
-    int border;
-    uint32_t nlist;
-    int found_idx;
-    uint32_t found_key;
-    uint32_t kminp;
-    // the nucleus: steps of the border, and of each CTA the entries, the tokens kept and their mass
-    uint32_t bin0, bin1, cnt[kRowMaxCluster], above[kRowMaxCluster];
-    unsigned long long mass[kRowMaxCluster];
-};
-
-template <bool F32>
-struct Ctx {
-    Row<F32> r;
-    int gb, n;            // this CTA's granules: gb .. gb + n
-    int wb, we;           // this warp's, within them
-    int cached;           // of them in shared memory
-    const uint4 *cache;
-    Shared *sh;
-    int C;
-    unsigned rank;
-    int turn;             // of the all-reduce buffers
-
-    // Granule v of this CTA's, NaN replaced by -inf.
-    __device__ __forceinline__ uint4 get(int v) const
-    {
-        uint4 x = v < cached ? cache[v] : load_granule<F32>(r, gb + v);
-        if constexpr (F32) {
-            x.x = __float_as_uint(fmaxf(__uint_as_float(x.x), -INFINITY));
-            x.y = __float_as_uint(fmaxf(__uint_as_float(x.y), -INFINITY));
-            x.z = __float_as_uint(fmaxf(__uint_as_float(x.z), -INFINITY));
-            x.w = __float_as_uint(fmaxf(__uint_as_float(x.w), -INFINITY));
-        } else {
-            x.x = bf16x2_max(x.x, 0xff80ff80u);
-            x.y = bf16x2_max(x.y, 0xff80ff80u);
-            x.z = bf16x2_max(x.z, 0xff80ff80u);
-            x.w = bf16x2_max(x.w, 0xff80ff80u);
-        }
-        return x;
-    }
-    // One element of granule v.
-    __device__ __forceinline__ float get(int v, int j) const
-    {
-        float x;
-        if constexpr (F32) {
-            x = v < cached ? reinterpret_cast<const float *>(cache + v)[j] : __uint_as_float(pick(load_granule<F32>(r, gb + v), j));
-        } else {
-            x = v < cached ? __uint_as_float((uint32_t)reinterpret_cast<const uint16_t *>(cache + v)[j] << 16)
-                           : __uint_as_float(pick(load_granule<F32>(r, gb + v), j >> 1) << ((j & 1) ? 0 : 16) & 0xffff0000u);
-        }
-        return x == x ? x : -INFINITY;
-    }
-    static __device__ __forceinline__ uint32_t pick(const uint4 &x, int w)
-    {
-        return w == 0 ? x.x : w == 1 ? x.y : w == 2 ? x.z : x.w;
-    }
-};
-
-__device__ __forceinline__ unsigned long long warp_sum_u64(unsigned long long v)
-{
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    return v;
-}
-
-// Sum over the CTA; the warps' parts stay in sh->wsum until the next call.  Every thread gets the total.
-__device__ __forceinline__ unsigned long long block_sum_u64(unsigned long long v, Shared *sh)
-{
-    v = warp_sum_u64(v);
-    __syncthreads();   // (whoever still reads the parts of the last call)
-    if ((threadIdx.x & 31) == 0) sh->wsum[threadIdx.x >> 5] = v;
-    __syncthreads();
-    unsigned long long t = 0;
-#pragma unroll
-    for (int w = 0; w < kSelWarps; ++w) t += sh->wsum[w];
-    return t;
-}
-
-// Exclusive sums of the threads' values over the CTA, the total in *total.
-__device__ __forceinline__ unsigned long long block_scan_u64(unsigned long long v, Shared *sh, unsigned long long *total)
-{
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    unsigned long long incl = v;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const unsigned long long u = __shfl_up_sync(0xffffffffu, incl, o);
-        if (lane >= o) incl += u;
-    }
-    __syncthreads();
-    if (lane == 31) sh->scan[warp] = incl;
-    __syncthreads();
-    unsigned long long before = 0, t = 0;
-#pragma unroll
-    for (int w = 0; w < kSelWarps; ++w) {
-        if (w < warp) before += sh->scan[w];
-        t += sh->scan[w];
-    }
-    *total = t;
-    return before + incl - v;
-}
-
-// The CTAs' values, in every CTA's slots; returns their buffer (of second values: behind the first ones).
-template <bool F32>
-__device__ __forceinline__ const unsigned long long *cluster_gather(Ctx<F32> &c, unsigned long long v,
-                                                                    unsigned long long second = 0)
-{
-    unsigned long long (*slot)[kRowMaxCluster] = c.sh->slot[c.turn];
-    c.turn ^= 1;
-    if (c.C == 1) {
-        if (threadIdx.x == 0) {
-            slot[0][0] = v;
-            slot[1][0] = second;
-        }
-        __syncthreads();
-        return slot[0];
-    }
-    if (threadIdx.x < (unsigned)c.C) {
-        st_peer_u64(peer_addr(&slot[0][c.rank], threadIdx.x), v);
-        st_peer_u64(peer_addr(&slot[1][c.rank], threadIdx.x), second);
-    }
-    cluster_sync_all();
-    return slot[0];
-}
-
-__device__ __forceinline__ unsigned long long slot_sum(const unsigned long long *slot, int C)
-{
-    unsigned long long t = 0;
-    for (int k = 0; k < C; ++k) t += slot[k];
-    return t;
-}
-
-template <bool F32>
-__device__ __forceinline__ unsigned long long cluster_sum(Ctx<F32> &c, unsigned long long v)
-{
-    return slot_sum(cluster_gather(c, block_sum_u64(v, c.sh)), c.C);
-}
-
-// What is kept: keys above `key`, and of those equal to it the ones up to index `idx` (INT_MIN: none; the places of a
-// granule before the row have indices below 0).
-struct Cut {
-    uint32_t key;
-    int idx;
-    __device__ __forceinline__ bool keeps(uint32_t k, int i) const { return k > key || (k == key && i <= idx); }
-};
-
-// A sum over the row's tokens is given by a functor: elem(logit, key, index) for one of them, granule(c, v) for the
-// ones of granule v.  ByElem makes one of a function of an element.
-template <typename F>
-struct ByElem {
-    F f;
-    __device__ __forceinline__ unsigned long long elem(float x, uint32_t k, int i) const { return f(x, k, i); }
-    template <bool F32>
-    __device__ __forceinline__ unsigned long long granule(const Ctx<F32> &c, int v) const
-    {
-        constexpr int E = RowElem<F32>::kPer;
-        float x[E];
-        granule_floats<F32>(c.get(v), x);
-        const int i0 = c.r.first(c.gb + v);
-        unsigned long long s = 0;
-#pragma unroll
-        for (int j = 0; j < E; ++j) {
-            const uint32_t k = key_of(x[j]);
-            if (k > kKeyNone) s += f(x[j], k, i0 + j);   // (places outside the row are -inf)
-        }
-        return s;
-    }
-};
-template <typename F>
-__device__ __forceinline__ ByElem<F> by_elem(F f) { return ByElem<F>{f}; }
-
-// Sum over this thread's granules, lanes in turn over the warp's run of them.
-template <bool F32, typename S>
-__device__ __forceinline__ unsigned long long thread_sum(const Ctx<F32> &c, const S &f)
-{
-    unsigned long long s = 0;
-    for (int v = c.wb + (int)(threadIdx.x & 31); v < c.we; v += 32) s += f.granule(c, v);
-    return s;
-}
-
-// The first token in the vocabulary's order at which the running sum of f passes `target` (which is below the sum
-// over the row): found(idx, key) by one thread.  The warps' sums are in sh->wsum (block_sum_u64 of thread_sum), the
-// CTAs' are in `slot`.  The CTA that holds the token narrows a run of granules down
-// sixteenfold a step until its threads have a few elements each.
-template <bool F32, typename S, typename Found>
-__device__ __forceinline__ void locate(Ctx<F32> &c, unsigned long long target, const S &f,
-                                       const unsigned long long *slot, Found found)
-{
-    Shared *sh = c.sh;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    unsigned long long before = 0;
-    for (unsigned k = 0; k < c.rank; ++k) before += slot[k];
-    if (target >= before && target - before < slot[c.rank]) {   // (one CTA)
-        unsigned long long t = target - before;
-        int a = 0, b = c.n, per = (c.n + kSelWarps - 1) / kSelWarps;
-        for (;;) {
-            int w = 0;
-            while (w < kSelWarps - 1 && t >= sh->wsum[w]) t -= sh->wsum[w++];
-            a = a + w * per;
-            b = min(b, a + per);
-            if (b - a <= kSelThreads * kFew / RowElem<F32>::kPer) break;
-            per = (b - a + kSelWarps - 1) / kSelWarps;
-            unsigned long long s = 0;
-            const int wb = min(b, a + warp * per), we = min(b, wb + per);
-            for (int v = wb + lane; v < we; v += 32) s += f.granule(c, v);
-            block_sum_u64(s, sh);
-        }
-        // a few elements per thread, in order
-        constexpr int E = RowElem<F32>::kPer;
-        const int n = (b - a) * E, each = (n + kSelThreads - 1) / kSelThreads, first = tid * each;
-        const int i0 = c.r.first(c.gb + a);
-        const auto at = [&](int e, uint32_t *k) {
-            const float x = c.get(a + e / E, e % E);
-            *k = key_of(x);
-            return *k > kKeyNone ? f.elem(x, *k, i0 + e) : 0ull;
-        };
-        uint32_t k;
-        unsigned long long s = 0, total;
-        for (int e = first; e < min(n, first + each); ++e) s += at(e, &k);
-        unsigned long long run = block_scan_u64(s, sh, &total);
-        if (t >= run && t - run < s) {   // (one thread)
-            int e = first;
-            for (const int last = min(n, first + each) - 1;; ++e) {
-                run += at(e, &k);
-                if (run > t || e == last) break;   // (t is below the sum of the thread's elements)
-            }
-            found(i0 + e, k);
-        }
-    }
-}
-
-// The same, with the sums to be taken first; *idx, *key in every CTA.
-template <bool F32, typename S>
-__device__ void sum_and_locate(Ctx<F32> &c, unsigned long long target, const S &f, int *idx, uint32_t *key)
-{
-    const unsigned long long mine = block_sum_u64(thread_sum(c, f), c.sh);
-    const unsigned long long *slot = cluster_gather(c, mine);
-    Shared *sh = c.sh;
-    locate(c, target, f, slot, [&](int i, uint32_t k) {
-        for (int q = 0; q < c.C; ++q) {
-            st_peer_u32(peer_addr(&sh->found_idx, q), (uint32_t)i);
-            st_peer_u32(peer_addr(&sh->found_key, q), k);
-        }
-    });
-    if (c.C > 1) cluster_sync_all();
-    else __syncthreads();
-    *idx = sh->found_idx;
-    *key = sh->found_key;
-}
-
-// The largest key at which sum(f over keys >= it) is at least `want` (1 <= want <= the sum over all): between kmin and
-// kmax, the least and the largest key that f counts.  The sum over the keys above it in *above.
-template <bool F32, typename F>
-__device__ uint32_t bisect_key(Ctx<F32> &c, uint32_t kmin, uint32_t kmax, unsigned long long want, F f,
-                               unsigned long long *above)
-{
-    uint32_t lo = kmin, hi = kmax + 1;   // sum(lo) >= want > sum(hi)
-    unsigned long long s_hi = 0;
-    while (hi - lo > 1) {
-        const uint32_t mid = lo + (hi - lo) / 2;
-        const auto from_mid = by_elem([&](float x, uint32_t k, int i) { return k >= mid ? f(x, k, i) : 0ull; });
-        const unsigned long long s = cluster_sum(c, thread_sum(c, from_mid));
-        if (s >= want) lo = mid;
-        else { hi = mid; s_hi = s; }
-    }
-    *above = s_hi;
-    return lo;
-}
-
-// The cut that keeps the k largest (ties by the lower index); no cut where the row has no more than k.
-template <bool F32>
-__device__ Cut cut_count(Ctx<F32> &c, uint32_t kmax, int k)
-{
-    const auto one = [](float, uint32_t, int) { return 1ull; };
-    if (cluster_sum(c, thread_sum(c, by_elem(one))) <= (unsigned long long)k) return Cut{kKeyNone, INT_MIN};
-    unsigned long long above;
-    Cut cut;
-    cut.key = bisect_key(c, kKeyNone + 1, kmax, (unsigned long long)k, one, &above);
-    const uint32_t at = cut.key;
-    uint32_t key;
-    sum_and_locate(c, (unsigned long long)k - above - 1ull,
-                   by_elem([at](float, uint32_t q, int) { return q == at ? 1ull : 0ull; }), &cut.idx, &key);
-    return cut;
-}
-
 // Granules whose weights' parts add up in 32 bits (256 weights of at most 2^21 and less).
 constexpr int kFlush = 32;
 
@@ -543,151 +226,6 @@ struct KeptMass {
             sum += whole_weight(a1, a2, s);
         }
         return sum;
-    }
-};
-
-// ------------------------------------------------------------------ the list
-constexpr int kListPer = kListCap / kSelThreads;   // list entries of a thread, in a row
-
-// Sorts n2 (a power of two) words descending; all threads of the CTA.
-__device__ void sort_desc(unsigned long long *a, int n2)
-{
-    __syncthreads();
-    for (int k = 2; k <= n2; k <<= 1) {
-        for (int j = k >> 1; j > 0; j >>= 1) {
-            for (int t = threadIdx.x; t < n2 / 2; t += kSelThreads) {
-                const int i = 2 * t - (t & (j - 1));
-                const unsigned long long x = a[i], y = a[i + j];
-                if ((x < y) == ((i & k) == 0)) {
-                    a[i] = y;
-                    a[i + j] = x;
-                }
-            }
-            // pairs at a distance of at most 32 stay within the 64 words of one warp's pairs
-            if (j > 32 || (j == 1 && k >= 64)) __syncthreads();
-            else __syncwarp();
-        }
-    }
-    __syncthreads();
-}
-
-__device__ __forceinline__ int pow2_at_least(int n) { return n <= 1 ? 1 : 1 << (32 - __clz(n - 1)); }
-
-// Brings the CTAs' parts of the list (sh->nlist entries each, of which up to kListCap are there) together in the
-// cluster's first CTA.  Returns how many there are (in every CTA); *ok: they fit and are there.
-template <bool F32>
-__device__ int push_list(Ctx<F32> &c, unsigned long long *list, bool *ok)
-{
-    Shared *sh = c.sh;
-    __syncthreads();
-    const uint32_t mine = sh->nlist;
-    const unsigned long long *slot = cluster_gather(c, (unsigned long long)mine);
-    unsigned long long total = 0, before = 0;
-    for (int k = 0; k < c.C; ++k) {
-        if (k < (int)c.rank) before += slot[k];
-        total += slot[k];
-    }
-    *ok = total <= kListCap;
-    if (*ok && c.C > 1) {
-        if (c.rank != 0)
-            for (uint32_t i = threadIdx.x; i < mine; i += kSelThreads)
-                st_peer_u64(peer_addr(list + before + i, 0), list[i]);
-        cluster_sync_all();
-    }
-    return (int)(total < (unsigned long long)INT_MAX ? total : INT_MAX);
-}
-
-// Elements with keys from `bound` on that `cut` keeps, to the list of the cluster's first CTA, in no order (push_list).
-template <bool F32>
-__device__ int gather_list(Ctx<F32> &c, unsigned long long *list, uint32_t bound, Cut cut, bool *ok)
-{
-    constexpr int E = RowElem<F32>::kPer;
-    Shared *sh = c.sh;
-    const float fb = key_float(bound);
-    if (threadIdx.x == 0) sh->nlist = 0;
-    __syncthreads();
-    for (int v = c.wb + (int)(threadIdx.x & 31); v < c.we; v += 32) {
-        const uint4 x = c.get(v);
-        if (!(granule_max<F32>(x) >= fb)) continue;
-        float f[E];
-        granule_floats<F32>(x, f);
-        const int i0 = c.r.first(c.gb + v);
-#pragma unroll
-        for (int j = 0; j < E; ++j) {
-            const uint32_t k = key_of(f[j]);
-            if (k >= bound && k > kKeyNone && cut.keeps(k, i0 + j)) {
-                const uint32_t at = atomicAdd(&sh->nlist, 1u);
-                if (at < kListCap) list[at] = ((unsigned long long)k << 32) | (uint32_t)~(uint32_t)(i0 + j);
-            }
-        }
-    }
-    return push_list(c, list, ok);
-}
-
-// Pads the list with zeros and sorts it; n <= kListCap.  (First CTA.)
-__device__ void sort_list(unsigned long long *list, int n)
-{
-    const int n2 = pow2_at_least(n);
-    for (int i = n + threadIdx.x; i < n2; i += kSelThreads) list[i] = 0ull;
-    sort_desc(list, n2);
-}
-
-// A list of at most kSmall entries needs no sorting: each is compared with all others, by kSelThreads / (the entries'
-// number, rounded up to a power of two) threads each.  (128 entries: sorting took 3 us, this a fifth of it.)
-constexpr int kSmall = 256;
-struct Small {
-    unsigned long long e;   // (key << 32) | ~index
-    int i, part, per;       // the entry, the thread's part of the comparisons, threads per entry (a power of two <= 16)
-    bool on;
-
-    __device__ __forceinline__ Small(const unsigned long long *list, int n)
-    {
-        const int n2 = max(32, pow2_at_least(n));
-        per = kSelThreads / n2;
-        i = (int)threadIdx.x / per;
-        part = (int)threadIdx.x & (per - 1);
-        on = i < n;
-        e = on ? list[i] : 0ull;
-    }
-    __device__ __forceinline__ uint32_t key() const { return (uint32_t)(e >> 32); }
-    __device__ __forceinline__ int idx() const { return (int)~(uint32_t)e; }
-    // Weights lie behind the entries.
-    __device__ __forceinline__ void put_weight(unsigned long long *list, unsigned long long w) const
-    {
-        if (part == 0 && on) list[kSmall + i] = w;
-    }
-    // Number of the entries before this one in descending order, and (weights given) their sum.
-    __device__ __forceinline__ int larger(const unsigned long long *list, int n) const
-    {
-        int rank = 0;
-        for (int j = part; j < n; j += per) rank += list[j] > e;
-        for (int o = per / 2; o > 0; o >>= 1) rank += __shfl_xor_sync(0xffffffffu, rank, o);
-        return rank;
-    }
-    __device__ __forceinline__ void larger(const unsigned long long *list, int n, int *rank, unsigned long long *sum) const
-    {
-        int r = 0;
-        unsigned long long s = 0;
-        for (int j = part; j < n; j += per)
-            if (list[j] > e) {
-                ++r;
-                s += list[kSmall + j];
-            }
-        for (int o = per / 2; o > 0; o >>= 1) {
-            r += __shfl_xor_sync(0xffffffffu, r, o);
-            s += __shfl_xor_sync(0xffffffffu, s, o);
-        }
-        *rank = r;
-        *sum = s;
-    }
-    // Sum of the weights of the entries with lower indices.
-    __device__ __forceinline__ unsigned long long earlier(const unsigned long long *list, int n) const
-    {
-        unsigned long long s = 0;
-        for (int j = part; j < n; j += per)
-            if ((uint32_t)list[j] > (uint32_t)e) s += list[kSmall + j];
-        for (int o = per / 2; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-        return s;
     }
 };
 
@@ -988,167 +526,6 @@ __device__ Nucleus cut_mass(Ctx<F32> &c, const Scale &s, const float2 *tab, unsi
     return Nucleus{cut_ties(c, key, weight(key_float(key), s, tab), above, want, by_k), false};
 }
 
-// Sends for a thread's first granules.
-template <bool F32>
-__device__ __forceinline__ void start_row(const Ctx<F32> &c, uint4 *cache)
-{
-    if (c.C > 1) cluster_arrive();   // (load_row waits)
-    const int end = min(c.we, c.cached);
-    for (int i = 0; i < kAhead; ++i) {
-        const int v = c.wb + (int)(threadIdx.x & 31) + 32 * i;
-        if (v < end) fetch_granule<F32>(c.r, c.gb + v, cache + v);
-        cp_async_commit();
-    }
-}
-
-// Brings the row in and finds its largest key and, for want > 0, a bound with at least `want` elements at or above
-// it (or below every element, if there are not so many).  scratch: kBoundBins words.
-constexpr int kBoundBins = 512;
-template <bool F32>
-__device__ void load_row(Ctx<F32> &c, uint4 *cache, int want, uint32_t *scratch, uint32_t *kmax, uint32_t *bound)
-{
-    constexpr int NG = F32 ? 4 : 8;   // groups of a thread
-    Shared *sh = c.sh;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    if (want > 0)
-        for (int i = tid; i < kBoundBins; i += kSelThreads) scratch[i] = 0u;
-    uint32_t gm[4] = {0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u};
-    if constexpr (!F32)
-        for (int k = 0; k < 4; ++k) gm[k] = 0xff80ff80u;
-    const auto join = [&](const uint4 &x) {
-        if constexpr (F32) {
-            gm[0] = __float_as_uint(fmaxf(__uint_as_float(gm[0]), __uint_as_float(x.x)));
-            gm[1] = __float_as_uint(fmaxf(__uint_as_float(gm[1]), __uint_as_float(x.y)));
-            gm[2] = __float_as_uint(fmaxf(__uint_as_float(gm[2]), __uint_as_float(x.z)));
-            gm[3] = __float_as_uint(fmaxf(__uint_as_float(gm[3]), __uint_as_float(x.w)));
-        } else {
-            gm[0] = bf16x2_max(gm[0], x.x);
-            gm[1] = bf16x2_max(gm[1], x.y);
-            gm[2] = bf16x2_max(gm[2], x.z);
-            gm[3] = bf16x2_max(gm[3], x.w);
-        }
-    };
-    const int end = min(c.we, c.cached);
-    for (int v = c.wb + lane; v < end; v += 32) {
-        cp_async_wait<kAhead - 1>();
-        join(cache[v]);
-        const int next = v + 32 * kAhead;
-        if (next < end) fetch_granule<F32>(c.r, c.gb + next, cache + next);
-        cp_async_commit();
-    }
-    for (int v = max(c.wb, c.cached) + lane; v < c.we; v += 32) join(load_granule<F32>(c.r, c.gb + v));
-
-    // the groups' keys, the largest and the least that is one
-    uint32_t key[NG], top = 0, least = 0xffffffffu;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        if constexpr (F32) {
-            key[k] = key_of(__uint_as_float(gm[k]));
-        } else {
-            key[2 * k] = key_of(bf16_lo(gm[k]));
-            key[2 * k + 1] = key_of(bf16_hi(gm[k]));
-        }
-    }
-#pragma unroll
-    for (int k = 0; k < NG; ++k) {
-        top = max(top, key[k]);
-        if (key[k] > kKeyNone) least = min(least, key[k]);
-    }
-    top = __reduce_max_sync(0xffffffffu, top);
-    least = __reduce_min_sync(0xffffffffu, least);
-    if (lane == 0) {
-        sh->ktop[warp] = top;
-        sh->klow[warp] = least;
-    }
-    if (tid == 0) sh->border = kBoundBins;
-    __syncthreads();
-    top = __reduce_max_sync(0xffffffffu, sh->ktop[lane & (kSelWarps - 1)]);
-    least = __reduce_min_sync(0xffffffffu, sh->klow[lane & (kSelWarps - 1)]);
-
-    uint32_t low = kKeyNone + 1;
-    if (want > 0) {
-        // a value that R of this CTA's group maxima reach: their histogram from the largest down, in equal steps
-        const int R = (want + c.C - 1) / c.C;
-        const float ft = key_float(top), range = ft - key_float(least);
-        const float scale = range > 0.f && range < INFINITY ? (float)kBoundBins / range : 0.f;
-        const auto bin = [&](uint32_t k) { return (int)fminf((ft - key_float(k)) * scale, (float)(kBoundBins - 1)); };
-#pragma unroll
-        for (int k = 0; k < NG; ++k)
-            if (key[k] > kKeyNone) atomicAdd(scratch + (scale > 0.f ? bin(key[k]) : 0), 1u);
-        __syncthreads();
-        if (warp == 0) {
-            constexpr int kPer = kBoundBins / 32;
-            uint32_t n[kPer], sum = 0;
-#pragma unroll
-            for (int k = 0; k < kPer; ++k) {
-                n[k] = scratch[lane * kPer + k];
-                sum += n[k];
-            }
-            uint32_t incl = sum;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const uint32_t u = __shfl_up_sync(0xffffffffu, incl, o);
-                if (lane >= o) incl += u;
-            }
-            uint32_t run = incl - sum;
-            if (run < (uint32_t)R && incl >= (uint32_t)R) {   // (at most one lane)
-                int b = lane * kPer;
-#pragma unroll
-                for (int k = 0; k < kPer; ++k) {
-                    run += n[k];
-                    b += run < (uint32_t)R;
-                }
-                sh->border = b;
-            }
-        }
-        __syncthreads();
-        // the least group maximum down to that step; everything, where there are fewer than R
-        const int border = sh->border;
-        uint32_t at = 0xffffffffu;
-#pragma unroll
-        for (int k = 0; k < NG; ++k)
-            if (key[k] > kKeyNone && (scale > 0.f ? bin(key[k]) : 0) <= border) at = min(at, key[k]);
-        at = __reduce_min_sync(0xffffffffu, at);
-        if (lane == 0) sh->klow[warp] = at;
-        __syncthreads();
-        at = __reduce_min_sync(0xffffffffu, sh->klow[lane & (kSelWarps - 1)]);
-        if (border < kBoundBins) low = at;
-    }
-    if (c.C > 1) {
-        cluster_wait();
-        if (tid < c.C) {
-            st_peer_u32(peer_addr(&sh->kmax[c.rank], tid), top);
-            st_peer_u32(peer_addr(&sh->bound[c.rank], tid), low);
-        }
-        cluster_sync_all();
-        for (int k = 0; k < c.C; ++k) {
-            top = max(top, sh->kmax[k]);
-            low = min(low, sh->bound[k]);
-        }
-    } else {
-        __syncthreads();
-    }
-    *kmax = top;
-    *bound = low;
-}
-
-template <bool F32>
-__device__ __forceinline__ void set_ctx(Ctx<F32> &c, const uint4 *cache, int cached, int C, Shared *sh)
-{
-    c.C = C;
-    c.rank = blockIdx.x % C;
-    const int per = (c.r.G + C - 1) / C;
-    c.gb = min(c.r.G, (int)c.rank * per);
-    c.n = min(c.r.G - c.gb, per);
-    const int wper = (c.n + kSelWarps - 1) / kSelWarps, warp = threadIdx.x >> 5;
-    c.wb = min(c.n, warp * wper);
-    c.we = min(c.n, c.wb + wper);
-    c.cached = cached;
-    c.cache = cache;
-    c.sh = sh;
-    c.turn = 0;
-}
-
 // The lowest index that has the largest key.
 template <bool F32>
 __device__ int lowest_at(Ctx<F32> &c, uint32_t kmax)
@@ -1174,55 +551,6 @@ __device__ int lowest_at(Ctx<F32> &c, uint32_t kmax)
     const unsigned long long *slot = cluster_gather(c, (unsigned long long)(unsigned)best);
     for (int k = 0; k < c.C; ++k) best = min(best, (int)(unsigned)slot[k]);
     return best;
-}
-
-struct TopParams {
-    const void *z;
-    int64_t ld;
-    int T, V, K;
-    float *values;
-    int32_t *idx;
-    int cluster, cached;
-};
-
-template <bool F32>
-__global__ void __launch_bounds__(kSelThreads, kSelPerSm) top_kernel(const TopParams p)
-{
-    extern __shared__ __align__(16) uint4 smem[];
-    __shared__ Shared sh;
-    const int row = blockIdx.x / p.cluster;
-    unsigned long long *list = reinterpret_cast<unsigned long long *>(smem + p.cached);
-    Ctx<F32> c{Row<F32>(p.z, row, p.ld, p.V)};
-    set_ctx(c, smem, p.cached, p.cluster, &sh);
-    start_row(c, smem);
-    uint32_t kmax, bound;
-    load_row(c, smem, p.K, reinterpret_cast<uint32_t *>(list), &kmax, &bound);
-    bool ok;
-    int n = gather_list(c, list, bound, Cut{kKeyNone, INT_MIN}, &ok);
-    if (!ok) {   // (the same in every CTA of the row)
-        const Cut cut = cut_count(c, kmax, p.K);
-        n = gather_list(c, list, max(cut.key, kKeyNone + 1), cut, &ok);   // at most K
-    }
-    if (c.rank != 0) return;   // (nobody reads this CTA's memory any more)
-    if (n <= kSmall) {
-        const Small e(list, n);
-        const int at = e.larger(list, n);
-        if (e.on && e.part == 0 && at < p.K) {
-            p.values[(size_t)row * p.K + at] = key_float(e.key());
-            p.idx[(size_t)row * p.K + at] = e.idx();
-        }
-        for (int i = n + threadIdx.x; i < p.K; i += kSelThreads) {
-            p.values[(size_t)row * p.K + i] = -INFINITY;
-            p.idx[(size_t)row * p.K + i] = -1;
-        }
-        return;
-    }
-    sort_list(list, n);
-    for (int i = threadIdx.x; i < p.K; i += kSelThreads) {
-        const unsigned long long e = i < n ? list[i] : 0ull;
-        p.values[(size_t)row * p.K + i] = i < n ? key_float((uint32_t)(e >> 32)) : -INFINITY;
-        p.idx[(size_t)row * p.K + i] = i < n ? (int32_t)~(uint32_t)e : -1;
-    }
 }
 
 struct SampleParams {
@@ -1425,53 +753,6 @@ __global__ void __launch_bounds__(kSelThreads, kSelPerSm) sample_kernel(const Sa
     });
 }
 
-int logits_cluster(int rows, int64_t row_bytes)
-{
-    int C = 1;
-    while (C < kRowMaxCluster && (row_bytes > (int64_t)C * (int64_t)kShare ||
-                                  ((int64_t)rows * C < 2 * 152 && row_bytes >= 2 * (int64_t)C * kSelThreads * 16)))
-        C *= 2;
-    return C;
-}
-
-// Cluster and shared memory of a launch over `rows` rows.
-constexpr size_t kMaxSmem = kMaxCache + (size_t)kListCap * 8;
-static_assert(kMaxSmem + 11 * 1024 <= kSmemPerCta, "with the kernels' static part");
-
-template <bool F32, auto Kern, typename P>
-cudaError_t launch_rows(P p, int rows, cudaStream_t st)
-{
-    const int64_t bytes = (int64_t)p.V * RowElem<F32>::kBytes;
-    p.cluster = logits_cluster(rows, bytes);
-    const size_t share = (size_t)((bytes + 32 + p.cluster - 1) / p.cluster) + 32;
-    p.cached = (int)((share < kMaxCache ? share : kMaxCache) / 16);
-    const size_t smem = (size_t)p.cached * 16 + kListCap * 8;
-    return launch_clusters<Kern>((int64_t)rows * p.cluster, kSelThreads, smem, kMaxSmem, p.cluster, st, p);
-}
-
-sats_status check_rows(const void *logits, int64_t ld, int rows, int V, int bytes)
-{
-    if (rows < 0 || V < 1 || ld < V) return SATS_EINVAL;
-    if (V > INT_MAX - 64 || rows > INT_MAX / kRowMaxCluster || ld > (int64_t)1 << 40) return SATS_ESHAPE;
-    if (rows > 0 && (!logits || reinterpret_cast<uintptr_t>(logits) % bytes)) return SATS_EINVAL;
-    return SATS_OK;
-}
-
-template <bool F32>
-sats_status top_logits(const void *logits, int64_t ld, int T, int V, int K, float *values, int32_t *idx, void *stream)
-{
-    const sats_status s = check_rows(logits, ld, T, V, RowElem<F32>::kBytes);
-    if (s != SATS_OK) return s;
-    if (K < 1 || K > V) return SATS_EINVAL;
-    if (K > kMaxTop) return SATS_ESHAPE;
-    if (T == 0) return SATS_OK;
-    if (!values || !idx) return SATS_EINVAL;
-    TopParams p{};
-    p.z = logits; p.ld = ld; p.T = T; p.V = V; p.K = K; p.values = values; p.idx = idx;
-    const cudaError_t e = launch_rows<F32, top_kernel<F32>>(p, T, static_cast<cudaStream_t>(stream));
-    return e == cudaSuccess ? SATS_OK : cuda_fail(e, "top-logits kernel launch");
-}
-
 template <bool F32>
 sats_status sample(const void *logits, int64_t ld, int B, int V, const float *temperature, const int32_t *top_k,
                    const float *top_p, const float *min_p, const float *u, int32_t *ids, float *logprob,
@@ -1491,18 +772,6 @@ sats_status sample(const void *logits, int64_t ld, int B, int V, const float *te
 }  // namespace sats
 
 extern "C" {
-
-sats_status sats_top_logits(const void *logits, int64_t ld, int T, int V, int K, float *values, int32_t *idx,
-                            void *stream)
-{
-    return sats::top_logits<false>(logits, ld, T, V, K, values, idx, stream);
-}
-
-sats_status sats_top_logits_f32(const float *logits, int64_t ld, int T, int V, int K, float *values, int32_t *idx,
-                                void *stream)
-{
-    return sats::top_logits<true>(logits, ld, T, V, K, values, idx, stream);
-}
 
 sats_status sats_sample(const void *logits, int64_t ld, int B, int V, const float *temperature, const int32_t *top_k,
                         const float *top_p, const float *min_p, const float *u, int32_t *ids, float *logprob,
