@@ -69,11 +69,13 @@ struct Ctx {
     int C;
     unsigned rank;
     int turn;             // of the all-reduce buffers
+    int cap;              // entries of the list, kListCap at most
 
-    // Granule v of this CTA's, NaN replaced by -inf.
-    __device__ __forceinline__ uint4 get(int v) const
+    // Granule v of this CTA's; get: with NaN replaced by -inf.
+    __device__ __forceinline__ uint4 raw(int v) const { return v < cached ? cache[v] : load_granule<F32>(r, gb + v); }
+    __device__ __forceinline__ uint4 get(int v) const { return clean(raw(v)); }
+    static __device__ __forceinline__ uint4 clean(uint4 x)
     {
-        uint4 x = v < cached ? cache[v] : load_granule<F32>(r, gb + v);
         if constexpr (F32) {
             x.x = __float_as_uint(fmaxf(__uint_as_float(x.x), -INFINITY));
             x.y = __float_as_uint(fmaxf(__uint_as_float(x.y), -INFINITY));
@@ -358,21 +360,19 @@ __device__ void sort_desc(unsigned long long *a, int n2)
 
 __device__ __forceinline__ int pow2_at_least(int n) { return n <= 1 ? 1 : 1 << (32 - __clz(n - 1)); }
 
-// Brings the CTAs' parts of the list (sh->nlist entries each, of which up to kListCap are there) together in the
+// Brings the CTAs' parts of the list (sh->nlist entries each, of which up to c.cap are there) together in the
 // cluster's first CTA.  Returns how many there are (in every CTA); *ok: they fit and are there.
 template <bool F32>
 __device__ int push_list(Ctx<F32> &c, unsigned long long *list, bool *ok)
 {
-    Shared *sh = c.sh;
-    __syncthreads();
-    const uint32_t mine = sh->nlist;
+    const uint32_t mine = c.sh->nlist;
     const unsigned long long *slot = cluster_gather(c, (unsigned long long)mine);
     unsigned long long total = 0, before = 0;
     for (int k = 0; k < c.C; ++k) {
         if (k < (int)c.rank) before += slot[k];
         total += slot[k];
     }
-    *ok = total <= kListCap;
+    *ok = total <= (unsigned long long)c.cap;
     if (*ok && c.C > 1) {
         if (c.rank != 0)
             for (uint32_t i = threadIdx.x; i < mine; i += kSelThreads)
@@ -382,9 +382,10 @@ __device__ int push_list(Ctx<F32> &c, unsigned long long *list, bool *ok)
     return (int)(total < (unsigned long long)INT_MAX ? total : INT_MAX);
 }
 
-// Elements with keys from `bound` on that `cut` keeps, to the list of the cluster's first CTA, in no order (push_list).
+// This CTA's elements with keys from `bound` on that `cut` keeps, to `list`, in no order; returns how many there are (of
+// which `cap` at most are in the list).
 template <bool F32>
-__device__ int gather_list(Ctx<F32> &c, unsigned long long *list, uint32_t bound, Cut cut, bool *ok)
+__device__ int collect(Ctx<F32> &c, unsigned long long *list, int cap, uint32_t bound, Cut cut)
 {
     constexpr int E = RowElem<F32>::kPer;
     Shared *sh = c.sh;
@@ -392,20 +393,30 @@ __device__ int gather_list(Ctx<F32> &c, unsigned long long *list, uint32_t bound
     if (threadIdx.x == 0) sh->nlist = 0;
     __syncthreads();
     for (int v = c.wb + (int)(threadIdx.x & 31); v < c.we; v += 32) {
-        const uint4 x = c.get(v);
+        const uint4 x = c.raw(v);
         if (!(granule_max<F32>(x) >= fb)) continue;
         float f[E];
-        granule_floats<F32>(x, f);
+        granule_floats<F32>(c.clean(x), f);
         const int i0 = c.r.first(c.gb + v);
 #pragma unroll
         for (int j = 0; j < E; ++j) {
+            if (!(f[j] >= fb)) continue;
             const uint32_t k = key_of(f[j]);
             if (k >= bound && k > kKeyNone && cut.keeps(k, i0 + j)) {
                 const uint32_t at = atomicAdd(&sh->nlist, 1u);
-                if (at < kListCap) list[at] = ((unsigned long long)k << 32) | (uint32_t)~(uint32_t)(i0 + j);
+                if (at < (uint32_t)cap) list[at] = ((unsigned long long)k << 32) | (uint32_t)~(uint32_t)(i0 + j);
             }
         }
     }
+    __syncthreads();
+    return (int)sh->nlist;
+}
+
+// The same of the whole row, to the list of the cluster's first CTA (push_list).
+template <bool F32>
+__device__ int gather_list(Ctx<F32> &c, unsigned long long *list, uint32_t bound, Cut cut, bool *ok)
+{
+    collect(c, list, c.cap, bound, cut);
     return push_list(c, list, ok);
 }
 
@@ -419,7 +430,8 @@ __device__ void sort_list(unsigned long long *list, int n)
 
 // A list of at most kSmall entries needs no sorting: each is compared with all others, by kSelThreads / (the entries'
 // number, rounded up to a power of two) threads each.  (128 entries: sorting took 3 us, this a fifth of it.)
-constexpr int kSmall = 256;
+constexpr int kSmall = 256;   // (at most kSelThreads)
+static_assert(kSmall <= kSelThreads, "a thread per entry");
 struct Small {
     unsigned long long e;   // (key << 32) | ~index
     int i, part, per;       // the entry, the thread's part of the comparisons, threads per entry (a power of two <= 16)
@@ -526,24 +538,24 @@ __device__ void load_row(Ctx<F32> &c, uint4 *cache, int want, uint32_t *scratch,
     }
     for (int v = max(c.wb, c.cached) + lane; v < c.we; v += 32) join(load_granule<F32>(c.r, c.gb + v));
 
-    // the groups' keys, the largest and the least that is one
-    uint32_t key[NG], top = 0, least = 0xffffffffu;
+    // the groups' maxima, the largest and the least that is above -inf
+    float g[NG], hi = -INFINITY, lo = INFINITY;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         if constexpr (F32) {
-            key[k] = key_of(__uint_as_float(gm[k]));
+            g[k] = fmaxf(__uint_as_float(gm[k]), -INFINITY);
         } else {
-            key[2 * k] = key_of(bf16_lo(gm[k]));
-            key[2 * k + 1] = key_of(bf16_hi(gm[k]));
+            g[2 * k] = fmaxf(bf16_lo(gm[k]), -INFINITY);
+            g[2 * k + 1] = fmaxf(bf16_hi(gm[k]), -INFINITY);
         }
     }
 #pragma unroll
     for (int k = 0; k < NG; ++k) {
-        top = max(top, key[k]);
-        if (key[k] > kKeyNone) least = min(least, key[k]);
+        hi = fmaxf(hi, g[k]);
+        if (want > 0 && g[k] > -INFINITY) lo = fminf(lo, g[k]);
     }
-    top = __reduce_max_sync(0xffffffffu, top);
-    least = __reduce_min_sync(0xffffffffu, least);
+    uint32_t top = __reduce_max_sync(0xffffffffu, key_of(hi));
+    uint32_t least = __reduce_min_sync(0xffffffffu, key_of(lo));
     if (lane == 0) {
         sh->ktop[warp] = top;
         sh->klow[warp] = least;
@@ -551,18 +563,20 @@ __device__ void load_row(Ctx<F32> &c, uint4 *cache, int want, uint32_t *scratch,
     if (tid == 0) sh->border = kBoundBins;
     __syncthreads();
     top = __reduce_max_sync(0xffffffffu, sh->ktop[lane & (kSelWarps - 1)]);
-    least = __reduce_min_sync(0xffffffffu, sh->klow[lane & (kSelWarps - 1)]);
 
     uint32_t low = kKeyNone + 1;
     if (want > 0) {
         // a value that R of this CTA's group maxima reach: their histogram from the largest down, in equal steps
-        const int R = (want + c.C - 1) / c.C;
+        least = __reduce_min_sync(0xffffffffu, sh->klow[lane & (kSelWarps - 1)]);
+        const int R = (want + c.C - 1) >> (31 - __clz(c.C));
         const float ft = key_float(top), range = ft - key_float(least);
-        const float scale = range > 0.f && range < INFINITY ? (float)kBoundBins / range : 0.f;
-        const auto bin = [&](uint32_t k) { return (int)fminf((ft - key_float(k)) * scale, (float)(kBoundBins - 1)); };
+        const float scale = range > 0.f && range < INFINITY ? (float)kBoundBins / range : 0.f;   // (0: one step)
+        int bin[NG];
 #pragma unroll
-        for (int k = 0; k < NG; ++k)
-            if (key[k] > kKeyNone) atomicAdd(scratch + (scale > 0.f ? bin(key[k]) : 0), 1u);
+        for (int k = 0; k < NG; ++k) {
+            bin[k] = scale > 0.f ? (int)fminf((ft - g[k]) * scale, (float)(kBoundBins - 1)) : 0;
+            if (g[k] > -INFINITY) atomicAdd(scratch + bin[k], 1u);
+        }
         __syncthreads();
         if (warp == 0) {
             constexpr int kPer = kBoundBins / 32;
@@ -592,15 +606,15 @@ __device__ void load_row(Ctx<F32> &c, uint4 *cache, int want, uint32_t *scratch,
         __syncthreads();
         // the least group maximum down to that step; everything, where there are fewer than R
         const int border = sh->border;
-        uint32_t at = 0xffffffffu;
+        float at = INFINITY;
 #pragma unroll
         for (int k = 0; k < NG; ++k)
-            if (key[k] > kKeyNone && (scale > 0.f ? bin(key[k]) : 0) <= border) at = min(at, key[k]);
-        at = __reduce_min_sync(0xffffffffu, at);
-        if (lane == 0) sh->klow[warp] = at;
+            if (bin[k] <= border && g[k] > -INFINITY) at = fminf(at, g[k]);
+        least = __reduce_min_sync(0xffffffffu, key_of(at));
+        if (lane == 0) sh->klow[warp] = least;
         __syncthreads();
-        at = __reduce_min_sync(0xffffffffu, sh->klow[lane & (kSelWarps - 1)]);
-        if (border < kBoundBins) low = at;
+        least = __reduce_min_sync(0xffffffffu, sh->klow[lane & (kSelWarps - 1)]);
+        if (border < kBoundBins) low = least;
     }
     if (c.C > 1) {
         cluster_wait();
@@ -621,11 +635,13 @@ __device__ void load_row(Ctx<F32> &c, uint4 *cache, int want, uint32_t *scratch,
 }
 
 template <bool F32>
-__device__ __forceinline__ void set_ctx(Ctx<F32> &c, const uint4 *cache, int cached, int C, Shared *sh)
+__device__ __forceinline__ void set_ctx(Ctx<F32> &c, const uint4 *cache, int cached, int C, Shared *sh,
+                                        int cap = kListCap)
 {
     c.C = C;
-    c.rank = blockIdx.x % C;
-    const int per = (c.r.G + C - 1) / C;
+    c.cap = cap;
+    c.rank = blockIdx.x & (C - 1);
+    const int per = (c.r.G + C - 1) >> (31 - __clz(C));   // (C is a power of two)
     c.gb = min(c.r.G, (int)c.rank * per);
     c.n = min(c.r.G - c.gb, per);
     const int wper = (c.n + kSelWarps - 1) / kSelWarps, warp = threadIdx.x >> 5;
@@ -638,11 +654,14 @@ __device__ __forceinline__ void set_ctx(Ctx<F32> &c, const uint4 *cache, int cac
 }
 
 // ------------------------------------------------------------------ launches (host)
-int logits_cluster(int rows, int64_t row_bytes)
+// CTAs of a row: so many that a share leaves room for other CTAs on the SM, that few rows fill the GPU, and that the
+// list of `want` entries falls to each in parts of at most kSmall.
+int logits_cluster(int rows, int64_t row_bytes, int want)
 {
     int C = 1;
     while (C < kRowMaxCluster && (row_bytes > (int64_t)C * (int64_t)kShare ||
-                                  ((int64_t)rows * C < 2 * 152 && row_bytes >= 2 * (int64_t)C * kSelThreads * 16)))
+                                  (((int64_t)rows * C < 2 * 152 || want > C * (kSmall * 3 / 4)) &&
+                                   row_bytes >= 2 * (int64_t)C * kSelThreads * 16)))
         C *= 2;
     return C;
 }
@@ -652,13 +671,13 @@ constexpr size_t kMaxSmem = kMaxCache + (size_t)kListCap * 8;
 static_assert(kMaxSmem + 11 * 1024 <= kSmemPerCta, "with the kernels' static part");
 
 template <bool F32, auto Kern, typename P>
-cudaError_t launch_rows(P p, int rows, cudaStream_t st)
+cudaError_t launch_rows(P p, int rows, int cap, int want, cudaStream_t st)
 {
     const int64_t bytes = (int64_t)p.V * RowElem<F32>::kBytes;
-    p.cluster = logits_cluster(rows, bytes);
+    p.cluster = logits_cluster(rows, bytes, want);
     const size_t share = (size_t)((bytes + 32 + p.cluster - 1) / p.cluster) + 32;
     p.cached = (int)((share < kMaxCache ? share : kMaxCache) / 16);
-    const size_t smem = (size_t)p.cached * 16 + kListCap * 8;
+    const size_t smem = (size_t)p.cached * 16 + (size_t)cap * 8;
     return launch_clusters<Kern>((int64_t)rows * p.cluster, kSelThreads, smem, kMaxSmem, p.cluster, st, p);
 }
 

@@ -190,10 +190,10 @@ struct KeptMass {
     __device__ __forceinline__ void add(const Ctx<F32> &c, int v, int &a1, int &a2, int &n) const
     {
         constexpr int P = RowElem<F32>::kPer / 2;
-        const uint4 x = c.get(v);
+        const uint4 x = c.raw(v);
         if (!(granule_max<F32>(x) >= at)) return;
         f32x2 z[P];
-        granule_pairs<F32>(x, z);
+        granule_pairs<F32>(c.clean(x), z);
         const int i0 = c.r.first(c.gb + v);
         if (s.hard) {
 #pragma unroll
@@ -587,7 +587,7 @@ __global__ void __launch_bounds__(kSelThreads, kSelPerSm) sample_kernel(const Sa
     extern __shared__ __align__(16) uint4 smem[];
     __shared__ Shared sh;
     __shared__ float2 tab[1024];
-    const int row = blockIdx.x / p.cluster, tid = threadIdx.x;
+    const int row = (int)(blockIdx.x >> (31 - __clz(p.cluster))), tid = threadIdx.x;
     unsigned long long *list = reinterpret_cast<unsigned long long *>(smem + p.cached);
     Ctx<F32> c{Row<F32>(p.z, row, p.ld, p.V)};
     set_ctx(c, smem, p.cached, p.cluster, &sh);
@@ -597,7 +597,7 @@ __global__ void __launch_bounds__(kSelThreads, kSelPerSm) sample_kernel(const Sa
     const float u = p.u[row];
     int k = p.top_k ? p.top_k[row] : 0;
     if (!(T >= 0.f) || T == INFINITY || top_p != top_p || !(min_p <= 1.f) || !(u >= 0.f && u < 1.f)) {
-        if (blockIdx.x % p.cluster == 0 && tid == 0) {
+        if (c.rank == 0 && tid == 0) {
             put_sample(p, row, -1, __int_as_float(0x7fffffff), 0);
             if (p.status) atomicOr(p.status, kStatusBadToken);
         }
@@ -764,7 +764,7 @@ sats_status sample(const void *logits, int64_t ld, int B, int V, const float *te
     SampleParams p{};
     p.z = logits; p.ld = ld; p.B = B; p.V = V; p.temperature = temperature; p.top_k = top_k; p.top_p = top_p;
     p.min_p = min_p; p.u = u; p.ids = ids; p.logprob = logprob; p.n_kept = n_kept; p.status = dev_status;
-    const cudaError_t e = launch_rows<F32, sample_kernel<F32>>(p, B, static_cast<cudaStream_t>(stream));
+    const cudaError_t e = launch_rows<F32, sample_kernel<F32>>(p, B, kListCap, 0, static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? SATS_OK : cuda_fail(e, "sampling kernel launch");
 }
 
