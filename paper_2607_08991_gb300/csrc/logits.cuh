@@ -1,7 +1,6 @@
 // logits.cuh -- the top logits of a row and the drawing of a token from it: what top_logits.cu and sample.cu share.
 //
-// One row per thread-block cluster.  The row's share of a CTA is brought to shared memory once; all passes after
-// that run there.  Both calls start from the row's largest logits:
+// One row per thread-block cluster.  Both calls start from the row's largest logits:
 //   - while the row arrives, each thread keeps the maxima of a few groups of its elements.  At least R groups have
 //     their maximum at or above the R-th largest of these maxima, so that at least R elements do: with
 //     R = ceil(K / C) in each of C CTAs, the least of their bounds has K elements of the row at or above it;
@@ -25,9 +24,6 @@ constexpr int kMaxTop = 1024;          // largest K of the list's way
 constexpr int kListCap = 2048;         // entries of the list
 constexpr uint32_t kKeyNone = 0x007fffffu;   // key of -inf: never selected
 constexpr int kFew = 8;                // elements per thread at the end of a search
-constexpr int kAhead = 8;              // granules in flight per thread while the row arrives
-constexpr size_t kShare = 64 * 1024;   // of a row's bytes per CTA, where the cluster allows
-constexpr size_t kMaxCache = 184 * 1024;
 
 // Keys order as the floats do; both zeros have one key.  NaN has none (cleaned to -inf before).
 __device__ __forceinline__ uint32_t key_of(float x)
@@ -49,7 +45,7 @@ struct Shared {
     int part[kSelWarps];
     uint32_t ktop[kSelWarps], klow[kSelWarps];
     int border;
-    uint32_t nlist;
+    uint32_t nlist, nhits;
     int found_idx;
     uint32_t found_key;
     uint32_t kminp;
@@ -488,150 +484,72 @@ struct Small {
     }
 };
 
-// Sends for a thread's first granules.
-template <bool F32>
-__device__ __forceinline__ void start_row(const Ctx<F32> &c, uint4 *cache)
-{
-    if (c.C > 1) cluster_arrive();   // (load_row waits)
-    const int end = min(c.we, c.cached);
-    for (int i = 0; i < kAhead; ++i) {
-        const int v = c.wb + (int)(threadIdx.x & 31) + 32 * i;
-        if (v < end) fetch_granule<F32>(c.r, c.gb + v, cache + v);
-        cp_async_commit();
-    }
-}
-
-// Brings the row in and finds its largest key and, for want > 0, a bound with at least `want` elements at or above
-// it (or below every element, if there are not so many).  scratch: kBoundBins words.
+// ------------------------------------------------------------------ the bound
+// A key that the maxima of at least R of the CTA's groups reach (kKeyNone + 1 if there are not so many, or R is 0), and
+// the largest key in *top.  hi, lo: the largest of the thread's maxima and the least above -inf; each(f): f(maximum) for
+// all of them.  A histogram of the maxima from the largest down, in equal steps; scratch: its kBoundBins words, zero, a
+// barrier ahead.
 constexpr int kBoundBins = 512;
-template <bool F32>
-__device__ void load_row(Ctx<F32> &c, uint4 *cache, int want, uint32_t *scratch, uint32_t *kmax, uint32_t *bound)
+template <typename Each>
+__device__ __forceinline__ uint32_t group_bound(Shared *sh, uint32_t *scratch, int R, float hi, float lo, uint32_t *top,
+                                                Each each)
 {
-    constexpr int NG = F32 ? 4 : 8;   // groups of a thread
-    Shared *sh = c.sh;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    if (want > 0)
-        for (int i = tid; i < kBoundBins; i += kSelThreads) scratch[i] = 0u;
-    uint32_t gm[4] = {0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u};
-    if constexpr (!F32)
-        for (int k = 0; k < 4; ++k) gm[k] = 0xff80ff80u;
-    const auto join = [&](const uint4 &x) {
-        if constexpr (F32) {
-            gm[0] = __float_as_uint(fmaxf(__uint_as_float(gm[0]), __uint_as_float(x.x)));
-            gm[1] = __float_as_uint(fmaxf(__uint_as_float(gm[1]), __uint_as_float(x.y)));
-            gm[2] = __float_as_uint(fmaxf(__uint_as_float(gm[2]), __uint_as_float(x.z)));
-            gm[3] = __float_as_uint(fmaxf(__uint_as_float(gm[3]), __uint_as_float(x.w)));
-        } else {
-            gm[0] = bf16x2_max(gm[0], x.x);
-            gm[1] = bf16x2_max(gm[1], x.y);
-            gm[2] = bf16x2_max(gm[2], x.z);
-            gm[3] = bf16x2_max(gm[3], x.w);
-        }
-    };
-    const int end = min(c.we, c.cached);
-    for (int v = c.wb + lane; v < end; v += 32) {
-        cp_async_wait<kAhead - 1>();
-        join(cache[v]);
-        const int next = v + 32 * kAhead;
-        if (next < end) fetch_granule<F32>(c.r, c.gb + next, cache + next);
-        cp_async_commit();
-    }
-    for (int v = max(c.wb, c.cached) + lane; v < c.we; v += 32) join(load_granule<F32>(c.r, c.gb + v));
-
-    // the groups' maxima, the largest and the least that is above -inf
-    float g[NG], hi = -INFINITY, lo = INFINITY;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        if constexpr (F32) {
-            g[k] = fmaxf(__uint_as_float(gm[k]), -INFINITY);
-        } else {
-            g[2 * k] = fmaxf(bf16_lo(gm[k]), -INFINITY);
-            g[2 * k + 1] = fmaxf(bf16_hi(gm[k]), -INFINITY);
-        }
-    }
-#pragma unroll
-    for (int k = 0; k < NG; ++k) {
-        hi = fmaxf(hi, g[k]);
-        if (want > 0 && g[k] > -INFINITY) lo = fminf(lo, g[k]);
-    }
-    uint32_t top = __reduce_max_sync(0xffffffffu, key_of(hi));
-    uint32_t least = __reduce_min_sync(0xffffffffu, key_of(lo));
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const uint32_t khi = __reduce_max_sync(0xffffffffu, key_of(hi));
+    uint32_t klo = __reduce_min_sync(0xffffffffu, key_of(lo));
     if (lane == 0) {
-        sh->ktop[warp] = top;
-        sh->klow[warp] = least;
+        sh->ktop[warp] = khi;
+        sh->klow[warp] = klo;
     }
-    if (tid == 0) sh->border = kBoundBins;
+    if (threadIdx.x == 0) sh->border = kBoundBins;
     __syncthreads();
-    top = __reduce_max_sync(0xffffffffu, sh->ktop[lane & (kSelWarps - 1)]);
-
-    uint32_t low = kKeyNone + 1;
-    if (want > 0) {
-        // a value that R of this CTA's group maxima reach: their histogram from the largest down, in equal steps
-        least = __reduce_min_sync(0xffffffffu, sh->klow[lane & (kSelWarps - 1)]);
-        const int R = (want + c.C - 1) >> (31 - __clz(c.C));
-        const float ft = key_float(top), range = ft - key_float(least);
-        const float scale = range > 0.f && range < INFINITY ? (float)kBoundBins / range : 0.f;   // (0: one step)
-        int bin[NG];
+    *top = __reduce_max_sync(0xffffffffu, sh->ktop[lane & (kSelWarps - 1)]);
+    if (R <= 0) return kKeyNone + 1;
+    klo = __reduce_min_sync(0xffffffffu, sh->klow[lane & (kSelWarps - 1)]);
+    const float ft = key_float(*top), range = ft - key_float(klo);
+    const float scale = range > 0.f && range < INFINITY ? (float)kBoundBins / range : 0.f;   // (0: one step)
+    const auto bin = [&](float g) { return scale > 0.f ? (int)fminf((ft - g) * scale, (float)(kBoundBins - 1)) : 0; };
+    each([&](float g) {
+        if (g > -INFINITY) atomicAdd(scratch + bin(g), 1u);
+    });
+    __syncthreads();
+    if (warp == 0) {
+        constexpr int kPer = kBoundBins / 32;
+        uint32_t n[kPer], sum = 0;
 #pragma unroll
-        for (int k = 0; k < NG; ++k) {
-            bin[k] = scale > 0.f ? (int)fminf((ft - g[k]) * scale, (float)(kBoundBins - 1)) : 0;
-            if (g[k] > -INFINITY) atomicAdd(scratch + bin[k], 1u);
+        for (int k = 0; k < kPer; ++k) {
+            n[k] = scratch[lane * kPer + k];
+            sum += n[k];
         }
-        __syncthreads();
-        if (warp == 0) {
-            constexpr int kPer = kBoundBins / 32;
-            uint32_t n[kPer], sum = 0;
+        uint32_t incl = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t u = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += u;
+        }
+        uint32_t run = incl - sum;
+        if (run < (uint32_t)R && incl >= (uint32_t)R) {   // (at most one lane)
+            int b = lane * kPer;
 #pragma unroll
             for (int k = 0; k < kPer; ++k) {
-                n[k] = scratch[lane * kPer + k];
-                sum += n[k];
+                run += n[k];
+                b += run < (uint32_t)R;
             }
-            uint32_t incl = sum;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const uint32_t u = __shfl_up_sync(0xffffffffu, incl, o);
-                if (lane >= o) incl += u;
-            }
-            uint32_t run = incl - sum;
-            if (run < (uint32_t)R && incl >= (uint32_t)R) {   // (at most one lane)
-                int b = lane * kPer;
-#pragma unroll
-                for (int k = 0; k < kPer; ++k) {
-                    run += n[k];
-                    b += run < (uint32_t)R;
-                }
-                sh->border = b;
-            }
+            sh->border = b;
         }
-        __syncthreads();
-        // the least group maximum down to that step; everything, where there are fewer than R
-        const int border = sh->border;
-        float at = INFINITY;
-#pragma unroll
-        for (int k = 0; k < NG; ++k)
-            if (bin[k] <= border && g[k] > -INFINITY) at = fminf(at, g[k]);
-        least = __reduce_min_sync(0xffffffffu, key_of(at));
-        if (lane == 0) sh->klow[warp] = least;
-        __syncthreads();
-        least = __reduce_min_sync(0xffffffffu, sh->klow[lane & (kSelWarps - 1)]);
-        if (border < kBoundBins) low = least;
     }
-    if (c.C > 1) {
-        cluster_wait();
-        if (tid < c.C) {
-            st_peer_u32(peer_addr(&sh->kmax[c.rank], tid), top);
-            st_peer_u32(peer_addr(&sh->bound[c.rank], tid), low);
-        }
-        cluster_sync_all();
-        for (int k = 0; k < c.C; ++k) {
-            top = max(top, sh->kmax[k]);
-            low = min(low, sh->bound[k]);
-        }
-    } else {
-        __syncthreads();
-    }
-    *kmax = top;
-    *bound = low;
+    __syncthreads();
+    // the least maximum down to that step; everything, where there are fewer than R
+    const int border = sh->border;
+    float at = INFINITY;
+    each([&](float g) {
+        if (g > -INFINITY && bin(g) <= border) at = fminf(at, g);
+    });
+    klo = __reduce_min_sync(0xffffffffu, key_of(at));
+    if (lane == 0) sh->klow[warp] = klo;
+    __syncthreads();
+    klo = __reduce_min_sync(0xffffffffu, sh->klow[lane & (kSelWarps - 1)]);
+    return border < kBoundBins ? klo : kKeyNone + 1;
 }
 
 template <bool F32>
@@ -654,31 +572,19 @@ __device__ __forceinline__ void set_ctx(Ctx<F32> &c, const uint4 *cache, int cac
 }
 
 // ------------------------------------------------------------------ launches (host)
-// CTAs of a row: so many that a share leaves room for other CTAs on the SM, that few rows fill the GPU, and that the
-// list of `want` entries falls to each in parts of at most kSmall.
-int logits_cluster(int rows, int64_t row_bytes, int want)
+constexpr int kSms = 152;
+
+// CTAs of a row: one where the rows alone fill the GPU, more where they do not, as long as each has a few granules per
+// thread; so many that a row's list of `want` entries falls to them in parts of at most kSmall, and that a share of at
+// most `share` bytes (0: any) is left to each.
+int logits_cluster(int rows, int64_t row_bytes, int want, size_t share)
 {
     int C = 1;
-    while (C < kRowMaxCluster && (row_bytes > (int64_t)C * (int64_t)kShare ||
-                                  (((int64_t)rows * C < 2 * 152 || want > C * (kSmall * 3 / 4)) &&
+    while (C < kRowMaxCluster && ((share && row_bytes > (int64_t)C * (int64_t)share) ||
+                                  (((int64_t)rows * C < 2 * kSms || want > C * (kSmall * 3 / 4)) &&
                                    row_bytes >= 2 * (int64_t)C * kSelThreads * 16)))
         C *= 2;
     return C;
-}
-
-// Cluster and shared memory of a launch over `rows` rows.
-constexpr size_t kMaxSmem = kMaxCache + (size_t)kListCap * 8;
-static_assert(kMaxSmem + 11 * 1024 <= kSmemPerCta, "with the kernels' static part");
-
-template <bool F32, auto Kern, typename P>
-cudaError_t launch_rows(P p, int rows, int cap, int want, cudaStream_t st)
-{
-    const int64_t bytes = (int64_t)p.V * RowElem<F32>::kBytes;
-    p.cluster = logits_cluster(rows, bytes, want);
-    const size_t share = (size_t)((bytes + 32 + p.cluster - 1) / p.cluster) + 32;
-    p.cached = (int)((share < kMaxCache ? share : kMaxCache) / 16);
-    const size_t smem = (size_t)p.cached * 16 + (size_t)cap * 8;
-    return launch_clusters<Kern>((int64_t)rows * p.cluster, kSelThreads, smem, kMaxSmem, p.cluster, st, p);
 }
 
 sats_status check_rows(const void *logits, int64_t ld, int rows, int V, int bytes)

@@ -1,5 +1,7 @@
 // sample.cu -- drawing a token from each row of logits (sats_sample).
 //
+// The row's share of a CTA is brought to shared memory once; all passes after that run there.
+//
 // Drawing needs sums over up to V tokens that decide next to borders as close as the smallest token's probability.
 // A token's weight is therefore a whole number, w = 2^F exp((z - max) / T) to about 35 bits relative (never less
 // than 2^-F absolute), computed in pairs of floats; sums of whole numbers do not depend on their order, and every
@@ -16,6 +18,12 @@ constexpr int kSelThreads = 256, kSelPerSm = 3;
 
 namespace sats {
 namespace {
+
+constexpr int kAhead = 8;              // granules in flight per thread while the row arrives
+constexpr size_t kShare = 64 * 1024;   // of a row's bytes per CTA, where the cluster allows
+constexpr size_t kMaxCache = 184 * 1024;
+constexpr size_t kMaxSmem = kMaxCache + (size_t)kListCap * 8;
+static_assert(kMaxSmem + 11 * 1024 <= kSmemPerCta, "with the kernel's static part");
 
 // ------------------------------------------------------------------ weights
 // 2^(-j / 1024) in two floats.
@@ -228,6 +236,95 @@ struct KeptMass {
         return sum;
     }
 };
+
+// ------------------------------------------------------------------ the row
+// Sends for a thread's first granules.
+template <bool F32>
+__device__ __forceinline__ void start_row(const Ctx<F32> &c, uint4 *cache)
+{
+    if (c.C > 1) cluster_arrive();   // (load_row waits)
+    const int end = min(c.we, c.cached);
+    for (int i = 0; i < kAhead; ++i) {
+        const int v = c.wb + (int)(threadIdx.x & 31) + 32 * i;
+        if (v < end) fetch_granule<F32>(c.r, c.gb + v, cache + v);
+        cp_async_commit();
+    }
+}
+
+// Brings the row in and finds its largest key and, for want > 0, a bound with at least `want` elements at or above
+// it (or below every element, if there are not so many).  scratch: kBoundBins words.
+template <bool F32>
+__device__ void load_row(Ctx<F32> &c, uint4 *cache, int want, uint32_t *scratch, uint32_t *kmax, uint32_t *bound)
+{
+    constexpr int NG = F32 ? 4 : 8;   // groups of a thread
+    Shared *sh = c.sh;
+    const int tid = threadIdx.x, lane = tid & 31;
+    if (want > 0)
+        for (int i = tid; i < kBoundBins; i += kSelThreads) scratch[i] = 0u;
+    uint32_t gm[4] = {0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u};
+    if constexpr (!F32)
+        for (int k = 0; k < 4; ++k) gm[k] = 0xff80ff80u;
+    const auto join = [&](const uint4 &x) {
+        if constexpr (F32) {
+            gm[0] = __float_as_uint(fmaxf(__uint_as_float(gm[0]), __uint_as_float(x.x)));
+            gm[1] = __float_as_uint(fmaxf(__uint_as_float(gm[1]), __uint_as_float(x.y)));
+            gm[2] = __float_as_uint(fmaxf(__uint_as_float(gm[2]), __uint_as_float(x.z)));
+            gm[3] = __float_as_uint(fmaxf(__uint_as_float(gm[3]), __uint_as_float(x.w)));
+        } else {
+            gm[0] = bf16x2_max(gm[0], x.x);
+            gm[1] = bf16x2_max(gm[1], x.y);
+            gm[2] = bf16x2_max(gm[2], x.z);
+            gm[3] = bf16x2_max(gm[3], x.w);
+        }
+    };
+    const int end = min(c.we, c.cached);
+    for (int v = c.wb + lane; v < end; v += 32) {
+        cp_async_wait<kAhead - 1>();
+        join(cache[v]);
+        const int next = v + 32 * kAhead;
+        if (next < end) fetch_granule<F32>(c.r, c.gb + next, cache + next);
+        cp_async_commit();
+    }
+    for (int v = max(c.wb, c.cached) + lane; v < c.we; v += 32) join(load_granule<F32>(c.r, c.gb + v));
+
+    // the groups' maxima
+    float g[NG], hi = -INFINITY, lo = INFINITY;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        if constexpr (F32) {
+            g[k] = fmaxf(__uint_as_float(gm[k]), -INFINITY);
+        } else {
+            g[2 * k] = fmaxf(bf16_lo(gm[k]), -INFINITY);
+            g[2 * k + 1] = fmaxf(bf16_hi(gm[k]), -INFINITY);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < NG; ++k) {
+        hi = fmaxf(hi, g[k]);
+        if (want > 0 && g[k] > -INFINITY) lo = fminf(lo, g[k]);
+    }
+    uint32_t top;
+    uint32_t low = group_bound(sh, scratch, (want + c.C - 1) >> (31 - __clz(c.C)), hi, lo, &top, [&](auto f) {
+#pragma unroll
+        for (int k = 0; k < NG; ++k) f(g[k]);
+    });
+    if (c.C > 1) {
+        cluster_wait();
+        if (tid < c.C) {
+            st_peer_u32(peer_addr(&sh->kmax[c.rank], tid), top);
+            st_peer_u32(peer_addr(&sh->bound[c.rank], tid), low);
+        }
+        cluster_sync_all();
+        for (int k = 0; k < c.C; ++k) {
+            top = max(top, sh->kmax[k]);
+            low = min(low, sh->bound[k]);
+        }
+    } else {
+        __syncthreads();
+    }
+    *kmax = top;
+    *bound = low;
+}
 
 // ------------------------------------------------------------------ the nucleus
 // Where the mass from the top reaches a share of the whole, in two passes over the row.  The first counts the tokens in
@@ -764,7 +861,13 @@ sats_status sample(const void *logits, int64_t ld, int B, int V, const float *te
     SampleParams p{};
     p.z = logits; p.ld = ld; p.B = B; p.V = V; p.temperature = temperature; p.top_k = top_k; p.top_p = top_p;
     p.min_p = min_p; p.u = u; p.ids = ids; p.logprob = logprob; p.n_kept = n_kept; p.status = dev_status;
-    const cudaError_t e = launch_rows<F32, sample_kernel<F32>>(p, B, kListCap, 0, static_cast<cudaStream_t>(stream));
+    const int64_t bytes = (int64_t)V * RowElem<F32>::kBytes;
+    p.cluster = logits_cluster(B, bytes, 0, kShare);
+    const size_t share = (size_t)((bytes + 32 + p.cluster - 1) / p.cluster) + 32;
+    p.cached = (int)((share < kMaxCache ? share : kMaxCache) / 16);
+    const cudaError_t e = launch_clusters<sample_kernel<F32>>((int64_t)B * p.cluster, kSelThreads,
+                                                              (size_t)p.cached * 16 + kListCap * 8, kMaxSmem, p.cluster,
+                                                              static_cast<cudaStream_t>(stream), p);
     return e == cudaSuccess ? SATS_OK : cuda_fail(e, "sampling kernel launch");
 }
 
