@@ -22,7 +22,7 @@ namespace {
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr int kMaxEntries = 1024;             // teacher entries of a row
 constexpr size_t kMaxCache = 180 * 1024;      // of a row's share in shared memory
-constexpr size_t kMaxSmem = kSmemPerCta - 2 * 1024;   // dynamic: a row's share, a stage, two tables of entries
+constexpr size_t kMaxSmem = kSmemPerCta - 2 * 1024;   // dynamic: a row's share, two tables of entries
 constexpr size_t kStepShare = 72 * 1024;      // of a row per CTA, where the cluster allows: several CTAs to an SM
 constexpr int kLossThreads = 512, kGradThreads = 256, kStepThreads = 256, kStepPerSm = 3;
 
@@ -43,7 +43,6 @@ struct DistillParams {
     int32_t *status;
     int cluster;              // CTAs of a row
     int cached;               // granules of a CTA's share that stay in shared memory
-    int work;                 // granules of shared memory behind them, where the gradient's rows lie otherwise
     int slots;                // of the table of entries' indices (a power of two)
 };
 
@@ -164,47 +163,70 @@ __device__ __forceinline__ void st_row_v4(void *p, const uint4 &v)
                  : "memory");
 }
 
-// Stores the elements of the n granules from g0 on (their values in `stage`) to a row of the output that does not
-// lie on the granules' boundaries: whole 16-byte vectors of the output where these granules cover them, single
-// elements at both ends.  All threads of the CTA; `stage` complete before, free again after the call's end and a sync.
-template <bool F32, int TH>
-__device__ __forceinline__ void store_shifted(char *out, const Row<F32> &r, int g0, int n, const uint4 *stage)
+// Elements [from, to) of a granule whose first element is number `first` of a row, one by one.
+template <bool F32>
+__device__ __noinline__ void put_elements(char *out, int first, int V, uint4 o, int from, int to)
 {
-    constexpr int E = RowElem<F32>::kPer, B = RowElem<F32>::kBytes;
-    const int f0 = r.first(g0);
-    const int64_t lo = f0 > 0 ? f0 : 0;
-    const int64_t end = (int64_t)f0 + (int64_t)n * E, hi = end < r.V ? end : r.V;
-    const int oh = (int)(reinterpret_cast<uintptr_t>(out) & 15u) / B;
-    const int64_t o0 = (lo + oh) / E, o1 = (hi + oh + E - 1) / E;
-    for (int64_t o = o0 + threadIdx.x; o < o1; o += TH) {
-        const int64_t e0 = o * E - oh;
-        uint32_t w[4];
-        const bool full = e0 >= lo && e0 + E <= hi;
-        if constexpr (F32) {
-            const uint32_t *s = reinterpret_cast<const uint32_t *>(stage);
+    constexpr int E = RowElem<F32>::kPer;
 #pragma unroll
-            for (int j = 0; j < E; ++j) {
-                const int64_t e = e0 + j;
-                w[j] = e >= lo && e < hi ? s[e - f0] : 0u;
-                if (!full && e >= lo && e < hi) store_elem<F32>(out, e, w[j]);
-            }
-        } else {
-            const uint16_t *s = reinterpret_cast<const uint16_t *>(stage);
-#pragma unroll
-            for (int j = 0; j < E / 2; ++j) {
-                const int64_t e = e0 + 2 * j;
-                const uint32_t a = e >= lo && e < hi ? s[e - f0] : 0u;
-                const uint32_t b = e + 1 >= lo && e + 1 < hi ? s[e + 1 - f0] : 0u;
-                w[j] = a | (b << 16);
-                if (!full) {
-                    if (e >= lo && e < hi) store_elem<F32>(out, e, a);
-                    if (e + 1 >= lo && e + 1 < hi) store_elem<F32>(out, e + 1, b);
-                }
-            }
-        }
-        if (full) st_row_v4(out + e0 * B, make_uint4(w[0], w[1], w[2], w[3]));
-    }
+    for (int j = 0; j < E; ++j)
+        if (j >= from && j < to && (unsigned)(first + j) < (unsigned)V) store_elem<F32>(out, first + j, granule_elem<F32>(o, j));
 }
+
+// Stores a warp's run of consecutive granules, 32 in each turn, to a row of the output that does not lie on their
+// 16-byte boundaries.  A vector of the output is the end of one granule and the beginning of the next: a lane takes the
+// one before its own from the lane before it, the first lane from the last one's of the turn before.  What has no whole
+// neighbour goes element by element: the ends of the run.
+template <bool F32>
+struct Shifted {
+    char *out;
+    int V, cut;            // elements of a granule that complete the vector begun by the one before it
+    uint32_t last[4];      // the lane's granule of the turn before
+    int was;               // 1: there was one, 2: and it was all row
+
+    __device__ __forceinline__ Shifted(char *o, const Row<F32> &r, int v) : out(o), V(v), last{0, 0, 0, 0}, was(0)
+    {
+        constexpr int E = RowElem<F32>::kPer, B = RowElem<F32>::kBytes;
+        const int at = (int)((reinterpret_cast<uintptr_t>(o) / B - (uintptr_t)r.head) & (E - 1));   // of a granule in its vector
+        cut = E - at;      // (at is not 0: the boundaries differ)
+    }
+    // All lanes; first: the granule's first element; state: 0 where there is none, else as `was`.  After the last turn
+    // once more with nothing.
+    __device__ __forceinline__ void put(int first, int state, const uint4 &o)
+    {
+        constexpr int E = RowElem<F32>::kPer, B = RowElem<F32>::kBytes;
+        const int lane = threadIdx.x & 31, from = (lane + 31) & 31;
+        const bool end = lane == 31;
+        uint32_t w[8] = {0, 0, 0, 0, o.x, o.y, o.z, o.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = __shfl_sync(0xffffffffu, end ? last[k] : w[4 + k], from);
+        const int left = __shfl_sync(0xffffffffu, end ? was : state, from);
+        const int skip = cut * B;
+        if ((state & 2) && (left & 2)) {
+            uint4 v = make_uint4(0, 0, 0, 0);
+            const int bits = (skip & 3) * 8;
+            switch (skip >> 2) {   // (the same in every lane)
+            case 0: v = make_uint4(__funnelshift_r(w[0], w[1], bits), __funnelshift_r(w[1], w[2], bits),
+                                   __funnelshift_r(w[2], w[3], bits), __funnelshift_r(w[3], w[4], bits)); break;
+            case 1: v = make_uint4(__funnelshift_r(w[1], w[2], bits), __funnelshift_r(w[2], w[3], bits),
+                                   __funnelshift_r(w[3], w[4], bits), __funnelshift_r(w[4], w[5], bits)); break;
+            case 2: v = make_uint4(__funnelshift_r(w[2], w[3], bits), __funnelshift_r(w[3], w[4], bits),
+                                   __funnelshift_r(w[4], w[5], bits), __funnelshift_r(w[5], w[6], bits)); break;
+            default: v = make_uint4(__funnelshift_r(w[3], w[4], bits), __funnelshift_r(w[4], w[5], bits),
+                                    __funnelshift_r(w[5], w[6], bits), __funnelshift_r(w[6], w[7], bits)); break;
+            }
+            st_row_v4(out + ((int64_t)(first - E) * B + skip), v);
+        } else {
+            if (left) put_elements<F32>(out, first - E, V, make_uint4(w[0], w[1], w[2], w[3]), cut, E);
+            if (state) put_elements<F32>(out, first, V, o, 0, cut);
+        }
+        last[0] = o.x;
+        last[1] = o.y;
+        last[2] = o.z;
+        last[3] = o.w;
+        was = state;
+    }
+};
 
 // A row's entries in shared memory (of K each).
 struct Entries {
@@ -564,8 +586,7 @@ __global__ void __launch_bounds__(kGradThreads, 4) distill_grad_kernel(const Dis
     char *out = reinterpret_cast<char *>(p.d) + (size_t)((int64_t)row * p.ldd) * B;
     // whether the output's vectors lie on the same boundaries as the input's
     const bool same = ((reinterpret_cast<uintptr_t>(out) - (uintptr_t)r.head * B) & 15u) == 0;
-    uint4 *stage = smem;
-    const Entries ent(smem + p.work, p.K);
+    const Entries ent(smem, p.K);
     const Seen seen{reinterpret_cast<int *>(ent.z + p.K), (unsigned)p.slots - 1u};
     const int label = p.labels ? p.labels[row] : 0;
     const bool bad = p.labels && label >= p.V, ignored = label < 0 || bad;
@@ -610,12 +631,24 @@ __global__ void __launch_bounds__(kGradThreads, 4) distill_grad_kernel(const Dis
             }
         for (; v < run.y; v += TH) put_granule<F32>(out, r, run.x + v, value(v));
     } else {
-        for (int v0 = 0; v0 < run.y; v0 += TH) {
-            if (v0 + tid < run.y) stage[tid] = value(v0 + tid);
-            __syncthreads();
-            store_shifted<F32, TH>(out, r, run.x + v0, min(TH, run.y - v0), stage);
-            __syncthreads();
+        constexpr int U = 4;
+        const int wper = (run.y + WARPS - 1) / WARPS, w0 = min(run.y, (tid >> 5) * wper), w1 = min(run.y, w0 + wper);
+        Shifted<F32> to(out, r, p.V);
+        for (int v0 = w0; v0 < w1; v0 += 32 * U) {
+            uint4 x[U];
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                const int v = v0 + 32 * k + (tid & 31);
+                x[k] = v < w1 && !ignored ? load_granule<F32>(r, run.x + v) : make_uint4(0, 0, 0, 0);
+            }
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                const int v = v0 + 32 * k + (tid & 31);
+                const uint4 o = ignored ? make_uint4(0, 0, 0, 0) : grad.template granule<F32>(x[k]);
+                to.put(r.first(run.x + v), v < w1 ? 1 + 2 * r.whole(run.x + v) : 0, o);
+            }
         }
+        to.put(r.first(run.x + w0 + ((w1 - w0 + 32 * U - 1) / (32 * U)) * 32 * U + (tid & 31)), 0, make_uint4(0, 0, 0, 0));
     }
     if (ignored) return;
     bool twice = false;
@@ -635,7 +668,9 @@ __global__ void __launch_bounds__(kGradThreads, 4) distill_grad_kernel(const Dis
 // nobody else touches it, so the next row arrives while this one is stored, without a barrier.  The CTAs of a row
 // exchange their sums by stores that count on an mbarrier of the receiver (a cluster barrier would wait for the
 // gradient's stores as well); a wait that gives up leaves NaN and says so in the status word.
-template <bool F32, int NT>
+// SHIFT: some rows of the gradient lie on other 16-byte boundaries than the logits' rows; a warp then has a run of
+// consecutive granules (as Shifted wants them) and not every eighth run of 32, which is 6 % faster.
+template <bool F32, int NT, bool SHIFT>
 __global__ void __launch_bounds__(kStepThreads, kStepPerSm) distill_step_kernel(const DistillParams p)
 {
     constexpr int TH = kStepThreads, WARPS = TH / 32, E = RowElem<F32>::kPer, B = RowElem<F32>::kBytes;
@@ -649,8 +684,7 @@ __global__ void __launch_bounds__(kStepThreads, kStepPerSm) distill_step_kernel(
     __shared__ int never;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int C = p.cluster, rank = blockIdx.x % C, stride = gridDim.x / C;
-    uint4 *stage = row_smem + p.cached;
-    char *tables = reinterpret_cast<char *>(stage + p.work);   // entries and their indices' table, two of each in turn
+    char *tables = reinterpret_cast<char *>(row_smem + p.cached);   // entries and their indices' table, two of each in turn
     const size_t table_bytes = (size_t)p.K * 12 + (size_t)p.slots * 4;
     const auto seen_in = [&](int t) {
         return Seen{reinterpret_cast<int *>(tables + t * table_bytes + (size_t)p.K * 12), (unsigned)p.slots - 1u};
@@ -660,7 +694,12 @@ __global__ void __launch_bounds__(kStepThreads, kStepPerSm) distill_step_kernel(
     set_factors(c, p, ctau);
     const bool soft = p.alpha > 0.f && p.K > 0, hard = p.alpha < 1.f && p.labels;
     const float wh = hard ? 1.f - p.alpha : 0.f;
-    const int turns = (p.cached + TH - 1) / TH;   // cached granules per thread, at most
+    // a thread's places in shared memory, the same for every row: at0 and every kHop-th after it, before `end`
+    constexpr int kHop = SHIFT ? 32 : TH;
+    const int wper = (p.cached + WARPS - 1) / WARPS;
+    const int at0 = SHIFT ? warp * wper + lane : tid, end = SHIFT ? min(p.cached, (warp + 1) * wper) : p.cached;
+    const int turns = SHIFT ? (wper + 31) / 32 : (p.cached + TH - 1) / TH;
+    const auto place = [&](int i) { return SHIFT && at0 + kHop * i >= end ? INT_MAX : at0 + kHop * i; };
 
     const auto label_of = [&](int row) { return p.labels && row < p.T ? p.labels[row] : 0; };
     const auto alive = [&](int row, int label) { return row < p.T && label >= 0 && label < p.V; };
@@ -680,7 +719,7 @@ __global__ void __launch_bounds__(kStepThreads, kStepPerSm) distill_step_kernel(
         const int2 run = run_of(r, C, rank);
         const int n = alive(row, label) ? min(run.y, p.cached) : 0;
         for (int i = 0; i < turns; ++i) {
-            const int v = tid + i * TH;
+            const int v = place(i);
             if (v < n) fetch_granule<F32>(r, run.x + v, row_smem + v);
             cp_async_commit();
         }
@@ -722,20 +761,21 @@ __global__ void __launch_bounds__(kStepThreads, kStepPerSm) distill_step_kernel(
             up = p.g ? p.g[row] : 1.f;
 
             RunSum<NT> sum = empty_sum<NT>();
-            int v = tid;
-            const auto batches = [&](int end) {
-                for (; v + (kBatch - 1) * TH < end; v += kBatch * TH) {
+            int v = at0;
+            const int stop = min(nc, end);
+            const auto batches = [&](int until) {
+                for (; v + (kBatch - 1) * kHop < until; v += kBatch * kHop) {
                     uint4 x[kBatch];
 #pragma unroll
-                    for (int k = 0; k < kBatch; ++k) x[k] = row_smem[v + k * TH];
+                    for (int k = 0; k < kBatch; ++k) x[k] = row_smem[v + k * kHop];
                     run_add<F32, NT, kBatch>(sum, x, c);
                 }
             };
             cp_async_wait<kLate>();
-            batches(min(nc, (turns - kLate) * TH));
+            batches(min(stop, (SHIFT ? warp * wper : 0) + (turns - kLate) * kHop));
             cp_async_wait<0>();
-            batches(nc);
-            for (; v < nc; v += TH) {
+            batches(stop);
+            for (; v < stop; v += kHop) {
                 const uint4 one[1] = {row_smem[v]};
                 run_add<F32, NT, 1>(sum, one, c);
             }
@@ -799,48 +839,55 @@ __global__ void __launch_bounds__(kStepThreads, kStepPerSm) distill_step_kernel(
             return grad.template granule<F32>(v < nc ? row_smem[v] : load_granule<F32>(r, run.x + v));
         };
         const auto send = [&](int i) {
-            const int v = tid + i * TH;
+            const int v = place(i);
             if (v < nn) fetch_granule<F32>(nr, nrun.x + v, row_smem + v);
             cp_async_commit();
         };
-        if (same) {
+        if (!SHIFT || same) {
             const int2 whole = whole_of(r, run), nwhole = whole_of(nr, nrun);
-            // turns in which every thread has a whole granule to store and one to send for
-            const int plain0 = whole.x | nwhole.x;
-            const int plain1 = live && next ? min(min(whole.y, nc), min(nwhole.y, nn)) / TH : 0;
+            // turns in which the whole warp (all threads) has whole granules to store and to send for
+            const int first = SHIFT ? warp * wper : 0, last = min(min(min(whole.y, nc), min(nwhole.y, nn)), end);
+            const int plain1 = live && next && last > first ? (last - first) / kHop : 0;
             const auto turn_of = [&](int i) {
-                const int v = tid + i * TH;
+                const int v = place(i);
                 if (v < nc) put_granule<F32>(out, r, run.x + v, value(v));
                 send(i);
             };
             int i = 0;
-            if (plain0 && turns > 0) turn_of(i++);
-            char *dst = out + ((int64_t)r.first(run.x) * B + (int64_t)tid * 16);   // (aligned)
-            const char *src = nr.base + ((size_t)nrun.x + tid) * 16;
-            uint4 *at = row_smem + tid;
+            if (first < max(whole.x, nwhole.x)) turn_of(i++);
+            char *dst = out + ((int64_t)r.first(run.x) * B + (int64_t)at0 * 16);   // (aligned)
+            const char *src = nr.base + ((size_t)nrun.x + at0) * 16;
+            uint4 *at = row_smem + at0;
             for (; i + kBatch <= plain1; i += kBatch) {
                 uint4 x[kBatch];
 #pragma unroll
-                for (int k = 0; k < kBatch; ++k) x[k] = at[(i + k) * TH];
+                for (int k = 0; k < kBatch; ++k) x[k] = at[(i + k) * kHop];
 #pragma unroll
                 for (int k = 0; k < kBatch; ++k) {
-                    const size_t o = (size_t)(i + k) * (TH * 16);
+                    const size_t o = (size_t)(i + k) * (kHop * 16);
                     st_row_v4(dst + o, grad.template granule<F32>(x[k]));
-                    cp_async16(at + (i + k) * TH, src + o);
+                    cp_async16(at + (i + k) * kHop, src + o);
                     cp_async_commit();
                 }
             }
             for (; i < turns; ++i) turn_of(i);
             for (int v = nc + tid; v < n; v += TH) put_granule<F32>(out, r, run.x + v, value(v));
         } else {
-            for (int v0 = 0; v0 < n; v0 += TH) {
-                if (v0 + tid < n) stage[tid] = value(v0 + tid);
-                if (v0 / TH < turns) send(v0 / TH);
-                __syncthreads();
-                store_shifted<F32, TH>(out, r, run.x + v0, min(TH, n - v0), stage);
-                __syncthreads();
+            Shifted<F32> to(out, r, p.V);
+            for (int i = 0; i < turns; ++i) {
+                const int v = place(i);
+                const bool on = v < nc;
+                const uint4 o = on ? value(v) : make_uint4(0, 0, 0, 0);
+                send(i);
+                to.put(r.first(run.x + at0 + 32 * i), on ? 1 + 2 * r.whole(run.x + v) : 0, o);
             }
-            for (int i = (n + TH - 1) / TH; i < turns; ++i) send(i);
+            to.put(r.first(run.x + at0 + 32 * turns), 0, make_uint4(0, 0, 0, 0));
+            for (int v0 = nc + 32 * warp; v0 < n; v0 += TH) {   // (what did not fit: each turn a run of its own)
+                const int v = v0 + lane;
+                to.put(r.first(run.x + v), v < n ? 1 + 2 * r.whole(run.x + v) : 0,
+                       v < n ? value(v) : make_uint4(0, 0, 0, 0));
+                to.put(r.first(run.x + v + 32), 0, make_uint4(0, 0, 0, 0));
+            }
         }
         if (live) {
             if (rank == 0 && any) {
@@ -895,18 +942,13 @@ cudaError_t launch_loss(DistillParams p, cudaStream_t st)
                : launch_clusters<distill_loss_kernel<F32, 1>>(ctas, kLossThreads, smem, kMaxSmem, p.cluster, st, p);
 }
 
-// Shared memory of the gradient's kernels behind the cached row: a stage where the gradient's rows do not lie on the
-// logits' 16-byte boundaries, and the entries and the table of their indices, once or twice.
-template <bool F32>
-size_t plan_grad(DistillParams &p, int threads, int tables)
+// Shared memory of the gradient's kernels: the cached granules, and the entries and the table of their indices, once or
+// twice.
+size_t plan_grad(DistillParams &p, int tables)
 {
-    constexpr int B = RowElem<F32>::kBytes;
-    const bool same = (reinterpret_cast<uintptr_t>(p.z) - reinterpret_cast<uintptr_t>(p.d)) % 16 == 0 &&
-                      (p.T == 1 || (p.ldz - p.ldd) * B % 16 == 0);
-    p.work = same ? 0 : threads;
     p.slots = 32;
     while (p.slots < 2 * p.K) p.slots *= 2;
-    return ((size_t)p.cached + p.work) * 16 + tables * ((size_t)p.K * 12 + (size_t)p.slots * 4);
+    return (size_t)p.cached * 16 + tables * ((size_t)p.K * 12 + (size_t)p.slots * 4);
 }
 
 template <bool F32>
@@ -914,33 +956,38 @@ cudaError_t launch_grad(DistillParams p, cudaStream_t st)
 {
     p.cluster = row_cluster(p.T, (int64_t)p.V * RowElem<F32>::kBytes, 0);
     p.cached = 0;
-    const size_t smem = plan_grad<F32>(p, kGradThreads, 1);
+    const size_t smem = plan_grad(p, 1);
     // (the CTAs of a row need no cluster)
     const int64_t ctas = (int64_t)p.T * p.cluster;
     return two_sums(p) ? launch_clusters<distill_grad_kernel<F32, 2>>(ctas, kGradThreads, smem, kMaxSmem, 1, st, p)
                        : launch_clusters<distill_grad_kernel<F32, 1>>(ctas, kGradThreads, smem, kMaxSmem, 1, st, p);
 }
 
-template <bool F32, int NT>
+template <bool F32, int NT, bool SHIFT>
 cudaError_t launch_step(DistillParams p, cudaStream_t st)
 {
     const int64_t bytes = (int64_t)p.V * RowElem<F32>::kBytes;
     p.cluster = row_cluster(p.T, bytes, kStepShare);
     const size_t share = al16((size_t)((bytes + 32 + p.cluster - 1) / p.cluster) + 32);
     p.cached = (int)((share < kMaxCache ? share : kMaxCache) / 16);
-    const size_t smem = plan_grad<F32>(p, kStepThreads, 2);
+    const size_t smem = plan_grad(p, 2);
     // as many clusters as the GPU holds at a time, each for every so many rows
     int fit = 0;
-    const cudaError_t e = resident_clusters<distill_step_kernel<F32, NT>>(kStepThreads, smem, kMaxSmem, p.cluster, &fit);
+    const cudaError_t e = resident_clusters<distill_step_kernel<F32, NT, SHIFT>>(kStepThreads, smem, kMaxSmem, p.cluster, &fit);
     if (e != cudaSuccess) return e;
     const int64_t clusters = p.T < fit ? p.T : fit < 1 ? 1 : fit;
-    return launch_clusters<distill_step_kernel<F32, NT>>(clusters * p.cluster, kStepThreads, smem, kMaxSmem, p.cluster, st, p);
+    return launch_clusters<distill_step_kernel<F32, NT, SHIFT>>(clusters * p.cluster, kStepThreads, smem, kMaxSmem,
+                                                                p.cluster, st, p);
 }
 
 template <bool F32>
 cudaError_t launch_step(const DistillParams &p, cudaStream_t st)
 {
-    return two_sums(p) ? launch_step<F32, 2>(p, st) : launch_step<F32, 1>(p, st);
+    constexpr int B = RowElem<F32>::kBytes;
+    const bool same = (reinterpret_cast<uintptr_t>(p.z) - reinterpret_cast<uintptr_t>(p.d)) % 16 == 0 &&
+                      (p.T == 1 || (p.ldz - p.ldd) * B % 16 == 0);
+    if (two_sums(p)) return same ? launch_step<F32, 2, false>(p, st) : launch_step<F32, 2, true>(p, st);
+    return same ? launch_step<F32, 1, false>(p, st) : launch_step<F32, 1, true>(p, st);
 }
 
 // What the three calls have in common; their own outputs are checked by each.
