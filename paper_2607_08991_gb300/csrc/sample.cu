@@ -194,20 +194,22 @@ struct KeptMass {
         add(c, v, a1, a2, n);
         return whole_weight(a1, a2, s);   // (eight weights at most)
     }
-    template <bool F32>
+    // (CUT: something is cut; without, every token above -inf is kept)
+    template <bool CUT = true, bool F32>
     __device__ __forceinline__ void add(const Ctx<F32> &c, int v, int &a1, int &a2, int &n) const
     {
         constexpr int P = RowElem<F32>::kPer / 2;
         const uint4 x = c.raw(v);
-        if (!(granule_max<F32>(x) >= at)) return;
+        if (CUT && !(granule_max<F32>(x) >= at)) return;
         f32x2 z[P];
         granule_pairs<F32>(c.clean(x), z);
         const int i0 = c.r.first(c.gb + v);
+        const auto kept = [&](float f, int i) { return CUT ? keeps(f, i) : f > -INFINITY; };
         if (s.hard) {
 #pragma unroll
             for (int j = 0; j < P; ++j) {
                 const float2 y = unpack2(z[j]);
-                const bool k0 = keeps(y.x, i0 + 2 * j), k1 = keeps(y.y, i0 + 2 * j + 1);
+                const bool k0 = kept(y.x, i0 + 2 * j), k1 = kept(y.y, i0 + 2 * j + 1);
                 n += k0 + k1;
                 a1 += ((k0 && y.x == s.top) + (k1 && y.y == s.top)) << 21;
             }
@@ -216,7 +218,7 @@ struct KeptMass {
             for (int j = 0; j < P; ++j) {
                 const float2 y = unpack2(z[j]);
                 const Weights2 w = weights2(z[j], s, tab);
-                const bool k0 = keeps(y.x, i0 + 2 * j), k1 = keeps(y.y, i0 + 2 * j + 1);
+                const bool k0 = kept(y.x, i0 + 2 * j), k1 = kept(y.y, i0 + 2 * j + 1);
                 n += k0 + k1;
                 if (k0 && w.in[0]) { a1 += w.i1[0]; a2 += w.i2[0]; }
                 if (k1 && w.in[1]) { a1 += w.i1[1]; a2 += w.i2[1]; }
@@ -224,13 +226,13 @@ struct KeptMass {
         }
     }
     // Sum over this thread's granules.
-    template <bool F32>
+    template <bool CUT, bool F32>
     __device__ __forceinline__ unsigned long long over_row(const Ctx<F32> &c, int &n) const
     {
         unsigned long long sum = 0;
         for (int v0 = c.wb + (int)(threadIdx.x & 31); v0 < c.we; v0 += 32 * kFlush) {
             int a1 = 0, a2 = 0;
-            for (int v = v0; v < min(c.we, v0 + 32 * kFlush); v += 32) add(c, v, a1, a2, n);
+            for (int v = v0; v < min(c.we, v0 + 32 * kFlush); v += 32) add<CUT>(c, v, a1, a2, n);
             sum += whole_weight(a1, a2, s);
         }
         return sum;
@@ -357,10 +359,47 @@ __device__ Cut cut_ties(Ctx<F32> &c, uint32_t key, unsigned long long w, unsigne
     return cut;
 }
 
+// The parts of a list that lie `seg` entries apart (sh->cnt of each), one behind another.
+__device__ __noinline__ void one_behind_another(unsigned long long *list, int seg, int n, int C, Shared *sh)
+{
+    for (int i0 = 0; i0 < n; i0 += kSelThreads) {   // (from the first on: nothing is overwritten before it is read)
+        const int i = i0 + (int)threadIdx.x;
+        unsigned long long e = 0;
+        if (i < n) {
+            int k = 0, from = 0;
+            while (i - from >= (int)sh->cnt[k]) from += (int)sh->cnt[k++];
+            e = list[k * seg + i - from];
+        }
+        __syncthreads();
+        if (i < n) list[i] = e;
+        __syncthreads();
+    }
+}
+
+// The last entry, from the largest down, that the mass `want` still reaches: to sh->found_key and found_idx.  For lists
+// that are sorted for it.
+__device__ __noinline__ void cut_in_list(unsigned long long *list, int n, unsigned long long want, Scale s,
+                                         const float2 *tab, Shared *sh)
+{
+    sort_list(list, n);
+    const int first = (int)threadIdx.x * kListPer;
+    unsigned long long sum = 0, rest;
+    for (int i = first; i < min(n, first + kListPer); ++i) sum += weight(key_float((uint32_t)(list[i] >> 32)), s, tab);
+    unsigned long long before = block_scan_u64(sum, sh, &rest);
+    for (int i = first; i < min(n, first + kListPer); ++i) {
+        const unsigned long long x = list[i], w = weight(key_float((uint32_t)(x >> 32)), s, tab);
+        if (before < want && want - before <= w) {   // (one thread)
+            sh->found_key = (uint32_t)(x >> 32);
+            sh->found_idx = (int)~(uint32_t)x;
+        }
+        before += w;
+    }
+}
+
 // The cut that keeps, of what by_k keeps, the largest up to a share top_p < 1 of the mass, by counts and exact weights;
 // false (the same in every CTA of the row) where the border does not lie where the counts have it, or among more
 // tokens than the list holds.
-template <bool F32>
+template <bool FILTERED, bool F32>
 __device__ bool cut_by_counts(Ctx<F32> &c, const Scale &s, const float2 *tab, unsigned long long *list, Cut by_k,
                               float top_p, Nucleus *res)
 {
@@ -368,7 +407,6 @@ __device__ bool cut_by_counts(Ctx<F32> &c, const Scale &s, const float2 *tab, un
     Shared *sh = c.sh;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, C = c.C;
     const KeptMass all(s, tab, by_k);
-    const bool filtered = by_k.key > kKeyNone;
     // steps as fine as 128 logits, or what weighs more than 2^-64, allow
     int shift = 0;
     while (shift < 5 && (float)(2 << shift) < 128.f * s.chi) ++shift;
@@ -392,8 +430,8 @@ __device__ bool cut_by_counts(Ctx<F32> &c, const Scale &s, const float2 *tab, un
             for (int j = 0; j < P; ++j) {
                 const f32x2 y2 = fmul2(fadd2(z[j], nt), chi);   // (as weights2 does)
                 const float2 f = unpack2(z[j]), y = unpack2(y2), m = unpack2(fadd2(y2, magic));
-                if (!filtered || all.keeps(f.x, i0 + 2 * j)) add(y.x, m.x);
-                if (!filtered || all.keeps(f.y, i0 + 2 * j + 1)) add(y.y, m.y);
+                if (!FILTERED || all.keeps(f.x, i0 + 2 * j)) add(y.x, m.x);
+                if (!FILTERED || all.keeps(f.y, i0 + 2 * j + 1)) add(y.y, m.y);
             }
         }
     }
@@ -472,10 +510,10 @@ __device__ bool cut_by_counts(Ctx<F32> &c, const Scale &s, const float2 *tab, un
                 for (int h = 0; h < 2; ++h) {
                     const float f = h ? y.y : y.x;
                     const int i = i0 + 2 * j + h, d = w.g[h];
-                    const bool in = w.in[h] && (!filtered || all.keeps(f, i));
+                    const bool in = w.in[h] && (!FILTERED || all.keeps(f, i));
                     if (in) { t1 += w.i1[h]; t2 += w.i2[h]; }
                     if (in && d < d0) { a1 += w.i1[h]; a2 += w.i2[h]; ++n_above; }
-                    if (in && d >= d0 && d < d1) {
+                    if (in && (unsigned)(d - d0) < (unsigned)(d1 - d0)) {
                         const uint32_t at = atomicAdd(&sh->nlist, 1u);
                         if (at < (uint32_t)seg) own[at] = ((unsigned long long)key_of(f) << 32) | (uint32_t)~(uint32_t)i;
                     }
@@ -523,23 +561,8 @@ __device__ bool cut_by_counts(Ctx<F32> &c, const Scale &s, const float2 *tab, un
     const unsigned long long want = target - A;
     // every CTA does what follows: the entries one behind another, and the last one that is kept
     if (tid == 0) sh->found_idx = -1;
-    {
-        unsigned long long e[kListPer];
-#pragma unroll
-        for (int j = 0; j < kListPer; ++j) {
-            int i = tid + j * kSelThreads, k = 0, from = 0;
-            e[j] = 0;
-            if (i < n) {
-                while (i - from >= (int)sh->cnt[k]) from += (int)sh->cnt[k++];
-                e[j] = list[k * seg + i - from];
-            }
-        }
-        __syncthreads();
-#pragma unroll
-        for (int j = 0; j < kListPer; ++j)
-            if (tid + j * kSelThreads < n) list[tid + j * kSelThreads] = e[j];
-        __syncthreads();
-    }
+    if (C > 1) one_behind_another(list, seg, n, C, sh);
+    else __syncthreads();
     if (n <= kSmall) {
         const Small m(list, n);
         const unsigned long long w = m.on ? weight(key_float(m.key()), s, tab) : 0ull;
@@ -553,24 +576,7 @@ __device__ bool cut_by_counts(Ctx<F32> &c, const Scale &s, const float2 *tab, un
             sh->found_idx = m.idx();
         }
     } else {
-        sort_list(list, n);
-        unsigned long long w[kListPer], sum = 0, rest;
-#pragma unroll
-        for (int j = 0; j < kListPer; ++j) {
-            const int i = tid * kListPer + j;
-            w[j] = i < n ? weight(key_float((uint32_t)(list[i] >> 32)), s, tab) : 0ull;
-            sum += w[j];
-        }
-        unsigned long long before = block_scan_u64(sum, sh, &rest);
-#pragma unroll
-        for (int j = 0; j < kListPer; ++j) {
-            if (before < want && want - before <= w[j]) {   // (one thread)
-                const unsigned long long x = list[tid * kListPer + j];
-                sh->found_key = (uint32_t)(x >> 32);
-                sh->found_idx = (int)~(uint32_t)x;
-            }
-            before += w[j];
-        }
+        cut_in_list(list, n, want, s, tab, sh);
     }
     __syncthreads();
     const Cut cut{sh->found_key, sh->found_idx};
@@ -614,7 +620,9 @@ __device__ Nucleus cut_mass(Ctx<F32> &c, const Scale &s, const float2 *tab, unsi
                             Cut by_k, float top_p)
 {
     Nucleus res;
-    if (!s.hard && cut_by_counts(c, s, tab, list, by_k, top_p, &res)) return res;
+    if (!s.hard && (by_k.key > kKeyNone ? cut_by_counts<true>(c, s, tab, list, by_k, top_p, &res)
+                                        : cut_by_counts<false>(c, s, tab, list, by_k, top_p, &res)))
+        return res;
     const KeptMass all(s, tab, by_k);
     const auto f = [&](float x, uint32_t q, int i) { return by_k.keeps(q, i) ? weight(x, s, tab) : 0ull; };
     const unsigned long long Z = cluster_sum(c, thread_sum(c, all)), want = share_ceil(top_p, Z);
@@ -676,6 +684,53 @@ __device__ __forceinline__ float log_share(float z, float T, const Scale &s, uns
 {
     const float rest = (float)(long long)(total - (1ull << s.F)) * exp2f(-(float)s.F);
     return (z == s.top ? 0.f : (z - s.top) / T) - log1pf(rest);
+}
+
+// The draw from a list of the row's largest n >= k entries that is sorted for it.
+__device__ __noinline__ void draw_from_list(const SampleParams &p, int row, unsigned long long *list, int n, int k,
+                                            float top_p, uint32_t kminp, float u, float T, Scale s, const float2 *tab,
+                                            Shared *sh)
+{
+    sort_list(list, n);
+    const int first = (int)threadIdx.x * kListPer;
+    const auto weight_at = [&](int i, int shift) { return weight(key_float((uint32_t)(list[i] >> shift)), s, tab); };
+    int m = min(n, k);
+    unsigned long long sum = 0, total;
+    if (top_p < 1.f || kminp > 0) {
+        int in_p = 0, in_minp = 0;
+        for (int i = first; i < min(m, first + kListPer); ++i) {
+            sum += weight_at(i, 32);
+            in_minp += (uint32_t)(list[i] >> 32) >= kminp;
+        }
+        unsigned long long run = block_scan_u64(sum, sh, &total);
+        const unsigned long long target = top_p < 1.f ? share_ceil(top_p, total) : ~0ull;
+        for (int i = first; i < min(m, first + kListPer); ++i) {
+            in_p += run < target;
+            run += weight_at(i, 32);
+        }
+        const unsigned long long both = block_sum_u64(((unsigned long long)(unsigned)in_p << 32) | (unsigned)in_minp, sh);
+        m = min((int)(both >> 32), (int)(uint32_t)both);
+    }
+    // the kept ones in the vocabulary's order
+    const int m2 = pow2_at_least(m);
+    __syncthreads();
+    for (int i = threadIdx.x; i < m2; i += kSelThreads) {
+        const unsigned long long e = list[i];
+        list[i] = i < m ? (e << 32) | (e >> 32) : 0ull;
+    }
+    sort_desc(list, m2);
+    sum = 0;
+    for (int i = first; i < min(m, first + kListPer); ++i) sum += weight_at(i, 0);
+    unsigned long long run = block_scan_u64(sum, sh, &total);
+    const unsigned long long target = share_floor(u, total);
+    for (int i = first; i < min(m, first + kListPer); ++i) {
+        const unsigned long long next = run + weight_at(i, 0);
+        if (target >= run && target < next) {   // one entry
+            const unsigned long long e = list[i];
+            put_sample(p, row, (int)~(uint32_t)(e >> 32), log_share(key_float((uint32_t)e), T, s, total), m);
+        }
+        run = next;
+    }
 }
 
 template <bool F32>
@@ -760,57 +815,7 @@ __global__ void __launch_bounds__(kSelThreads, kSelPerSm) sample_kernel(const Sa
                     put_sample(p, row, e.idx(), log_share(key_float(e.key()), T, s, total), m);
                 return;
             }
-            sort_list(list, n);
-            int m = min(n, k);
-            unsigned long long w[kListPer], sum = 0, total;
-            if (nucleus || kminp > 0) {
-                int in_minp = 0;
-#pragma unroll
-                for (int j = 0; j < kListPer; ++j) {
-                    const int i = tid * kListPer + j;
-                    const uint32_t key = i < m ? (uint32_t)(list[i] >> 32) : 0u;
-                    w[j] = i < m ? weight(key_float(key), s, tab) : 0ull;
-                    sum += w[j];
-                    in_minp += i < m && key >= kminp;
-                }
-                unsigned long long run = block_scan_u64(sum, &sh, &total);
-                const unsigned long long target = nucleus ? share_ceil(top_p, total) : ~0ull;
-                int in_p = 0;
-#pragma unroll
-                for (int j = 0; j < kListPer; ++j) {
-                    in_p += tid * kListPer + j < m && run < target;
-                    run += w[j];
-                }
-                const unsigned long long both =
-                    block_sum_u64(((unsigned long long)(unsigned)in_p << 32) | (unsigned)in_minp, &sh);
-                m = min((int)(both >> 32), (int)(uint32_t)both);
-            }
-            // the kept ones in the vocabulary's order
-            const int m2 = pow2_at_least(m);
-            __syncthreads();
-            for (int i = tid; i < m2; i += kSelThreads) {
-                const unsigned long long e = list[i];
-                list[i] = i < m ? (e << 32) | (e >> 32) : 0ull;
-            }
-            sort_desc(list, m2);
-            sum = 0;
-#pragma unroll
-            for (int j = 0; j < kListPer; ++j) {
-                const int i = tid * kListPer + j;
-                w[j] = i < m ? weight(key_float((uint32_t)list[i]), s, tab) : 0ull;
-                sum += w[j];
-            }
-            unsigned long long run = block_scan_u64(sum, &sh, &total);
-            const unsigned long long target = share_floor(u, total);
-#pragma unroll
-            for (int j = 0; j < kListPer; ++j) {
-                const unsigned long long next = run + w[j];
-                if (target >= run && target < next) {   // one entry
-                    const unsigned long long e = list[tid * kListPer + j];
-                    put_sample(p, row, (int)~(uint32_t)(e >> 32), log_share(key_float((uint32_t)e), T, s, total), m);
-                }
-                run = next;
-            }
+            draw_from_list(p, row, list, n, k, nucleus ? top_p : 1.f, kminp, u, T, s, tab, &sh);
             return;
         }
     }
@@ -835,7 +840,7 @@ __global__ void __launch_bounds__(kSelThreads, kSelPerSm) sample_kernel(const Sa
         for (int q = 0; q < c.C; ++q) count += sh.above[q];
     } else {
         int n = 0;
-        unsigned long long mine = kept.over_row(c, n);
+        unsigned long long mine = cut.key > kKeyNone ? kept.over_row<true>(c, n) : kept.over_row<false>(c, n);
         n = (int)__reduce_add_sync(0xffffffffu, n);
         __syncthreads();
         if ((tid & 31) == 0) sh.part[tid >> 5] = n;
