@@ -436,10 +436,12 @@ SATS_API sats_status sats_route_calibrate(const float *score, int V, const int32
  * In all of them logits is a device array of rows of V elements (bf16, or fp32
  * in the _f32 calls), row r starting at element r * ld (ld >= V; what lies
  * between the rows is not read).  A pointer needs the alignment of its elements
- * only; rows that start on 16-byte boundaries are no faster.  The calls need
- * no workspace, their waits are the hardware's own, and what they write does
- * not depend on the order in which their threads run.  V up to 2^31 - 65 and
- * 2^28 - 1 rows (else SATS_ESHAPE); no rows: nothing is done.
+ * only.  The calls need no workspace, and what they write does not depend on the
+ * order in which their threads run.  In sats_distill_loss_grad the CTAs of a row
+ * wait, bounded, for one another's sums: if one gives up, the row's loss and
+ * gradient are NaN and dev_status tells (SATS_ETIMEOUT from
+ * sats_get_status_word).  V up to 2^31 - 65 and 2^28 - 1 rows (else
+ * SATS_ESHAPE); no rows: nothing is done.
  *
  * sats_top_logits -- the K largest logits of each row, as a teacher hands them
  *   over: values (device fp32 [T][K]) in descending order, ties by the lower
@@ -459,6 +461,7 @@ SATS_API sats_status sats_route_calibrate(const float *score, int V, const int32
  *   top_idx, top_val : device int32 and fp32 [T][K] (K 0 to 1024; NULL if 0).  An
  *                index below 0 is an absent entry, and so is one with the value
  *                -inf; a row without any has KD = 0.  An index may occur twice.
+ *                A NaN or +inf value makes the row's loss NaN.
  *   labels     : device int32 [T], or NULL for no CE term (CE = 0).  A label
  *                below 0 makes its row an ignored one: nothing of it is read,
  *                its loss, lse and gradient are 0.
@@ -471,6 +474,8 @@ SATS_API sats_status sats_route_calibrate(const float *score, int V, const int32
  *                (SATS_EDEVICE from sats_get_status_word); the entry is then
  *                absent, the row an ignored one.
  *   A row with a NaN or +inf logit, or with none above -inf, has the loss NaN.
+ *   Logits are divided by tau in fp32: where tau < 1, what of them passes fp32's
+ *   range counts as an infinity in lse.
  *
  * sats_distill_grad -- its backward pass:
  *     dlogits_j = g (alpha tau (softmax(z / tau)_j - sum_{k: top_idx_k = j} q_k)

@@ -442,46 +442,45 @@ def route_calibrate(score: torch.Tensor, heldout_ids: torch.Tensor, r_tar: float
 # must be the current one.
 
 def _rows(t: torch.Tensor, name: str):
-    if not t.is_cuda:
+    dev = t.get_device()
+    if dev < 0:
         raise ValueError("%s must be a CUDA tensor" % name)
     if t.dtype not in (torch.float32, torch.bfloat16, torch.int16):
         raise ValueError("%s must be fp32 or bf16 (or int16 bit patterns of bf16)" % name)
     if t.dim() != 2 or t.shape[1] < 1 or (t.shape[1] > 1 and t.stride(1) != 1):
         raise ValueError("%s must be [rows][V] with consecutive elements in a row" % name)
-    if t.device.index != torch._C._cuda_getDevice():
+    if dev != torch._C._cuda_getDevice():
         raise ValueError("%s must be on the current CUDA device" % name)
     R, V = t.shape
     ld = t.stride(0) if R > 1 else V
     if ld < V:
         raise ValueError("%s must not have overlapping rows" % name)
-    return t.data_ptr(), int(ld), int(R), int(V), t.dtype == torch.float32
+    return t.data_ptr(), ld, R, V, t.dtype is torch.float32, dev
 
 
-def _beside(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, shape, device) -> Optional[int]:
+def _beside(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, shape: tuple, dev: int) -> Optional[int]:
     if t is None:
         return None
-    if t.device != device:
-        raise ValueError("%s must be on the logits' device" % name)
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
-        raise ValueError("%s must be %s of shape %s" % (name, dtype, tuple(shape)))
-    return _ptr(t, name)
+    if t.dtype is dtype and t.shape == shape and t.get_device() == dev and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError("%s must be a contiguous %s tensor of shape %s on the logits' device" % (name, dtype, tuple(shape)))
 
 
 def top_logits(logits: torch.Tensor, values: torch.Tensor, idx: torch.Tensor,
                stream: Optional[torch.cuda.Stream] = None):
     """The K largest logits of each row (fp32 [T][K], descending, ties by the lower index) and their indices (int32
     [T][K]); K is the outputs' width."""
-    z, ld, T, V, f32 = _rows(logits, "logits")
+    z, ld, T, V, f32, dev = _rows(logits, "logits")
     if values.dim() != 2:
         raise ValueError("values must be [T][K]")
     K = values.shape[1]
     fn, name = (lib().sats_top_logits_f32, "sats_top_logits_f32") if f32 else (lib().sats_top_logits, "sats_top_logits")
-    _check(fn(z, ld, T, V, K, _beside(values, "values", torch.float32, (T, K), logits.device),
-              _beside(idx, "idx", torch.int32, (T, K), logits.device), _stream(stream)), name)
+    _check(fn(z, ld, T, V, K, _beside(values, "values", torch.float32, (T, K), dev),
+              _beside(idx, "idx", torch.int32, (T, K), dev), _stream(stream)), name)
 
 
 def _distill_args(logits, top_idx, top_val, labels, tau, alpha):
-    z, ld, T, V, f32 = _rows(logits, "logits")
+    z, ld, T, V, f32, dev = _rows(logits, "logits")
     if (top_idx is None) != (top_val is None):
         raise ValueError("top_idx and top_val go together")
     K = 0
@@ -489,10 +488,9 @@ def _distill_args(logits, top_idx, top_val, labels, tau, alpha):
         if top_idx.dim() != 2:
             raise ValueError("top_idx must be [T][K]")
         K = top_idx.shape[1]
-    dev = logits.device
     return (z, ld, T, V, _beside(top_idx, "top_idx", torch.int32, (T, K), dev),
             _beside(top_val, "top_val", torch.float32, (T, K), dev), K,
-            _beside(labels, "labels", torch.int32, (T,), dev), float(tau), float(alpha)), f32
+            _beside(labels, "labels", torch.int32, (T,), dev), float(tau), float(alpha)), f32, dev
 
 
 def distill_loss(logits: torch.Tensor, top_idx: Optional[torch.Tensor], top_val: Optional[torch.Tensor],
@@ -501,16 +499,16 @@ def distill_loss(logits: torch.Tensor, top_idx: Optional[torch.Tensor], top_val:
                  stream: Optional[torch.cuda.Stream] = None):
     """Per-row distillation loss against a teacher's top logits, mixed with the cross entropy of the labels
     (sats_distill_loss); lse (fp32 [T][2]) is for distill_grad."""
-    args, f32 = _distill_args(logits, top_idx, top_val, labels, tau, alpha)
-    T, dev = args[2], logits.device
+    args, f32, dev = _distill_args(logits, top_idx, top_val, labels, tau, alpha)
+    T = args[2]
     fn = lib().sats_distill_loss_f32 if f32 else lib().sats_distill_loss
     _check(fn(*args, _beside(loss, "loss", torch.float32, (T,), dev), _beside(lse, "lse", torch.float32, (T, 2), dev),
               _beside(dev_status, "dev_status", torch.int32, (1,), dev), _stream(stream)), "sats_distill_loss")
 
 
 def _dlogits(dlogits, logits):
-    d, ld, T, V, f32 = _rows(dlogits, "dlogits")
-    if dlogits.shape != logits.shape or f32 != (logits.dtype == torch.float32) or dlogits.device != logits.device:
+    d, ld, _, _, f32, dev = _rows(dlogits, "dlogits")
+    if dlogits.shape != logits.shape or f32 != (logits.dtype is torch.float32) or dev != logits.get_device():
         raise ValueError("dlogits must have the logits' shape, type and device")
     return d, ld
 
@@ -521,8 +519,8 @@ def distill_grad(logits: torch.Tensor, top_idx: Optional[torch.Tensor], top_val:
                  stream: Optional[torch.cuda.Stream] = None):
     """The gradient of sum(g * loss) with respect to the logits, from the lse of distill_loss (sats_distill_grad);
     dlogits may be the logits."""
-    args, f32 = _distill_args(logits, top_idx, top_val, labels, tau, alpha)
-    T, dev = args[2], logits.device
+    args, f32, dev = _distill_args(logits, top_idx, top_val, labels, tau, alpha)
+    T = args[2]
     d, ld_d = _dlogits(dlogits, logits)
     fn = lib().sats_distill_grad_f32 if f32 else lib().sats_distill_grad
     _check(fn(*args, _beside(lse, "lse", torch.float32, (T, 2), dev), _beside(g, "g", torch.float32, (T,), dev), d, ld_d,
@@ -534,8 +532,8 @@ def distill_loss_grad(logits: torch.Tensor, top_idx: Optional[torch.Tensor], top
                       dlogits: torch.Tensor, g: Optional[torch.Tensor] = None,
                       dev_status: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
     """Loss and gradient in one pass over the logits (sats_distill_loss_grad); dlogits may be the logits."""
-    args, f32 = _distill_args(logits, top_idx, top_val, labels, tau, alpha)
-    T, dev = args[2], logits.device
+    args, f32, dev = _distill_args(logits, top_idx, top_val, labels, tau, alpha)
+    T = args[2]
     d, ld_d = _dlogits(dlogits, logits)
     fn = lib().sats_distill_loss_grad_f32 if f32 else lib().sats_distill_loss_grad
     _check(fn(*args, _beside(g, "g", torch.float32, (T,), dev), _beside(loss, "loss", torch.float32, (T,), dev), d, ld_d,
@@ -549,9 +547,9 @@ def sample(logits: torch.Tensor, u: torch.Tensor, ids: torch.Tensor, temperature
            stream: Optional[torch.cuda.Stream] = None):
     """Draws a token id per row (int32 [B]) from the random numbers u (fp32 [B] in [0, 1)) with each row's own
     temperature, top-k, top-p and min-p (sats_sample)."""
-    z, ld, B, V, f32 = _rows(logits, "logits")
-    dev = logits.device
-    vec = lambda t, name, dtype=torch.float32: _beside(t, name, dtype, (B,), dev)
+    z, ld, B, V, f32, dev = _rows(logits, "logits")
+    one = (B,)
+    vec = lambda t, name, dtype=torch.float32: _beside(t, name, dtype, one, dev)
     fn = lib().sats_sample_f32 if f32 else lib().sats_sample
     _check(fn(z, ld, B, V, vec(temperature, "temperature"), vec(top_k, "top_k", torch.int32), vec(top_p, "top_p"),
               vec(min_p, "min_p"), vec(u, "u"), vec(ids, "ids", torch.int32), vec(logprob, "logprob"),

@@ -151,6 +151,52 @@ def test_rows_larger_than_the_cluster_memory(sats, dtype, V):
     check(sats, rows(z, dtype, pad=3), idx, val, y, up, 1.5, 0.5, d_pad=2)
 
 
+def test_large_offsets(sats):
+    # rows so far apart that their offsets pass 32 bits, of the logits and of the gradient
+    V, T, ld = 2003, 3, (1 << 31) + 5
+    z, idx, val, y, up = case(T, V, 8, 33)
+    buf, out = (torch.empty((T - 1) * ld + V, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    zd, d = (torch.as_strided(b, (T, V), (ld, 1)) for b in (buf, out))
+    zd.copy_(torch.from_numpy(z))
+    a = (zd, to_dev(idx), to_dev(val), to_dev(y), 2.0, 0.5)
+    loss, lse = torch.zeros(T, device="cuda"), torch.zeros(T, 2, device="cuda")
+    rl, _, rd = vocab.distill(zd.double().cpu().numpy(), idx, val.astype(np.float64), y, 2.0, 0.5, up)
+    for one_pass in (False, True):
+        out.zero_()
+        if one_pass:
+            sats.distill_loss_grad(*a, loss, d, g=to_dev(up))
+        else:
+            sats.distill_loss(*a, loss, lse=lse)
+            sats.distill_grad(*a, lse, d, g=to_dev(up))
+        close(loss.double().cpu().numpy(), rl, 12 * DELTA, 2.0 ** -20)
+        close(d.double().cpu().numpy(), rd, 16 * DELTA * np.abs(up).max(), 2.0 ** -8)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_every_pair_of_boundaries(sats, dtype):
+    # the logits' and the gradient's rows on all combinations of places within 16 bytes, rows of a few granules to many
+    E = 4 if dtype == torch.float32 else 8
+    for V in (E - 1, 3 * E + 1, 1000):
+        z, idx, val, y, up = case(4, V, 3, 34)
+        for a in range(E):
+            for b in range(0, E, 1 if V < 100 else 3):
+                check(sats, rows(z, dtype, pad=(a * 3) % E, off=a), idx, val, y, up, 1.5, 0.5, d_pad=(b * 5) % E, d_off=b)
+
+
+def test_many_rows_of_one_cluster(sats):
+    # clusters go from row to row: live, ignored, without entries, with repeated ones, in every order
+    T, V, K = 2500, 500, 5
+    g = np.random.default_rng(35)
+    z, idx, val, y, up = case(T, V, K, 36)
+    y[g.random(T) < 0.4] = -1
+    idx[g.random(T) < 0.3] = -1
+    rep = g.random(T) < 0.3
+    idx[rep, 3] = idx[rep, 0]
+    for dtype, pad in ((torch.float32, 0), (torch.bfloat16, 3)):
+        check(sats, rows(z, dtype, pad=pad), idx, val, y, up, 2.0, 0.5, d_pad=1)
+        check(sats, rows(z, dtype, pad=pad), idx, val, y, up, 1.0, 1.0, d_pad=pad)
+
+
 def test_without_labels_and_without_entries(sats):
     z, idx, val, y, up = case(5, 3001, 16, 24)
     check(sats, rows(z, torch.float32), idx, val, None, up, 2.0, 0.25)

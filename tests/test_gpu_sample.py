@@ -166,6 +166,56 @@ def test_batches(sats, B):
     check(sats, rows(logits("normal", B, V, 53), torch.bfloat16, pad=1), *settings(B, V, 54))
 
 
+def test_large_offsets(sats):
+    # rows so far apart that their offsets pass 32 bits
+    V, B, ld = 4099, 3, (1 << 31) + 5
+    buf = torch.empty((B - 1) * ld + V, dtype=torch.bfloat16, device="cuda")
+    z = torch.as_strided(buf, (B, V), (ld, 1))
+    z.copy_(torch.from_numpy(logits("normal", B, V, 60)))
+    check(sats, z, [0.1, 0.5, 0.9], p=[0.9, 1.0, 0.3], k=[0, 0, 100])
+
+
+def test_long_lists(sats):
+    # sets that are sorted: a top-k near the list's limit, nuclei whose border lies among many equal tokens
+    B, V = 6, 40009
+    u = np.linspace(0.05, 0.95, B)
+    for dtype in (torch.float32, torch.bfloat16):
+        z = rows(logits("normal", B, V, 61), dtype)
+        check(sats, z, u, k=[1024, 1000, 700, 512, 300, 257], p=[0.99, 1.0, 0.5, 0.999, 0.7, 1.0], mp=[0, 0.01, 0, 0, 0.2, 0])
+        ties = logits("ties", B, V, 62)
+        ties[3:] = np.round(ties[3:] / 3) * 3      # thousands of tokens share a value
+        check(sats, rows(ties, dtype), u, p=[0.2, 0.6, 0.95, 0.2, 0.6, 0.95])
+        check(sats, rows(ties, dtype), u, p=[0.2, 0.6, 0.95, 0.2, 0.6, 0.95], k=[2000, 5000, 1500, 2000, 5000, 1500])
+    # a few hundred different values within one step of the weight
+    near = np.full((B, V), -30.0, np.float32)
+    near[:, ::50] = 1.0 + np.arange(near[:, ::50].shape[1], dtype=np.float32) * 1e-6
+    check(sats, rows(near, torch.float32), u, p=[0.1, 0.3, 0.5, 0.7, 0.9, 0.99])
+
+
+@pytest.mark.parametrize("T", [4.0, 20.0, 300.0])
+def test_high_temperatures(sats, T):
+    # weights so alike that many steps of the weight are within a logit of each other
+    B, V = 5, 30011
+    z = rows(logits("normal", B, V, 63), torch.float32)
+    check(sats, z, np.linspace(0.01, 0.99, B), T=np.full(B, T), p=[0.05, 0.3, 0.7, 0.95, 0.9999])
+
+
+def test_first_call_captured(sats):
+    # a shape that no call has had before, captured at once
+    B, V = 3, 77777
+    z = rows(logits("normal", B, V, 64), torch.float32)
+    ud, ids = dev([0.2, 0.5, 0.8]), torch.zeros(B, dtype=torch.int32, device="cuda")
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        sats.sample(z, ud, ids, stream=s)
+    g.replay()
+    torch.cuda.synchronize()
+    ri, _, _, margin = vocab.sample(z.double().cpu().numpy(), ud.double().cpu().numpy())
+    assert (margin > NEAR).all() and np.array_equal(ids.cpu().numpy(), ri)
+
+
 def test_bad_settings(sats):
     V = 1000
     z = rows(logits("normal", 8, V, 55), torch.float32)
