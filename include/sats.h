@@ -465,7 +465,7 @@ SATS_API sats_status sats_route_calibrate(const float *score, int V, const int32
  *   labels     : device int32 [T], or NULL for no CE term (CE = 0).  A label
  *                below 0 makes its row an ignored one: nothing of it is read,
  *                its loss, lse and gradient are 0.
- *   tau, alpha : 0 < tau < inf, 0 <= alpha <= 1; at least one of the two terms
+ *   tau, alpha : 2^-10 <= tau <= 2^10, 0 <= alpha <= 1; at least one of the two terms
  *                must be there (else SATS_EINVAL).
  *   loss       : device fp32 [T], written.
  *   lse        : device fp32 [T][2] or NULL; log sum_j exp(z_j / tau) and
@@ -480,7 +480,8 @@ SATS_API sats_status sats_route_calibrate(const float *score, int V, const int32
  * sats_distill_grad -- its backward pass:
  *     dlogits_j = g (alpha tau (softmax(z / tau)_j - sum_{k: top_idx_k = j} q_k)
  *                    + (1 - alpha) (softmax(z)_j - [j = label]))
- *   from the same arguments and the lse that sats_distill_loss wrote.
+ *   from the same arguments and the lse that sats_distill_loss wrote, whose
+ *   rounding it inherits: 2^-24 |lse| relative.
  *   g          : device fp32 [T], the gradient of each row's loss, or NULL for 1.
  *   dlogits    : device, the logits' type, rows of V elements ld_d >= V apart,
  *                written (each value rounded once).  It may be the logits
@@ -500,7 +501,8 @@ SATS_API sats_status sats_route_calibrate(const float *score, int V, const int32
  *   running sum of w exceeds u times its total over the kept ones.
  *   temperature, top_k, top_p, min_p : device fp32 / int32 / fp32 / fp32 [B],
  *                or NULL for 1, off, off, off.  T >= 0 and finite, 0: the largest
- *                logit (the lowest index that has it).  top_k <= 0 or >= V is off,
+ *                logit (the lowest index that has it); above 0 and below 1e-30: one
+ *                of the largest, all alike.  top_k <= 0 or >= V is off,
  *                top_p >= 1 is off, top_p <= 0 keeps one, min_p <= 0 is off,
  *                min_p <= 1.
  *   u          : device fp32 [B], random numbers in [0, 1).

@@ -21,6 +21,7 @@ namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr int kMaxEntries = 1024;             // teacher entries of a row
+constexpr float kMinTau = 0x1p-10f;           // to its inverse: a log-sum-exp at tau keeps some of its bits
 constexpr size_t kMaxCache = 180 * 1024;      // of a row's share in shared memory
 constexpr size_t kMaxSmem = kSmemPerCta - 2 * 1024;   // dynamic: a row's share, two tables of entries
 constexpr size_t kStepShare = 72 * 1024;      // of a row per CTA, where the cluster allows: several CTAs to an SM
@@ -601,7 +602,7 @@ __global__ void __launch_bounds__(kGradThreads, 4) distill_grad_kernel(const Dis
         const float ctau = kLog2e / p.tau;
         if (p.alpha > 0.f && p.K > 0)
             any = load_entries<F32, TH>(ent, p, row, label, lo, hi, ctau, part, rank == 0, &shares, &facts);
-        if (hard) zy = load_logit(p.z, (int64_t)row * p.ldz + label, F32);
+        if (hard && label >= lo && label < hi) zy = load_logit(p.z, (int64_t)row * p.ldz + label, F32);
         __syncthreads();   // in place: the targets' logits are read before anybody stores
     }
     const float wt = any ? p.alpha : 0.f, wh = hard ? 1.f - p.alpha : 0.f;
@@ -682,6 +683,7 @@ __global__ void __launch_bounds__(kStepThreads, kStepPerSm) distill_step_kernel(
     __shared__ __align__(16) float csum[2][kRowMaxCluster][4];
     __shared__ uint64_t arrived[2];
     __shared__ int never;
+    __shared__ float label_logit;            // the first thread's: in place, it is read before the row's sums go out
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int C = p.cluster, rank = blockIdx.x % C, stride = gridDim.x / C;
     char *tables = reinterpret_cast<char *>(row_smem + p.cached);   // entries and their indices' table, two of each in turn
@@ -746,7 +748,7 @@ __global__ void __launch_bounds__(kStepThreads, kStepPerSm) distill_step_kernel(
         const Entries ent(tables + turn * table_bytes, p.K);
         GradFn<NT, false> grad;
         Shares shares;
-        float up = 0.f, wt = 0.f, zy = 0.f, off = 0.f, l2[NT];
+        float up = 0.f, wt = 0.f, off = 0.f, l2[NT];
         int facts = 0;
         bool any = false;
         if (live) {
@@ -757,7 +759,7 @@ __global__ void __launch_bounds__(kStepThreads, kStepPerSm) distill_step_kernel(
                 i0 = p.idx[(size_t)row * p.K + tid];
                 g0 = p.val[(size_t)row * p.K + tid];
             }
-            if (hard) zy = load_logit(p.z, (int64_t)row * p.ldz + label, F32);
+            const float zy = hard && tid == 0 ? load_logit(p.z, (int64_t)row * p.ldz + label, F32) : 0.f;
             up = p.g ? p.g[row] : 1.f;
 
             RunSum<NT> sum = empty_sum<NT>();
@@ -795,6 +797,7 @@ __global__ void __launch_bounds__(kStepThreads, kStepPerSm) distill_step_kernel(
             }
             warp_join(sum, c, 32);
             if (lane == 0) put_sum(wsum[warp], sum);
+            if (tid == 0) label_logit = zy;
             __syncthreads();
             sum = get_sum<NT>(wsum[lane & (WARPS - 1)]);
             warp_join(sum, c, WARPS);
@@ -890,6 +893,7 @@ __global__ void __launch_bounds__(kStepThreads, kStepPerSm) distill_step_kernel(
             }
         }
         if (live) {
+            const float zy = tid == 0 ? label_logit : 0.f;
             if (rank == 0 && any) {
                 const float kd = warp_sum(kd_part<TH>(ent, p.K, shares, off, l2[0]));
                 if (lane == 0) wkd[warp] = kd;
@@ -912,13 +916,17 @@ __global__ void __launch_bounds__(kStepThreads, kStepPerSm) distill_step_kernel(
 
 size_t al16(size_t v) { return (v + 15) & ~(size_t)15; }
 
-// CTAs of a row: one where the rows alone fill the GPU, more where they do not, as long as each still has a granule
-// per thread; and as many as it takes for the share that stays on chip to leave room for other CTAs on the SM.
-int row_cluster(int T, int64_t row_bytes, size_t share)
+// CTAs of a row: one where the rows alone fill the GPU with `fill` CTAs to an SM, more where they do not, as long as each
+// still has a granule for each of `threads`; and as many as it takes for the share that stays on chip to leave room for
+// other CTAs on the SM.  Measured with 1 / 2 / 4 / 8 CTAs a row (us; loss: 151936 bf16 logits, 2 CTAs to an SM; gradient:
+// 151936 fp32 ones, 4 to an SM): loss of 76 rows 14.8 / 12.0 / 11.4 / 16.0, of 304 rows 20.7 / 25.0 / 31.8 / 45.7, of
+// 1216 rows 65 / 83 / 110 / 160 (a cluster costs about a microsecond of every wave); gradient of 76 rows 46 / 30 / 26 /
+// 22, of 304 rows 72 / 66 / 68 / 71, of 1216 rows 235 / 234 / 238 / 256.
+int row_cluster(int T, int64_t row_bytes, size_t share, int fill, int threads)
 {
     int C = 1;
     while (C < kRowMaxCluster && ((share && row_bytes > (int64_t)C * (int64_t)share) ||
-                                  ((int64_t)T * C < 2 * 152 && row_bytes >= 2 * (int64_t)C * kRowThreads * 16)))
+                                  ((int64_t)T * C < fill * 152 && row_bytes >= 2 * (int64_t)C * threads * 16)))
         C *= 2;
     return C;
 }
@@ -934,7 +942,7 @@ bool two_sums(const DistillParams &p) { return p.tau != 1.f && p.alpha > 0.f && 
 template <bool F32>
 cudaError_t launch_loss(DistillParams p, cudaStream_t st)
 {
-    p.cluster = row_cluster(p.T, (int64_t)p.V * RowElem<F32>::kBytes, 0);
+    p.cluster = row_cluster(p.T, (int64_t)p.V * RowElem<F32>::kBytes, 0, 2, kLossThreads);
     const size_t smem = (size_t)p.K * 12;
     const bool two = two_sums(p) || (p.lse && p.tau != 1.f);   // both log-sum-exps are asked for
     const int64_t ctas = (int64_t)p.T * p.cluster;
@@ -954,7 +962,7 @@ size_t plan_grad(DistillParams &p, int tables)
 template <bool F32>
 cudaError_t launch_grad(DistillParams p, cudaStream_t st)
 {
-    p.cluster = row_cluster(p.T, (int64_t)p.V * RowElem<F32>::kBytes, 0);
+    p.cluster = row_cluster(p.T, (int64_t)p.V * RowElem<F32>::kBytes, 0, 4, kGradThreads);
     p.cached = 0;
     const size_t smem = plan_grad(p, 1);
     // (the CTAs of a row need no cluster)
@@ -967,7 +975,7 @@ template <bool F32, int NT, bool SHIFT>
 cudaError_t launch_step(DistillParams p, cudaStream_t st)
 {
     const int64_t bytes = (int64_t)p.V * RowElem<F32>::kBytes;
-    p.cluster = row_cluster(p.T, bytes, kStepShare);
+    p.cluster = row_cluster(p.T, bytes, kStepShare, 2, 2 * kStepThreads);
     const size_t share = al16((size_t)((bytes + 32 + p.cluster - 1) / p.cluster) + 32);
     p.cached = (int)((share < kMaxCache ? share : kMaxCache) / 16);
     const size_t smem = plan_grad(p, 2);
@@ -996,7 +1004,7 @@ sats_status check_distill(const DistillParams &p)
 {
     constexpr int B = RowElem<F32>::kBytes;
     if (p.T < 0 || p.V < 1 || p.ldz < p.V || p.K < 0) return SATS_EINVAL;
-    if (!(p.tau > 0.f) || std::isinf(p.tau) || !(p.alpha >= 0.f && p.alpha <= 1.f)) return SATS_EINVAL;
+    if (!(p.tau >= kMinTau && p.tau <= 1.f / kMinTau) || !(p.alpha >= 0.f && p.alpha <= 1.f)) return SATS_EINVAL;
     if (p.K > kMaxEntries || p.V > INT_MAX - 64 || p.T > INT_MAX / kRowMaxCluster) return SATS_ESHAPE;
     if (p.ldz > (int64_t)1 << 40 || p.ldd > (int64_t)1 << 40) return SATS_ESHAPE;
     if (p.T == 0) return SATS_OK;

@@ -1,5 +1,5 @@
 // rows.cuh -- rows of vocabulary logits on a thread-block cluster (sm_103a): what the kernels of distill.cu and
-// logits.cu share.
+// logits.cuh share.
 //
 // A row of V logits (bf16 or fp32) is cut into granules of 16 bytes on the row's own 16-byte boundaries, so that a
 // row that starts anywhere still moves in whole vectors; the places of the first and last granule that lie outside
@@ -14,7 +14,6 @@
 
 namespace sats {
 
-constexpr int kRowThreads = 512, kRowWarps = kRowThreads / 32;
 constexpr int kRowMaxCluster = 8;   // the portable limit
 
 template <bool F32>
@@ -173,13 +172,6 @@ __device__ __forceinline__ float granule_max(const uint4 &v)
 }
 
 // ------------------------------------------------------------------ clusters
-__device__ __forceinline__ unsigned cluster_rank()
-{
-    unsigned r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-
 // A barrier of all threads of all CTAs of the cluster, in two halves.  A kernel arrives at its start and waits before
 // it first reaches another CTA's memory: that CTA has to run by then.
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }

@@ -151,6 +151,15 @@ def test_rows_larger_than_the_cluster_memory(sats, dtype, V):
     check(sats, rows(z, dtype, pad=3), idx, val, y, up, 1.5, 0.5, d_pad=2)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_extreme_temperatures(sats, dtype):
+    z, idx, val, y, up = case(5, 3001, 9, 37)
+    # (the logits and values scaled so that their quotients by tau are ordinary ones)
+    for tau, size in ((2.0 ** -10, 2.0 ** -10), (2.0 ** 10, 2.0 ** 5)):
+        check(sats, rows(z * np.float32(size), dtype), idx, val * np.float32(size), y, up, tau, 1.0)
+        check(sats, rows(z * np.float32(size), dtype), idx, val * np.float32(size), y, up, tau, 0.5)
+
+
 def test_large_offsets(sats):
     # rows so far apart that their offsets pass 32 bits, of the logits and of the gradient
     V, T, ld = 2003, 3, (1 << 31) + 5

@@ -50,6 +50,14 @@ def _both(s, z=0x100000, ld=8, T=2, V=8, idx=0x2000, val=0x3000, K=2, labels=0x4
     return fn(z, ld, T, V, idx, val, K, labels, tau, alpha, None, loss, d, ld_d, None, None)
 
 
+def test_distill_tau(sats):
+    for call in (_loss, _grad, _both):
+        for tau in (2.0**-10 * (1 - 2.0**-24), 2.0**10 * (1 + 2.0**-23), 1e-45, 3e38):
+            assert call(sats, tau=tau) == sats.EINVAL
+        for tau in (2.0**-10, 2.0**10):
+            assert call(sats, tau=tau, T=0) == sats.OK
+
+
 def test_distill(sats):
     s = sats
     for call in (_loss, _grad, _both):
