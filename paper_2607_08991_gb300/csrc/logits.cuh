@@ -552,6 +552,104 @@ __device__ __forceinline__ uint32_t group_bound(Shared *sh, uint32_t *scratch, i
     return border < kBoundBins ? klo : kKeyNone + 1;
 }
 
+// ------------------------------------------------------------------ groups of a row that streams through registers
+constexpr int kTurn = 8;               // granules in flight per thread
+constexpr int kMaxGroups = 16;         // groups of a thread, at most
+
+// Granules of a group: `size` (1, 2, 4 or 8) in each of `turns` (1 unless size is 8) turns.
+struct Groups {
+    int size, turns;
+};
+
+// The maxima of a thread's groups of U granules in each of `turns` turns, to gm[group][thread]; the largest and the
+// least above -inf.  Granules go to the threads in turn.
+template <bool F32, int U>
+__device__ __forceinline__ void group_maxima(const Ctx<F32> &c, int turns, float *gm, float *hi, float *lo)
+{
+    constexpr int kPer = kTurn / U;
+    const int tid = threadIdx.x;
+    float most = -INFINITY;   // (of a group that goes on)
+    int left = turns;
+    for (int v0 = tid; v0 < c.n; v0 += kTurn * kSelThreads) {
+        uint4 x[kTurn];
+#pragma unroll
+        for (int k = 0; k < kTurn; ++k) {
+            const uint32_t none = F32 ? 0xff800000u : 0xff80ff80u;
+            x[k] = v0 + k * kSelThreads < c.n ? load_granule<F32>(c.r, c.gb + v0 + k * kSelThreads)
+                                              : make_uint4(none, none, none, none);
+        }
+#pragma unroll
+        for (int g = 0; g < kPer; ++g) {
+            float m = granule_max<F32>(x[g * U]);
+#pragma unroll
+            for (int k = 1; k < U; ++k) m = fmaxf(m, granule_max<F32>(x[g * U + k]));
+            most = fmaxf(most, m);
+            if (U == kTurn && --left > 0 && v0 + kTurn * kSelThreads < c.n) continue;
+            *gm = most;
+            gm += kSelThreads;
+            *hi = fmaxf(*hi, most);
+            if (most > -INFINITY) *lo = fminf(*lo, most);
+            most = -INFINITY;
+            left = turns;
+        }
+    }
+}
+
+// Their maxima to gm[group][thread], kMaxGroups at most; returns how many groups the thread has.
+template <bool F32>
+__device__ __forceinline__ int group_maxima(const Ctx<F32> &c, Groups q, float *gm, float *hi, float *lo)
+{
+    const int tid = threadIdx.x;
+    switch (q.size) {
+    case 1: group_maxima<F32, 1>(c, 1, gm + tid, hi, lo); break;
+    case 2: group_maxima<F32, 2>(c, 1, gm + tid, hi, lo); break;
+    case 4: group_maxima<F32, 4>(c, 1, gm + tid, hi, lo); break;
+    default: group_maxima<F32, 8>(c, q.turns, gm + tid, hi, lo); break;
+    }
+    const int S = q.size * q.turns, turns = tid < c.n ? (c.n - tid + kTurn * kSelThreads - 1) / (kTurn * kSelThreads) : 0;
+    return (turns * kTurn + S - 1) / S;
+}
+
+// The CTA's elements from fb on, read again in the groups whose maximum is: to `own`, in no order; sh->nlist says how many
+// there are (or more than cap), of which the first cap are there.  hits: cap words.
+template <bool F32>
+__device__ __forceinline__ void collect_groups(const Ctx<F32> &c, Groups q, const float *gm, int mine, int *hits, float fb,
+                                               unsigned long long *own, int cap)
+{
+    constexpr int E = RowElem<F32>::kPer;
+    Shared *sh = c.sh;
+    const int tid = threadIdx.x, S = q.size * q.turns;
+    if (tid == 0) sh->nlist = sh->nhits = 0;
+    __syncthreads();
+    for (int g = 0; g < mine; ++g)
+        if (gm[g * kSelThreads + tid] >= fb) {
+            const uint32_t at = atomicAdd(&sh->nhits, 1u);
+            if (at < (uint32_t)cap) hits[at] = g * kSelThreads + tid;
+        }
+    __syncthreads();
+    const int nhits = min((int)sh->nhits, cap);
+    // granule j of group g of thread t is number (g S + j) kSelThreads + t of the CTA's
+    for (int w = tid; w < nhits * S; w += kSelThreads) {
+        const int h = hits[w / S], v = (h / kSelThreads * S + w % S) * kSelThreads + h % kSelThreads;
+        if (v >= c.n) continue;
+        const uint4 x = load_granule<F32>(c.r, c.gb + v);
+        if (!(granule_max<F32>(x) >= fb)) continue;
+        float f[E];
+        granule_floats<F32>(c.clean(x), f);
+        const int i0 = c.r.first(c.gb + v);
+#pragma unroll
+        for (int j = 0; j < E; ++j)
+            if (f[j] >= fb && f[j] > -INFINITY) {
+                const uint32_t at = atomicAdd(&sh->nlist, 1u);
+                if (at < (uint32_t)cap) own[at] = ((unsigned long long)key_of(f[j]) << 32) | (uint32_t)~(uint32_t)(i0 + j);
+            }
+    }
+    __syncthreads();
+    // (a group has a candidate: with more groups than that there are too many of them)
+    if (tid == 0 && sh->nhits > (uint32_t)cap) sh->nlist = sh->nhits;
+    __syncthreads();
+}
+
 template <bool F32>
 __device__ __forceinline__ void set_ctx(Ctx<F32> &c, const uint4 *cache, int cached, int C, Shared *sh,
                                         int cap = kListCap)
@@ -585,6 +683,17 @@ int logits_cluster(int rows, int64_t row_bytes, int want, size_t share)
                                    row_bytes >= 2 * (int64_t)C * kSelThreads * 16)))
         C *= 2;
     return C;
+}
+
+// Groups of a row's granules for `groups` (4 to kMaxGroups) of each thread.
+Groups plan_groups(int64_t row_bytes, int cluster, int groups)
+{
+    const int64_t each = (row_bytes / 16 / cluster + 4 + kSelThreads - 1) / kSelThreads;   // granules of a thread, at most
+    const int64_t rounded = (each + kTurn - 1) / kTurn * kTurn;
+    Groups q{1, 1};
+    while (q.size < kTurn && q.size * groups < rounded) q.size *= 2;
+    while ((int64_t)q.size * q.turns * groups < rounded) q.turns *= 2;
+    return q;
 }
 
 sats_status check_rows(const void *logits, int64_t ld, int rows, int V, int bytes)

@@ -6,6 +6,8 @@
 // A token's weight is therefore a whole number, w = 2^F exp((z - max) / T) to about 35 bits relative (never less
 // than 2^-F absolute), computed in pairs of floats; sums of whole numbers do not depend on their order, and every
 // decision (the nucleus, the drawn token) is the same in whichever grouping it is found.
+#include <algorithm>
+
 #include "internal.h"
 #include "rows.cuh"
 
@@ -21,9 +23,9 @@ namespace {
 
 constexpr int kAhead = 8;              // granules in flight per thread while the row arrives
 constexpr size_t kShare = 64 * 1024;   // of a row's bytes per CTA, where the cluster allows
-constexpr size_t kMaxCache = 184 * 1024;
+constexpr size_t kMaxCache = 182 * 1024;
 constexpr size_t kMaxSmem = kMaxCache + (size_t)kListCap * 8;
-static_assert(kMaxSmem + 11 * 1024 <= kSmemPerCta, "with the kernel's static part");
+static_assert(kMaxSmem + 13 * 1024 <= kSmemPerCta, "with the kernel's static part");
 
 // ------------------------------------------------------------------ weights
 // 2^(-j / 1024) in two floats.
@@ -396,6 +398,23 @@ __device__ __noinline__ void cut_in_list(unsigned long long *list, int n, unsign
     }
 }
 
+// Gives each CTA its run of the kBins words `count` of all CTAs, one CTA's behind another's: to `got`, or in place where
+// there is one CTA.  A barrier ahead.
+template <bool F32>
+__device__ __forceinline__ uint32_t *exchange_counts(Ctx<F32> &c, uint32_t *count, uint32_t *got)
+{
+    if (c.C == 1) return count;
+    const int nb = kBins / c.C;
+    for (int i = threadIdx.x; i < kBins / 4; i += kSelThreads) {
+        const uint4 q = reinterpret_cast<const uint4 *>(count)[i];
+        const int b = 4 * i;
+        st_peer_v4(peer_addr(got + c.rank * nb + b % nb, b / nb), __uint_as_float(q.x), __uint_as_float(q.y),
+                   __uint_as_float(q.z), __uint_as_float(q.w));
+    }
+    cluster_sync_all();
+    return got;
+}
+
 // The cut that keeps, of what by_k keeps, the largest up to a share top_p < 1 of the mass, by counts and exact weights;
 // false (the same in every CTA of the row) where the border does not lie where the counts have it, or among more
 // tokens than the list holds.
@@ -436,19 +455,8 @@ __device__ bool cut_by_counts(Ctx<F32> &c, const Scale &s, const float2 *tab, un
         }
     }
     __syncthreads();
-    // a run of steps per CTA: its counts in all CTAs
     const int nb = kBins / C;
-    if (C > 1) {
-        for (int i = tid; i < kBins / 4; i += kSelThreads) {
-            const uint4 q = reinterpret_cast<const uint4 *>(count)[i];
-            const int b = 4 * i;
-            st_peer_v4(peer_addr(got + c.rank * nb + b % nb, b / nb), __uint_as_float(q.x), __uint_as_float(q.y),
-                       __uint_as_float(q.z), __uint_as_float(q.w));
-        }
-        cluster_sync_all();
-    } else {
-        got = count;
-    }
+    got = exchange_counts(c, count, got);
     constexpr int kMost = kBins / kSelThreads;
     const int per = (nb + kSelThreads - 1) / kSelThreads;
     unsigned long long m[kMost], mine = 0;   // masses in whole numbers: their sums are the same in every CTA
@@ -670,6 +678,7 @@ struct SampleParams {
     int32_t *n_kept;
     int32_t *status;
     int cluster, cached;
+    Groups groups;
 };
 
 __device__ __forceinline__ void put_sample(const SampleParams &p, int row, int id, float logprob, long long n)
@@ -733,89 +742,106 @@ __device__ __noinline__ void draw_from_list(const SampleParams &p, int row, unsi
     }
 }
 
-template <bool F32>
-__global__ void __launch_bounds__(kSelThreads, kSelPerSm) sample_kernel(const SampleParams p)
-{
-    extern __shared__ __align__(16) uint4 smem[];
-    __shared__ Shared sh;
-    __shared__ float2 tab[1024];
-    const int row = (int)(blockIdx.x >> (31 - __clz(p.cluster))), tid = threadIdx.x;
-    unsigned long long *list = reinterpret_cast<unsigned long long *>(smem + p.cached);
-    Ctx<F32> c{Row<F32>(p.z, row, p.ld, p.V)};
-    set_ctx(c, smem, p.cached, p.cluster, &sh);
-    start_row(c, smem);
-    const float T = p.temperature ? p.temperature[row] : 1.f;
-    const float top_p = p.top_p ? p.top_p[row] : 1.f, min_p = p.min_p ? p.min_p[row] : 0.f;
-    const float u = p.u[row];
-    int k = p.top_k ? p.top_k[row] : 0;
-    if (!(T >= 0.f) || T == INFINITY || top_p != top_p || !(min_p <= 1.f) || !(u >= 0.f && u < 1.f)) {
-        if (c.rank == 0 && tid == 0) {
-            put_sample(p, row, -1, __int_as_float(0x7fffffff), 0);
-            if (p.status) atomicOr(p.status, kStatusBadToken);
-        }
-        cp_async_wait<0>();
-        if (c.C > 1) cluster_wait();
-        return;   // (every CTA of the row)
+// What a row asks for.
+struct Settings {
+    float T, top_p, min_p, u;
+    int k;                  // 0: off
+    bool bad, greedy, nucleus;
+
+    __device__ __forceinline__ Settings(const SampleParams &p, int row)
+    {
+        T = p.temperature ? p.temperature[row] : 1.f;
+        top_p = p.top_p ? p.top_p[row] : 1.f;
+        min_p = p.min_p ? p.min_p[row] : 0.f;
+        u = p.u[row];
+        k = p.top_k ? p.top_k[row] : 0;
+        bad = !(T >= 0.f) || T == INFINITY || top_p != top_p || !(min_p <= 1.f) || !(u >= 0.f && u < 1.f);
+        if (k < 0 || k >= p.V) k = 0;
+        greedy = T == 0.f || k == 1 || top_p <= 0.f;
+        nucleus = top_p < 1.f;
     }
-    if (k < 0 || k >= p.V) k = 0;
-    const bool greedy = T == 0.f || k == 1 || top_p <= 0.f;
-    const bool nucleus = top_p < 1.f;
-    const int want = !greedy && k > 0 && k <= kMaxTop ? k : 0;   // what the list serves
-    if (!greedy)
-        for (int i = tid; i < 1024; i += kSelThreads) tab[i] = kExp2.v[i];
+};
+
+__device__ __forceinline__ void put_bad(const SampleParams &p, int row)
+{
+    put_sample(p, row, -1, __int_as_float(0x7fffffff), 0);
+    if (p.status) atomicOr(p.status, kStatusBadToken);
+}
+
+// min-p as the least key that is kept: exp((z - top) / T) >= min_p where z >= top + T log(min_p).  All threads.
+__device__ __forceinline__ uint32_t least_key(const Settings &set, const Scale &s, Shared *sh)
+{
+    if (!(set.min_p > 0.f)) return 0;
+    if (threadIdx.x == 0) {
+        const double v = s.hard ? (double)s.top : (double)s.top + (double)set.T * log((double)set.min_p);
+        float f = (float)v;
+        if ((double)f < v) f = nextafterf(f, INFINITY);
+        sh->kminp = key_of(f);
+    }
+    __syncthreads();
+    return sh->kminp;
+}
+
+// The draw from the n largest entries of a row, the k largest among them (k 0: all that is kept is).
+__device__ __forceinline__ void draw_list(const SampleParams &p, int row, const Settings &set, const Scale &s,
+                                          unsigned long long *list, int n, uint32_t kminp, const float2 *tab, Shared *sh)
+{
+    const int k = set.k > 0 ? set.k : INT_MAX;
+    const float T = set.T, u = set.u, top_p = set.top_p;
+    if (n <= kSmall) {
+        const Small e(list, n);
+        const unsigned long long w = e.on ? weight(key_float(e.key()), s, tab) : 0ull;
+        e.put_weight(list, w);
+        __syncthreads();
+        int at;
+        unsigned long long above;
+        e.larger(list, n, &at, &above);
+        bool kept = e.on && at < k && e.key() >= kminp;
+        if (set.nucleus) {
+            const unsigned long long Z = block_sum_u64(e.on && e.part == 0 && at < k ? w : 0ull, sh);
+            kept = kept && above < share_ceil(top_p, Z);
+        }
+        const int m = __syncthreads_count(kept && e.part == 0);
+        e.put_weight(list, kept ? w : 0ull);
+        const unsigned long long total = block_sum_u64(kept && e.part == 0 ? w : 0ull, sh);
+        const unsigned long long before = e.earlier(list, n), target = share_floor(u, total);
+        if (kept && e.part == 0 && target >= before && target - before < w)   // one entry
+            put_sample(p, row, e.idx(), log_share(key_float(e.key()), T, s, total), m);
+        return;
+    }
+    draw_from_list(p, row, list, n, k, set.nucleus ? top_p : 1.f, kminp, u, T, s, tab, sh);
+}
+
+// The draw in any case, after start_row.
+template <bool F32>
+__device__ __forceinline__ void sample_row(Ctx<F32> &c, const SampleParams &p, int row, const Settings &set, uint4 *cache,
+                                           unsigned long long *list, const float2 *tab)
+{
+    Shared &sh = *c.sh;
+    const int tid = threadIdx.x, k = set.k;
+    const float T = set.T, u = set.u, top_p = set.top_p;
+    const int want = !set.greedy && k > 0 && k <= kMaxTop ? k : 0;   // what the list serves
     uint32_t kmax, bound;
-    load_row(c, smem, want, reinterpret_cast<uint32_t *>(list), &kmax, &bound);
+    load_row(c, cache, want, reinterpret_cast<uint32_t *>(list), &kmax, &bound);
     if (kmax <= kKeyNone) {   // nothing can be drawn
         if (c.rank == 0 && tid == 0) put_sample(p, row, -1, -INFINITY, 0);
         return;
     }
-    if (greedy) {
+    if (set.greedy) {
         const int id = lowest_at(c, kmax);
         if (c.rank == 0 && tid == 0) put_sample(p, row, id, 0.f, 1);
         return;
     }
     Scale s;
     set_scale(s, key_float(kmax), T, p.V);
-    // min-p as the least key that is kept: exp((z - top) / T) >= min_p where z >= top + T log(min_p)
-    uint32_t kminp = 0;
-    if (min_p > 0.f) {
-        if (tid == 0) {
-            const double v = s.hard ? (double)s.top : (double)s.top + (double)T * log((double)min_p);
-            float f = (float)v;
-            if ((double)f < v) f = nextafterf(f, INFINITY);
-            sh.kminp = key_of(f);
-        }
-        __syncthreads();
-        kminp = sh.kminp;
-    }
+    const uint32_t kminp = least_key(set, s, &sh);
 
     if (want > 0) {
         bool ok;
         const int n = gather_list(c, list, bound, Cut{kKeyNone, INT_MIN}, &ok);
         if (ok) {   // (the same in every CTA of the row)
             if (c.rank != 0) return;   // (nobody reads this CTA's memory any more)
-            if (n <= kSmall) {
-                const Small e(list, n);
-                const unsigned long long w = e.on ? weight(key_float(e.key()), s, tab) : 0ull;
-                e.put_weight(list, w);
-                __syncthreads();
-                int at;
-                unsigned long long above;
-                e.larger(list, n, &at, &above);
-                bool kept = e.on && at < k && e.key() >= kminp;
-                if (nucleus) {
-                    const unsigned long long Z = block_sum_u64(e.on && e.part == 0 && at < k ? w : 0ull, &sh);
-                    kept = kept && above < share_ceil(top_p, Z);
-                }
-                const int m = __syncthreads_count(kept && e.part == 0);
-                e.put_weight(list, kept ? w : 0ull);
-                const unsigned long long total = block_sum_u64(kept && e.part == 0 ? w : 0ull, &sh);
-                const unsigned long long before = e.earlier(list, n), target = share_floor(u, total);
-                if (kept && e.part == 0 && target >= before && target - before < w)   // one entry
-                    put_sample(p, row, e.idx(), log_share(key_float(e.key()), T, s, total), m);
-                return;
-            }
-            draw_from_list(p, row, list, n, k, nucleus ? top_p : 1.f, kminp, u, T, s, tab, &sh);
+            draw_list(p, row, set, s, list, n, kminp, tab, &sh);
             return;
         }
     }
@@ -824,7 +850,7 @@ __global__ void __launch_bounds__(kSelThreads, kSelPerSm) sample_kernel(const Sa
     Cut cut{kKeyNone, INT_MIN};
     if (k > 0) cut = cut_count(c, kmax, k);
     bool sums = false;
-    if (nucleus) {
+    if (set.nucleus) {
         const Nucleus q = cut_mass(c, s, tab, list, kmax, cut, top_p);
         cut = q.cut;
         sums = q.sums;
@@ -840,7 +866,7 @@ __global__ void __launch_bounds__(kSelThreads, kSelPerSm) sample_kernel(const Sa
         for (int q = 0; q < c.C; ++q) count += sh.above[q];
     } else {
         int n = 0;
-        unsigned long long mine = cut.key > kKeyNone ? kept.over_row<true>(c, n) : kept.over_row<false>(c, n);
+        unsigned long long mine = cut.key > kKeyNone ? kept.template over_row<true>(c, n) : kept.template over_row<false>(c, n);
         n = (int)__reduce_add_sync(0xffffffffu, n);
         __syncthreads();
         if ((tid & 31) == 0) sh.part[tid >> 5] = n;
@@ -856,6 +882,657 @@ __global__ void __launch_bounds__(kSelThreads, kSelPerSm) sample_kernel(const Sa
 }
 
 template <bool F32>
+__global__ void __launch_bounds__(kSelThreads, kSelPerSm) sample_kernel(const SampleParams p)
+{
+    extern __shared__ __align__(16) uint4 smem[];
+    __shared__ Shared sh;
+    __shared__ float2 tab[1024];
+    const int row = (int)(blockIdx.x >> (31 - __clz(p.cluster))), tid = threadIdx.x;
+    unsigned long long *list = reinterpret_cast<unsigned long long *>(smem + p.cached);
+    Ctx<F32> c{Row<F32>(p.z, row, p.ld, p.V)};
+    set_ctx(c, smem, p.cached, p.cluster, &sh);
+    start_row(c, smem);
+    const Settings set(p, row);
+    if (set.bad) {
+        if (c.rank == 0 && tid == 0) put_bad(p, row);
+        cp_async_wait<0>();
+        if (c.C > 1) cluster_wait();
+        return;   // (every CTA of the row)
+    }
+    if (!set.greedy)
+        for (int i = tid; i < 1024; i += kSelThreads) tab[i] = kExp2.v[i];
+    sample_row(c, p, row, set, smem, list, tab);
+}
+
+// ------------------------------------------------------------------ bf16 rows by their values
+// A bf16 row has few different values that weigh anything: the tokens of each are counted while the row streams through
+// registers, and all that is asked for (the k-th largest, the mass, the nucleus' border, the kept mass of every CTA)
+// follows exactly from the counts and one weight per value.  Only the CTA in which the token lies reads its tokens again
+// (from the L2) and adds their weights from a table of the values.
+//
+// The values of magnitudes from 2^-10 to below 2^6 have a step each, in descending order.  Smaller ones are listed one by
+// one; of those from -2^6 down, which have no weight, the number is known.  What does not fit this (larger logits, many tiny
+// ones, a border among the listed ones) is drawn the general way.
+constexpr int kSteps = 2 * kBins;   // two counts of 16 bits in a word
+constexpr int kFewMax = kSelThreads;
+constexpr int kLeastMag = 117 << 7, kFarMag = 133 << 7;   // magnitudes as bits
+static_assert(kFarMag - kLeastMag == kSteps / 2, "a step for each value");
+constexpr int kValuesPerSm = 4;
+constexpr int kValuesFrom = 4096;          // tokens of a row
+constexpr int kValuesTo = 65536 - 128;     // of a CTA: counts of 16 bits
+constexpr size_t kValuesShare = 96 * 1024;  // of a row's bytes per CTA, where the cluster allows
+constexpr int kValuesTop = 192;            // the largest top-k that goes by a list
+constexpr uint32_t kNoWay = 0xffffffffu;
+
+__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b)
+{
+    uint32_t d;
+    asm("max.u16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+__device__ __forceinline__ uint32_t min_u16x2(uint32_t a, uint32_t b)
+{
+    uint32_t d;
+    asm("min.u16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+
+__device__ __forceinline__ float step_value(int step)
+{
+    const uint32_t m = step < kSteps / 2 ? (uint32_t)(kFarMag - 1 - step) : (uint32_t)(kLeastMag + step - kSteps / 2) | 0x8000u;
+    return __uint_as_float(m << 16);
+}
+__device__ __forceinline__ int step_of(uint32_t bits)   // (of a value that has one)
+{
+    const int m = (int)(bits & 0x7fffu) - kLeastMag;
+    return bits & 0x8000u ? kSteps / 2 + m : kSteps / 2 - 1 - m;
+}
+
+// The steps of a granule's eight values, in pairs; false: not all of them have one.
+__device__ __forceinline__ bool granule_steps(const uint4 &q, uint32_t (&step)[4])
+{
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+    uint32_t big = 0, least = 0xffffffffu;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const uint32_t mag = w[k] & 0x7fff7fffu;
+        big = max_u16x2(big, mag);
+        least = min_u16x2(least, mag);
+        uint32_t neg;   // all ones in the halves of negative values
+        asm("prmt.b32 %0, %1, 0, 0xbb99;" : "=r"(neg) : "r"(w[k]));
+        // with m = mag - kLeastMag (below 2048): 2047 - m, or 2048 + m of a negative value
+        step[k] = ((mag + 0x10001u * (0x8000u - kLeastMag)) ^ neg ^ 0x07ff07ffu) & 0x0fff0fffu;
+    }
+    return (((least + 0x10001u * (0x8000u - kLeastMag)) & ~(big + 0x10001u * (0x8000u - kFarMag))) & 0x80008000u) == 0x80008000u;
+}
+
+__device__ __forceinline__ uint32_t granule_elem16(const uint4 &q, int j)
+{
+    const uint32_t w = j < 4 ? (j < 2 ? q.x : q.y) : (j < 6 ? q.z : q.w);
+    return (w >> ((j & 1) * 16)) & 0xffffu;
+}
+// Which of the eight have no step, as bits.
+__device__ __forceinline__ uint32_t odd_ones(const uint4 &q)
+{
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+    uint32_t odd = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const uint32_t lo = w[k] & 0x7fffu, hi = (w[k] >> 16) & 0x7fffu;
+        odd |= (lo - kLeastMag >= kFarMag - kLeastMag ? 1u << (2 * k) : 0u) | (hi - kLeastMag >= kFarMag - kLeastMag ? 2u << (2 * k) : 0u);
+    }
+    return odd;
+}
+
+struct ValueShared {
+    float few[kFewMax];
+    unsigned long long part[kSelWarps][kRowMaxCluster], few_mass[kSelWarps], few_kept[kSelWarps];
+    uint32_t part_n[kSelWarps], few_n[kSelWarps];
+    // written by the CTAs of the row
+    unsigned long long mass[kRowMaxCluster][kRowMaxCluster];   // [of the sender's steps][of the CTA]
+    unsigned long long listed[kRowMaxCluster];                 // kept ones among the listed
+    uint32_t n[kRowMaxCluster], listed_n[kRowMaxCluster], there[kRowMaxCluster], below[kRowMaxCluster],
+        counted[kRowMaxCluster];
+    uint32_t border, ties, ties_kept;   // the last kept step; its tokens in this CTA, and the kept ones among them
+    unsigned long long of_k;            // mass of the k largest
+};
+
+// A token's weight from the table (0 where it is cut), for `locate`.
+struct TableMass {
+    const unsigned long long *table;
+    const Scale &s;
+    const float2 *tab;
+    uint32_t kminp;
+    bool listed;             // the ones without a step are kept, from kminp on
+    int tie, idx;            // a step of which only the tokens up to an index are kept (-1: none), its weight 0 in the table
+    unsigned long long tie_w;
+
+    __device__ __forceinline__ unsigned long long elem(float x, uint32_t k, int i) const
+    {
+        const uint32_t bits = __float_as_uint(x) >> 16;
+        const int mag = (int)(bits & 0x7fffu);
+        if (mag >= kFarMag) return 0ull;
+        if (mag < kLeastMag) return listed && k >= kminp ? weight(x, s, tab) : 0ull;
+        const int step = step_of(bits);
+        return step == tie ? (i <= idx ? tie_w : 0ull) : table[step];
+    }
+    // i0: the index of the first of them
+    __device__ __forceinline__ unsigned long long granule(const uint4 &q, int i0) const
+    {
+        uint32_t step[4], odd = granule_steps(q, step) ? 0u : odd_ones(q);
+        unsigned long long a = 0, b = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            a += table[step[k] & 0xffffu];
+            b += table[step[k] >> 16];
+        }
+        if (tie >= 0) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if ((int)(step[k] & 0xffffu) == tie && !(odd & (1u << (2 * k))) && i0 + 2 * k <= idx) a += tie_w;
+                if ((int)(step[k] >> 16) == tie && !(odd & (2u << (2 * k))) && i0 + 2 * k + 1 <= idx) b += tie_w;
+            }
+        }
+        for (; odd != 0; odd &= odd - 1u) {
+            const int j = __ffs(odd) - 1;
+            const uint32_t w = step[j >> 1], x = granule_elem16(q, j) << 16;
+            a -= table[j & 1 ? w >> 16 : w & 0xffffu];
+            a += elem(__uint_as_float(x), key_of(__uint_as_float(x)), i0 + j);   // (-inf and NaN weigh nothing)
+        }
+        return a + b;
+    }
+};
+
+// The tokens of one value.
+struct TieCount {
+    uint32_t bits;   // of it
+    __device__ __forceinline__ unsigned long long elem(float x, uint32_t, int) const
+    {
+        return __float_as_uint(x) >> 16 == bits;
+    }
+    __device__ __forceinline__ unsigned long long granule(const uint4 &q, int) const
+    {
+        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+        uint32_t n = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) n += ((w[k] & 0xffffu) == bits) + (w[k] >> 16 == bits);
+        return n;
+    }
+};
+
+// The first token of this CTA's, in order, at which the running sum of f passes `target` (below their sum): found(idx,
+// key) by one thread.  Sums of 32 granules each, then the elements of the ones that hold it.  seg: kSegs words.
+constexpr int kSegs = kSelThreads;
+static_assert(kValuesTo / 8 + 8 <= kSegs * 32, "a thread per sum");
+static_assert(32 * 8 == kSelThreads, "a thread per element of them");
+template <typename S, typename Found>
+__device__ __forceinline__ void find_in_share(const Ctx<false> &c, unsigned long long target, const S &f,
+                                              unsigned long long *seg, Found found)
+{
+    constexpr int U = 4;
+    Shared *sh = c.sh;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int wper = (c.n + kSelWarps - 1) / kSelWarps, each = (wper + 31) / 32;   // sums of a warp
+    for (int i0 = 0; i0 < each; i0 += U) {
+        uint4 x[U];
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            const int v = c.wb + 32 * (i0 + k) + lane;
+            x[k] = v < c.we ? load_granule<false>(c.r, c.gb + v) : make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u);
+        }
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            const int v = c.wb + 32 * (i0 + k) + lane;
+            const unsigned long long a = warp_sum_u64(v < c.we ? f.granule(x[k], c.r.first(c.gb + v)) : 0ull);
+            if (lane == 0 && i0 + k < each) seg[warp * each + i0 + k] = a;
+        }
+    }
+    __syncthreads();
+    unsigned long long mine = tid < kSelWarps * each ? seg[tid] : 0ull, total;
+    unsigned long long run = block_scan_u64(mine, sh, &total);
+    if (target >= run && target - run < mine) {   // (one thread)
+        sh->border = tid;
+        sh->mass[0] = run;
+    }
+    __syncthreads();
+    const int at = sh->border, w = at / each, v = w * wper + 32 * (at - w * each) + (tid >> 3);
+    target -= sh->mass[0];
+    const int i = c.r.first(c.gb + v) + (tid & 7);
+    const float x = v < min(c.n, (w + 1) * wper) ? c.get(v, tid & 7) : -INFINITY;
+    const uint32_t key = key_of(x);
+    mine = key > kKeyNone ? f.elem(x, key, i) : 0ull;
+    run = block_scan_u64(mine, sh, &total);
+    if (target >= run && target - run < mine) found(i, key);   // (one thread)
+}
+
+__device__ __noinline__ void sample_row_again(Ctx<false> c, const SampleParams &p, int row, const Settings &set,
+                                              unsigned long long *list, const float2 *tab)
+{
+    start_row(c, nullptr);
+    sample_row(c, p, row, set, static_cast<uint4 *>(nullptr), list, tab);
+}
+
+__global__ void __launch_bounds__(kSelThreads, kValuesPerSm) sample_values_kernel(const SampleParams p)
+{
+    extern __shared__ __align__(16) uint4 smem[];
+    __shared__ Shared sh;
+    __shared__ ValueShared sv;
+    __shared__ float2 tab[1024];
+    const int row = (int)(blockIdx.x >> (31 - __clz(p.cluster))), tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    Ctx<false> c{Row<false>(p.z, row, p.ld, p.V)};
+    set_ctx(c, nullptr, 0, p.cluster, &sh);
+    const int C = c.C;
+    if (C > 1) cluster_arrive();
+    const Settings set(p, row);
+    if (set.bad) {
+        if (c.rank == 0 && tid == 0) put_bad(p, row);
+        if (C > 1) cluster_wait();
+        return;   // (every CTA of the row)
+    }
+    unsigned long long *list = reinterpret_cast<unsigned long long *>(smem);
+    if (!set.greedy)
+        for (int i = tid; i < 1024; i += kSelThreads) tab[i] = kExp2.v[i];
+    bool met = C == 1;   // every CTA of the row runs
+    if (!set.greedy && (set.k > 0 ? set.k <= kValuesTop : set.min_p > 0.f && !set.nucleus)) {
+        // few tokens are kept, as a rule: a list of the k largest, or of the ones that min-p keeps
+        uint32_t *scratch = reinterpret_cast<uint32_t *>(list);
+        float *gm = reinterpret_cast<float *>(list + kListCap);
+        int *hits = reinterpret_cast<int *>(gm + kMaxGroups * kSelThreads);
+        for (int i = tid; i < kBoundBins; i += kSelThreads) scratch[i] = 0u;
+        float hi = -INFINITY, lo = INFINITY;
+        const int mine = group_maxima(c, p.groups, gm, &hi, &lo);
+        uint32_t top;
+        uint32_t bound = group_bound(&sh, scratch, (set.k + C - 1) >> (31 - __clz(C)), hi, lo, &top, [&](auto f) {
+            for (int g = 0; g < mine; ++g) f(gm[g * kSelThreads + tid]);
+        });
+        if (C > 1) {
+            cluster_wait();
+            met = true;
+            if (tid < C) {
+                st_peer_u32(peer_addr(&sh.kmax[c.rank], tid), top);
+                st_peer_u32(peer_addr(&sh.bound[c.rank], tid), bound);
+            }
+            cluster_sync_all();
+            for (int k = 0; k < C; ++k) {
+                top = max(top, sh.kmax[k]);
+                bound = min(bound, sh.bound[k]);
+            }
+        }
+        if (top <= kKeyNone) {   // nothing can be drawn
+            if (c.rank == 0 && tid == 0) put_sample(p, row, -1, -INFINITY, 0);
+            return;
+        }
+        Scale s;
+        set_scale(s, key_float(top), set.T, p.V);
+        const uint32_t kminp = least_key(set, s, &sh);
+        if (set.k == 0) bound = max(kminp, kKeyNone + 1);
+        collect_groups(c, p.groups, gm, mine, hits, key_float(bound), list, kListCap);
+        bool ok;
+        const int n = push_list(c, list, &ok);
+        if (ok && (set.k > 0 || n <= kSmall)) {   // (the same in every CTA of the row)
+            if (c.rank != 0) return;   // (nobody reads this CTA's memory any more)
+            draw_list(p, row, set, s, list, n, kminp, tab, &sh);
+            return;
+        }
+        __syncthreads();
+    }
+    uint32_t *count = reinterpret_cast<uint32_t *>(smem), *got = count + kBins;
+    unsigned long long *table = list, *seg = table + kSteps;   // (after the counts)
+    if (!set.greedy)
+        for (int i = tid; i < kBins / 4; i += kSelThreads) smem[i] = make_uint4(0, 0, 0, 0);
+    if (tid == 0) {
+        sh.nlist = 0;
+        sv.border = kNoWay;
+        sv.of_k = 0;
+    }
+    __syncthreads();
+
+    // the row
+    uint32_t most = 0xff80ff80u, below = 0;
+    bool far = false;
+    {
+        constexpr int U = 4;
+        const auto add = [&](uint32_t step) { atomicAdd(count + (step >> 1), 1u << ((step & 1u) << 4)); };
+        for (int v0 = tid; v0 < c.n; v0 += U * kSelThreads) {
+            uint4 x[U];
+#pragma unroll
+            for (int k = 0; k < U; ++k)
+                x[k] = v0 + k * kSelThreads < c.n ? load_granule<false>(c.r, c.gb + v0 + k * kSelThreads)
+                                                  : make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u);
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                const uint4 q = x[k];
+                most = bf16x2_max(most, bf16x2_max(bf16x2_max(q.x, q.y), bf16x2_max(q.z, q.w)));
+                if (set.greedy || v0 + k * kSelThreads >= c.n) continue;
+                uint32_t step[4];
+                if (granule_steps(q, step)) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        add(step[j] & 0xffffu);
+                        add(step[j] >> 16);
+                    }
+                } else {
+                    uint32_t odd = odd_ones(q);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        if (!(odd & (1u << (2 * j)))) add(step[j] & 0xffffu);
+                        if (!(odd & (2u << (2 * j)))) add(step[j] >> 16);
+                    }
+                    for (; odd != 0; odd &= odd - 1u) {
+                        const uint32_t b = granule_elem16(q, __ffs(odd) - 1), mag = b & 0x7fffu;
+                        if (mag > 0x7f80u || b == 0xff80u) continue;   // NaN, -inf
+                        if (mag >= kFarMag) {
+                            if (b & 0x8000u) ++below;
+                            else far = true;
+                        } else {
+                            const uint32_t at = atomicAdd(&sh.nlist, 1u);
+                            if (at < kFewMax) sv.few[at] = __uint_as_float(b << 16);
+                        }
+                    }
+                }
+            }
+        }
+    }
+    {
+        const float m = fmaxf(fmaxf(bf16_lo(most), bf16_hi(most)), -INFINITY);
+        const uint32_t key = __reduce_max_sync(0xffffffffu, key_of(m));
+        below = __reduce_add_sync(0xffffffffu, below);
+        if (lane == 0) {
+            sh.ktop[warp] = key;
+            sh.part[warp] = (int)below;
+        }
+    }
+    far = __syncthreads_or(far);
+    const int nfew = (int)sh.nlist;
+    uint32_t kmax = __reduce_max_sync(0xffffffffu, sh.ktop[lane & (kSelWarps - 1)]);
+    if (!met) cluster_wait();
+    if (tid < C) {
+        st_peer_u32(peer_addr(&sh.kmax[c.rank], tid), kmax);
+        st_peer_u32(peer_addr(&sv.there[c.rank], tid), far ? kNoWay : (uint32_t)nfew);
+        uint32_t n = 0;
+        for (int w = 0; w < kSelWarps; ++w) n += (uint32_t)sh.part[w];
+        st_peer_u32(peer_addr(&sv.below[c.rank], tid), n);
+    }
+    if (!set.greedy) {
+        got = exchange_counts(c, count, got);
+        if (C == 1) __syncthreads();
+    } else if (C > 1) {
+        cluster_sync_all();
+    } else {
+        __syncthreads();
+    }
+    unsigned first = 0;   // the first CTA that has the largest logit
+    kmax = sh.kmax[0];
+    for (int k = 1; k < C; ++k)
+        if (sh.kmax[k] > kmax) {
+            kmax = sh.kmax[k];
+            first = k;
+        }
+    if (kmax <= kKeyNone) {   // nothing can be drawn
+        if (c.rank == 0 && tid == 0) put_sample(p, row, -1, -INFINITY, 0);
+        return;
+    }
+    if (set.greedy) {
+        if (c.rank != first) return;
+        Ctx<false> one = c;
+        one.C = 1;
+        one.rank = 0;
+        const int id = lowest_at(one, kmax);
+        if (tid == 0) put_sample(p, row, id, 0.f, 1);
+        return;
+    }
+    Scale s;
+    set_scale(s, key_float(kmax), set.T, p.V);
+    uint32_t all_below = 0, all_few = 0;
+    bool way = !s.hard;
+    for (int k = 0; k < C; ++k) {
+        way = way && sv.there[k] <= (uint32_t)kFewMax;
+        all_few += sv.there[k];
+        all_below += sv.below[k];
+    }
+    // (what lies below the steps has no weight: 45 octaves below the top and more)
+    way = way && (all_below == 0 || s.top + 64.f >= 31.4f * set.T);
+    const uint32_t kminp = least_key(set, s, &sh);
+    int last = kSteps - 1;   // min-p: the last step that is kept
+    if (kminp > 0) {
+        const uint32_t b = __float_as_uint(key_float(kminp)), up = b & 0x80000000u ? b >> 16 : (b + 0xffffu) >> 16;
+        const int mag = (int)(up & 0x7fffu);   // (up: the least bf16 value from there on)
+        if (mag < kLeastMag) last = kSteps / 2 - 1;
+        else if (mag < kFarMag) last = step_of(up);
+        else way = way && all_below == 0;   // (it is -2^6 or below: larger than the top it cannot be)
+    }
+    if (!way) {   // (the same in every CTA of the row)
+        __syncthreads();
+        sample_row_again(c, p, row, set, reinterpret_cast<unsigned long long *>(smem), tab);
+        return;
+    }
+
+    // the listed ones' masses: of all, and of what min-p keeps
+    if (32 * warp < nfew) {
+        const bool on = tid < nfew;
+        const float x = on ? sv.few[tid] : 0.f;
+        const unsigned long long w = on ? weight(x, s, tab) : 0ull;
+        const bool in = on && key_of(x) >= kminp;
+        const unsigned long long a = warp_sum_u64(w), b = warp_sum_u64(in ? w : 0ull);
+        const uint32_t n = (uint32_t)__popc(__ballot_sync(0xffffffffu, in));
+        if (lane == 0) {
+            sv.few_mass[warp] = a;
+            sv.few_kept[warp] = b;
+            sv.few_n[warp] = n;
+        }
+    }
+    // a run of steps per CTA, of it a run per thread: the masses of the CTAs' tokens there (up to `last`, the rest apart)
+    const int nw = kBins / C, per = (nw + kSelThreads - 1) / kSelThreads;   // words
+    const int w0 = min(nw, tid * per), w1 = min(nw, w0 + per);
+    const int base = (int)c.rank * nw, b0 = 2 * (base + w0), b1 = 2 * (base + w1);
+    const auto counted = [&](int k, int b) { return (got[k * nw + (b >> 1) - base] >> ((b & 1) << 4)) & 0xffffu; };
+    const auto in_step = [&](int b) {
+        uint32_t t = 0;
+        for (int k = 0; k < C; ++k) t += counted(k, b);
+        return t;
+    };
+    unsigned long long acc[kRowMaxCluster], mine = 0;
+    uint32_t n = 0, tokens = 0;
+#pragma unroll
+    for (int k = 0; k < kRowMaxCluster; ++k) acc[k] = 0;
+    for (int w = w0; w < w1; ++w) {
+        const int b = 2 * (base + w);
+        uint32_t any = 0;
+        for (int k = 0; k < C; ++k) any |= got[k * nw + w];
+        if (any == 0) continue;
+        const Weights2 q = weights2(pack2(step_value(b), step_value(b + 1)), s, tab);
+        // (steps above the top are empty)
+        const unsigned long long wa = q.in[0] ? whole_weight(q.i1[0], q.i2[0], s) : 0ull;
+        const unsigned long long wb = q.in[1] ? whole_weight(q.i1[1], q.i2[1], s) : 0ull;
+        const bool ina = b <= last, inb = b + 1 <= last;
+#pragma unroll
+        for (int k = 0; k < kRowMaxCluster; ++k) {
+            if (k >= C) break;
+            const uint32_t x = got[k * nw + w], na = x & 0xffffu, nb = x >> 16;
+            const unsigned long long ma = na * wa, mb = nb * wb;
+            tokens += na + nb;
+            n += (ina ? na : 0u) + (inb ? nb : 0u);
+            acc[k] += (ina ? ma : 0ull) + (inb ? mb : 0ull);
+            mine += ma + mb;
+        }
+    }
+    const auto drop = [&]() {
+        n = 0;
+#pragma unroll
+        for (int k = 0; k < kRowMaxCluster; ++k) acc[k] = 0;
+    };
+    bool cut = set.nucleus;
+    uint32_t all_tokens = 0;
+    if (set.nucleus || set.k > 0) {
+        unsigned long long total, total_n = 0;
+        unsigned long long run = block_scan_u64(mine, &sh, &total);
+        uint32_t run_n = 0;
+        if (set.k > 0) run_n = (uint32_t)block_scan_u64(tokens, &sh, &total_n);
+        unsigned long long few = 0;
+        for (int w = 0; 32 * w < nfew; ++w) few += sv.few_mass[w];
+        if (tid < C) st_peer_u32(peer_addr(&sv.counted[c.rank], tid), (uint32_t)total_n);
+        const unsigned long long *slot = cluster_gather(c, total, few);
+        few = slot_sum(slot + kRowMaxCluster, C);
+        unsigned long long Z = slot_sum(slot, C) + few;
+        for (unsigned k = 0; k < c.rank; ++k) {
+            run += slot[k];
+            run_n += sv.counted[k];
+        }
+        if (b0 >= kSteps / 2) {   // (the listed ones are between the positive and the negative steps)
+            run += few;
+            run_n += all_few;
+        }
+        uint32_t most_n = 0xffffffffu;
+        if (set.k > 0) {
+            all_tokens = all_few;
+            for (int k = 0; k < C; ++k) all_tokens += sv.counted[k];
+            if ((uint32_t)set.k < all_tokens) {
+                most_n = (uint32_t)set.k;
+                cut = true;
+            }
+        }
+        // the thread's steps in order, while `more` says so: more(step, tokens before, mass before, tokens, weight)
+        const auto walk = [&](auto more) {
+            unsigned long long m = run;
+            uint32_t before = run_n;
+            for (int b = b0; b < b1; ++b) {
+                const uint32_t t = in_step(b);
+                if (t == 0) continue;
+                const unsigned long long w = weight(step_value(b), s, tab);
+                if (!more(b, before, m, t, w)) return;
+                m += t * w;
+                before += t;
+            }
+        };
+        unsigned long long target = ~0ull;
+        if (set.nucleus) {
+            if (most_n != 0xffffffffu) {
+                if (run_n < most_n && run_n + tokens >= most_n)   // (one thread)
+                    walk([&](int, uint32_t before, unsigned long long m, uint32_t t, unsigned long long w) {
+                        if (before + t < most_n) return true;
+                        m += (most_n - before) * w;
+                        for (int k = 0; k < C; ++k) st_peer_u64(peer_addr(&sv.of_k, k), m);
+                        return false;
+                    });
+                if (C > 1) cluster_sync_all();
+                else __syncthreads();
+                Z = sv.of_k;   // (0: the k-th largest is a listed one)
+            }
+            target = share_ceil(set.top_p, Z);
+        }
+        if (run >= target || run_n >= most_n) {
+            drop();
+        } else if (cut && (run + mine >= target || (most_n != 0xffffffffu && run_n + tokens >= most_n))) {   // (one thread)
+            drop();
+            walk([&](int b, uint32_t before, unsigned long long m, uint32_t t, unsigned long long w) {
+                uint32_t left = min(t, most_n - before);
+                bool border = most_n != 0xffffffffu && before + t >= most_n;
+                if (target - m <= left * w) {
+                    border = true;
+                    left = (uint32_t)((target - m + w - 1ull) / w);
+                }
+                if (b <= last) n += left;
+                for (int k = 0; k < C; ++k) {
+                    const uint32_t there = counted(k, b), kept = min(there, left);
+                    left -= kept;
+#pragma unroll
+                    for (int q = 0; q < kRowMaxCluster; ++q)
+                        if (q == k && b <= last) acc[q] += kept * w;
+                    if (border) {
+                        st_peer_u32(peer_addr(&sv.border, k), (uint32_t)b);
+                        st_peer_u32(peer_addr(&sv.ties, k), there);
+                        st_peer_u32(peer_addr(&sv.ties_kept, k), kept);
+                    }
+                }
+                return !border;
+            });
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < kRowMaxCluster; ++k) {
+        if (k >= C) break;
+        const unsigned long long a = warp_sum_u64(acc[k]);
+        if (lane == 0) sv.part[warp][k] = a;
+    }
+    n = __reduce_add_sync(0xffffffffu, n);
+    if (lane == 0) sv.part_n[warp] = n;
+    __syncthreads();
+    if (tid < C * C) {
+        const int k = tid & (C - 1), to = tid >> (31 - __clz(C));
+        unsigned long long a = 0;
+        for (int w = 0; w < kSelWarps; ++w) a += sv.part[w][k];
+        st_peer_u64(peer_addr(&sv.mass[c.rank][k], to), a);
+    }
+    if (tid < C) {
+        unsigned long long kept = 0;
+        uint32_t kept_n = 0;
+        n = 0;
+        for (int w = 0; w < kSelWarps; ++w) n += sv.part_n[w];
+        for (int w = 0; 32 * w < nfew; ++w) {
+            kept += sv.few_kept[w];
+            kept_n += sv.few_n[w];
+        }
+        st_peer_u32(peer_addr(&sv.n[c.rank], tid), n);
+        st_peer_u32(peer_addr(&sv.listed_n[c.rank], tid), kept_n);
+        st_peer_u64(peer_addr(&sv.listed[c.rank], tid), kept);
+    }
+    if (C > 1) cluster_sync_all();
+    else __syncthreads();
+    const int border = (int)sv.border;
+    if (cut && border < 0) {   // (the same in every CTA of the row)
+        sample_row_again(c, p, row, set, reinterpret_cast<unsigned long long *>(smem), tab);
+        return;
+    }
+    const bool listed = !cut || border >= kSteps / 2;
+    unsigned long long total = 0, before = 0, here = 0;
+    uint32_t kept_n = cut || kminp > 0 ? 0u : all_below;
+    for (int k = 0; k < C; ++k) {
+        unsigned long long a = listed ? sv.listed[k] : 0ull;
+        for (int q = 0; q < C; ++q) a += sv.mass[q][k];
+        if (k < (int)c.rank) before += a;
+        if (k == (int)c.rank) here = a;
+        total += a;
+        kept_n += sv.n[k] + (listed ? sv.listed_n[k] : 0u);
+    }
+    if (set.k > 0) kept_n = min(kept_n, (uint32_t)set.k);
+    const unsigned long long target = share_floor(set.u, total);
+    if (target < before || target - before >= here) return;   // another CTA has it
+
+    // this CTA alone from here on
+    Ctx<false> one = c;
+    one.C = 1;
+    one.rank = 0;
+    TableMass mass{table, s, tab, kminp, listed, -1, INT_MIN, 0ull};
+    if (cut && border <= last && sv.ties_kept < sv.ties) {
+        mass.tie = border;
+        mass.tie_w = weight(step_value(border), s, tab);
+        if (sv.ties_kept > 0) {
+            find_in_share(one, (unsigned long long)sv.ties_kept - 1ull, TieCount{__float_as_uint(step_value(border)) >> 16},
+                          seg, [&](int i, uint32_t) { sh.found_idx = i; });
+            __syncthreads();
+            mass.idx = sh.found_idx;
+        }
+    }
+    const int end = min(last, cut ? border : kSteps - 1);
+    const int begin = fabsf(s.top) >= step_value(kSteps / 2 - 1) ? step_of(__float_as_uint(s.top) >> 16) : kSteps / 2 - 1;
+    for (int b = 2 * tid; b < kSteps; b += 2 * kSelThreads) {
+        ulonglong2 w = make_ulonglong2(0ull, 0ull);
+        if (b <= end && b + 1 >= begin) {
+            const Weights2 q = weights2(pack2(step_value(b), step_value(b + 1)), s, tab);
+            if (q.in[0] && b != mass.tie) w.x = whole_weight(q.i1[0], q.i2[0], s);
+            if (q.in[1] && b + 1 <= end && b + 1 != mass.tie) w.y = whole_weight(q.i1[1], q.i2[1], s);
+        }
+        *reinterpret_cast<ulonglong2 *>(table + b) = w;
+    }
+    __syncthreads();
+    find_in_share(one, target - before, mass, seg, [&](int id, uint32_t key) {
+        put_sample(p, row, id, log_share(key_float(key), set.T, s, total), (long long)kept_n);
+    });
+}
+
+constexpr size_t kValuesSmem = std::max<size_t>((kSteps + kSegs) * 8, kListCap * 12 + kMaxGroups * kSelThreads * 4);
+
+template <bool F32>
 sats_status sample(const void *logits, int64_t ld, int B, int V, const float *temperature, const int32_t *top_k,
                    const float *top_p, const float *min_p, const float *u, int32_t *ids, float *logprob,
                    int32_t *n_kept, int32_t *dev_status, void *stream)
@@ -867,6 +1544,13 @@ sats_status sample(const void *logits, int64_t ld, int B, int V, const float *te
     p.z = logits; p.ld = ld; p.B = B; p.V = V; p.temperature = temperature; p.top_k = top_k; p.top_p = top_p;
     p.min_p = min_p; p.u = u; p.ids = ids; p.logprob = logprob; p.n_kept = n_kept; p.status = dev_status;
     const int64_t bytes = (int64_t)V * RowElem<F32>::kBytes;
+    p.cluster = logits_cluster(B, bytes, 0, kValuesShare);
+    if (!F32 && V >= kValuesFrom && V / p.cluster < kValuesTo) {
+        p.groups = plan_groups(bytes, p.cluster, kMaxGroups);
+        const cudaError_t e = launch_clusters<sample_values_kernel>((int64_t)B * p.cluster, kSelThreads, kValuesSmem, kValuesSmem,
+                                                                    p.cluster, static_cast<cudaStream_t>(stream), p);
+        return e == cudaSuccess ? SATS_OK : cuda_fail(e, "sampling kernel launch");
+    }
     p.cluster = logits_cluster(B, bytes, 0, kShare);
     const size_t share = (size_t)((bytes + 32 + p.cluster - 1) / p.cluster) + 32;
     p.cached = (int)((share < kMaxCache ? share : kMaxCache) / 16);
