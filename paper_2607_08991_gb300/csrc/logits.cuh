@@ -679,7 +679,7 @@ int logits_cluster(int rows, int64_t row_bytes, int want, size_t share)
 {
     int C = 1;
     while (C < kRowMaxCluster && ((share && row_bytes > (int64_t)C * (int64_t)share) ||
-                                  (((int64_t)rows * C < 2 * kSms || want > C * (kSmall * 3 / 4)) &&
+                                  (((int64_t)rows * C < 2 * kSms || (want > C * (kSmall * 3 / 4) && rows < kSms)) &&
                                    row_bytes >= 2 * (int64_t)C * kSelThreads * 16)))
         C *= 2;
     return C;

@@ -13,6 +13,7 @@ namespace sats {
 namespace {
 
 constexpr size_t kMaxSmem = (size_t)kListCap * 12 + (size_t)kMaxGroups * kSelThreads * 4;
+static_assert(kListCap * 8 <= kMaxGroups * kSelThreads * 4 && kListCap >= 2 * 512, "where the list's entries are placed");
 
 struct TopParams {
     const void *z;
@@ -24,6 +25,77 @@ struct TopParams {
     int cap;          // entries of the list
     Groups groups;
 };
+
+// Puts the n entries of the list (the largest is `top`) where they belong in descending order, without sorting:
+// equal steps of the logit give each entry a run of places, the entries of its step (a few, as a rule) its place there.
+// False where a step has too many.  other: room for the list; count: 2 kPlaceSteps words behind it.
+constexpr int kPlaceSteps = 512, kPlaceMost = 128;
+__device__ __forceinline__ bool put_by_steps(const unsigned long long *list, int n, uint32_t top,
+                                             unsigned long long *other, uint32_t *count, Shared *sh, float *values,
+                                             int32_t *idx, int K)
+{
+    constexpr int kPer = kListCap / kSelThreads, kRun = kPlaceSteps / kSelThreads;
+    const int tid = threadIdx.x;
+    __syncthreads();
+    uint32_t low = 0xffffffffu;
+    for (int i = tid; i < n; i += kSelThreads) low = min(low, (uint32_t)(list[i] >> 32));
+    low = __reduce_min_sync(0xffffffffu, low);
+    if ((tid & 31) == 0) sh->klow[tid >> 5] = low;
+    for (int i = tid; i < kPlaceSteps; i += kSelThreads) count[i] = 0u;
+    __syncthreads();
+    low = __reduce_min_sync(0xffffffffu, sh->klow[tid & (kSelWarps - 1)]);
+    const float ft = key_float(top), range = ft - key_float(low);
+    if (!(range > 0.f && range < INFINITY)) return false;
+    const float scale = (float)kPlaceSteps / range;
+    if (scale == INFINITY) return false;
+    uint32_t *first = count + kPlaceSteps;
+    const auto step_of = [&](unsigned long long e) {
+        return (int)fminf((ft - key_float((uint32_t)(e >> 32))) * scale, (float)(kPlaceSteps - 1));
+    };
+    uint32_t at[kPer];
+#pragma unroll
+    for (int k = 0; k < kPer; ++k)
+        if (tid + k * kSelThreads < n) at[k] = atomicAdd(count + step_of(list[tid + k * kSelThreads]), 1u);
+    __syncthreads();
+    uint32_t run[kRun], sum = 0, most = 0;
+#pragma unroll
+    for (int k = 0; k < kRun; ++k) {
+        run[k] = count[tid * kRun + k];
+        most = max(most, run[k]);
+        sum += run[k];
+    }
+    if (__syncthreads_or(most > (uint32_t)kPlaceMost)) return false;
+    unsigned long long total;
+    uint32_t from = (uint32_t)block_scan_u64(sum, sh, &total);
+#pragma unroll
+    for (int k = 0; k < kRun; ++k) {
+        first[tid * kRun + k] = from;
+        from += run[k];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kPer; ++k)
+        if (tid + k * kSelThreads < n) {
+            const unsigned long long e = list[tid + k * kSelThreads];
+            other[first[step_of(e)] + at[k]] = e;
+        }
+    __syncthreads();
+    for (int i = tid; i < n; i += kSelThreads) {   // (neighbours have the same step, or nearly)
+        const unsigned long long e = other[i];
+        const int s = step_of(e), f = (int)first[s], m = (int)count[s];
+        int place = f;
+        for (int j = f; j < f + m; ++j) place += other[j] > e;
+        if (place < K) {
+            values[place] = key_float((uint32_t)(e >> 32));
+            idx[place] = (int32_t)~(uint32_t)e;
+        }
+    }
+    for (int i = n + tid; i < K; i += kSelThreads) {
+        values[i] = -INFINITY;
+        idx[i] = -1;
+    }
+    return true;
+}
 
 // The row streams through registers once; only the groups whose maximum reaches the bound are read again, from the L2.
 template <bool F32>
@@ -77,7 +149,10 @@ __global__ void __launch_bounds__(kSelThreads, kSelPerSm) top_kernel(const TopPa
                 for (int q = 1; q < C; ++q) st_peer_u64(peer_addr(own + at, (c.rank + q) & (C - 1)), e.e);
             }
         }
-        if (tid < C) st_peer_u32(peer_addr(&sh.cnt[c.rank], tid), fits ? (uint32_t)here : 0xffffffffu);
+        if (tid < C) {
+            st_peer_u32(peer_addr(&sh.cnt[c.rank], tid), fits ? (uint32_t)here : 0xffffffffu);
+            st_peer_u32(peer_addr(&sh.above[c.rank], tid), (uint32_t)here);
+        }
         if (C > 1) cluster_sync_all();
         else __syncthreads();
         bool all = true;
@@ -115,13 +190,33 @@ __global__ void __launch_bounds__(kSelThreads, kSelPerSm) top_kernel(const TopPa
         }
     }
     // more candidates than that: one list of all of them, or of exactly the K largest
-    bool ok;
-    int n = gather_list(c, list, bound, Cut{kKeyNone, INT_MIN}, &ok);
-    if (!ok) {   // (the same in every CTA of the row)
-        const Cut cut = cut_count(c, top, p.K);
-        n = gather_list(c, list, max(cut.key, kKeyNone + 1), cut, &ok);   // at most K
+    bool there = true;
+    int n = 0, before = 0;
+    for (int k = 0; k < c.C; ++k) {
+        if (k == (int)c.rank) before = n;
+        there = there && sh.above[k] <= (uint32_t)(c.cap / c.C);
+        n += (int)sh.above[k];
+    }
+    if (there) {   // (the same in every CTA of the row)
+        unsigned long long *own = list + c.rank * (c.cap / c.C);
+        if (c.C > 1) {
+            // the first CTA's list behind its own entries: the others' places there are free
+            const int mine = (int)sh.nlist;
+            if (c.rank != 0)
+                for (int i = tid; i < mine; i += kSelThreads) st_peer_u64(peer_addr(list + before + i, 0), own[i]);
+            cluster_sync_all();
+        }
+    } else {
+        bool ok;
+        n = gather_list(c, list, bound, Cut{kKeyNone, INT_MIN}, &ok);
+        if (!ok) {   // (the same in every CTA of the row)
+            const Cut cut = cut_count(c, top, p.K);
+            n = gather_list(c, list, max(cut.key, kKeyNone + 1), cut, &ok);   // at most K
+        }
     }
     if (c.rank != 0) return;   // (nobody reads this CTA's memory any more)
+    unsigned long long *other = reinterpret_cast<unsigned long long *>(gm);
+    if (put_by_steps(list, n, top, other, reinterpret_cast<uint32_t *>(other + p.cap), &sh, values, idx, p.K)) return;
     sort_list(list, n);
     for (int i = threadIdx.x; i < p.K; i += kSelThreads) {
         const unsigned long long e = i < n ? list[i] : 0ull;
