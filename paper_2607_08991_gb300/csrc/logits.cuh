@@ -552,6 +552,29 @@ __device__ __forceinline__ uint32_t group_bound(Shared *sh, uint32_t *scratch, i
     return border < kBoundBins ? klo : kKeyNone + 1;
 }
 
+// The same with every element a group: where the granules are too few for groups of them to give a close bound.
+template <bool F32>
+__device__ __noinline__ uint32_t element_bound(const Ctx<F32> &c, uint32_t *scratch, int R, uint32_t *top)
+{
+    constexpr int E = RowElem<F32>::kPer;
+    const auto each = [&](auto f) {
+        for (int v = threadIdx.x; v < c.n; v += kSelThreads) {
+            float x[E];
+            granule_floats<F32>(c.get(v), x);
+#pragma unroll
+            for (int j = 0; j < E; ++j) f(x[j]);
+        }
+    };
+    float hi = -INFINITY, lo = INFINITY;
+    each([&](float x) {
+        hi = fmaxf(hi, x);
+        if (x > -INFINITY) lo = fminf(lo, x);
+    });
+    return group_bound(c.sh, scratch, R, hi, lo, top, each);
+}
+// (With fewer groups than R there is no bound at all, with not many more a loose one; a short row the list takes whole.)
+__host__ __device__ inline bool few_groups(int groups, int elements, int R) { return groups < 2 * R && elements > 512; }
+
 // ------------------------------------------------------------------ groups of a row that streams through registers
 constexpr int kTurn = 8;               // granules in flight per thread
 constexpr int kMaxGroups = 16;         // groups of a thread, at most

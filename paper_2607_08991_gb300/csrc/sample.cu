@@ -307,11 +307,17 @@ __device__ void load_row(Ctx<F32> &c, uint4 *cache, int want, uint32_t *scratch,
         hi = fmaxf(hi, g[k]);
         if (want > 0 && g[k] > -INFINITY) lo = fminf(lo, g[k]);
     }
-    uint32_t top;
-    uint32_t low = group_bound(sh, scratch, (want + c.C - 1) >> (31 - __clz(c.C)), hi, lo, &top, [&](auto f) {
+    uint32_t top, low;
+    const int R = (want + c.C - 1) >> (31 - __clz(c.C));
+    if (few_groups(min(c.n, kSelThreads) * NG, min(c.n, 1 << 20) * RowElem<F32>::kPer, R)) {
+        __syncthreads();   // (others' granules)
+        low = element_bound(c, scratch, R, &top);
+    } else {
+        low = group_bound(sh, scratch, R, hi, lo, &top, [&](auto f) {
 #pragma unroll
-        for (int k = 0; k < NG; ++k) f(g[k]);
-    });
+            for (int k = 0; k < NG; ++k) f(g[k]);
+        });
+    }
     if (c.C > 1) {
         cluster_wait();
         if (tid < c.C) {

@@ -1,4 +1,6 @@
 // top_logits.cu -- the K largest logits of each row (sats_top_logits).
+#include <algorithm>
+
 #include "internal.h"
 #include "rows.cuh"
 
@@ -98,7 +100,8 @@ __device__ __forceinline__ bool put_by_steps(const unsigned long long *list, int
 }
 
 // The row streams through registers once; only the groups whose maximum reaches the bound are read again, from the L2.
-template <bool F32>
+// FEW: few_groups.
+template <bool F32, bool FEW>
 __global__ void __launch_bounds__(kSelThreads, kSelPerSm) top_kernel(const TopParams p)
 {
     extern __shared__ __align__(16) uint4 smem[];
@@ -115,9 +118,14 @@ __global__ void __launch_bounds__(kSelThreads, kSelPerSm) top_kernel(const TopPa
     float hi = -INFINITY, lo = INFINITY;
     const int mine = group_maxima(c, p.groups, gm, &hi, &lo);
     uint32_t top;
-    uint32_t bound = group_bound(&sh, scratch, (p.K + c.C - 1) >> (31 - __clz(c.C)), hi, lo, &top, [&](auto f) {
-        for (int g = 0; g < mine; ++g) f(gm[g * kSelThreads + tid]);
-    });
+    const int R = (p.K + c.C - 1) >> (31 - __clz(c.C));
+    uint32_t bound;
+    if constexpr (FEW)
+        bound = element_bound(c, scratch, R, &top);
+    else
+        bound = group_bound(&sh, scratch, R, hi, lo, &top, [&](auto f) {
+            for (int g = 0; g < mine; ++g) f(gm[g * kSelThreads + tid]);
+        });
     if (c.C > 1) {
         cluster_wait();
         if (tid < c.C) {
@@ -244,8 +252,13 @@ sats_status top_logits(const void *logits, int64_t ld, int T, int V, int K, floa
     while (groups < kMaxGroups && (int64_t)groups * kSelThreads * p.cluster < 64 * (int64_t)K) groups *= 2;
     p.groups = plan_groups(bytes, p.cluster, groups);
     const size_t smem = (size_t)p.cap * 12 + (size_t)kMaxGroups * kSelThreads * 4;
-    const cudaError_t e = launch_clusters<top_kernel<F32>>((int64_t)T * p.cluster, kSelThreads, smem, kMaxSmem, p.cluster,
-                                                           static_cast<cudaStream_t>(stream), p);
+    const int64_t ctas = (int64_t)T * p.cluster;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const int granules = (int)std::min<int64_t>((bytes + 15) / 16 / p.cluster, 1 << 20);   // (a group has one at least)
+    const cudaError_t e =
+        few_groups(granules, granules * RowElem<F32>::kPer, (K + p.cluster - 1) / p.cluster)
+            ? launch_clusters<top_kernel<F32, true>>(ctas, kSelThreads, smem, kMaxSmem, p.cluster, st, p)
+            : launch_clusters<top_kernel<F32, false>>(ctas, kSelThreads, smem, kMaxSmem, p.cluster, st, p);
     return e == cudaSuccess ? SATS_OK : cuda_fail(e, "top-logits kernel launch");
 }
 
