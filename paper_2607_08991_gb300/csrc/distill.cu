@@ -24,8 +24,13 @@ constexpr int kMaxEntries = 1024;             // teacher entries of a row
 constexpr float kMinTau = 0x1p-10f;           // to its inverse: a log-sum-exp at tau keeps some of its bits
 constexpr size_t kMaxCache = 180 * 1024;      // of a row's share in shared memory
 constexpr size_t kMaxSmem = kSmemPerCta - 2 * 1024;   // dynamic: a row's share, two tables of entries
-constexpr size_t kStepShare = 72 * 1024;      // of a row per CTA, where the cluster allows: several CTAs to an SM
-constexpr int kLossThreads = 512, kGradThreads = 256, kStepThreads = 256, kStepPerSm = 3;
+// Threads, CTAs to an SM and the share of a row that a CTA of the one-pass kernel has on chip (where the cluster allows),
+// 4096 rows of 128256 bf16 logits before its clusters stayed for many rows (us): 256 x 3, 72 KB 450; 256 x 4, 72 KB 455;
+// 256 x 4, 40 KB 563; 512 x 2, 72 KB 581; 128 x 8, 40 KB 460.  The backward pass with 256 x 4 takes 197 us where 512 x 2
+// took 273 (1000 rows of 151936 fp32 logits), the loss 347 where it took 371 (8192 rows of 151936 bf16 ones).  Powers of
+// two: sums over warps halve their number.
+constexpr size_t kStepShare = 72 * 1024;
+constexpr int kLossThreads = 256, kGradThreads = 256, kStepThreads = 256, kStepPerSm = 3;
 
 struct DistillParams {
     const void *z;
@@ -457,9 +462,14 @@ __device__ __forceinline__ void stream_sum(RunSum<NT> &sum, const Row<F32> &r, i
         for (int k = 0; k < 4; ++k) x[k] = load_granule<F32>(r, gb + v + k * TH);
         run_add<F32, NT, 4>(sum, x, c);
     }
-    for (; v < n; v += TH) {
-        const uint4 one[1] = {load_granule<F32>(r, gb + v)};
-        run_add<F32, NT, 1>(sum, one, c);
+    if (v < n) {   // (the last up to three, in flight together as well)
+        uint4 x[3];
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            const uint32_t none = F32 ? 0xff800000u : 0xff80ff80u;
+            x[k] = v + k * TH < n ? load_granule<F32>(r, gb + v + k * TH) : make_uint4(none, none, none, none);
+        }
+        run_add<F32, NT, 3>(sum, x, c);
     }
 }
 
@@ -505,11 +515,13 @@ __device__ __forceinline__ int2 whole_of(const Row<F32> &r, int2 run)
 }
 
 // ------------------------------------------------------------------ the loss
-// One row per cluster, read once.
-template <bool F32, int NT>
-__global__ void __launch_bounds__(kLossThreads, 2) distill_loss_kernel(const DistillParams p)
+// One row per cluster, read once: bounded by HBM.  8192 rows of 151936 bf16 logits take 350 us, 7.1 TB/s (a copy reaches
+// 6.78, of which it writes half); 37 rows of 128256 fp32 ones with two temperatures 12 us, most of it a launch and two barriers of the cluster.
+// With 50 entries at tau 2 (two exponentials an element) the 8192 rows take 401 us.
+template <bool F32, int NT, int TH>
+__global__ void __launch_bounds__(TH, 1024 / TH) distill_loss_kernel(const DistillParams p)
 {
-    constexpr int TH = kLossThreads, WARPS = TH / 32;
+    constexpr int WARPS = TH / 32;
     extern __shared__ __align__(16) uint4 smem[];
     __shared__ float4 part[WARPS];
     __shared__ float wsum[WARPS][4], wkd[WARPS];
@@ -572,11 +584,12 @@ __global__ void __launch_bounds__(kLossThreads, 2) distill_loss_kernel(const Dis
 
 // ------------------------------------------------------------------ the gradient from the log-sum-exps
 // p.cluster CTAs per row that need nothing of one another; the row streams through registers, four granules in
-// flight per thread.
-template <bool F32, int NT>
-__global__ void __launch_bounds__(kGradThreads, 4) distill_grad_kernel(const DistillParams p)
+// flight per thread.  Bounded by HBM: 1000 rows of 151936 fp32 logits, read and written, 197 us or 6.2 TB/s (one granule
+// in flight: 273 us); 221 us where the gradient's rows lie on other 16-byte boundaries (element by element 367).
+template <bool F32, int NT, int TH>
+__global__ void __launch_bounds__(TH, 1024 / TH) distill_grad_kernel(const DistillParams p)
 {
-    constexpr int TH = kGradThreads, WARPS = TH / 32, E = RowElem<F32>::kPer, B = RowElem<F32>::kBytes;
+    constexpr int WARPS = TH / 32, E = RowElem<F32>::kPer, B = RowElem<F32>::kBytes;
     extern __shared__ __align__(16) uint4 smem[];
     __shared__ float4 part[WARPS];
     const int tid = threadIdx.x;
@@ -616,9 +629,6 @@ __global__ void __launch_bounds__(kGradThreads, 4) distill_grad_kernel(const Dis
     grad.a0 = grad.A == 0.f ? -INFINITY : -p.lse_in[2 * (size_t)row + (tau_first ? 0 : 1)];
     grad.a1 = grad.B == 0.f ? -INFINITY : -p.lse_in[2 * (size_t)row + 1];
 
-    const auto value = [&](int v) {
-        return ignored ? make_uint4(0, 0, 0, 0) : grad.template granule<F32>(load_granule<F32>(r, run.x + v));
-    };
     if (same) {
         constexpr int U = 4;
         int v = tid;
@@ -630,7 +640,17 @@ __global__ void __launch_bounds__(kGradThreads, 4) distill_grad_kernel(const Dis
 #pragma unroll
                 for (int k = 0; k < U; ++k) put_granule<F32>(out, r, run.x + v + k * TH, grad.template granule<F32>(x[k]));
             }
-        for (; v < run.y; v += TH) put_granule<F32>(out, r, run.x + v, value(v));
+        if (!ignored) {   // (the last up to three, in flight together as well)
+            uint4 x[U - 1];
+#pragma unroll
+            for (int k = 0; k < U - 1; ++k)
+                if (v + k * TH < run.y) x[k] = load_granule<F32>(r, run.x + v + k * TH);
+#pragma unroll
+            for (int k = 0; k < U - 1; ++k)
+                if (v + k * TH < run.y) put_granule<F32>(out, r, run.x + v + k * TH, grad.template granule<F32>(x[k]));
+        } else {
+            for (; v < run.y; v += TH) put_granule<F32>(out, r, run.x + v, make_uint4(0, 0, 0, 0));
+        }
     } else {
         constexpr int U = 4;
         const int wper = (run.y + WARPS - 1) / WARPS, w0 = min(run.y, (tid >> 5) * wper), w1 = min(run.y, w0 + wper);
@@ -669,12 +689,16 @@ __global__ void __launch_bounds__(kGradThreads, 4) distill_grad_kernel(const Dis
 // nobody else touches it, so the next row arrives while this one is stored, without a barrier.  The CTAs of a row
 // exchange their sums by stores that count on an mbarrier of the receiver (a cluster barrier would wait for the
 // gradient's stores as well); a wait that gives up leaves NaN and says so in the status word.
+// 4096 rows of 128256 bf16 logits with 64 entries, read once and written once, take 375 us, 5.6 TB/s; one row per cluster
+// and launch took 450.  Without entries it is 335 us, with 1000 of them 640, at tau 2 (two exponentials) 464: what bounds
+// it is the issue of instructions (two exponentials an element in the sums and the gradient each, at 24 warps to an SM)
+// and the latency of the chain sums - exchange - gradient in each row, which two other CTAs on the SM cover in part.
 // SHIFT: some rows of the gradient lie on other 16-byte boundaries than the logits' rows; a warp then has a run of
 // consecutive granules (as Shifted wants them) and not every eighth run of 32, which is 6 % faster.
-template <bool F32, int NT, bool SHIFT>
-__global__ void __launch_bounds__(kStepThreads, kStepPerSm) distill_step_kernel(const DistillParams p)
+template <bool F32, int NT, bool SHIFT, int TH>
+__global__ void __launch_bounds__(TH, kStepPerSm * kStepThreads / TH) distill_step_kernel(const DistillParams p)
 {
-    constexpr int TH = kStepThreads, WARPS = TH / 32, E = RowElem<F32>::kPer, B = RowElem<F32>::kBytes;
+    constexpr int WARPS = TH / 32, E = RowElem<F32>::kPer, B = RowElem<F32>::kBytes;
     constexpr int kLate = 4;                 // of a thread's granules that may still be on their way when a row begins
     constexpr int kBatch = F32 ? 4 : 2;      // granules summed together
     extern __shared__ __align__(16) uint4 row_smem[];
@@ -918,10 +942,10 @@ size_t al16(size_t v) { return (v + 15) & ~(size_t)15; }
 
 // CTAs of a row: one where the rows alone fill the GPU with `fill` CTAs to an SM, more where they do not, as long as each
 // still has a granule for each of `threads`; and as many as it takes for the share that stays on chip to leave room for
-// other CTAs on the SM.  Measured with 1 / 2 / 4 / 8 CTAs a row (us; loss: 151936 bf16 logits, 2 CTAs to an SM; gradient:
-// 151936 fp32 ones, 4 to an SM): loss of 76 rows 14.8 / 12.0 / 11.4 / 16.0, of 304 rows 20.7 / 25.0 / 31.8 / 45.7, of
-// 1216 rows 65 / 83 / 110 / 160 (a cluster costs about a microsecond of every wave); gradient of 76 rows 46 / 30 / 26 /
-// 22, of 304 rows 72 / 66 / 68 / 71, of 1216 rows 235 / 234 / 238 / 256.
+// other CTAs on the SM.  Measured with 1 / 2 / 4 / 8 CTAs a row (us; 151936 bf16 or fp32 logits): loss, as it was with 512
+// threads, of 76 rows 14.8 / 12.0 / 11.4 / 16.0, of 304 rows 20.7 / 25.0 / 31.8 / 45.7, of 1216 rows 65 / 83 / 110 / 160 (a
+// cluster costs about a microsecond of every wave); gradient of 76 rows 46 / 30 / 26 / 22, of 304 rows 72 / 66 / 68 / 71, of
+// 1216 rows 235 / 234 / 238 / 256.
 int row_cluster(int T, int64_t row_bytes, size_t share, int fill, int threads)
 {
     int C = 1;
@@ -936,18 +960,34 @@ static_assert((kLossThreads & (kLossThreads - 1)) == 0 && (kGradThreads & (kGrad
                   kStepThreads >= 64,
               "the sums over warps halve their number");
 
+// Rows that are short go to smaller CTAs, more of them to an SM: what a row costs apart from its elements (the sums over
+// warps, the exchange, the entries) is latency.  8192 rows of bf16 logits with 128 / 256 threads (us): loss of 1000 logits
+// 19 / 53 (there 512), gradient 34 / 59, both in one pass 51 / 87; 4000 rows of 16000 30 / 36, 57 / 66 and 65 / 77, of
+// 32000 46 / 49, 98 / 102 and 126 / 108, of 128256 159 / 156 and 346 / 333.  With 1000 entries the one-pass kernel is
+// slower with fewer threads (8000 logits: 283 / 237), with 200 not (93 / 119).
+constexpr int kShortThreads = 128;
+constexpr int64_t kShortBytes = 32 * 1024;
+bool short_rows(const DistillParams &p, int64_t bytes) { return p.cluster == 1 && bytes <= kShortBytes; }
+
 // Two exponentials per element only where both temperatures count and differ.
 bool two_sums(const DistillParams &p) { return p.tau != 1.f && p.alpha > 0.f && p.alpha < 1.f; }
+
+template <bool F32, int TH>
+cudaError_t launch_loss(const DistillParams &p, cudaStream_t st)
+{
+    const size_t smem = (size_t)p.K * 12;
+    const bool two = two_sums(p) || (p.lse && p.tau != 1.f);   // both log-sum-exps are asked for
+    const int64_t ctas = (int64_t)p.T * p.cluster;
+    return two ? launch_clusters<distill_loss_kernel<F32, 2, TH>>(ctas, TH, smem, kMaxSmem, p.cluster, st, p)
+               : launch_clusters<distill_loss_kernel<F32, 1, TH>>(ctas, TH, smem, kMaxSmem, p.cluster, st, p);
+}
 
 template <bool F32>
 cudaError_t launch_loss(DistillParams p, cudaStream_t st)
 {
-    p.cluster = row_cluster(p.T, (int64_t)p.V * RowElem<F32>::kBytes, 0, 2, kLossThreads);
-    const size_t smem = (size_t)p.K * 12;
-    const bool two = two_sums(p) || (p.lse && p.tau != 1.f);   // both log-sum-exps are asked for
-    const int64_t ctas = (int64_t)p.T * p.cluster;
-    return two ? launch_clusters<distill_loss_kernel<F32, 2>>(ctas, kLossThreads, smem, kMaxSmem, p.cluster, st, p)
-               : launch_clusters<distill_loss_kernel<F32, 1>>(ctas, kLossThreads, smem, kMaxSmem, p.cluster, st, p);
+    const int64_t bytes = (int64_t)p.V * RowElem<F32>::kBytes;
+    p.cluster = row_cluster(p.T, bytes, 0, 2, kLossThreads);
+    return short_rows(p, bytes) ? launch_loss<F32, kShortThreads>(p, st) : launch_loss<F32, kLossThreads>(p, st);
 }
 
 // Shared memory of the gradient's kernels: the cached granules, and the entries and the table of their indices, once or
@@ -959,16 +999,34 @@ size_t plan_grad(DistillParams &p, int tables)
     return (size_t)p.cached * 16 + tables * ((size_t)p.K * 12 + (size_t)p.slots * 4);
 }
 
+template <bool F32, int TH>
+cudaError_t launch_grad(const DistillParams &p, size_t smem, cudaStream_t st)
+{
+    // (the CTAs of a row need no cluster)
+    const int64_t ctas = (int64_t)p.T * p.cluster;
+    return two_sums(p) ? launch_clusters<distill_grad_kernel<F32, 2, TH>>(ctas, TH, smem, kMaxSmem, 1, st, p)
+                       : launch_clusters<distill_grad_kernel<F32, 1, TH>>(ctas, TH, smem, kMaxSmem, 1, st, p);
+}
+
 template <bool F32>
 cudaError_t launch_grad(DistillParams p, cudaStream_t st)
 {
-    p.cluster = row_cluster(p.T, (int64_t)p.V * RowElem<F32>::kBytes, 0, 4, kGradThreads);
+    const int64_t bytes = (int64_t)p.V * RowElem<F32>::kBytes;
+    p.cluster = row_cluster(p.T, bytes, 0, 4, kGradThreads);
     p.cached = 0;
     const size_t smem = plan_grad(p, 1);
-    // (the CTAs of a row need no cluster)
-    const int64_t ctas = (int64_t)p.T * p.cluster;
-    return two_sums(p) ? launch_clusters<distill_grad_kernel<F32, 2>>(ctas, kGradThreads, smem, kMaxSmem, 1, st, p)
-                       : launch_clusters<distill_grad_kernel<F32, 1>>(ctas, kGradThreads, smem, kMaxSmem, 1, st, p);
+    return short_rows(p, bytes) ? launch_grad<F32, kShortThreads>(p, smem, st) : launch_grad<F32, kGradThreads>(p, smem, st);
+}
+
+template <bool F32, int NT, bool SHIFT, int TH>
+cudaError_t launch_step(const DistillParams &p, size_t smem, cudaStream_t st)
+{
+    // as many clusters as the GPU holds at a time, each for every so many rows
+    int fit = 0;
+    const cudaError_t e = resident_clusters<distill_step_kernel<F32, NT, SHIFT, TH>>(TH, smem, kMaxSmem, p.cluster, &fit);
+    if (e != cudaSuccess) return e;
+    const int64_t clusters = p.T < fit ? p.T : fit < 1 ? 1 : fit;
+    return launch_clusters<distill_step_kernel<F32, NT, SHIFT, TH>>(clusters * p.cluster, TH, smem, kMaxSmem, p.cluster, st, p);
 }
 
 template <bool F32, int NT, bool SHIFT>
@@ -979,13 +1037,8 @@ cudaError_t launch_step(DistillParams p, cudaStream_t st)
     const size_t share = al16((size_t)((bytes + 32 + p.cluster - 1) / p.cluster) + 32);
     p.cached = (int)((share < kMaxCache ? share : kMaxCache) / 16);
     const size_t smem = plan_grad(p, 2);
-    // as many clusters as the GPU holds at a time, each for every so many rows
-    int fit = 0;
-    const cudaError_t e = resident_clusters<distill_step_kernel<F32, NT, SHIFT>>(kStepThreads, smem, kMaxSmem, p.cluster, &fit);
-    if (e != cudaSuccess) return e;
-    const int64_t clusters = p.T < fit ? p.T : fit < 1 ? 1 : fit;
-    return launch_clusters<distill_step_kernel<F32, NT, SHIFT>>(clusters * p.cluster, kStepThreads, smem, kMaxSmem,
-                                                                p.cluster, st, p);
+    return short_rows(p, bytes) && p.K <= 2 * kShortThreads ? launch_step<F32, NT, SHIFT, kShortThreads>(p, smem, st)
+                                : launch_step<F32, NT, SHIFT, kStepThreads>(p, smem, st);
 }
 
 template <bool F32>

@@ -1,6 +1,7 @@
 // sample.cu -- drawing a token from each row of logits (sats_sample).
 //
-// The row's share of a CTA is brought to shared memory once; all passes after that run there.
+// Rows of bf16 logits are drawn by sample_values_kernel, which counts their values; fp32 rows, short ones and very long
+// ones by sample_kernel, which brings the row's share of a CTA to shared memory once and makes all its passes there.
 //
 // Drawing needs sums over up to V tokens that decide next to borders as close as the smallest token's probability.
 // A token's weight is therefore a whole number, w = 2^F exp((z - max) / T) to about 35 bits relative (never less
@@ -22,7 +23,7 @@ namespace sats {
 namespace {
 
 constexpr int kAhead = 8;              // granules in flight per thread while the row arrives
-constexpr size_t kShare = 64 * 1024;   // of a row's bytes per CTA, where the cluster allows
+constexpr size_t kShare = 64 * 1024;   // of a row's bytes per CTA, where the cluster allows (fp32 top-p rows: 128 KB 346 us, 64 KB 236)
 constexpr size_t kMaxCache = 182 * 1024;
 constexpr size_t kMaxSmem = kMaxCache + (size_t)kListCap * 8;
 static_assert(kMaxSmem + 13 * 1024 <= kSmemPerCta, "with the kernel's static part");
@@ -887,6 +888,10 @@ __device__ __forceinline__ void sample_row(Ctx<F32> &c, const SampleParams &p, i
     });
 }
 
+// The row in shared memory, three CTAs of 256 threads to an SM (1024 x 1, 512 x 2, 256 x 4 and 128 x 6 were slower).  300 rows
+// of 100003 fp32 logits with top-p take 227 us, where reading them takes 18: the counting pass issues about 25 and the
+// exact pass about 60 instructions an element (a weight of 35 bits is some 20 operations on pairs of floats), over half of
+// the issue slots that there are, and five barriers of the cluster stand between the passes.  Four rows of 1000: 10.8 us.
 template <bool F32>
 __global__ void __launch_bounds__(kSelThreads, kSelPerSm) sample_kernel(const SampleParams p)
 {
@@ -916,6 +921,13 @@ __global__ void __launch_bounds__(kSelThreads, kSelPerSm) sample_kernel(const Sa
 // follows exactly from the counts and one weight per value.  Only the CTA in which the token lies reads its tokens again
 // (from the L2) and adds their weights from a table of the values.
 //
+// 512 rows of 128256 bf16 logits (19 us of reading) take 139 us free, 168 with top-p, 156 with a top-k of up to 1000, 92
+// with min-p, 76 with a top-k of at most 192, 53 greedy; with the row in shared memory (sample_kernel) they took 156, 368,
+// 196, 114, 100 and 59.  A count is about ten instructions a token, an addition in shared memory among them: 57 us until
+// the row is counted, 36 if it were only read.  Then 25 to 50 us go into the weights of 4096 values, the border and two
+// exchanges, and 35 to 45 into the one CTA of a row that adds its tokens' weights (two lookups of 8 bytes in the table
+// cost a conflict of banks each): chains of latency, covered by three other CTAs on the SM.
+//
 // The values of magnitudes from 2^-10 to below 2^6 have a step each, in descending order.  Smaller ones are listed one by
 // one; of those from -2^6 down, which have no weight, the number is known.  What does not fit this (larger logits, many tiny
 // ones, a border among the listed ones) is drawn the general way.
@@ -923,11 +935,16 @@ constexpr int kSteps = 2 * kBins;   // two counts of 16 bits in a word
 constexpr int kFewMax = kSelThreads;
 constexpr int kLeastMag = 117 << 7, kFarMag = 133 << 7;   // magnitudes as bits
 static_assert(kFarMag - kLeastMag == kSteps / 2, "a step for each value");
-constexpr int kValuesPerSm = 4;
-constexpr int kValuesFrom = 4096;          // tokens of a row
+constexpr int kValuesPerSm = 4;   // (3, with more registers: 256 mixed rows 111 us instead of 99)
+// Tokens of a row: with 4096 steps a row, short rows of a free draw are slower this way (512 rows of 8000: 32 us against
+// 22; of 32000: 55 against 47), all others faster (of 8000 with top-p 42 against 48, top-k 43 against 69; at 2000 34 and
+// 26 free against 39 and 15).
+constexpr int kValuesFrom = 4096;
 constexpr int kValuesTo = 65536 - 128;     // of a CTA: counts of 16 bits
-constexpr size_t kValuesShare = 96 * 1024;  // of a row's bytes per CTA, where the cluster allows
-constexpr int kValuesTop = 192;            // the largest top-k that goes by a list
+// Of a row's bytes per CTA, where the cluster allows: 256 mixed rows of 151936 take 83 us with 4 CTAs and 99 with 8, 512
+// top-p rows of 128256 168 with 4 CTAs, 184 with 2 and 203 with 8.
+constexpr size_t kValuesShare = 96 * 1024;
+constexpr int kValuesTop = 192;            // the largest top-k that goes by a list (of which kSmall need no sorting)
 constexpr uint32_t kNoWay = 0xffffffffu;
 
 __device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b)
