@@ -258,10 +258,11 @@ __device__ __forceinline__ void start_row(const Ctx<F32> &c, uint4 *cache)
 
 // Brings the row in and finds its largest key and, for want > 0, a bound with at least `want` elements at or above
 // it (or below every element, if there are not so many).  scratch: kBoundBins words.
-template <bool F32>
+__host__ __device__ constexpr int groups_of(bool f32) { return f32 ? 4 : 8; }   // of a thread
+template <bool FEW, bool F32>
 __device__ void load_row(Ctx<F32> &c, uint4 *cache, int want, uint32_t *scratch, uint32_t *kmax, uint32_t *bound)
 {
-    constexpr int NG = F32 ? 4 : 8;   // groups of a thread
+    constexpr int NG = groups_of(F32);
     Shared *sh = c.sh;
     const int tid = threadIdx.x, lane = tid & 31;
     if (want > 0)
@@ -310,10 +311,15 @@ __device__ void load_row(Ctx<F32> &c, uint4 *cache, int want, uint32_t *scratch,
     }
     uint32_t top, low;
     const int R = (want + c.C - 1) >> (31 - __clz(c.C));
-    if (few_groups(min(c.n, kSelThreads) * NG, min(c.n, 1 << 20) * RowElem<F32>::kPer, R)) {
-        __syncthreads();   // (others' granules)
-        low = element_bound(c, scratch, R, &top);
-    } else {
+    bool few = false;
+    if constexpr (FEW) {
+        few = few_groups(min(c.n, kSelThreads) * NG, min(c.n, 1 << 20) * RowElem<F32>::kPer, R);
+        if (few) {
+            __syncthreads();   // (others' granules)
+            low = element_bound(c, scratch, R, &top);
+        }
+    }
+    if (!few) {
         low = group_bound(sh, scratch, R, hi, lo, &top, [&](auto f) {
 #pragma unroll
             for (int k = 0; k < NG; ++k) f(g[k]);
@@ -820,7 +826,7 @@ __device__ __forceinline__ void draw_list(const SampleParams &p, int row, const 
 }
 
 // The draw in any case, after start_row.
-template <bool F32>
+template <bool FEW, bool F32>
 __device__ __forceinline__ void sample_row(Ctx<F32> &c, const SampleParams &p, int row, const Settings &set, uint4 *cache,
                                            unsigned long long *list, const float2 *tab)
 {
@@ -829,7 +835,7 @@ __device__ __forceinline__ void sample_row(Ctx<F32> &c, const SampleParams &p, i
     const float T = set.T, u = set.u, top_p = set.top_p;
     const int want = !set.greedy && k > 0 && k <= kMaxTop ? k : 0;   // what the list serves
     uint32_t kmax, bound;
-    load_row(c, cache, want, reinterpret_cast<uint32_t *>(list), &kmax, &bound);
+    load_row<FEW>(c, cache, want, reinterpret_cast<uint32_t *>(list), &kmax, &bound);
     if (kmax <= kKeyNone) {   // nothing can be drawn
         if (c.rank == 0 && tid == 0) put_sample(p, row, -1, -INFINITY, 0);
         return;
@@ -892,7 +898,9 @@ __device__ __forceinline__ void sample_row(Ctx<F32> &c, const SampleParams &p, i
 // of 100003 fp32 logits with top-p take 227 us, where reading them takes 18: the counting pass issues about 25 and the
 // exact pass about 60 instructions an element (a weight of 35 bits is some 20 operations on pairs of floats), over half of
 // the issue slots that there are, and five barriers of the cluster stand between the passes.  Four rows of 1000: 10.8 us.
-template <bool F32>
+//
+// FEW: there may be few_groups (the calls to see to it cost 4 to 8 % of the other draws).
+template <bool F32, bool FEW>
 __global__ void __launch_bounds__(kSelThreads, kSelPerSm) sample_kernel(const SampleParams p)
 {
     extern __shared__ __align__(16) uint4 smem[];
@@ -912,7 +920,7 @@ __global__ void __launch_bounds__(kSelThreads, kSelPerSm) sample_kernel(const Sa
     }
     if (!set.greedy)
         for (int i = tid; i < 1024; i += kSelThreads) tab[i] = kExp2.v[i];
-    sample_row(c, p, row, set, smem, list, tab);
+    sample_row<FEW>(c, p, row, set, smem, list, tab);
 }
 
 // ------------------------------------------------------------------ bf16 rows by their values
@@ -1132,7 +1140,7 @@ __device__ __noinline__ void sample_row_again(Ctx<false> c, const SampleParams &
                                               unsigned long long *list, const float2 *tab)
 {
     start_row(c, nullptr);
-    sample_row(c, p, row, set, static_cast<uint4 *>(nullptr), list, tab);
+    sample_row<false>(c, p, row, set, static_cast<uint4 *>(nullptr), list, tab);
 }
 
 __global__ void __launch_bounds__(kSelThreads, kValuesPerSm) sample_values_kernel(const SampleParams p)
@@ -1577,9 +1585,14 @@ sats_status sample(const void *logits, int64_t ld, int B, int V, const float *te
     p.cluster = logits_cluster(B, bytes, 0, kShare);
     const size_t share = (size_t)((bytes + 32 + p.cluster - 1) / p.cluster) + 32;
     p.cached = (int)((share < kMaxCache ? share : kMaxCache) / 16);
-    const cudaError_t e = launch_clusters<sample_kernel<F32>>((int64_t)B * p.cluster, kSelThreads,
-                                                              (size_t)p.cached * 16 + kListCap * 8, kMaxSmem, p.cluster,
-                                                              static_cast<cudaStream_t>(stream), p);
+    const int granules = (int)std::min<int64_t>((bytes + 15) / 16 / p.cluster, 1 << 20);
+    const bool few = top_k && few_groups(std::min(granules, kSelThreads) * groups_of(F32), granules * RowElem<F32>::kPer,
+                                         std::min(V, kMaxTop) / p.cluster);
+    const int64_t ctas = (int64_t)B * p.cluster;
+    const size_t smem = (size_t)p.cached * 16 + kListCap * 8;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const cudaError_t e = few ? launch_clusters<sample_kernel<F32, true>>(ctas, kSelThreads, smem, kMaxSmem, p.cluster, st, p)
+                              : launch_clusters<sample_kernel<F32, false>>(ctas, kSelThreads, smem, kMaxSmem, p.cluster, st, p);
     return e == cudaSuccess ? SATS_OK : cuda_fail(e, "sampling kernel launch");
 }
 
