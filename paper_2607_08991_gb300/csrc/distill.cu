@@ -271,16 +271,14 @@ struct Seen {
 // Facts about a row's entries that its threads join.
 enum { kEntryTwice = 1, kEntryNan = 2, kEntryLabel = 4 };
 
-// One entry of a row: its index, its value and (within [lo, hi)) its logit to shared memory.  *gm: the largest value of
-// the thread's.
-template <bool F32>
-__device__ __forceinline__ void put_entry(const Entries &e, const DistillParams &p, int row, int k, int i, float g,
-                                          int label, int lo, int hi, bool report, float *gm, int *facts)
+// One entry of a row: its index, its value and its logit to shared memory.  *gm: the largest value of the thread's.
+__device__ __forceinline__ void put_entry(const Entries &e, const DistillParams &p, int k, int i, float g, float z,
+                                          int label, bool report, float *gm, int *facts)
 {
     const bool there = i >= 0 && i < p.V;
     e.i[k] = there ? i : -1;
     e.g[k] = there ? g : -INFINITY;
-    if (i >= lo && i < hi) e.z[k] = load_logit(p.z, (int64_t)row * p.ldz + i, F32);
+    e.z[k] = z;
     if (there) {
         *gm = fmaxf(*gm, g);
         *facts |= (g != g ? kEntryNan : 0) | (i == label ? kEntryLabel : 0);
@@ -322,9 +320,11 @@ __device__ __forceinline__ bool load_entries(const Entries &e, const DistillPara
 {
     float gm = -INFINITY;
     int mine = 0;
-    for (int k = threadIdx.x; k < p.K; k += TH)
-        put_entry<F32>(e, p, row, k, p.idx[(size_t)row * p.K + k], p.val[(size_t)row * p.K + k], label, lo, hi,
-                       report, &gm, &mine);
+    for (int k = threadIdx.x; k < p.K; k += TH) {
+        const int i = p.idx[(size_t)row * p.K + k];
+        const float z = i >= lo && i < hi ? load_logit(p.z, (int64_t)row * p.ldz + i, F32) : 0.f;
+        put_entry(e, p, k, i, p.val[(size_t)row * p.K + k], z, label, report, &gm, &mine);
+    }
     const float4 w = warp_shares<TH>(e, p.K, c, gm, mine);
     if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = w;
     __syncthreads();
@@ -690,7 +690,7 @@ __global__ void __launch_bounds__(TH, 1024 / TH) distill_grad_kernel(const Disti
 // exchange their sums by stores that count on an mbarrier of the receiver (a cluster barrier would wait for the
 // gradient's stores as well); a wait that gives up leaves NaN and says so in the status word.
 // 4096 rows of 128256 bf16 logits with 64 entries, read once and written once, take 375 us, 5.6 TB/s; one row per cluster
-// and launch took 450.  Without entries it is 335 us, with 1000 of them 640, at tau 2 (two exponentials) 464: what bounds
+// and launch took 450.  Without entries it is 335 us, with 1000 of them 544, at tau 2 (two exponentials) 464: what bounds
 // it is the issue of instructions (two exponentials an element in the sums and the gradient each, at 24 warps to an SM)
 // and the latency of the chain sums - exchange - gradient in each row, which two other CTAs on the SM cover in part.
 // SHIFT: some rows of the gradient lie on other 16-byte boundaries than the logits' rows; a warp then has a run of
@@ -710,11 +710,9 @@ __global__ void __launch_bounds__(TH, kStepPerSm * kStepThreads / TH) distill_st
     __shared__ float label_logit;            // the first thread's: in place, it is read before the row's sums go out
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int C = p.cluster, rank = blockIdx.x % C, stride = gridDim.x / C;
-    char *tables = reinterpret_cast<char *>(row_smem + p.cached);   // entries and their indices' table, two of each in turn
-    const size_t table_bytes = (size_t)p.K * 12 + (size_t)p.slots * 4;
-    const auto seen_in = [&](int t) {
-        return Seen{reinterpret_cast<int *>(tables + t * table_bytes + (size_t)p.K * 12), (unsigned)p.slots - 1u};
-    };
+    char *tables = reinterpret_cast<char *>(row_smem + p.cached);   // entries, two of them in turn, and their indices' table
+    const size_t table_bytes = (size_t)p.K * 12;
+    const Seen seen{reinterpret_cast<int *>(tables + 2 * table_bytes), (unsigned)p.slots - 1u};
     const float ctau = kLog2e / p.tau;
     float c[NT];
     set_factors(c, p, ctau);
@@ -737,8 +735,7 @@ __global__ void __launch_bounds__(TH, kStepPerSm * kStepThreads / TH) distill_st
         never = 0;
     }
     if (soft)
-        for (int t = 0; t < 2; ++t)
-            for (int i = tid; i < p.slots; i += TH) seen_in(t).slot[i] = -1;
+        for (int i = tid; i < p.slots; i += TH) seen.slot[i] = -1;
     int row = blockIdx.x / C, label = label_of(row), uses = 0;
     {
         const Row<F32> r(p.z, row, p.ldz, p.V);
@@ -777,12 +774,12 @@ __global__ void __launch_bounds__(TH, kStepPerSm * kStepThreads / TH) distill_st
         bool any = false;
         if (live) {
             // the entries and the label's logit are on their way while the row is summed
-            int i0 = -1;
-            float g0 = 0.f;
-            if (soft && tid < p.K) {
-                i0 = p.idx[(size_t)row * p.K + tid];
-                g0 = p.val[(size_t)row * p.K + tid];
-            }
+            if (soft)
+                for (int k = tid; k < p.K; k += TH) {
+                    cp_async4(ent.i + k, p.idx + (size_t)row * p.K + k);
+                    cp_async4(ent.g + k, p.val + (size_t)row * p.K + k);
+                }
+            cp_async_commit();
             const float zy = hard && tid == 0 ? load_logit(p.z, (int64_t)row * p.ldz + label, F32) : 0.f;
             up = p.g ? p.g[row] : 1.f;
 
@@ -797,7 +794,7 @@ __global__ void __launch_bounds__(TH, kStepPerSm * kStepThreads / TH) distill_st
                     run_add<F32, NT, kBatch>(sum, x, c);
                 }
             };
-            cp_async_wait<kLate>();
+            cp_async_wait<kLate + 1>();   // (the last group is the entries')
             batches(min(stop, (SHIFT ? warp * wper : 0) + (turns - kLate) * kHop));
             cp_async_wait<0>();
             batches(stop);
@@ -807,14 +804,25 @@ __global__ void __launch_bounds__(TH, kStepPerSm * kStepThreads / TH) distill_st
             }
             stream_sum<F32, NT, TH>(sum, r, run.x, nc, n, c);
             if (soft) {
-                const Seen seen = seen_in(turn);
                 float gm = -INFINITY;
                 int mine = 0;
-                for (int k = tid; k < p.K; k += TH) {
-                    const int i = k == tid ? i0 : p.idx[(size_t)row * p.K + k];
-                    const float g = k == tid ? g0 : p.val[(size_t)row * p.K + k];
-                    put_entry<F32>(ent, p, row, k, i, g, label, rank ? lo : 0, rank ? hi : p.V, rank == 0, &gm, &mine);
-                    if (i >= lo && i < hi && seen.before(i)) mine |= kEntryTwice;
+                const int from = rank ? lo : 0, to = rank ? hi : p.V;
+                constexpr int U = 4;   // entries of a thread whose logits are on their way together
+                for (int k0 = tid; k0 < p.K; k0 += U * TH) {
+                    int i[U];
+                    float z[U];
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        i[u] = k0 + u * TH < p.K ? ent.i[k0 + u * TH] : -1;
+                        z[u] = i[u] >= from && i[u] < to ? load_logit(p.z, (int64_t)row * p.ldz + i[u], F32) : 0.f;
+                    }
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        const int k = k0 + u * TH;
+                        if (k >= p.K) break;
+                        put_entry(ent, p, k, i[u], ent.g[k], z[u], label, rank == 0, &gm, &mine);
+                        if (i[u] >= lo && i[u] < hi && seen.before(i[u])) mine |= kEntryTwice;
+                    }
                 }
                 const float4 w = warp_shares<TH>(ent, p.K, ctau, gm, mine);
                 if (lane == 0) part[warp] = w;
@@ -834,9 +842,7 @@ __global__ void __launch_bounds__(TH, kStepPerSm * kStepThreads / TH) distill_st
             }
             if (soft) {
                 any = join_shares<WARPS>(part, ctau, &shares, &facts);
-                // the table that the next row uses
-                const Seen seen = seen_in(turn ^ 1);
-                for (int i = tid; i < p.slots; i += TH) seen.slot[i] = -1;
+                for (int i = tid; i < p.slots; i += TH) seen.slot[i] = -1;   // (all have looked; a barrier ahead of the next row)
             }
             if (C > 1) {
                 met = mbar_wait(&arrived[turn], (uses >> 1) & 1, &never);
@@ -990,13 +996,12 @@ cudaError_t launch_loss(DistillParams p, cudaStream_t st)
     return short_rows(p, bytes) ? launch_loss<F32, kShortThreads>(p, st) : launch_loss<F32, kLossThreads>(p, st);
 }
 
-// Shared memory of the gradient's kernels: the cached granules, and the entries and the table of their indices, once or
-// twice.
-size_t plan_grad(DistillParams &p, int tables)
+// Shared memory for a row's entries, `copies` of them, and the table of their indices.
+size_t plan_entries(DistillParams &p, int copies)
 {
     p.slots = 32;
     while (p.slots < 2 * p.K) p.slots *= 2;
-    return (size_t)p.cached * 16 + tables * ((size_t)p.K * 12 + (size_t)p.slots * 4);
+    return copies * ((size_t)p.K * 12) + (size_t)p.slots * 4;
 }
 
 template <bool F32, int TH>
@@ -1013,8 +1018,7 @@ cudaError_t launch_grad(DistillParams p, cudaStream_t st)
 {
     const int64_t bytes = (int64_t)p.V * RowElem<F32>::kBytes;
     p.cluster = row_cluster(p.T, bytes, 0, 4, kGradThreads);
-    p.cached = 0;
-    const size_t smem = plan_grad(p, 1);
+    const size_t smem = plan_entries(p, 1);
     return short_rows(p, bytes) ? launch_grad<F32, kShortThreads>(p, smem, st) : launch_grad<F32, kGradThreads>(p, smem, st);
 }
 
@@ -1033,10 +1037,11 @@ template <bool F32, int NT, bool SHIFT>
 cudaError_t launch_step(DistillParams p, cudaStream_t st)
 {
     const int64_t bytes = (int64_t)p.V * RowElem<F32>::kBytes;
+    const size_t entries = plan_entries(p, 2);
     p.cluster = row_cluster(p.T, bytes, kStepShare, 2, 2 * kStepThreads);
     const size_t share = al16((size_t)((bytes + 32 + p.cluster - 1) / p.cluster) + 32);
     p.cached = (int)((share < kMaxCache ? share : kMaxCache) / 16);
-    const size_t smem = plan_grad(p, 2);
+    const size_t smem = (size_t)p.cached * 16 + entries;
     return short_rows(p, bytes) && p.K <= 2 * kShortThreads ? launch_step<F32, NT, SHIFT, kShortThreads>(p, smem, st)
                                 : launch_step<F32, NT, SHIFT, kStepThreads>(p, smem, st);
 }

@@ -269,6 +269,17 @@ def test_values_of_long_rows(sats):
             check(sats, z, [0.3, 0.99], p=[0.7, 1.0], k=[0, 70000])
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [700, 2500, 6001])
+def test_top_k_of_short_rows(sats, V, dtype):
+    # as many rows as share the GPU out to one CTA each, top-k with more entries than groups
+    B = 310
+    g = np.random.default_rng([72, V])
+    for kind in ("normal", "ties", "masked"):
+        check(sats, rows(logits(kind, B, V, 73), dtype, pad=1), g.random(B), k=g.integers(1, 1100, B),
+              p=np.where(g.random(B) < 0.5, 1.0, g.uniform(0.1, 0.99, B)), unsure=3)
+
+
 def test_first_call_captured(sats):
     # a shape that no call has had before, captured at once
     B, V = 3, 77777

@@ -95,6 +95,32 @@ def test_rows_larger_than_the_cluster_memory(sats, dtype, V):
         check(sats, rows(logits(kind, 2, V, 14), dtype, pad=1), 100)
 
 
+def long_lists(kind, T, V, seed):
+    """Rows whose long lists are unevenly spread."""
+    g = np.random.default_rng([seed, T, V])
+    if kind == "outliers":             # nearly all of the list within one step of it
+        z = g.normal(0, 1e-3, (T, V))
+        z[:, V // 3] = 50.0
+        z[:, 0] = np.finfo(np.float32).min
+    elif kind == "narrow":             # neighbouring numbers
+        z = 1.0 + g.integers(0, 300, (T, V)) * 2.0 ** -23
+    elif kind == "bounded":            # the K-th largest among hundreds of equal ones
+        z = np.where(g.random((T, V)) < 0.1, 2.0, g.normal(-3, 1, (T, V)))
+    else:
+        return logits(kind, T, V, seed)
+    return z.astype(np.float32)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("kind", KINDS + ["outliers", "narrow", "bounded"])
+def test_long_lists(sats, kind, dtype):
+    # few rows to many (one CTA a row), rows of fewer groups than entries to long ones
+    for T, V in ((2, 1500), (3, 30011), (160, 2003), (320, 5003)):
+        z = rows(long_lists(kind, T, V, 16), dtype, pad=1, off=1)
+        for K in (130, 257, 1000, 1024):
+            check(sats, z, K)
+
+
 def test_large_offsets(sats):
     # rows so far apart that their offsets pass 32 bits
     V, T = 4099, 3
