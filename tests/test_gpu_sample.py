@@ -200,6 +200,22 @@ def test_high_temperatures(sats, T):
     check(sats, z, np.linspace(0.01, 0.99, B), T=np.full(B, T), p=[0.05, 0.3, 0.7, 0.95, 0.9999])
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("large", [None, 70.0, 300.0])
+def test_flat_nuclei(sats, large, dtype):
+    # thousands of tokens in every step of the weight, one far above them, few rows to many, with and without a top-k
+    for B, V in ((4, 100003), (320, 20011)):
+        g = np.random.default_rng([74, B])
+        z = logits("normal", B, V, 75)
+        if large:
+            z[:, 11] = large
+        z = rows(z, dtype, pad=1)
+        T = np.resize([2.0, 4.0, 8.0, 20.0, 60.0], B)
+        p = g.uniform(0.05, 0.999, B)
+        check(sats, z, g.random(B), T=T, p=p, unsure=3)
+        check(sats, z, g.random(B), T=T, p=p, k=g.integers(1025, V, B), unsure=3)
+
+
 def few_values(kind, B, V, seed):
     """Rows that a count of their values serves badly, or not at all (bf16 numbers)."""
     g = np.random.default_rng([seed, B, V])
