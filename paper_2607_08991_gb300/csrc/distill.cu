@@ -515,9 +515,9 @@ __device__ __forceinline__ int2 whole_of(const Row<F32> &r, int2 run)
 }
 
 // ------------------------------------------------------------------ the loss
-// One row per cluster, read once: bounded by HBM.  8192 rows of 151936 bf16 logits take 350 us, 7.1 TB/s (a copy reaches
-// 6.78, of which it writes half); 37 rows of 128256 fp32 ones with two temperatures 12 us, most of it a launch and two barriers of the cluster.
-// With 50 entries at tau 2 (two exponentials an element) the 8192 rows take 401 us.
+// One row per cluster, read once: bounded by HBM.  8192 rows of 151936 bf16 logits (one in twenty ignored) take 350 us,
+// 6.76 TB/s of what is read (a copy reaches 6.78); 37 rows of 128256 fp32 ones with two temperatures 11 us, most of it a
+// launch and two barriers of the cluster.  With 50 entries at tau 2 (two exponentials an element) the 8192 rows take 401.
 template <bool F32, int NT, int TH>
 __global__ void __launch_bounds__(TH, 1024 / TH) distill_loss_kernel(const DistillParams p)
 {
@@ -584,8 +584,9 @@ __global__ void __launch_bounds__(TH, 1024 / TH) distill_loss_kernel(const Disti
 
 // ------------------------------------------------------------------ the gradient from the log-sum-exps
 // p.cluster CTAs per row that need nothing of one another; the row streams through registers, four granules in
-// flight per thread.  Bounded by HBM: 1000 rows of 151936 fp32 logits, read and written, 197 us or 6.2 TB/s (one granule
-// in flight: 273 us); 221 us where the gradient's rows lie on other 16-byte boundaries (element by element 367).
+// flight per thread.  Bounded by HBM: 1000 rows of 151936 fp32 logits, read and written, 195 us or 6.1 TB/s of the rows
+// that count (one granule in flight: 273 us); 221 us where the gradient's rows lie on other 16-byte boundaries (element by
+// element 367).
 template <bool F32, int NT, int TH>
 __global__ void __launch_bounds__(TH, 1024 / TH) distill_grad_kernel(const DistillParams p)
 {
@@ -689,9 +690,9 @@ __global__ void __launch_bounds__(TH, 1024 / TH) distill_grad_kernel(const Disti
 // nobody else touches it, so the next row arrives while this one is stored, without a barrier.  The CTAs of a row
 // exchange their sums by stores that count on an mbarrier of the receiver (a cluster barrier would wait for the
 // gradient's stores as well); a wait that gives up leaves NaN and says so in the status word.
-// 4096 rows of 128256 bf16 logits with 64 entries, read once and written once, take 375 us, 5.6 TB/s; one row per cluster
+// 4096 rows of 128256 bf16 logits with 64 entries, read once and written once, take 377 us, 5.4 TB/s; one row per cluster
 // and launch took 450.  Without entries it is 335 us, with 1000 of them 544, at tau 2 (two exponentials) 464: what bounds
-// it is the issue of instructions (two exponentials an element in the sums and the gradient each, at 24 warps to an SM)
+// it is the issue of instructions (an exponential an element in the sums and another in the gradient, 24 warps to an SM)
 // and the latency of the chain sums - exchange - gradient in each row, which two other CTAs on the SM cover in part.
 // SHIFT: some rows of the gradient lie on other 16-byte boundaries than the logits' rows; a warp then has a run of
 // consecutive granules (as Shifted wants them) and not every eighth run of 32, which is 6 % faster.
