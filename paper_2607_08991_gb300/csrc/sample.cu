@@ -1177,31 +1177,33 @@ struct TieCount {
 };
 
 // The first token of this CTA's, in order, at which the running sum of f passes `target` (below their sum): found(idx,
-// key) by one thread.  Sums of 32 granules each, then the elements of the ones that hold it.  seg: kSegs words.
-constexpr int kSegs = kSelThreads;
-static_assert(kValuesTo / 8 + 8 <= kSegs * 32, "a thread per sum");
-static_assert(32 * 8 == kSelThreads, "a thread per element of them");
+// key) by one thread.  Sums of kSegGranules granules each, then the elements of the ones that hold it.  seg: kSegs words.
+constexpr int kSegGranules = 128, kSegs = 64;
+static_assert(kSegs % kSelWarps == 0 && kValuesTo / 8 + kSelWarps <= kSegs * kSegGranules && kSegs <= kSelThreads, "a thread per sum");
+static_assert(kSegGranules * 8 == kSelThreads * 4, "four elements of them per thread");
 template <typename S, typename Found>
 __device__ __forceinline__ void find_in_share(const Ctx<false> &c, unsigned long long target, const S &f,
                                               unsigned long long *seg, Found found)
 {
-    constexpr int U = 4;
+    constexpr int U = kSegGranules / 32;
     Shared *sh = c.sh;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int wper = (c.n + kSelWarps - 1) / kSelWarps, each = (wper + 31) / 32;   // sums of a warp
-    for (int i0 = 0; i0 < each; i0 += U) {
+    const int wper = (c.n + kSelWarps - 1) / kSelWarps, each = (wper + kSegGranules - 1) / kSegGranules;   // sums of a warp
+    for (int i = 0; i < each; ++i) {
         uint4 x[U];
 #pragma unroll
         for (int k = 0; k < U; ++k) {
-            const int v = c.wb + 32 * (i0 + k) + lane;
+            const int v = c.wb + kSegGranules * i + 32 * k + lane;
             x[k] = v < c.we ? load_granule<false>(c.r, c.gb + v) : make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u);
         }
+        unsigned long long a = 0;
 #pragma unroll
         for (int k = 0; k < U; ++k) {
-            const int v = c.wb + 32 * (i0 + k) + lane;
-            const unsigned long long a = warp_sum_u64(v < c.we ? f.granule(x[k], c.r.first(c.gb + v)) : 0ull);
-            if (lane == 0 && i0 + k < each) seg[warp * each + i0 + k] = a;
+            const int v = c.wb + kSegGranules * i + 32 * k + lane;
+            if (v < c.we) a += f.granule(x[k], c.r.first(c.gb + v));
         }
+        a = warp_sum_u64(a);
+        if (lane == 0) seg[warp * each + i] = a;
     }
     __syncthreads();
     unsigned long long mine = tid < kSelWarps * each ? seg[tid] : 0ull, total;
@@ -1211,14 +1213,25 @@ __device__ __forceinline__ void find_in_share(const Ctx<false> &c, unsigned long
         sh->mass[0] = run;
     }
     __syncthreads();
-    const int at = sh->border, w = at / each, v = w * wper + 32 * (at - w * each) + (tid >> 3);
+    const int at = sh->border, w = at / each, v = w * wper + kSegGranules * (at - w * each) + (tid >> 1);
     target -= sh->mass[0];
-    const int i = c.r.first(c.gb + v) + (tid & 7);
-    const float x = v < min(c.n, (w + 1) * wper) ? c.get(v, tid & 7) : -INFINITY;
-    const uint32_t key = key_of(x);
-    mine = key > kKeyNone ? f.elem(x, key, i) : 0ull;
+    const int j0 = (tid & 1) * 4, i0 = c.r.first(c.gb + v) + j0;
+    const bool on = v < min(c.n, (w + 1) * wper);
+    const uint4 q = on ? load_granule<false>(c.r, c.gb + v) : make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u);
+    unsigned long long m[4];
+    mine = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float x = __uint_as_float(granule_elem16(q, j0 + j) << 16);
+        m[j] = x > -INFINITY ? f.elem(x, key_of(x), i0 + j) : 0ull;   // (a NaN is not above it)
+        mine += m[j];
+    }
     run = block_scan_u64(mine, sh, &total);
-    if (target >= run && target - run < mine) found(i, key);   // (one thread)
+    if (target >= run && target - run < mine) {   // (one thread)
+        int j = 0;
+        while (j < 3 && target - run >= m[j]) run += m[j++];
+        found(i0 + j, key_of(__uint_as_float(granule_elem16(q, j0 + j) << 16)));
+    }
 }
 
 __device__ __noinline__ void sample_row_again(Ctx<false> c, const SampleParams &p, int row, const Settings &set,
