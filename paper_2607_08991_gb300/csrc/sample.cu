@@ -23,7 +23,8 @@ namespace sats {
 namespace {
 
 constexpr int kAhead = 8;              // granules in flight per thread while the row arrives
-constexpr size_t kShare = 64 * 1024;   // of a row's bytes per CTA, where the cluster allows (fp32 top-p rows: 128 KB 346 us, 64 KB 236)
+// Of a row's bytes per CTA, where the cluster allows (300 fp32 top-p rows with 128 KB 346 us, with 64 KB 236).
+constexpr size_t kShare = 64 * 1024;
 constexpr size_t kMaxCache = 182 * 1024;
 constexpr size_t kMaxSmem = kMaxCache + (size_t)kListCap * 8;
 static_assert(kMaxSmem + 13 * 1024 <= kSmemPerCta, "with the kernel's static part");
@@ -437,7 +438,7 @@ __device__ __noinline__ unsigned long long list_of_one_step(Ctx<F32> c, Scale s,
                                                             unsigned long long *list, int d0, int d1, unsigned long long want)
 {
     constexpr int E = RowElem<F32>::kPer, P = E / 2, kFine = 128;
-    static_assert((kRowMaxCluster + 1) * kFine + 1 <= kListCap && kFine <= kSelThreads, "all CTAs' masses lie where the list does");
+    static_assert((kRowMaxCluster + 1) * kFine + 1 <= kListCap && kFine <= kSelThreads, "the masses lie where the list does");
     Shared *sh = c.sh;
     const KeptMass all(s, tab, by_k);
     const int tid = threadIdx.x, lane = tid & 31, C = c.C;
@@ -454,9 +455,10 @@ __device__ __noinline__ unsigned long long list_of_one_step(Ctx<F32> c, Scale s,
             for (int j = 0; j < P; ++j) {
                 const f32x2 y2 = fmul2(fadd2(z[j], nt), chi);   // (as weights2 does)
                 const float2 x = unpack2(z[j]), y = unpack2(y2), m = unpack2(fadd2(y2, magic));
-                const int a = __float_as_int(m.x) - __float_as_int(kMagicG) - from, b = __float_as_int(m.y) - __float_as_int(kMagicG) - from;
-                if (y.x < 60.f && (unsigned)a < (unsigned)n && (!FILTERED || all.keeps(x.x, i0 + 2 * j))) f(x.x, i0 + 2 * j, a);
-                if (y.y < 60.f && (unsigned)b < (unsigned)n && (!FILTERED || all.keeps(x.y, i0 + 2 * j + 1))) f(x.y, i0 + 2 * j + 1, b);
+                const int base = __float_as_int(kMagicG) + from, i = i0 + 2 * j;
+                const int a = __float_as_int(m.x) - base, b = __float_as_int(m.y) - base;
+                if (y.x < 60.f && (unsigned)a < (unsigned)n && (!FILTERED || all.keeps(x.x, i))) f(x.x, i, a);
+                if (y.y < 60.f && (unsigned)b < (unsigned)n && (!FILTERED || all.keeps(x.y, i + 1))) f(x.y, i + 1, b);
             }
         }
     };
@@ -1095,7 +1097,8 @@ __device__ __forceinline__ uint32_t odd_ones(const uint4 &q)
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         const uint32_t lo = w[k] & 0x7fffu, hi = (w[k] >> 16) & 0x7fffu;
-        odd |= (lo - kLeastMag >= kFarMag - kLeastMag ? 1u << (2 * k) : 0u) | (hi - kLeastMag >= kFarMag - kLeastMag ? 2u << (2 * k) : 0u);
+        odd |= lo - kLeastMag >= kFarMag - kLeastMag ? 1u << (2 * k) : 0u;
+        odd |= hi - kLeastMag >= kFarMag - kLeastMag ? 2u << (2 * k) : 0u;
     }
     return odd;
 }
@@ -1179,7 +1182,8 @@ struct TieCount {
 // The first token of this CTA's, in order, at which the running sum of f passes `target` (below their sum): found(idx,
 // key) by one thread.  Sums of kSegGranules granules each, then the elements of the ones that hold it.  seg: kSegs words.
 constexpr int kSegGranules = 128, kSegs = 64;
-static_assert(kSegs % kSelWarps == 0 && kValuesTo / 8 + kSelWarps <= kSegs * kSegGranules && kSegs <= kSelThreads, "a thread per sum");
+static_assert(kSegs % kSelWarps == 0 && kValuesTo / 8 + kSelWarps <= kSegs * kSegGranules && kSegs <= kSelThreads,
+              "a thread per sum");
 static_assert(kSegGranules * 8 == kSelThreads * 4, "four elements of them per thread");
 template <typename S, typename Found>
 __device__ __forceinline__ void find_in_share(const Ctx<false> &c, unsigned long long target, const S &f,
@@ -1194,7 +1198,7 @@ __device__ __forceinline__ void find_in_share(const Ctx<false> &c, unsigned long
 #pragma unroll
         for (int k = 0; k < U; ++k) {
             const int v = c.wb + kSegGranules * i + 32 * k + lane;
-            x[k] = v < c.we ? load_granule<false>(c.r, c.gb + v) : make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u);
+            if (v < c.we) x[k] = load_granule<false>(c.r, c.gb + v);
         }
         unsigned long long a = 0;
 #pragma unroll
