@@ -349,7 +349,9 @@ __device__ void load_row(Ctx<F32> &c, uint4 *cache, int want, uint32_t *scratch,
 // 2048 equal steps of the weight's logarithm, each as 4096 times its weight relative to the middle of its step (right
 // to kOff): no exponential, one addition in shared memory a token.  From all CTAs' counts follow the steps in which the
 // border can lie, as a rule one or two.  The second pass takes the exact weights: of all tokens, of the ones above these
-// steps, and a list of the ones within, which settles the border; that it lies there at all is checked.
+// steps, and a list of the ones within, which settles the border; that it lies there at all is checked.  (A step's 32 bits
+// hold 2^20 tokens of a CTA, less a few: rows of over 8 million logits can run them over, to any number.  A border that
+// they then put in a wrong place fails that check; counts of 0 in all, as 2^20 alike in each CTA leave, put it nowhere.)
 constexpr int kBins = 2048;
 static_assert(2 * kBins * 4 <= kListCap * 8, "the counts, and their exchange, lie where the list does");
 // Half a 1 / 1024 octave, the straight line instead of the power within a step, the rounding to 1 / 4096.
@@ -570,7 +572,8 @@ __device__ bool cut_by_counts(Ctx<F32> &c, const Scale &s, const float2 *tab, un
     unsigned long long total;
     unsigned long long run = block_scan_u64(mine, sh, &total);
     const unsigned long long *slot = cluster_gather(c, total);
-    unsigned long long Zs = slot_sum(slot, C);
+    const unsigned long long Zs = slot_sum(slot, C);
+    if (Zs == 0) return false;   // (the same in every CTA of the row; from here on one step is the border's, each way)
     for (unsigned k = 0; k < c.rank; ++k) run += slot[k];
     {
         const float rest = 1.f - top_p;

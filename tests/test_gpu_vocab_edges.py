@@ -1,0 +1,37 @@
+"""Inputs at the edges of what the vocabulary operators allow."""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def sats():
+    import __graft_entry__
+    __graft_entry__.build()
+    from paper_2607_08991_gb300 import sats as s
+    return s
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V,apart", [(1 << 23, 0), ((1 << 23) + 8, 0), (1 << 24, 0), (1 << 24, 30)])
+def test_nucleus_of_millions_of_equal_tokens(sats, V, apart, dtype):
+    # so many tokens of one weight in each CTA that 32-bit counts of them pass their range, some to exactly 0.  All weigh
+    # 1, or every second one next to nothing at all (30 / T is past 62 octaves): the n = ceil(p number) first ones are kept,
+    # and of those number floor(u n) is drawn, whatever the way there (u and p are exact in binary)
+    u, p = [0.0, 0.25, 0.8125], [0.5, 0.4375, 0.75]
+    z = torch.zeros(3, V, dtype=dtype, device="cuda")
+    T = 100.0
+    if apart:
+        z[:, 1::2] = -float(apart) * T * 2
+    ids, n = (torch.full((3,), 77, dtype=torch.int32, device="cuda") for _ in range(2))
+    lp = torch.full((3,), 7.0, device="cuda")
+    dev = lambda a: torch.tensor(a, device="cuda")
+    sats.sample(z, dev(u), ids, temperature=dev([T] * 3), top_p=dev(p), logprob=lp, n_kept=n)
+    number, step = (V // 2, 2) if apart else (V, 1)
+    kept = [int(np.ceil(x * number)) for x in p]
+    assert n.tolist() == kept
+    assert ids.tolist() == [int(np.floor(x * m)) * step for x, m in zip(u, kept)]
+    # the logarithm of a whole number, rounded a few times
+    np.testing.assert_allclose(lp.cpu().numpy(), -np.log(np.array(kept, np.float64)), rtol=2.0 ** -21)
