@@ -438,9 +438,10 @@ SATS_API sats_status sats_route_calibrate(const float *score, int V, const int32
  * between the rows is not read).  A pointer needs the alignment of its elements
  * only.  The calls need no workspace, and what they write does not depend on the
  * order in which their threads run.  In sats_distill_loss_grad the CTAs of a row
- * wait, bounded, for one another's sums: if one gives up, the row's loss and
- * gradient are NaN and dev_status tells (SATS_ETIMEOUT from
- * sats_get_status_word).  V up to 2^31 - 65 and 2^28 - 1 rows (else
+ * wait, bounded, for one another's sums: if one gives up, dev_status tells
+ * (SATS_ETIMEOUT from sats_get_status_word), and the loss and gradient of that
+ * row and of the rows that these CTAs serve after it are NaN wherever they are
+ * not right.  V up to 2^31 - 65 and 2^28 - 1 rows (else
  * SATS_ESHAPE); no rows: nothing is done.
  *
  * sats_top_logits -- the K largest logits of each row, as a teacher hands them
@@ -571,6 +572,18 @@ SATS_API sats_status sats_selftest_wait_timeout(void *ws, size_t ws_bytes, void 
  */
 SATS_API sats_status sats_selftest_select_timeout(const float *a, int64_t n, float *t_out, void *ws,
                                                   size_t ws_bytes, void *stream);
+
+/*
+ * sats_selftest_distill_timeout -- the same for sats_distill_loss_grad: a call
+ * on bf16 logits with labels alone (tau 1, alpha 0, g NULL; arguments as there,
+ * 0 <= row < T), in which one CTA of the given row does not get another's sums.
+ * Where a row has more than one CTA (rows beyond 72 KB, or few of them), the
+ * wait for them gives up after 2 s and those that depend on it after 2 s more;
+ * dev_status says SATS_ETIMEOUT.
+ */
+SATS_API sats_status sats_selftest_distill_timeout(const void *logits, int64_t ld, int T, int V, const int32_t *labels,
+                                                   float *loss, void *dlogits, int64_t ld_d, int row,
+                                                   int32_t *dev_status, void *stream);
 
 /*
  * sats_get_error -- synchronises `stream`, reads the status word in the

@@ -50,6 +50,7 @@ struct DistillParams {
     int cluster;              // CTAs of a row
     int cached;               // granules of a CTA's share that stay in shared memory
     int slots;                // of the table of entries' indices (a power of two)
+    int withheld;             // a row whose sums the second CTA does not send to the first (the self-test's; -1)
 };
 
 // Sums of 2^((z - m) c) for one or two c, m the largest z so far.
@@ -689,7 +690,9 @@ __global__ void __launch_bounds__(TH, 1024 / TH) distill_grad_kernel(const Disti
 // as a thread has a granule's gradient it sends for the same granule of the cluster's next row, into the same place:
 // nobody else touches it, so the next row arrives while this one is stored, without a barrier.  The CTAs of a row
 // exchange their sums by stores that count on an mbarrier of the receiver (a cluster barrier would wait for the
-// gradient's stores as well); a wait that gives up leaves NaN and says so in the status word.
+// gradient's stores as well).  A CTA whose wait gives up says so in the status word; its mbarriers' phases are out of step
+// from then on, so that it neither arms nor waits nor sends any more and leaves NaN in its part of all rows to come.  The
+// others miss its sums in the next row, and do the same after one more limit at most.
 // 4096 rows of 128256 bf16 logits with 64 entries, read once and written once, take 377 us, 5.4 TB/s; one row per cluster
 // and launch took 450.  Without entries it is 335 us, with 1000 of them 544, at tau 2 (two exponentials) 464: what bounds
 // it is the issue of instructions (an exponential an element in the sums and another in the gradient, 24 warps to an SM)
@@ -707,7 +710,7 @@ __global__ void __launch_bounds__(TH, kStepPerSm * kStepThreads / TH) distill_st
     __shared__ float wsum[WARPS][4], wkd[WARPS];
     __shared__ __align__(16) float csum[2][kRowMaxCluster][4];
     __shared__ uint64_t arrived[2];
-    __shared__ int never;
+    __shared__ int gave_up;                  // set between a row's first barrier and its last one, read before the first
     __shared__ float label_logit;            // the first thread's: in place, it is read before the row's sums go out
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int C = p.cluster, rank = blockIdx.x % C, stride = gridDim.x / C;
@@ -733,7 +736,7 @@ __global__ void __launch_bounds__(TH, kStepPerSm * kStepThreads / TH) distill_st
         mbar_init(&arrived[0], 1);
         mbar_init(&arrived[1], 1);
         mbar_init_fence();
-        never = 0;
+        gave_up = 0;
     }
     if (soft)
         for (int i = tid; i < p.slots; i += TH) seen.slot[i] = -1;
@@ -774,6 +777,7 @@ __global__ void __launch_bounds__(TH, kStepPerSm * kStepThreads / TH) distill_st
         int facts = 0;
         bool any = false;
         if (live) {
+            const bool alone = *(volatile int *)&gave_up != 0;   // (the same in all threads)
             // the entries and the label's logit are on their way while the row is summed
             if (soft)
                 for (int k = tid; k < p.K; k += TH) {
@@ -836,8 +840,8 @@ __global__ void __launch_bounds__(TH, kStepPerSm * kStepThreads / TH) distill_st
             warp_join(sum, c, WARPS);
             bool met = true;
             if (C > 1) {
-                if (tid == 0) mbar_arrive_expect_tx(&arrived[turn], 16u * C);
-                if (tid < C)
+                if (tid == 0 && !alone) mbar_arrive_expect_tx(&arrived[turn], 16u * C);
+                if (tid < C && !alone && !(row == p.withheld && rank == 1 && tid == 0))
                     st_async_v4(peer_addr(csum[turn][rank], tid), sum.m, sum.s[0], sum.s[NT - 1], 0.f,
                                 peer_addr(&arrived[turn], tid));
             }
@@ -846,12 +850,15 @@ __global__ void __launch_bounds__(TH, kStepPerSm * kStepThreads / TH) distill_st
                 for (int i = tid; i < p.slots; i += TH) seen.slot[i] = -1;   // (all have looked; a barrier ahead of the next row)
             }
             if (C > 1) {
-                met = mbar_wait(&arrived[turn], (uses >> 1) & 1, &never);
+                met = !alone && mbar_wait(&arrived[turn], (uses >> 1) & 1, &gave_up);
                 sum = get_sum<NT>(csum[turn][lane & (C - 1)]);
                 warp_join(sum, c, C);
                 if (!met) {
                     sum.s[0] = sum.s[NT - 1] = __int_as_float(0x7fffffff);
-                    if (lane == 0 && p.status) atomicOr(p.status, kStatusTimeout);
+                    if (!alone) {
+                        *(volatile int *)&gave_up = 1;   // (who still waits gives up with it)
+                        if (p.status) atomicOr(p.status, kStatusTimeout);
+                    }
                 }
             }
             ++uses;
@@ -942,7 +949,13 @@ __global__ void __launch_bounds__(TH, kStepPerSm * kStepThreads / TH) distill_st
         }
         label = nlabel;
     }
-    if (C > 1) cluster_sync_all();   // nobody leaves while another may still write to its memory
+    if (C > 1) {
+        cluster_sync_all();   // nobody leaves while another may still write to its memory
+        if (gave_up) {        // what it has not waited for has a millisecond to arrive
+            const unsigned long long t0 = global_ns();
+            while (global_ns() - t0 < 1000000ull) __nanosleep(1000);
+        }
+    }
 }
 
 size_t al16(size_t v) { return (v + 15) & ~(size_t)15; }
@@ -1120,11 +1133,12 @@ sats_status distill_grad(const void *logits, int64_t ld, int T, int V, const int
 template <bool F32>
 sats_status distill_loss_grad(const void *logits, int64_t ld, int T, int V, const int32_t *idx, const float *val,
                               int K, const int32_t *labels, float tau, float alpha, const float *g, float *loss,
-                              void *dlogits, int64_t ld_d, int32_t *dev_status, void *stream)
+                              void *dlogits, int64_t ld_d, int32_t *dev_status, void *stream, int withheld = -1)
 {
     DistillParams p{};
     p.z = logits; p.ldz = ld; p.T = T; p.V = V; p.idx = idx; p.val = val; p.K = K; p.labels = labels;
     p.tau = tau; p.alpha = alpha; p.loss = loss; p.g = g; p.d = dlogits; p.ldd = ld_d; p.status = dev_status;
+    p.withheld = withheld;
     const sats_status s = check_distill<F32>(p);
     if (s != SATS_OK) return s;
     if (ld_d < V) return SATS_EINVAL;
@@ -1189,6 +1203,15 @@ sats_status sats_distill_loss_grad_f32(const float *logits, int64_t ld, int T, i
 {
     return sats::distill_loss_grad<true>(logits, ld, T, V, top_idx, top_val, K, labels, tau, alpha, g, loss, dlogits,
                                          ld_d, dev_status, stream);
+}
+
+sats_status sats_selftest_distill_timeout(const void *logits, int64_t ld, int T, int V, const int32_t *labels,
+                                          float *loss, void *dlogits, int64_t ld_d, int row, int32_t *dev_status,
+                                          void *stream)
+{
+    if (row < 0 || row >= T) return SATS_EINVAL;
+    return sats::distill_loss_grad<false>(logits, ld, T, V, nullptr, nullptr, 0, labels, 1.f, 0.f, nullptr, loss, dlogits,
+                                          ld_d, dev_status, stream, row);
 }
 
 }  // extern "C"

@@ -90,6 +90,7 @@ def lib() -> ctypes.CDLL:
             "sats_get_status_word": (I, [P, P]),
             "sats_selftest_wait_timeout": (I, [P, Z, P]),
             "sats_selftest_select_timeout": (I, [P, I64, ctypes.POINTER(F), P, Z, P]),
+            "sats_selftest_distill_timeout": (I, [P, I64, I, I, P, P, P, I64, I, P, P]),
         }
         for name, (res, args) in sig.items():
             fn = getattr(L, name)
@@ -113,7 +114,7 @@ def exported_symbols() -> Sequence[str]:
             "sats_top_logits", "sats_top_logits_f32", "sats_distill_loss", "sats_distill_loss_f32",
             "sats_distill_grad", "sats_distill_grad_f32", "sats_distill_loss_grad", "sats_distill_loss_grad_f32",
             "sats_sample", "sats_sample_f32", "sats_get_error", "sats_get_status_word", "sats_selftest_wait_timeout",
-            "sats_selftest_select_timeout")
+            "sats_selftest_select_timeout", "sats_selftest_distill_timeout")
 
 
 def status_string(s: int) -> str:
@@ -570,6 +571,20 @@ def selftest_select_timeout(a: torch.Tensor, sel_ws: torch.Tensor, stream: Optio
     s = lib().sats_selftest_select_timeout(_ptr(a, "a", 4), a.numel(), ctypes.byref(out), _ptr(sel_ws, "sel_ws"),
                                            sel_ws.numel() * sel_ws.element_size(), _stream(stream))
     return int(s), float(out.value)
+
+
+def selftest_distill_timeout(logits: torch.Tensor, labels: torch.Tensor, loss: torch.Tensor, dlogits: torch.Tensor,
+                             row: int, dev_status: torch.Tensor, stream: Optional[torch.cuda.Stream] = None):
+    """distill_loss_grad on bf16 logits with labels alone, the sums of one CTA of `row` withheld from another; the next
+    get_status_word(dev_status) reads ETIMEOUT (takes about 4 s) where a row has more than one CTA."""
+    z, ld, T, V, f32, dev = _rows(logits, "logits")
+    if f32:
+        raise ValueError("logits must be bf16")
+    d, ld_d = _dlogits(dlogits, logits)
+    _check(lib().sats_selftest_distill_timeout(z, ld, T, V, _beside(labels, "labels", torch.int32, (T,), dev),
+                                               _beside(loss, "loss", torch.float32, (T,), dev), d, ld_d, row,
+                                               _beside(dev_status, "dev_status", torch.int32, (1,), dev),
+                                               _stream(stream)), "sats_selftest_distill_timeout")
 
 
 def get_error(ws: Workspace, stream: Optional[torch.cuda.Stream] = None) -> int:
