@@ -85,15 +85,35 @@ __device__ __forceinline__ bool mbar_try_wait(uint64_t *bar, uint32_t parity)
     return ok != 0;
 }
 
+// The same for a phase that the stores of other CTAs of the cluster complete: what they stored is ordered before the
+// reads that follow (the scope of a CTA does not take in the senders).
+__device__ __forceinline__ bool mbar_try_wait_cluster(uint64_t *bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(smem_addr(bar)), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
+
 // Waits for the phase with the given parity to complete.  Gives up after
 // kWaitLimitNs or as soon as *abort becomes non-zero; returns false then.
-template <bool HINT = false>
+// CLUSTER: mbar_try_wait_cluster.
+template <bool HINT = false, bool CLUSTER = false>
 __device__ __forceinline__ bool mbar_wait(uint64_t *bar, uint32_t parity, volatile int *abort)
 {
-    if (mbar_try_wait<HINT>(bar, parity)) return true;
+    const auto done = [&] {
+        if constexpr (CLUSTER) return mbar_try_wait_cluster(bar, parity);
+        else return mbar_try_wait<HINT>(bar, parity);
+    };
+    if (done()) return true;
     const unsigned long long t0 = global_ns();
     for (;;) {
-        if (mbar_try_wait<HINT>(bar, parity)) return true;
+        if (done()) return true;
         if (*abort) return false;
         if (global_ns() - t0 > kWaitLimitNs) return false;
     }

@@ -850,7 +850,7 @@ __global__ void __launch_bounds__(TH, kStepPerSm * kStepThreads / TH) distill_st
                 for (int i = tid; i < p.slots; i += TH) seen.slot[i] = -1;   // (all have looked; a barrier ahead of the next row)
             }
             if (C > 1) {
-                met = !alone && mbar_wait(&arrived[turn], (uses >> 1) & 1, &gave_up);
+                met = !alone && mbar_wait<false, true>(&arrived[turn], (uses >> 1) & 1, &gave_up);
                 sum = get_sum<NT>(csum[turn][lane & (C - 1)]);
                 warp_join(sum, c, C);
                 if (!met) {
