@@ -134,7 +134,7 @@ __device__ __forceinline__ unsigned long long weight(float z, const Scale &s, co
     return w.in[0] ? whole_weight(w.i1[0], w.i2[0], s) : 0ull;
 }
 
-// f * total for 0 <= f < 1, exactly and rounded down (and up): shares of a mass at a border are not to depend on a
+// f * total for 0 <= f < 1 (not -0), exactly and rounded down (and up): shares of a mass at a border are not to depend on a
 // rounded product.
 __device__ __forceinline__ unsigned long long share_floor(float f, unsigned long long total, bool *exact)
 {
@@ -856,7 +856,7 @@ struct Settings {
         T = p.temperature ? p.temperature[row] : 1.f;
         top_p = p.top_p ? p.top_p[row] : 1.f;
         min_p = p.min_p ? p.min_p[row] : 0.f;
-        u = p.u[row];
+        u = p.u[row] + 0.f;   // (-0 is 0)
         k = p.top_k ? p.top_k[row] : 0;
         bad = !(T >= 0.f) || T == INFINITY || top_p != top_p || !(min_p <= 1.f) || !(u >= 0.f && u < 1.f);
         if (k < 0 || k >= p.V) k = 0;

@@ -3,6 +3,9 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import vocab
+from tests.test_gpu_top_logits import logits, rows
+
 pytestmark = pytest.mark.gpu
 
 
@@ -35,3 +38,22 @@ def test_nucleus_of_millions_of_equal_tokens(sats, V, apart, dtype):
     assert ids.tolist() == [int(np.floor(x * m)) * step for x, m in zip(u, kept)]
     # the logarithm of a whole number, rounded a few times
     np.testing.assert_allclose(lp.cpu().numpy(), -np.log(np.array(kept, np.float64)), rtol=2.0 ** -21)
+
+
+@pytest.mark.parametrize("dtype,V", [(torch.float32, 5), (torch.float32, 1000), (torch.bfloat16, 5003), (torch.float32, 100003)])
+@pytest.mark.parametrize("kw", [dict(), dict(top_k=20), dict(top_k=700), dict(top_p=0.5), dict(min_p=0.1), dict(temperature=-0.0)])
+def test_negative_zeros_are_zeros(sats, dtype, V, kw):
+    # a random number of -0 lies in [0, 1): the first kept token
+    z = rows(logits("normal", 4, V, 93), dtype, pad=1)
+    dev = lambda a, t: torch.tensor(a, dtype=t, device="cuda")
+    args = {k: dev([v] * 4, torch.int32 if k == "top_k" else torch.float32) for k, v in kw.items()}
+    got = []
+    for u in ([-0.0, 0.0, -0.0, 0.25], [0.0, 0.0, 0.0, 0.25]):
+        ids = torch.full((4,), -7, dtype=torch.int32, device="cuda")
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        sats.sample(z, dev(u, torch.float32), ids, dev_status=status, **args)
+        assert sats.get_status_word(status) == sats.OK
+        got.append(ids.tolist())
+    ref = {k: [v] * 4 for k, v in kw.items()}
+    ri = vocab.sample(z.double().cpu().numpy(), np.array([0.0, 0.0, 0.0, 0.25]), **ref)[0]
+    assert got[0] == got[1] == ri.tolist()
