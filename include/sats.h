@@ -486,8 +486,9 @@ SATS_API sats_status sats_route_calibrate(const float *score, int V, const int32
  *   g          : device fp32 [T], the gradient of each row's loss, or NULL for 1.
  *   dlogits    : device, the logits' type, rows of V elements ld_d >= V apart,
  *                written (each value rounded once).  It may be the logits
- *                themselves (the same pointer and row stride); any other
- *                overlap returns SATS_EINVAL.
+ *                themselves (the same pointer and row stride), or lie between
+ *                their rows (the same row stride); any other overlap of the two
+ *                areas returns SATS_EINVAL.
  *
  * sats_distill_loss_grad -- both in one pass over the logits, for a caller who
  *   knows g beforehand (a mean over the batch): loss and dlogits as above.

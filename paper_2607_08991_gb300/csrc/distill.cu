@@ -1086,7 +1086,8 @@ sats_status check_distill(const DistillParams &p)
     return SATS_OK;
 }
 
-// The gradient may overwrite the logits (the same rows at the same places); any other overlap is refused.
+// The gradient may overwrite the logits (the same rows at the same places) or lie between their rows, equally far apart;
+// any other overlap of the two areas is refused.
 template <bool F32>
 bool bad_overlap(const DistillParams &p)
 {
@@ -1094,7 +1095,12 @@ bool bad_overlap(const DistillParams &p)
     const uintptr_t z0 = reinterpret_cast<uintptr_t>(p.z), d0 = reinterpret_cast<uintptr_t>(p.d);
     const uintptr_t z1 = z0 + (uintptr_t)((p.T - 1) * p.ldz + p.V) * B, d1 = d0 + (uintptr_t)((p.T - 1) * p.ldd + p.V) * B;
     if (z0 == d0 && (p.T == 1 || p.ldz == p.ldd)) return false;
-    return z0 < d1 && d0 < z1;
+    if (!(z0 < d1 && d0 < z1)) return false;
+    if (p.T == 1 || p.ldz != p.ldd) return true;
+    // how far behind the beginning of a row of the logits one of the gradient begins
+    const uintptr_t step = (uintptr_t)p.ldz * B, row = (uintptr_t)p.V * B;
+    const uintptr_t behind = d0 >= z0 ? (d0 - z0) % step : (step - (z0 - d0) % step) % step;
+    return behind < row || behind > step - row;
 }
 
 sats_status launched(cudaError_t e) { return e == cudaSuccess ? SATS_OK : cuda_fail(e, "distillation kernel launch"); }

@@ -57,3 +57,36 @@ def test_negative_zeros_are_zeros(sats, dtype, V, kw):
     ref = {k: [v] * 4 for k, v in kw.items()}
     ri = vocab.sample(z.double().cpu().numpy(), np.array([0.0, 0.0, 0.0, 0.25]), **ref)[0]
     assert got[0] == got[1] == ri.tolist()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T,V,gap", [(5, 900, 0), (400, 900, 7), (30, 60001, 3)])
+def test_gradient_between_the_rows_of_the_logits(sats, T, V, gap, dtype):
+    # one buffer, in turn a row of logits and a row for its gradient, either of them first
+    g = np.random.default_rng([94, T])
+    values = logits("normal", T, V, 95)
+    y = torch.from_numpy(g.integers(-1, V, T).astype(np.int32)).cuda()
+    z = rows(values, dtype)
+    loss, lse, d = torch.zeros(T, device="cuda"), torch.zeros(T, 2, device="cuda"), torch.zeros_like(z)
+    sats.distill_loss(z, None, None, y, 1.0, 0.0, loss, lse=lse)
+    sats.distill_grad(z, None, None, y, 1.0, 0.0, lse, d)
+    for first in (True, False):
+        for one_pass in (False, True):
+            buf = torch.full((T, 2 * V + 2 * gap), 9.0, dtype=dtype, device="cuda")
+            own, out = buf[:, :V], buf[:, V + gap:2 * V + gap]
+            if not first:
+                own, out = out, own
+            own.copy_(z)
+            l2 = torch.zeros(T, device="cuda")
+            if one_pass:
+                sats.distill_loss_grad(own, None, None, y, 1.0, 0.0, l2, out)
+            else:
+                sats.distill_loss(own, None, None, y, 1.0, 0.0, l2)
+                sats.distill_grad(own, None, None, y, 1.0, 0.0, lse, out)
+            torch.cuda.synchronize()
+            assert torch.equal(own, z) and (buf[:, V:V + gap] == 9).all() and (buf[:, 2 * V + gap:] == 9).all()
+            # the sums in another order: within 2^-15 of one another (absolute, of a loss and of a probability; the
+            # gradient's rounding to its type on top)
+            assert ((l2 - loss).abs() <= 2.0 ** -14).all()
+            eps = 2.0 ** -7 if dtype == torch.bfloat16 else 2.0 ** -22
+            assert ((out.float() - d.float()).abs() <= 2.0 ** -14 + eps * d.float().abs()).all()
