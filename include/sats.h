@@ -474,7 +474,8 @@ SATS_API sats_status sats_route_calibrate(const float *score, int V, const int32
  *   dev_status : device int32 [1] or NULL.  An index or label >= V sets it
  *                (SATS_EDEVICE from sats_get_status_word); the entry is then
  *                absent, the row an ignored one.
- *   A row with a NaN or +inf logit, or with none above -inf, has the loss NaN.
+ *   A row with a NaN or +inf logit, or with none above -inf, has the loss NaN if a
+ *   term counts there (entries, with alpha > 0; a label, with alpha < 1), else 0.
  *   Logits are divided by tau in fp32: where tau < 1, what of them passes fp32's
  *   range counts as an infinity in lse.
  *
@@ -482,7 +483,10 @@ SATS_API sats_status sats_route_calibrate(const float *score, int V, const int32
  *     dlogits_j = g (alpha tau (softmax(z / tau)_j - sum_{k: top_idx_k = j} q_k)
  *                    + (1 - alpha) (softmax(z)_j - [j = label]))
  *   from the same arguments and the lse that sats_distill_loss wrote, whose
- *   rounding it inherits: 2^-24 |lse| relative.
+ *   rounding it inherits: 2^-24 |lse| relative.  Of a row whose loss its logits
+ *   make NaN it is NaN everywhere; if g is 0 or no term counts, 0 but for NaN at
+ *   the NaN and +inf logits.  A NaN or +inf value makes it NaN at the row's
+ *   entries.
  *   g          : device fp32 [T], the gradient of each row's loss, or NULL for 1.
  *   dlogits    : device, the logits' type, rows of V elements ld_d >= V apart,
  *                written (each value rounded once).  It may be the logits

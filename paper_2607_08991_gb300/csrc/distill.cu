@@ -346,7 +346,8 @@ __device__ __forceinline__ float kd_part(const Entries &e, int K, const Shares &
 
 // d_j = A 2^(x_0) + B 2^(x_1), less the targets; with one exponential (NT 1) it is one of the two, or both at tau = 1
 // in A.  From sums, x = (z - off) c; from log-sum-exps, x = (z / tau - lse) log2 e: the difference comes first, it is
-// exact where the probability is large.  A coefficient of 0 is exactly 0, also for a row that has no sum.
+// exact where the probability is large.  A coefficient of 0 is exactly 0, also for a row that has no sum (but at its NaN and
+// +inf logits).
 template <int NT, bool LSE>
 struct GradFn {
     float A, B, s0, a0, m0, a1;

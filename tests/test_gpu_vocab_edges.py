@@ -4,6 +4,7 @@ import pytest
 import torch
 
 from oracle import vocab
+from tests.test_gpu_distill import check, to_dev
 from tests.test_gpu_top_logits import logits, rows
 
 pytestmark = pytest.mark.gpu
@@ -90,3 +91,60 @@ def test_gradient_between_the_rows_of_the_logits(sats, T, V, gap, dtype):
             assert ((l2 - loss).abs() <= 2.0 ** -14).all()
             eps = 2.0 ** -7 if dtype == torch.bfloat16 else 2.0 ** -22
             assert ((out.float() - d.float()).abs() <= 2.0 ** -14 + eps * d.float().abs()).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T,V", [(12, 500), (12, 60001), (700, 500), (260, 60001)])
+@pytest.mark.parametrize("tau,alpha,labels,entries", [(1.0, 0.0, True, False), (1.0, 0.5, True, True), (2.0, 0.5, True, True),
+                                                      (2.0, 1.0, False, True), (2.0, 0.5, False, True), (1.0, 1.0, True, True)])
+def test_rows_without_a_finite_sum(sats, T, V, tau, alpha, labels, entries, dtype):
+    # all three calls, one row a cluster and many, one CTA a row and several: the rows that are not ordinary ones have NaN
+    # where the header says so, the others are what they would be without them
+    K, n = 6, 9
+    g = np.random.default_rng([96, T, V])
+    z = logits("normal", T, V, 97)
+    idx = np.stack([g.permutation(V)[:K] for _ in range(T)]).astype(np.int32)
+    val = g.normal(0, 2, (T, K)).astype(np.float32)
+    y = g.integers(0, V, T).astype(np.int32)
+    up = g.uniform(0.5, 1.5, T).astype(np.float32)
+    at = g.permutation(T)[:n]                        # where the special rows are
+    nan_at, inf_at = int(g.integers(0, V)), int(g.integers(0, V))
+    for r in at[[0, 4, 6]]:
+        z[r, nan_at] = np.nan
+    for r in at[[1, 7]]:
+        z[r, inf_at] = np.inf
+    z[at[[2, 8]]] = -np.inf
+    up[at[[4, 8]]] = 0.0                             # of which one has no weight ...
+    idx[at[[6, 7]]] = -1                             # ... or no entries
+    val[at[3], 2], val[at[5], 0] = np.nan, np.inf    # a teacher's value that is none
+    zd = rows(z, dtype, pad=1)
+    a = (to_dev(idx) if entries else None, to_dev(val) if entries else None, to_dev(y) if labels else None)
+    loss, loss2, lse = torch.zeros(T, device="cuda"), torch.zeros(T, device="cuda"), torch.zeros(T, 2, device="cuda")
+    d, d2 = torch.zeros_like(zd), torch.zeros_like(zd)
+    sats.distill_loss(zd, *a, tau, alpha, loss, lse=lse)
+    sats.distill_grad(zd, *a, tau, alpha, lse, d, g=to_dev(up))
+    sats.distill_loss_grad(zd, *a, tau, alpha, loss2, d2, g=to_dev(up))
+    soft, hard = entries and alpha > 0, labels and alpha < 1
+    nan_loss = np.zeros(T, bool)
+    nan_grad = np.zeros((T, V), bool)
+    for r in at:
+        counts = hard or (soft and (idx[r] >= 0).any())
+        numbers = np.isfinite(z[r]) | (z[r] == -np.inf)
+        odd_row = not numbers.all() or not np.isfinite(z[r]).any()
+        odd_val = soft and not np.isfinite(val[r]).all()
+        nan_loss[r] = odd_row and counts or odd_val
+        if odd_row:
+            nan_grad[r] = ~numbers if up[r] == 0 or not counts else True
+        elif odd_val:
+            nan_grad[r, idx[r]] = True
+    for got, name in ((loss, "loss"), (loss2, "one-pass loss")):
+        assert np.array_equal(torch.isnan(got).cpu().numpy(), nan_loss), name
+    for got, name in ((d, "gradient"), (d2, "one-pass gradient")):
+        got = got.float().cpu().numpy()
+        assert np.array_equal(np.isnan(got), nan_grad), (name, np.argwhere(np.isnan(got) != nan_grad)[:5], at)
+        gone = at[[r for r in range(n) if nan_grad[at[r]].any() and not nan_grad[at[r]].all() and r not in (3, 5)]]
+        assert (np.nan_to_num(got[gone]) == 0).all()
+    rest = np.setdiff1d(np.arange(T), at)[:40]
+    pick = lambda x: None if x is None else x[rest]
+    check(sats, rows(z[rest], dtype, pad=1), pick(idx) if entries else None, pick(val) if entries else None,
+          pick(y) if labels else None, pick(up), tau, alpha, d_pad=1)
