@@ -522,7 +522,8 @@ SATS_API sats_status sats_route_calibrate(const float *score, int V, const int32
  *   T < 0, min_p > 1, u outside [0, 1)) gives the id -1, logprob NaN and n_kept 0 and
  *   sets *dev_status (device int32 [1] or NULL; SATS_EDEVICE).
  *   The weights are whole multiples of 2^-43 of the largest (of 2^-(62 - bits of V)
- *   from V = 2^18 on), right to about 35 bits of themselves; their sums are exact.
+ *   from V = 2^18 on), right to about 35 bits of themselves (to fewer above
+ *   T = 2^110, whose inverse has fewer in fp32); their sums are exact.
  */
 SATS_API sats_status sats_top_logits(const void *logits, int64_t ld, int T, int V, int K, float *values, int32_t *idx,
                                      void *stream);
