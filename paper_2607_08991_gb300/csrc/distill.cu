@@ -27,7 +27,7 @@ constexpr size_t kMaxSmem = kSmemPerCta - 2 * 1024;   // dynamic: a row's share,
 // Threads, CTAs to an SM and the share of a row that a CTA of the one-pass kernel has on chip (where the cluster allows),
 // 4096 rows of 128256 bf16 logits before its clusters stayed for many rows (us): 256 x 3, 72 KB 450; 256 x 4, 72 KB 455;
 // 256 x 4, 40 KB 563; 512 x 2, 72 KB 581; 128 x 8, 40 KB 460.  The backward pass with 256 x 4 takes 197 us where 512 x 2
-// took 273 (1000 rows of 151936 fp32 logits), the loss 347 where it took 371 (8192 rows of 151936 bf16 ones).  Powers of
+// took 273 (1000 rows of 151936 fp32 logits), the loss 352 where it took 371 (8192 rows of 151936 bf16 ones).  Powers of
 // two: sums over warps halve their number.
 constexpr size_t kStepShare = 72 * 1024;
 constexpr int kLossThreads = 256, kGradThreads = 256, kStepThreads = 256, kStepPerSm = 3;
@@ -517,8 +517,8 @@ __device__ __forceinline__ int2 whole_of(const Row<F32> &r, int2 run)
 }
 
 // ------------------------------------------------------------------ the loss
-// One row per cluster, read once: bounded by HBM.  8192 rows of 151936 bf16 logits (one in twenty ignored) take 350 us,
-// 6.76 TB/s of what is read (a copy reaches 6.78); 37 rows of 128256 fp32 ones with two temperatures 11 us, most of it a
+// One row per cluster, read once: bounded by HBM.  8192 rows of 151936 bf16 logits (one in twenty ignored) take 352 us,
+// 6.71 TB/s of what is read (a copy reaches 6.78); 37 rows of 128256 fp32 ones with two temperatures 11 us, most of it a
 // launch and two barriers of the cluster.  With 50 entries at tau 2 (two exponentials an element) the 8192 rows take 401.
 template <bool F32, int NT, int TH>
 __global__ void __launch_bounds__(TH, 1024 / TH) distill_loss_kernel(const DistillParams p)
@@ -695,7 +695,7 @@ __global__ void __launch_bounds__(TH, 1024 / TH) distill_grad_kernel(const Disti
 // from then on, so that it neither arms nor waits nor sends any more and leaves NaN in its part of all rows to come.  The
 // others miss its sums in the next row, and do the same after one more limit at most.
 // 4096 rows of 128256 bf16 logits with 64 entries, read once and written once, take 377 us, 5.4 TB/s; one row per cluster
-// and launch took 450.  Without entries it is 335 us, with 1000 of them 544, at tau 2 (two exponentials) 464: what bounds
+// and launch took 450.  Without entries it is 333 us, with 1000 of them 544, at tau 2 (two exponentials) 466: what bounds
 // it is the issue of instructions (an exponential an element in the sums and another in the gradient, 24 warps to an SM)
 // and the latency of the chain sums - exchange - gradient in each row, which two other CTAs on the SM cover in part.
 // SHIFT: some rows of the gradient lie on other 16-byte boundaries than the logits' rows; a warp then has a run of
@@ -963,10 +963,10 @@ size_t al16(size_t v) { return (v + 15) & ~(size_t)15; }
 
 // CTAs of a row: one where the rows alone fill the GPU with `fill` CTAs to an SM, more where they do not, as long as each
 // still has a granule for each of `threads`; and as many as it takes for the share that stays on chip to leave room for
-// other CTAs on the SM.  Measured with 1 / 2 / 4 / 8 CTAs a row (us; 151936 bf16 or fp32 logits): loss, as it was with 512
-// threads, of 76 rows 14.8 / 12.0 / 11.4 / 16.0, of 304 rows 20.7 / 25.0 / 31.8 / 45.7, of 1216 rows 65 / 83 / 110 / 160 (a
-// cluster costs about a microsecond of every wave); gradient of 76 rows 46 / 30 / 26 / 22, of 304 rows 72 / 66 / 68 / 71, of
-// 1216 rows 235 / 234 / 238 / 256.
+// other CTAs on the SM.  Measured with 1 / 2 / 4 / 8 CTAs a row (us; 151936 bf16 or fp32 logits): loss of 76
+// rows 20.0 / 14.1 / 11.4 / 10.8, of 304 rows 25.6 / 22.1 / 23.6 / 31.7 (the rule's 1 is not the best there), of 1216 rows
+// 61 / 69 / 77 / 103 (a cluster costs about a microsecond of every wave); gradient of 76 rows 46 / 30 / 26 / 22, of 304 rows
+// 73 / 66 / 67 / 67, of 1216 rows 236 / 234 / 239 / 241.
 int row_cluster(int T, int64_t row_bytes, size_t share, int fill, int threads)
 {
     int C = 1;
@@ -983,8 +983,8 @@ static_assert((kLossThreads & (kLossThreads - 1)) == 0 && (kGradThreads & (kGrad
 
 // Rows that are short go to smaller CTAs, more of them to an SM: what a row costs apart from its elements (the sums over
 // warps, the exchange, the entries) is latency.  8192 rows of bf16 logits with 128 / 256 threads (us): loss of 1000 logits
-// 19 / 53 (there 512), gradient 34 / 59, both in one pass 51 / 87; 4000 rows of 16000 30 / 36, 57 / 66 and 65 / 77, of
-// 32000 46 / 49, 98 / 102 and 126 / 108, of 128256 159 / 156 and 346 / 333.  With 1000 entries the one-pass kernel is
+// 19 / 28, gradient 34 / 59, both in one pass 52 / 86; 4000 rows of 16000 30 / 36, 57 / 65 and 64 / 76, of 32000 46 / 49,
+// 98 / 102 and 127 / 108, of 128256 159 / 156 and 345 / 333 (loss and gradient).  With 1000 entries the one-pass kernel is
 // slower with fewer threads (8000 logits: 283 / 237), with 200 not (93 / 119).
 constexpr int kShortThreads = 128;
 constexpr int64_t kShortBytes = 32 * 1024;

@@ -699,9 +699,9 @@ constexpr int kSms = 152;
 // CTAs of a row: one where the rows alone fill the GPU, more where they do not, as long as each has a few granules per
 // thread; with few rows so many that a row's list of `want` entries falls to them in parts of at most kSmall; and so many
 // that a share of at most `share` bytes (0: any) is left to each.  Top logits of 128256 bf16 ones with 1 / 2 / 4 / 8 CTAs
-// (us): 38 rows, K 64 16.8 / 13.1 / 11.5 / 12.5; 304 rows 23.5 / 22.4 / 34.3 / 51.3; 1216 rows 64 / 75 / 101 / 170.  At
-// K 1000 (lists of more than kSmall sorted, as it was): 38 rows 47 / 36 / 40 / 19, 76 rows 53 / 38 / 52 / 32, 152 rows
-// 57 / 50 / 68 / 51, 304 rows 69 / 79 / 109 / 87.
+// (us): 38 rows, K 64 15.4 / 13.0 / 11.6 / 12.1; 76 rows 18.3 / 14.6 / 13.2 / 21.3; 304 rows 23.2 / 22.4 / 34.6 / 51.2;
+// 1216 rows 63 / 75 / 102 / 170.  At K 1000: 38 rows 33.8 / 23.3 / 20.0 / 19.4, 76 rows 40 / 25.5 / 22.5 / 32.5 (here the
+// rule's 8 are not the best: clusters of eight begin a second wave), 152 rows 45 / 29 / 36 / 51, 304 rows 49 / 39 / 53 / 88.
 int logits_cluster(int rows, int64_t row_bytes, int want, size_t share)
 {
     int C = 1;

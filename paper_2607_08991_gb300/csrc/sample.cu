@@ -23,7 +23,7 @@ namespace sats {
 namespace {
 
 constexpr int kAhead = 8;              // granules in flight per thread while the row arrives
-// Of a row's bytes per CTA, where the cluster allows (300 fp32 top-p rows with 128 KB 346 us, with 64 KB 236).
+// Of a row's bytes per CTA, where the cluster allows (300 fp32 top-p rows with 128 KB 307 us, with 64 KB 233).
 constexpr size_t kShare = 64 * 1024;
 constexpr size_t kMaxCache = 182 * 1024;
 constexpr size_t kMaxSmem = kMaxCache + (size_t)kListCap * 8;
@@ -985,7 +985,7 @@ __device__ __forceinline__ void sample_row(Ctx<F32> &c, const SampleParams &p, i
 }
 
 // The row in shared memory, three CTAs of 256 threads to an SM (1024 x 1, 512 x 2, 256 x 4 and 128 x 6 were slower).  300 rows
-// of 100003 fp32 logits with top-p take 227 us, where reading them takes 18: the counting pass issues about 25 and the
+// of 100003 fp32 logits with top-p take 233 us, where reading them takes 18: the counting pass issues about 25 and the
 // exact pass about 60 instructions an element (a weight of 35 bits is some 20 operations on pairs of floats), over half of
 // the issue slots that there are, and five barriers of the cluster stand between the passes.  Four rows of 1000: 10.8 us.
 //
@@ -1019,9 +1019,9 @@ __global__ void __launch_bounds__(kSelThreads, kSelPerSm) sample_kernel(const Sa
 // follows exactly from the counts and one weight per value.  Only the CTA in which the token lies reads its tokens again
 // (from the L2) and adds their weights from a table of the values.
 //
-// 512 rows of 128256 bf16 logits (19 us of reading) take 139 us free, 168 with top-p, 156 with a top-k of up to 1000, 92
-// with min-p, 76 with a top-k of at most 192, 53 greedy; with the row in shared memory (sample_kernel) they took 156, 368,
-// 196, 114, 100 and 59.  A count is about ten instructions a token, an addition in shared memory among them: 57 us until
+// 512 rows of 128256 bf16 logits (19 us of reading) take 135 us free, 165 with top-p, 155 with a top-k of up to 1000, 90
+// with min-p, 74 with a top-k of 50, 53 greedy; with the row in shared memory (sample_kernel) they take 159, 373, 198, 115,
+// 101 and 59.  A count is about ten instructions a token, an addition in shared memory among them: 57 us until
 // the row is counted, 36 if it were only read.  Then 25 to 50 us go into the weights of 4096 values, the border and two
 // exchanges, and 35 to 45 into the one CTA of a row that adds its tokens' weights (two lookups of 8 bytes in the table
 // cost a conflict of banks each): chains of latency, covered by three other CTAs on the SM.
@@ -1033,14 +1033,14 @@ constexpr int kSteps = 2 * kBins;   // two counts of 16 bits in a word
 constexpr int kFewMax = kSelThreads;
 constexpr int kLeastMag = 117 << 7, kFarMag = 133 << 7;   // magnitudes as bits
 static_assert(kFarMag - kLeastMag == kSteps / 2, "a step for each value");
-constexpr int kValuesPerSm = 4;   // (3, with more registers: 256 mixed rows 111 us instead of 99)
-// Tokens of a row: with 4096 steps a row, short rows of a free draw are slower this way (512 rows of 8000: 32 us against
-// 22; of 32000: 55 against 47), all others faster (of 8000 with top-p 42 against 48, top-k 43 against 69; at 2000 34 and
-// 26 free against 39 and 15).
+constexpr int kValuesPerSm = 4;   // (3, with more registers: 256 mixed rows 83 us, 512 free ones 140; with 4 81 and 135)
+// Tokens of a row: with 4096 steps a row, short rows of a free draw are slower this way (512 rows of 8000: 31 us against
+// 22; of 32000: 52 against 49), all others faster (of 8000 with top-p 42 against 49, top-k 43 against 70; of 2000 with top-p
+// 34 against 40, free 26 against 15).  One rule whatever the settings: which of them a row uses the host does not know.
 constexpr int kValuesFrom = 4096;
 constexpr int kValuesTo = 65536 - 128;     // of a CTA: counts of 16 bits
-// Of a row's bytes per CTA, where the cluster allows: 256 mixed rows of 151936 take 83 us with 4 CTAs and 99 with 8, 512
-// top-p rows of 128256 168 with 4 CTAs, 184 with 2 and 203 with 8.
+// Of a row's bytes per CTA, where the cluster allows: 256 mixed rows of 151936 take 81 us with 4 CTAs and 98 with 8, 512
+// top-p rows of 128256 165 with 4 CTAs, 177 with 2 and 209 with 8.
 constexpr size_t kValuesShare = 96 * 1024;
 constexpr int kValuesTop = 192;            // the largest top-k that goes by a list (of which kSmall need no sorting)
 constexpr uint32_t kNoWay = 0xffffffffu;

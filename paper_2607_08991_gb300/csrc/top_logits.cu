@@ -104,7 +104,7 @@ __device__ __forceinline__ bool put_by_steps(const unsigned long long *list, int
 // 2048 rows of 128256 bf16 logits at K 64 take 106 us, 4.95 TB/s, where 78 us is the stream: the rest is the chain after
 // it (histogram, one or two exchanges, the candidates), 6 to 8 us that the three other CTAs on the SM cover in part; one
 // row of 151936 takes 10.8 us.  With the rows kept in shared memory (2 CTAs to an SM) it was 210, with clusters that stay
-// for many rows and fetch ahead 329.  At K 400 and 1000 1216 rows take 91 and 127 us, at K 64 64.
+// for many rows and fetch ahead 329.  At K 400 and 1000 1216 rows take 90 and 126 us, at K 64 63.
 // FEW: few_groups.
 template <bool F32, bool FEW>
 __global__ void __launch_bounds__(kSelThreads, kSelPerSm) top_kernel(const TopParams p)
