@@ -477,7 +477,7 @@ SATS_API sats_status sats_route_calibrate(const float *score, int V, const int32
  *   A row with a NaN or +inf logit, or with none above -inf, has the loss NaN if a
  *   term counts there (entries, with alpha > 0; a label, with alpha < 1), else 0.
  *   Logits are divided by tau in fp32: where tau < 1, what of them passes fp32's
- *   range counts as an infinity in lse.
+ *   range counts as an infinity in lse.  A probability below 2^-126 may count as 0.
  *
  * sats_distill_grad -- its backward pass:
  *     dlogits_j = g (alpha tau (softmax(z / tau)_j - sum_{k: top_idx_k = j} q_k)

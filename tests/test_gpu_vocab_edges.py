@@ -148,3 +148,43 @@ def test_rows_without_a_finite_sum(sats, T, V, tau, alpha, labels, entries, dtyp
     pick = lambda x: None if x is None else x[rest]
     check(sats, rows(z[rest], dtype, pad=1), pick(idx) if entries else None, pick(val) if entries else None,
           pick(y) if labels else None, pick(up), tau, alpha, d_pad=1)
+
+
+def test_calls_at_once_on_two_streams(sats):
+    # eager calls on one stream while another replays a captured one: nothing is shared between them
+    V, T, K = 60001, 300, 16
+    z = [rows(logits("normal", T, V, 98 + i), torch.bfloat16, pad=i) for i in range(2)]
+    y = torch.arange(T, dtype=torch.int32, device="cuda")
+    u = torch.linspace(0, 0.999, T, device="cuda")
+
+    def outputs():
+        return (torch.zeros(T, K, device="cuda"), torch.zeros(T, K, dtype=torch.int32, device="cuda"),
+                torch.zeros(T, device="cuda"), torch.zeros(T, V, dtype=torch.bfloat16, device="cuda"),
+                torch.zeros(T, dtype=torch.int32, device="cuda"))
+
+    def calls(x, o, stream=None):
+        sats.top_logits(x, o[0], o[1], stream=stream)
+        sats.distill_loss_grad(x, o[1], o[0], y, 2.0, 0.5, o[2], o[3], stream=stream)
+        sats.sample(x, u, o[4], stream=stream)
+
+    alone = [outputs() for _ in range(2)]
+    for x, o in zip(z, alone):
+        calls(x, o)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [outputs() for _ in range(2)]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=streams[0]):
+        calls(z[0], got[0], streams[0])
+    for _ in range(4):
+        for o in got:
+            for t in o:
+                t.zero_()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(streams[0]):
+            graph.replay()
+        calls(z[1], got[1], streams[1])
+        torch.cuda.synchronize()
+        for a, b in zip(alone, got):
+            assert all(torch.equal(s, t) for s, t in zip(a, b))
