@@ -28,7 +28,8 @@
  *     sats_get_error; a call that synchronises returns them itself.
  *     sats_gate_act and sats_gate_act_f32 have no status word: a wait that
  *     runs out leaves NaN in a.  No call aborts, throws, or traps on the device.
- *   - Calls never allocate device memory, except sats_layer_create.
+ *   - Calls never allocate device memory, except sats_layer_create,
+ *     sats_lora_create and sats_q4_create.
  *   - Requirements: H a multiple of 8 and 8 <= H <= 8192; N >= 1; B >= 0.
  *   - SM occupancy: the single-token / two-token decode kernel (the small-batch
  *     path of sats_sparse_mlp and the calls built on it) runs one CTA on every
@@ -71,6 +72,7 @@ typedef enum {
 /* Opaque handle of one MLP block; owns its repacked device weights. */
 typedef struct sats_layer sats_layer;
 typedef struct sats_lora sats_lora;
+typedef struct sats_q4 sats_q4;
 
 /* Library version, (major << 16) | minor. */
 SATS_API int sats_version(void);
@@ -557,6 +559,107 @@ SATS_API sats_status sats_sample(const void *logits, int64_t ld, int B, int V, c
 SATS_API sats_status sats_sample_f32(const float *logits, int64_t ld, int B, int V, const float *temperature,
                                      const int32_t *top_k, const float *top_p, const float *min_p, const float *u,
                                      int32_t *ids, float *logprob, int32_t *n_kept, int32_t *dev_status, void *stream);
+
+/*
+ * Adjusted logits: what lies between the model's logits and sats_sample, and its gradient.
+ * logits, out, dout, dlogits are rows as in the vocabulary operators above (any alignment of whole
+ * elements, row strides of at least V elements).  The calls need no workspace, and what they write does not depend on the
+ * order in which their threads run.  V up to 2^31 - 65, 2^28 - 1 rows, L up to 2^30 (else SATS_ESHAPE).
+ *
+ * sats_adjust_logits -- for each of B rows z with its history of token ids:
+ *     z_v <- z_v > 0 ? z_v / r : z_v r      where v occurs in the history
+ *     z_v <- z_v - f c_v - p                where v occurs c_v > 0 times in the generated part of it
+ *     z_v <- z_v + bias_v
+ *     z_v <- -inf                           where the mask does not allow v
+ *   in fp32, rounded once.
+ *   hist       : device int32, row b at b * ld_hist, L ids at most (ld_hist 0: all rows share one; rows may overlap), or
+ *                NULL with L 0 (then hist_len and n_prompt are not looked at).  Ids below 0 are absent.
+ *   hist_len   : device int32 [B], how many ids of its row count (NULL: L).
+ *   n_prompt   : device int32 [B] or NULL for 0: the first n_prompt ids are the prompt, the others are generated.
+ *   repetition, presence, frequency : r, p, f, device fp32 [B] or NULL for off (1, 0, 0).  r > 0, all finite.
+ *                The history of a row whose three are off is not read.
+ *   bias_idx, bias_val : device int32 and fp32 [B][M] (M up to 1024, else SATS_ESHAPE; NULL if 0).  An index below 0 is an
+ *                absent entry; of entries with the same index the last one counts.  -inf makes the logit -inf.
+ *   mask       : device int32 words of 32 tokens each (bit v mod 32 of word v / 32: v is allowed), row i at i * ld_mask
+ *                (ld_mask >= ceil(V / 32)), n_masks rows; or NULL.
+ *   mask_row   : device int32 [B], the mask of each row; below 0: none.  NULL: mask b for row b (n_masks >= B).
+ *   out        : the logits' type; the logits themselves (same pointer and stride), or between their rows (same
+ *                stride), or elsewhere (another overlap: SATS_EINVAL).  In place only what changes is touched: a call
+ *                without a mask costs what its histories cost, whatever V is.
+ *   dev_status : device int32 [1] or NULL.  Set (SATS_EDEVICE) by a setting outside its range, which is off then; an id
+ *                or index >= V, a NaN or +inf bias, which are absent then; a length outside [0, L], which is taken as
+ *                the nearer of the two; a mask_row >= n_masks, which is none.
+ *   A NaN logit stays NaN unless it becomes -inf.
+ *
+ * sats_adjust_logits_grad -- its backward pass: dlogits_v = dout_v times 0 where the mask does not allow v (also where
+ *   dout is not finite), 1 / r or r where v occurs in the history (r at z_v = 0), else 1.  The biases and the other two
+ *   penalties are constants here.  logits: what sats_adjust_logits was given, read only at the tokens of the history.
+ *   dlogits may be dout or the logits (same pointer and stride), or lie between their rows.
+ */
+SATS_API sats_status sats_adjust_logits(const void *logits, int64_t ld, int B, int V, const int32_t *hist,
+                                        int64_t ld_hist, int L, const int32_t *hist_len, const int32_t *n_prompt,
+                                        const float *repetition, const float *presence, const float *frequency,
+                                        const int32_t *bias_idx, const float *bias_val, int M, const void *mask,
+                                        int64_t ld_mask, int n_masks, const int32_t *mask_row, void *out,
+                                        int64_t ld_out, int32_t *dev_status, void *stream);
+SATS_API sats_status sats_adjust_logits_f32(const float *logits, int64_t ld, int B, int V, const int32_t *hist,
+                                            int64_t ld_hist, int L, const int32_t *hist_len, const int32_t *n_prompt,
+                                            const float *repetition, const float *presence, const float *frequency,
+                                            const int32_t *bias_idx, const float *bias_val, int M, const void *mask,
+                                            int64_t ld_mask, int n_masks, const int32_t *mask_row, float *out,
+                                            int64_t ld_out, int32_t *dev_status, void *stream);
+SATS_API sats_status sats_adjust_logits_grad(const void *logits, int64_t ld, int B, int V, const int32_t *hist,
+                                             int64_t ld_hist, int L, const int32_t *hist_len, const float *repetition,
+                                             const void *mask, int64_t ld_mask, int n_masks, const int32_t *mask_row,
+                                             const void *dout, int64_t ld_dout, void *dlogits, int64_t ld_d,
+                                             int32_t *dev_status, void *stream);
+SATS_API sats_status sats_adjust_logits_grad_f32(const float *logits, int64_t ld, int B, int V, const int32_t *hist,
+                                                 int64_t ld_hist, int L, const int32_t *hist_len,
+                                                 const float *repetition, const void *mask, int64_t ld_mask,
+                                                 int n_masks, const int32_t *mask_row, const float *dout,
+                                                 int64_t ld_dout, float *dlogits, int64_t ld_d, int32_t *dev_status,
+                                                 void *stream);
+
+/*
+ * 4-bit weights with group scales: a matrix W [K][N] (y = x W; the vocabulary head, a projection) as whole numbers
+ * from -8 to 7 times a scale for every G consecutive k of a column:
+ *     W[k][n] = scales[k / G][n] * q[k][n]
+ *   codes  : uint8 [K / 2][N]; byte (i, n) holds q[2i][n] in its low and q[2i + 1][n] in its high half (two's complement)
+ *   scales : bf16 [ceil(K / G)][N], any sign; one that is not finite makes its column of y NaN.
+ * K a multiple of 8 and 8 <= K <= 65536; 1 <= N <= 2^24; G 32, 64 or 128 (else SATS_ESHAPE).
+ *
+ * sats_q4_quantize -- codes and scales (device, written) of a bf16 matrix W (device [K][N], rows ld >= N elements
+ *   apart): over each group s = amax / 7 rounded to bf16, q = w / s rounded half to even, within [-7, 7].  A group with a NaN or an
+ *   infinity gets the scale NaN.
+ * sats_q4_dequantize -- what codes and scales stand for: values device fp32 [K][N], exact.
+ *
+ * sats_q4_create -- packs codes and scales (device) into a handle, which owns its device memory (K N / 2 bytes, the
+ *   scales, 4 bytes per column).  Runs on `stream` and synchronises it; the caller may then free both.  Within a
+ *   column scales are kept to 8 significant bits from its largest one down to 2^-21 of it, below as multiples of 2^-29 of it.
+ * sats_q4_destroy frees it (synchronises the device first); sats_q4_shape reads back K, N, G (each may be NULL).
+ *
+ * sats_q4_matmul -- y = x W for B tokens (up to 2^20): x device bf16 [B][K] (fp32 in the _f32 call), y device [B][N], rows ld_y >= N
+ *   elements apart, fp32 if y_f32 is not 0, else bf16.  The tensor cores multiply the weights exactly and the activations
+ *   to 11 (bf16) or 22 (fp32) significant bits, absolute 2^-39 (2^-50) of a token's largest; sums are rounded to
+ *   fp32 every 128 products.  A token's result does not depend on the order in which the threads run.
+ *   ws: device, 256-byte aligned, of sats_q4_workspace_bytes(K, N, B) bytes (0: shape out of range), zero-filled once
+ *   before first use (sats_workspace_init), left ready for the next call; calls that share one must not overlap on the
+ *   GPU.  A bounded wait that gives up leaves y incomplete, sats_get_error(ws) says SATS_ETIMEOUT, and the workspace has to be
+ *   zero-filled again.
+ */
+SATS_API sats_status sats_q4_quantize(const void *W, int64_t ld, int K, int N, int G, uint8_t *codes, void *scales,
+                                      void *stream);
+SATS_API sats_status sats_q4_dequantize(const uint8_t *codes, const void *scales, int K, int N, int G, float *values,
+                                        void *stream);
+SATS_API sats_status sats_q4_create(const uint8_t *codes, const void *scales, int K, int N, int G, void *stream,
+                                    sats_q4 **out);
+SATS_API sats_status sats_q4_destroy(sats_q4 *w);
+SATS_API sats_status sats_q4_shape(const sats_q4 *w, int *K, int *N, int *G);
+SATS_API size_t sats_q4_workspace_bytes(int K, int N, int B);
+SATS_API sats_status sats_q4_matmul(const sats_q4 *w, const void *x, int B, void *y, int64_t ld_y, int y_f32, void *ws,
+                                    size_t ws_bytes, void *stream);
+SATS_API sats_status sats_q4_matmul_f32(const sats_q4 *w, const float *x, int B, void *y, int64_t ld_y, int y_f32,
+                                        void *ws, size_t ws_bytes, void *stream);
 
 /*
  * sats_selftest_wait_timeout -- exercises the failure path of the device-side

@@ -182,7 +182,7 @@ using namespace sats;
 
 extern "C" {
 
-int sats_version(void) { return (1 << 16) | 2; }
+int sats_version(void) { return (1 << 16) | 3; }
 
 const char *sats_status_string(sats_status s)
 {

@@ -1,0 +1,741 @@
+// q4.cu -- 4-bit weights with group scales: the product of rows of activations with them on the tensor cores
+// (sats_q4_matmul), their making from bf16 weights and reading back (sats_q4_quantize, sats_q4_dequantize), and the
+// handle that keeps them packed (sats_q4_create).
+//
+// A weight is s q, q a whole number from -8 to 7 and s the bf16 scale of its group of G (32, 64, 128) consecutive k: 11
+// significant bits at most, which is what fp16 has.  So the product runs in fp16 MMAs without rounding a weight: every
+// column's scales are divided by a power of two (kept beside them) that puts the largest at 2^10..2^11, and every
+// token's activations by one that puts the largest at 2^14..2^15; fp32 activations go as two fp16 parts.
+//
+// The weights are the A operand (128 of them a tile, M) and stay 4 bits wide until they are in registers: two
+// warpgroups turn a stage of 128 k into fp16 pairs and store them to TMEM, where the MMA reads its A operand from;
+// only the activations (N, the tokens) lie in shared memory as the MMA wants them.  Through shared memory the fp16
+// weights would cost four times the bytes that arrive from HBM, written once and read once.
+#include <algorithm>
+#include <climits>
+#include <cuda_fp16.h>
+#include <new>
+
+#include "tc_common.cuh"
+
+struct sats_q4 {
+    int K = 0, N = 0, G = 0, device = 0;
+    uint8_t *blk = nullptr;   // [row tiles][stages]: blocks as described at kCodeBytes
+    int *col_exp = nullptr;   // [N rounded up to 128]: the power of two that a column's scales were divided by
+};
+
+namespace sats {
+namespace {
+using namespace tc;
+
+constexpr int kRows = 128;                    // columns of the weight matrix in a tile (MMA M)
+constexpr int kStageK = 128;                  // k of a stage
+constexpr int kCodeBytes = kRows * kStageK / 2;
+// A block: for each half of 64 k and each piece of 32 k the 16 bytes of every row (row after row), then the fp16 scales,
+// group after group, 128 rows each.
+// A word holds 8 codes u = q + 8, those of k = 2p in its low and 2p + 1 in its high half, p = 0..3: bits 6..9, 10..13,
+// 2..5 of the half, and for p = 3 bits 14..17 of the word (even) and 30, 31, 0, 1 (odd), so that shifts by 4, -4 and a
+// rotation by 8 bring each pair to bits 6..9, where with the exponent of 1024 it reads as 64 (16 + u).
+constexpr int kMaxK = 65536;
+constexpr int64_t kMaxQ4N = (int64_t)1 << 24;
+constexpr int kMaxCtas = 320;                 // of the product's kernel
+constexpr int kLoShift = 11;                  // the second part of an fp32 activation is kept 2^11 times larger
+constexpr int kMaxSplitTiles = 10 * kMaxCtas; // more tiles are not split (launch_q4)
+constexpr int kCtlBytes = 256;
+
+__host__ __device__ constexpr int block_bytes(int G) { return kCodeBytes + kStageK / G * kRows * 2; }
+__host__ __device__ constexpr int div_up(int a, int b) { return (a + b - 1) / b; }
+
+// ------------------------------------------------------------------ quantising
+// amax over the group, s = bf16(amax / 7), q = w / s rounded half to even.  w / s is either a tie or further than 2^-10
+// from one (a ratio of two numbers of 8 bits), so a product with 1 / s that is first rounded to a multiple of 2^-11
+// decides as the division does.  A group with an infinity or a NaN gets the scale NaN and codes 0.
+constexpr int kQuantThreads = 128;
+
+__device__ __forceinline__ uint32_t quant_nibble(float w, float r, float s, bool tiny)
+{
+    constexpr float kGrid = 6144.f;        // 1.5 x 2^12: adding it leaves multiples of 2^-11
+    constexpr float kWhole = 12582912.f;   // 1.5 x 2^23: of 1
+    if (!tiny) {
+        const float snapped = __fsub_rn(__fmaf_rn(w, r, kGrid), kGrid);
+        return __float_as_uint(__fadd_rn(snapped, kWhole)) & 15u;
+    }
+    if (!(s > 0.f)) return 0u;
+    const float q = fminf(fmaxf(rintf(__fdiv_rn(w, s)), -7.f), 7.f);
+    return (uint32_t)(int)q & 15u;
+}
+
+__global__ void __launch_bounds__(kQuantThreads) q4_quantize_kernel(const uint16_t *W, int64_t ld, int K, int N, int G,
+                                                                     uint8_t *codes, uint16_t *scales)
+{
+    const int64_t n = (int64_t)blockIdx.x * kQuantThreads + threadIdx.x;
+    if (n >= N) return;
+    for (int g = blockIdx.y; g < div_up(K, G); g += gridDim.y) {
+        const int k0 = g * G, k1 = min(K, k0 + G);
+        const uint16_t *w = W + (int64_t)k0 * ld + n;
+        uint32_t top = 0;
+        for (int k = k0; k < k1; ++k) top = max(top, (uint32_t)w[(int64_t)(k - k0) * ld] & 0x7fffu);
+        const bool odd = top >= 0x7f80u;
+        const uint16_t sb = odd ? 0x7fc0u : bf16_bits(__fdiv_rn(__uint_as_float(top << 16), 7.f));
+        const float s = __uint_as_float((uint32_t)sb << 16);
+        const bool tiny = !(s >= 1.17549435e-38f);
+        const float r = tiny ? 0.f : __frcp_rn(s);
+        scales[(int64_t)g * N + n] = sb;
+        for (int k = k0; k < k1; k += 2) {
+            const float a = __uint_as_float((uint32_t)w[(int64_t)(k - k0) * ld] << 16);
+            const float b = __uint_as_float((uint32_t)w[(int64_t)(k + 1 - k0) * ld] << 16);
+            const uint32_t c = odd ? 0u : quant_nibble(a, r, s, tiny) | quant_nibble(b, r, s, tiny) << 4;
+            codes[(int64_t)(k / 2) * N + n] = (uint8_t)c;
+        }
+    }
+}
+
+__device__ __forceinline__ float code_value(uint32_t nibble) { return (float)((int)(nibble << 28) >> 28); }
+
+__global__ void __launch_bounds__(256) q4_dequantize_kernel(const uint8_t *codes, const uint16_t *scales, int K, int N, int G,
+                                                            float *values)
+{
+    const int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (n >= N) return;
+    for (int k2 = blockIdx.y; k2 < K / 2; k2 += gridDim.y) {
+        const uint32_t c = codes[(int64_t)k2 * N + n];
+        const float s = __uint_as_float((uint32_t)scales[(int64_t)(2 * k2 / G) * N + n] << 16);
+        values[(int64_t)(2 * k2) * N + n] = code_value(c) * s;
+        values[(int64_t)(2 * k2 + 1) * N + n] = code_value(c >> 4) * s;
+    }
+}
+
+// ------------------------------------------------------------------ packing
+// The power of two of each column: its largest finite scale becomes 2^10..2^11 (64 times what the block holds).
+__global__ void __launch_bounds__(128) q4_columns_kernel(const uint16_t *scales, int groups, int N, int *col_exp)
+{
+    const int64_t n = (int64_t)blockIdx.x * 128 + threadIdx.x;
+    uint32_t top = 0;
+    if (n < N)
+        for (int g = 0; g < groups; ++g) {
+            const uint32_t s = scales[(int64_t)g * N + n] & 0x7fffu;
+            if (s < 0x7f80u) top = max(top, s);
+        }
+    col_exp[n] = top ? ilogbf(__uint_as_float(top << 16)) - 10 : 0;
+}
+
+__global__ void __launch_bounds__(128) q4_pack_kernel(const uint8_t *codes, const uint16_t *scales, int K, int N, int G,
+                                                      const int *col_exp, uint8_t *blk)
+{
+    const int r = threadIdx.x, ks = blockIdx.x;
+    const int64_t rt = (int64_t)blockIdx.z * 65535 + blockIdx.y, n = rt * kRows + r;
+    if (rt * kRows >= N) return;
+    uint8_t *const b = blk + (rt * gridDim.x + ks) * block_bytes(G);
+    for (int piece = 0; piece < 4; ++piece) {
+        uint32_t w[4];
+        for (int i = 0; i < 4; ++i) {
+            uint32_t v = 0;
+            for (int p = 0; p < 4; ++p) {
+                const int k = ks * kStageK + piece * 32 + i * 8 + 2 * p;
+                const uint32_t c = (n < N && k < K) ? codes[(int64_t)(k / 2) * N + n] : 0u;
+                const uint32_t even = (c & 15u) ^ 8u, odd = (c >> 4) ^ 8u;   // q + 8
+                if (p < 3) {
+                    const int at = p == 0 ? 6 : p == 1 ? 10 : 2;
+                    v |= even << at | odd << (at + 16);
+                } else v |= even << 14 | odd << 30 | odd >> 2;
+            }
+            w[i] = v;
+        }
+        reinterpret_cast<uint4 *>(b)[piece * kRows + r] = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    __half *const sc = reinterpret_cast<__half *>(b + kCodeBytes);
+    for (int j = 0; j < kStageK / G; ++j) {
+        const int g = (ks * kStageK) / G + j;
+        float s = 0.f;
+        if (n < N && g * G < K) s = __uint_as_float((uint32_t)scales[(int64_t)g * N + n] << 16);
+        sc[j * kRows + r] = __float2half_rn(scalbnf(s, -col_exp[n] - 6));
+    }
+}
+
+// ------------------------------------------------------------------ activations
+// Tokens in tiles; for a tile and a stage of 128 k two halves of 64 k, each TN rows of 128 bytes in the order that the
+// 128-byte swizzle of the MMA's operand has.  With fp32 activations the first TN / 2 rows are the tokens' first parts,
+// the others their second ones.
+constexpr int kStageThreads = 256;
+
+struct StageParams {
+    const void *x;
+    char *xs;
+    int *tok_exp;
+    int B, K, KS, TN, per_tile;   // per_tile: tokens of a tile
+};
+
+template <bool F32>
+__global__ void __launch_bounds__(kStageThreads) q4_stage_kernel(const StageParams p)
+{
+    grid_launch_dependents();
+    __shared__ uint32_t top_s[kStageThreads / 32];
+    const int tid = threadIdx.x;
+    const int64_t b = blockIdx.x;
+    auto bits = [&](int k) -> uint32_t {
+        if constexpr (F32) return __float_as_uint(static_cast<const float *>(p.x)[b * p.K + k]);
+        else return (uint32_t) static_cast<const uint16_t *>(p.x)[b * p.K + k] << 16;
+    };
+    uint32_t top = 0;
+    for (int k = tid; k < p.K; k += kStageThreads) {
+        const uint32_t m = bits(k) & 0x7fffffffu;
+        if (m < 0x7f800000u) top = max(top, m);
+    }
+    top = __reduce_max_sync(0xffffffffu, top);
+    if ((tid & 31) == 0) top_s[tid >> 5] = top;
+    __syncthreads();
+    for (int i = 0; i < kStageThreads / 32; ++i) top = max(top, top_s[i]);
+    const int e = top ? ilogbf(__uint_as_float(top)) - 14 : 0;
+    if (tid == 0 && blockIdx.y == 0) p.tok_exp[b] = e;
+    const float f1 = scalbnf(1.f, -e / 2), f2 = scalbnf(1.f, -e - -e / 2);   // 2^-e alone can be out of range
+
+    const int tile = (int)(b / p.per_tile), row = (int)(b % p.per_tile);
+    char *const base = p.xs + (int64_t)tile * p.KS * p.TN * 256;
+    // 8 consecutive k are 16 bytes of a row
+    for (int c = blockIdx.y * kStageThreads + tid; c < p.KS * 16; c += gridDim.y * kStageThreads) {
+        uint32_t hi[4], lo[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            __half h[2], l[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int k = 8 * c + 2 * i + j;
+                const float v = k < p.K ? __uint_as_float(bits(k)) * f1 * f2 : 0.f;
+                h[j] = __float2half_rn(v);
+                const float rest = (v - __half2float(h[j])) * (float)(1 << kLoShift);
+                l[j] = __float2half_rn(isfinite(rest) ? rest : 0.f);
+            }
+            hi[i] = (uint32_t)__half_as_ushort(h[0]) | (uint32_t)__half_as_ushort(h[1]) << 16;
+            lo[i] = (uint32_t)__half_as_ushort(l[0]) | (uint32_t)__half_as_ushort(l[1]) << 16;
+        }
+        const int ks = c >> 4, half = c >> 3 & 1, piece = c & 7;
+        auto put = [&](int r, const uint32_t (&v)[4]) {
+            char *const at = base + ((int64_t)ks * 2 + half) * p.TN * 128 + r * 128 + ((piece ^ (r & 7)) << 4);
+            *reinterpret_cast<uint4 *>(at) = make_uint4(v[0], v[1], v[2], v[3]);
+        };
+        put(row, hi);
+        if constexpr (F32) put(p.TN / 2 + row, lo);
+    }
+}
+
+// ------------------------------------------------------------------ the product
+struct Q4Params {
+    const uint8_t *blk;
+    const int *col_exp;
+    const char *xs;
+    const int *tok_exp;
+    void *y;
+    int64_t ld_y;
+    int B, N, KS, TT, per_tile;   // TT: token tiles
+    int G;
+    int64_t units;                // of `quantum` stages each, all tiles one after another
+    int quantum;
+    int stages;                   // of the shared-memory ring
+    bool y_f32;
+    float *partial;               // [2 kMaxCtas][TN][128]
+    int *counters;                // [tiles], 0 between calls
+    int *ctl;
+};
+
+constexpr int kQ4Threads = 32 * 14;
+constexpr int kQ4MaxStages = 8;
+
+// Stages [begin, end) of CTA c; tile = stage / KS.
+__device__ __forceinline__ int64_t range_begin(const Q4Params &p, int64_t c)
+{
+    return p.units * c / gridDim.x * p.quantum;
+}
+
+// D += A B with A (fp16) in TMEM.
+__device__ __forceinline__ void mma_f16_tmem_if(uint32_t lead, uint32_t d_tmem, uint32_t a_tmem, uint64_t b,
+                                                uint32_t idesc, uint32_t acc)
+{
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_tmem), "l"(b), "r"(idesc), "r"(acc), "r"(lead)
+        : "memory");
+}
+
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+        "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]),
+        "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]),
+        "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+        : "memory");
+}
+
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// The 8 codes of a word times the group's scale, as fp16 pairs in the order of k: 64 (16 + u) t - 1536 t = (u - 8) 64 t
+// in one multiply-add, exact in its product, in 1536 t (10 bits) and in the result (11 bits).
+__device__ __forceinline__ void dequant8(uint32_t w, __half2 t, __half2 c, uint32_t *out)
+{
+    const uint32_t v[4] = {w, w >> 4, w << 4, __byte_perm(w, w, 0x0321)};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t m = (v[i] & 0x03c003c0u) | 0x64006400u;
+        const __half2 h = __hfma2(*reinterpret_cast<const __half2 *>(&m), t, c);
+        out[i] = *reinterpret_cast<const uint32_t *>(&h);
+    }
+}
+
+struct Q4Bars {
+    uint64_t full[kQ4MaxStages], empty[kQ4MaxStages];
+    uint64_t a_full[4][2], a_empty[4];
+    uint64_t d_full[2], d_empty[2];
+    uint64_t drain;
+};
+
+// TN: tokens of a tile (MMA N); NA: stages of fp16 weights in TMEM; PER_SM: resident CTAs.
+template <int TN, int NA, int PER_SM, bool F32>
+__global__ void __launch_bounds__(kQ4Threads, PER_SM) q4_matmul_kernel(const __grid_constant__ Q4Params p)
+{
+    constexpr int kCols = (2 * TN + NA * 64) <= 256 ? 256 : 512;   // TMEM: two accumulators, then the weights
+    constexpr int kX = TN * 256;                                   // bytes of the activations of a stage
+    constexpr uint32_t kIdesc = (1u << 4) | ((uint32_t)(TN >> 3) << 17) | ((uint32_t)(kRows >> 4) << 24);
+    static_assert(2 * TN + NA * 64 <= 512 && NA <= 4, "TMEM");
+    extern __shared__ char smem_raw[];
+    __shared__ Q4Bars bars;
+    __shared__ uint32_t tmem_slot;
+    __shared__ volatile int abort_flag;
+    __shared__ int last_flag;
+
+    const int warp = uniform_warp(), lane = threadIdx.x & 31;
+    char *const ring = reinterpret_cast<char *>(align1024(reinterpret_cast<uint8_t *>(smem_raw)));
+    const int blk = block_bytes(p.G);
+    char *const wring = ring + (size_t)p.stages * kX;
+    const int64_t begin = range_begin(p, blockIdx.x), end = range_begin(p, blockIdx.x + 1);
+    const int n_it = (int)(end - begin);
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kQ4MaxStages; ++i) {
+            mbar_init(&bars.full[i], 1);
+            mbar_init(&bars.empty[i], 9);   // eight warps that have read the codes, the MMAs that have read the activations
+        }
+        for (int i = 0; i < 4; ++i) {
+            mbar_init(&bars.a_full[i][0], 4);
+            mbar_init(&bars.a_full[i][1], 4);
+            mbar_init(&bars.a_empty[i], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&bars.d_full[i], 1);
+            mbar_init(&bars.d_empty[i], 4);
+        }
+        mbar_init(&bars.drain, 1);
+        abort_flag = 0;
+        mbar_init_fence();
+    }
+    if (warp == 13) tmem_alloc(&tmem_slot, kCols);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot;
+
+    if (warp == 12) {
+        // ---- loads
+        const uint32_t lead = elect_one();
+        auto load_w = [&](int it) {
+            const int s = it % p.stages;
+            const int64_t pos = begin + it, tile = pos / p.KS;
+            mbar_expect_if(lead, &bars.full[s], (uint32_t)(blk + kX));
+            bulk_load_shared_if(lead, wring + (size_t)s * blk,
+                                p.blk + ((tile / p.TT) * p.KS + (pos - tile * p.KS)) * blk, (uint32_t)blk, &bars.full[s]);
+        };
+        auto load_x = [&](int it) {
+            const int s = it % p.stages;
+            const int64_t pos = begin + it, tile = pos / p.KS;
+            bulk_load_shared_if(lead, ring + (size_t)s * kX, p.xs + ((tile % p.TT) * p.KS + (pos - tile * p.KS)) * kX,
+                                (uint32_t)kX, &bars.full[s]);
+        };
+        // the weights do not depend on the kernel that stages the activations
+        const int ahead = min(n_it, p.stages);
+        for (int it = 0; it < ahead; ++it) load_w(it);
+        grid_dependency_wait();
+        for (int it = 0; it < ahead; ++it) load_x(it);
+        int issued = ahead;
+        for (int it = ahead; it < n_it; ++it) {
+            if (!warp_wait(&bars.empty[it % p.stages], (uint32_t)((it / p.stages - 1) & 1), &abort_flag)) {
+                if (lane == 0) set_timeout(p.ctl, &abort_flag);
+                break;
+            }
+            load_w(it);
+            load_x(it);
+            issued = it + 1;
+        }
+        // nothing may arrive after the CTA's end
+        int never = 0;
+        for (int it = max(0, issued - p.stages); it < issued; ++it)
+            warp_wait(&bars.full[it % p.stages], (uint32_t)((it / p.stages) & 1), &never);
+    } else if (warp == 13) {
+        // ---- MMAs
+        const uint32_t lead = elect_one();
+        bool ok = true;
+        for (int it = 0; it < n_it && ok; ++it) {
+            const int s = it % p.stages, a = it % NA, d = it & 1;
+            ok = warp_wait(&bars.full[s], (uint32_t)((it / p.stages) & 1), &abort_flag);
+            if (ok && it >= 2) ok = warp_wait(&bars.d_empty[d], (uint32_t)((it / 2 - 1) & 1), &abort_flag);
+            const uint32_t xb = smem_addr(ring + (size_t)s * kX);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (ok) ok = warp_wait(&bars.a_full[a][h], (uint32_t)((it / NA) & 1), &abort_flag);
+                if (!ok) break;
+                tc_fence_after();
+                const uint64_t desc = smem_desc(xb + h * (TN * 128));
+#pragma unroll
+                for (int k = 0; k < 4; ++k)   // 16 k: 8 columns of TMEM, 32 bytes of the swizzled rows
+                    mma_f16_tmem_if(lead, tmem + d * TN, tmem + 2 * TN + a * 64 + h * 32 + k * 8, desc + 2 * k, kIdesc,
+                                    (uint32_t)(h + k > 0));
+            }
+            if (!ok) break;
+            mma_commit_if(lead, &bars.empty[s]);
+            mma_commit_if(lead, &bars.a_empty[a]);
+            mma_commit_if(lead, &bars.d_full[d]);
+        }
+        if (!ok && lane == 0) set_timeout(p.ctl, &abort_flag);
+        mma_commit_if(lead, &bars.drain);
+        int never = 0;
+        warp_wait(&bars.drain, 0u, &never);
+    } else if (warp >= 4) {
+        // ---- weights to fp16: warps 4 to 7 the first 64 k of a stage, 8 to 11 the others
+        const int h = (warp - 4) >> 2, quad = warp & 3, r = quad * 32 + lane;
+        const int per = kStageK / p.G;
+        const int sub0 = (2 * h * per) >> 2, sub1 = ((2 * h + 1) * per) >> 2;
+        const uint32_t dst = tmem + ((uint32_t)(quad * 32) << 16) + 2 * TN + h * 32;
+        bool ok = true;
+        for (int it = 0; it < n_it; ++it) {
+            const int s = it % p.stages, a = it % NA;
+            ok = warp_wait(&bars.full[s], (uint32_t)((it / p.stages) & 1), &abort_flag);
+            if (ok && it >= NA) ok = warp_wait(&bars.a_empty[a], (uint32_t)((it / NA - 1) & 1), &abort_flag);
+            if (!ok) break;
+            const char *const w = wring + (size_t)s * blk;
+            const uint4 q0 = reinterpret_cast<const uint4 *>(w)[(2 * h) * kRows + r];
+            const uint4 q1 = reinterpret_cast<const uint4 *>(w)[(2 * h + 1) * kRows + r];
+            const __half *const sc = reinterpret_cast<const __half *>(w + kCodeBytes);
+            const __half2 t0 = __half2half2(sc[sub0 * kRows + r]), t1 = __half2half2(sc[sub1 * kRows + r]);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bars.empty[s]);
+            const __half2 k1536 = __float2half2_rn(-1536.f);
+            const __half2 c0 = __hmul2(t0, k1536), c1 = __hmul2(t1, k1536);
+            uint32_t v[32];
+            dequant8(q0.x, t0, c0, v);
+            dequant8(q0.y, t0, c0, v + 4);
+            dequant8(q0.z, t0, c0, v + 8);
+            dequant8(q0.w, t0, c0, v + 12);
+            dequant8(q1.x, t1, c1, v + 16);
+            dequant8(q1.y, t1, c1, v + 20);
+            dequant8(q1.z, t1, c1, v + 24);
+            dequant8(q1.w, t1, c1, v + 28);
+            tc_fence_after();
+            tmem_st32(dst + a * 64, v);
+            tmem_st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bars.a_full[a][h]);
+        }
+        if (!ok && lane == 0) set_timeout(p.ctl, &abort_flag);
+    } else {
+        // ---- sums: each stage's 128 products are added up by the MMAs, the stages here in fp32 (the accumulator truncates)
+        constexpr int kOut = F32 ? TN / 2 : TN;
+        const int r = threadIdx.x;
+        float acc[TN];
+#pragma unroll
+        for (int i = 0; i < TN; ++i) acc[i] = 0.f;
+        bool ok = true;
+        for (int it = 0; it < n_it; ++it) {
+            const int d = it & 1;
+            ok = warp_wait(&bars.d_full[d], (uint32_t)((it / 2) & 1), &abort_flag);
+            if (!ok) break;
+            tc_fence_after();
+#pragma unroll
+            for (int c = 0; c < TN; c += 16) {
+                float v[16];
+                tmem_ld16(tmem + ((uint32_t)(warp * 32) << 16) + d * TN + c, v);
+                tmem_ld_wait();
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[c + i] += v[i];
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bars.d_empty[d]);
+
+            const int64_t pos = begin + it, tile = pos / p.KS;
+            const int ks = (int)(pos - tile * p.KS);
+            if (ks != p.KS - 1 && it != n_it - 1) continue;
+            // the end of a tile or of this CTA's share of one
+            if constexpr (F32)
+#pragma unroll
+                for (int i = 0; i < kOut; ++i) acc[i] += acc[i + TN / 2] * (1.f / (1 << kLoShift));
+            const int tt = (int)(tile % p.TT);
+            const int64_t n = (tile / p.TT) * kRows + r;
+            const int tokens = min(p.per_tile, p.B - tt * p.per_tile);
+            const int64_t t0 = tile * p.KS, t1 = t0 + p.KS;
+            bool write = true;
+            if (begin > t0 || ks != p.KS - 1) {
+                // the CTAs of the tile leave their sums in the workspace; the last one to come adds them in order
+                float *const mine = p.partial + (size_t)(2 * blockIdx.x + (begin < t0 ? 1 : 0)) * TN * kRows;
+#pragma unroll
+                for (int i = 0; i < kOut; ++i)
+                    if (i < tokens) __stcg(mine + i * kRows + r, acc[i]);
+                __threadfence();
+                named_barrier(1, 128);
+                // CTAs c0..c1 hold stages of the tile
+                int64_t c0 = blockIdx.x, c1 = blockIdx.x;
+                while (range_begin(p, c0) > t0) --c0;
+                while (range_begin(p, c1 + 1) < t1) ++c1;
+                if (r == 0) {
+                    const int old = atom_add_acq_rel_gpu(p.counters + tile, 1);
+                    last_flag = old == (int)(c1 - c0);
+                    if (last_flag) p.counters[tile] = 0;
+                }
+                named_barrier(1, 128);
+                write = last_flag != 0;
+                if (write) {
+                    __threadfence();
+#pragma unroll
+                    for (int i = 0; i < kOut; ++i) acc[i] = 0.f;
+                    for (int64_t c = c0; c <= c1; ++c) {
+                        const float *const part = p.partial + (size_t)(2 * c + (range_begin(p, c) < t0 ? 1 : 0)) * TN * kRows;
+#pragma unroll
+                        for (int i = 0; i < kOut; ++i)
+                            if (i < tokens) acc[i] += __ldcg(part + i * kRows + r);
+                    }
+                }
+            }
+            if (write && n < p.N) {
+                const int ce = p.col_exp[n];
+#pragma unroll
+                for (int i = 0; i < kOut; ++i) {
+                    if (i >= tokens) break;
+                    const int64_t token = (int64_t)tt * p.per_tile + i;
+                    const float v = scalbnf(acc[i], ce + p.tok_exp[token]);
+                    if (p.y_f32) static_cast<float *>(p.y)[token * p.ld_y + n] = v;
+                    else static_cast<__nv_bfloat16 *>(p.y)[token * p.ld_y + n] = __float2bfloat16_rn(v);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < TN; ++i) acc[i] = 0.f;
+        }
+        if (!ok && lane == 0) set_timeout(p.ctl, &abort_flag);
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 13) tmem_dealloc(tmem, kCols);
+}
+
+// ------------------------------------------------------------------ host
+// Tokens of a tile: fp32 activations take two columns each.
+int tile_tokens(int B, bool f32)
+{
+    const int64_t cols = (int64_t)B * (f32 ? 2 : 1);
+    return cols <= 16 ? 16 : cols <= 32 ? 32 : cols <= 64 ? 64 : 128;
+}
+
+struct Q4Layout {
+    size_t counters, tok_exp, partial, xs, total;
+};
+
+size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
+
+// For fp32 activations, which need the larger workspace.
+Q4Layout q4_layout(int K, int N, int B)
+{
+    Q4Layout L{};
+    const int b = std::max(B, 1);
+    size_t xs = 0, partial = 0, tiles = 0;
+    for (int f = 0; f < 2; ++f) {
+        const int TN = tile_tokens(b, f != 0);
+        const size_t tt = (size_t)div_up(b, f ? TN / 2 : TN);
+        xs = std::max(xs, tt * div_up(K, kStageK) * TN * 256);
+        partial = std::max(partial, (size_t)2 * kMaxCtas * TN * kRows * 4);
+        tiles = std::max(tiles, std::min(tt * div_up(N, kRows), (size_t)kMaxSplitTiles));
+    }
+    L.counters = kCtlBytes;
+    L.tok_exp = L.counters + up256(tiles * 4);
+    L.partial = L.tok_exp + up256((size_t)b * 4);
+    L.xs = L.partial + up256(partial);
+    L.total = L.xs + xs;
+    return L;
+}
+
+bool q4_shape_ok(int64_t K, int64_t N, int G)
+{
+    return K >= 8 && K <= kMaxK && K % 8 == 0 && N >= 1 && N <= kMaxQ4N && (G == 32 || G == 64 || G == 128);
+}
+
+template <int TN, int NA, int PER_SM, bool F32>
+cudaError_t launch_q4(Q4Params p, cudaStream_t st)
+{
+    static std::atomic<int> configured[64];
+    const int stage = block_bytes(p.G) + TN * 256;
+    const int budget = PER_SM == 2 ? 110 * 1024 : 220 * 1024;
+    p.stages = std::min(kQ4MaxStages, (budget - 1024) / stage);
+    const size_t smem = (size_t)p.stages * stage + 1024;
+    cudaError_t e = set_smem(q4_matmul_kernel<TN, NA, PER_SM, F32>, smem, configured);
+    if (e != cudaSuccess) return e;
+    const int64_t tiles = (int64_t)div_up(p.N, kRows) * p.TT;
+    const int64_t most = std::min(kMaxCtas, PER_SM * sm_count());
+    // Whole tiles where they fill the CTAs evenly, else any number of stages each.
+    const int64_t waves = (tiles + most - 1) / most;
+    const bool whole = tiles * 10 >= waves * most * 9;
+    p.quantum = whole ? p.KS : 1;
+    p.units = whole ? tiles : tiles * p.KS;
+    const int grid = (int)std::min<int64_t>(most, p.units);
+    return launch_pdl_cfg(q4_matmul_kernel<TN, NA, PER_SM, F32>, dim3(grid), kQ4Threads, smem, st, p);
+}
+
+template <bool F32>
+cudaError_t run_q4(const sats_q4 *w, const void *x, int B, void *y, int64_t ld_y, bool y_f32, char *ws, cudaStream_t st)
+{
+    const Q4Layout L = q4_layout(w->K, w->N, B);
+    const int TN = tile_tokens(B, F32);
+    Q4Params p{};
+    p.blk = w->blk; p.col_exp = w->col_exp; p.xs = ws + L.xs;
+    p.tok_exp = reinterpret_cast<int *>(ws + L.tok_exp);
+    p.y = y; p.ld_y = ld_y; p.B = B; p.N = w->N; p.G = w->G; p.y_f32 = y_f32;
+    p.KS = div_up(w->K, kStageK);
+    p.per_tile = F32 ? TN / 2 : TN;
+    p.TT = div_up(B, p.per_tile);
+    p.partial = reinterpret_cast<float *>(ws + L.partial);
+    p.counters = reinterpret_cast<int *>(ws + L.counters);
+    p.ctl = reinterpret_cast<int *>(ws);
+
+    StageParams sp{x, ws + L.xs, reinterpret_cast<int *>(ws + L.tok_exp), B, w->K, p.KS, TN, p.per_tile};
+    // a token's pieces go to several CTAs where there are few tokens
+    const int split = B >= 128 ? 1 : std::max(1, std::min(div_up(p.KS * 16, kStageThreads), 128 / B));
+    q4_stage_kernel<F32><<<dim3(B, split), kStageThreads, 0, st>>>(sp);
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+    switch (TN) {
+    case 16: return launch_q4<16, 3, 2, F32>(p, st);
+    case 32: return launch_q4<32, 3, 2, F32>(p, st);
+    case 64: return launch_q4<64, 4, 1, F32>(p, st);
+    default: return launch_q4<128, 4, 1, F32>(p, st);
+    }
+}
+
+template <bool F32>
+sats_status q4_matmul(const sats_q4 *w, const void *x, int B, void *y, int64_t ld_y, int y_f32, void *ws, size_t ws_bytes,
+                      void *stream)
+{
+    if (!w || !ws || B < 0) return SATS_EINVAL;
+    if (reinterpret_cast<uintptr_t>(ws) % 256) return SATS_EINVAL;
+    if (ld_y < w->N) return SATS_EINVAL;
+    if (B > 1 << 20 || ld_y > (int64_t)1 << 40) return SATS_ESHAPE;
+    if (ws_bytes < q4_layout(w->K, w->N, B).total) return SATS_ENOSPACE;
+    if (B == 0) return SATS_OK;
+    if (!x || !y || reinterpret_cast<uintptr_t>(x) % (F32 ? 4 : 2) || reinterpret_cast<uintptr_t>(y) % (y_f32 ? 4 : 2))
+        return SATS_EINVAL;
+    const cudaError_t e = run_q4<F32>(w, x, B, y, ld_y, y_f32 != 0, static_cast<char *>(ws),
+                                      static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? SATS_OK : cuda_fail(e, "4-bit product kernel launch");
+}
+
+}  // namespace
+}  // namespace sats
+
+using namespace sats;
+
+extern "C" {
+
+sats_status sats_q4_quantize(const void *W, int64_t ld, int K, int N, int G, uint8_t *codes, void *scales, void *stream)
+{
+    if (ld < N) return SATS_EINVAL;
+    if (!q4_shape_ok(K, N, G) || ld > (int64_t)1 << 40) return SATS_ESHAPE;
+    if (!W || !codes || !scales || reinterpret_cast<uintptr_t>(W) % 2 || reinterpret_cast<uintptr_t>(scales) % 2)
+        return SATS_EINVAL;
+    const dim3 grid(div_up(N, kQuantThreads), std::min(div_up(K, G), 65535));
+    q4_quantize_kernel<<<grid, kQuantThreads, 0, static_cast<cudaStream_t>(stream)>>>(
+        static_cast<const uint16_t *>(W), ld, K, N, G, codes, static_cast<uint16_t *>(scales));
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? SATS_OK : cuda_fail(e, "quantising kernel launch");
+}
+
+sats_status sats_q4_dequantize(const uint8_t *codes, const void *scales, int K, int N, int G, float *values, void *stream)
+{
+    if (!q4_shape_ok(K, N, G)) return SATS_ESHAPE;
+    if (!codes || !scales || !values || reinterpret_cast<uintptr_t>(scales) % 2 || reinterpret_cast<uintptr_t>(values) % 4)
+        return SATS_EINVAL;
+    const dim3 grid(div_up(N, 256), std::min(K / 2, 65535));
+    q4_dequantize_kernel<<<grid, 256, 0, static_cast<cudaStream_t>(stream)>>>(
+        codes, static_cast<const uint16_t *>(scales), K, N, G, values);
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? SATS_OK : cuda_fail(e, "reading back kernel launch");
+}
+
+sats_status sats_q4_create(const uint8_t *codes, const void *scales, int K, int N, int G, void *stream, sats_q4 **out)
+{
+    if (!out) return SATS_EINVAL;
+    *out = nullptr;
+    if (!codes || !scales || reinterpret_cast<uintptr_t>(scales) % 2) return SATS_EINVAL;
+    if (!q4_shape_ok(K, N, G)) return SATS_ESHAPE;
+    sats_q4 *w = new (std::nothrow) sats_q4();
+    if (!w) return cuda_fail(cudaErrorMemoryAllocation, "host allocation");
+    w->K = K;
+    w->N = N;
+    w->G = G;
+    cudaGetDevice(&w->device);
+    const int rt = div_up(N, kRows), ks = div_up(K, kStageK);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const uint16_t *sc = static_cast<const uint16_t *>(scales);
+    cudaError_t e = cudaMalloc(&w->blk, (size_t)rt * ks * block_bytes(G));
+    if (e == cudaSuccess) e = cudaMalloc(&w->col_exp, (size_t)rt * kRows * sizeof(int));
+    if (e == cudaSuccess) {
+        q4_columns_kernel<<<rt, 128, 0, st>>>(sc, div_up(K, G), N, w->col_exp);
+        q4_pack_kernel<<<dim3(ks, std::min(rt, 65535), div_up(rt, 65535)), 128, 0, st>>>(codes, sc, K, N, G, w->col_exp, w->blk);
+        e = cudaGetLastError();
+    }
+    if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+    if (e != cudaSuccess) {
+        cudaFree(w->blk);
+        cudaFree(w->col_exp);
+        delete w;
+        return cuda_fail(e, "4-bit weights: allocation or packing");
+    }
+    *out = w;
+    return SATS_OK;
+}
+
+sats_status sats_q4_destroy(sats_q4 *w)
+{
+    if (!w) return SATS_EINVAL;
+    cudaDeviceSynchronize();
+    const cudaError_t e1 = cudaFree(w->blk), e2 = cudaFree(w->col_exp);
+    delete w;
+    if (e1 != cudaSuccess) return cuda_fail(e1, "cudaFree");
+    return e2 == cudaSuccess ? SATS_OK : cuda_fail(e2, "cudaFree");
+}
+
+sats_status sats_q4_shape(const sats_q4 *w, int *K, int *N, int *G)
+{
+    if (!w) return SATS_EINVAL;
+    if (K) *K = w->K;
+    if (N) *N = w->N;
+    if (G) *G = w->G;
+    return SATS_OK;
+}
+
+size_t sats_q4_workspace_bytes(int K, int N, int B)
+{
+    if (!q4_shape_ok(K, N, 32) || B < 0 || B > 1 << 20) return 0;
+    return q4_layout(K, N, B).total;
+}
+
+sats_status sats_q4_matmul(const sats_q4 *w, const void *x, int B, void *y, int64_t ld_y, int y_f32, void *ws,
+                           size_t ws_bytes, void *stream)
+{
+    return q4_matmul<false>(w, x, B, y, ld_y, y_f32, ws, ws_bytes, stream);
+}
+
+sats_status sats_q4_matmul_f32(const sats_q4 *w, const float *x, int B, void *y, int64_t ld_y, int y_f32, void *ws,
+                               size_t ws_bytes, void *stream)
+{
+    return q4_matmul<true>(w, x, B, y, ld_y, y_f32, ws, ws_bytes, stream);
+}
+
+}  // extern "C"

@@ -86,6 +86,18 @@ def lib() -> ctypes.CDLL:
             "sats_distill_loss_grad_f32": (I, [P, I64, I, I, P, P, I, P, F, F, P, P, P, I64, P, P]),
             "sats_sample": (I, [P, I64, I, I, P, P, P, P, P, P, P, P, P, P]),
             "sats_sample_f32": (I, [P, I64, I, I, P, P, P, P, P, P, P, P, P, P]),
+            "sats_adjust_logits": (I, [P, I64, I, I, P, I64, I, P, P, P, P, P, P, P, I, P, I64, I, P, P, I64, P, P]),
+            "sats_adjust_logits_f32": (I, [P, I64, I, I, P, I64, I, P, P, P, P, P, P, P, I, P, I64, I, P, P, I64, P, P]),
+            "sats_adjust_logits_grad": (I, [P, I64, I, I, P, I64, I, P, P, P, I64, I, P, P, I64, P, I64, P, P]),
+            "sats_adjust_logits_grad_f32": (I, [P, I64, I, I, P, I64, I, P, P, P, I64, I, P, P, I64, P, I64, P, P]),
+            "sats_q4_quantize": (I, [P, I64, I, I, I, P, P, P]),
+            "sats_q4_dequantize": (I, [P, P, I, I, I, P, P]),
+            "sats_q4_create": (I, [P, P, I, I, I, P, ctypes.POINTER(P)]),
+            "sats_q4_destroy": (I, [P]),
+            "sats_q4_shape": (I, [P, ctypes.POINTER(I), ctypes.POINTER(I), ctypes.POINTER(I)]),
+            "sats_q4_workspace_bytes": (Z, [I, I, I]),
+            "sats_q4_matmul": (I, [P, P, I, P, I64, I, P, Z, P]),
+            "sats_q4_matmul_f32": (I, [P, P, I, P, I64, I, P, Z, P]),
             "sats_get_error": (I, [P, Z, P]),
             "sats_get_status_word": (I, [P, P]),
             "sats_selftest_wait_timeout": (I, [P, Z, P]),
@@ -113,7 +125,10 @@ def exported_symbols() -> Sequence[str]:
             "sats_sats_calibrate", "sats_route_calib_workspace_bytes", "sats_token_scores", "sats_route_calibrate",
             "sats_top_logits", "sats_top_logits_f32", "sats_distill_loss", "sats_distill_loss_f32",
             "sats_distill_grad", "sats_distill_grad_f32", "sats_distill_loss_grad", "sats_distill_loss_grad_f32",
-            "sats_sample", "sats_sample_f32", "sats_get_error", "sats_get_status_word", "sats_selftest_wait_timeout",
+            "sats_sample", "sats_sample_f32", "sats_adjust_logits", "sats_adjust_logits_f32",
+            "sats_adjust_logits_grad", "sats_adjust_logits_grad_f32", "sats_q4_quantize", "sats_q4_dequantize",
+            "sats_q4_create", "sats_q4_destroy", "sats_q4_shape", "sats_q4_workspace_bytes", "sats_q4_matmul",
+            "sats_q4_matmul_f32", "sats_get_error", "sats_get_status_word", "sats_selftest_wait_timeout",
             "sats_selftest_select_timeout", "sats_selftest_distill_timeout")
 
 
@@ -556,6 +571,168 @@ def sample(logits: torch.Tensor, u: torch.Tensor, ids: torch.Tensor, temperature
               vec(min_p, "min_p"), vec(u, "u"), vec(ids, "ids", torch.int32), vec(logprob, "logprob"),
               vec(n_kept, "n_kept", torch.int32), _beside(dev_status, "dev_status", torch.int32, (1,), dev),
               _stream(stream)), "sats_sample")
+
+
+# Adjusted logits: settings and histories beside the rows of logits, as the vocabulary operators take them.
+
+def _adjust_args(logits, hist, hist_len, mask, mask_row):
+    z, ld, B, V, f32, dev = _rows(logits, "logits")
+    h, ld_h, L = None, 0, 0
+    if hist is not None:
+        if hist.get_device() != dev or hist.dtype is not torch.int32 or hist.dim() != 2 or hist.shape[0] != B:
+            raise ValueError("hist must be an int32 tensor [rows][ids] on the logits' device")
+        L = hist.shape[1]
+        if L > 1 and hist.stride(1) != 1:
+            raise ValueError("hist must have consecutive ids in a row")
+        h, ld_h = hist.data_ptr(), hist.stride(0) if B > 1 else 0
+    m, ld_m, n = None, 0, 0
+    if mask is not None:
+        if (mask.get_device() != dev or mask.dtype is not torch.int32 or mask.dim() != 2
+                or mask.shape[1] != (V + 31) // 32 or (mask.shape[1] > 1 and mask.stride(1) != 1)):
+            raise ValueError("mask must be an int32 tensor [masks][ceil(V / 32)] on the logits' device")
+        m, n = mask.data_ptr(), mask.shape[0]
+        ld_m = mask.stride(0) if n > 1 else mask.shape[1]
+    return (z, ld, B, V, h, ld_h, L, _beside(hist_len, "hist_len", torch.int32, (B,), dev)), \
+        (m, ld_m, n, _beside(mask_row, "mask_row", torch.int32, (B,), dev)), B, f32, dev
+
+
+def _same_rows(t, name, logits):
+    p, ld, _, _, f32, dev = _rows(t, name)
+    if t.shape != logits.shape or f32 != (logits.dtype is torch.float32) or dev != logits.get_device():
+        raise ValueError("%s must have the logits' shape, type and device" % name)
+    return p, ld
+
+
+def adjust_logits(logits: torch.Tensor, out: torch.Tensor, hist: Optional[torch.Tensor] = None,
+                  hist_len: Optional[torch.Tensor] = None, n_prompt: Optional[torch.Tensor] = None,
+                  repetition: Optional[torch.Tensor] = None, presence: Optional[torch.Tensor] = None,
+                  frequency: Optional[torch.Tensor] = None, bias_idx: Optional[torch.Tensor] = None,
+                  bias_val: Optional[torch.Tensor] = None, mask: Optional[torch.Tensor] = None,
+                  mask_row: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None,
+                  stream: Optional[torch.cuda.Stream] = None):
+    """Penalties for the tokens of each row's history (int32 [B][L], rows may be expanded or overlap), biases and
+    masks on rows of logits, before they are sampled (sats_adjust_logits); out may be the logits."""
+    head, masks, B, f32, dev = _adjust_args(logits, hist, hist_len, mask, mask_row)
+    if (bias_idx is None) != (bias_val is None):
+        raise ValueError("bias_idx and bias_val go together")
+    M = 0
+    if bias_idx is not None:
+        if bias_idx.dim() != 2:
+            raise ValueError("bias_idx must be [B][M]")
+        M = bias_idx.shape[1]
+    o, ld_o = _same_rows(out, "out", logits)
+    vec = lambda t, name: _beside(t, name, torch.float32, (B,), dev)
+    fn = lib().sats_adjust_logits_f32 if f32 else lib().sats_adjust_logits
+    _check(fn(*head, _beside(n_prompt, "n_prompt", torch.int32, (B,), dev), vec(repetition, "repetition"),
+              vec(presence, "presence"), vec(frequency, "frequency"),
+              _beside(bias_idx, "bias_idx", torch.int32, (B, M), dev),
+              _beside(bias_val, "bias_val", torch.float32, (B, M), dev), M, *masks, o, ld_o,
+              _beside(dev_status, "dev_status", torch.int32, (1,), dev), _stream(stream)), "sats_adjust_logits")
+
+
+def adjust_logits_grad(logits: torch.Tensor, dout: torch.Tensor, dlogits: torch.Tensor,
+                       hist: Optional[torch.Tensor] = None, hist_len: Optional[torch.Tensor] = None,
+                       repetition: Optional[torch.Tensor] = None, mask: Optional[torch.Tensor] = None,
+                       mask_row: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None,
+                       stream: Optional[torch.cuda.Stream] = None):
+    """The gradient of adjust_logits with respect to the logits it was given (sats_adjust_logits_grad); dlogits may be
+    dout or the logits."""
+    head, masks, B, f32, dev = _adjust_args(logits, hist, hist_len, mask, mask_row)
+    g, ld_g = _same_rows(dout, "dout", logits)
+    d, ld_d = _same_rows(dlogits, "dlogits", logits)
+    fn = lib().sats_adjust_logits_grad_f32 if f32 else lib().sats_adjust_logits_grad
+    _check(fn(*head, _beside(repetition, "repetition", torch.float32, (B,), dev), *masks, g, ld_g, d, ld_d,
+              _beside(dev_status, "dev_status", torch.int32, (1,), dev), _stream(stream)), "sats_adjust_logits_grad")
+
+
+# 4-bit weights with group scales: codes uint8 [K / 2][N] (two rows of W to a byte), scales bf16 [ceil(K / G)][N] (or int16
+# bit patterns).
+
+def _q4_parts(codes, scales, G):
+    if codes.dim() != 2 or scales.dim() != 2:
+        raise ValueError("codes must be [K / 2][N], scales [ceil(K / G)][N]")
+    K, N = 2 * codes.shape[0], codes.shape[1]
+    if G < 1 or tuple(scales.shape) != ((K + G - 1) // G, N):
+        raise ValueError("scales must be [ceil(K / G)][N] of the codes' K and N")
+    return _current(_ptr(codes, "codes", 1), codes), _current(_ptr(scales, "scales", 2), scales), K, N
+
+
+def _current(p, t):
+    if t.get_device() != torch._C._cuda_getDevice():
+        raise ValueError("tensors must be on the current CUDA device")
+    return p
+
+
+def q4_quantize(W: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, G: int,
+                stream: Optional[torch.cuda.Stream] = None):
+    """Codes and scales of a bf16 matrix W [K][N], whose rows may lie further apart than N (sats_q4_quantize)."""
+    w, ld, K, N, f32, _ = _rows(W, "W")
+    if f32:
+        raise ValueError("W must be bf16 (or int16 bit patterns of bf16)")
+    c, s, Kc, Nc = _q4_parts(codes, scales, G)
+    if (Kc, Nc) != (K, N):
+        raise ValueError("codes must be [K / 2][N] of W's K and N")
+    _check(lib().sats_q4_quantize(w, ld, K, N, G, c, s, _stream(stream)), "sats_q4_quantize")
+
+
+def q4_dequantize(codes: torch.Tensor, scales: torch.Tensor, G: int, values: torch.Tensor,
+                  stream: Optional[torch.cuda.Stream] = None):
+    """What codes and scales stand for, as fp32 values [K][N] (sats_q4_dequantize)."""
+    c, s, K, N = _q4_parts(codes, scales, G)
+    if tuple(values.shape) != (K, N):
+        raise ValueError("values must be [K][N]")
+    _check(lib().sats_q4_dequantize(c, s, K, N, G, _current(_ptr(values, "values", 4), values), _stream(stream)),
+           "sats_q4_dequantize")
+
+
+class Q4:
+    """Handle of a packed matrix of 4-bit weights (sats_q4_create / sats_q4_destroy)."""
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, G: int, stream: Optional[torch.cuda.Stream] = None):
+        self.handle = None
+        c, s, K, N = _q4_parts(codes, scales, G)
+        h = ctypes.c_void_p()
+        _check(lib().sats_q4_create(c, s, K, N, G, _stream(stream), ctypes.byref(h)), "sats_q4_create")
+        self.handle = h.value
+        self.K, self.N, self.G = K, N, G
+        self.device = codes.get_device()
+
+    def close(self):
+        if self.handle:
+            _check(lib().sats_q4_destroy(self.handle), "sats_q4_destroy")
+        self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class Q4Workspace:
+    """A zero-initialised device workspace for products of up to B tokens with a Q4 matrix."""
+
+    def __init__(self, w: Q4, B: int, stream: Optional[torch.cuda.Stream] = None):
+        n = int(lib().sats_q4_workspace_bytes(w.K, w.N, B))
+        if n == 0:
+            raise ValueError("unsupported batch for a workspace: B=%d" % B)
+        self.buf = torch.empty(n, dtype=torch.uint8, device="cuda:%d" % w.device)
+        self.nbytes = n
+        _check(lib().sats_workspace_init(_ptr(self.buf, "ws"), n, _stream(stream)), "sats_workspace_init")
+
+
+def q4_matmul(w: Q4, x: torch.Tensor, y: torch.Tensor, ws: Q4Workspace, stream: Optional[torch.cuda.Stream] = None):
+    """y = x W: x bf16 (or its int16 bit patterns) or fp32 [B][K], y fp32 or bf16 [B][N], whose rows may lie further
+    apart than N (sats_q4_matmul)."""
+    if x.dim() != 2 or x.shape[1] != w.K or x.dtype not in (torch.float32, torch.bfloat16, torch.int16):
+        raise ValueError("x must be bf16 or fp32 [B][K]")
+    B = x.shape[0]
+    yp, ld, By, N, y_f32, dev = _rows(y, "y")
+    if By != B or N != w.N or dev != w.device or x.get_device() != dev:
+        raise ValueError("y must be [B][N] on the weights' device")
+    fn = lib().sats_q4_matmul_f32 if x.dtype is torch.float32 else lib().sats_q4_matmul
+    _check(fn(w.handle, _ptr(x, "x"), B, yp, ld, 1 if y_f32 else 0, ws.buf.data_ptr(), ws.nbytes, _stream(stream)),
+           "sats_q4_matmul")
 
 
 def selftest_wait_timeout(ws: Workspace, stream: Optional[torch.cuda.Stream] = None):
