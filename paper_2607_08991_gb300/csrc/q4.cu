@@ -228,23 +228,38 @@ struct Q4Params {
     int64_t ld_y;
     int B, N, KS, TT, per_tile;   // TT: token tiles
     int G;
-    int64_t units;                // of `quantum` stages each, all tiles one after another
-    int quantum;
-    int stages;                   // of the shared-memory ring
+    int per, rem;                 // units of a CTA: per, one more for the first rem
+    bool whole;                   // a unit is a tile, else a stage of 128 k
     bool y_f32;
-    float *partial;               // [2 kMaxCtas][TN][128]
+    int stages;                   // of the shared-memory ring
+    float *partial;               // [2 kMaxCtas][R][128]
     int *counters;                // [tiles], 0 between calls
     int *ctl;
 };
 
-constexpr int kQ4Threads = 32 * 14;
 constexpr int kQ4MaxStages = 8;
 
-// Stages [begin, end) of CTA c; tile = stage / KS.
-__device__ __forceinline__ int64_t range_begin(const Q4Params &p, int64_t c)
+// The first unit of CTA c.
+__device__ __forceinline__ int first_unit(const Q4Params &p, int c) { return c * p.per + min(c, p.rem); }
+// The CTA of a unit.
+__device__ __forceinline__ int unit_cta(const Q4Params &p, int u)
 {
-    return p.units * c / gridDim.x * p.quantum;
+    const int longer = p.rem * (p.per + 1);
+    return u < longer ? u / (p.per + 1) : p.rem + (u - longer) / p.per;
 }
+
+// A place in the ring of `n` slots and the parity of its use.
+struct Slot {
+    int i = 0;
+    uint32_t parity = 0;
+    __device__ __forceinline__ void next(int n)
+    {
+        if (++i == n) {
+            i = 0;
+            parity ^= 1u;
+        }
+    }
+};
 
 // D += A B with A (fp16) in TMEM.
 __device__ __forceinline__ void mma_f16_tmem_if(uint32_t lead, uint32_t d_tmem, uint32_t a_tmem, uint64_t b,
@@ -291,26 +306,56 @@ struct Q4Bars {
     uint64_t drain;
 };
 
-// TN: tokens of a tile (MMA N); NA: stages of fp16 weights in TMEM; PER_SM: resident CTAs.
-template <int TN, int NA, int PER_SM, bool F32>
-__global__ void __launch_bounds__(kQ4Threads, PER_SM) q4_matmul_kernel(const __grid_constant__ Q4Params p)
+template <int R, int EG>
+constexpr int q4_threads() { return 32 * (10 + 4 * EG); }
+
+// Columns [c, c + n) of this warp's lanes added to acc; n 8, 16 or a multiple of 16.
+template <int n>
+__device__ __forceinline__ void add_columns(uint32_t taddr, float (&acc)[n])
 {
+    if constexpr (n == 8) {
+        float v[8];
+        tmem_ld8(taddr, v);
+        tmem_ld_wait();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) acc[i] += v[i];
+    } else {
+#pragma unroll
+        for (int c = 0; c < n; c += 16) {
+            float v[16];
+            tmem_ld16(taddr + c, v);
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[c + i] += v[i];
+        }
+    }
+}
+
+// R: tokens of a tile that are there (columns of the accumulator that are used); TN >= 16: the MMA's N, whose rows past
+// R read whatever lies behind them in shared memory and land in columns that nobody reads.  NA: stages of fp16 weights in
+// TMEM; EG: warpgroups that add the sums up; PER_SM: resident CTAs.
+template <int R, int NA, int EG, int PER_SM, bool F32>
+__global__ void __launch_bounds__(q4_threads<R, EG>(), PER_SM) q4_matmul_kernel(const __grid_constant__ Q4Params p)
+{
+    constexpr int TN = R < 16 ? 16 : R;
     constexpr int kCols = (2 * TN + NA * 64) <= 256 ? 256 : 512;   // TMEM: two accumulators, then the weights
-    constexpr int kX = TN * 256;                                   // bytes of the activations of a stage
+    constexpr int kX = R * 256;                                    // bytes of the activations of a stage
     constexpr uint32_t kIdesc = (1u << 4) | ((uint32_t)(TN >> 3) << 17) | ((uint32_t)(kRows >> 4) << 24);
+    constexpr int kDeq = 4 * EG, kLoad = kDeq + 8, kMma = kDeq + 9;   // first warps of the roles
     static_assert(2 * TN + NA * 64 <= 512 && NA <= 4, "TMEM");
     extern __shared__ char smem_raw[];
     __shared__ Q4Bars bars;
     __shared__ uint32_t tmem_slot;
     __shared__ volatile int abort_flag;
-    __shared__ int last_flag;
+    __shared__ int last_flag[EG];
 
     const int warp = uniform_warp(), lane = threadIdx.x & 31;
     char *const ring = reinterpret_cast<char *>(align1024(reinterpret_cast<uint8_t *>(smem_raw)));
     const int blk = block_bytes(p.G);
     char *const wring = ring + (size_t)p.stages * kX;
-    const int64_t begin = range_begin(p, blockIdx.x), end = range_begin(p, blockIdx.x + 1);
-    const int n_it = (int)(end - begin);
+    const int u0 = first_unit(p, blockIdx.x), u1 = first_unit(p, blockIdx.x + 1);
+    const int n_it = p.whole ? (u1 - u0) * p.KS : u1 - u0;
+    const int tile0 = p.whole ? u0 : u0 / p.KS, ks0 = p.whole ? 0 : u0 - tile0 * p.KS;
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < kQ4MaxStages; ++i) {
@@ -324,102 +369,126 @@ __global__ void __launch_bounds__(kQ4Threads, PER_SM) q4_matmul_kernel(const __g
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&bars.d_full[i], 1);
-            mbar_init(&bars.d_empty[i], 4);
+            mbar_init(&bars.d_empty[i], 4 * EG);
         }
         mbar_init(&bars.drain, 1);
         abort_flag = 0;
         mbar_init_fence();
     }
-    if (warp == 13) tmem_alloc(&tmem_slot, kCols);
+    if (warp == kMma) tmem_alloc(&tmem_slot, kCols);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = tmem_slot;
 
-    if (warp == 12) {
+    if (warp == kLoad) {
         // ---- loads
         const uint32_t lead = elect_one();
-        auto load_w = [&](int it) {
-            const int s = it % p.stages;
-            const int64_t pos = begin + it, tile = pos / p.KS;
-            mbar_expect_if(lead, &bars.full[s], (uint32_t)(blk + kX));
-            bulk_load_shared_if(lead, wring + (size_t)s * blk,
-                                p.blk + ((tile / p.TT) * p.KS + (pos - tile * p.KS)) * blk, (uint32_t)blk, &bars.full[s]);
-        };
-        auto load_x = [&](int it) {
-            const int s = it % p.stages;
-            const int64_t pos = begin + it, tile = pos / p.KS;
-            bulk_load_shared_if(lead, ring + (size_t)s * kX, p.xs + ((tile % p.TT) * p.KS + (pos - tile * p.KS)) * kX,
-                                (uint32_t)kX, &bars.full[s]);
-        };
-        // the weights do not depend on the kernel that stages the activations
         const int ahead = min(n_it, p.stages);
-        for (int it = 0; it < ahead; ++it) load_w(it);
+        // the weights do not depend on the kernel that stages the activations
+        int ks = ks0, tt = tile0 % p.TT;
+        const uint8_t *w = p.blk + ((int64_t)(tile0 / p.TT) * p.KS + ks) * blk;
+        auto step_w = [&](int &ks_, int &tt_) {   // (the same row tile again for the next token tile)
+            w += blk;
+            if (++ks_ == p.KS) {
+                ks_ = 0;
+                if (++tt_ == p.TT) tt_ = 0;
+                else w -= (int64_t)p.KS * blk;
+            }
+        };
+        for (int it = 0; it < ahead; ++it) {
+            mbar_expect_if(lead, &bars.full[it], (uint32_t)(blk + kX));
+            bulk_load_shared_if(lead, wring + (size_t)it * blk, w, (uint32_t)blk, &bars.full[it]);
+            step_w(ks, tt);
+        }
         grid_dependency_wait();
-        for (int it = 0; it < ahead; ++it) load_x(it);
+        int xks = ks0, xtt = tile0 % p.TT;
+        const char *x = p.xs + ((int64_t)xtt * p.KS + xks) * kX;
+        auto step_x = [&] {
+            x += kX;
+            if (++xks == p.KS) {
+                xks = 0;
+                if (++xtt == p.TT) {
+                    xtt = 0;
+                    x = p.xs;
+                }
+            }
+        };
+        for (int it = 0; it < ahead; ++it) {
+            bulk_load_shared_if(lead, ring + (size_t)it * kX, x, (uint32_t)kX, &bars.full[it]);
+            step_x();
+        }
+        Slot s;   // parity: of the use before
+        s.i = ahead == p.stages ? 0 : ahead;
         int issued = ahead;
         for (int it = ahead; it < n_it; ++it) {
-            if (!warp_wait(&bars.empty[it % p.stages], (uint32_t)((it / p.stages - 1) & 1), &abort_flag)) {
+            if (!warp_wait(&bars.empty[s.i], s.parity, &abort_flag)) {
                 if (lane == 0) set_timeout(p.ctl, &abort_flag);
                 break;
             }
-            load_w(it);
-            load_x(it);
+            mbar_expect_if(lead, &bars.full[s.i], (uint32_t)(blk + kX));
+            bulk_load_shared_if(lead, wring + (size_t)s.i * blk, w, (uint32_t)blk, &bars.full[s.i]);
+            bulk_load_shared_if(lead, ring + (size_t)s.i * kX, x, (uint32_t)kX, &bars.full[s.i]);
+            step_w(ks, tt);
+            step_x();
+            s.next(p.stages);
             issued = it + 1;
         }
         // nothing may arrive after the CTA's end
         int never = 0;
         for (int it = max(0, issued - p.stages); it < issued; ++it)
             warp_wait(&bars.full[it % p.stages], (uint32_t)((it / p.stages) & 1), &never);
-    } else if (warp == 13) {
+    } else if (warp == kMma) {
         // ---- MMAs
         const uint32_t lead = elect_one();
         bool ok = true;
-        for (int it = 0; it < n_it && ok; ++it) {
-            const int s = it % p.stages, a = it % NA, d = it & 1;
-            ok = warp_wait(&bars.full[s], (uint32_t)((it / p.stages) & 1), &abort_flag);
-            if (ok && it >= 2) ok = warp_wait(&bars.d_empty[d], (uint32_t)((it / 2 - 1) & 1), &abort_flag);
-            const uint32_t xb = smem_addr(ring + (size_t)s * kX);
+        Slot s, a, d;
+        const uint64_t desc0 = smem_desc(smem_addr(ring));
+        for (int it = 0; it < n_it; ++it) {
+            ok = warp_wait(&bars.full[s.i], s.parity, &abort_flag);
+            if (ok && it >= 2) ok = warp_wait(&bars.d_empty[d.i], d.parity ^ 1u, &abort_flag);
+            const uint64_t desc = desc0 + (uint64_t)(s.i * (kX >> 4));
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                if (ok) ok = warp_wait(&bars.a_full[a][h], (uint32_t)((it / NA) & 1), &abort_flag);
+                if (ok) ok = warp_wait(&bars.a_full[a.i][h], a.parity, &abort_flag);
                 if (!ok) break;
                 tc_fence_after();
-                const uint64_t desc = smem_desc(xb + h * (TN * 128));
 #pragma unroll
                 for (int k = 0; k < 4; ++k)   // 16 k: 8 columns of TMEM, 32 bytes of the swizzled rows
-                    mma_f16_tmem_if(lead, tmem + d * TN, tmem + 2 * TN + a * 64 + h * 32 + k * 8, desc + 2 * k, kIdesc,
-                                    (uint32_t)(h + k > 0));
+                    mma_f16_tmem_if(lead, tmem + d.i * TN, tmem + 2 * TN + a.i * 64 + h * 32 + k * 8,
+                                    desc + h * (R * 128 >> 4) + 2 * k, kIdesc, (uint32_t)(h + k > 0));
             }
             if (!ok) break;
-            mma_commit_if(lead, &bars.empty[s]);
-            mma_commit_if(lead, &bars.a_empty[a]);
-            mma_commit_if(lead, &bars.d_full[d]);
+            mma_commit_if(lead, &bars.empty[s.i]);
+            mma_commit_if(lead, &bars.a_empty[a.i]);
+            mma_commit_if(lead, &bars.d_full[d.i]);
+            s.next(p.stages);
+            a.next(NA);
+            d.next(2);
         }
         if (!ok && lane == 0) set_timeout(p.ctl, &abort_flag);
         mma_commit_if(lead, &bars.drain);
         int never = 0;
         warp_wait(&bars.drain, 0u, &never);
-    } else if (warp >= 4) {
-        // ---- weights to fp16: warps 4 to 7 the first 64 k of a stage, 8 to 11 the others
-        const int h = (warp - 4) >> 2, quad = warp & 3, r = quad * 32 + lane;
+    } else if (warp >= kDeq) {
+        // ---- weights to fp16: four warps the first 64 k of a stage, four the others
+        const int h = (warp - kDeq) >> 2, quad = warp & 3, r = quad * 32 + lane;
         const int per = kStageK / p.G;
         const int sub0 = (2 * h * per) >> 2, sub1 = ((2 * h + 1) * per) >> 2;
         const uint32_t dst = tmem + ((uint32_t)(quad * 32) << 16) + 2 * TN + h * 32;
+        const __half2 k1536 = __float2half2_rn(-1536.f);
         bool ok = true;
+        Slot s, a;
         for (int it = 0; it < n_it; ++it) {
-            const int s = it % p.stages, a = it % NA;
-            ok = warp_wait(&bars.full[s], (uint32_t)((it / p.stages) & 1), &abort_flag);
-            if (ok && it >= NA) ok = warp_wait(&bars.a_empty[a], (uint32_t)((it / NA - 1) & 1), &abort_flag);
+            ok = warp_wait(&bars.full[s.i], s.parity, &abort_flag);
             if (!ok) break;
-            const char *const w = wring + (size_t)s * blk;
+            const char *const w = wring + (size_t)s.i * blk;
             const uint4 q0 = reinterpret_cast<const uint4 *>(w)[(2 * h) * kRows + r];
             const uint4 q1 = reinterpret_cast<const uint4 *>(w)[(2 * h + 1) * kRows + r];
             const __half *const sc = reinterpret_cast<const __half *>(w + kCodeBytes);
             const __half2 t0 = __half2half2(sc[sub0 * kRows + r]), t1 = __half2half2(sc[sub1 * kRows + r]);
             __syncwarp();
-            if (lane == 0) mbar_arrive(&bars.empty[s]);
-            const __half2 k1536 = __float2half2_rn(-1536.f);
+            if (lane == 0) mbar_arrive(&bars.empty[s.i]);
             const __half2 c0 = __hmul2(t0, k1536), c1 = __hmul2(t1, k1536);
             uint32_t v[32];
             dequant8(q0.x, t0, c0, v);
@@ -430,79 +499,91 @@ __global__ void __launch_bounds__(kQ4Threads, PER_SM) q4_matmul_kernel(const __g
             dequant8(q1.y, t1, c1, v + 20);
             dequant8(q1.z, t1, c1, v + 24);
             dequant8(q1.w, t1, c1, v + 28);
+            if (it >= NA) ok = warp_wait(&bars.a_empty[a.i], a.parity ^ 1u, &abort_flag);
+            if (!ok) break;
             tc_fence_after();
-            tmem_st32(dst + a * 64, v);
+            tmem_st32(dst + a.i * 64, v);
             tmem_st_wait();
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&bars.a_full[a][h]);
+            if (lane == 0) mbar_arrive(&bars.a_full[a.i][h]);
+            s.next(p.stages);
+            a.next(NA);
         }
         if (!ok && lane == 0) set_timeout(p.ctl, &abort_flag);
     } else {
-        // ---- sums: each stage's 128 products are added up by the MMAs, the stages here in fp32 (the accumulator truncates)
-        constexpr int kOut = F32 ? TN / 2 : TN;
-        const int r = threadIdx.x;
-        float acc[TN];
+        // ---- sums: each stage's 128 products are added up by the MMAs, the stages here in fp32 (the accumulator truncates).
+        // Warpgroup e has columns [e C, (e + 1) C); with fp32 activations R / 2 second parts follow R / 2 first ones, so
+        // each warpgroup takes half of both.
+        constexpr int C = R / EG, kOut = F32 ? C / 2 : C;
+        constexpr int kPieces = F32 && EG > 1 ? 2 : 1, P = C / kPieces;
+        const int e = warp >> 2, quad = warp & 3, r = quad * 32 + lane;
+        const uint32_t src = tmem + ((uint32_t)(quad * 32) << 16) + e * P;
+        float acc[kPieces][P];
 #pragma unroll
-        for (int i = 0; i < TN; ++i) acc[i] = 0.f;
+        for (int j = 0; j < kPieces; ++j)
+#pragma unroll
+            for (int i = 0; i < P; ++i) acc[j][i] = 0.f;
         bool ok = true;
+        Slot d;
+        int ks = ks0, tile = tile0;
         for (int it = 0; it < n_it; ++it) {
-            const int d = it & 1;
-            ok = warp_wait(&bars.d_full[d], (uint32_t)((it / 2) & 1), &abort_flag);
+            ok = warp_wait(&bars.d_full[d.i], d.parity, &abort_flag);
             if (!ok) break;
             tc_fence_after();
 #pragma unroll
-            for (int c = 0; c < TN; c += 16) {
-                float v[16];
-                tmem_ld16(tmem + ((uint32_t)(warp * 32) << 16) + d * TN + c, v);
-                tmem_ld_wait();
-#pragma unroll
-                for (int i = 0; i < 16; ++i) acc[c + i] += v[i];
-            }
+            for (int j = 0; j < kPieces; ++j) add_columns<P>(src + d.i * TN + j * (R / 2), acc[j]);
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&bars.d_empty[d]);
+            if (lane == 0) mbar_arrive(&bars.d_empty[d.i]);
+            d.next(2);
+            const bool tile_end = ++ks == p.KS;
+            if (!tile_end && it != n_it - 1) continue;
 
-            const int64_t pos = begin + it, tile = pos / p.KS;
-            const int ks = (int)(pos - tile * p.KS);
-            if (ks != p.KS - 1 && it != n_it - 1) continue;
             // the end of a tile or of this CTA's share of one
-            if constexpr (F32)
+            float sum[kOut];
 #pragma unroll
-                for (int i = 0; i < kOut; ++i) acc[i] += acc[i + TN / 2] * (1.f / (1 << kLoShift));
-            const int tt = (int)(tile % p.TT);
-            const int64_t n = (tile / p.TT) * kRows + r;
-            const int tokens = min(p.per_tile, p.B - tt * p.per_tile);
-            const int64_t t0 = tile * p.KS, t1 = t0 + p.KS;
+            for (int i = 0; i < kOut; ++i) {
+                if constexpr (!F32) sum[i] = acc[0][i];
+                else if constexpr (kPieces == 2) sum[i] = acc[0][i] + acc[1][i] * (1.f / (1 << kLoShift));
+                else sum[i] = acc[0][i] + acc[0][i + kOut] * (1.f / (1 << kLoShift));
+            }
+            const int tt = tile % p.TT, token0 = tt * p.per_tile + e * kOut;
+            const int n = (tile / p.TT) * kRows + r;
+            const int tokens = min(p.per_tile - e * kOut, p.B - token0);   // (of the next ones, if more than kOut)
             bool write = true;
-            if (begin > t0 || ks != p.KS - 1) {
+            auto group_barrier = [](int group) {   // (literal numbers: else a CTA reserves all barriers)
+                if (EG == 1 || group == 0) named_barrier(1, 128);
+                else named_barrier(2, 128);
+            };
+            if (!p.whole && (u0 > tile * p.KS || !tile_end)) {
                 // the CTAs of the tile leave their sums in the workspace; the last one to come adds them in order
-                float *const mine = p.partial + (size_t)(2 * blockIdx.x + (begin < t0 ? 1 : 0)) * TN * kRows;
+                const int t0 = tile * p.KS, c0 = unit_cta(p, t0), c1 = unit_cta(p, t0 + p.KS - 1);
+                auto slot = [&](int c, int begin) {   // a CTA's second slot is for the tile that it begins
+                    return p.partial + ((size_t)(2 * c + (begin < t0 ? 1 : 0)) * R + e * kOut) * kRows + r;
+                };
+                float *const mine = slot(blockIdx.x, u0);
 #pragma unroll
                 for (int i = 0; i < kOut; ++i)
-                    if (i < tokens) __stcg(mine + i * kRows + r, acc[i]);
+                    if (i < tokens) __stcg(mine + i * kRows, sum[i]);
                 __threadfence();
-                named_barrier(1, 128);
-                // CTAs c0..c1 hold stages of the tile
-                int64_t c0 = blockIdx.x, c1 = blockIdx.x;
-                while (range_begin(p, c0) > t0) --c0;
-                while (range_begin(p, c1 + 1) < t1) ++c1;
+                group_barrier(e);
                 if (r == 0) {
-                    const int old = atom_add_acq_rel_gpu(p.counters + tile, 1);
-                    last_flag = old == (int)(c1 - c0);
-                    if (last_flag) p.counters[tile] = 0;
+                    const int old = atom_add_acq_rel_gpu(p.counters + EG * tile + e, 1);
+                    last_flag[e] = old == c1 - c0;
+                    if (old == c1 - c0) p.counters[EG * tile + e] = 0;
                 }
-                named_barrier(1, 128);
-                write = last_flag != 0;
+                group_barrier(e);
+                write = last_flag[e] != 0;
                 if (write) {
                     __threadfence();
 #pragma unroll
-                    for (int i = 0; i < kOut; ++i) acc[i] = 0.f;
-                    for (int64_t c = c0; c <= c1; ++c) {
-                        const float *const part = p.partial + (size_t)(2 * c + (range_begin(p, c) < t0 ? 1 : 0)) * TN * kRows;
+                    for (int i = 0; i < kOut; ++i) sum[i] = 0.f;
+                    for (int c = c0; c <= c1; ++c) {
+                        const float *const part = slot(c, first_unit(p, c));
 #pragma unroll
                         for (int i = 0; i < kOut; ++i)
-                            if (i < tokens) acc[i] += __ldcg(part + i * kRows + r);
+                            if (i < tokens) sum[i] += __ldcg(part + i * kRows);
                     }
                 }
             }
@@ -510,22 +591,29 @@ __global__ void __launch_bounds__(kQ4Threads, PER_SM) q4_matmul_kernel(const __g
                 const int ce = p.col_exp[n];
 #pragma unroll
                 for (int i = 0; i < kOut; ++i) {
-                    if (i >= tokens) break;
-                    const int64_t token = (int64_t)tt * p.per_tile + i;
-                    const float v = scalbnf(acc[i], ce + p.tok_exp[token]);
-                    if (p.y_f32) static_cast<float *>(p.y)[token * p.ld_y + n] = v;
-                    else static_cast<__nv_bfloat16 *>(p.y)[token * p.ld_y + n] = __float2bfloat16_rn(v);
+                    if (i < tokens) {
+                        const int64_t at = (int64_t)(token0 + i) * p.ld_y + n;
+                        const float v = scalbnf(sum[i], ce + p.tok_exp[token0 + i]);
+                        if (p.y_f32) static_cast<float *>(p.y)[at] = v;
+                        else static_cast<__nv_bfloat16 *>(p.y)[at] = __float2bfloat16_rn(v);
+                    }
                 }
             }
 #pragma unroll
-            for (int i = 0; i < TN; ++i) acc[i] = 0.f;
+            for (int j = 0; j < kPieces; ++j)
+#pragma unroll
+                for (int i = 0; i < P; ++i) acc[j][i] = 0.f;
+            if (tile_end) {
+                ks = 0;
+                ++tile;
+            }
         }
         if (!ok && lane == 0) set_timeout(p.ctl, &abort_flag);
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp == 13) tmem_dealloc(tmem, kCols);
+    if (warp == kMma) tmem_dealloc(tmem, kCols);
 }
 
 // ------------------------------------------------------------------ host
@@ -533,7 +621,7 @@ __global__ void __launch_bounds__(kQ4Threads, PER_SM) q4_matmul_kernel(const __g
 int tile_tokens(int B, bool f32)
 {
     const int64_t cols = (int64_t)B * (f32 ? 2 : 1);
-    return cols <= 16 ? 16 : cols <= 32 ? 32 : cols <= 64 ? 64 : 128;
+    return cols <= 8 ? 8 : cols <= 16 ? 16 : cols <= 32 ? 32 : cols <= 64 ? 64 : 128;
 }
 
 struct Q4Layout {
@@ -553,7 +641,7 @@ Q4Layout q4_layout(int K, int N, int B)
         const size_t tt = (size_t)div_up(b, f ? TN / 2 : TN);
         xs = std::max(xs, tt * div_up(K, kStageK) * TN * 256);
         partial = std::max(partial, (size_t)2 * kMaxCtas * TN * kRows * 4);
-        tiles = std::max(tiles, std::min(tt * div_up(N, kRows), (size_t)kMaxSplitTiles));
+        tiles = std::max(tiles, std::min(tt * div_up(N, kRows), (size_t)kMaxSplitTiles) * 2);
     }
     L.counters = kCtlBytes;
     L.tok_exp = L.counters + up256(tiles * 4);
@@ -568,25 +656,26 @@ bool q4_shape_ok(int64_t K, int64_t N, int G)
     return K >= 8 && K <= kMaxK && K % 8 == 0 && N >= 1 && N <= kMaxQ4N && (G == 32 || G == 64 || G == 128);
 }
 
-template <int TN, int NA, int PER_SM, bool F32>
+template <int R, int NA, int EG, int PER_SM, bool F32>
 cudaError_t launch_q4(Q4Params p, cudaStream_t st)
 {
     static std::atomic<int> configured[64];
-    const int stage = block_bytes(p.G) + TN * 256;
-    const int budget = PER_SM == 2 ? 110 * 1024 : 220 * 1024;
+    const int stage = block_bytes(p.G) + R * 256;
+    const int budget = PER_SM == 2 ? 110 * 1024 : 222 * 1024;
     p.stages = std::min(kQ4MaxStages, (budget - 1024) / stage);
     const size_t smem = (size_t)p.stages * stage + 1024;
-    cudaError_t e = set_smem(q4_matmul_kernel<TN, NA, PER_SM, F32>, smem, configured);
+    cudaError_t e = set_smem(q4_matmul_kernel<R, NA, EG, PER_SM, F32>, smem, configured);
     if (e != cudaSuccess) return e;
-    const int64_t tiles = (int64_t)div_up(p.N, kRows) * p.TT;
-    const int64_t most = std::min(kMaxCtas, PER_SM * sm_count());
+    const int tiles = div_up(p.N, kRows) * p.TT;
+    const int most = std::min(kMaxCtas, PER_SM * sm_count());
     // Whole tiles where they fill the CTAs evenly, else any number of stages each.
     const int64_t waves = (tiles + most - 1) / most;
-    const bool whole = tiles * 10 >= waves * most * 9;
-    p.quantum = whole ? p.KS : 1;
-    p.units = whole ? tiles : tiles * p.KS;
-    const int grid = (int)std::min<int64_t>(most, p.units);
-    return launch_pdl_cfg(q4_matmul_kernel<TN, NA, PER_SM, F32>, dim3(grid), kQ4Threads, smem, st, p);
+    p.whole = (int64_t)tiles * 10 >= waves * most * 9;
+    const int units = p.whole ? tiles : tiles * p.KS;
+    const int grid = std::min(most, units);
+    p.per = units / grid;
+    p.rem = units % grid;
+    return launch_pdl_cfg(q4_matmul_kernel<R, NA, EG, PER_SM, F32>, dim3(grid), q4_threads<R, EG>(), smem, st, p);
 }
 
 template <bool F32>
@@ -612,10 +701,11 @@ cudaError_t run_q4(const sats_q4 *w, const void *x, int B, void *y, int64_t ld_y
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     switch (TN) {
-    case 16: return launch_q4<16, 3, 2, F32>(p, st);
-    case 32: return launch_q4<32, 3, 2, F32>(p, st);
-    case 64: return launch_q4<64, 4, 1, F32>(p, st);
-    default: return launch_q4<128, 4, 1, F32>(p, st);
+    case 8: return launch_q4<8, 3, 1, 2, F32>(p, st);
+    case 16: return launch_q4<16, 3, 1, 2, F32>(p, st);
+    case 32: return launch_q4<32, 3, 1, 2, F32>(p, st);
+    case 64: return launch_q4<64, 4, 1, 1, F32>(p, st);
+    default: return launch_q4<128, 4, 2, 1, F32>(p, st);
     }
 }
 
