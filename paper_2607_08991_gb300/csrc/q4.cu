@@ -34,8 +34,8 @@ constexpr int kCodeBytes = kRows * kStageK / 2;
 // A block: for each half of 64 k and each piece of 32 k the 16 bytes of every row (row after row), then the fp16 scales,
 // group after group, 128 rows each.
 // A word holds 8 codes u = q + 8, those of k = 2p in its low and 2p + 1 in its high half, p = 0..3: bits 6..9, 10..13,
-// 2..5 of the half, and for p = 3 bits 14..17 of the word (even) and 30, 31, 0, 1 (odd), so that shifts by 4, -4 and a
-// rotation by 8 bring each pair to bits 6..9, where with the exponent of 1024 it reads as 64 (16 + u).
+// 2..5 of the half, and for p = 3 bits 14..17 of the word (even) and 30, 31, 0, 1 (odd): as it is and rotated by 8 bits the
+// word has every pair at bits 6..9 or 2..5 of its halves, where with the exponent of 1024 they read as fp16 numbers.
 constexpr int kMaxK = 65536;
 constexpr int64_t kMaxQ4N = (int64_t)1 << 24;
 constexpr int kMaxCtas = 320;                 // of the product's kernel
@@ -286,22 +286,59 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32
 
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// The 8 codes of a word times the group's scale, as fp16 pairs in the order of k: 64 (16 + u) t - 1536 t = (u - 8) 64 t
-// in one multiply-add, exact in its product, in 1536 t (10 bits) and in the result (11 bits).
-__device__ __forceinline__ void dequant8(uint32_t w, __half2 t, __half2 c, uint32_t *out)
-{
-    const uint32_t v[4] = {w, w >> 4, w << 4, __byte_perm(w, w, 0x0321)};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t m = (v[i] & 0x03c003c0u) | 0x64006400u;
-        const __half2 h = __hfma2(*reinterpret_cast<const __half2 *>(&m), t, c);
-        out[i] = *reinterpret_cast<const uint32_t *>(&h);
+// The 8 codes of a word times the group's scale (t: a 64th of it), as fp16 pairs in the order of k.  At bits 6..9 a field
+// reads as 64 (16 + u): 64 (16 + u) t - 1536 t = (u - 8) 64 t in one multiply-add, exact in its product, in 1536 t (10 bits)
+// and in the result (11 bits).  At bits 2..5 it reads as 1024 + 4 u, from which 1056 leaves 4 (u - 8): a subtraction and a
+// product, which the multiply-add pipe has time for, where a shift to bits 6..9 would go to the logic pipe like the masks.
+struct Scale {
+    __half2 t, c, t16;
+    __device__ __forceinline__ explicit Scale(__half s)
+    {
+        t = __half2half2(s);
+        c = __hmul2(t, __float2half2_rn(-1536.f));
+        t16 = __hmul2(t, __float2half2_rn(16.f));
     }
+};
+
+__device__ __forceinline__ void dequant8(uint32_t w, const Scale &s, uint32_t *out)
+{
+    const uint32_t rot = __byte_perm(w, w, 0x0321);
+    // (v & mask) | the exponents of 1024, one instruction: left to itself the compiler makes two, 8 of 19 for a word
+    const auto field = [](uint32_t v, uint32_t mask) {
+        uint32_t d;
+        asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(d) : "r"(v), "r"(mask), "r"(0x64006400u));
+        return d;
+    };
+    const auto half = [](uint32_t v) { return *reinterpret_cast<const __half2 *>(&v); };
+    const auto word = [](__half2 h) { return *reinterpret_cast<const uint32_t *>(&h); };
+    const __half2 k1056 = __float2half2_rn(1056.f);
+    out[0] = word(__hfma2(half(field(w, 0x03c003c0u)), s.t, s.c));
+    out[1] = word(__hmul2(__hsub2(half(field(rot, 0x003c003cu)), k1056), s.t16));
+    out[2] = word(__hmul2(__hsub2(half(field(w, 0x003c003cu)), k1056), s.t16));
+    out[3] = word(__hfma2(half(field(rot, 0x03c003c0u)), s.t, s.c));
+}
+
+// warp_wait (tc_common.cuh) with fewer instructions while it waits: the limit and the abort flag are looked at after every
+// 16 tries, each of which the hardware suspends for a while.
+__device__ __forceinline__ bool role_wait(uint64_t *bar, uint32_t parity, volatile int *abort)
+{
+    bool ok = mbar_try_wait(bar, parity);
+    if (!__all_sync(0xffffffffu, ok)) {
+        const unsigned long long t0 = global_ns();
+        for (;;) {
+#pragma unroll 1
+            for (int i = 0; i < 16 && !ok; ++i) ok = mbar_try_wait(bar, parity);
+            if (__all_sync(0xffffffffu, ok)) break;
+            if (__any_sync(0xffffffffu, *abort != 0 || global_ns() - t0 > kWaitLimitNs)) return false;
+        }
+    }
+    __syncwarp();
+    return true;
 }
 
 struct Q4Bars {
     uint64_t full[kQ4MaxStages], empty[kQ4MaxStages];
-    uint64_t a_full[4][2], a_empty[4];
+    uint64_t a_full[4], a_empty[4];
     uint64_t d_full[2], d_empty[2];
     uint64_t drain;
 };
@@ -350,7 +387,7 @@ __global__ void __launch_bounds__(q4_threads<R, EG>(), PER_SM) q4_matmul_kernel(
     __shared__ int last_flag[EG];
 
     const int warp = uniform_warp(), lane = threadIdx.x & 31;
-    char *const ring = reinterpret_cast<char *>(align1024(reinterpret_cast<uint8_t *>(smem_raw)));
+    char *const ring = smem_raw + (-smem_addr(smem_raw) & 1023u);   // (not through an integer: loads stay shared-memory loads)
     const int blk = block_bytes(p.G);
     char *const wring = ring + (size_t)p.stages * kX;
     const int u0 = first_unit(p, blockIdx.x), u1 = first_unit(p, blockIdx.x + 1);
@@ -360,11 +397,10 @@ __global__ void __launch_bounds__(q4_threads<R, EG>(), PER_SM) q4_matmul_kernel(
     if (threadIdx.x == 0) {
         for (int i = 0; i < kQ4MaxStages; ++i) {
             mbar_init(&bars.full[i], 1);
-            mbar_init(&bars.empty[i], 9);   // eight warps that have read the codes, the MMAs that have read the activations
+            mbar_init(&bars.empty[i], 5);   // four warps that have read the codes, the MMAs that have read the activations
         }
         for (int i = 0; i < 4; ++i) {
-            mbar_init(&bars.a_full[i][0], 4);
-            mbar_init(&bars.a_full[i][1], 4);
+            mbar_init(&bars.a_full[i], 4);
             mbar_init(&bars.a_empty[i], 1);
         }
         for (int i = 0; i < 2; ++i) {
@@ -422,7 +458,7 @@ __global__ void __launch_bounds__(q4_threads<R, EG>(), PER_SM) q4_matmul_kernel(
         s.i = ahead == p.stages ? 0 : ahead;
         int issued = ahead;
         for (int it = ahead; it < n_it; ++it) {
-            if (!warp_wait(&bars.empty[s.i], s.parity, &abort_flag)) {
+            if (!role_wait(&bars.empty[s.i], s.parity, &abort_flag)) {
                 if (lane == 0) set_timeout(p.ctl, &abort_flag);
                 break;
             }
@@ -437,7 +473,7 @@ __global__ void __launch_bounds__(q4_threads<R, EG>(), PER_SM) q4_matmul_kernel(
         // nothing may arrive after the CTA's end
         int never = 0;
         for (int it = max(0, issued - p.stages); it < issued; ++it)
-            warp_wait(&bars.full[it % p.stages], (uint32_t)((it / p.stages) & 1), &never);
+            role_wait(&bars.full[it % p.stages], (uint32_t)((it / p.stages) & 1), &never);
     } else if (warp == kMma) {
         // ---- MMAs
         const uint32_t lead = elect_one();
@@ -445,20 +481,16 @@ __global__ void __launch_bounds__(q4_threads<R, EG>(), PER_SM) q4_matmul_kernel(
         Slot s, a, d;
         const uint64_t desc0 = smem_desc(smem_addr(ring));
         for (int it = 0; it < n_it; ++it) {
-            ok = warp_wait(&bars.full[s.i], s.parity, &abort_flag);
-            if (ok && it >= 2) ok = warp_wait(&bars.d_empty[d.i], d.parity ^ 1u, &abort_flag);
+            ok = role_wait(&bars.full[s.i], s.parity, &abort_flag);
+            if (ok && it >= 2) ok = role_wait(&bars.d_empty[d.i], d.parity ^ 1u, &abort_flag);
             const uint64_t desc = desc0 + (uint64_t)(s.i * (kX >> 4));
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                if (ok) ok = warp_wait(&bars.a_full[a.i][h], a.parity, &abort_flag);
-                if (!ok) break;
-                tc_fence_after();
-#pragma unroll
-                for (int k = 0; k < 4; ++k)   // 16 k: 8 columns of TMEM, 32 bytes of the swizzled rows
-                    mma_f16_tmem_if(lead, tmem + d.i * TN, tmem + 2 * TN + a.i * 64 + h * 32 + k * 8,
-                                    desc + h * (R * 128 >> 4) + 2 * k, kIdesc, (uint32_t)(h + k > 0));
-            }
+            if (ok) ok = role_wait(&bars.a_full[a.i], a.parity, &abort_flag);
             if (!ok) break;
+            tc_fence_after();
+#pragma unroll
+            for (int k = 0; k < 8; ++k)   // 16 k: 8 columns of TMEM, 32 bytes of the swizzled rows
+                mma_f16_tmem_if(lead, tmem + d.i * TN, tmem + 2 * TN + a.i * 64 + k * 8,
+                                desc + (k >> 2) * (R * 128 >> 4) + 2 * (k & 3), kIdesc, (uint32_t)(k > 0));
             mma_commit_if(lead, &bars.empty[s.i]);
             mma_commit_if(lead, &bars.a_empty[a.i]);
             mma_commit_if(lead, &bars.d_full[d.i]);
@@ -469,45 +501,55 @@ __global__ void __launch_bounds__(q4_threads<R, EG>(), PER_SM) q4_matmul_kernel(
         if (!ok && lane == 0) set_timeout(p.ctl, &abort_flag);
         mma_commit_if(lead, &bars.drain);
         int never = 0;
-        warp_wait(&bars.drain, 0u, &never);
+        role_wait(&bars.drain, 0u, &never);
     } else if (warp >= kDeq) {
-        // ---- weights to fp16: four warps the first 64 k of a stage, four the others
-        const int h = (warp - kDeq) >> 2, quad = warp & 3, r = quad * 32 + lane;
+        // ---- weights to fp16: two warpgroups take turns at the stages
+        const int group = (warp - kDeq) >> 2, quad = warp & 3, r = quad * 32 + lane;
         const int per = kStageK / p.G;
-        const int sub0 = (2 * h * per) >> 2, sub1 = ((2 * h + 1) * per) >> 2;
-        const uint32_t dst = tmem + ((uint32_t)(quad * 32) << 16) + 2 * TN + h * 32;
-        const __half2 k1536 = __float2half2_rn(-1536.f);
+        const uint32_t dst = tmem + ((uint32_t)(quad * 32) << 16) + 2 * TN;
         bool ok = true;
         Slot s, a;
-        for (int it = 0; it < n_it; ++it) {
-            ok = warp_wait(&bars.full[s.i], s.parity, &abort_flag);
+        if (group) {
+            s.next(p.stages);
+            a.next(NA);
+        }
+        for (int it = group; it < n_it; it += 2) {
+            ok = role_wait(&bars.full[s.i], s.parity, &abort_flag);
             if (!ok) break;
             const char *const w = wring + (size_t)s.i * blk;
-            const uint4 q0 = reinterpret_cast<const uint4 *>(w)[(2 * h) * kRows + r];
-            const uint4 q1 = reinterpret_cast<const uint4 *>(w)[(2 * h + 1) * kRows + r];
-            const __half *const sc = reinterpret_cast<const __half *>(w + kCodeBytes);
-            const __half2 t0 = __half2half2(sc[sub0 * kRows + r]), t1 = __half2half2(sc[sub1 * kRows + r]);
+            uint4 q[4];
+            __half sc[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                q[j] = reinterpret_cast<const uint4 *>(w)[j * kRows + r];
+                sc[j] = reinterpret_cast<const __half *>(w + kCodeBytes)[((j * per) >> 2) * kRows + r];
+            }
             __syncwarp();
             if (lane == 0) mbar_arrive(&bars.empty[s.i]);
-            const __half2 c0 = __hmul2(t0, k1536), c1 = __hmul2(t1, k1536);
-            uint32_t v[32];
-            dequant8(q0.x, t0, c0, v);
-            dequant8(q0.y, t0, c0, v + 4);
-            dequant8(q0.z, t0, c0, v + 8);
-            dequant8(q0.w, t0, c0, v + 12);
-            dequant8(q1.x, t1, c1, v + 16);
-            dequant8(q1.y, t1, c1, v + 20);
-            dequant8(q1.z, t1, c1, v + 24);
-            dequant8(q1.w, t1, c1, v + 28);
-            if (it >= NA) ok = warp_wait(&bars.a_empty[a.i], a.parity ^ 1u, &abort_flag);
+            if (it >= NA) ok = role_wait(&bars.a_empty[a.i], a.parity ^ 1u, &abort_flag);
             if (!ok) break;
             tc_fence_after();
-            tmem_st32(dst + a.i * 64, v);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                uint32_t v[32];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const Scale t(sc[2 * h + j]);
+                    const uint4 c = q[2 * h + j];
+                    dequant8(c.x, t, v + 16 * j);
+                    dequant8(c.y, t, v + 16 * j + 4);
+                    dequant8(c.z, t, v + 16 * j + 8);
+                    dequant8(c.w, t, v + 16 * j + 12);
+                }
+                tmem_st32(dst + a.i * 64 + h * 32, v);
+            }
             tmem_st_wait();
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&bars.a_full[a.i][h]);
+            if (lane == 0) mbar_arrive(&bars.a_full[a.i]);
             s.next(p.stages);
+            s.next(p.stages);
+            a.next(NA);
             a.next(NA);
         }
         if (!ok && lane == 0) set_timeout(p.ctl, &abort_flag);
@@ -528,7 +570,7 @@ __global__ void __launch_bounds__(q4_threads<R, EG>(), PER_SM) q4_matmul_kernel(
         Slot d;
         int ks = ks0, tile = tile0;
         for (int it = 0; it < n_it; ++it) {
-            ok = warp_wait(&bars.d_full[d.i], d.parity, &abort_flag);
+            ok = role_wait(&bars.d_full[d.i], d.parity, &abort_flag);
             if (!ok) break;
             tc_fence_after();
 #pragma unroll
