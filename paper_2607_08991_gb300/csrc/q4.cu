@@ -16,6 +16,7 @@
 #include <cuda_fp16.h>
 #include <new>
 
+#include "rows.cuh"
 #include "tc_common.cuh"
 
 struct sats_q4 {
@@ -50,58 +51,175 @@ __host__ __device__ constexpr int div_up(int a, int b) { return (a + b - 1) / b;
 // amax over the group, s = bf16(amax / 7), q = w / s rounded half to even.  w / s is either a tie or further than 2^-10
 // from one (a ratio of two numbers of 8 bits), so a product with 1 / s that is first rounded to a multiple of 2^-11
 // decides as the division does.  A group with an infinity or a NaN gets the scale NaN and codes 0.
-constexpr int kQuantThreads = 128;
+//
+// A warp has 128 columns and 32 rows: a thread's 32 x 4 values stay in registers between amax and codes, so W is read
+// once; the warps of a group meet in shared memory for its amax.  The codes of two rows are one multiply-add of the
+// whole numbers' floating-point bits.
+constexpr int kQuantWarps = 4, kQuantRows = 32, kQuantCols = 128;
 
-__device__ __forceinline__ uint32_t quant_nibble(float w, float r, float s, bool tiny)
+// Whether rows of `elems` elements from p on can be read or written in vectors of four elements.
+bool in_fours(const void *p, int64_t elems, int elem_bytes)
 {
-    constexpr float kGrid = 6144.f;        // 1.5 x 2^12: adding it leaves multiples of 2^-11
-    constexpr float kWhole = 12582912.f;   // 1.5 x 2^23: of 1
-    if (!tiny) {
-        const float snapped = __fsub_rn(__fmaf_rn(w, r, kGrid), kGrid);
-        return __float_as_uint(__fadd_rn(snapped, kWhole)) & 15u;
-    }
-    if (!(s > 0.f)) return 0u;
-    const float q = fminf(fmaxf(rintf(__fdiv_rn(w, s)), -7.f), 7.f);
-    return (uint32_t)(int)q & 15u;
+    return reinterpret_cast<uintptr_t>(p) % (4 * elem_bytes) == 0 && elems % 4 == 0;
 }
 
-__global__ void __launch_bounds__(kQuantThreads) q4_quantize_kernel(const uint16_t *W, int64_t ld, int K, int N, int G,
-                                                                     uint8_t *codes, uint16_t *scales)
+// Four bytes of each lane, for columns n..n + 3 of a row of bytes that starts anywhere.
+__device__ __forceinline__ void store_row_bytes(uint8_t *row, int n, int N, uint32_t v, int lane)
 {
-    const int64_t n = (int64_t)blockIdx.x * kQuantThreads + threadIdx.x;
-    if (n >= N) return;
-    for (int g = blockIdx.y; g < div_up(K, G); g += gridDim.y) {
-        const int k0 = g * G, k1 = min(K, k0 + G);
-        const uint16_t *w = W + (int64_t)k0 * ld + n;
-        uint32_t top = 0;
-        for (int k = k0; k < k1; ++k) top = max(top, (uint32_t)w[(int64_t)(k - k0) * ld] & 0x7fffu);
-        const bool odd = top >= 0x7f80u;
-        const uint16_t sb = odd ? 0x7fc0u : bf16_bits(__fdiv_rn(__uint_as_float(top << 16), 7.f));
-        const float s = __uint_as_float((uint32_t)sb << 16);
-        const bool tiny = !(s >= 1.17549435e-38f);
-        const float r = tiny ? 0.f : __frcp_rn(s);
-        scales[(int64_t)g * N + n] = sb;
-        for (int k = k0; k < k1; k += 2) {
-            const float a = __uint_as_float((uint32_t)w[(int64_t)(k - k0) * ld] << 16);
-            const float b = __uint_as_float((uint32_t)w[(int64_t)(k + 1 - k0) * ld] << 16);
-            const uint32_t c = odd ? 0u : quant_nibble(a, r, s, tiny) | quant_nibble(b, r, s, tiny) << 4;
-            codes[(int64_t)(k / 2) * N + n] = (uint8_t)c;
+    const int lead = (int)(reinterpret_cast<uintptr_t>(row + n - 4 * lane) & 3u);   // the same in all lanes
+    const uint32_t before = __shfl_up_sync(0xffffffffu, v, 1);
+    if (lead == 0) {
+        if (n + 4 <= N) *reinterpret_cast<uint32_t *>(row + n) = v;
+        else
+            for (int j = 0; n + j < N; ++j) row[n + j] = (uint8_t)(v >> 8 * j);
+        return;
+    }
+    // the aligned word that begins `lead` bytes before n: the last bytes of the lane before and the first of this one
+    const uint32_t w = __funnelshift_l(before, v, 8 * lead);
+    if (lane > 0 && n - lead + 4 <= N) *reinterpret_cast<uint32_t *>(row + n - lead) = w;
+    else
+        for (int j = lane > 0 ? -lead : 0; j < 4 - lead && n + j < N; ++j) row[n + j] = (uint8_t)(w >> 8 * (j + lead));
+    if (lane == 31)
+        for (int j = 4 - lead; j < 4 && n + j < N; ++j) row[n + j] = (uint8_t)(v >> 8 * j);
+}
+
+template <bool FOURS>
+__global__ void __launch_bounds__(32 * kQuantWarps) q4_quantize_kernel(const uint16_t *W, int64_t ld, int K, int N, int G,
+                                                                       uint8_t *codes, uint16_t *scales)
+{
+    __shared__ uint32_t tops[kQuantWarps][32][4];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int n = blockIdx.x * kQuantCols + 4 * lane;
+    const int per = G / kQuantRows;   // warps of a group
+    for (int k0 = (blockIdx.y * kQuantWarps + warp) * kQuantRows; k0 - warp * kQuantRows < K;
+         k0 += gridDim.y * kQuantWarps * kQuantRows) {
+        uint32_t w[kQuantRows][2];   // columns n, n + 1 and n + 2, n + 3
+#pragma unroll
+        for (int i = 0; i < kQuantRows; ++i) {
+            w[i][0] = w[i][1] = 0u;
+            if (k0 + i >= K) continue;
+            const uint16_t *const p = W + (int64_t)(k0 + i) * ld + n;
+            if (FOURS && n + 4 <= N) {
+                const uint2 q = __ldcs(reinterpret_cast<const uint2 *>(p));
+                w[i][0] = q.x;
+                w[i][1] = q.y;
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (n + j < N) w[i][j >> 1] |= (uint32_t)p[j] << 16 * (j & 1);
+            }
+        }
+        // magnitudes as whole numbers: they order as the values do, infinities and NaN above
+        uint32_t m[2] = {0u, 0u};
+#pragma unroll
+        for (int i = 0; i < kQuantRows; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) m[j] = __vmaxu2(m[j], w[i][j] & 0x7fff7fffu);
+        uint32_t top[4] = {m[0] & 0xffffu, m[0] >> 16, m[1] & 0xffffu, m[1] >> 16};
+        if (per > 1) {
+            *reinterpret_cast<uint4 *>(tops[warp][lane]) = make_uint4(top[0], top[1], top[2], top[3]);
+            __syncthreads();
+            for (int o = warp / per * per; o < (warp / per + 1) * per; ++o)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) top[j] = max(top[j], tops[o][lane][j]);
+            __syncthreads();
+        }
+        if (k0 >= K) continue;
+        float s[4], r[4];
+        uint16_t sb[4];
+        bool slow = false;   // subnormal scales and groups that are not finite
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            sb[j] = top[j] >= 0x7f80u ? 0x7fc0u : bf16_bits(__fdiv_rn(__uint_as_float(top[j] << 16), 7.f));
+            s[j] = __uint_as_float((uint32_t)sb[j] << 16);
+            const bool fine = s[j] >= 1.17549435e-38f;
+            slow = slow || (!fine && top[j] != 0u);
+            r[j] = fine ? __frcp_rn(s[j]) : 0.f;
+        }
+        if (k0 % G == 0) {
+            uint16_t *const p = scales + (int64_t)(k0 / G) * N + n;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (n + j < N) p[j] = sb[j];
+        }
+        const f32x2 r01 = pack2(r[0], r[1]), r23 = pack2(r[2], r[3]);
+        const f32x2 grid = pack2(6144.f, 6144.f), no_grid = pack2(-6144.f, -6144.f);   // 1.5 x 2^12: multiples of 2^-11
+        const f32x2 whole = pack2(12582920.f, 12582920.f);                             // 1.5 x 2^23 + 8: of 1; bits: q + 8
+        auto rounded = [&](uint32_t v, f32x2 rr) {
+            return fadd2(fadd2(ffma2(bf16x2_to_f32x2(v), rr, grid), no_grid), whole);
+        };
+#pragma unroll
+        for (int i = 0; i < kQuantRows; i += 2) {
+            if (k0 + i >= K) break;
+            uint32_t b[4];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const float2 even = unpack2(rounded(w[i][j], j ? r23 : r01)), odd = unpack2(rounded(w[i + 1][j], j ? r23 : r01));
+                b[2 * j] = __float_as_uint(odd.x) * 16u + __float_as_uint(even.x);
+                b[2 * j + 1] = __float_as_uint(odd.y) * 16u + __float_as_uint(even.y);
+            }
+            uint32_t v = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410) ^ 0x88888888u;
+            if (slow) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float sj = s[j];
+                    if (sj >= 1.17549435e-38f) continue;
+                    uint32_t c = 0;
+#pragma unroll
+                    for (int o = 0; o < 2; ++o) {
+                        const float x = __uint_as_float(w[i + o][j >> 1] >> 16 * (j & 1) << 16);
+                        const float q = sj > 0.f ? fminf(fmaxf(rintf(__fdiv_rn(x, sj)), -7.f), 7.f) : 0.f;
+                        c |= ((uint32_t)(int)q & 15u) << 4 * o;
+                    }
+                    v = (v & ~(0xffu << 8 * j)) | c << 8 * j;
+                }
+            }
+            store_row_bytes(codes + (int64_t)((k0 + i) / 2) * N, n, N, v, lane);
         }
     }
 }
 
-__device__ __forceinline__ float code_value(uint32_t nibble) { return (float)((int)(nibble << 28) >> 28); }
+// Eight bytes of codes of a thread at a time; a nibble's value from the bits of a float.
+constexpr int kReadRows = 16;   // of codes, 32 of values: within a group
 
+__device__ __forceinline__ float code_value(uint32_t nibble)   // (what lies above the nibble does not matter)
+{
+    return __uint_as_float(((nibble & 15u) ^ 8u) | 0x4b000000u) - 8388616.f;
+}
+
+template <bool FOURS>
 __global__ void __launch_bounds__(256) q4_dequantize_kernel(const uint8_t *codes, const uint16_t *scales, int K, int N, int G,
                                                             float *values)
 {
-    const int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    constexpr int C = FOURS ? 4 : 1;
+    const int64_t n = ((int64_t)blockIdx.x * 256 + threadIdx.x) * C;
     if (n >= N) return;
-    for (int k2 = blockIdx.y; k2 < K / 2; k2 += gridDim.y) {
-        const uint32_t c = codes[(int64_t)k2 * N + n];
-        const float s = __uint_as_float((uint32_t)scales[(int64_t)(2 * k2 / G) * N + n] << 16);
-        values[(int64_t)(2 * k2) * N + n] = code_value(c) * s;
-        values[(int64_t)(2 * k2 + 1) * N + n] = code_value(c >> 4) * s;
+    const int rows = K / 2;
+    for (int i0 = blockIdx.y * kReadRows; i0 < rows; i0 += gridDim.y * kReadRows) {
+        uint32_t c[kReadRows];
+#pragma unroll
+        for (int i = 0; i < kReadRows; ++i) {
+            c[i] = 0u;
+            if (i0 + i >= rows) continue;
+            const uint8_t *const p = codes + (int64_t)(i0 + i) * N + n;
+            c[i] = FOURS ? __ldcs(reinterpret_cast<const uint32_t *>(p)) : __ldcs(p);
+        }
+        float s[C];
+#pragma unroll
+        for (int j = 0; j < C; ++j) s[j] = __uint_as_float((uint32_t)scales[(int64_t)(2 * i0 / G) * N + n + j] << 16);
+#pragma unroll
+        for (int i = 0; i < kReadRows; ++i) {
+            if (i0 + i >= rows) break;
+            float *const p = values + (int64_t)(i0 + i) * 2 * N + n;
+#pragma unroll
+            for (int o = 0; o < 2; ++o) {
+                float v[C];
+#pragma unroll
+                for (int j = 0; j < C; ++j) v[j] = code_value(c[i] >> (8 * j + 4 * o)) * s[j];
+                if constexpr (FOURS) __stcs(reinterpret_cast<float4 *>(p + (int64_t)o * N), make_float4(v[0], v[1], v[2], v[3]));
+                else __stcs(p + (int64_t)o * N, v[0]);
+            }
+        }
     }
 }
 
@@ -781,9 +899,12 @@ sats_status sats_q4_quantize(const void *W, int64_t ld, int K, int N, int G, uin
     if (!q4_shape_ok(K, N, G) || ld > (int64_t)1 << 40) return SATS_ESHAPE;
     if (!W || !codes || !scales || reinterpret_cast<uintptr_t>(W) % 2 || reinterpret_cast<uintptr_t>(scales) % 2)
         return SATS_EINVAL;
-    const dim3 grid(div_up(N, kQuantThreads), std::min(div_up(K, G), 65535));
-    q4_quantize_kernel<<<grid, kQuantThreads, 0, static_cast<cudaStream_t>(stream)>>>(
-        static_cast<const uint16_t *>(W), ld, K, N, G, codes, static_cast<uint16_t *>(scales));
+    const dim3 grid(div_up(N, kQuantCols), div_up(K, kQuantWarps * kQuantRows));
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const uint16_t *const w = static_cast<const uint16_t *>(W);
+    uint16_t *const sc = static_cast<uint16_t *>(scales);
+    if (in_fours(W, ld, 2)) q4_quantize_kernel<true><<<grid, 32 * kQuantWarps, 0, st>>>(w, ld, K, N, G, codes, sc);
+    else q4_quantize_kernel<false><<<grid, 32 * kQuantWarps, 0, st>>>(w, ld, K, N, G, codes, sc);
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? SATS_OK : cuda_fail(e, "quantising kernel launch");
 }
@@ -793,9 +914,12 @@ sats_status sats_q4_dequantize(const uint8_t *codes, const void *scales, int K, 
     if (!q4_shape_ok(K, N, G)) return SATS_ESHAPE;
     if (!codes || !scales || !values || reinterpret_cast<uintptr_t>(scales) % 2 || reinterpret_cast<uintptr_t>(values) % 4)
         return SATS_EINVAL;
-    const dim3 grid(div_up(N, 256), std::min(K / 2, 65535));
-    q4_dequantize_kernel<<<grid, 256, 0, static_cast<cudaStream_t>(stream)>>>(
-        codes, static_cast<const uint16_t *>(scales), K, N, G, values);
+    const bool fours = in_fours(codes, N, 1) && in_fours(values, N, 4);
+    const dim3 grid(div_up(N, fours ? 1024 : 256), div_up(K / 2, kReadRows));
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const uint16_t *const sc = static_cast<const uint16_t *>(scales);
+    if (fours) q4_dequantize_kernel<true><<<grid, 256, 0, st>>>(codes, sc, K, N, G, values);
+    else q4_dequantize_kernel<false><<<grid, 256, 0, st>>>(codes, sc, K, N, G, values);
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? SATS_OK : cuda_fail(e, "reading back kernel launch");
 }
