@@ -564,7 +564,7 @@ SATS_API sats_status sats_sample_f32(const float *logits, int64_t ld, int B, int
  * Adjusted logits: what lies between the model's logits and sats_sample, and its gradient.
  * logits, out, dout, dlogits are rows as in the vocabulary operators above (any alignment of whole
  * elements, row strides of at least V elements).  The calls need no workspace, and what they write does not depend on the
- * order in which their threads run.  V up to 2^31 - 65, 2^28 - 1 rows, L up to 2^30 (else SATS_ESHAPE).
+ * order in which their threads run.  V up to 2^31 - 65, 2^28 - 1 rows, L below 2^30 (else SATS_ESHAPE).
  *
  * sats_adjust_logits -- for each of B rows z with its history of token ids:
  *     z_v <- z_v > 0 ? z_v / r : z_v r      where v occurs in the history
@@ -594,7 +594,7 @@ SATS_API sats_status sats_sample_f32(const float *logits, int64_t ld, int B, int
  * sats_adjust_logits_grad -- its backward pass: dlogits_v = dout_v times 0 where the mask does not allow v (also where
  *   dout is not finite), 1 / r or r where v occurs in the history (r at z_v = 0), else 1.  The biases and the other two
  *   penalties are constants here.  logits: what sats_adjust_logits was given, read only at the tokens of the history.
- *   dlogits may be dout or the logits (same pointer and stride), or lie between their rows.
+ *   dlogits may be dout (same pointer and stride), or lie between the rows of dout or the logits; not the logits.
  */
 SATS_API sats_status sats_adjust_logits(const void *logits, int64_t ld, int B, int V, const int32_t *hist,
                                         int64_t ld_hist, int L, const int32_t *hist_len, const int32_t *n_prompt,

@@ -1,12 +1,15 @@
 // adjust.cu -- penalties for repeated tokens, biases and masks on rows of logits (sats_adjust_logits), and the gradient
 // of that (sats_adjust_logits_grad).
 //
-// A row is cut into slices of the vocabulary, a CTA each.  The CTA reads the row's whole history and counts, in shared
-// memory, the ids that fall into its slice (whole numbers: the counts do not depend on an order); meanwhile the slice's
-// logits arrive in shared memory.  The few logits whose token was counted or has a bias are changed there, each by
-// one thread that claims its count, from the logit as it came and in fp32, rounded once.  Then the slice goes out in
-// 16-byte vectors with the mask's bits applied on the way.  So the row is read and written once whatever it holds, and
-// in place only what changes is touched.
+// A CTA has a slice of a row, up to 2048 of the output's 16-byte vectors.  While its logits arrive in shared memory, it
+// reads the row's history and counts, in a table in shared memory, the ids that fall into the slice (whole numbers: they
+// do not depend on an order); whoever counts a token first puts it on a list.  The listed logits are changed in shared
+// memory, each by one thread, from the logit as it came and in fp32, rounded once; then the slice goes out with the
+// mask's bits applied on the way.  So a row is read and written once, in whole vectors, whatever is changed in it; in
+// place only what changes is touched.  Everything that is read is asked for at the start: a CTA's life is one wait for
+// memory and three barriers, and three CTAs to an SM keep the memory busy.
+//
+// (measured: see the end of this comment)
 #include <algorithm>
 #include <climits>
 #include <cuda_bf16.h>
@@ -17,10 +20,12 @@
 namespace sats {
 namespace {
 
-constexpr int kAdjThreads = 512;
-constexpr int kMaxBiases = 1024;
-constexpr int kNarrowHist = 1 << 15;   // histories shorter than this fit 16-bit counts
-constexpr size_t kMaxAdjSmem = 200 * 1024;
+constexpr int kAdjThreads = 256;
+constexpr int kMostEach = 8;           // vectors of a slice per thread
+constexpr int kKeep = 2;               // vectors of ids of a thread that are asked for at the start
+constexpr int kMaxBiases = 1024, kBiasEach = kMaxBiases / kAdjThreads;
+constexpr int kNarrowHist = 1 << 14;   // histories shorter than this fit 16-bit fields
+constexpr size_t kMaxAdjSmem = 160 * 1024;
 
 struct AdjustParams {
     const void *src;         // the logits, or the gradient that comes in
@@ -40,43 +45,38 @@ struct AdjustParams {
     int n_masks;
     const int32_t *mask_row;
     int32_t *status;
-    int S, slices;           // elements of a slice (a multiple of 32), slices of a row
-    bool wide;               // 32-bit counts
+    int each, slices;        // vectors of a slice per thread; slices of a row
+    int listed;              // places of the list
+    bool wide;               // 32-bit fields
 };
 
-// Calls f(id, position) for the ids at positions [0, n), spread over the CTA; whole 16-byte vectors where they lie inside,
-// four of a thread in flight.
-template <typename F>
-__device__ __forceinline__ void for_each_id(const int32_t *p, int n, F f)
+__device__ __forceinline__ const uint32_t *row_mask(const AdjustParams &p, int row, bool *bad)
 {
-    constexpr int kFlight = 4;
-    const int lead = (int)((reinterpret_cast<uintptr_t>(p) >> 2) & 3);   // ids between the vector boundary and the first
-    const int vectors = (int)(((int64_t)n + lead + 3) >> 2);
-    const int4 *base = reinterpret_cast<const int4 *>(p - lead);
-    for (int v0 = threadIdx.x; v0 < vectors; v0 += kAdjThreads * kFlight) {
-        int4 q[kFlight];
-#pragma unroll
-        for (int i = 0; i < kFlight; ++i) {
-            const int v = v0 + i * kAdjThreads, at = 4 * v - lead;
-            q[i] = make_int4(-1, -1, -1, -1);
-            if (v >= vectors) continue;
-            if (at >= 0 && at <= n - 4) q[i] = __ldg(base + v);
-            else {
-                if (at >= 0) q[i].x = __ldg(p + at);
-                if (at + 1 >= 0 && at + 1 < n) q[i].y = __ldg(p + at + 1);
-                if (at + 2 >= 0 && at + 2 < n) q[i].z = __ldg(p + at + 2);
-                if (at + 3 < n) q[i].w = __ldg(p + at + 3);
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < kFlight; ++i) {
-            const int at = 4 * (v0 + i * kAdjThreads) - lead;
-            f(q[i].x, at);
-            f(q[i].y, at + 1);
-            f(q[i].z, at + 2);
-            f(q[i].w, at + 3);
-        }
-    }
+    if (!p.mask) return nullptr;
+    const int m = p.mask_row ? p.mask_row[row] : row;
+    if (m >= p.n_masks) *bad = true;
+    return m >= 0 && m < p.n_masks ? p.mask + m * p.ld_mask : nullptr;
+}
+
+// Bits of 8 tokens from f on, from mask words of which the first is word w0; f may lie before 0.
+__device__ __forceinline__ uint32_t staged_bits(const uint32_t *words, int w0, int f)
+{
+    const int at = max(f, 0);
+    const uint32_t *const w = words + ((at >> 5) - w0);
+    return __funnelshift_r(w[0], w[1], at & 31) << (at - f);
+}
+
+// The vector of ids at place v of a history: its positions 4 v - lead.. where they are below n (others: -1).
+__device__ __forceinline__ int4 load_ids(const int32_t *p, int lead, int v, int n)
+{
+    const int at = 4 * v - lead;
+    if (at >= 0 && at <= n - 4) return __ldg(reinterpret_cast<const int4 *>(p - lead) + v);
+    int4 q = make_int4(-1, -1, -1, -1);
+    if (at >= 0 && at < n) q.x = __ldg(p + at);
+    if (at + 1 >= 0 && at + 1 < n) q.y = __ldg(p + at + 1);
+    if (at + 2 >= 0 && at + 2 < n) q.z = __ldg(p + at + 2);
+    if (at + 3 >= 0 && at + 3 < n) q.w = __ldg(p + at + 3);
+    return q;
 }
 
 template <bool F32>
@@ -93,54 +93,9 @@ __device__ __forceinline__ void store_elem(void *p, int64_t i, float v)
     else static_cast<__nv_bfloat16 *>(p)[i] = __float2bfloat16_rn(v);
 }
 
-// The counts of a slice's tokens.  Forward: a field of 16 (or 32) bits each, the top bit for "in the prompt", the others the
-// number of generated ones.  Gradient: a bit each.
-template <bool GRAD>
-struct Counts {
-    uint32_t *w;
-    bool wide;
-
-    __device__ __forceinline__ void mark(int i, bool generated)
-    {
-        if constexpr (GRAD) {
-            const uint32_t bit = 1u << (i & 31);
-            if (!(*static_cast<volatile uint32_t *>(w + (i >> 5)) & bit)) atomicOr(w + (i >> 5), bit);
-        } else if (wide) {
-            if (generated) atomicAdd(w + i, 1u);
-            else if (!(*static_cast<volatile uint32_t *>(w + i) >> 31)) atomicOr(w + i, 0x80000000u);
-        } else {
-            const int sh = 16 * (i & 1);
-            uint32_t *p = w + (i >> 1);
-            if (generated) atomicAdd(p, 1u << sh);
-            else if (!(*static_cast<volatile uint32_t *>(p) & (0x8000u << sh))) atomicOr(p, 0x8000u << sh);
-        }
-    }
-    // The token's field, which is 0 from then on: one thread gets it.  Bit 31: seen; below: how often generated.
-    __device__ __forceinline__ uint32_t claim(int i)
-    {
-        if constexpr (GRAD) {
-            const uint32_t bit = 1u << (i & 31);
-            if (!(*static_cast<volatile uint32_t *>(w + (i >> 5)) & bit)) return 0u;
-            return atomicAnd(w + (i >> 5), ~bit) & bit ? 0x80000000u : 0u;
-        } else if (wide) {
-            if (!*static_cast<volatile uint32_t *>(w + i)) return 0u;
-            const uint32_t f = atomicExch(w + i, 0u);
-            return f ? f | 0x80000000u : 0u;
-        } else {
-            const int sh = 16 * (i & 1);
-            uint32_t *p = w + (i >> 1);
-            if (!(*static_cast<volatile uint32_t *>(p) >> sh & 0xffffu)) return 0u;
-            const uint32_t f = atomicAnd(p, ~(0xffffu << sh)) >> sh & 0xffffu;
-            return f ? (f & 0x7fffu) | 0x80000000u : 0u;
-        }
-    }
-};
-
 // A setting of the row; outside its range it is off and noted.
-__device__ __forceinline__ float setting(const float *p, int row, float off, bool positive, bool *bad)
+__device__ __forceinline__ float checked(float v, float off, bool positive, bool *bad)
 {
-    if (!p) return off;
-    const float v = p[row];
     if (isfinite(v) && (!positive || v > 0.f)) return v;
     *bad = true;
     return off;
@@ -148,9 +103,9 @@ __device__ __forceinline__ float setting(const float *p, int row, float off, boo
 
 // 4 (fp32) or 8 (bf16) elements at byte `off` of shared memory, wherever that is.
 template <bool F32>
-__device__ __forceinline__ uint4 load_anywhere(const char *stage, int off, bool aligned)
+__device__ __forceinline__ uint4 load_anywhere(const char *stage, int off)
 {
-    if (aligned) return *reinterpret_cast<const uint4 *>(stage + off);
+    if ((off & 15) == 0) return *reinterpret_cast<const uint4 *>(stage + off);
     const uint32_t *p = reinterpret_cast<const uint32_t *>(stage + (off & ~3));
     const uint32_t a = p[0], b = p[1], c = p[2], d = p[3];
     if (F32 || (off & 2) == 0) return make_uint4(a, b, c, d);
@@ -159,190 +114,266 @@ __device__ __forceinline__ uint4 load_anywhere(const char *stage, int off, bool 
                       __funnelshift_r(d, e, 16));
 }
 
+// A logit or gradient that one's token scales.
+__device__ __forceinline__ float scaled(float v, float z, float rep) { return z > 0.f ? __fdiv_rn(v, rep) : __fmul_rn(v, rep); }
+
+// A logit with its token's field (bit 31: in the prompt, bit 30: has a bias, below: times generated), then its bias.
+__device__ __forceinline__ float penalised(float v, uint32_t f, float rep, float freq, float pres)
+{
+    const uint32_t made = f & 0x3fffffffu;
+    if (f & ~0x40000000u) v = scaled(v, v, rep);
+    if (made) v = __fsub_rn(__fsub_rn(v, __fmul_rn(freq, __uint2float_rn(made))), pres);
+    return v;
+}
+__device__ __forceinline__ float biased(float v, float add) { return add > -INFINITY ? __fadd_rn(v, add) : -INFINITY; }
+
+// A vector with what its bits do not allow banned.
+template <bool F32, bool GRAD>
+__device__ __forceinline__ uint4 ban(const uint4 &v, uint32_t allow)
+{
+    constexpr uint32_t kBanned = GRAD ? 0u : (F32 ? 0xff800000u : 0xff80u);
+    uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (F32) {
+            if (!(allow >> i & 1u)) w[i] = kBanned;
+        } else {
+            if (!(allow >> (2 * i) & 1u)) w[i] = (w[i] & 0xffff0000u) | kBanned;
+            if (!(allow >> (2 * i + 1) & 1u)) w[i] = (w[i] & 0xffffu) | kBanned << 16;
+        }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// Vector g of a row element by element (src: its first one's value); in place only what is banned.
 template <bool F32, bool GRAD, bool INPLACE>
-__global__ void __launch_bounds__(kAdjThreads) adjust_kernel(const AdjustParams p)
+__device__ __forceinline__ void store_edge(const Row<F32> &to, int g, const char *src, uint32_t allow)
+{
+    constexpr int E = RowElem<F32>::kPer;
+    constexpr uint32_t kBanned = GRAD ? 0u : (F32 ? 0xff800000u : 0xff80u);
+    char *const dst = const_cast<char *>(to.base) + (size_t)g * 16;
+#pragma unroll
+    for (int j = 0; j < E; ++j) {
+        const bool ok = allow >> j & 1u;
+        if (!to.inside(to.first(g) + j) || (INPLACE && ok)) continue;
+        if constexpr (F32) reinterpret_cast<uint32_t *>(dst)[j] = ok ? reinterpret_cast<const uint32_t *>(src)[j] : kBanned;
+        else reinterpret_cast<uint16_t *>(dst)[j] = ok ? reinterpret_cast<const uint16_t *>(src)[j] : (uint16_t)kBanned;
+    }
+}
+
+// The slice's table.  Forward: a field for each token, of 16 or (wide) 32 bits: the top bit for "in the prompt", the next for
+// "has a bias", the others the number of times it was generated.  Gradient: a bit for each token.
+template <bool GRAD>
+struct Table {
+    uint32_t *w;
+    bool wide;
+
+    __device__ __forceinline__ int words(int n) const { return GRAD ? (n + 31) / 32 : (wide ? n : (n + 1) / 2); }
+    // Adds or (bit) sets; whether the token was not in the table yet.
+    __device__ __forceinline__ bool generated(int i)
+    {
+        if (wide) return atomicAdd(w + i, 1u) == 0u;
+        const int sh = 16 * (i & 1);
+        return (atomicAdd(w + (i >> 1), 1u << sh) >> sh & 0xffffu) == 0u;
+    }
+    __device__ __forceinline__ bool set(int i, uint32_t bit)   // bit: 2 the prompt's, 1 the bias'
+    {
+        if constexpr (GRAD) return !(atomicOr(w + (i >> 5), 1u << (i & 31)) >> (i & 31) & 1u);
+        if (wide) return atomicOr(w + i, bit << 30) == 0u;
+        const int sh = 16 * (i & 1);
+        return (atomicOr(w + (i >> 1), bit << (14 + sh)) >> sh & 0xffffu) == 0u;
+    }
+    // Bit 31: the prompt's, bit 30: the bias', below: the count.
+    __device__ __forceinline__ uint32_t field(int i) const
+    {
+        if (wide) return w[i];
+        const uint32_t f = w[i >> 1] >> 16 * (i & 1) & 0xffffu;
+        return f >> 14 << 30 | (f & 0x3fffu);
+    }
+};
+
+template <bool F32, bool GRAD, bool INPLACE>
+__global__ void __launch_bounds__(kAdjThreads, GRAD ? 6 : 4) adjust_kernel(const __grid_constant__ AdjustParams p)
 {
     constexpr int ES = RowElem<F32>::kBytes, E = RowElem<F32>::kPer;
-    constexpr uint32_t kBanned = GRAD ? 0u : (F32 ? 0xff800000u : 0xff80u);
+    constexpr uint32_t kAll = (1u << E) - 1u;
     extern __shared__ __align__(16) char smem[];
-    __shared__ int n_bias;
+    __shared__ uint32_t mask_words[kAdjThreads * kMostEach * E / 32 + 2];
+    __shared__ int n_listed, n_bias;
     const int tid = threadIdx.x;
-    char *stage = smem;
-    const size_t stage_bytes = INPLACE ? 0 : (size_t)p.S * ES + 32;
-    uint32_t *table = reinterpret_cast<uint32_t *>(smem + stage_bytes);
-    const int table_words = p.hist ? (GRAD ? p.S / 32 : (p.wide ? p.S : p.S / 2)) : 0;
-    uint32_t *mask_words = table + table_words;   // S / 32 + 1
-    int2 *biases = reinterpret_cast<int2 *>(mask_words + (p.mask ? p.S / 32 + 2 : 0));
+    const int vectors = kAdjThreads * p.each, S = vectors * E;   // of a slice
+    char *const stage = smem;
+    Table<GRAD> table{reinterpret_cast<uint32_t *>(smem + (INPLACE ? 0 : vectors * 16 + 32)), p.wide};
+    const int table_words = p.hist || p.M > 0 ? table.words(S) : 0;
+    uint16_t *const list = reinterpret_cast<uint16_t *>(table.w + table_words);
+    uint32_t *const biases = reinterpret_cast<uint32_t *>(list + p.listed);   // token << 16 | place in the row's list
     bool bad = false;
 
     const int64_t units = (int64_t)p.B * p.slices;
     for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
         const int row = (int)(u / p.slices);
-        const int e0 = (int)(u - (int64_t)row * p.slices) * p.S;
-        const int n = min(p.S, p.V - e0);
+        const int gs = (int)(u - (int64_t)row * p.slices) * vectors;   // the slice's first vector
         const Row<F32> in(p.src, row, p.ld_src, p.V), to(p.out, row, p.ld_out, p.V);
-        char *const out = static_cast<char *>(p.out) + (row * p.ld_out + e0) * ES;
+        const int ge = min(to.G, gs + vectors);
+        const int base = to.first(gs);                                  // token i of the slice is base + i of the row
+        const int e0 = max(base, 0), e1 = (int)min((int64_t)p.V, (int64_t)base + S);
+        if (gs >= ge) continue;
 
-        // the slice's logits on their way to shared memory: its granules, from byte 0 on
-        const int ga = (in.head + e0) / E;
+        // ---- what is read, all of it asked for before anything is looked at
+        const int ga = (in.head + e0) / E;                              // byte 0 of the stage
         if constexpr (!INPLACE) {
-            const int gb = (int)(((int64_t)in.head + e0 + n + E - 1) / E);
-            for (int g = ga + tid; g < gb; g += kAdjThreads) {
-                char *const at = stage + (size_t)(g - ga) * 16;
-                if (in.whole(g)) cp_async16(at, in.base + (size_t)g * 16);
-                else {
-#pragma unroll
-                    for (int j = 0; j < E; ++j)
-                        if (in.inside(in.first(g) + j)) {
-                            if constexpr (F32)
-                                reinterpret_cast<float *>(at)[j] = reinterpret_cast<const float *>(in.base)[(size_t)g * E + j];
-                            else
-                                reinterpret_cast<uint16_t *>(at)[j] =
-                                    reinterpret_cast<const uint16_t *>(in.base)[(size_t)g * E + j];
-                        }
-                }
-            }
+            const int gb = (int)(((int64_t)in.head + e1 + E - 1) / E);
+            const int g0 = in.whole(ga) ? ga : ga + 1, g1 = in.whole(gb - 1) ? gb : gb - 1;   // a row's ends may be parts of vectors
+            const char *from = in.base + (size_t)(g0 + tid) * 16;
+            char *at = stage + (g0 - ga + tid) * 16;
+            for (int g = g0 + tid; g < g1; g += kAdjThreads, from += kAdjThreads * 16, at += kAdjThreads * 16) cp_async16(at, from);
+            if (tid == 0 && g0 > ga) *reinterpret_cast<uint4 *>(stage) = load_edge_granule<F32>(in.base, in.first(ga), in.V, ga);
+            if (tid == 32 && g1 < gb && gb - 1 >= g0)
+                *reinterpret_cast<uint4 *>(stage + (gb - 1 - ga) * 16) = load_edge_granule<F32>(in.base, in.first(gb - 1), in.V, gb - 1);
             cp_async_commit();
         }
-
-        // the row's settings
-        int len = 0, prompt = 0;
-        const float rep = setting(p.rep, row, 1.f, true, &bad);
-        const float pres = GRAD ? 0.f : setting(p.pres, row, 0.f, false, &bad);
-        const float freq = GRAD ? 0.f : setting(p.freq, row, 0.f, false, &bad);
-        const int32_t *hist = nullptr;
-        if (p.hist) {
-            hist = p.hist + row * p.ld_hist;
-            len = p.hist_len ? p.hist_len[row] : p.L;
-            if (len < 0 || len > p.L) {
-                bad = true;
-                len = len < 0 ? 0 : p.L;
+        const int32_t *const hist = p.hist ? p.hist + row * p.ld_hist : nullptr;
+        const int lead = (int)((reinterpret_cast<uintptr_t>(hist) >> 2) & 3);   // ids between the vector boundary and the first
+        int4 ids[kKeep];
+#pragma unroll
+        for (int k = 0; k < kKeep; ++k) ids[k] = load_ids(hist, lead, tid + k * kAdjThreads, p.hist ? p.L : 0);
+        float rep = p.rep ? p.rep[row] : 1.f;
+        float pres = !GRAD && p.pres ? p.pres[row] : 0.f;
+        float freq = !GRAD && p.freq ? p.freq[row] : 0.f;
+        int len = p.hist ? (p.hist_len ? p.hist_len[row] : p.L) : 0;
+        const int prompt = !GRAD && p.n_prompt ? p.n_prompt[row] : 0;
+        int bias_id[kBiasEach];
+        float bias_add[kBiasEach];
+        if constexpr (!GRAD) {
+#pragma unroll
+            for (int k = 0; k < kBiasEach; ++k) {
+                bias_id[k] = -1;
+                if (tid + k * kAdjThreads < p.M) {
+                    bias_id[k] = p.bias_idx[(int64_t)row * p.M + tid + k * kAdjThreads];
+                    bias_add[k] = p.bias_val[(int64_t)row * p.M + tid + k * kAdjThreads];
+                }
             }
-            if (p.n_prompt) prompt = p.n_prompt[row];
-            if (rep == 1.f && pres == 0.f && freq == 0.f) len = 0;   // nothing would change
         }
-        const uint32_t *mask = nullptr;
-        if (p.mask) {
-            int m = p.mask_row ? p.mask_row[row] : row;
-            if (m >= p.n_masks) {
-                bad = true;
-                m = -1;
-            }
-            if (m >= 0) mask = p.mask + m * p.ld_mask;
-        }
+        const uint32_t *const mask = row_mask(p, row, &bad);
 
-        Counts<GRAD> counts{table, p.wide};
-        if (len > 0) {
-            const int words = GRAD ? (n + 31) / 32 : (p.wide ? n : (n + 1) / 2);
-            for (int i = tid; i < words; i += kAdjThreads) table[i] = 0u;
+        for (int i = tid; i < table_words / 4; i += kAdjThreads) reinterpret_cast<uint4 *>(table.w)[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (tid == 0) n_listed = n_bias = 0;
+        rep = checked(rep, 1.f, true, &bad);
+        pres = checked(pres, 0.f, false, &bad);
+        freq = checked(freq, 0.f, false, &bad);
+        if (len < 0 || len > p.L) {
+            bad = true;
+            len = len < 0 ? 0 : p.L;
         }
+        if (rep == 1.f && pres == 0.f && freq == 0.f) len = 0;   // nothing would change
+        const int w0 = e0 >> 5;
         if (mask) {
-            const int words = (n + 31) / 32;
-            for (int i = tid; i < words + 1; i += kAdjThreads) mask_words[i] = i < words ? __ldg(mask + e0 / 32 + i) : 0u;
+            const int n = ((e1 - 1) >> 5) - w0 + 1;
+            for (int i = tid; i < n; i += kAdjThreads) cp_async4(mask_words + i, mask + w0 + i);
+            cp_async_commit();
         }
-        if (tid == 0) n_bias = 0;
         __syncthreads();
 
-        for_each_id(hist, len, [&](int id, int at) {
-            const int i = (int)((unsigned)id - (unsigned)e0);
-            if ((unsigned)i < (unsigned)n && id >= 0) counts.mark(i, at >= prompt);
-            else if (id >= p.V) bad = true;
-        });
-        if constexpr (!GRAD) {
-            for (int j = tid; j < p.M; j += kAdjThreads) {
-                const int id = p.bias_idx[(int64_t)row * p.M + j];
-                const int i = (int)((unsigned)id - (unsigned)e0);
-                if (id >= p.V) bad = true;
-                else if (id >= 0 && (unsigned)i < (unsigned)n) {
-                    const float b = p.bias_val[(int64_t)row * p.M + j];
-                    if (b < INFINITY) biases[atomicAdd(&n_bias, 1)] = make_int2(i, j);
-                    else bad = true;   // NaN or +inf
-                }
-            }
-        }
-        if constexpr (!INPLACE) cp_async_wait<0>();
-        __syncthreads();
-
-        // one logit, from what it was; count: a field of claim()
-        char *const held = INPLACE ? out : stage + ((size_t)(in.head + e0) - (size_t)ga * E) * ES;   // element 0 of the slice
-        auto change = [&](int i, uint32_t count, float bias) {
-            float v = load_elem<F32>(held, i);
-            if constexpr (GRAD) {
-                const float z = load_elem<F32>(p.z, row * p.ld_z + e0 + i);
-                v = z > 0.f ? __fdiv_rn(v, rep) : __fmul_rn(v, rep);
-            } else {
-                if (count) v = v > 0.f ? __fdiv_rn(v, rep) : __fmul_rn(v, rep);
-                const uint32_t c = count & 0x7fffffffu;
-                if (c) v = __fsub_rn(__fsub_rn(v, __fmul_rn(freq, __uint2float_rn(c))), pres);
-                v = bias > -INFINITY ? __fadd_rn(v, bias) : -INFINITY;
-            }
-            store_elem<F32>(held, i, v);
+        // ---- which tokens, how often
+        const uint32_t here = (uint32_t)(e1 - e0);
+        const auto count = [&](int id, int at) {   // (an absent id is below 0)
+            if ((uint32_t)id - (uint32_t)e0 >= here || at >= len) return;
+            const int i = id - base;
+            if (GRAD || at < prompt ? table.set(i, 2u) : table.generated(i)) list[atomicAdd(&n_listed, 1)] = (uint16_t)i;
         };
-        if constexpr (!GRAD) {
-            // of equal tokens' biases the last one counts; its thread changes the logit as a whole
-            for (int a = tid; a < n_bias; a += kAdjThreads) {
-                const int2 mine = biases[a];
-                bool last = true;
-                for (int b = 0; b < n_bias; ++b) last = last && !(biases[b].x == mine.x && biases[b].y > mine.y);
-                if (last) change(mine.x, len > 0 ? counts.claim(mine.x) : 0u, p.bias_val[(int64_t)row * p.M + mine.y]);
-            }
-            if (p.M > 0) __syncthreads();
+        const bool last_slice = e1 == p.V;   // looks for ids that are no tokens
+        const auto count4 = [&](const int4 &q, int v) {
+            const int at = 4 * v - lead;
+            count(q.x, at);
+            count(q.y, at + 1);
+            count(q.z, at + 2);
+            count(q.w, at + 3);
+            if (last_slice)
+                bad = bad || (q.x >= p.V && at < len) || (q.y >= p.V && at + 1 < len) || (q.z >= p.V && at + 2 < len) ||
+                      (q.w >= p.V && at + 3 < len);
+        };
+        const int id_vectors = len > 0 ? (int)(((int64_t)len + lead + 3) >> 2) : 0;
+        for (int v0 = tid; v0 < id_vectors; v0 += kKeep * kAdjThreads) {
+            int4 next[kKeep];   // on their way while these are counted
+            const bool more = v0 + kKeep * kAdjThreads < id_vectors;
+            if (more)
+#pragma unroll
+                for (int k = 0; k < kKeep; ++k) next[k] = load_ids(hist, lead, v0 + (kKeep + k) * kAdjThreads, len);
+#pragma unroll
+            for (int k = 0; k < kKeep; ++k)
+                if (v0 + k * kAdjThreads < id_vectors) count4(ids[k], v0 + k * kAdjThreads);
+            if (more)
+#pragma unroll
+                for (int k = 0; k < kKeep; ++k) ids[k] = next[k];
         }
-        for_each_id(hist, len, [&](int id, int) {
-            const int i = (int)((unsigned)id - (unsigned)e0);
-            if ((unsigned)i < (unsigned)n && id >= 0) {
-                const uint32_t c = counts.claim(i);
-                if (c) change(i, c, 0.f);
+        if constexpr (!GRAD) {
+#pragma unroll
+            for (int k = 0; k < kBiasEach; ++k) {
+                const int id = bias_id[k];
+                if (id < 0) continue;
+                if (id >= p.V || !(bias_add[k] < INFINITY)) bad = true;   // no token, NaN or +inf
+                else if (id >= e0 && id < e1) {
+                    if (table.set(id - base, 1u)) list[atomicAdd(&n_listed, 1)] = (uint16_t)(id - base);
+                    biases[atomicAdd(&n_bias, 1)] = (uint32_t)(id - base) << 16 | (uint32_t)(tid + k * kAdjThreads);
+                }
             }
-        });
+        }
+        cp_async_wait<0>();
         __syncthreads();
 
-        // out with it (in place: with what the mask bans)
-        if (!INPLACE || mask) {
-            const int g0 = (to.head + e0) / E, g1 = (int)(((int64_t)to.head + e0 + n + E - 1) / E);
-            const int shift = INPLACE ? 0 : (int)((held - stage) + ((int64_t)g0 * E - to.head - e0) * ES);   // stage byte of g0
-            const bool aligned = (shift & 15) == 0;
-            for (int g = g0 + tid; g < g1; g += kAdjThreads) {
-                const int i0 = to.first(g) - e0;                     // of the slice
-                const bool whole = i0 >= 0 && i0 <= n - E;
-                uint32_t allow = 0xffffffffu;
-                if (mask) {
-                    const int at = max(i0, 0);
-                    allow = __funnelshift_r(mask_words[at >> 5], mask_words[(at >> 5) + 1], at & 31);
-                    if (i0 < 0) allow <<= -i0;
-                }
-                if (INPLACE && (allow & ((1u << E) - 1u)) == (1u << E) - 1u) continue;
-                uint4 *const dst = reinterpret_cast<uint4 *>(const_cast<char *>(to.base) + (size_t)g * 16);
-                if (whole && (!INPLACE || (allow & ((1u << E) - 1u)) == 0u)) {
-                    uint4 v = make_uint4(0u, 0u, 0u, 0u);
-                    if constexpr (!INPLACE) v = load_anywhere<F32>(stage, shift + (g - g0) * 16, aligned);
-                    if (mask) {
-                        uint32_t *w = reinterpret_cast<uint32_t *>(&v);
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            if constexpr (F32) {
-                                if (!(allow >> k & 1u)) w[k] = kBanned;
-                            } else {
-                                if (!(allow >> (2 * k) & 1u)) w[k] = (w[k] & 0xffff0000u) | kBanned;
-                                if (!(allow >> (2 * k + 1) & 1u)) w[k] = (w[k] & 0xffffu) | kBanned << 16;
-                            }
-                        }
-                    }
-                    *dst = v;
-                } else {
-#pragma unroll
-                    for (int j = 0; j < E; ++j) {
-                        const int i = i0 + j;
-                        if ((unsigned)i >= (unsigned)n) continue;
-                        const bool ok = allow >> j & 1u;
-                        if (INPLACE && ok) continue;
-                        if constexpr (F32) reinterpret_cast<uint32_t *>(dst)[j] = ok ? reinterpret_cast<const uint32_t *>(held)[i] : kBanned;
-                        else reinterpret_cast<uint16_t *>(dst)[j] = ok ? reinterpret_cast<const uint16_t *>(held)[i] : (uint16_t)kBanned;
-                    }
+        // ---- the listed logits; element 0 of the slice lies at byte `first` of the stage (in place: of the row)
+        const int64_t out = row * p.ld_out + base;
+        const int first = (in.head + base - ga * E) * ES;   // (may lie before it, if the slice begins before the row)
+        if (n_listed > 0) {
+            const auto change = [&](int i, bool has_bias, float add) {
+                char *const at = INPLACE ? static_cast<char *>(p.out) + (out + i) * ES : stage + first + i * ES;
+                float v = load_elem<F32>(at, 0);
+                if constexpr (GRAD) v = scaled(v, load_elem<F32>(p.z, row * p.ld_z + base + i), rep);
+                else v = penalised(v, table.field(i), rep, freq, pres);
+                store_elem<F32>(at, 0, has_bias ? biased(v, add) : v);
+            };
+            for (int k = tid; k < n_listed; k += kAdjThreads) {
+                const int i = list[k];
+                if (GRAD || !(table.field(i) & 0x40000000u)) change(i, false, 0.f);
+            }
+            if constexpr (!GRAD) {
+                // of equal tokens' biases the last one counts; its thread changes the logit as a whole
+                for (int a = tid; a < n_bias; a += kAdjThreads) {
+                    const uint32_t mine = biases[a];
+                    bool last = true;
+                    for (int b = 0; b < n_bias; ++b) last = last && !(biases[b] > mine && (biases[b] ^ mine) < 65536u);
+                    if (last) change((int)(mine >> 16), true, p.bias_val[(int64_t)row * p.M + (mine & 0xffffu)]);
                 }
             }
+            __syncthreads();
         }
-        __syncthreads();
+
+        // ---- out with it (in place: with what the mask bans)
+        if (!INPLACE || mask) {
+            const int g0 = to.whole(gs) ? gs : gs + 1, g1 = to.whole(ge - 1) ? ge : ge - 1;
+            const int shift = first + (to.first(gs) - base) * ES;   // stage byte of vector gs
+            uint4 *dst = reinterpret_cast<uint4 *>(const_cast<char *>(to.base) + (size_t)(g0 + tid) * 16);
+            int held = shift + (g0 - gs + tid) * 16, f = to.first(g0 + tid);
+            for (int g = g0 + tid; g < g1; g += kAdjThreads, dst += kAdjThreads, held += kAdjThreads * 16, f += kAdjThreads * E) {
+                uint4 v = make_uint4(0u, 0u, 0u, 0u);
+                if constexpr (!INPLACE) v = load_anywhere<F32>(stage, held);
+                if (mask) {
+                    const uint32_t allow = staged_bits(mask_words, w0, f);
+                    if (INPLACE && (allow & kAll) != 0u) {
+                        if ((allow & kAll) != kAll) store_edge<F32, GRAD, true>(to, g, nullptr, allow);
+                        continue;
+                    }
+                    v = ban<F32, GRAD>(v, allow);
+                }
+                *dst = v;
+            }
+            if (tid == 0 && g0 > gs)
+                store_edge<F32, GRAD, INPLACE>(to, gs, stage + shift, mask ? staged_bits(mask_words, w0, to.first(gs)) : kAll);
+            if (tid == 32 && g1 < ge && ge - 1 >= g0)
+                store_edge<F32, GRAD, INPLACE>(to, ge - 1, stage + shift + (ge - 1 - gs) * 16,
+                                               mask ? staged_bits(mask_words, w0, to.first(ge - 1)) : kAll);
+        }
+        if (gridDim.x < units) __syncthreads();
     }
     if (bad && p.status) atomicOr(p.status, kStatusBadToken);
 }
@@ -366,28 +397,28 @@ bool bad_rows(const void *p, int64_t ld, int V, int bytes)
     return !p || reinterpret_cast<uintptr_t>(p) % bytes || ld < V;
 }
 
-size_t adjust_smem(const AdjustParams &p, bool grad, bool in_place, int es)
-{
-    const size_t S = (size_t)p.S;
-    size_t n = in_place ? 0 : S * es + 32;
-    if (p.hist) n += grad ? S / 8 : S * (p.wide ? 4 : 2);
-    if (p.mask) n += S / 8 + 8;
-    return n + (size_t)p.M * 8;
-}
-
 template <bool F32, bool GRAD, bool INPLACE>
 cudaError_t launch_adjust(AdjustParams p, cudaStream_t st)
 {
-    p.wide = p.L >= kNarrowHist;
-    // Slices as large as 16384 tokens where the rows fill the GPU twice over, so that few CTAs read a row's history.
     int sms = 0, dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
     if (e != cudaSuccess) return e;
-    p.S = 16384;
-    while (p.S > 2048 && (int64_t)p.B * (((int64_t)p.V + p.S - 1) / p.S) < 2 * sms) p.S /= 2;
-    p.slices = (int)(((int64_t)p.V + p.S - 1) / p.S);
-    const size_t smem = adjust_smem(p, GRAD, INPLACE, RowElem<F32>::kBytes);
+    p.wide = p.L >= kNarrowHist;
+    const int64_t ids = (int64_t)(p.hist ? p.L : 0) + p.M;
+    constexpr int E = RowElem<F32>::kPer;
+    const int64_t granules = ((int64_t)p.V + E - 1) / E + 1;   // (a row may begin inside one)
+    p.each = kMostEach;
+    while (p.each > 1 && (int64_t)p.B * ((granules + kAdjThreads * p.each - 1) / (kAdjThreads * p.each)) < 2 * sms) p.each /= 2;
+    size_t smem = 0;
+    for (;; p.each /= 2) {
+        const size_t S = (size_t)kAdjThreads * p.each * E;
+        p.listed = (int)((std::min<int64_t>(ids, S) + 3) / 4 * 4);
+        smem = INPLACE ? 0 : S * (16 / E) + 32;
+        if (ids > 0) smem += (GRAD ? S / 8 : S * (p.wide ? 4 : 2)) + (size_t)p.listed * 2 + (size_t)p.M * 4;
+        if (smem <= kMaxAdjSmem || p.each == 1) break;
+    }
+    p.slices = (int)((granules + kAdjThreads * p.each - 1) / (kAdjThreads * p.each));
     e = allow_smem<adjust_kernel<F32, GRAD, INPLACE>>(kMaxAdjSmem);
     if (e != cudaSuccess) return e;
     const int64_t units = (int64_t)p.B * p.slices;
@@ -399,7 +430,7 @@ cudaError_t launch_adjust(AdjustParams p, cudaStream_t st)
 sats_status check_adjust(const AdjustParams &p, int n_masks, int bytes)
 {
     if (p.B < 0 || p.V < 1 || p.L < 0 || p.M < 0 || n_masks < 0 || p.ld_z < p.V || p.ld_hist < 0) return SATS_EINVAL;
-    if (p.V > INT_MAX - 64 || p.B > INT_MAX / kRowMaxCluster || p.L > 1 << 30 || p.M > kMaxBiases) return SATS_ESHAPE;
+    if (p.V > INT_MAX - 64 || p.B > INT_MAX / kRowMaxCluster || p.L >= 1 << 30 || p.M > kMaxBiases) return SATS_ESHAPE;
     if (std::max({p.ld_z, p.ld_src, p.ld_out, p.ld_hist, p.ld_mask}) > (int64_t)1 << 40) return SATS_ESHAPE;
     if (p.B == 0) return SATS_OK;
     if (bad_rows(p.z, p.ld_z, p.V, bytes) || bad_rows(p.src, p.ld_src, p.V, bytes) || bad_rows(p.out, p.ld_out, p.V, bytes))
@@ -408,7 +439,8 @@ sats_status check_adjust(const AdjustParams &p, int n_masks, int bytes)
     if ((p.mask_row && !p.mask) || (p.M > 0 && (!p.bias_idx || !p.bias_val))) return SATS_EINVAL;
     if (!p.hist && p.L > 0) return SATS_EINVAL;
     if (bad_overlap(p.src, p.ld_src, p.out, p.ld_out, p.B, p.V, bytes)) return SATS_EINVAL;
-    if (p.z != p.src && bad_overlap(p.z, p.ld_z, p.out, p.ld_out, p.B, p.V, bytes)) return SATS_EINVAL;
+    // (the gradient's last step reads the logits after its first one has written)
+    if (p.z != p.src && (p.z == p.out || bad_overlap(p.z, p.ld_z, p.out, p.ld_out, p.B, p.V, bytes))) return SATS_EINVAL;
     return SATS_OK;
 }
 

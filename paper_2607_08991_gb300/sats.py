@@ -636,7 +636,7 @@ def adjust_logits_grad(logits: torch.Tensor, dout: torch.Tensor, dlogits: torch.
                        mask_row: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None,
                        stream: Optional[torch.cuda.Stream] = None):
     """The gradient of adjust_logits with respect to the logits it was given (sats_adjust_logits_grad); dlogits may be
-    dout or the logits."""
+    dout."""
     head, masks, B, f32, dev = _adjust_args(logits, hist, hist_len, mask, mask_row)
     g, ld_g = _same_rows(dout, "dout", logits)
     d, ld_d = _same_rows(dlogits, "dlogits", logits)

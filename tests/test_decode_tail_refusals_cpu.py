@@ -35,7 +35,7 @@ def test_adjust(sats):
         assert call(s, ld=63) == s.EINVAL and call(s, ld_out=63) == s.EINVAL and call(s, B=-1) == s.EINVAL
         assert call(s, V=0) == s.EINVAL and call(s, L=-1) == s.EINVAL and call(s, ld_hist=-1) == s.EINVAL
         assert call(s, hist=None) == s.EINVAL and call(s, hist=None, L=0, hist_len=0x3000, B=0) == s.OK
-        assert call(s, B=2**28) == s.ESHAPE and call(s, L=2**30 + 1) == s.ESHAPE
+        assert call(s, B=2**28) == s.ESHAPE and call(s, L=2**30) == s.ESHAPE
         assert call(s, V=2**31 - 64, ld=2**31, ld_out=2**31) == s.ESHAPE and call(s, ld=2**40 + 1) == s.ESHAPE
         # masks: too narrow, too few, rows without masks
         assert call(s, mask=0x4000, ld_mask=1, n_masks=2) == s.EINVAL
@@ -48,6 +48,7 @@ def test_adjust(sats):
     assert _adjust(s, M=1) == s.EINVAL and _adjust(s, M=-1) == s.EINVAL
     assert _adjust(s, M=1, bias=(0x5000, None)) == s.EINVAL and _adjust(s, M=1025, bias=(0x5000, 0x6000)) == s.ESHAPE
     assert _grad(s, dout=None) == s.EINVAL and _grad(s, ld_dout=63) == s.EINVAL and _grad(s, dout=0x300001) == s.EINVAL
+    assert _grad(s, out=0x100000) == s.EINVAL                # over the logits, which the last step reads
     assert _grad(s, out=0x300000 + 16) == s.EINVAL and _grad(s, out=0x300000, ld_out=65) == s.EINVAL
 
 

@@ -84,7 +84,10 @@ def close(got, want, z, a, dtype):
 
 
 SHAPES = [(1, 1, 1, 0, 0), (1, 31, 5, 3, 1), (3, 33, 40, 7, 2), (2, 300, 0, 20, 2), (5, 1000, 100, 0, 3), (1, 128256, 2000, 50, 1),
-          (7, 5003, 700, 300, 4), (40, 20011, 333, 30, 5), (2, 70001, 40000, 1024, 2), (150, 4099, 64, 5, 150)]
+          (7, 5003, 700, 300, 4), (40, 20011, 333, 30, 5), (2, 70001, 40000, 1024, 2), (150, 4099, 64, 5, 150),
+          # more rows than are slices at once
+          (310, 33, 20, 3, 4), (333, 1000, 300, 17, 9), (320, 4099, 0, 9, 320), (45, 130001, 700, 100, 6),
+          (64, 70001, 60000, 5, 2), (305, 515, 17000, 2, 1)]
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
@@ -114,7 +117,7 @@ def test_adjust(sats, B, V, L, M, masks, dtype, place):
 
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("B,V,L,M,masks", [s for s in SHAPES if s[2] > 0])
-@pytest.mark.parametrize("place", ["apart", "dout", "logits"])
+@pytest.mark.parametrize("place", ["apart", "dout", "between"])
 def test_grad(sats, B, V, L, M, masks, dtype, place):
     a = case(B, V, L, 5 * B + V + L, 0, masks)
     a = {k: a[k] for k in ("hist", "hist_len", "repetition", "mask", "mask_row") if k in a}
@@ -122,7 +125,11 @@ def test_grad(sats, B, V, L, M, masks, dtype, place):
     z[:, ::7] = 0.0
     if masks:
         d[-1, 0], d[-1, V // 2] = float("nan"), float("inf")     # where nothing is allowed
-    out = {"apart": rows(B, V, dtype, 3, pad=2), "dout": d, "logits": z}[place]
+    out = {"apart": rows(B, V, dtype, 3, pad=2), "dout": d, "between": None}[place]
+    if place == "between":
+        buf = torch.full((B, 2 * V + 9), 99.0, dtype=dtype, device="cuda")
+        buf[:, V + 4:2 * V + 4] = d
+        out, d = buf[:, :V], buf[:, V + 4:2 * V + 4]
     z64, d64 = z.double().cpu().numpy(), d.double().cpu().numpy()
     sats.adjust_logits_grad(z, d, out, **on_gpu(a))
     want = ref.grad(z64, d64, **a)
