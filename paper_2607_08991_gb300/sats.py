@@ -458,20 +458,23 @@ def route_calibrate(score: torch.Tensor, heldout_ids: torch.Tensor, r_tar: float
 # must be the current one.
 
 def _rows(t: torch.Tensor, name: str):
+    dtype = t.dtype
+    f32 = dtype is torch.float32
     dev = t.get_device()
     if dev < 0:
         raise ValueError("%s must be a CUDA tensor" % name)
-    if t.dtype not in (torch.float32, torch.bfloat16, torch.int16):
+    if not f32 and dtype is not torch.bfloat16 and dtype is not torch.int16:
         raise ValueError("%s must be fp32 or bf16 (or int16 bit patterns of bf16)" % name)
-    if t.dim() != 2 or t.shape[1] < 1 or (t.shape[1] > 1 and t.stride(1) != 1):
+    shape, strides = t.shape, t.stride()
+    if len(shape) != 2 or shape[1] < 1 or (strides[1] != 1 and shape[1] > 1):
         raise ValueError("%s must be [rows][V] with consecutive elements in a row" % name)
     if dev != torch._C._cuda_getDevice():
         raise ValueError("%s must be on the current CUDA device" % name)
-    R, V = t.shape
-    ld = t.stride(0) if R > 1 else V
+    R, V = shape
+    ld = strides[0] if R > 1 else V
     if ld < V:
         raise ValueError("%s must not have overlapping rows" % name)
-    return t.data_ptr(), ld, R, V, t.dtype is torch.float32, dev
+    return t.data_ptr(), ld, R, V, f32, dev
 
 
 def _beside(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, shape: tuple, dev: int) -> Optional[int]:
@@ -579,27 +582,36 @@ def _adjust_args(logits, hist, hist_len, mask, mask_row):
     z, ld, B, V, f32, dev = _rows(logits, "logits")
     h, ld_h, L = None, 0, 0
     if hist is not None:
-        if hist.get_device() != dev or hist.dtype is not torch.int32 or hist.dim() != 2 or hist.shape[0] != B:
+        shape, strides = hist.shape, hist.stride()
+        if hist.dtype is not torch.int32 or hist.get_device() != dev or len(shape) != 2 or shape[0] != B:
             raise ValueError("hist must be an int32 tensor [rows][ids] on the logits' device")
-        L = hist.shape[1]
-        if L > 1 and hist.stride(1) != 1:
+        L = shape[1]
+        if strides[1] != 1 and L > 1:
             raise ValueError("hist must have consecutive ids in a row")
-        h, ld_h = hist.data_ptr(), hist.stride(0) if B > 1 else 0
+        h, ld_h = hist.data_ptr(), strides[0] if B > 1 else 0
     m, ld_m, n = None, 0, 0
     if mask is not None:
-        if (mask.get_device() != dev or mask.dtype is not torch.int32 or mask.dim() != 2
-                or mask.shape[1] != (V + 31) // 32 or (mask.shape[1] > 1 and mask.stride(1) != 1)):
+        shape, strides = mask.shape, mask.stride()
+        if (mask.dtype is not torch.int32 or mask.get_device() != dev or len(shape) != 2 or shape[1] != (V + 31) // 32
+                or (strides[1] != 1 and shape[1] > 1)):
             raise ValueError("mask must be an int32 tensor [masks][ceil(V / 32)] on the logits' device")
-        m, n = mask.data_ptr(), mask.shape[0]
-        ld_m = mask.stride(0) if n > 1 else mask.shape[1]
-    return (z, ld, B, V, h, ld_h, L, _beside(hist_len, "hist_len", torch.int32, (B,), dev)), \
-        (m, ld_m, n, _beside(mask_row, "mask_row", torch.int32, (B,), dev)), B, f32, dev
+        m, n = mask.data_ptr(), shape[0]
+        ld_m = strides[0] if n > 1 else shape[1]
+    return (z, ld, B, V, h, ld_h, L, None if hist_len is None else _vector(hist_len, "hist_len", torch.int32, B, dev),
+            m, ld_m, n, None if mask_row is None else _vector(mask_row, "mask_row", torch.int32, B, dev), f32, dev)
 
 
-def _same_rows(t, name, logits):
-    p, ld, _, _, f32, dev = _rows(t, name)
-    if t.shape != logits.shape or f32 != (logits.dtype is torch.float32) or dev != logits.get_device():
-        raise ValueError("%s must have the logits' shape, type and device" % name)
+def _vector(t, name, dtype, n, dev):
+    """As _beside for n consecutive values, with fewer questions asked."""
+    if t.dtype is dtype and t.numel() == n and t.get_device() == dev and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError("%s must be a contiguous %s tensor of %d values on the logits' device" % (name, dtype, n))
+
+
+def _same_rows(t, name, V, B, f32):
+    p, ld, R, W, g32, _ = _rows(t, name)
+    if R != B or W != V or g32 is not f32:
+        raise ValueError("%s must have the logits' shape and type" % name)
     return p, ld
 
 
@@ -612,22 +624,30 @@ def adjust_logits(logits: torch.Tensor, out: torch.Tensor, hist: Optional[torch.
                   stream: Optional[torch.cuda.Stream] = None):
     """Penalties for the tokens of each row's history (int32 [B][L], rows may be expanded or overlap), biases and
     masks on rows of logits, before they are sampled (sats_adjust_logits); out may be the logits."""
-    head, masks, B, f32, dev = _adjust_args(logits, hist, hist_len, mask, mask_row)
-    if (bias_idx is None) != (bias_val is None):
-        raise ValueError("bias_idx and bias_val go together")
+    z, ld, B, V, h, ld_h, L, n, m, ld_m, n_m, m_row, f32, dev = _adjust_args(logits, hist, hist_len, mask, mask_row)
+    bi = bv = None
     M = 0
-    if bias_idx is not None:
+    if bias_idx is not None or bias_val is not None:
+        if bias_idx is None or bias_val is None:
+            raise ValueError("bias_idx and bias_val go together")
         if bias_idx.dim() != 2:
             raise ValueError("bias_idx must be [B][M]")
         M = bias_idx.shape[1]
-    o, ld_o = _same_rows(out, "out", logits)
-    vec = lambda t, name: _beside(t, name, torch.float32, (B,), dev)
-    fn = lib().sats_adjust_logits_f32 if f32 else lib().sats_adjust_logits
-    _check(fn(*head, _beside(n_prompt, "n_prompt", torch.int32, (B,), dev), vec(repetition, "repetition"),
-              vec(presence, "presence"), vec(frequency, "frequency"),
-              _beside(bias_idx, "bias_idx", torch.int32, (B, M), dev),
-              _beside(bias_val, "bias_val", torch.float32, (B, M), dev), M, *masks, o, ld_o,
-              _beside(dev_status, "dev_status", torch.int32, (1,), dev), _stream(stream)), "sats_adjust_logits")
+        bi = _beside(bias_idx, "bias_idx", torch.int32, (B, M), dev)
+        bv = _beside(bias_val, "bias_val", torch.float32, (B, M), dev)
+    o, ld_o = _same_rows(out, "out", V, B, f32)
+    float32 = torch.float32
+    L_ = _lib or lib()
+    s = (L_.sats_adjust_logits_f32 if f32 else L_.sats_adjust_logits)(
+        z, ld, B, V, h, ld_h, L, n,
+        None if n_prompt is None else _vector(n_prompt, "n_prompt", torch.int32, B, dev),
+        None if repetition is None else _vector(repetition, "repetition", float32, B, dev),
+        None if presence is None else _vector(presence, "presence", float32, B, dev),
+        None if frequency is None else _vector(frequency, "frequency", float32, B, dev),
+        bi, bv, M, m, ld_m, n_m, m_row, o, ld_o,
+        None if dev_status is None else _vector(dev_status, "dev_status", torch.int32, 1, dev), _stream(stream))
+    if s:
+        _check(s, "sats_adjust_logits")
 
 
 def adjust_logits_grad(logits: torch.Tensor, dout: torch.Tensor, dlogits: torch.Tensor,
@@ -637,12 +657,17 @@ def adjust_logits_grad(logits: torch.Tensor, dout: torch.Tensor, dlogits: torch.
                        stream: Optional[torch.cuda.Stream] = None):
     """The gradient of adjust_logits with respect to the logits it was given (sats_adjust_logits_grad); dlogits may be
     dout."""
-    head, masks, B, f32, dev = _adjust_args(logits, hist, hist_len, mask, mask_row)
-    g, ld_g = _same_rows(dout, "dout", logits)
-    d, ld_d = _same_rows(dlogits, "dlogits", logits)
-    fn = lib().sats_adjust_logits_grad_f32 if f32 else lib().sats_adjust_logits_grad
-    _check(fn(*head, _beside(repetition, "repetition", torch.float32, (B,), dev), *masks, g, ld_g, d, ld_d,
-              _beside(dev_status, "dev_status", torch.int32, (1,), dev), _stream(stream)), "sats_adjust_logits_grad")
+    z, ld, B, V, h, ld_h, L, n, m, ld_m, n_m, m_row, f32, dev = _adjust_args(logits, hist, hist_len, mask, mask_row)
+    g, ld_g = _same_rows(dout, "dout", V, B, f32)
+    d, ld_d = _same_rows(dlogits, "dlogits", V, B, f32)
+    L_ = _lib or lib()
+    s = (L_.sats_adjust_logits_grad_f32 if f32 else L_.sats_adjust_logits_grad)(
+        z, ld, B, V, h, ld_h, L, n,
+        None if repetition is None else _vector(repetition, "repetition", torch.float32, B, dev), m, ld_m, n_m, m_row,
+        g, ld_g, d, ld_d, None if dev_status is None else _vector(dev_status, "dev_status", torch.int32, 1, dev),
+        _stream(stream))
+    if s:
+        _check(s, "sats_adjust_logits_grad")
 
 
 # 4-bit weights with group scales: codes uint8 [K / 2][N] (two rows of W to a byte), scales bf16 [ceil(K / G)][N] (or int16
@@ -724,15 +749,20 @@ class Q4Workspace:
 def q4_matmul(w: Q4, x: torch.Tensor, y: torch.Tensor, ws: Q4Workspace, stream: Optional[torch.cuda.Stream] = None):
     """y = x W: x bf16 (or its int16 bit patterns) or fp32 [B][K], y fp32 or bf16 [B][N], whose rows may lie further
     apart than N (sats_q4_matmul)."""
-    if x.dim() != 2 or x.shape[1] != w.K or x.dtype not in (torch.float32, torch.bfloat16, torch.int16):
+    yp, ld, B, N, y_f32, dev = _rows(y, "y")
+    shape, dtype = x.shape, x.dtype
+    x_f32 = dtype is torch.float32
+    if len(shape) != 2 or shape[1] != w.K or not (x_f32 or dtype is torch.bfloat16 or dtype is torch.int16):
         raise ValueError("x must be bf16 or fp32 [B][K]")
-    B = x.shape[0]
-    yp, ld, By, N, y_f32, dev = _rows(y, "y")
-    if By != B or N != w.N or dev != w.device or x.get_device() != dev:
-        raise ValueError("y must be [B][N] on the weights' device")
-    fn = lib().sats_q4_matmul_f32 if x.dtype is torch.float32 else lib().sats_q4_matmul
-    _check(fn(w.handle, _ptr(x, "x"), B, yp, ld, 1 if y_f32 else 0, ws.buf.data_ptr(), ws.nbytes, _stream(stream)),
-           "sats_q4_matmul")
+    if shape[0] != B or N != w.N or dev != w.device or x.get_device() != dev:
+        raise ValueError("x must be [B][K] and y [B][N] on the weights' device")
+    if not x.is_contiguous():
+        raise ValueError("x must be contiguous")
+    L_ = _lib or lib()
+    s = (L_.sats_q4_matmul_f32 if x_f32 else L_.sats_q4_matmul)(
+        w.handle, x.data_ptr(), B, yp, ld, 1 if y_f32 else 0, ws.buf.data_ptr(), ws.nbytes, _stream(stream))
+    if s:
+        _check(s, "sats_q4_matmul")
 
 
 def selftest_wait_timeout(ws: Workspace, stream: Optional[torch.cuda.Stream] = None):
