@@ -42,6 +42,7 @@ constexpr int64_t kMaxQ4N = (int64_t)1 << 24;
 constexpr int kMaxCtas = 320;                 // of the product's kernel
 constexpr int kLoShift = 11;                  // the second part of an fp32 activation is kept 2^11 times larger
 constexpr int kMaxSplitTiles = 10 * kMaxCtas; // more tiles are not split (launch_q4)
+constexpr int kDirectTokens = 16;             // columns (fp32 activations: two a token) that a CTA may stage itself
 constexpr int kCtlBytes = 256;
 
 __host__ __device__ constexpr int block_bytes(int G) { return kCodeBytes + kStageK / G * kRows * 2; }
@@ -271,6 +272,25 @@ __global__ void __launch_bounds__(128) q4_pack_kernel(const uint8_t *codes, cons
 }
 
 // ------------------------------------------------------------------ activations
+// 8 values times f1 f2 as fp16 pairs, first and (fp32) second parts.
+template <bool F32>
+__device__ __forceinline__ void split8(const float (&x)[8], float f1, float f2, uint32_t (&hi)[4], uint32_t (&lo)[4])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        __half h[2], l[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const float v = x[2 * i + j] * f1 * f2;
+            h[j] = __float2half_rn(v);
+            const float rest = (v - __half2float(h[j])) * (float)(1 << kLoShift);
+            l[j] = __float2half_rn(isfinite(rest) ? rest : 0.f);
+        }
+        hi[i] = (uint32_t)__half_as_ushort(h[0]) | (uint32_t)__half_as_ushort(h[1]) << 16;
+        lo[i] = F32 ? (uint32_t)__half_as_ushort(l[0]) | (uint32_t)__half_as_ushort(l[1]) << 16 : 0u;
+    }
+}
+
 // Tokens in tiles; for a tile and a stage of 128 k two halves of 64 k, each TN rows of 128 bytes in the order that the
 // 128-byte swizzle of the MMA's operand has.  With fp32 activations the first TN / 2 rows are the tokens' first parts,
 // the others their second ones.
@@ -311,21 +331,11 @@ __global__ void __launch_bounds__(kStageThreads) q4_stage_kernel(const StagePara
     char *const base = p.xs + (int64_t)tile * p.KS * p.TN * 256;
     // 8 consecutive k are 16 bytes of a row
     for (int c = blockIdx.y * kStageThreads + tid; c < p.KS * 16; c += gridDim.y * kStageThreads) {
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = 8 * c + i < p.K ? __uint_as_float(bits(8 * c + i)) : 0.f;
         uint32_t hi[4], lo[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            __half h[2], l[2];
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const int k = 8 * c + 2 * i + j;
-                const float v = k < p.K ? __uint_as_float(bits(k)) * f1 * f2 : 0.f;
-                h[j] = __float2half_rn(v);
-                const float rest = (v - __half2float(h[j])) * (float)(1 << kLoShift);
-                l[j] = __float2half_rn(isfinite(rest) ? rest : 0.f);
-            }
-            hi[i] = (uint32_t)__half_as_ushort(h[0]) | (uint32_t)__half_as_ushort(h[1]) << 16;
-            lo[i] = (uint32_t)__half_as_ushort(l[0]) | (uint32_t)__half_as_ushort(l[1]) << 16;
-        }
+        split8<F32>(v, f1, f2, hi, lo);
         const int ks = c >> 4, half = c >> 3 & 1, piece = c & 7;
         auto put = [&](int r, const uint32_t (&v)[4]) {
             char *const at = base + ((int64_t)ks * 2 + half) * p.TN * 128 + r * 128 + ((piece ^ (r & 7)) << 4);
@@ -350,6 +360,9 @@ struct Q4Params {
     bool whole;                   // a unit is a tile, else a stage of 128 k
     bool y_f32;
     int stages;                   // of the shared-memory ring
+    const void *x;                // the kernels that stage it themselves
+    int K;
+    int slots;                    // .. stages of x that a CTA has, at most
     float *partial;               // [2 kMaxCtas][R][128]
     int *counters;                // [tiles], 0 between calls
     int *ctl;
@@ -458,6 +471,7 @@ struct Q4Bars {
     uint64_t full[kQ4MaxStages], empty[kQ4MaxStages];
     uint64_t a_full[4], a_empty[4];
     uint64_t d_full[2], d_empty[2];
+    uint64_t x_full;
     uint64_t drain;
 };
 
@@ -489,7 +503,18 @@ __device__ __forceinline__ void add_columns(uint32_t taddr, float (&acc)[n])
 // R: tokens of a tile that are there (columns of the accumulator that are used); TN >= 16: the MMA's N, whose rows past
 // R read whatever lies behind them in shared memory and land in columns that nobody reads.  NA: stages of fp16 weights in
 // TMEM; EG: warpgroups that add the sums up; PER_SM: resident CTAs.
-template <int R, int NA, int EG, int PER_SM, bool F32>
+// v 2^e for a sum v of scaled products (1e-30 < |v| < 1e30, or 0) and any e that two scales' exponents add up to: rounded once
+// where the result is subnormal (below e = -252 it is 0).
+__device__ __forceinline__ float times_pow2(float v, int e)
+{
+    e = max(e, -252);
+    const int half = e >> 1;
+    return v * __int_as_float((half + 127) << 23) * __int_as_float((e - half + 127) << 23);
+}
+
+// DIRECT (a few tokens): the CTA brings the activations of its stages to shared memory itself, at its start, with a power of
+// two of its own for each token; no second kernel, and the ring holds weights alone.
+template <int R, int NA, int EG, int PER_SM, bool F32, bool DIRECT>
 __global__ void __launch_bounds__(q4_threads<R, EG>(), PER_SM) q4_matmul_kernel(const __grid_constant__ Q4Params p)
 {
     constexpr int TN = R < 16 ? 16 : R;
@@ -503,11 +528,13 @@ __global__ void __launch_bounds__(q4_threads<R, EG>(), PER_SM) q4_matmul_kernel(
     __shared__ uint32_t tmem_slot;
     __shared__ volatile int abort_flag;
     __shared__ int last_flag[EG];
+    __shared__ uint32_t tops[DIRECT ? R : 1];
 
     const int warp = uniform_warp(), lane = threadIdx.x & 31;
     char *const ring = smem_raw + (-smem_addr(smem_raw) & 1023u);   // (not through an integer: loads stay shared-memory loads)
     const int blk = block_bytes(p.G);
-    char *const wring = ring + (size_t)p.stages * kX;
+    char *const wring = ring + (size_t)(DIRECT ? p.slots : p.stages) * kX;
+    constexpr int kLoaded = DIRECT ? 0 : kX;   // of x, with each stage of the ring
     const int u0 = first_unit(p, blockIdx.x), u1 = first_unit(p, blockIdx.x + 1);
     const int n_it = p.whole ? (u1 - u0) * p.KS : u1 - u0;
     const int tile0 = p.whole ? u0 : u0 / p.KS, ks0 = p.whole ? 0 : u0 - tile0 * p.KS;
@@ -525,16 +552,107 @@ __global__ void __launch_bounds__(q4_threads<R, EG>(), PER_SM) q4_matmul_kernel(
             mbar_init(&bars.d_full[i], 1);
             mbar_init(&bars.d_empty[i], 4 * EG);
         }
+        mbar_init(&bars.x_full, kDeq + 8);
         mbar_init(&bars.drain, 1);
         abort_flag = 0;
         mbar_init_fence();
     }
+    if (DIRECT && threadIdx.x < R) tops[threadIdx.x] = 0u;
     if (warp == kMma) tmem_alloc(&tmem_slot, kCols);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = tmem_slot;
+    // the next kernel, if it asks to, may come to the SMs that this one leaves free
+    if constexpr (DIRECT) grid_launch_dependents();
 
+    if (DIRECT && warp < kLoad) {
+        // ---- the activations: 8 consecutive k of a token are 16 bytes of a row
+        constexpr int kThreads = 32 * (kDeq + 8);
+        grid_dependency_wait();
+        const int n_slots = min(n_it, p.KS), groups = n_slots * 16, first = n_it < p.KS ? ks0 : 0;
+        const bool fours = (reinterpret_cast<uintptr_t>(p.x) & 15u) == 0;
+        const auto values = [&](int piece, bool there, float (&v)[8]) {
+            const int b = piece / groups, g = piece - b * groups;
+            int ks = first + (g >> 4);
+            if (ks >= p.KS) ks -= p.KS;
+            const int k = ks * kStageK + (g & 15) * 8;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = 0.f;
+            if (!there || k >= p.K) return;
+            if constexpr (F32) {
+                const float *const x = static_cast<const float *>(p.x) + (int64_t)b * p.K + k;
+                if (fours) {
+                    const float4 q = *reinterpret_cast<const float4 *>(x), r = *reinterpret_cast<const float4 *>(x + 4);
+                    v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w; v[4] = r.x; v[5] = r.y; v[6] = r.z; v[7] = r.w;
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] = x[i];
+                }
+            } else {
+                const uint16_t *const x = static_cast<const uint16_t *>(p.x) + (int64_t)b * p.K + k;
+                if (fours) unpack8(*reinterpret_cast<const uint4 *>(x), v);
+                else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float((uint32_t)x[i] << 16);
+                }
+            }
+        };
+        // all tokens' pieces at once; the first kHeld of a thread stay in registers between the two steps
+        constexpr int kHeld = 2;
+        float kept[kHeld][8];
+        const int total = p.B * groups;
+        const auto largest = [&](int i, const float (&v)[8]) {   // (a multiple of 16 pieces to a token: half a warp has one token)
+            uint32_t top = 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint32_t m = __float_as_uint(v[j]) & 0x7fffffffu;
+                if (m < 0x7f800000u) top = max(top, m);
+            }
+#pragma unroll
+            for (int o = 8; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+            if ((lane & 15) == 0 && i < total) atomicMax(&tops[i / groups], top);
+        };
+        const auto put = [&](int i, const float (&v)[8]) {
+            const int b = i / groups, g = i - b * groups;
+            const int e = tops[b] ? ilogbf(__uint_as_float(tops[b])) - 14 : 0;
+            const float f1 = scalbnf(1.f, -e / 2), f2 = scalbnf(1.f, -e - -e / 2);   // 2^-e alone can be out of range
+            uint32_t hi[4], lo[4];
+            split8<F32>(v, f1, f2, hi, lo);
+            char *const half = ring + (size_t)(g >> 3) * (R * 128);
+            const int piece = g & 7;
+            *reinterpret_cast<uint4 *>(half + b * 128 + ((piece ^ (b & 7)) << 4)) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+            if constexpr (F32) {
+                const int r = R / 2 + b;
+                *reinterpret_cast<uint4 *>(half + r * 128 + ((piece ^ (r & 7)) << 4)) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+            }
+        };
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k) {
+            const int i = threadIdx.x + k * kThreads;
+            values(i, i < total, kept[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k) largest(threadIdx.x + k * kThreads, kept[k]);
+        for (int i0 = kHeld * kThreads; i0 < total; i0 += kThreads) {
+            const int i = i0 + threadIdx.x;
+            float v[8];
+            values(i, i < total, v);
+            largest(i, v);
+        }
+        named_barrier(3, kThreads);
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k)
+            if (threadIdx.x + k * kThreads < total) put(threadIdx.x + k * kThreads, kept[k]);
+        for (int i = threadIdx.x + kHeld * kThreads; i < total; i += kThreads) {
+            float v[8];
+            values(i, true, v);
+            put(i, v);
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the MMAs read what has been written here
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bars.x_full);
+    }
     if (warp == kLoad) {
         // ---- loads
         const uint32_t lead = elect_one();
@@ -551,11 +669,11 @@ __global__ void __launch_bounds__(q4_threads<R, EG>(), PER_SM) q4_matmul_kernel(
             }
         };
         for (int it = 0; it < ahead; ++it) {
-            mbar_expect_if(lead, &bars.full[it], (uint32_t)(blk + kX));
+            mbar_expect_if(lead, &bars.full[it], (uint32_t)(blk + kLoaded));
             bulk_load_shared_if(lead, wring + (size_t)it * blk, w, (uint32_t)blk, &bars.full[it]);
             step_w(ks, tt);
         }
-        grid_dependency_wait();
+        if constexpr (!DIRECT) grid_dependency_wait();
         int xks = ks0, xtt = tile0 % p.TT;
         const char *x = p.xs + ((int64_t)xtt * p.KS + xks) * kX;
         auto step_x = [&] {
@@ -568,10 +686,11 @@ __global__ void __launch_bounds__(q4_threads<R, EG>(), PER_SM) q4_matmul_kernel(
                 }
             }
         };
-        for (int it = 0; it < ahead; ++it) {
-            bulk_load_shared_if(lead, ring + (size_t)it * kX, x, (uint32_t)kX, &bars.full[it]);
-            step_x();
-        }
+        if constexpr (!DIRECT)
+            for (int it = 0; it < ahead; ++it) {
+                bulk_load_shared_if(lead, ring + (size_t)it * kX, x, (uint32_t)kX, &bars.full[it]);
+                step_x();
+            }
         Slot s;   // parity: of the use before
         s.i = ahead == p.stages ? 0 : ahead;
         int issued = ahead;
@@ -580,11 +699,13 @@ __global__ void __launch_bounds__(q4_threads<R, EG>(), PER_SM) q4_matmul_kernel(
                 if (lane == 0) set_timeout(p.ctl, &abort_flag);
                 break;
             }
-            mbar_expect_if(lead, &bars.full[s.i], (uint32_t)(blk + kX));
+            mbar_expect_if(lead, &bars.full[s.i], (uint32_t)(blk + kLoaded));
             bulk_load_shared_if(lead, wring + (size_t)s.i * blk, w, (uint32_t)blk, &bars.full[s.i]);
-            bulk_load_shared_if(lead, ring + (size_t)s.i * kX, x, (uint32_t)kX, &bars.full[s.i]);
+            if constexpr (!DIRECT) {
+                bulk_load_shared_if(lead, ring + (size_t)s.i * kX, x, (uint32_t)kX, &bars.full[s.i]);
+                step_x();
+            }
             step_w(ks, tt);
-            step_x();
             s.next(p.stages);
             issued = it + 1;
         }
@@ -598,10 +719,13 @@ __global__ void __launch_bounds__(q4_threads<R, EG>(), PER_SM) q4_matmul_kernel(
         bool ok = true;
         Slot s, a, d;
         const uint64_t desc0 = smem_desc(smem_addr(ring));
+        int slot = n_it < p.KS ? 0 : ks0;   // (DIRECT) of x
+        if constexpr (DIRECT) ok = role_wait(&bars.x_full, 0u, &abort_flag);
         for (int it = 0; it < n_it; ++it) {
-            ok = role_wait(&bars.full[s.i], s.parity, &abort_flag);
+            if (ok) ok = role_wait(&bars.full[s.i], s.parity, &abort_flag);
             if (ok && it >= 2) ok = role_wait(&bars.d_empty[d.i], d.parity ^ 1u, &abort_flag);
-            const uint64_t desc = desc0 + (uint64_t)(s.i * (kX >> 4));
+            const uint64_t desc = desc0 + (uint64_t)((DIRECT ? slot : s.i) * (kX >> 4));
+            if (DIRECT && ++slot == p.KS) slot = 0;
             if (ok) ok = role_wait(&bars.a_full[a.i], a.parity, &abort_flag);
             if (!ok) break;
             tc_fence_after();
@@ -679,6 +803,11 @@ __global__ void __launch_bounds__(q4_threads<R, EG>(), PER_SM) q4_matmul_kernel(
         constexpr int kPieces = F32 && EG > 1 ? 2 : 1, P = C / kPieces;
         const int e = warp >> 2, quad = warp & 3, r = quad * 32 + lane;
         const uint32_t src = tmem + ((uint32_t)(quad * 32) << 16) + e * P;
+        // The power of two that token i's activations were divided by (in this CTA).
+        const auto token_exp = [&](int token0, int i) {
+            if constexpr (!DIRECT) return p.tok_exp[token0 + i];
+            else return tops[i] ? ilogbf(__uint_as_float(tops[i])) - 14 : 0;
+        };
         float acc[kPieces][P];
 #pragma unroll
         for (int j = 0; j < kPieces; ++j)
@@ -711,6 +840,12 @@ __global__ void __launch_bounds__(q4_threads<R, EG>(), PER_SM) q4_matmul_kernel(
             const int tt = tile % p.TT, token0 = tt * p.per_tile + e * kOut;
             const int n = (tile / p.TT) * kRows + r;
             const int tokens = min(p.per_tile - e * kOut, p.B - token0);   // (of the next ones, if more than kOut)
+            {
+                const int ce = n < p.N ? p.col_exp[n] : 0;
+#pragma unroll
+                for (int i = 0; i < kOut; ++i)
+                    if (i < tokens) sum[i] = times_pow2(sum[i], ce + token_exp(token0, i));
+            }
             bool write = true;
             auto group_barrier = [](int group) {   // (literal numbers: else a CTA reserves all barriers)
                 if (EG == 1 || group == 0) named_barrier(1, 128);
@@ -719,10 +854,10 @@ __global__ void __launch_bounds__(q4_threads<R, EG>(), PER_SM) q4_matmul_kernel(
             if (!p.whole && (u0 > tile * p.KS || !tile_end)) {
                 // the CTAs of the tile leave their sums in the workspace; the last one to come adds them in order
                 const int t0 = tile * p.KS, c0 = unit_cta(p, t0), c1 = unit_cta(p, t0 + p.KS - 1);
-                auto slot = [&](int c, int begin) {   // a CTA's second slot is for the tile that it begins
-                    return p.partial + ((size_t)(2 * c + (begin < t0 ? 1 : 0)) * R + e * kOut) * kRows + r;
+                auto slot = [&](int c) {   // a CTA's second slot is for the tile that it begins
+                    return p.partial + ((size_t)(2 * c + (first_unit(p, c) < t0 ? 1 : 0)) * R + e * kOut) * kRows + r;
                 };
-                float *const mine = slot(blockIdx.x, u0);
+                float *const mine = slot(blockIdx.x);
 #pragma unroll
                 for (int i = 0; i < kOut; ++i)
                     if (i < tokens) __stcg(mine + i * kRows, sum[i]);
@@ -737,25 +872,37 @@ __global__ void __launch_bounds__(q4_threads<R, EG>(), PER_SM) q4_matmul_kernel(
                 write = last_flag[e] != 0;
                 if (write) {
                     __threadfence();
+                    // a few tokens at a time, of which a few CTAs' sums are on their way
+                    constexpr int kTok = kOut < 8 ? kOut : 8, kAtOnce = 4;
 #pragma unroll
-                    for (int i = 0; i < kOut; ++i) sum[i] = 0.f;
-                    for (int c = c0; c <= c1; ++c) {
-                        const float *const part = slot(c, first_unit(p, c));
+                    for (int i0 = 0; i0 < kOut; i0 += kTok) {
+                        if (i0 >= tokens) break;
 #pragma unroll
-                        for (int i = 0; i < kOut; ++i)
-                            if (i < tokens) sum[i] += __ldcg(part + i * kRows);
+                        for (int i = 0; i < kTok; ++i) sum[i0 + i] = 0.f;
+                        for (int c = c0; c <= c1; c += kAtOnce) {
+                            float part[kAtOnce][kTok];
+#pragma unroll
+                            for (int j = 0; j < kAtOnce; ++j) {
+                                const float *const from = slot(min(c + j, c1));
+#pragma unroll
+                                for (int i = 0; i < kTok; ++i)
+                                    part[j][i] = i0 + i < tokens && c + j <= c1 ? __ldcg(from + (i0 + i) * kRows) : 0.f;
+                            }
+#pragma unroll
+                            for (int j = 0; j < kAtOnce; ++j)
+#pragma unroll
+                                for (int i = 0; i < kTok; ++i) sum[i0 + i] += part[j][i];
+                        }
                     }
                 }
             }
             if (write && n < p.N) {
-                const int ce = p.col_exp[n];
 #pragma unroll
                 for (int i = 0; i < kOut; ++i) {
                     if (i < tokens) {
                         const int64_t at = (int64_t)(token0 + i) * p.ld_y + n;
-                        const float v = scalbnf(sum[i], ce + p.tok_exp[token0 + i]);
-                        if (p.y_f32) static_cast<float *>(p.y)[at] = v;
-                        else static_cast<__nv_bfloat16 *>(p.y)[at] = __float2bfloat16_rn(v);
+                        if (p.y_f32) static_cast<float *>(p.y)[at] = sum[i];
+                        else static_cast<__nv_bfloat16 *>(p.y)[at] = __float2bfloat16_rn(sum[i]);
                     }
                 }
             }
@@ -816,26 +963,36 @@ bool q4_shape_ok(int64_t K, int64_t N, int G)
     return K >= 8 && K <= kMaxK && K % 8 == 0 && N >= 1 && N <= kMaxQ4N && (G == 32 || G == 64 || G == 128);
 }
 
-template <int R, int NA, int EG, int PER_SM, bool F32>
-cudaError_t launch_q4(Q4Params p, cudaStream_t st)
+constexpr int kSmemPair = 110 * 1024, kSmemOne = 222 * 1024;   // of a CTA, two or one to an SM
+constexpr int kDirectRing = 4;   // stages of weights that have to fit beside the activations
+
+// How the stages go to the CTAs.
+void plan_q4(Q4Params &p, int per_sm, int *grid)
 {
-    static std::atomic<int> configured[64];
-    const int stage = block_bytes(p.G) + R * 256;
-    const int budget = PER_SM == 2 ? 110 * 1024 : 222 * 1024;
-    p.stages = std::min(kQ4MaxStages, (budget - 1024) / stage);
-    const size_t smem = (size_t)p.stages * stage + 1024;
-    cudaError_t e = set_smem(q4_matmul_kernel<R, NA, EG, PER_SM, F32>, smem, configured);
-    if (e != cudaSuccess) return e;
     const int tiles = div_up(p.N, kRows) * p.TT;
-    const int most = std::min(kMaxCtas, PER_SM * sm_count());
+    const int most = std::min(kMaxCtas, per_sm * sm_count());
     // Whole tiles where they fill the CTAs evenly, else any number of stages each.
     const int64_t waves = (tiles + most - 1) / most;
     p.whole = (int64_t)tiles * 10 >= waves * most * 9;
     const int units = p.whole ? tiles : tiles * p.KS;
-    const int grid = std::min(most, units);
-    p.per = units / grid;
-    p.rem = units % grid;
-    return launch_pdl_cfg(q4_matmul_kernel<R, NA, EG, PER_SM, F32>, dim3(grid), q4_threads<R, EG>(), smem, st, p);
+    *grid = std::min(most, units);
+    p.per = units / *grid;
+    p.rem = units % *grid;
+    p.slots = std::min<int64_t>(p.KS, (int64_t)(p.per + (p.rem > 0 ? 1 : 0)) * (p.whole ? p.KS : 1));
+}
+
+template <int R, int NA, int EG, int PER_SM, bool F32, bool DIRECT>
+cudaError_t launch_q4(const Q4Params &planned, int grid, cudaStream_t st)
+{
+    static std::atomic<int> configured[64];
+    Q4Params p = planned;
+    const int stage = block_bytes(p.G) + (DIRECT ? 0 : R * 256);
+    const int kept = 1024 + (DIRECT ? p.slots * R * 256 : 0);
+    p.stages = std::min(kQ4MaxStages, ((PER_SM == 2 ? kSmemPair : kSmemOne) - kept) / stage);
+    const size_t smem = (size_t)p.stages * stage + kept;
+    const cudaError_t e = set_smem(q4_matmul_kernel<R, NA, EG, PER_SM, F32, DIRECT>, smem, configured);
+    if (e != cudaSuccess) return e;
+    return launch_pdl_cfg(q4_matmul_kernel<R, NA, EG, PER_SM, F32, DIRECT>, dim3(grid), q4_threads<R, EG>(), smem, st, p);
 }
 
 template <bool F32>
@@ -854,6 +1011,13 @@ cudaError_t run_q4(const sats_q4 *w, const void *x, int B, void *y, int64_t ld_y
     p.counters = reinterpret_cast<int *>(ws + L.counters);
     p.ctl = reinterpret_cast<int *>(ws);
 
+    p.x = x;
+    p.K = w->K;
+    int grid = 0;
+    plan_q4(p, TN <= 32 ? 2 : 1, &grid);
+    if (TN <= kDirectTokens && 1024 + p.slots * TN * 256 + kDirectRing * block_bytes(p.G) <= kSmemPair)
+        return TN == 8 ? launch_q4<8, 3, 1, 2, F32, true>(p, grid, st) : launch_q4<16, 3, 1, 2, F32, true>(p, grid, st);
+
     StageParams sp{x, ws + L.xs, reinterpret_cast<int *>(ws + L.tok_exp), B, w->K, p.KS, TN, p.per_tile};
     // a token's pieces go to several CTAs where there are few tokens
     const int split = B >= 128 ? 1 : std::max(1, std::min(div_up(p.KS * 16, kStageThreads), 128 / B));
@@ -861,11 +1025,11 @@ cudaError_t run_q4(const sats_q4 *w, const void *x, int B, void *y, int64_t ld_y
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     switch (TN) {
-    case 8: return launch_q4<8, 3, 1, 2, F32>(p, st);
-    case 16: return launch_q4<16, 3, 1, 2, F32>(p, st);
-    case 32: return launch_q4<32, 3, 1, 2, F32>(p, st);
-    case 64: return launch_q4<64, 4, 1, 1, F32>(p, st);
-    default: return launch_q4<128, 4, 2, 1, F32>(p, st);
+    case 8: return launch_q4<8, 3, 1, 2, F32, false>(p, grid, st);
+    case 16: return launch_q4<16, 3, 1, 2, F32, false>(p, grid, st);
+    case 32: return launch_q4<32, 3, 1, 2, F32, false>(p, grid, st);
+    case 64: return launch_q4<64, 4, 1, 1, F32, false>(p, grid, st);
+    default: return launch_q4<128, 4, 2, 1, F32, false>(p, grid, st);
     }
 }
 
