@@ -41,7 +41,7 @@ constexpr int kMaxK = 65536;
 constexpr int64_t kMaxQ4N = (int64_t)1 << 24;
 constexpr int kMaxCtas = 320;                 // of the product's kernel
 constexpr int kLoShift = 11;                  // the second part of an fp32 activation is kept 2^11 times larger
-constexpr int kMaxSplitTiles = 10 * kMaxCtas; // more tiles are not split (launch_q4)
+constexpr int kMaxSplitTiles = 64 * kMaxCtas; // more tiles are not split (plan_q4)
 constexpr int kDirectTokens = 16;             // columns (fp32 activations: two a token) that a CTA may stage itself
 constexpr int kCtlBytes = 256;
 
@@ -467,16 +467,53 @@ __device__ __forceinline__ bool role_wait(uint64_t *bar, uint32_t parity, volati
     return true;
 }
 
+// A row's 128 codes of a block with their scales, and their way to TMEM.
+struct Codes {
+    uint4 q[4];
+    __half sc[4];
+
+    __device__ __forceinline__ void load(const char *block, int per, int r)   // per: groups of a block
+    {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            q[j] = reinterpret_cast<const uint4 *>(block)[j * kRows + r];
+            sc[j] = reinterpret_cast<const __half *>(block + kCodeBytes)[((j * per) >> 2) * kRows + r];
+        }
+    }
+    __device__ __forceinline__ void store(uint32_t taddr) const
+    {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            uint32_t v[32];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const Scale t(sc[2 * h + j]);
+                const uint4 c = q[2 * h + j];
+                dequant8(c.x, t, v + 16 * j);
+                dequant8(c.y, t, v + 16 * j + 4);
+                dequant8(c.z, t, v + 16 * j + 8);
+                dequant8(c.w, t, v + 16 * j + 12);
+            }
+            tmem_st32(taddr + h * 32, v);
+        }
+    }
+};
+
 struct Q4Bars {
     uint64_t full[kQ4MaxStages], empty[kQ4MaxStages];
     uint64_t a_full[4], a_empty[4];
-    uint64_t d_full[2], d_empty[2];
+    uint64_t d_full[4], d_empty[4];   // (with as many accumulators as stages of weights, d_full says that these are free, too)
+    uint64_t group[2];
     uint64_t x_full;
     uint64_t drain;
 };
 
+// Warpgroups that turn weights to fp16.
+template <int R>
+__host__ __device__ constexpr int q4_groups() { return 2; }
+
 template <int R, int EG>
-constexpr int q4_threads() { return 32 * (10 + 4 * EG); }
+constexpr int q4_threads() { return 32 * (2 + 4 * q4_groups<R>() + 4 * EG); }
 
 // Columns [c, c + n) of this warp's lanes added to acc; n 8, 16 or a multiple of 16.
 template <int n>
@@ -501,8 +538,8 @@ __device__ __forceinline__ void add_columns(uint32_t taddr, float (&acc)[n])
 }
 
 // R: tokens of a tile that are there (columns of the accumulator that are used); TN >= 16: the MMA's N, whose rows past
-// R read whatever lies behind them in shared memory and land in columns that nobody reads.  NA: stages of fp16 weights in
-// TMEM; EG: warpgroups that add the sums up; PER_SM: resident CTAs.
+// R read whatever lies behind them in shared memory and land in columns that nobody reads.  NA, ND: stages of fp16 weights
+// and accumulators in TMEM; EG: warpgroups that add the sums up; PER_SM: resident CTAs.
 // v 2^e for a sum v of scaled products (1e-30 < |v| < 1e30, or 0) and any e that two scales' exponents add up to: rounded once
 // where the result is subnormal (below e = -252 it is 0).
 __device__ __forceinline__ float times_pow2(float v, int e)
@@ -514,15 +551,16 @@ __device__ __forceinline__ float times_pow2(float v, int e)
 
 // DIRECT (a few tokens): the CTA brings the activations of its stages to shared memory itself, at its start, with a power of
 // two of its own for each token; no second kernel, and the ring holds weights alone.
-template <int R, int NA, int EG, int PER_SM, bool F32, bool DIRECT>
+template <int R, int NA, int ND, int EG, int PER_SM, bool F32, bool DIRECT>
 __global__ void __launch_bounds__(q4_threads<R, EG>(), PER_SM) q4_matmul_kernel(const __grid_constant__ Q4Params p)
 {
     constexpr int TN = R < 16 ? 16 : R;
-    constexpr int kCols = (2 * TN + NA * 64) <= 256 ? 256 : 512;   // TMEM: two accumulators, then the weights
+    constexpr int kCols = (ND * TN + NA * 64) <= 256 ? 256 : 512;   // TMEM: accumulators, then the weights
     constexpr int kX = R * 256;                                    // bytes of the activations of a stage
     constexpr uint32_t kIdesc = (1u << 4) | ((uint32_t)(TN >> 3) << 17) | ((uint32_t)(kRows >> 4) << 24);
-    constexpr int kDeq = 4 * EG, kLoad = kDeq + 8, kMma = kDeq + 9;   // first warps of the roles
-    static_assert(2 * TN + NA * 64 <= 512 && NA <= 4, "TMEM");
+    constexpr int kGroups = q4_groups<R>();
+    constexpr int kDeq = 4 * EG, kLoad = kDeq + 4 * kGroups, kMma = kLoad + 1;   // first warps of the roles
+    static_assert(ND * TN + NA * 64 <= kCols && kCols * PER_SM <= 512 && NA <= 4 && ND <= 4, "TMEM");
     extern __shared__ char smem_raw[];
     __shared__ Q4Bars bars;
     __shared__ uint32_t tmem_slot;
@@ -542,17 +580,19 @@ __global__ void __launch_bounds__(q4_threads<R, EG>(), PER_SM) q4_matmul_kernel(
     if (threadIdx.x == 0) {
         for (int i = 0; i < kQ4MaxStages; ++i) {
             mbar_init(&bars.full[i], 1);
-            mbar_init(&bars.empty[i], 5);   // four warps that have read the codes, the MMAs that have read the activations
+            mbar_init(&bars.empty[i], DIRECT ? 4 : 5);   // four warps that have read the codes, the MMAs that have read the activations
         }
         for (int i = 0; i < 4; ++i) {
             mbar_init(&bars.a_full[i], 4);
             mbar_init(&bars.a_empty[i], 1);
         }
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < 4; ++i) {
             mbar_init(&bars.d_full[i], 1);
             mbar_init(&bars.d_empty[i], 4 * EG);
         }
-        mbar_init(&bars.x_full, kDeq + 8);
+        mbar_init(&bars.group[0], 4);
+        mbar_init(&bars.group[1], 4);
+        mbar_init(&bars.x_full, kLoad);
         mbar_init(&bars.drain, 1);
         abort_flag = 0;
         mbar_init_fence();
@@ -568,7 +608,7 @@ __global__ void __launch_bounds__(q4_threads<R, EG>(), PER_SM) q4_matmul_kernel(
 
     if (DIRECT && warp < kLoad) {
         // ---- the activations: 8 consecutive k of a token are 16 bytes of a row
-        constexpr int kThreads = 32 * (kDeq + 8);
+        constexpr int kThreads = 32 * kLoad;
         grid_dependency_wait();
         const int n_slots = min(n_it, p.KS), groups = n_slots * 16, first = n_it < p.KS ? ks0 : 0;
         const bool fours = (reinterpret_cast<uintptr_t>(p.x) & 15u) == 0;
@@ -716,83 +756,74 @@ __global__ void __launch_bounds__(q4_threads<R, EG>(), PER_SM) q4_matmul_kernel(
     } else if (warp == kMma) {
         // ---- MMAs
         const uint32_t lead = elect_one();
+        // This warp's instructions are one chain, the longest of a small tile's stage (64 registers' worth of address
+        // arithmetic between 8 MMAs), so its places in the rings are literals: it takes U stages a turn.
+        constexpr int U = NA == ND ? NA : NA * ND / (NA % 2 == 0 && ND % 2 == 0 ? 2 : 1);
         bool ok = true;
-        Slot s, a, d;
+        Slot s;
         const uint64_t desc0 = smem_desc(smem_addr(ring));
         int slot = n_it < p.KS ? 0 : ks0;   // (DIRECT) of x
         if constexpr (DIRECT) ok = role_wait(&bars.x_full, 0u, &abort_flag);
-        for (int it = 0; it < n_it; ++it) {
-            if (ok) ok = role_wait(&bars.full[s.i], s.parity, &abort_flag);
-            if (ok && it >= 2) ok = role_wait(&bars.d_empty[d.i], d.parity ^ 1u, &abort_flag);
-            const uint64_t desc = desc0 + (uint64_t)((DIRECT ? slot : s.i) * (kX >> 4));
-            if (DIRECT && ++slot == p.KS) slot = 0;
-            if (ok) ok = role_wait(&bars.a_full[a.i], a.parity, &abort_flag);
-            if (!ok) break;
-            tc_fence_after();
+        uint32_t odd = 0;
+        for (int it0 = 0; it0 < n_it && ok; it0 += U, odd ^= 1u) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k)   // 16 k: 8 columns of TMEM, 32 bytes of the swizzled rows
-                mma_f16_tmem_if(lead, tmem + d.i * TN, tmem + 2 * TN + a.i * 64 + k * 8,
-                                desc + (k >> 2) * (R * 128 >> 4) + 2 * (k & 3), kIdesc, (uint32_t)(k > 0));
-            mma_commit_if(lead, &bars.empty[s.i]);
-            mma_commit_if(lead, &bars.a_empty[a.i]);
-            mma_commit_if(lead, &bars.d_full[d.i]);
-            s.next(p.stages);
-            a.next(NA);
-            d.next(2);
+            for (int j = 0; j < U; ++j) {
+                if (it0 + j >= n_it) break;
+                const int a = j % NA, d = j % ND;
+                const uint32_t a_parity = (U / NA * odd + j / NA) & 1u, d_parity = (U / ND * odd + j / ND) & 1u;
+                if constexpr (!DIRECT) ok = role_wait(&bars.full[s.i], s.parity, &abort_flag);
+                if (ok && (it0 > 0 || j >= ND)) ok = role_wait(&bars.d_empty[d], d_parity ^ 1u, &abort_flag);
+                if (ok) ok = role_wait(&bars.a_full[a], a_parity, &abort_flag);
+                if (!ok) break;
+                tc_fence_after();
+                const uint64_t desc = desc0 + (uint64_t)((DIRECT ? slot : s.i) * (kX >> 4));
+#pragma unroll
+                for (int k = 0; k < 8; ++k)   // 16 k: 8 columns of TMEM, 32 bytes of the swizzled rows
+                    mma_f16_tmem_if(lead, tmem + d * TN, tmem + ND * TN + a * 64 + k * 8,
+                                    desc + (k >> 2) * (R * 128 >> 4) + 2 * (k & 3), kIdesc, (uint32_t)(k > 0));
+                if constexpr (!DIRECT) mma_commit_if(lead, &bars.empty[s.i]);
+                if constexpr (NA != ND) mma_commit_if(lead, &bars.a_empty[a]);
+                mma_commit_if(lead, &bars.d_full[d]);
+                if constexpr (DIRECT) slot = slot + 1 == p.KS ? 0 : slot + 1;
+                else s.next(p.stages);
+            }
         }
         if (!ok && lane == 0) set_timeout(p.ctl, &abort_flag);
         mma_commit_if(lead, &bars.drain);
         int never = 0;
         role_wait(&bars.drain, 0u, &never);
     } else if (warp >= kDeq) {
-        // ---- weights to fp16: two warpgroups take turns at the stages
+        // ---- weights to fp16: the warpgroups take turns at the stages
         const int group = (warp - kDeq) >> 2, quad = warp & 3, r = quad * 32 + lane;
         const int per = kStageK / p.G;
-        const uint32_t dst = tmem + ((uint32_t)(quad * 32) << 16) + 2 * TN;
+        const uint32_t dst = tmem + ((uint32_t)(quad * 32) << 16) + ND * TN;
         bool ok = true;
         Slot s, a;
-        if (group) {
+        for (int i = 0; i < group; ++i) {
             s.next(p.stages);
             a.next(NA);
         }
-        for (int it = group; it < n_it; it += 2) {
+        for (int it = group; it < n_it; it += kGroups) {
             ok = role_wait(&bars.full[s.i], s.parity, &abort_flag);
             if (!ok) break;
             const char *const w = wring + (size_t)s.i * blk;
-            uint4 q[4];
-            __half sc[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                q[j] = reinterpret_cast<const uint4 *>(w)[j * kRows + r];
-                sc[j] = reinterpret_cast<const __half *>(w + kCodeBytes)[((j * per) >> 2) * kRows + r];
-            }
+            Codes q;
+            q.load(w, per, r);
             __syncwarp();
             if (lane == 0) mbar_arrive(&bars.empty[s.i]);
-            if (it >= NA) ok = role_wait(&bars.a_empty[a.i], a.parity ^ 1u, &abort_flag);
+            if (it >= NA) ok = role_wait(NA == ND ? &bars.d_full[a.i] : &bars.a_empty[a.i], a.parity ^ 1u, &abort_flag);
             if (!ok) break;
             tc_fence_after();
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                uint32_t v[32];
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const Scale t(sc[2 * h + j]);
-                    const uint4 c = q[2 * h + j];
-                    dequant8(c.x, t, v + 16 * j);
-                    dequant8(c.y, t, v + 16 * j + 4);
-                    dequant8(c.z, t, v + 16 * j + 8);
-                    dequant8(c.w, t, v + 16 * j + 12);
-                }
-                tmem_st32(dst + a.i * 64 + h * 32, v);
-            }
+            q.store(dst + a.i * 64);
             tmem_st_wait();
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(&bars.a_full[a.i]);
-            s.next(p.stages);
-            s.next(p.stages);
-            a.next(NA);
-            a.next(NA);
+#pragma unroll
+            for (int i = 0; i < kGroups; ++i) {
+                s.next(p.stages);
+                a.next(NA);
+            }
         }
         if (!ok && lane == 0) set_timeout(p.ctl, &abort_flag);
     } else {
@@ -807,6 +838,15 @@ __global__ void __launch_bounds__(q4_threads<R, EG>(), PER_SM) q4_matmul_kernel(
         const auto token_exp = [&](int token0, int i) {
             if constexpr (!DIRECT) return p.tok_exp[token0 + i];
             else return tops[i] ? ilogbf(__uint_as_float(tops[i])) - 14 : 0;
+        };
+        // A barrier of the warpgroup whose wait is bounded like the others (a warp that has given up is not coming).
+        uint32_t group_parity = 0;
+        const auto group_sync = [&] {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bars.group[e]);
+            const bool all = role_wait(&bars.group[e], group_parity, &abort_flag);
+            group_parity ^= 1u;
+            return all;
         };
         float acc[kPieces][P];
 #pragma unroll
@@ -825,7 +865,7 @@ __global__ void __launch_bounds__(q4_threads<R, EG>(), PER_SM) q4_matmul_kernel(
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(&bars.d_empty[d.i]);
-            d.next(2);
+            d.next(ND);
             const bool tile_end = ++ks == p.KS;
             if (!tile_end && it != n_it - 1) continue;
 
@@ -847,10 +887,6 @@ __global__ void __launch_bounds__(q4_threads<R, EG>(), PER_SM) q4_matmul_kernel(
                     if (i < tokens) sum[i] = times_pow2(sum[i], ce + token_exp(token0, i));
             }
             bool write = true;
-            auto group_barrier = [](int group) {   // (literal numbers: else a CTA reserves all barriers)
-                if (EG == 1 || group == 0) named_barrier(1, 128);
-                else named_barrier(2, 128);
-            };
             if (!p.whole && (u0 > tile * p.KS || !tile_end)) {
                 // the CTAs of the tile leave their sums in the workspace; the last one to come adds them in order
                 const int t0 = tile * p.KS, c0 = unit_cta(p, t0), c1 = unit_cta(p, t0 + p.KS - 1);
@@ -862,13 +898,13 @@ __global__ void __launch_bounds__(q4_threads<R, EG>(), PER_SM) q4_matmul_kernel(
                 for (int i = 0; i < kOut; ++i)
                     if (i < tokens) __stcg(mine + i * kRows, sum[i]);
                 __threadfence();
-                group_barrier(e);
+                if (!(ok = group_sync())) break;
                 if (r == 0) {
                     const int old = atom_add_acq_rel_gpu(p.counters + EG * tile + e, 1);
                     last_flag[e] = old == c1 - c0;
                     if (old == c1 - c0) p.counters[EG * tile + e] = 0;
                 }
-                group_barrier(e);
+                if (!(ok = group_sync())) break;
                 write = last_flag[e] != 0;
                 if (write) {
                     __threadfence();
@@ -923,6 +959,215 @@ __global__ void __launch_bounds__(q4_threads<R, EG>(), PER_SM) q4_matmul_kernel(
     if (warp == kMma) tmem_dealloc(tmem, kCols);
 }
 
+// ------------------------------------------------------------------ the product for many tokens
+// Two row tiles (256 columns of the weights) to a tile of 128 columns of activations, so that these come through the L2
+// half as often: at 128 x 128 they are 41 KB a stage of 512 cycles of MMAs, more than the L2 gives every SM (2048
+// tokens through 4096 x 14336 took 279 us, 179 of them without dequantising, MMAs or sums).  A tile's sums stay in
+// TMEM for all of K: the accumulator cuts 24-bit sums off in each of K / 16 steps, 1e-5 of the result at K 4096, which a
+// bf16 result does not show; fp32 results take the kernel above, which adds the stages up itself.
+constexpr int kWideR = 128, kWideGroups = 4, kWideEpi = 8;
+constexpr int kWideThreads = 32 * (kWideEpi + 4 * kWideGroups + 2);
+constexpr int kWideNA = 4;
+constexpr int kWideStages = 4;
+
+struct WideBars {
+    uint64_t full[kWideStages], empty[kWideStages];
+    uint64_t a_full[kWideNA], a_empty[kWideNA];
+    uint64_t d_full[2], d_empty[2];
+    uint64_t drain;
+};
+
+template <bool F32>
+__global__ void __launch_bounds__(kWideThreads, 1) q4_wide_kernel(const __grid_constant__ Q4Params p)
+{
+    constexpr int R = kWideR, kX = R * 256, kCols = 512;
+    constexpr uint32_t kIdesc = (1u << 4) | ((uint32_t)(R >> 3) << 17) | ((uint32_t)(kRows >> 4) << 24);
+    constexpr int kLoad = kWideEpi + 4 * kWideGroups, kMma = kLoad + 1;
+    extern __shared__ char smem_raw[];
+    __shared__ WideBars bars;
+    __shared__ uint32_t tmem_slot;
+    __shared__ volatile int abort_flag;
+
+    const int warp = uniform_warp(), lane = threadIdx.x & 31;
+    char *const ring = smem_raw + (-smem_addr(smem_raw) & 1023u);
+    const int blk = block_bytes(p.G);
+    char *const wring = ring + (size_t)p.stages * kX;
+    const int tile0 = first_unit(p, blockIdx.x), n_tiles = first_unit(p, blockIdx.x + 1) - tile0;   // pairs of row tiles
+    const int n_it = n_tiles * p.KS, last_rt = (p.N - 1) / kRows;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kWideStages; ++i) {
+            mbar_init(&bars.full[i], 1);
+            mbar_init(&bars.empty[i], 9);   // four warps to each of the two blocks of codes, the MMAs
+        }
+        for (int i = 0; i < kWideNA; ++i) {
+            mbar_init(&bars.a_full[i], 4);
+            mbar_init(&bars.a_empty[i], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&bars.d_full[i], 1);
+            mbar_init(&bars.d_empty[i], kWideEpi);
+        }
+        mbar_init(&bars.drain, 1);
+        abort_flag = 0;
+        mbar_init_fence();
+    }
+    if (warp == kMma) tmem_alloc(&tmem_slot, kCols);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot;
+
+    if (warp == kLoad) {
+        // ---- loads
+        const uint32_t lead = elect_one();
+        grid_dependency_wait();
+        int tile = tile0, ks = 0, issued = 0;
+        const uint8_t *w = nullptr;
+        const char *x = nullptr;
+        int64_t second = 0;   // how far the second row tile's blocks lie behind the first's (0: there is none)
+        Slot s;
+        for (int it = 0; it < n_it; ++it) {
+            if (ks == 0) {
+                const int rt = tile / p.TT * 2;
+                w = p.blk + (int64_t)rt * p.KS * blk;
+                x = p.xs + (int64_t)(tile % p.TT) * p.KS * kX;
+                second = rt < last_rt ? (int64_t)p.KS * blk : 0;
+            }
+            if (it >= p.stages && !role_wait(&bars.empty[s.i], s.parity ^ 1u, &abort_flag)) {
+                if (lane == 0) set_timeout(p.ctl, &abort_flag);
+                break;
+            }
+            mbar_expect_if(lead, &bars.full[s.i], (uint32_t)(2 * blk + kX));
+            bulk_load_shared_if(lead, wring + (size_t)s.i * 2 * blk, w, (uint32_t)blk, &bars.full[s.i]);
+            bulk_load_shared_if(lead, wring + (size_t)(s.i * 2 + 1) * blk, w + second, (uint32_t)blk, &bars.full[s.i]);
+            bulk_load_shared_if(lead, ring + (size_t)s.i * kX, x, (uint32_t)kX, &bars.full[s.i]);
+            w += blk;
+            x += kX;
+            issued = it + 1;
+            s.next(p.stages);
+            if (++ks == p.KS) {
+                ks = 0;
+                ++tile;
+            }
+        }
+        // nothing may arrive after the CTA's end
+        int never = 0;
+        for (int it = max(0, issued - p.stages); it < issued; ++it)
+            role_wait(&bars.full[it % p.stages], (uint32_t)((it / p.stages) & 1), &never);
+    } else if (warp == kMma) {
+        // ---- MMAs: of a stage the first row tile's, then the second's
+        const uint32_t lead = elect_one();
+        bool ok = true;
+        Slot s;
+        int ks = 0;
+        uint32_t d_parity = 1;   // of the tile before
+        const uint64_t desc0 = smem_desc(smem_addr(ring));
+        uint32_t odd = 0;        // of the turn through the four places for weights
+        for (int it0 = 0; it0 < n_it && ok; it0 += 2, odd ^= 1u) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int d = j & 1;
+                if (it0 + (j >> 1) >= n_it) break;
+                if (d == 0) ok = role_wait(&bars.full[s.i], s.parity, &abort_flag);
+                if (ok && ks == 0 && it0 + (j >> 1) > 0) ok = role_wait(&bars.d_empty[d], d_parity, &abort_flag);
+                if (ok) ok = role_wait(&bars.a_full[j], odd, &abort_flag);
+                if (!ok) break;
+                tc_fence_after();
+                const uint64_t desc = desc0 + (uint64_t)(s.i * (kX >> 4));
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    mma_f16_tmem_if(lead, tmem + d * R, tmem + 2 * R + j * 64 + k * 8,
+                                    desc + (k >> 2) * (R * 128 >> 4) + 2 * (k & 3), kIdesc, (uint32_t)(ks > 0 || k > 0));
+                mma_commit_if(lead, &bars.a_empty[j]);
+                if (ks == p.KS - 1) mma_commit_if(lead, &bars.d_full[d]);
+                if (d == 1) {
+                    mma_commit_if(lead, &bars.empty[s.i]);
+                    s.next(p.stages);
+                    if (++ks == p.KS) {
+                        ks = 0;
+                        d_parity ^= 1u;
+                    }
+                }
+            }
+        }
+        if (!ok && lane == 0) set_timeout(p.ctl, &abort_flag);
+        mma_commit_if(lead, &bars.drain);
+        int never = 0;
+        role_wait(&bars.drain, 0u, &never);
+    } else if (warp >= kWideEpi) {
+        // ---- weights to fp16: the warpgroups take turns at the blocks, two to a stage
+        static_assert(kWideGroups == kWideNA, "a warpgroup has one place in TMEM");
+        const int group = (warp - kWideEpi) >> 2, quad = warp & 3, r = quad * 32 + lane;
+        const int per = kStageK / p.G;
+        const uint32_t dst = tmem + ((uint32_t)(quad * 32) << 16) + 2 * R + group * 64;
+        bool ok = true;
+        Slot s;
+        uint32_t used = 0;   // times this place has been
+        if (group >= 2) s.next(p.stages);
+        for (int it = group >> 1; it < n_it; it += 2, ++used) {
+            ok = role_wait(&bars.full[s.i], s.parity, &abort_flag);
+            if (!ok) break;
+            Codes q;
+            q.load(wring + (size_t)(s.i * 2 + (group & 1)) * blk, per, r);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bars.empty[s.i]);
+            if (used > 0) ok = role_wait(&bars.a_empty[group], (used - 1) & 1u, &abort_flag);
+            if (!ok) break;
+            tc_fence_after();
+            q.store(dst);
+            tmem_st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bars.a_full[group]);
+            s.next(p.stages);
+            s.next(p.stages);
+        }
+        if (!ok && lane == 0) set_timeout(p.ctl, &abort_flag);
+    } else {
+        // ---- results: warpgroup e has the columns [64 e, 64 e + 64) (fp32 activations: half of the first and of the second parts)
+        constexpr int kOut = F32 ? 32 : 64;
+        const int e = warp >> 2, quad = warp & 3, r = quad * 32 + lane;
+        bool ok = true;
+        grid_dependency_wait();   // (the tokens' powers of two)
+        for (int t = 0; t < n_tiles && ok; ++t) {
+            const int tile = tile0 + t, token0 = tile % p.TT * p.per_tile + e * kOut;
+            const int tokens = min(kOut, p.B - token0);
+#pragma unroll 1
+            for (int d = 0; d < 2; ++d) {
+                const int n = (tile / p.TT * 2 + d) * kRows + r;
+                const int ce = n < p.N ? p.col_exp[n] : 0;
+                ok = role_wait(&bars.d_full[d], (uint32_t)(t & 1), &abort_flag);
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t src = tmem + ((uint32_t)(quad * 32) << 16) + d * R + e * kOut;
+#pragma unroll 1
+                for (int c = 0; c < kOut; c += 16) {
+                    float v[16], lo[16];
+                    tmem_ld16(src + c, v);
+                    if constexpr (F32) tmem_ld16(src + R / 2 + c, lo);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        if (c + i >= tokens || n >= p.N) continue;
+                        if constexpr (F32) v[i] += lo[i] * (1.f / (1 << kLoShift));
+                        const float y = times_pow2(v[i], ce + p.tok_exp[token0 + c + i]);
+                        static_cast<__nv_bfloat16 *>(p.y)[(int64_t)(token0 + c + i) * p.ld_y + n] = __float2bfloat16_rn(y);
+                    }
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bars.d_empty[d]);
+            }
+        }
+        if (!ok && lane == 0) set_timeout(p.ctl, &abort_flag);
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == kMma) tmem_dealloc(tmem, kCols);
+}
+
 // ------------------------------------------------------------------ host
 // Tokens of a tile: fp32 activations take two columns each.
 int tile_tokens(int B, bool f32)
@@ -967,13 +1212,14 @@ constexpr int kSmemPair = 110 * 1024, kSmemOne = 222 * 1024;   // of a CTA, two 
 constexpr int kDirectRing = 4;   // stages of weights that have to fit beside the activations
 
 // How the stages go to the CTAs.
-void plan_q4(Q4Params &p, int per_sm, int *grid)
+void plan_q4(Q4Params &p, int R, int per_sm, int *grid)
 {
     const int tiles = div_up(p.N, kRows) * p.TT;
     const int most = std::min(kMaxCtas, per_sm * sm_count());
-    // Whole tiles where they fill the CTAs evenly, else any number of stages each.
+    // Whole tiles where that is at most so many stages more for the busiest CTA, else any number of stages each.
+    const int loss = R >= 64 ? 32 : 16;
     const int64_t waves = (tiles + most - 1) / most;
-    p.whole = (int64_t)tiles * 10 >= waves * most * 9;
+    p.whole = waves > 64 || waves * p.KS - (int64_t)tiles * p.KS / most <= loss;
     const int units = p.whole ? tiles : tiles * p.KS;
     *grid = std::min(most, units);
     p.per = units / *grid;
@@ -981,7 +1227,7 @@ void plan_q4(Q4Params &p, int per_sm, int *grid)
     p.slots = std::min<int64_t>(p.KS, (int64_t)(p.per + (p.rem > 0 ? 1 : 0)) * (p.whole ? p.KS : 1));
 }
 
-template <int R, int NA, int EG, int PER_SM, bool F32, bool DIRECT>
+template <int R, int NA, int ND, int EG, int PER_SM, bool F32, bool DIRECT>
 cudaError_t launch_q4(const Q4Params &planned, int grid, cudaStream_t st)
 {
     static std::atomic<int> configured[64];
@@ -990,9 +1236,34 @@ cudaError_t launch_q4(const Q4Params &planned, int grid, cudaStream_t st)
     const int kept = 1024 + (DIRECT ? p.slots * R * 256 : 0);
     p.stages = std::min(kQ4MaxStages, ((PER_SM == 2 ? kSmemPair : kSmemOne) - kept) / stage);
     const size_t smem = (size_t)p.stages * stage + kept;
-    const cudaError_t e = set_smem(q4_matmul_kernel<R, NA, EG, PER_SM, F32, DIRECT>, smem, configured);
+    const cudaError_t e = set_smem(q4_matmul_kernel<R, NA, ND, EG, PER_SM, F32, DIRECT>, smem, configured);
     if (e != cudaSuccess) return e;
-    return launch_pdl_cfg(q4_matmul_kernel<R, NA, EG, PER_SM, F32, DIRECT>, dim3(grid), q4_threads<R, EG>(), smem, st, p);
+    return launch_pdl_cfg(q4_matmul_kernel<R, NA, ND, EG, PER_SM, F32, DIRECT>, dim3(grid), q4_threads<R, EG>(), smem, st, p);
+}
+
+// Whether the kernel for many tokens takes a call: pairs of row tiles that fill the SMs evenly enough.
+bool plan_wide(Q4Params &p, int R, int *grid)
+{
+    const int sms = std::min(kMaxCtas, sm_count());
+    const int64_t pairs = (int64_t)div_up(div_up(p.N, kRows), 2) * p.TT, waves = (pairs + sms - 1) / sms;
+    if (p.y_f32 || R != kWideR || pairs * 4 < waves * sms * 3) return false;
+    *grid = sms;
+    p.per = (int)(pairs / sms);
+    p.rem = (int)(pairs % sms);
+    return true;
+}
+
+template <bool F32>
+cudaError_t launch_wide(const Q4Params &planned, int grid, cudaStream_t st)
+{
+    static std::atomic<int> configured[64];
+    Q4Params p = planned;
+    const int stage = 2 * block_bytes(p.G) + kWideR * 256;
+    p.stages = std::min(kWideStages, (kSmemOne - 1024) / stage);
+    const size_t smem = (size_t)p.stages * stage + 1024;
+    const cudaError_t e = set_smem(q4_wide_kernel<F32>, smem, configured);
+    if (e != cudaSuccess) return e;
+    return launch_pdl_cfg(q4_wide_kernel<F32>, dim3(grid), kWideThreads, smem, st, p);
 }
 
 template <bool F32>
@@ -1014,9 +1285,9 @@ cudaError_t run_q4(const sats_q4 *w, const void *x, int B, void *y, int64_t ld_y
     p.x = x;
     p.K = w->K;
     int grid = 0;
-    plan_q4(p, TN <= 32 ? 2 : 1, &grid);
+    plan_q4(p, TN, TN <= 32 ? 2 : 1, &grid);
     if (TN <= kDirectTokens && 1024 + p.slots * TN * 256 + kDirectRing * block_bytes(p.G) <= kSmemPair)
-        return TN == 8 ? launch_q4<8, 3, 1, 2, F32, true>(p, grid, st) : launch_q4<16, 3, 1, 2, F32, true>(p, grid, st);
+        return TN == 8 ? launch_q4<8, 3, 3, 1, 2, F32, true>(p, grid, st) : launch_q4<16, 3, 3, 1, 2, F32, true>(p, grid, st);
 
     StageParams sp{x, ws + L.xs, reinterpret_cast<int *>(ws + L.tok_exp), B, w->K, p.KS, TN, p.per_tile};
     // a token's pieces go to several CTAs where there are few tokens
@@ -1024,12 +1295,14 @@ cudaError_t run_q4(const sats_q4 *w, const void *x, int B, void *y, int64_t ld_y
     q4_stage_kernel<F32><<<dim3(B, split), kStageThreads, 0, st>>>(sp);
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
+    int wide = 0;
+    if (plan_wide(p, TN, &wide)) return launch_wide<F32>(p, wide, st);
     switch (TN) {
-    case 8: return launch_q4<8, 3, 1, 2, F32, false>(p, grid, st);
-    case 16: return launch_q4<16, 3, 1, 2, F32, false>(p, grid, st);
-    case 32: return launch_q4<32, 3, 1, 2, F32, false>(p, grid, st);
-    case 64: return launch_q4<64, 4, 1, 1, F32, false>(p, grid, st);
-    default: return launch_q4<128, 4, 2, 1, F32, false>(p, grid, st);
+    case 8: return launch_q4<8, 3, 3, 1, 2, F32, false>(p, grid, st);
+    case 16: return launch_q4<16, 3, 3, 1, 2, F32, false>(p, grid, st);
+    case 32: return launch_q4<32, 2, 2, 1, 2, F32, false>(p, grid, st);
+    case 64: return launch_q4<64, 4, 2, 1, 1, F32, false>(p, grid, st);
+    default: return launch_q4<128, 4, 2, 2, 1, F32, false>(p, grid, st);
     }
 }
 

@@ -92,6 +92,25 @@ def test_many_columns(sats, B, N):
     check(y, x, q, s, G)
 
 
+@pytest.mark.parametrize("B,K,N,G,x_dtype", [(1000, 384, 4400, 64, torch.bfloat16), (1000, 200, 4600, 32, torch.bfloat16),
+                                             (513, 520, 4001, 128, torch.float32), (2000, 256, 9000, 64, torch.bfloat16),
+                                             (1025, 4096, 4097, 64, torch.float32)])
+def test_many_tokens(sats, B, K, N, G, x_dtype):
+    """bf16 results whose sums stay in the tensor cores' accumulators for all of K: K / 16 steps, each of which cuts no more than
+    2^-21 of the largest (check() allows 8 of them); against 64 bits on the GPU."""
+    q, s = weights(K, N, G, B + N)
+    x = activations(B, K, x_dtype, B)
+    y, _ = product(sats, q, s, G, x, torch.bfloat16, pad=1)
+    W = torch.from_numpy(q4.values(q, s, G)).cuda()
+    x64 = x.double()
+    ref, A = x64 @ W, x64.abs() @ W.abs()
+    tol = A * (2.0 ** -22 + (K // 16 + 1) * 2.0 ** -21) + ref.abs() * 2.0 ** -8 + 2.0 ** -133
+    err = (y.double() - ref).abs()
+    assert (err <= tol).all(), float((err / tol).max())
+    # and on the whole no further off than rounding to bf16 puts it (half a step uniformly: 2^-9 / sqrt(3) at most)
+    assert float(err.norm() / ref.norm()) <= 2.0 ** -9
+
+
 def test_one_product_each(sats):
     """Single activations: every weight comes out as it is."""
     K, N, G = 264, 200, 32
