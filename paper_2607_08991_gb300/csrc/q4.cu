@@ -303,46 +303,100 @@ struct StageParams {
     int B, K, KS, TN, per_tile;   // per_tile: tokens of a tile
 };
 
+// 8 consecutive activations from k on, 0 from K on; fours: x begins on a 16-byte boundary (K is a multiple of 8).
+template <bool F32>
+__device__ __forceinline__ void load8(const void *x, int64_t token, int k, int K, bool fours, float (&v)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = 0.f;
+    if (k >= K) return;
+    if constexpr (F32) {
+        const float *const at = static_cast<const float *>(x) + token * K + k;
+        if (fours) {
+            const float4 q = *reinterpret_cast<const float4 *>(at), r = *reinterpret_cast<const float4 *>(at + 4);
+            v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w; v[4] = r.x; v[5] = r.y; v[6] = r.z; v[7] = r.w;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = at[i];
+        }
+    } else {
+        const uint16_t *const at = static_cast<const uint16_t *>(x) + token * K + k;
+        if (fours) unpack8(*reinterpret_cast<const uint4 *>(at), v);
+        else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = __uint_as_float((uint32_t)at[i] << 16);
+        }
+    }
+}
+
+// Largest finite magnitude, as its bits.
+__device__ __forceinline__ uint32_t largest8(const float (&v)[8])
+{
+    uint32_t top = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const uint32_t m = __float_as_uint(v[j]) & 0x7fffffffu;
+        if (m < 0x7f800000u) top = max(top, m);
+    }
+    return top;
+}
+
+// The power of two that puts a token's largest magnitude (its bits) at 2^14..2^15, and factors whose product divides by it
+// (2^-e alone can be out of range).
+__device__ __forceinline__ int token_power(uint32_t top) { return top ? ilogbf(__uint_as_float(top)) - 14 : 0; }
+__device__ __forceinline__ float2 power_factors(int e) { return make_float2(scalbnf(1.f, -e / 2), scalbnf(1.f, -e - -e / 2)); }
+
+// One CTA to a token: all of it in registers up to K = 8192, so that it is read once.
 template <bool F32>
 __global__ void __launch_bounds__(kStageThreads) q4_stage_kernel(const StageParams p)
 {
+    constexpr int kHeld = 4;
     grid_launch_dependents();
     __shared__ uint32_t top_s[kStageThreads / 32];
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, pieces = p.KS * 16;
     const int64_t b = blockIdx.x;
-    auto bits = [&](int k) -> uint32_t {
-        if constexpr (F32) return __float_as_uint(static_cast<const float *>(p.x)[b * p.K + k]);
-        else return (uint32_t) static_cast<const uint16_t *>(p.x)[b * p.K + k] << 16;
-    };
+    const bool fours = (reinterpret_cast<uintptr_t>(p.x) & 15u) == 0;
+    grid_dependency_wait();
+    float v[kHeld][8];
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k) load8<F32>(p.x, b, (tid + k * kStageThreads) * 8, p.K, fours, v[k]);
     uint32_t top = 0;
-    for (int k = tid; k < p.K; k += kStageThreads) {
-        const uint32_t m = bits(k) & 0x7fffffffu;
-        if (m < 0x7f800000u) top = max(top, m);
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k) top = max(top, largest8(v[k]));
+    for (int c = tid + kHeld * kStageThreads; c < pieces; c += kStageThreads) {
+        float w[8];
+        load8<F32>(p.x, b, c * 8, p.K, fours, w);
+        top = max(top, largest8(w));
     }
     top = __reduce_max_sync(0xffffffffu, top);
     if ((tid & 31) == 0) top_s[tid >> 5] = top;
     __syncthreads();
+#pragma unroll
     for (int i = 0; i < kStageThreads / 32; ++i) top = max(top, top_s[i]);
-    const int e = top ? ilogbf(__uint_as_float(top)) - 14 : 0;
-    if (tid == 0 && blockIdx.y == 0) p.tok_exp[b] = e;
-    const float f1 = scalbnf(1.f, -e / 2), f2 = scalbnf(1.f, -e - -e / 2);   // 2^-e alone can be out of range
+    const int e = token_power(top);
+    if (tid == 0) p.tok_exp[b] = e;
+    const float2 f = power_factors(e);
 
     const int tile = (int)(b / p.per_tile), row = (int)(b % p.per_tile);
     char *const base = p.xs + (int64_t)tile * p.KS * p.TN * 256;
-    // 8 consecutive k are 16 bytes of a row
-    for (int c = blockIdx.y * kStageThreads + tid; c < p.KS * 16; c += gridDim.y * kStageThreads) {
-        float v[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = 8 * c + i < p.K ? __uint_as_float(bits(8 * c + i)) : 0.f;
+    const auto put = [&](int c, const float (&w)[8]) {   // 8 consecutive k are 16 bytes of a row
         uint32_t hi[4], lo[4];
-        split8<F32>(v, f1, f2, hi, lo);
-        const int ks = c >> 4, half = c >> 3 & 1, piece = c & 7;
-        auto put = [&](int r, const uint32_t (&v)[4]) {
-            char *const at = base + ((int64_t)ks * 2 + half) * p.TN * 128 + r * 128 + ((piece ^ (r & 7)) << 4);
-            *reinterpret_cast<uint4 *>(at) = make_uint4(v[0], v[1], v[2], v[3]);
-        };
-        put(row, hi);
-        if constexpr (F32) put(p.TN / 2 + row, lo);
+        split8<F32>(w, f.x, f.y, hi, lo);
+        char *const half = base + (int64_t)(c >> 3) * p.TN * 128;
+        const int piece = c & 7;
+        *reinterpret_cast<uint4 *>(half + row * 128 + ((piece ^ (row & 7)) << 4)) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+        if constexpr (F32) {
+            const int r = p.TN / 2 + row;
+            *reinterpret_cast<uint4 *>(half + r * 128 + ((piece ^ (r & 7)) << 4)) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+        }
+    };
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k)
+        if (tid + k * kStageThreads < pieces) put(tid + k * kStageThreads, v[k]);
+    for (int c = tid + kHeld * kStageThreads; c < pieces; c += kStageThreads) {
+        float w[8];
+        load8<F32>(p.x, b, c * 8, p.K, fours, w);
+        put(c, w);
     }
 }
 
@@ -616,49 +670,23 @@ __global__ void __launch_bounds__(q4_threads<R, EG>(), PER_SM) q4_matmul_kernel(
             const int b = piece / groups, g = piece - b * groups;
             int ks = first + (g >> 4);
             if (ks >= p.KS) ks -= p.KS;
-            const int k = ks * kStageK + (g & 15) * 8;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = 0.f;
-            if (!there || k >= p.K) return;
-            if constexpr (F32) {
-                const float *const x = static_cast<const float *>(p.x) + (int64_t)b * p.K + k;
-                if (fours) {
-                    const float4 q = *reinterpret_cast<const float4 *>(x), r = *reinterpret_cast<const float4 *>(x + 4);
-                    v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w; v[4] = r.x; v[5] = r.y; v[6] = r.z; v[7] = r.w;
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) v[i] = x[i];
-                }
-            } else {
-                const uint16_t *const x = static_cast<const uint16_t *>(p.x) + (int64_t)b * p.K + k;
-                if (fours) unpack8(*reinterpret_cast<const uint4 *>(x), v);
-                else {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float((uint32_t)x[i] << 16);
-                }
-            }
+            load8<F32>(p.x, b, there ? ks * kStageK + (g & 15) * 8 : p.K, p.K, fours, v);
         };
         // all tokens' pieces at once; the first kHeld of a thread stay in registers between the two steps
         constexpr int kHeld = 2;
         float kept[kHeld][8];
         const int total = p.B * groups;
         const auto largest = [&](int i, const float (&v)[8]) {   // (a multiple of 16 pieces to a token: half a warp has one token)
-            uint32_t top = 0;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const uint32_t m = __float_as_uint(v[j]) & 0x7fffffffu;
-                if (m < 0x7f800000u) top = max(top, m);
-            }
+            uint32_t top = largest8(v);
 #pragma unroll
             for (int o = 8; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
             if ((lane & 15) == 0 && i < total) atomicMax(&tops[i / groups], top);
         };
         const auto put = [&](int i, const float (&v)[8]) {
             const int b = i / groups, g = i - b * groups;
-            const int e = tops[b] ? ilogbf(__uint_as_float(tops[b])) - 14 : 0;
-            const float f1 = scalbnf(1.f, -e / 2), f2 = scalbnf(1.f, -e - -e / 2);   // 2^-e alone can be out of range
+            const float2 f = power_factors(token_power(tops[b]));
             uint32_t hi[4], lo[4];
-            split8<F32>(v, f1, f2, hi, lo);
+            split8<F32>(v, f.x, f.y, hi, lo);
             char *const half = ring + (size_t)(g >> 3) * (R * 128);
             const int piece = g & 7;
             *reinterpret_cast<uint4 *>(half + b * 128 + ((piece ^ (b & 7)) << 4)) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
@@ -837,7 +865,7 @@ __global__ void __launch_bounds__(q4_threads<R, EG>(), PER_SM) q4_matmul_kernel(
         // The power of two that token i's activations were divided by (in this CTA).
         const auto token_exp = [&](int token0, int i) {
             if constexpr (!DIRECT) return p.tok_exp[token0 + i];
-            else return tops[i] ? ilogbf(__uint_as_float(tops[i])) - 14 : 0;
+            else return token_power(tops[i]);
         };
         // A barrier of the warpgroup whose wait is bounded like the others (a warp that has given up is not coming).
         uint32_t group_parity = 0;
@@ -1290,10 +1318,7 @@ cudaError_t run_q4(const sats_q4 *w, const void *x, int B, void *y, int64_t ld_y
         return TN == 8 ? launch_q4<8, 3, 3, 1, 2, F32, true>(p, grid, st) : launch_q4<16, 3, 3, 1, 2, F32, true>(p, grid, st);
 
     StageParams sp{x, ws + L.xs, reinterpret_cast<int *>(ws + L.tok_exp), B, w->K, p.KS, TN, p.per_tile};
-    // a token's pieces go to several CTAs where there are few tokens
-    const int split = B >= 128 ? 1 : std::max(1, std::min(div_up(p.KS * 16, kStageThreads), 128 / B));
-    q4_stage_kernel<F32><<<dim3(B, split), kStageThreads, 0, st>>>(sp);
-    const cudaError_t e = cudaGetLastError();
+    const cudaError_t e = launch_pdl_threads(q4_stage_kernel<F32>, dim3(B), kStageThreads, st, sp);
     if (e != cudaSuccess) return e;
     int wide = 0;
     if (plan_wide(p, TN, &wide)) return launch_wide<F32>(p, wide, st);
