@@ -49,14 +49,16 @@ __host__ __device__ constexpr int block_bytes(int G) { return kCodeBytes + kStag
 __host__ __device__ constexpr int div_up(int a, int b) { return (a + b - 1) / b; }
 
 // ------------------------------------------------------------------ quantising
-// amax over the group, s = bf16(amax / 7), q = w / s rounded half to even.  w / s is either a tie or further than 2^-10
-// from one (a ratio of two numbers of 8 bits), so a product with 1 / s that is first rounded to a multiple of 2^-11
-// decides as the division does.  A group with an infinity or a NaN gets the scale NaN and codes 0.
+// amax over the group, s = bf16(amax / 7), q = w / s rounded half to even.  amax / 7 is further than 2^-12 (relative) from
+// the middle of two bf16 numbers, so a product with 1 / 7 decides as the division does; w / s is either a tie or further
+// than 2^-10 from one (a ratio of two numbers of 8 bits), so a product with 1 / s, off by 2^-20 at most, that is first
+// rounded to a multiple of 2^-11 does.  A group with an infinity or a NaN gets the scale NaN and codes 0.
 //
-// A warp has 128 columns and 32 rows: a thread's 32 x 4 values stay in registers between amax and codes, so W is read
-// once; the warps of a group meet in shared memory for its amax.  The codes of two rows are one multiply-add of the
+// A warp has 128 columns and 16 rows: a thread's 16 x 4 values stay in registers between amax and codes, so W is read
+// once; the warps of a group meet in shared memory for its amax.  (With 32 rows to a warp half as many warps share an SM: a
+// 4096 x 14336 layer 52 us.)  The codes of two rows are one multiply-add of the
 // whole numbers' floating-point bits.
-constexpr int kQuantWarps = 4, kQuantRows = 32, kQuantCols = 128;
+constexpr int kQuantWarps = 8, kQuantRows = 16, kQuantCols = 128;
 
 // Whether rows of `elems` elements from p on can be read or written in vectors of four elements.
 bool in_fours(const void *p, int64_t elems, int elem_bytes)
@@ -64,28 +66,36 @@ bool in_fours(const void *p, int64_t elems, int elem_bytes)
     return reinterpret_cast<uintptr_t>(p) % (4 * elem_bytes) == 0 && elems % 4 == 0;
 }
 
-// Four bytes of each lane, for columns n..n + 3 of a row of bytes that starts anywhere.
-__device__ __forceinline__ void store_row_bytes(uint8_t *row, int n, int N, uint32_t v, int lane)
+// Four bytes of each lane, for columns n..n + 3 of a row of bytes that starts anywhere; inside: all lanes' columns are there.
+__device__ __forceinline__ void store_row_bytes(uint8_t *row, int n, int N, uint32_t v, int lane, bool inside)
 {
-    const int lead = (int)(reinterpret_cast<uintptr_t>(row + n - 4 * lane) & 3u);   // the same in all lanes
-    const uint32_t before = __shfl_up_sync(0xffffffffu, v, 1);
-    if (lead == 0) {
-        if (n + 4 <= N) *reinterpret_cast<uint32_t *>(row + n) = v;
-        else
-            for (int j = 0; n + j < N; ++j) row[n + j] = (uint8_t)(v >> 8 * j);
-        return;
+    // The aligned word that begins `lead` bytes before n: the last bytes of the lane before and the first of this one.
+    // What is left at the warp's ends goes out byte by byte.
+    const int lead = (int)(reinterpret_cast<uintptr_t>(row + n) & 3u);   // the same in all lanes
+    const uint32_t w = __funnelshift_l(__shfl_up_sync(0xffffffffu, v, 1), v, 8 * lead);
+    uint8_t *const at = row + (n - lead);
+    if ((lane > 0 || lead == 0) && (inside || n - lead + 4 <= N)) *reinterpret_cast<uint32_t *>(at) = w;
+    else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if ((lane > 0 || j >= lead) && n - lead + j < N) at[j] = (uint8_t)(w >> 8 * j);
     }
-    // the aligned word that begins `lead` bytes before n: the last bytes of the lane before and the first of this one
-    const uint32_t w = __funnelshift_l(before, v, 8 * lead);
-    if (lane > 0 && n - lead + 4 <= N) *reinterpret_cast<uint32_t *>(row + n - lead) = w;
-    else
-        for (int j = lane > 0 ? -lead : 0; j < 4 - lead && n + j < N; ++j) row[n + j] = (uint8_t)(w >> 8 * (j + lead));
-    if (lane == 31)
-        for (int j = 4 - lead; j < 4 && n + j < N; ++j) row[n + j] = (uint8_t)(v >> 8 * j);
+    if (lane == 31 && lead > 0) {
+#pragma unroll
+        for (int j = 1; j < 4; ++j)
+            if (j >= 4 - lead && n + j < N) row[n + j] = (uint8_t)(v >> 8 * j);
+    }
 }
 
-template <bool FOURS>
-__global__ void __launch_bounds__(32 * kQuantWarps) q4_quantize_kernel(const uint16_t *W, int64_t ld, int K, int N, int G,
+__device__ __forceinline__ float rcp_approx(float x)   // 1 / x to 1 ulp
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+template <bool FOURS, bool OUT4>
+__global__ void __launch_bounds__(32 * kQuantWarps, 3) q4_quantize_kernel(const uint16_t *W, int64_t ld, int K, int N, int G,
                                                                        uint8_t *codes, uint16_t *scales)
 {
     __shared__ uint32_t tops[kQuantWarps][32][4];
@@ -95,19 +105,23 @@ __global__ void __launch_bounds__(32 * kQuantWarps) q4_quantize_kernel(const uin
     for (int k0 = (blockIdx.y * kQuantWarps + warp) * kQuantRows; k0 - warp * kQuantRows < K;
          k0 += gridDim.y * kQuantWarps * kQuantRows) {
         uint32_t w[kQuantRows][2];   // columns n, n + 1 and n + 2, n + 3
+        const uint16_t *from = W + (int64_t)k0 * ld + n;
+        const int rows = K - k0;
+        const bool inside = rows >= kQuantRows && (blockIdx.x + 1) * kQuantCols <= N;   // the warp's whole tile
+        if (FOURS && inside) {
 #pragma unroll
-        for (int i = 0; i < kQuantRows; ++i) {
-            w[i][0] = w[i][1] = 0u;
-            if (k0 + i >= K) continue;
-            const uint16_t *const p = W + (int64_t)(k0 + i) * ld + n;
-            if (FOURS && n + 4 <= N) {
-                const uint2 q = __ldcs(reinterpret_cast<const uint2 *>(p));
+            for (int i = 0; i < kQuantRows; ++i, from += ld) {
+                const uint2 q = __ldcs(reinterpret_cast<const uint2 *>(from));
                 w[i][0] = q.x;
                 w[i][1] = q.y;
-            } else {
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kQuantRows; ++i, from += ld) {
+                w[i][0] = w[i][1] = 0u;
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    if (n + j < N) w[i][j >> 1] |= (uint32_t)p[j] << 16 * (j & 1);
+                    if (i < rows && n + j < N) w[i][j >> 1] |= (uint32_t)from[j] << 16 * (j & 1);
             }
         }
         // magnitudes as whole numbers: they order as the values do, infinities and NaN above
@@ -117,25 +131,27 @@ __global__ void __launch_bounds__(32 * kQuantWarps) q4_quantize_kernel(const uin
 #pragma unroll
             for (int j = 0; j < 2; ++j) m[j] = __vmaxu2(m[j], w[i][j] & 0x7fff7fffu);
         uint32_t top[4] = {m[0] & 0xffffu, m[0] >> 16, m[1] & 0xffffu, m[1] >> 16};
-        if (per > 1) {
-            *reinterpret_cast<uint4 *>(tops[warp][lane]) = make_uint4(top[0], top[1], top[2], top[3]);
-            __syncthreads();
-            for (int o = warp / per * per; o < (warp / per + 1) * per; ++o)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) top[j] = max(top[j], tops[o][lane][j]);
-            __syncthreads();
+        *reinterpret_cast<uint4 *>(tops[warp][lane]) = make_uint4(top[0], top[1], top[2], top[3]);
+        __syncthreads();
+        for (int o = warp / per * per; o < (warp / per + 1) * per; ++o) {
+            const uint4 t = *reinterpret_cast<const uint4 *>(tops[o][lane]);
+            top[0] = max(top[0], t.x);
+            top[1] = max(top[1], t.y);
+            top[2] = max(top[2], t.z);
+            top[3] = max(top[3], t.w);
         }
+        __syncthreads();
         if (k0 >= K) continue;
         float s[4], r[4];
         uint16_t sb[4];
         bool slow = false;   // subnormal scales and groups that are not finite
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            sb[j] = top[j] >= 0x7f80u ? 0x7fc0u : bf16_bits(__fdiv_rn(__uint_as_float(top[j] << 16), 7.f));
+            sb[j] = top[j] >= 0x7f80u ? 0x7fc0u : bf16_bits(__fmul_rn(__uint_as_float(top[j] << 16), 1.f / 7.f));
             s[j] = __uint_as_float((uint32_t)sb[j] << 16);
             const bool fine = s[j] >= 1.17549435e-38f;
             slow = slow || (!fine && top[j] != 0u);
-            r[j] = fine ? __frcp_rn(s[j]) : 0.f;
+            r[j] = fine ? rcp_approx(s[j]) : 0.f;
         }
         if (k0 % G == 0) {
             uint16_t *const p = scales + (int64_t)(k0 / G) * N + n;
@@ -146,12 +162,11 @@ __global__ void __launch_bounds__(32 * kQuantWarps) q4_quantize_kernel(const uin
         const f32x2 r01 = pack2(r[0], r[1]), r23 = pack2(r[2], r[3]);
         const f32x2 grid = pack2(6144.f, 6144.f), no_grid = pack2(-6144.f, -6144.f);   // 1.5 x 2^12: multiples of 2^-11
         const f32x2 whole = pack2(12582920.f, 12582920.f);                             // 1.5 x 2^23 + 8: of 1; bits: q + 8
+        uint8_t *to = codes + (int64_t)(k0 / 2) * N;
         auto rounded = [&](uint32_t v, f32x2 rr) {
             return fadd2(fadd2(ffma2(bf16x2_to_f32x2(v), rr, grid), no_grid), whole);
         };
-#pragma unroll
-        for (int i = 0; i < kQuantRows; i += 2) {
-            if (k0 + i >= K) break;
+        const auto code4 = [&](int i) {   // of rows i and i + 1
             uint32_t b[4];
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
@@ -159,7 +174,17 @@ __global__ void __launch_bounds__(32 * kQuantWarps) q4_quantize_kernel(const uin
                 b[2 * j] = __float_as_uint(odd.x) * 16u + __float_as_uint(even.x);
                 b[2 * j + 1] = __float_as_uint(odd.y) * 16u + __float_as_uint(even.y);
             }
-            uint32_t v = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410) ^ 0x88888888u;
+            return __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410) ^ 0x88888888u;
+        };
+        if (OUT4 && inside && !__any_sync(0xffffffffu, slow)) {
+#pragma unroll
+            for (int i = 0; i < kQuantRows; i += 2, to += N) __stcs(reinterpret_cast<uint32_t *>(to + n), code4(i));
+            continue;
+        }
+#pragma unroll
+        for (int i = 0; i < kQuantRows; i += 2, to += N) {
+            if (i >= rows) break;
+            uint32_t v = code4(i);
             if (slow) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
@@ -175,7 +200,7 @@ __global__ void __launch_bounds__(32 * kQuantWarps) q4_quantize_kernel(const uin
                     v = (v & ~(0xffu << 8 * j)) | c << 8 * j;
                 }
             }
-            store_row_bytes(codes + (int64_t)((k0 + i) / 2) * N, n, N, v, lane);
+            store_row_bytes(to, n, N, v, lane, inside);
         }
     }
 }
@@ -197,30 +222,33 @@ __global__ void __launch_bounds__(256) q4_dequantize_kernel(const uint8_t *codes
     if (n >= N) return;
     const int rows = K / 2;
     for (int i0 = blockIdx.y * kReadRows; i0 < rows; i0 += gridDim.y * kReadRows) {
-        uint32_t c[kReadRows];
-#pragma unroll
-        for (int i = 0; i < kReadRows; ++i) {
-            c[i] = 0u;
-            if (i0 + i >= rows) continue;
-            const uint8_t *const p = codes + (int64_t)(i0 + i) * N + n;
-            c[i] = FOURS ? __ldcs(reinterpret_cast<const uint32_t *>(p)) : __ldcs(p);
-        }
         float s[C];
 #pragma unroll
         for (int j = 0; j < C; ++j) s[j] = __uint_as_float((uint32_t)scales[(int64_t)(2 * i0 / G) * N + n + j] << 16);
+        const uint8_t *from = codes + (int64_t)i0 * N + n;
+        float *to = values + (int64_t)i0 * 2 * N + n;
+        const auto code = [&] {
+            if constexpr (FOURS) return __ldcs(reinterpret_cast<const uint32_t *>(from));
+            else return (uint32_t)__ldcs(from);
+        };
+        const auto put = [&](uint32_t c) {
 #pragma unroll
-        for (int i = 0; i < kReadRows; ++i) {
-            if (i0 + i >= rows) break;
-            float *const p = values + (int64_t)(i0 + i) * 2 * N + n;
-#pragma unroll
-            for (int o = 0; o < 2; ++o) {
+            for (int o = 0; o < 2; ++o, to += N) {
                 float v[C];
 #pragma unroll
-                for (int j = 0; j < C; ++j) v[j] = code_value(c[i] >> (8 * j + 4 * o)) * s[j];
-                if constexpr (FOURS) __stcs(reinterpret_cast<float4 *>(p + (int64_t)o * N), make_float4(v[0], v[1], v[2], v[3]));
-                else __stcs(p + (int64_t)o * N, v[0]);
+                for (int j = 0; j < C; ++j) v[j] = code_value(c >> (8 * j + 4 * o)) * s[j];
+                if constexpr (FOURS) __stcs(reinterpret_cast<float4 *>(to), make_float4(v[0], v[1], v[2], v[3]));
+                else __stcs(to, v[0]);
             }
-        }
+        };
+        if (i0 + kReadRows <= rows) {
+            uint32_t c[kReadRows];
+#pragma unroll
+            for (int i = 0; i < kReadRows; ++i, from += N) c[i] = code();
+#pragma unroll
+            for (int i = 0; i < kReadRows; ++i) put(c[i]);
+        } else
+            for (int i = i0; i < rows; ++i, from += N) put(code());
     }
 }
 
@@ -1365,8 +1393,10 @@ sats_status sats_q4_quantize(const void *W, int64_t ld, int K, int N, int G, uin
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const uint16_t *const w = static_cast<const uint16_t *>(W);
     uint16_t *const sc = static_cast<uint16_t *>(scales);
-    if (in_fours(W, ld, 2)) q4_quantize_kernel<true><<<grid, 32 * kQuantWarps, 0, st>>>(w, ld, K, N, G, codes, sc);
-    else q4_quantize_kernel<false><<<grid, 32 * kQuantWarps, 0, st>>>(w, ld, K, N, G, codes, sc);
+    const bool in4 = in_fours(W, ld, 2), out4 = in_fours(codes, N, 1);
+    const auto kernel = in4 ? (out4 ? q4_quantize_kernel<true, true> : q4_quantize_kernel<true, false>)
+                            : (out4 ? q4_quantize_kernel<false, true> : q4_quantize_kernel<false, false>);
+    kernel<<<grid, 32 * kQuantWarps, 0, st>>>(w, ld, K, N, G, codes, sc);
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? SATS_OK : cuda_fail(e, "quantising kernel launch");
 }
