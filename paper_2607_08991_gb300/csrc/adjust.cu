@@ -9,7 +9,16 @@
 // place only what changes is touched.  Everything that is read is asked for at the start: a CTA's life is one wait for
 // memory and three barriers, and three CTAs to an SM keep the memory busy.
 //
-// (measured: see the end of this comment)
+// Bound by HBM for the gradient of many rows (1024 rows of 128256 bf16 logits 88 us, 5.9 TB/s); by the instructions and waits
+// of a slice where every slice has thousands of ids to look at (256 rows of 151936 bf16 logits with 4096 ids 48 us, 3.3
+// TB/s; 77 rows of 50001 fp32 logits with 30000 ids 44 us); by the chain settings and ids - table - logits for few rows (one
+// row with 2000 ids 3.3 us).  256 threads to a CTA: 512 have half the slice each and the same instructions beside it (59 and
+// 130 us for the first two).
+// Other ways, measured on 256 rows / on the gradient of 1024 (us): every slice reads what it needs when it needs it, and
+// the ids twice 69 / 183; one kernel that moves the rows and one of a CTA a row that changes single logits behind it, ids in a
+// hash table 54 / 107, by bits and their running counts 47 / 115 (each read and written in a sector of 32 bytes); a cluster a
+// row, one CTA of which counts 105 / 131; a cluster whose CTAs count the ids once, through distributed shared memory 99 /
+// 172; slices that go over their tables in place of lists 63 / 105; CTAs that stay, the next slice arriving meanwhile 65 / 125.
 #include <algorithm>
 #include <climits>
 #include <cuda_bf16.h>
@@ -25,7 +34,7 @@ constexpr int kMostEach = 8;           // vectors of a slice per thread
 constexpr int kKeep = 2;               // vectors of ids of a thread that are asked for at the start
 constexpr int kMaxBiases = 1024, kBiasEach = kMaxBiases / kAdjThreads;
 constexpr int kNarrowHist = 1 << 14;   // histories shorter than this fit 16-bit fields
-constexpr size_t kMaxAdjSmem = 160 * 1024;
+constexpr size_t kMaxAdjSmem = 68 * 1024;   // three CTAs to an SM, with the kernel's static part
 
 struct AdjustParams {
     const void *src;         // the logits, or the gradient that comes in
@@ -199,6 +208,7 @@ __global__ void __launch_bounds__(kAdjThreads, GRAD ? 6 : 4) adjust_kernel(const
     constexpr uint32_t kAll = (1u << E) - 1u;
     extern __shared__ __align__(16) char smem[];
     __shared__ uint32_t mask_words[kAdjThreads * kMostEach * E / 32 + 2];
+    __shared__ uint16_t aside[kAdjThreads * 4 * kKeep];   // token of the slice, bit 15: of the prompt
     __shared__ int n_listed, n_bias;
     const int tid = threadIdx.x;
     const int vectors = kAdjThreads * p.each, S = vectors * E;   // of a slice
@@ -275,36 +285,56 @@ __global__ void __launch_bounds__(kAdjThreads, GRAD ? 6 : 4) adjust_kernel(const
         __syncthreads();
 
         // ---- which tokens, how often
-        const uint32_t here = (uint32_t)(e1 - e0);
-        const auto count = [&](int id, int at) {   // (an absent id is below 0)
-            if ((uint32_t)id - (uint32_t)e0 >= here || at >= len) return;
-            const int i = id - base;
-            if (GRAD || at < prompt ? table.set(i, 2u) : table.generated(i)) list[atomicAdd(&n_listed, 1)] = (uint16_t)i;
+        // A thread puts the few of its ids that fall into the slice aside; a warp then enters as many at a time as its lanes
+        // have, instead of at every id the one lane in ten that has one.
+        const uint32_t here = (uint32_t)(e1 - e0), low = (uint32_t)e0;
+        const int skew = e0 - base;
+        uint16_t *const mine = aside + tid;
+        int n_aside = 0;
+        const auto look = [&](int id, bool early) {   // (an absent id is below 0)
+            const uint32_t i = (uint32_t)id - low;
+            if (i < here) {
+                mine[n_aside * kAdjThreads] = (uint16_t)((i + skew) | (early ? 0x8000u : 0u));
+                ++n_aside;
+            }
+        };
+        const auto enter = [&] {
+            for (int k = 0; __any_sync(0xffffffffu, k < n_aside); ++k) {
+                if (k >= n_aside) continue;
+                const uint32_t x = mine[k * kAdjThreads];
+                const int i = (int)(x & 0x7fffu);
+                if (GRAD || (x & 0x8000u) ? table.set(i, 2u) : table.generated(i)) list[atomicAdd(&n_listed, 1)] = (uint16_t)i;
+            }
+            n_aside = 0;
         };
         const bool last_slice = e1 == p.V;   // looks for ids that are no tokens
-        const auto count4 = [&](const int4 &q, int v) {
-            const int at = 4 * v - lead;
-            count(q.x, at);
-            count(q.y, at + 1);
-            count(q.z, at + 2);
-            count(q.w, at + 3);
-            if (last_slice)
-                bad = bad || (q.x >= p.V && at < len) || (q.y >= p.V && at + 1 < len) || (q.z >= p.V && at + 2 < len) ||
-                      (q.w >= p.V && at + 3 < len);
+        const auto look4 = [&](const int4 &q, int at) {
+            look(q.x, at < prompt);
+            look(q.y, at + 1 < prompt);
+            look(q.z, at + 2 < prompt);
+            look(q.w, at + 3 < prompt);
+            if (last_slice) bad = bad || max(max(q.x, q.y), max(q.z, q.w)) >= p.V;
         };
         const int id_vectors = len > 0 ? (int)(((int64_t)len + lead + 3) >> 2) : 0;
-        for (int v0 = tid; v0 < id_vectors; v0 += kKeep * kAdjThreads) {
-            int4 next[kKeep];   // on their way while these are counted
-            const bool more = v0 + kKeep * kAdjThreads < id_vectors;
-            if (more)
+        // the vectors that lie wholly in the history, then (one thread each) what is before and behind them
+        const int whole0 = lead > 0 ? 1 : 0, whole1 = (int)(((int64_t)len + lead) >> 2);
+        const int4 *const vectors4 = reinterpret_cast<const int4 *>(hist - lead);
+        for (int v0 = tid & ~31; v0 < id_vectors; v0 += kKeep * kAdjThreads) {   // (the same turns for a whole warp)
+            const int v1 = v0 + (tid & 31);
+            if (v0 > 0 && v0 >= kKeep * kAdjThreads) {
 #pragma unroll
-                for (int k = 0; k < kKeep; ++k) next[k] = load_ids(hist, lead, v0 + (kKeep + k) * kAdjThreads, len);
+                for (int k = 0; k < kKeep; ++k) {
+                    const int v = v1 + k * kAdjThreads;
+                    ids[k] = v >= whole0 && v < whole1 ? __ldg(vectors4 + v) : make_int4(-1, -1, -1, -1);
+                }
+            }
 #pragma unroll
-            for (int k = 0; k < kKeep; ++k)
-                if (v0 + k * kAdjThreads < id_vectors) count4(ids[k], v0 + k * kAdjThreads);
-            if (more)
-#pragma unroll
-                for (int k = 0; k < kKeep; ++k) ids[k] = next[k];
+            for (int k = 0; k < kKeep; ++k) {
+                const int v = v1 + k * kAdjThreads;
+                if (v >= whole0 && v < whole1) look4(ids[k], 4 * v - lead);
+                else if (v < id_vectors) look4(load_ids(hist, lead, v, len), 4 * v - lead);
+            }
+            enter();
         }
         if constexpr (!GRAD) {
 #pragma unroll
@@ -411,7 +441,7 @@ cudaError_t launch_adjust(AdjustParams p, cudaStream_t st)
     p.each = kMostEach;
     while (p.each > 1 && (int64_t)p.B * ((granules + kAdjThreads * p.each - 1) / (kAdjThreads * p.each)) < 2 * sms) p.each /= 2;
     size_t smem = 0;
-    for (;; p.each /= 2) {
+    for (;; --p.each) {
         const size_t S = (size_t)kAdjThreads * p.each * E;
         p.listed = (int)((std::min<int64_t>(ids, S) + 3) / 4 * 4);
         smem = INPLACE ? 0 : S * (16 / E) + 32;
