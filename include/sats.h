@@ -635,17 +635,22 @@ SATS_API sats_status sats_adjust_logits_grad_f32(const float *logits, int64_t ld
  *
  * sats_q4_create -- packs codes and scales (device) into a handle, which owns its device memory (K N / 2 bytes, the
  *   scales, 4 bytes per column).  Runs on `stream` and synchronises it; the caller may then free both.  Within a
- *   column scales are kept to 8 significant bits from its largest one down to 2^-21 of it, below as multiples of 2^-29 of it.
+ *   column scales are kept to 8 significant bits from its largest one down to 2^-21 of it, below as multiples of 2^-28 of it.
  * sats_q4_destroy frees it (synchronises the device first); sats_q4_shape reads back K, N, G (each may be NULL).
  *
- * sats_q4_matmul -- y = x W for B tokens (up to 2^20): x device bf16 [B][K] (fp32 in the _f32 call), y device [B][N], rows ld_y >= N
- *   elements apart, fp32 if y_f32 is not 0, else bf16.  The tensor cores multiply the weights exactly and the activations
- *   to 11 (bf16) or 22 (fp32) significant bits, absolute 2^-39 (2^-50) of a token's largest; sums are rounded to
- *   fp32 every 128 products.  A token's result does not depend on the order in which the threads run.
- *   ws: device, 256-byte aligned, of sats_q4_workspace_bytes(K, N, B) bytes (0: shape out of range), zero-filled once
- *   before first use (sats_workspace_init), left ready for the next call; calls that share one must not overlap on the
- *   GPU.  A bounded wait that gives up leaves y incomplete, sats_get_error(ws) says SATS_ETIMEOUT, and the workspace has to be
- *   zero-filled again.
+ * sats_q4_matmul -- y = x W for B tokens (up to 2^20): x device bf16 [B][K] (fp32 in the _f32 call), y device [B][N],
+ *   rows ld_y >= N elements apart, fp32 if y_f32 is not 0, else bf16; both need the alignment of their elements only.  The
+ *   tensor cores multiply the weights exactly and the activations to 11 (bf16: all of its 8) or 22 (fp32) significant bits, absolute
+ *   2^-39 (2^-50) of a token's largest.  Sums are rounded to fp32 every 128 products, on the way there cut to about as
+ *   many bits (2^-22 of sum |x| |W|); bf16 results of many tokens (more than 64, fp32 activations 32) may keep their sums in the
+ *   tensor cores for all of K (2^-25 K of it).  Where K is divided among CTAs the parts are fp32 numbers of the result's own
+ *   size: one that passes fp32's range makes the result an infinity.  The same call gives the same bits every time;
+ *   another batch size may give a token's others.
+ *   ws: device, 256-byte aligned, of sats_q4_workspace_bytes(K, N, B) bytes or more (0: shape out of range), zero-filled
+ *   once before first use (sats_workspace_init), left ready for the next call, of any batch and weights that fit; calls
+ *   that share one must not overlap on the GPU.  A bounded wait that gives up leaves y incomplete, sats_get_error(ws)
+ *   says SATS_ETIMEOUT, and the workspace has to be zero-filled again.  As the decode kernel the call's own kernels
+ *   may begin before the kernel before them in the stream has ended, reading the weights only until it has.
  */
 SATS_API sats_status sats_q4_quantize(const void *W, int64_t ld, int K, int N, int G, uint8_t *codes, void *scales,
                                       void *stream);

@@ -41,7 +41,8 @@ constexpr int kMaxK = 65536;
 constexpr int64_t kMaxQ4N = (int64_t)1 << 24;
 constexpr int kMaxCtas = 320;                 // of the product's kernel
 constexpr int kLoShift = 11;                  // the second part of an fp32 activation is kept 2^11 times larger
-constexpr int kMaxSplitTiles = 64 * kMaxCtas; // more tiles are not split (plan_q4)
+constexpr int kMaxSplitWaves = 16;            // tiles of more waves are not split (plan_q4)
+constexpr int kMaxSplitTiles = kMaxSplitWaves * kMaxCtas;
 constexpr int kDirectTokens = 16;             // columns (fp32 activations: two a token) that a CTA may stage itself
 constexpr int kCtlBytes = 256;
 
@@ -1186,6 +1187,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) q4_wide_kernel(const __grid_c
         const int e = warp >> 2, quad = warp & 3, r = quad * 32 + lane;
         bool ok = true;
         grid_dependency_wait();   // (the tokens' powers of two)
+        const bool twos = (reinterpret_cast<uintptr_t>(p.y) & 3u) == 0 && p.ld_y % 2 == 0;
         for (int t = 0; t < n_tiles && ok; ++t) {
             const int tile = tile0 + t, token0 = tile % p.TT * p.per_tile + e * kOut;
             const int tokens = min(kOut, p.B - token0);
@@ -1205,10 +1207,23 @@ __global__ void __launch_bounds__(kWideThreads, 1) q4_wide_kernel(const __grid_c
                     tmem_ld_wait();
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        if (c + i >= tokens || n >= p.N) continue;
                         if constexpr (F32) v[i] += lo[i] * (1.f / (1 << kLoShift));
-                        const float y = times_pow2(v[i], ce + p.tok_exp[token0 + c + i]);
-                        static_cast<__nv_bfloat16 *>(p.y)[(int64_t)(token0 + c + i) * p.ld_y + n] = __float2bfloat16_rn(y);
+                        v[i] = times_pow2(v[i], ce + (c + i < tokens ? p.tok_exp[token0 + c + i] : 0));
+                    }
+                    // two lanes' columns of a token in one store: of each pair of tokens the even lane writes the first, the odd one the second
+#pragma unroll
+                    for (int i = 0; i < 16; i += 2) {
+                        const bool odd = lane & 1;
+                        const float other = __shfl_xor_sync(0xffffffffu, odd ? v[i] : v[i + 1], 1);
+                        const int token = c + i + (odd ? 1 : 0), n0 = n & ~1;
+                        const uint16_t first = bf16_bits(odd ? other : v[i]), second = bf16_bits(odd ? v[i + 1] : other);
+                        if (token >= tokens) continue;
+                        uint16_t *const at = static_cast<uint16_t *>(p.y) + (int64_t)(token0 + token) * p.ld_y + n0;
+                        if (twos && n0 + 1 < p.N) *reinterpret_cast<uint32_t *>(at) = (uint32_t)first | (uint32_t)second << 16;
+                        else {
+                            if (n0 < p.N) at[0] = first;
+                            if (n0 + 1 < p.N) at[1] = second;
+                        }
                     }
                 }
                 tc_fence_before();
@@ -1238,21 +1253,21 @@ struct Q4Layout {
 
 size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
 
-// For fp32 activations, which need the larger workspace.
+// The counters, which are 0 between calls, have the same place in every call's layout: a workspace serves smaller batches
+// and other weights, too.  Room for either type of activations.
 Q4Layout q4_layout(int K, int N, int B)
 {
     Q4Layout L{};
     const int b = std::max(B, 1);
-    size_t xs = 0, partial = 0, tiles = 0;
+    size_t xs = 0, partial = 0;
     for (int f = 0; f < 2; ++f) {
         const int TN = tile_tokens(b, f != 0);
         const size_t tt = (size_t)div_up(b, f ? TN / 2 : TN);
         xs = std::max(xs, tt * div_up(K, kStageK) * TN * 256);
         partial = std::max(partial, (size_t)2 * kMaxCtas * TN * kRows * 4);
-        tiles = std::max(tiles, std::min(tt * div_up(N, kRows), (size_t)kMaxSplitTiles) * 2);
     }
     L.counters = kCtlBytes;
-    L.tok_exp = L.counters + up256(tiles * 4);
+    L.tok_exp = L.counters + up256((size_t)kMaxSplitTiles * 2 * 4);
     L.partial = L.tok_exp + up256((size_t)b * 4);
     L.xs = L.partial + up256(partial);
     L.total = L.xs + xs;
@@ -1275,7 +1290,7 @@ void plan_q4(Q4Params &p, int R, int per_sm, int *grid)
     // Whole tiles where that is at most so many stages more for the busiest CTA, else any number of stages each.
     const int loss = R >= 64 ? 32 : 16;
     const int64_t waves = (tiles + most - 1) / most;
-    p.whole = waves > 64 || waves * p.KS - (int64_t)tiles * p.KS / most <= loss;
+    p.whole = waves > kMaxSplitWaves || waves * p.KS - (int64_t)tiles * p.KS / most <= loss;
     const int units = p.whole ? tiles : tiles * p.KS;
     *grid = std::min(most, units);
     p.per = units / *grid;

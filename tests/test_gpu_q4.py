@@ -225,6 +225,22 @@ def test_unaligned_activations_and_no_tokens(sats):
         sats.q4_matmul(w, x[:0], y[:0], ws)
 
 
+def test_one_workspace_for_all_batches(sats):
+    """A workspace of the largest batch serves smaller ones and other weights in any order."""
+    made = []
+    for K, N, G, seed in ((2048, 700, 64, 20), (512, 5000, 32, 21)):
+        q, s = weights(K, N, G, seed)
+        made.append((q, s, G, sats.Q4(torch.from_numpy(q4.pack(q)).cuda(), to_bf16(s), G)))
+    big = max((sats.Q4Workspace(w[3], 300) for w in made), key=lambda ws: ws.nbytes)
+    for turn, (B, which) in enumerate([(300, 0), (1, 0), (40, 1), (3, 1), (300, 1), (17, 0), (70, 0), (1, 1), (200, 1), (5, 0)] * 2):
+        q, s, G, w = made[which]
+        x = activations(B, w.K, torch.float32 if turn % 3 else torch.bfloat16, turn)
+        y = torch.full((B, w.N), float("nan"), device="cuda")
+        sats.q4_matmul(w, x, y, big)
+        check(y, x, q, s, G)
+    assert sats.get_error(big) == sats.OK
+
+
 def test_workspace_too_small(sats):
     q, s = weights(64, 40, 32, 16)
     w = sats.Q4(torch.from_numpy(q4.pack(q)).cuda(), to_bf16(s), 32)
