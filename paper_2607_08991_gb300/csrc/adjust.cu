@@ -12,8 +12,8 @@
 // Bound by HBM for the gradient of many rows (1024 rows of 128256 bf16 logits 88 us, 5.9 TB/s); by the instructions and waits
 // of a slice where every slice has thousands of ids to look at (256 rows of 151936 bf16 logits with 4096 ids 48 us, 3.3
 // TB/s; 77 rows of 50001 fp32 logits with 30000 ids 44 us); by the chain settings and ids - table - logits for few rows (one
-// row with 2000 ids 3.3 us).  256 threads to a CTA: 512 have half the slice each and the same instructions beside it (59 and
-// 130 us for the first two).
+// row with 2000 ids 3.3 us).  Times of the GPU alone, from graphs.  256 threads to a CTA: 512, with slices of 2 to 4 vectors a
+// thread, took 57 to 70 us for the 256 rows and 105 to 132 for the gradient.
 // Other ways, measured on 256 rows / on the gradient of 1024 (us): every slice reads what it needs when it needs it, and
 // the ids twice 69 / 183; one kernel that moves the rows and one of a CTA a row that changes single logits behind it, ids in a
 // hash table 54 / 107, by bits and their running counts 47 / 115 (each read and written in a sector of 32 bytes); a cluster a
