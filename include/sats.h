@@ -582,13 +582,14 @@ SATS_API sats_status sats_sample_f32(const float *logits, int64_t ld, int B, int
  *                absent entry; of entries with the same index the last one counts.  -inf makes the logit -inf.
  *   mask       : device int32 words of 32 tokens each (bit v mod 32 of word v / 32: v is allowed), row i at i * ld_mask
  *                (ld_mask >= ceil(V / 32)), n_masks rows; or NULL.
+ *                A pointer to int32 or fp32 values, the mask's too, that is not 4-byte aligned: SATS_EINVAL.
  *   mask_row   : device int32 [B], the mask of each row; below 0: none.  NULL: mask b for row b (n_masks >= B).
  *   out        : the logits' type; the logits themselves (same pointer and stride), or between their rows (same
  *                stride), or elsewhere (another overlap: SATS_EINVAL).  In place only what changes is touched: a call
  *                without a mask costs what its histories cost, whatever V is.
  *   dev_status : device int32 [1] or NULL.  Set (SATS_EDEVICE) by a setting outside its range, which is off then; an id
- *                or index >= V, a NaN or +inf bias, which are absent then; a length outside [0, L], which is taken as
- *                the nearer of the two; a mask_row >= n_masks, which is none.
+ *                or index >= V, a NaN or +inf bias, which are absent then; a hist_len outside [0, L], which is taken
+ *                as the nearer of the two (so is n_prompt, without being noted); a mask_row >= n_masks, which is none.
  *   A NaN logit stays NaN unless it becomes -inf.
  *
  * sats_adjust_logits_grad -- its backward pass: dlogits_v = dout_v times 0 where the mask does not allow v (also where

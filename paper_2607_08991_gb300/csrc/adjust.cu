@@ -468,6 +468,10 @@ sats_status check_adjust(const AdjustParams &p, int n_masks, int bytes)
     if (p.mask && (p.ld_mask < (p.V + 31) / 32 || (!p.mask_row && n_masks < p.B))) return SATS_EINVAL;
     if ((p.mask_row && !p.mask) || (p.M > 0 && (!p.bias_idx || !p.bias_val))) return SATS_EINVAL;
     if (!p.hist && p.L > 0) return SATS_EINVAL;
+    const void *const words[] = {p.hist, p.hist_len, p.n_prompt, p.rep, p.pres, p.freq, p.bias_idx, p.bias_val, p.mask, p.mask_row,
+                                 p.status};
+    for (const void *w : words)
+        if (reinterpret_cast<uintptr_t>(w) % 4) return SATS_EINVAL;
     if (bad_overlap(p.src, p.ld_src, p.out, p.ld_out, p.B, p.V, bytes)) return SATS_EINVAL;
     // (the gradient's last step reads the logits after its first one has written)
     if (p.z != p.src && (p.z == p.out || bad_overlap(p.z, p.ld_z, p.out, p.ld_out, p.B, p.V, bytes))) return SATS_EINVAL;

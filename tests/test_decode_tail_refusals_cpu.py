@@ -52,6 +52,19 @@ def test_adjust(sats):
     assert _grad(s, out=0x300000 + 16) == s.EINVAL and _grad(s, out=0x300000, ld_out=65) == s.EINVAL
 
 
+def test_adjust_pointers_of_words(sats):
+    """Ids, settings, biases and masks are read in words and vectors of them: none may begin inside a word."""
+    s = sats
+    for f32 in (False, True):
+        for call in (_adjust, _grad):
+            assert call(s, hist=0x2002, f32=f32) == s.EINVAL and call(s, hist_len=0x3001, f32=f32) == s.EINVAL
+            assert call(s, mask=0x4002, ld_mask=2, n_masks=2, f32=f32) == s.EINVAL
+            assert call(s, mask=0x4000, ld_mask=2, n_masks=2, mask_row=0x5001, f32=f32) == s.EINVAL
+        assert _adjust(s, n_prompt=0x3002, f32=f32) == s.EINVAL
+        assert _adjust(s, M=1, bias=(0x5002, 0x6000), f32=f32) == s.EINVAL
+        assert _adjust(s, M=1, bias=(0x5000, 0x6001), f32=f32) == s.EINVAL
+
+
 def test_q4_shapes(sats):
     L, s = sats.lib(), sats
     out = ctypes.c_void_p()
