@@ -149,6 +149,7 @@ __device__ __forceinline__ void bulk_prefetch_l2(const void *src, uint32_t bytes
 // Barrier among `count` threads (a multiple of 32) on hardware barrier `id`.
 __device__ __forceinline__ void named_barrier(int id, int count)
 {
+    __syncwarp();   // (bar.sync is .aligned)
     asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(count) : "memory");
 }
 

@@ -116,8 +116,12 @@ __device__ __forceinline__ void mma_commit_if(uint32_t lead, uint64_t *bar)
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 
+// The .aligned instructions below want all lanes of the warp at them together, and nothing but a barrier of the warp says
+// that they are: a branch of single lanes before them (an arrival, a store of the rows that are there) need not have come
+// back together by itself.  (The waits follow the loads that they wait for.)
 __device__ __forceinline__ void tmem_alloc(uint32_t *slot, uint32_t ncols)
 {
+    __syncwarp();
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(slot)), "r"(ncols)
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -125,12 +129,14 @@ __device__ __forceinline__ void tmem_alloc(uint32_t *slot, uint32_t ncols)
 
 __device__ __forceinline__ void tmem_dealloc(uint32_t taddr, uint32_t ncols)
 {
+    __syncwarp();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(ncols) : "memory");
 }
 
 // 16 consecutive fp32 columns of this warp's 32 TMEM lanes (one row per thread).
 __device__ __forceinline__ void tmem_ld16(uint32_t taddr, float (&v)[16])
 {
+    __syncwarp();
     uint32_t r[16];
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
@@ -145,6 +151,7 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, float (&v)[16])
 // As tmem_ld16, 8 columns.
 __device__ __forceinline__ void tmem_ld8(uint32_t taddr, float (&v)[8])
 {
+    __syncwarp();
     uint32_t r[8];
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
