@@ -643,10 +643,9 @@ SATS_API sats_status sats_adjust_logits_grad_f32(const float *logits, int64_t ld
  *   rows ld_y >= N elements apart, fp32 if y_f32 is not 0, else bf16; both need the alignment of their elements only.  The
  *   tensor cores multiply the weights exactly and the activations to 11 (bf16: all of its 8) or 22 (fp32) significant bits, absolute
  *   2^-39 (2^-50) of a token's largest.  Sums are rounded to fp32 every 128 products, on the way there cut to about as
- *   many bits (2^-22 of sum |x| |W|); bf16 results of many tokens (more than 64, fp32 activations 32) may keep their sums in the
- *   tensor cores for all of K (2^-25 K of it).  Where K is divided among CTAs the parts are fp32 numbers of the result's own
- *   size: one that passes fp32's range makes the result an infinity.  The same call gives the same bits every time;
- *   another batch size may give a token's others.
+ *   many bits (2^-22 of sum |x| |W|), whatever the number of tokens.  Where K is divided among CTAs the parts are fp32
+ *   numbers of the result's own size: one that passes fp32's range makes the result an infinity.  The same call gives the
+ *   same bits every time; another batch size may divide K otherwise and give a token's others.
  *   ws: device, 256-byte aligned, of sats_q4_workspace_bytes(K, N, B) bytes or more (0: shape out of range), zero-filled
  *   once before first use (sats_workspace_init), left ready for the next call, of any batch and weights that fit; calls
  *   that share one must not overlap on the GPU.  A bounded wait that gives up leaves y incomplete, sats_get_error(ws)

@@ -498,6 +498,16 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32
         : "memory");
 }
 
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16])
+{
+    __syncwarp();
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+        "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
+}
+
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // The 8 codes of a word times the group's scale (t: a 64th of it), as fp16 pairs in the order of k.  At bits 6..9 a field
@@ -1020,13 +1030,33 @@ __global__ void __launch_bounds__(q4_threads<R, EG>(), PER_SM) q4_matmul_kernel(
 // ------------------------------------------------------------------ the product for many tokens
 // Two row tiles (256 columns of the weights) to a tile of 128 columns of activations, so that these come through the L2
 // half as often: at 128 x 128 they are 41 KB a stage of 512 cycles of MMAs, more than the L2 gives every SM (2048
-// tokens through 4096 x 14336 took 279 us, 179 of them without dequantising, MMAs or sums).  A tile's sums stay in
-// TMEM for all of K: the accumulator cuts 24-bit sums off in each of K / 16 steps, 1e-5 of the result at K 4096, which a
-// bf16 result does not show; fp32 results take the kernel above, which adds the stages up itself.
+// tokens through 4096 x 14336 took 279 us, 179 of them without dequantising, MMAs or sums).  Each row tile has an
+// accumulator; while the MMAs of a stage fill one, two warpgroups add the other's 128 products up, in registers like the
+// kernel above: 128 sums a thread, for which they take registers from the other warps.  2048 tokens 199 us, of which
+// writing the results 30 (the sums are not read meanwhile); with sums that stay in the accumulators for all of K 187, but
+// those are cut off K / 16 times.
 constexpr int kWideR = 128, kWideGroups = 4, kWideEpi = 8;
-constexpr int kWideThreads = 32 * (kWideEpi + 4 * kWideGroups + 2);
+constexpr int kWideThreads = 32 * (kWideEpi + 4 * kWideGroups + 4);   // (two warps of the last four: loads, MMAs)
 constexpr int kWideNA = 4;
 constexpr int kWideStages = 4;
+// Registers a thread at the launch, and of the three kinds of warpgroups from then on: what is given up has to cover
+// what is taken, or the taking waits for ever.
+constexpr int kWideRegs = 72, kWideEpiRegs = 152, kWideDeqRegs = 40, kWideRestRegs = 32;
+static_assert(kWideEpiRegs * 32 * kWideEpi + kWideDeqRegs * 128 * kWideGroups + kWideRestRegs * 128 <= kWideRegs * kWideThreads,
+              "registers that there are");
+
+template <int n>
+__device__ __forceinline__ void more_registers()
+{
+    __syncwarp();
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(n));
+}
+template <int n>
+__device__ __forceinline__ void fewer_registers()
+{
+    __syncwarp();
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(n));
+}
 
 struct WideBars {
     uint64_t full[kWideStages], empty[kWideStages];
@@ -1076,85 +1106,84 @@ __global__ void __launch_bounds__(kWideThreads, 1) q4_wide_kernel(const __grid_c
     tc_fence_after();
     const uint32_t tmem = tmem_slot;
 
-    if (warp == kLoad) {
-        // ---- loads
-        const uint32_t lead = elect_one();
-        grid_dependency_wait();
-        int tile = tile0, ks = 0, issued = 0;
-        const uint8_t *w = nullptr;
-        const char *x = nullptr;
-        int64_t second = 0;   // how far the second row tile's blocks lie behind the first's (0: there is none)
-        Slot s;
-        for (int it = 0; it < n_it; ++it) {
-            if (ks == 0) {
-                const int rt = tile / p.TT * 2;
-                w = p.blk + (int64_t)rt * p.KS * blk;
-                x = p.xs + (int64_t)(tile % p.TT) * p.KS * kX;
-                second = rt < last_rt ? (int64_t)p.KS * blk : 0;
+    if (warp >= kLoad) {
+        fewer_registers<kWideRestRegs>();
+        if (warp == kLoad) {
+            // ---- loads
+            const uint32_t lead = elect_one();
+            grid_dependency_wait();
+            int tile = tile0, ks = 0, issued = 0;
+            const uint8_t *w = nullptr;
+            const char *x = nullptr;
+            int64_t second = 0;   // how far the second row tile's blocks lie behind the first's (0: there is none)
+            Slot s;
+            for (int it = 0; it < n_it; ++it) {
+                if (ks == 0) {
+                    const int rt = tile / p.TT * 2;
+                    w = p.blk + (int64_t)rt * p.KS * blk;
+                    x = p.xs + (int64_t)(tile % p.TT) * p.KS * kX;
+                    second = rt < last_rt ? (int64_t)p.KS * blk : 0;
+                }
+                if (it >= p.stages && !role_wait(&bars.empty[s.i], s.parity ^ 1u, &abort_flag)) {
+                    if (lane == 0) set_timeout(p.ctl, &abort_flag);
+                    break;
+                }
+                mbar_expect_if(lead, &bars.full[s.i], (uint32_t)(2 * blk + kX));
+                bulk_load_shared_if(lead, wring + (size_t)s.i * 2 * blk, w, (uint32_t)blk, &bars.full[s.i]);
+                bulk_load_shared_if(lead, wring + (size_t)(s.i * 2 + 1) * blk, w + second, (uint32_t)blk, &bars.full[s.i]);
+                bulk_load_shared_if(lead, ring + (size_t)s.i * kX, x, (uint32_t)kX, &bars.full[s.i]);
+                w += blk;
+                x += kX;
+                issued = it + 1;
+                s.next(p.stages);
+                if (++ks == p.KS) {
+                    ks = 0;
+                    ++tile;
+                }
             }
-            if (it >= p.stages && !role_wait(&bars.empty[s.i], s.parity ^ 1u, &abort_flag)) {
-                if (lane == 0) set_timeout(p.ctl, &abort_flag);
-                break;
-            }
-            mbar_expect_if(lead, &bars.full[s.i], (uint32_t)(2 * blk + kX));
-            bulk_load_shared_if(lead, wring + (size_t)s.i * 2 * blk, w, (uint32_t)blk, &bars.full[s.i]);
-            bulk_load_shared_if(lead, wring + (size_t)(s.i * 2 + 1) * blk, w + second, (uint32_t)blk, &bars.full[s.i]);
-            bulk_load_shared_if(lead, ring + (size_t)s.i * kX, x, (uint32_t)kX, &bars.full[s.i]);
-            w += blk;
-            x += kX;
-            issued = it + 1;
-            s.next(p.stages);
-            if (++ks == p.KS) {
-                ks = 0;
-                ++tile;
-            }
-        }
-        // nothing may arrive after the CTA's end
-        int never = 0;
-        for (int it = max(0, issued - p.stages); it < issued; ++it)
-            role_wait(&bars.full[it % p.stages], (uint32_t)((it / p.stages) & 1), &never);
-    } else if (warp == kMma) {
-        // ---- MMAs: of a stage the first row tile's, then the second's
-        const uint32_t lead = elect_one();
-        bool ok = true;
-        Slot s;
-        int ks = 0;
-        uint32_t d_parity = 1;   // of the tile before
-        const uint64_t desc0 = smem_desc(smem_addr(ring));
-        uint32_t odd = 0;        // of the turn through the four places for weights
-        for (int it0 = 0; it0 < n_it && ok; it0 += 2, odd ^= 1u) {
+            // nothing may arrive after the CTA's end
+            int never = 0;
+            for (int it = max(0, issued - p.stages); it < issued; ++it)
+                role_wait(&bars.full[it % p.stages], (uint32_t)((it / p.stages) & 1), &never);
+        } else if (warp == kMma) {
+            // ---- MMAs: of a stage the first row tile's, then the second's
+            const uint32_t lead = elect_one();
+            bool ok = true;
+            Slot s;
+            const uint64_t desc0 = smem_desc(smem_addr(ring));
+            uint32_t odd = 0;        // of the turn through the four places for weights
+            for (int it0 = 0; it0 < n_it && ok; it0 += 2, odd ^= 1u) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int d = j & 1;
-                if (it0 + (j >> 1) >= n_it) break;
-                if (d == 0) ok = role_wait(&bars.full[s.i], s.parity, &abort_flag);
-                if (ok && ks == 0 && it0 + (j >> 1) > 0) ok = role_wait(&bars.d_empty[d], d_parity, &abort_flag);
-                if (ok) ok = role_wait(&bars.a_full[j], odd, &abort_flag);
-                if (!ok) break;
-                tc_fence_after();
-                const uint64_t desc = desc0 + (uint64_t)(s.i * (kX >> 4));
+                for (int j = 0; j < 4; ++j) {
+                    const int d = j & 1;
+                    const uint32_t before = (uint32_t)(j >> 1) ^ 1u;   // parity of the accumulator's use before
+                    if (it0 + (j >> 1) >= n_it) break;
+                    if (d == 0) ok = role_wait(&bars.full[s.i], s.parity, &abort_flag);
+                    if (ok && it0 + (j >> 1) > 0) ok = role_wait(&bars.d_empty[d], before, &abort_flag);
+                    if (ok) ok = role_wait(&bars.a_full[j], odd, &abort_flag);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint64_t desc = desc0 + (uint64_t)(s.i * (kX >> 4));
 #pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    mma_f16_tmem_if(lead, tmem + d * R, tmem + 2 * R + j * 64 + k * 8,
-                                    desc + (k >> 2) * (R * 128 >> 4) + 2 * (k & 3), kIdesc, (uint32_t)(ks > 0 || k > 0));
-                mma_commit_if(lead, &bars.a_empty[j]);
-                if (ks == p.KS - 1) mma_commit_if(lead, &bars.d_full[d]);
-                if (d == 1) {
-                    mma_commit_if(lead, &bars.empty[s.i]);
-                    s.next(p.stages);
-                    if (++ks == p.KS) {
-                        ks = 0;
-                        d_parity ^= 1u;
+                    for (int k = 0; k < 8; ++k)
+                        mma_f16_tmem_if(lead, tmem + d * R, tmem + 2 * R + j * 64 + k * 8,
+                                        desc + (k >> 2) * (R * 128 >> 4) + 2 * (k & 3), kIdesc, (uint32_t)(k > 0));
+                    mma_commit_if(lead, &bars.a_empty[j]);
+                    mma_commit_if(lead, &bars.d_full[d]);
+                    if (d == 1) {
+                        mma_commit_if(lead, &bars.empty[s.i]);
+                        s.next(p.stages);
                     }
                 }
             }
+            if (!ok && lane == 0) set_timeout(p.ctl, &abort_flag);
+            mma_commit_if(lead, &bars.drain);
+            int never = 0;
+            role_wait(&bars.drain, 0u, &never);
         }
-        if (!ok && lane == 0) set_timeout(p.ctl, &abort_flag);
-        mma_commit_if(lead, &bars.drain);
-        int never = 0;
-        role_wait(&bars.drain, 0u, &never);
     } else if (warp >= kWideEpi) {
         // ---- weights to fp16: the warpgroups take turns at the blocks, two to a stage
+        fewer_registers<kWideDeqRegs>();
         static_assert(kWideGroups == kWideNA, "a warpgroup has one place in TMEM");
         const int group = (warp - kWideEpi) >> 2, quad = warp & 3, r = quad * 32 + lane;
         const int per = kStageK / p.G;
@@ -1166,14 +1195,23 @@ __global__ void __launch_bounds__(kWideThreads, 1) q4_wide_kernel(const __grid_c
         for (int it = group >> 1; it < n_it; it += 2, ++used) {
             ok = role_wait(&bars.full[s.i], s.parity, &abort_flag);
             if (!ok) break;
-            Codes q;
-            q.load(wring + (size_t)(s.i * 2 + (group & 1)) * blk, per, r);
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&bars.empty[s.i]);
             if (used > 0) ok = role_wait(&bars.a_empty[group], (used - 1) & 1u, &abort_flag);
             if (!ok) break;
             tc_fence_after();
-            q.store(dst);
+            const char *const block = wring + (size_t)(s.i * 2 + (group & 1)) * blk;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint4 q = reinterpret_cast<const uint4 *>(block)[j * kRows + r];
+                const Scale t(reinterpret_cast<const __half *>(block + kCodeBytes)[((j * per) >> 2) * kRows + r]);
+                uint32_t v[16];
+                dequant8(q.x, t, v);
+                dequant8(q.y, t, v + 4);
+                dequant8(q.z, t, v + 8);
+                dequant8(q.w, t, v + 12);
+                tmem_st16(dst + j * 16, v);
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bars.empty[s.i]);
             tmem_st_wait();
             tc_fence_before();
             __syncwarp();
@@ -1183,54 +1221,90 @@ __global__ void __launch_bounds__(kWideThreads, 1) q4_wide_kernel(const __grid_c
         }
         if (!ok && lane == 0) set_timeout(p.ctl, &abort_flag);
     } else {
-        // ---- results: warpgroup e has the columns [64 e, 64 e + 64) (fp32 activations: half of the first and of the second parts)
+        // ---- sums and results: warpgroup e has the columns [64 e, 64 e + 64) of both row tiles (fp32 activations: half
+        // of the first and of the second parts)
+        more_registers<kWideEpiRegs>();
         constexpr int kOut = F32 ? 32 : 64;
         const int e = warp >> 2, quad = warp & 3, r = quad * 32 + lane;
-        bool ok = true;
+        const uint32_t src = tmem + ((uint32_t)(quad * 32) << 16) + e * kOut;
         grid_dependency_wait();   // (the tokens' powers of two)
         const bool twos = (reinterpret_cast<uintptr_t>(p.y) & 3u) == 0 && p.ld_y % 2 == 0;
-        for (int t = 0; t < n_tiles && ok; ++t) {
-            const int tile = tile0 + t, token0 = tile % p.TT * p.per_tile + e * kOut;
-            const int tokens = min(kOut, p.B - token0);
-#pragma unroll 1
+        f32x2 acc[2][32];         // columns src + 0.. and (fp32 activations, from the 16th pair on) src + R / 2 + 0..
+#pragma unroll
+        for (int i = 0; i < 32; ++i) acc[0][i] = acc[1][i] = pack2(0.f, 0.f);
+        bool ok = true;
+        int ks = 0, tile = tile0;
+        for (int it = 0; it < n_it && ok; ++it) {
+            const bool tile_end = ks + 1 == p.KS;
+#pragma unroll
             for (int d = 0; d < 2; ++d) {
-                const int n = (tile / p.TT * 2 + d) * kRows + r;
-                const int ce = n < p.N ? p.col_exp[n] : 0;
-                ok = role_wait(&bars.d_full[d], (uint32_t)(t & 1), &abort_flag);
+                if (ok) ok = role_wait(&bars.d_full[d], (uint32_t)(it & 1), &abort_flag);
                 if (!ok) break;
                 tc_fence_after();
-                const uint32_t src = tmem + ((uint32_t)(quad * 32) << 16) + d * R + e * kOut;
-#pragma unroll 1
-                for (int c = 0; c < kOut; c += 16) {
-                    float v[16], lo[16];
-                    tmem_ld16(src + c, v);
-                    if constexpr (F32) tmem_ld16(src + R / 2 + c, lo);
+#pragma unroll
+                for (int c = 0; c < 64; c += 16) {
+                    float v[16];
+                    tmem_ld16(src + d * R + (F32 && c >= 32 ? R / 2 - 32 : 0) + c, v);
                     tmem_ld_wait();
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        if constexpr (F32) v[i] += lo[i] * (1.f / (1 << kLoShift));
-                        v[i] = times_pow2(v[i], ce + (c + i < tokens ? p.tok_exp[token0 + c + i] : 0));
-                    }
-                    // two lanes' columns of a token in one store: of each pair of tokens the even lane writes the first, the odd one the second
-#pragma unroll
-                    for (int i = 0; i < 16; i += 2) {
-                        const bool odd = lane & 1;
-                        const float other = __shfl_xor_sync(0xffffffffu, odd ? v[i] : v[i + 1], 1);
-                        const int token = c + i + (odd ? 1 : 0), n0 = n & ~1;
-                        const uint16_t first = bf16_bits(odd ? other : v[i]), second = bf16_bits(odd ? v[i + 1] : other);
-                        if (token >= tokens) continue;
-                        uint16_t *const at = static_cast<uint16_t *>(p.y) + (int64_t)(token0 + token) * p.ld_y + n0;
-                        if (twos && n0 + 1 < p.N) *reinterpret_cast<uint32_t *>(at) = (uint32_t)first | (uint32_t)second << 16;
-                        else {
-                            if (n0 < p.N) at[0] = first;
-                            if (n0 + 1 < p.N) at[1] = second;
-                        }
+                    for (int i = 0; i < 8; ++i) {
+                        f32x2 &a = acc[d][c / 2 + i];
+                        const f32x2 b = pack2(v[2 * i], v[2 * i + 1]);
+                        a = fadd2(a, b);
                     }
                 }
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&bars.d_empty[d]);
             }
+            if (!ok) break;
+            if (tile_end) {
+                const int token0 = tile % p.TT * p.per_tile + e * kOut, tokens = min(kOut, p.B - token0);
+                // a lane has two tokens' powers of two: loads between the stores would each wait for the L2
+                int te[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    te[i] = i * 32 + lane < tokens ? p.tok_exp[token0 + i * 32 + lane] : 0;
+                const bool near_tokens = __all_sync(0xffffffffu, abs(te[0]) <= 40 && abs(te[1]) <= 40);
+#pragma unroll
+                for (int d = 0; d < 2; ++d) {
+                    const int n = (tile / p.TT * 2 + d) * kRows + r, n0 = n & ~1;
+                    const int ce = n < p.N ? p.col_exp[n] : 0;
+                    // powers of two that are far from fp32's ends in every lane: one factor (the sums are 0 or 2^-60 to 2^60)
+                    const bool near = near_tokens && __all_sync(0xffffffffu, abs(ce) <= 40);
+                    const auto times = [&](float v, int i) {
+                        const int t = __shfl_sync(0xffffffffu, te[i / 32], i % 32);
+                        return near ? v * __int_as_float((ce + 127 + t) << 23) : times_pow2(v, ce + t);
+                    };
+                    uint16_t *at = static_cast<uint16_t *>(p.y) + (int64_t)(token0 + (lane & 1)) * p.ld_y + n0;
+                    const uint32_t pick = lane & 1 ? 0x3276u : 0x5410u;
+                    int left = tokens - (lane & 1);
+#pragma unroll
+                    for (int i = 0; i < kOut; i += 2, at += 2 * p.ld_y, left -= 2) {
+                        float2 v = unpack2(acc[d][i / 2]);
+                        if constexpr (F32) {
+                            const float2 lo = unpack2(acc[d][16 + i / 2]);
+                            v.x += lo.x * (1.f / (1 << kLoShift));
+                            v.y += lo.y * (1.f / (1 << kLoShift));
+                        }
+                        const float v0 = times(v.x, i), v1 = times(v.y, i + 1);
+                        // two lanes' columns of a token in one store: the even lane writes the first token's, the odd one the second's
+                        const __nv_bfloat162 h = __floats2bfloat162_rn(v0, v1);
+                        const uint32_t mine = *reinterpret_cast<const uint32_t *>(&h);
+                        const uint32_t both = __byte_perm(mine, __shfl_xor_sync(0xffffffffu, mine, 1), pick);
+                        if (left <= 0) continue;
+                        if (twos && n0 + 1 < p.N) *reinterpret_cast<uint32_t *>(at) = both;
+                        else {
+                            if (n0 < p.N) at[0] = (uint16_t)both;
+                            if (n0 + 1 < p.N) at[1] = (uint16_t)(both >> 16);
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) acc[d][i] = pack2(0.f, 0.f);
+                }
+                ++tile;
+            }
+            ks = tile_end ? 0 : ks + 1;
         }
         if (!ok && lane == 0) set_timeout(p.ctl, &abort_flag);
     }
@@ -1329,6 +1403,15 @@ template <bool F32>
 cudaError_t launch_wide(const Q4Params &planned, int grid, cudaStream_t st)
 {
     static std::atomic<int> configured[64];
+    // (asked once: a build that gives the threads fewer registers must not begin to exchange them)
+    static std::atomic<int> registers{0};
+    if (registers.load() == 0) {
+        cudaFuncAttributes attr{};
+        const cudaError_t e = cudaFuncGetAttributes(&attr, q4_wide_kernel<F32>);
+        if (e != cudaSuccess) return e;
+        registers.store(attr.numRegs);
+    }
+    if (registers.load() < kWideRegs) return cudaErrorInvalidDeviceFunction;
     Q4Params p = planned;
     const int stage = 2 * block_bytes(p.G) + kWideR * 256;
     p.stages = std::min(kWideStages, (kSmemOne - 1024) / stage);
