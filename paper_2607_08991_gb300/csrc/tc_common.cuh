@@ -348,13 +348,17 @@ int smem_optin()
 }
 
 // Raises the kernel's dynamic shared-memory limit on the current device to at
-// least `bytes`; `configured` is the caller's per-device record for this kernel.
+// least `bytes`; `configured` is the caller's per-device record for this kernel.  The limit is only ever raised, and by one
+// thread at a time: of two that ask for different sizes at once the smaller one must not come last.
 template <typename K>
 cudaError_t set_smem(K kernel, size_t bytes, std::atomic<int> (&configured)[64])
 {
+    static std::mutex one_at_a_time;
     int dev = 0;
     cudaGetDevice(&dev);
     std::atomic<int> &have = configured[dev & 63];
+    if ((int)bytes <= have.load()) return cudaSuccess;
+    const std::lock_guard<std::mutex> lock(one_at_a_time);
     if ((int)bytes <= have.load()) return cudaSuccess;
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
     if (e == cudaSuccess) have.store((int)bytes);
