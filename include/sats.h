@@ -640,7 +640,8 @@ SATS_API sats_status sats_adjust_logits_grad_f32(const float *logits, int64_t ld
  * sats_q4_destroy frees it (synchronises the device first); sats_q4_shape reads back K, N, G (each may be NULL).
  *
  * sats_q4_matmul -- y = x W for B tokens (up to 2^20): x device bf16 [B][K] (fp32 in the _f32 call), y device [B][N],
- *   rows ld_y >= N elements apart, fp32 if y_f32 is not 0, else bf16; both need the alignment of their elements only.  The
+ *   rows ld_y >= N elements apart, fp32 if y_f32 is not 0, else bf16; both need the alignment of their elements only.  x, y
+ *   (its rows) and what the call needs of ws must not overlap (SATS_EINVAL).  The
  *   tensor cores multiply the weights exactly and the activations to 11 (bf16: all of its 8) or 22 (fp32) significant bits, absolute
  *   2^-39 (2^-50) of a token's largest.  Sums are rounded to fp32 every 128 products, on the way there cut to about as
  *   many bits (2^-22 of sum |x| |W|), whatever the number of tokens.  Where K is divided among CTAs the parts are fp32

@@ -1458,6 +1458,16 @@ cudaError_t run_q4(const sats_q4 *w, const void *x, int B, void *y, int64_t ld_y
     }
 }
 
+// Whether `n` bytes from a on and `rows` rows of `row` bytes, `step` apart, from b on have a byte in common.
+bool overlap(const void *a, size_t n, const void *b, size_t rows, size_t row, size_t step)
+{
+    const uintptr_t a0 = reinterpret_cast<uintptr_t>(a), b0 = reinterpret_cast<uintptr_t>(b);
+    if (a0 + n <= b0 || b0 + (rows - 1) * step + row <= a0) return false;
+    if (a0 <= b0) return true;
+    const size_t in = (a0 - b0) % step;   // a begins in, or behind, a row that is there
+    return in < row || ((a0 - b0) / step + 1 < rows && in + n > step);
+}
+
 template <bool F32>
 sats_status q4_matmul(const sats_q4 *w, const void *x, int B, void *y, int64_t ld_y, int y_f32, void *ws, size_t ws_bytes,
                       void *stream)
@@ -1466,9 +1476,14 @@ sats_status q4_matmul(const sats_q4 *w, const void *x, int B, void *y, int64_t l
     if (reinterpret_cast<uintptr_t>(ws) % 256) return SATS_EINVAL;
     if (ld_y < w->N) return SATS_EINVAL;
     if (B > 1 << 20 || ld_y > (int64_t)1 << 40) return SATS_ESHAPE;
-    if (ws_bytes < q4_layout(w->K, w->N, B).total) return SATS_ENOSPACE;
+    const size_t need = q4_layout(w->K, w->N, B).total;
+    if (ws_bytes < need) return SATS_ENOSPACE;
     if (B == 0) return SATS_OK;
     if (!x || !y || reinterpret_cast<uintptr_t>(x) % (F32 ? 4 : 2) || reinterpret_cast<uintptr_t>(y) % (y_f32 ? 4 : 2))
+        return SATS_EINVAL;
+    // (CTAs write results while others still read activations)
+    const size_t x_bytes = (size_t)B * w->K * (F32 ? 4 : 2), y_es = y_f32 ? 4 : 2, row = w->N * y_es, step = ld_y * y_es;
+    if (overlap(x, x_bytes, y, B, row, step) || overlap(ws, need, x, 1, x_bytes, x_bytes) || overlap(ws, need, y, B, row, step))
         return SATS_EINVAL;
     const cudaError_t e = run_q4<F32>(w, x, B, y, ld_y, y_f32 != 0, static_cast<char *>(ws),
                                       static_cast<cudaStream_t>(stream));
