@@ -637,7 +637,8 @@ SATS_API sats_status sats_adjust_logits_grad_f32(const float *logits, int64_t ld
  * sats_q4_create -- packs codes and scales (device) into a handle, which owns its device memory (K N / 2 bytes, the
  *   scales, 4 bytes per column).  Runs on `stream` and synchronises it; the caller may then free both.  Within a
  *   column scales are kept to 8 significant bits from its largest one down to 2^-21 of it, below as multiples of 2^-28 of it.
- * sats_q4_destroy frees it (synchronises the device first); sats_q4_shape reads back K, N, G (each may be NULL).
+ *   It belongs to the device that is current then; products with another current device are refused (SATS_EINVAL).
+ * sats_q4_destroy frees it (synchronises its device first); sats_q4_shape reads back K, N, G (each may be NULL).
  *
  * sats_q4_matmul -- y = x W for B tokens (up to 2^20): x device bf16 [B][K] (fp32 in the _f32 call), y device [B][N],
  *   rows ld_y >= N elements apart, fp32 if y_f32 is not 0, else bf16; both need the alignment of their elements only.  x, y

@@ -1485,8 +1485,11 @@ sats_status q4_matmul(const sats_q4 *w, const void *x, int B, void *y, int64_t l
     const size_t x_bytes = (size_t)B * w->K * (F32 ? 4 : 2), y_es = y_f32 ? 4 : 2, row = w->N * y_es, step = ld_y * y_es;
     if (overlap(x, x_bytes, y, B, row, step) || overlap(ws, need, x, 1, x_bytes, x_bytes) || overlap(ws, need, y, B, row, step))
         return SATS_EINVAL;
-    const cudaError_t e = run_q4<F32>(w, x, B, y, ld_y, y_f32 != 0, static_cast<char *>(ws),
-                                      static_cast<cudaStream_t>(stream));
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return cuda_fail(e, "cudaGetDevice");
+    if (dev != w->device) return SATS_EINVAL;
+    e = run_q4<F32>(w, x, B, y, ld_y, y_f32 != 0, static_cast<char *>(ws), static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? SATS_OK : cuda_fail(e, "4-bit product kernel launch");
 }
 
@@ -1566,8 +1569,13 @@ sats_status sats_q4_create(const uint8_t *codes, const void *scales, int K, int 
 sats_status sats_q4_destroy(sats_q4 *w)
 {
     if (!w) return SATS_EINVAL;
+    // (the device that may still be at work with it, whichever is the current one)
+    int dev = w->device;
+    cudaGetDevice(&dev);
+    if (dev != w->device) cudaSetDevice(w->device);
     cudaDeviceSynchronize();
     const cudaError_t e1 = cudaFree(w->blk), e2 = cudaFree(w->col_exp);
+    if (dev != w->device) cudaSetDevice(dev);
     delete w;
     if (e1 != cudaSuccess) return cuda_fail(e1, "cudaFree");
     return e2 == cudaSuccess ? SATS_OK : cuda_fail(e2, "cudaFree");
