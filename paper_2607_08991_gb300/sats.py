@@ -754,13 +754,14 @@ def q4_matmul(w: Q4, x: torch.Tensor, y: torch.Tensor, ws: Q4Workspace, stream: 
     x_f32 = dtype is torch.float32
     if len(shape) != 2 or shape[1] != w.K or not (x_f32 or dtype is torch.bfloat16 or dtype is torch.int16):
         raise ValueError("x must be bf16 or fp32 [B][K]")
-    if shape[0] != B or N != w.N or dev != w.device or x.get_device() != dev:
-        raise ValueError("x must be [B][K] and y [B][N] on the weights' device")
+    buf = ws.buf
+    if shape[0] != B or N != w.N or dev != w.device or x.get_device() != dev or buf.get_device() != dev:
+        raise ValueError("x must be [B][K] and y [B][N], and they and the workspace on the weights' device")
     if not x.is_contiguous():
         raise ValueError("x must be contiguous")
     L_ = _lib or lib()
     s = (L_.sats_q4_matmul_f32 if x_f32 else L_.sats_q4_matmul)(
-        w.handle, x.data_ptr(), B, yp, ld, 1 if y_f32 else 0, ws.buf.data_ptr(), ws.nbytes, _stream(stream))
+        w.handle, x.data_ptr(), B, yp, ld, 1 if y_f32 else 0, buf.data_ptr(), ws.nbytes, _stream(stream))
     if s:
         _check(s, "sats_q4_matmul")
 

@@ -57,3 +57,34 @@ def test_over_the_workspace(sats):
 def _gpu():
     import torch
     return torch.cuda.is_available()
+
+
+class _Tensor:
+    """What the binding asks of a tensor, on a device of one's choice."""
+
+    def __init__(self, shape, dtype, device):
+        self.shape, self.dtype, self.device = shape, dtype, device
+
+    def get_device(self):
+        return self.device
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return 0x1000
+
+
+def test_workspace_on_another_device(sats, monkeypatch):
+    import torch
+    monkeypatch.setattr(sats, "_rows", lambda t, name: (0x2000, 8, 1, 8, True, 0))
+    monkeypatch.setattr(sats, "_stream", lambda s: None)
+    w, ws = sats.Q4.__new__(sats.Q4), sats.Q4Workspace.__new__(sats.Q4Workspace)
+    w.handle, w.K, w.N, w.device = None, 64, 8, 0
+    ws.nbytes, ws.buf = 1 << 30, _Tensor((1 << 30,), torch.uint8, 1)
+    x = _Tensor((1, 64), torch.float32, 0)
+    with pytest.raises(ValueError):
+        sats.q4_matmul(w, x, None, ws)
+    ws.buf.device = 0
+    with pytest.raises(sats.SatsError):      # (then the library refuses the empty handle)
+        sats.q4_matmul(w, x, None, ws)
