@@ -473,8 +473,10 @@ sats_status check_adjust(const AdjustParams &p, int n_masks, int bytes)
     for (const void *w : words)
         if (reinterpret_cast<uintptr_t>(w) % 4) return SATS_EINVAL;
     if (bad_overlap(p.src, p.ld_src, p.out, p.ld_out, p.B, p.V, bytes)) return SATS_EINVAL;
-    // (the gradient's last step reads the logits after its first one has written)
-    if (p.z != p.src && (p.z == p.out || bad_overlap(p.z, p.ld_z, p.out, p.ld_out, p.B, p.V, bytes))) return SATS_EINVAL;
+    // (a thread reads its logit and then writes its gradient, others theirs meanwhile: over the logits only if they are
+    // what comes in, row for row)
+    const bool alike = p.z == p.src && (p.B == 1 || p.ld_z == p.ld_src);
+    if (!alike && (p.z == p.out || bad_overlap(p.z, p.ld_z, p.out, p.ld_out, p.B, p.V, bytes))) return SATS_EINVAL;
     return SATS_OK;
 }
 
