@@ -577,7 +577,7 @@ SATS_API sats_status sats_sample_f32(const float *logits, int64_t ld, int B, int
  *   hist_len   : device int32 [B], how many ids of its row count (NULL: L).
  *   n_prompt   : device int32 [B] or NULL for 0: the first n_prompt ids are the prompt, the others are generated.
  *   repetition, presence, frequency : r, p, f, device fp32 [B] or NULL for off (1, 0, 0).  r > 0, all finite.
- *                The history of a row whose three are off is not read.
+ *                The history of a row whose three are off is not read, of another one no more than the ids that count.
  *   bias_idx, bias_val : device int32 and fp32 [B][M] (M up to 1024, else SATS_ESHAPE; NULL if 0).  An index below 0 is an
  *                absent entry; of entries with the same index the last one counts.  -inf makes the logit -inf.
  *   mask       : device int32 words of 32 tokens each (bit v mod 32 of word v / 32: v is allowed), row i at i * ld_mask

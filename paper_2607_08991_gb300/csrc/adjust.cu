@@ -6,8 +6,10 @@
 // do not depend on an order); whoever counts a token first puts it on a list.  The listed logits are changed in shared
 // memory, each by one thread, from the logit as it came and in fp32, rounded once; then the slice goes out with the
 // mask's bits applied on the way.  So a row is read and written once, in whole vectors, whatever is changed in it; in
-// place only what changes is touched.  Everything that is read is asked for at the start: a CTA's life is one wait for
-// memory and three barriers, and three CTAs to an SM keep the memory busy.
+// place only what changes is touched.  What is read is asked for at the start, the ids as soon as the row's settings and
+// length say which: a CTA's life is one wait for the row's vectors and three barriers, and three CTAs to an SM keep the
+// memory busy.  (Ids asked for before the settings are there, up to the histories' capacity: 256 rows 1 us less, a gradient of
+// 1024 rows as well; but then histories that do not count are read.)
 //
 // Bound by HBM for the gradient of many rows (1024 rows of 128256 bf16 logits 88 us, 5.9 TB/s); by the instructions and waits
 // of a slice where every slice has thousands of ids to look at (256 rows of 151936 bf16 logits with 4096 ids 48 us, 3.3
@@ -229,7 +231,7 @@ __global__ void __launch_bounds__(kAdjThreads, GRAD ? 6 : 4) adjust_kernel(const
         const int e0 = max(base, 0), e1 = (int)min((int64_t)p.V, (int64_t)base + S);
         if (gs >= ge) continue;
 
-        // ---- what is read, all of it asked for before anything is looked at
+        // ---- what is read, all of it but the ids asked for before anything is looked at
         const int ga = (in.head + e0) / E;                              // byte 0 of the stage
         if constexpr (!INPLACE) {
             const int gb = (int)(((int64_t)in.head + e1 + E - 1) / E);
@@ -242,11 +244,6 @@ __global__ void __launch_bounds__(kAdjThreads, GRAD ? 6 : 4) adjust_kernel(const
                 *reinterpret_cast<uint4 *>(stage + (gb - 1 - ga) * 16) = load_edge_granule<F32>(in.base, in.first(gb - 1), in.V, gb - 1);
             cp_async_commit();
         }
-        const int32_t *const hist = p.hist ? p.hist + row * p.ld_hist : nullptr;
-        const int lead = (int)((reinterpret_cast<uintptr_t>(hist) >> 2) & 3);   // ids between the vector boundary and the first
-        int4 ids[kKeep];
-#pragma unroll
-        for (int k = 0; k < kKeep; ++k) ids[k] = load_ids(hist, lead, tid + k * kAdjThreads, p.hist ? p.L : 0);
         float rep = p.rep ? p.rep[row] : 1.f;
         float pres = !GRAD && p.pres ? p.pres[row] : 0.f;
         float freq = !GRAD && p.freq ? p.freq[row] : 0.f;
@@ -276,6 +273,12 @@ __global__ void __launch_bounds__(kAdjThreads, GRAD ? 6 : 4) adjust_kernel(const
             len = len < 0 ? 0 : p.L;
         }
         if (rep == 1.f && pres == 0.f && freq == 0.f) len = 0;   // nothing would change
+        // ids: of a row that has settings, as many as count, and nothing else of the history
+        const int32_t *const hist = p.hist ? p.hist + row * p.ld_hist : nullptr;
+        const int lead = (int)((reinterpret_cast<uintptr_t>(hist) >> 2) & 3);   // ids between the vector boundary and the first
+        int4 ids[kKeep];
+#pragma unroll
+        for (int k = 0; k < kKeep; ++k) ids[k] = load_ids(hist, lead, tid + k * kAdjThreads, len);
         const int w0 = e0 >> 5;
         if (mask) {
             const int n = ((e1 - 1) >> 5) - w0 + 1;

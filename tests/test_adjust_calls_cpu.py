@@ -14,3 +14,19 @@ def test_gradient_over_logits_of_other_strides(sats, f32):  # noqa: F811
     assert _grad(s, f32=f32, z=at, ld=64, dout=at, ld_dout=128, out=at, ld_out=128) == s.EINVAL
     # elsewhere than dout, but over the logits' second row
     assert _grad(s, f32=f32, z=at, ld=256, dout=at, ld_dout=64, out=at + 250 * es, ld_out=256) == s.EINVAL
+
+
+def test_only_ids_that_count_are_read():
+    """A row without settings need not have a history behind it, nor one with a short history more ids: every read of ids comes
+    after the row's length is known, which is 0 where the settings are off, and is bounded by it."""
+    import os
+    import re
+    from paper_2607_08991_gb300 import build
+    with open(os.path.join(build.CSRC, "adjust.cu")) as f:
+        text = f.read()
+    kernel = text[text.index("adjust_kernel(const __grid_constant__"):text.index("// ------------------------------------------------------------------ host")]
+    known = kernel.index("freq == 0.f) len = 0;")
+    reads = [m.start() for m in re.finditer(r"load_ids\(|vectors4 \+", kernel)]
+    assert len(reads) >= 3 and min(reads) > known
+    assert "p.L" not in kernel[known:]
+    assert re.findall(r"load_ids\(.*?, (\w+)\)", kernel[known:]) == ["len"] * 2
