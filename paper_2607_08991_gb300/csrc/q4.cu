@@ -1373,6 +1373,13 @@ void plan_q4(Q4Params &p, int R, int per_sm, int *grid)
     p.slots = std::min<int64_t>(p.KS, (int64_t)(p.per + (p.rem > 0 ? 1 : 0)) * (p.whole ? p.KS : 1));
 }
 
+// Places of a ring of which `groups` warpgroups take the stages in turns, at most n.  With an odd number of places a warpgroup sees
+// every second use of one, and by the parity it waits for, the use before last passes for its own while the other
+// warpgroup's between is still arriving.  That one has arrived once the MMAs of the stage n before are done; a warpgroup that
+// has finished its own stage before knows this of the stage NA + groups before.  (128 columns had 5 places and 4 of
+// weights: a result of 256 tokens in 250 had a tile with wrong stages.)
+int ring_stages(int n, int NA, int groups) { return n % groups != 0 && n < NA + groups ? n / groups * groups : n; }
+
 template <int R, int NA, int ND, int EG, int PER_SM, bool F32, bool DIRECT>
 cudaError_t launch_q4(const Q4Params &planned, int grid, cudaStream_t st)
 {
@@ -1381,6 +1388,7 @@ cudaError_t launch_q4(const Q4Params &planned, int grid, cudaStream_t st)
     const int stage = block_bytes(p.G) + (DIRECT ? 0 : R * 256);
     const int kept = 1024 + (DIRECT ? p.slots * R * 256 : 0);
     p.stages = std::min(kQ4MaxStages, ((PER_SM == 2 ? kSmemPair : kSmemOne) - kept) / stage);
+    p.stages = ring_stages(p.stages, NA, q4_groups<R>());
     const size_t smem = (size_t)p.stages * stage + kept;
     const cudaError_t e = set_smem(q4_matmul_kernel<R, NA, ND, EG, PER_SM, F32, DIRECT>, smem, configured);
     if (e != cudaSuccess) return e;
