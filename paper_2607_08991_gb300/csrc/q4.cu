@@ -902,6 +902,8 @@ __global__ void __launch_bounds__(q4_threads<R, EG>(), PER_SM) q4_matmul_kernel(
         constexpr int kPieces = F32 && EG > 1 ? 2 : 1, P = C / kPieces;
         const int e = warp >> 2, quad = warp & 3, r = quad * 32 + lane;
         const uint32_t src = tmem + ((uint32_t)(quad * 32) << 16) + e * P;
+        // (the tokens' powers of two come from the preceding kernel: for what is read with plain loads a role waits itself)
+        if constexpr (!DIRECT) grid_dependency_wait();
         // The power of two that token i's activations were divided by (in this CTA).
         const auto token_exp = [&](int token0, int i) {
             if constexpr (!DIRECT) return p.tok_exp[token0 + i];

@@ -129,3 +129,16 @@ def test_the_library_has_the_rule():
     assert "p.stages = ring_stages(p.stages, NA, q4_groups<R>());" in text
     wide = text[text.index("constexpr int kWideStages"):text.index("constexpr int kWideStages") + 40]
     assert "= 4;" in wide                                    # the kernel for many tokens: an even number, always the same
+
+
+def test_what_the_kernel_before_wrote_is_waited_for_where_it_is_read():
+    """The tokens' powers of two, by plain loads of the warps that write results: behind a wait of their own, in both kernels."""
+    import os
+    from paper_2607_08991_gb300 import build
+    with open(os.path.join(build.CSRC, "q4.cu")) as f:
+        text = f.read()
+    reads = [i for i in range(len(text)) if text.startswith("p.tok_exp[", i)][1:]          # (the first: the kernel that writes them)
+    assert len(reads) == 2
+    for i in reads:
+        role = max(text.rindex("// ---- sums", 0, i), text.rindex("__launch_bounds__", 0, i))
+        assert "// ---- sums" in text[role:i] and "grid_dependency_wait();" in text[role:i]
