@@ -679,6 +679,8 @@ def _q4_parts(codes, scales, G):
     K, N = 2 * codes.shape[0], codes.shape[1]
     if G < 1 or tuple(scales.shape) != ((K + G - 1) // G, N):
         raise ValueError("scales must be [ceil(K / G)][N] of the codes' K and N")
+    if codes.dtype not in (torch.uint8, torch.int8) or scales.dtype not in (torch.bfloat16, torch.int16):
+        raise ValueError("codes must be uint8 or int8, scales bf16 (or int16 bit patterns of bf16)")
     return _current(_ptr(codes, "codes", 1), codes), _current(_ptr(scales, "scales", 2), scales), K, N
 
 
@@ -704,8 +706,8 @@ def q4_dequantize(codes: torch.Tensor, scales: torch.Tensor, G: int, values: tor
                   stream: Optional[torch.cuda.Stream] = None):
     """What codes and scales stand for, as fp32 values [K][N] (sats_q4_dequantize)."""
     c, s, K, N = _q4_parts(codes, scales, G)
-    if tuple(values.shape) != (K, N):
-        raise ValueError("values must be [K][N]")
+    if tuple(values.shape) != (K, N) or values.dtype is not torch.float32:
+        raise ValueError("values must be fp32 [K][N]")
     _check(lib().sats_q4_dequantize(c, s, K, N, G, _current(_ptr(values, "values", 4), values), _stream(stream)),
            "sats_q4_dequantize")
 

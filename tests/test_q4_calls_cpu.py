@@ -88,3 +88,18 @@ def test_workspace_on_another_device(sats, monkeypatch):
     ws.buf.device = 0
     with pytest.raises(sats.SatsError):      # (then the library refuses the empty handle)
         sats.q4_matmul(w, x, None, ws)
+
+
+def test_parts_of_other_types(sats, monkeypatch):
+    """fp16 scales have bf16's size, int32 values fp32's: not taken for them."""
+    import torch
+    monkeypatch.setattr(sats, "_ptr", lambda t, name, elem=None: 0x1000)
+    monkeypatch.setattr(sats, "_current", lambda p, t: p)
+    codes, scales = torch.zeros(32, 8, dtype=torch.uint8), torch.zeros(2, 8, dtype=torch.bfloat16)
+    assert sats._q4_parts(codes, scales, 32) == (0x1000, 0x1000, 64, 8)
+    assert sats._q4_parts(codes.to(torch.int8), scales.view(torch.int16), 32) == (0x1000, 0x1000, 64, 8)
+    for c, s in ((codes, scales.half()), (codes.bool(), scales), (codes, scales.view(torch.int16).to(torch.uint16))):
+        with pytest.raises(ValueError):
+            sats._q4_parts(c, s, 32)
+    with pytest.raises(ValueError):
+        sats.q4_dequantize(codes, scales, 32, torch.zeros(64, 8, dtype=torch.int32))
