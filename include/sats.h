@@ -585,8 +585,8 @@ SATS_API sats_status sats_sample_f32(const float *logits, int64_t ld, int B, int
  *                A pointer to int32 or fp32 values, the mask's too, that is not 4-byte aligned: SATS_EINVAL.
  *   mask_row   : device int32 [B], the mask of each row; below 0: none.  NULL: mask b for row b (n_masks >= B).
  *   out        : the logits' type; the logits themselves (same pointer and stride), or between their rows (same
- *                stride), or elsewhere (another overlap: SATS_EINVAL).  In place only what changes is touched: a call
- *                without a mask costs what its histories cost, whatever V is.
+ *                stride), or elsewhere (another overlap: SATS_EINVAL).  In place only the logits that change are
+ *                read and written; a row's ids are looked at once for every 1024 to 16384 of its V logits all the same.
  *   dev_status : device int32 [1] or NULL.  Set (SATS_EDEVICE) by a setting outside its range, which is off then; an id
  *                or index >= V, a NaN or +inf bias, which are absent then; a hist_len outside [0, L], which is taken
  *                as the nearer of the two (so is n_prompt, without being noted); a mask_row >= n_masks, which is none.
@@ -634,20 +634,24 @@ SATS_API sats_status sats_adjust_logits_grad_f32(const float *logits, int64_t ld
  *   infinity gets the scale NaN.
  * sats_q4_dequantize -- what codes and scales stand for: values device fp32 [K][N], exact.
  *
- * sats_q4_create -- packs codes and scales (device) into a handle, which owns its device memory (K N / 2 bytes, the
- *   scales, 4 bytes per column).  Runs on `stream` and synchronises it; the caller may then free both.  Within a
- *   column scales are kept to 8 significant bits from its largest one down to 2^-21 of it, below as multiples of 2^-28 of it.
- *   It belongs to the device that is current then; products with another current device are refused (SATS_EINVAL).
+ * sats_q4_create -- packs codes and scales (device) into a handle, which owns its device memory: with K and N rounded
+ *   up to multiples of 128, K N / 2 bytes, 2 K N / G for the scales and 4 per column. Runs on `stream` and synchronises
+ *   it; the caller may then free both. Within a column scales are kept to 8 significant bits from its largest one down
+ *   to 2^-21 of it, below as multiples of 2^-28 of it. It belongs to the device that is current then; products with
+ *   another current device are refused (SATS_EINVAL).
  * sats_q4_destroy frees it (synchronises its device first); sats_q4_shape reads back K, N, G (each may be NULL).
  *
  * sats_q4_matmul -- y = x W for B tokens (up to 2^20): x device bf16 [B][K] (fp32 in the _f32 call), y device [B][N],
- *   rows ld_y >= N elements apart, fp32 if y_f32 is not 0, else bf16; both need the alignment of their elements only.  x, y
- *   (its rows) and what the call needs of ws must not overlap (SATS_EINVAL).  The
- *   tensor cores multiply the weights exactly and the activations to 11 (bf16: all of its 8) or 22 (fp32) significant bits, absolute
- *   2^-39 (2^-50) of a token's largest.  Sums are rounded to fp32 every 128 products, on the way there cut to about as
- *   many bits (2^-22 of sum |x| |W|), whatever the number of tokens.  Where K is divided among CTAs the parts are fp32
- *   numbers of the result's own size: one that passes fp32's range makes the result an infinity.  The same call gives the
- *   same bits every time; another batch size may divide K otherwise and give a token's others.
+ *   rows ld_y >= N elements apart, fp32 if y_f32 is not 0, else bf16; both need the alignment of their elements only.
+ *   x, y (its rows) and what the call needs of ws must not overlap (SATS_EINVAL). The tensor cores multiply the weights
+ *   exactly and the activations to 11 (bf16: all of its 8) or 22 (fp32) significant bits, absolute 2^-39 (2^-50) of a
+ *   token's largest. Sums are rounded to fp32 every 128 products, whatever the number of tokens; on the way there the
+ *   tensor cores cut them in 8 steps, each to no fewer than 22 bits. So a result is off by at most 2^-18 + (K / 128 +
+ *   2) 2^-24 of its sum |x| |W| (fp32 activations 2^-22 more), before it is rounded to bf16 where that is asked for;
+ *   observed: 2^-19.8 where all terms have one sign, so that the cuts add up; 1e-7 to 4e-7 of the norm. Where K is
+ *   divided among CTAs the parts are fp32 numbers of the result's own size: one that passes fp32's range makes the
+ *   result an infinity. The same call gives the same bits every time; another batch size may divide K otherwise and
+ *   give a token's others.
  *   ws: device, 256-byte aligned, of sats_q4_workspace_bytes(K, N, B) bytes or more (0: shape out of range), zero-filled
  *   once before first use (sats_workspace_init), left ready for the next call, of any batch and weights that fit; calls
  *   that share one must not overlap on the GPU.  A bounded wait that gives up leaves y incomplete, sats_get_error(ws)
