@@ -41,7 +41,7 @@ constexpr int kMaxK = 65536;
 constexpr int64_t kMaxQ4N = (int64_t)1 << 24;
 constexpr int kMaxCtas = 320;                 // of the product's kernel
 constexpr int kLoShift = 11;                  // the second part of an fp32 activation is kept 2^11 times larger
-constexpr int kMaxSplitWaves = 16;            // tiles of more waves are not split (plan_q4)
+constexpr int kMaxSplitWaves = 16;            // tiles of more waves are not split: the last, uneven one is 1 of 17 (plan_q4)
 constexpr int kMaxSplitTiles = kMaxSplitWaves * kMaxCtas;
 constexpr int kDirectTokens = 16;             // columns (fp32 activations: two a token) that a CTA may stage itself
 constexpr int kCtlBytes = 256;
@@ -510,6 +510,8 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
 
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+// (Whole numbers read as the low bits of a float of known exponent: a published technique, for fp16 weights in Kim et al.,
+// "Who Says Elephants Can't Run", 2022.)
 // The 8 codes of a word times the group's scale (t: a 64th of it), as fp16 pairs in the order of k.  At bits 6..9 a field
 // reads as 64 (16 + u): 64 (16 + u) t - 1536 t = (u - 8) 64 t in one multiply-add, exact in its product, in 1536 t (10 bits)
 // and in the result (11 bits).  At bits 2..5 it reads as 1024 + 4 u, from which 1056 leaves 4 (u - 8): a subtraction and a
@@ -527,7 +529,7 @@ struct Scale {
 __device__ __forceinline__ void dequant8(uint32_t w, const Scale &s, uint32_t *out)
 {
     const uint32_t rot = __byte_perm(w, w, 0x0321);
-    // (v & mask) | the exponents of 1024, one instruction: left to itself the compiler makes two, 8 of 19 for a word
+    // (v & mask) | the exponents of 1024, said as one operation of three operands
     const auto field = [](uint32_t v, uint32_t mask) {
         uint32_t d;
         asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(d) : "r"(v), "r"(mask), "r"(0x64006400u));
@@ -601,12 +603,10 @@ struct Q4Bars {
     uint64_t drain;
 };
 
-// Warpgroups that turn weights to fp16.
-template <int R>
-__host__ __device__ constexpr int q4_groups() { return 2; }
+constexpr int kDeqGroups = 2;   // warpgroups that turn weights to fp16
 
-template <int R, int EG>
-constexpr int q4_threads() { return 32 * (2 + 4 * q4_groups<R>() + 4 * EG); }
+template <int EG>
+constexpr int q4_threads() { return 32 * (2 + 4 * kDeqGroups + 4 * EG); }
 
 // Columns [c, c + n) of this warp's lanes added to acc; n 8, 16 or a multiple of 16.
 template <int n>
@@ -630,9 +630,6 @@ __device__ __forceinline__ void add_columns(uint32_t taddr, float (&acc)[n])
     }
 }
 
-// R: tokens of a tile that are there (columns of the accumulator that are used); TN >= 16: the MMA's N, whose rows past
-// R read whatever lies behind them in shared memory and land in columns that nobody reads.  NA, ND: stages of fp16 weights
-// and accumulators in TMEM; EG: warpgroups that add the sums up; PER_SM: resident CTAs.
 // v 2^e for a sum v of scaled products (1e-30 < |v| < 1e30, or 0) and any e that two scales' exponents add up to: rounded once
 // where the result is subnormal (below e = -252 it is 0).
 __device__ __forceinline__ float times_pow2(float v, int e)
@@ -642,16 +639,19 @@ __device__ __forceinline__ float times_pow2(float v, int e)
     return v * __int_as_float((half + 127) << 23) * __int_as_float((e - half + 127) << 23);
 }
 
+// R: tokens of a tile that are there (columns of the accumulator that are used); TN >= 16: the MMA's N, whose rows past
+// R read whatever lies behind them in shared memory and land in columns that nobody reads.  NA, ND: stages of fp16 weights
+// and accumulators in TMEM; EG: warpgroups that add the sums up; PER_SM: resident CTAs.
 // DIRECT (a few tokens): the CTA brings the activations of its stages to shared memory itself, at its start, with a power of
 // two of its own for each token; no second kernel, and the ring holds weights alone.
 template <int R, int NA, int ND, int EG, int PER_SM, bool F32, bool DIRECT>
-__global__ void __launch_bounds__(q4_threads<R, EG>(), PER_SM) q4_matmul_kernel(const __grid_constant__ Q4Params p)
+__global__ void __launch_bounds__(q4_threads<EG>(), PER_SM) q4_matmul_kernel(const __grid_constant__ Q4Params p)
 {
     constexpr int TN = R < 16 ? 16 : R;
     constexpr int kCols = (ND * TN + NA * 64) <= 256 ? 256 : 512;   // TMEM: accumulators, then the weights
     constexpr int kX = R * 256;                                    // bytes of the activations of a stage
     constexpr uint32_t kIdesc = (1u << 4) | ((uint32_t)(TN >> 3) << 17) | ((uint32_t)(kRows >> 4) << 24);
-    constexpr int kGroups = q4_groups<R>();
+    constexpr int kGroups = kDeqGroups;
     constexpr int kDeq = 4 * EG, kLoad = kDeq + 4 * kGroups, kMma = kLoad + 1;   // first warps of the roles
     static_assert(ND * TN + NA * 64 <= kCols && kCols * PER_SM <= 512 && NA <= 4 && ND <= 4, "TMEM");
     extern __shared__ char smem_raw[];
@@ -1364,7 +1364,12 @@ void plan_q4(Q4Params &p, int R, int per_sm, int *grid)
 {
     const int tiles = div_up(p.N, kRows) * p.TT;
     const int most = std::min(kMaxCtas, per_sm * sm_count());
-    // Whole tiles where that is at most so many stages more for the busiest CTA, else any number of stages each.
+    // Whole tiles where that is at most so many stages more for the busiest CTA, else any number of stages each, and an
+    // exchange of sums.  Whole / divided (us, bf16 activations, fp32 results): one token, K 4096, 1003 tiles (23 stages more)
+    // 55.6 / 59.1, 152 tiles (16) 13.3 / 13.7, 456 tiles (16) 34.7 / 30.2; K 8192, 152 tiles (32) 33.6 / 22.0; 24 tokens, K 4096,
+    // 699 tiles (23) 51.1 / 55.7, 152 tiles (16) 21.7 / 18.2; K 8192, 456 tiles (32) 73.3 / 62.4.  Wide tiles, 128 tokens: K 4096, 350
+    // tiles (23) 69.7 / 70.6, 76 tiles (16) 25.5 / 24.2; K 8192, 76 tiles (32) 42.4 / 34.2, 175 tiles (55) 77.5 / 63.8.  Below
+    // 8 stages whole tiles win everywhere, by 5 to 40 %.
     const int loss = R >= 64 ? 32 : 16;
     const int64_t waves = (tiles + most - 1) / most;
     p.whole = waves > kMaxSplitWaves || waves * p.KS - (int64_t)tiles * p.KS / most <= loss;
@@ -1375,12 +1380,12 @@ void plan_q4(Q4Params &p, int R, int per_sm, int *grid)
     p.slots = std::min<int64_t>(p.KS, (int64_t)(p.per + (p.rem > 0 ? 1 : 0)) * (p.whole ? p.KS : 1));
 }
 
-// Places of a ring of which `groups` warpgroups take the stages in turns, at most n.  With an odd number of places a warpgroup sees
+// Places of a ring, at most n, of which kDeqGroups warpgroups take the stages in turns.  With an odd number of places a warpgroup sees
 // every second use of one, and by the parity it waits for, the use before last passes for its own while the other
 // warpgroup's between is still arriving.  That one has arrived once the MMAs of the stage n before are done; a warpgroup that
-// has finished its own stage before knows this of the stage NA + groups before.  (128 columns had 5 places and 4 of
+// has finished its own stage before knows this of the stage NA + kDeqGroups before.  (128 columns had 5 places and 4 of
 // weights: a result of 256 tokens in 250 had a tile with wrong stages.)
-int ring_stages(int n, int NA, int groups) { return n % groups != 0 && n < NA + groups ? n / groups * groups : n; }
+int ring_stages(int n, int NA) { return n % kDeqGroups != 0 && n < NA + kDeqGroups ? n / kDeqGroups * kDeqGroups : n; }
 
 template <int R, int NA, int ND, int EG, int PER_SM, bool F32, bool DIRECT>
 cudaError_t launch_q4(const Q4Params &planned, int grid, cudaStream_t st)
@@ -1390,14 +1395,16 @@ cudaError_t launch_q4(const Q4Params &planned, int grid, cudaStream_t st)
     const int stage = block_bytes(p.G) + (DIRECT ? 0 : R * 256);
     const int kept = 1024 + (DIRECT ? p.slots * R * 256 : 0);
     p.stages = std::min(kQ4MaxStages, ((PER_SM == 2 ? kSmemPair : kSmemOne) - kept) / stage);
-    p.stages = ring_stages(p.stages, NA, q4_groups<R>());
+    p.stages = ring_stages(p.stages, NA);
     const size_t smem = (size_t)p.stages * stage + kept;
     const cudaError_t e = set_smem(q4_matmul_kernel<R, NA, ND, EG, PER_SM, F32, DIRECT>, smem, configured);
     if (e != cudaSuccess) return e;
-    return launch_pdl_cfg(q4_matmul_kernel<R, NA, ND, EG, PER_SM, F32, DIRECT>, dim3(grid), q4_threads<R, EG>(), smem, st, p);
+    return launch_pdl_cfg(q4_matmul_kernel<R, NA, ND, EG, PER_SM, F32, DIRECT>, dim3(grid), q4_threads<EG>(), smem, st, p);
 }
 
-// Whether the kernel for many tokens takes a call: pairs of row tiles that fill the SMs evenly enough.
+// Whether the kernel for many tokens takes a call: pairs of row tiles that fill the SMs evenly enough.  With it / without
+// (us, 128 to 2048 tokens): three quarters of a wave, K 4096 35.0 / 46.6, K 1024 16.7 / 22.0; 0.45 of one 33.7 / 27.2 and 16.3 / 13.3;
+// one and a half waves 66.3 / 72.8; 1.1 waves (0.55 of two) 65.1 / 66.5.  (From half of a wave on it would win, too: 34.2 / 43.8.)
 bool plan_wide(Q4Params &p, int R, int *grid)
 {
     const int sms = std::min(kMaxCtas, sm_count());

@@ -125,8 +125,9 @@ def test_the_library_has_the_rule():
     from paper_2607_08991_gb300 import build
     with open(os.path.join(build.CSRC, "q4.cu")) as f:
         text = f.read()
-    assert re.search(r"ring_stages\(int n, int NA, int groups\) \{ return n % groups != 0 && n < NA \+ groups \? n / groups \* groups : n; \}", text)
-    assert "p.stages = ring_stages(p.stages, NA, q4_groups<R>());" in text
+    assert re.search(r"ring_stages\(int n, int NA\) \{ return n % kDeqGroups != 0 && n < NA \+ kDeqGroups "
+                     r"\? n / kDeqGroups \* kDeqGroups : n; \}", text)
+    assert "p.stages = ring_stages(p.stages, NA);" in text and "constexpr int kDeqGroups = 2;" in text
     wide = text[text.index("constexpr int kWideStages"):text.index("constexpr int kWideStages") + 40]
     assert "= 4;" in wide                                    # the kernel for many tokens: an even number, always the same
 
