@@ -11,10 +11,10 @@
 // memory busy.  (Ids asked for before the settings are there, up to the histories' capacity: 256 rows 1 us less, a gradient of
 // 1024 rows as well; but then histories that do not count are read.)
 //
-// Bound by HBM for the gradient of many rows (1024 rows of 128256 bf16 logits 88 us, 5.9 TB/s); by the instructions and waits
-// of a slice where every slice has thousands of ids to look at (256 rows of 151936 bf16 logits with 4096 ids 48 us, 3.3
-// TB/s; 77 rows of 50001 fp32 logits with 30000 ids 44 us); by the chain settings and ids - table - logits for few rows (one
-// row with 2000 ids 3.3 us).  Times of the GPU alone, from graphs.  256 threads to a CTA: 512, with slices of 2 to 4 vectors a
+// Bound by HBM for the gradient of many rows (1024 rows of 128256 bf16 logits 89.5 us, 5.9 TB/s); by the instructions and waits
+// of a slice where every slice has thousands of ids to look at (256 rows of 151936 bf16 logits with 4096 ids 50 us, 3.1
+// TB/s; 77 rows of 50001 fp32 logits with 30000 ids 43 us); by the chain settings and ids - table - logits for few rows (one
+// row with 2000 ids 3.2 us).  Times of the GPU alone, from graphs.  256 threads to a CTA: 512, with slices of 2 to 4 vectors a
 // thread, took 57 to 70 us for the 256 rows and 105 to 132 for the gradient.
 // Other ways, measured on 256 rows / on the gradient of 1024 (us): every slice reads what it needs when it needs it, and
 // the ids twice 69 / 183; one kernel that moves the rows and one of a CTA a row that changes single logits behind it, ids in a

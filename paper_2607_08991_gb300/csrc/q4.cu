@@ -1034,7 +1034,7 @@ __global__ void __launch_bounds__(q4_threads<EG>(), PER_SM) q4_matmul_kernel(con
 // half as often: at 128 x 128 they are 41 KB a stage of 512 cycles of MMAs, more than the L2 gives every SM (2048
 // tokens through 4096 x 14336 took 279 us, 179 of them without dequantising, MMAs or sums).  Each row tile has an
 // accumulator; while the MMAs of a stage fill one, two warpgroups add the other's 128 products up, in registers like the
-// kernel above: 128 sums a thread, for which they take registers from the other warps.  2048 tokens 199 us, of which
+// kernel above: 128 sums a thread, for which they take registers from the other warps.  2048 tokens 197 us, of which
 // writing the results 30 (the sums are not read meanwhile); with sums that stay in the accumulators for all of K 187, but
 // those are cut off K / 16 times.
 constexpr int kWideR = 128, kWideGroups = 4, kWideEpi = 8;
